@@ -67,6 +67,9 @@ typedef enum {
 
 typedef enum { TFG_F32 = 0, TFG_BF16 = 1 } tfg_dtype;
 typedef enum { TFG_SUM = 0, TFG_MEAN = 1, TFG_MAX = 2 } tfg_reduce;
+/* Activations of tfg_group_norm: y, max(y, 0), y / (1 + exp(-y)),
+ * y (1 + erf(y / sqrt 2)) / 2. */
+typedef enum { TFG_ACT_NONE = 0, TFG_ACT_RELU = 1, TFG_ACT_SILU = 2, TFG_ACT_GELU = 3 } tfg_activation;
 
 /* Library version (major * 10000 + minor * 100 + patch). */
 int tfg_version(void);
@@ -519,6 +522,158 @@ int tfg_batch_graphs(int64_t num_graphs, const int64_t *node_counts, const int64
                      int64_t *out_edge_index, int64_t *batch, int64_t *node_offsets,
                      void *workspace, size_t workspace_bytes, int32_t *status,
                      tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Embedding lookup with scaling, and its gradient.  Nodes whose input is an
+ * id (an atom kind, a user, a word) get their feature row from a table before
+ * the first aggregation; the gradient of the table is the reduction by key of
+ * Fig. 5b with the id as the key.  The paper names no such layer; the calls
+ * follow its functional style (Section 2.1.5).
+ *   out[i, :]        = scale * table[ids[i], :]
+ *   grad_table[v, :] = scale * sum over i with ids[i] == v of grad_out[i, :]
+ *
+ *   ids (device) int64 [num_ids], or int32 for the calls that end in 32.
+ *   padding_id: positions with this id stand for no row: their output row is
+ *        zeros and they pass no gradient.  Any value, also one outside
+ *        [0, num_rows); INT64_MIN if there are none (in an int32 list a value
+ *        that no int32 has matches nothing).
+ *   table (device) [num_rows, num_features] row-major, table_dtype TFG_F32 or
+ *        TFG_BF16; out (device) [num_ids, num_features], out_dtype likewise.
+ *        The product is formed in fp32 and rounded once more for TFG_BF16.
+ *   status (device) int32 [1]: 0, or TFG_ERR_INDEX_RANGE when an id lies
+ *        outside [0, num_rows) and is not padding_id (treated as padding).
+ *
+ * tfg_group_ids orders the positions by id, once per list of ids (the caller
+ *   keeps the result while the ids stay):
+ *   rowptr     (device) int32 [num_rows + 1]: the positions of id v are
+ *              perm[rowptr[v]] .. perm[rowptr[v + 1] - 1], in increasing order.
+ *   sorted_ids (device) int32 [num_ids]: the id of each place of perm;
+ *              num_rows for the positions that stand for no row, which come
+ *              last, from place rowptr[num_rows] on.
+ *   perm       (device) int32 [num_ids].
+ *   workspace  (device) >= tfg_group_ids_workspace_size() bytes, 256-byte
+ *              aligned.
+ * tfg_embedding_backward: grad_out (device) [num_ids, num_features],
+ *   grad_dtype TFG_F32 or TFG_BF16; grad_table (device) fp32 [num_rows,
+ *   num_features], written (zeros in rows that no id names).  Sums in fp32 in
+ *   a fixed order: bitwise reproducible.  workspace (device) >=
+ *   tfg_embedding_backward_workspace_size() bytes, 16-byte aligned.
+ * num_rows, num_ids < 2^31 - 1; num_features <= 8,388,480 (65,535 * 128).  out and
+ * grad_table must not overlap the inputs.  16-byte aligned pointers and
+ * num_features a multiple of 4 (8 between bf16 arrays) select the vector
+ * kernels; the results are the same.
+ * ---------------------------------------------------------------------- */
+int tfg_embedding_lookup(const int64_t *ids, int64_t num_ids, const void *table, int table_dtype,
+                         int64_t num_rows, int64_t num_features, float scale, int64_t padding_id,
+                         void *out, int out_dtype, int32_t *status, tfg_stream_t stream);
+int tfg_embedding_lookup32(const int32_t *ids, int64_t num_ids, const void *table, int table_dtype,
+                           int64_t num_rows, int64_t num_features, float scale,
+                           int64_t padding_id, void *out, int out_dtype, int32_t *status,
+                           tfg_stream_t stream);
+int tfg_group_ids_workspace_size(int64_t num_rows, int64_t num_ids, size_t *bytes);
+int tfg_group_ids(const int64_t *ids, int64_t num_ids, int64_t num_rows, int64_t padding_id,
+                  int32_t *rowptr, int32_t *sorted_ids, int32_t *perm, void *workspace,
+                  size_t workspace_bytes, int32_t *status, tfg_stream_t stream);
+int tfg_group_ids32(const int32_t *ids, int64_t num_ids, int64_t num_rows, int64_t padding_id,
+                    int32_t *rowptr, int32_t *sorted_ids, int32_t *perm, void *workspace,
+                    size_t workspace_bytes, int32_t *status, tfg_stream_t stream);
+int tfg_embedding_backward_workspace_size(int64_t num_features, size_t *bytes);
+int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, const int32_t *perm,
+                           const void *grad_out, int grad_dtype, int64_t num_ids,
+                           int64_t num_rows, int64_t num_features, float scale,
+                           float *grad_table, void *workspace, size_t workspace_bytes,
+                           tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Group norm with an activation over the graphs of a batch, channels last.
+ * Between two aggregations of a batched model (Section 2.1.1 BatchGraph) the
+ * features of each graph are normalised by themselves: the channels fall into
+ * num_groups groups of C = num_features / num_groups, and with M = n_g * C
+ * values in group k of graph g
+ *   m = sum x / M,  v = sum (x - m)^2 / M,  r = (v + eps)^(-1/2)
+ *   y = gamma_c (x - m) r + beta_c,  out = act(y)
+ * num_groups = 1 is a layer norm over a graph, num_groups = num_features
+ * normalises every channel by itself.
+ *
+ *   x (device) [num_nodes, num_features] row-major, TFG_F32 or TFG_BF16.
+ *   node_offsets (device) int64 [num_graphs + 1], non-decreasing, in
+ *        [0, num_nodes], as tfg_batch_graphs writes them: graph g holds rows
+ *        node_offsets[g] .. node_offsets[g + 1] - 1.  Rows before the first
+ *        and from the last offset on (a padded batch) are left as they were
+ *        in out and grad_x and take no part in anything.
+ *   gamma, beta (device) fp32 [num_features], or NULL for 1 and 0.
+ *   eps: finite, > 0.  activation: tfg_activation.
+ *   out (device) [num_nodes, num_features], out_dtype TFG_F32 or TFG_BF16;
+ *        must not overlap x.
+ *   mean, rstd (device) fp32 [num_graphs, num_groups]: m and r, written for
+ *        the backward; both or neither may be NULL.  0 for an empty graph.
+ *   status (device) int32 [1]: 0, or TFG_ERR_INDEX_RANGE when an offset lies
+ *        outside [0, num_nodes] or the offsets decrease.
+ *   workspace (device) >= tfg_group_norm_workspace_size() bytes, 16-byte
+ *        aligned; 0 bytes when any graph fits one CTA, and then it may be NULL.
+ *
+ * tfg_group_norm_backward: with g = dL/dout, h = (x - m) r, d = g act'(y):
+ *   grad_beta_c  = sum over all nodes of d,  grad_gamma_c = sum of d h
+ *   grad_x = r (gamma d - (s1 + h s2) / M),
+ *   s1 = sum of gamma d, s2 = sum of gamma d h over the (graph, group).
+ *   mean, rstd: the forward's.  grad_out and grad_x (device) [num_nodes,
+ *   num_features] of type grad_dtype; grad_x must not overlap the inputs.
+ *   grad_gamma, grad_beta (device) fp32 [num_features], written (0 without
+ *   nodes); both or neither may be NULL.  The derivative of TFG_ACT_RELU at 0 is 0.
+ *   The offsets are the forward's: they are not reported a second time.
+ * At most 1,024 channels per group (TFG_ERR_TOO_LARGE).  Statistics and sums
+ * in fp32 in a fixed order: bitwise reproducible.
+ * ---------------------------------------------------------------------- */
+int tfg_group_norm_workspace_size(int64_t num_nodes, int64_t num_graphs, int64_t num_features,
+                                  int64_t num_groups, size_t *bytes);
+int tfg_group_norm(const void *x, int x_dtype, const int64_t *node_offsets, int64_t num_nodes,
+                   int64_t num_graphs, int64_t num_features, int64_t num_groups,
+                   const float *gamma, const float *beta, float eps, int activation, void *out,
+                   int out_dtype, float *mean, float *rstd, void *workspace,
+                   size_t workspace_bytes, int32_t *status, tfg_stream_t stream);
+int tfg_group_norm_backward_workspace_size(int64_t num_nodes, int64_t num_graphs,
+                                           int64_t num_features, int64_t num_groups,
+                                           size_t *bytes);
+int tfg_group_norm_backward(const void *x, int x_dtype, const int64_t *node_offsets,
+                            int64_t num_nodes, int64_t num_graphs, int64_t num_features,
+                            int64_t num_groups, const float *gamma, const float *beta,
+                            const float *mean, const float *rstd, int activation,
+                            const void *grad_out, int grad_dtype, void *grad_x,
+                            float *grad_gamma, float *grad_beta, void *workspace,
+                            size_t workspace_bytes, tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Global gradient norm over many tensors, and clipping by it: the end of a
+ * training step over the gradients that the backward calls give.
+ *   norm = sqrt(sum over tensors t and their values of t^2)
+ *   outs[i] = tensors[i] * clip_norm / max(norm, clip_norm)
+ *
+ *   tensors, outs: HOST arrays of num_tensors device pointers; sizes, dtypes:
+ *        HOST arrays (values per tensor; TFG_F32 or TFG_BF16, of the output
+ *        too).  They are read before the call returns.  A tensor is
+ *        contiguous, aligned to its element, and may be empty (its pointer
+ *        may then be NULL).
+ *   outs[i] may be tensors[i] (in place); apart from that an output overlaps
+ *        no input and no other output, and in place no tensor is listed twice
+ *        (TFG_ERR_INVALID_ARG).
+ *   clip_norm: finite, > 0.
+ *   norm (device) fp32 [1], written: the norm before clipping, 0 without
+ *        values.  Where it is no finite number (a gradient is not, or the norm
+ *        passes the range of fp32), every output value is NaN.  A norm of at
+ *        most clip_norm leaves every value as it is.
+ *   workspace (device) >= tfg_global_norm_workspace_size() bytes, 16-byte
+ *        aligned.
+ * Squares are summed in fp32 with the additions' errors carried, in fp64
+ * where they leave its range; the joined sum, the root and the quotient are
+ * fp64.  Fixed order: bitwise reproducible.
+ * ---------------------------------------------------------------------- */
+int tfg_global_norm_workspace_size(int64_t num_tensors, size_t *bytes);
+int tfg_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes,
+                    const int *dtypes, float *norm, void *workspace, size_t workspace_bytes,
+                    tfg_stream_t stream);
+int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes,
+                            const int *dtypes, float clip_norm, void *const *outs, float *norm,
+                            void *workspace, size_t workspace_bytes, tfg_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Gather-only floor (a measurement call; the paper has no counterpart).

@@ -1,8 +1,12 @@
 // C ABI of libtfg: host-side argument checks, then the launchers.
 // Every entry point validates before it touches the GPU, so a rejected call
 // enqueues nothing.  See include/tfg.h for the contract of each call.
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <memory>
+#include <new>
 
 #include "common.cuh"
 
@@ -172,12 +176,34 @@ int debug_csr(const char *fn, const char *which, const int32_t *rowptr, const in
 }
 #define TFG_DEBUG(expr) TFG_TRY(expr)
 
-size_t elem_bytes(int dtype) { return dtype == TFG_BF16 ? 2 : 4; }
 #else
 #define TFG_DEBUG(expr) \
     do {                \
     } while (0)
 #endif
+
+size_t elem_bytes(int dtype) { return dtype == TFG_BF16 ? 2 : 4; }
+
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+int check_workspace(const char *fn, const void *ws, size_t given, size_t need, size_t align) {
+    if (need == 0) return TFG_OK;
+    if (ws == nullptr || given < need)
+        return fail(TFG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? given : size_t(0));
+    if (reinterpret_cast<uintptr_t>(ws) % align != 0)
+        return fail(TFG_ERR_INVALID_ARG, "%s: workspace must be %zu-byte aligned", fn, align);
+    return TFG_OK;
+}
+
+int check_element(const char *fn, const char *name, const void *p, int dtype) {
+    if (reinterpret_cast<uintptr_t>(p) % elem_bytes(dtype) != 0)
+        return fail(TFG_ERR_INVALID_ARG, "%s: %s is not aligned to its element", fn, name);
+    return TFG_OK;
+}
 
 int aggregate_common(const char *fn, int mode, const int32_t *rowptr, const int32_t *col,
                      const float *w, const float *dinv, const void *x, int dtype, int64_t n,
@@ -952,6 +978,387 @@ int tfg_segment_pool(const void *x, int x_dtype, const int64_t *batch, int64_t n
     return cuda_result(tfg::launch_segment_pool(x, x_dtype, batch, num_nodes, num_graphs,
                                                 num_features, reduce, out, status,
                                                 reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+// ---- embedding lookup and its gradient --------------------------------------------
+namespace {
+constexpr int64_t kMaxEmbeddingFeatures = int64_t(65535) * 128;
+
+int check_embedding(const char *fn, int64_t num_ids, int64_t num_rows, int64_t num_features) {
+    if (num_ids < 0 || num_rows < 0)
+        return fail(TFG_ERR_INVALID_ARG, "%s: negative size (ids=%lld, rows=%lld)", fn, (long long)num_ids, (long long)num_rows);
+    if (num_ids >= kIndexLimit - 1 || num_rows >= kIndexLimit - 1)
+        return fail(TFG_ERR_TOO_LARGE, "%s: ids and rows must be < 2^31 - 1 (ids=%lld, rows=%lld)", fn, (long long)num_ids,
+                    (long long)num_rows);
+    if (num_features < 1) return fail(TFG_ERR_INVALID_ARG, "%s: feature count must be positive", fn);
+    if (num_features > kMaxEmbeddingFeatures)
+        return fail(TFG_ERR_TOO_LARGE, "%s: at most %lld features", fn, (long long)kMaxEmbeddingFeatures);
+    if ((num_ids > num_rows ? num_ids : num_rows) * num_features >= (int64_t(1) << 46))
+        return fail(TFG_ERR_TOO_LARGE, "%s: rows * features too large", fn);
+    return TFG_OK;
+}
+
+int lookup_common(const char *fn, const void *ids, bool id32, int64_t num_ids, const void *table, int table_dtype,
+                  int64_t num_rows, int64_t num_features, float scale, int64_t padding_id, void *out, int out_dtype,
+                  int32_t *status, tfg_stream_t stream) {
+    TFG_RANGE(fn);
+    TFG_TRY(check_embedding(fn, num_ids, num_rows, num_features));
+    TFG_TRY(check_dtype(fn, table_dtype));
+    TFG_TRY(check_dtype(fn, out_dtype));
+    TFG_NEED(ids, num_ids > 0, fn, "ids");
+    TFG_NEED(table, num_rows > 0, fn, "table");
+    TFG_NEED(out, num_ids > 0, fn, "out");
+    TFG_NEED(status, true, fn, "status");
+    TFG_TRY(check_element(fn, "table", table, table_dtype));
+    TFG_TRY(check_element(fn, "out", out, out_dtype));
+    const size_t id_bytes = (id32 ? sizeof(int32_t) : sizeof(int64_t)) * size_t(num_ids);
+    const size_t table_bytes = elem_bytes(table_dtype) * size_t(num_rows * num_features);
+    const size_t out_bytes = elem_bytes(out_dtype) * size_t(num_ids * num_features);
+    if (overlap(out, out_bytes, table, table_bytes) || overlap(out, out_bytes, ids, id_bytes))
+        return fail(TFG_ERR_INVALID_ARG, "%s: out overlaps an input", fn);
+    TFG_DEBUG(debug_extent(fn, "ids", ids, id_bytes));
+    TFG_DEBUG(debug_extent(fn, "table", table, table_bytes));
+    TFG_DEBUG(debug_extent(fn, "out", out, out_bytes));
+    return cuda_result(tfg::launch_embedding_lookup(ids, id32, num_ids, table, table_dtype, num_rows, num_features, scale,
+                                                    padding_id, out, out_dtype, status,
+                                                    reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int group_ids_common(const char *fn, const void *ids, bool id32, int64_t num_ids, int64_t num_rows, int64_t padding_id,
+                     int32_t *rowptr, int32_t *sorted_ids, int32_t *perm, void *workspace, size_t workspace_bytes,
+                     int32_t *status, tfg_stream_t stream) {
+    TFG_RANGE(fn);
+    TFG_TRY(check_embedding(fn, num_ids, num_rows, 1));
+    TFG_NEED(ids, num_ids > 0, fn, "ids");
+    TFG_NEED(rowptr, true, fn, "rowptr");
+    TFG_NEED(sorted_ids, num_ids > 0, fn, "sorted_ids");
+    TFG_NEED(perm, num_ids > 0, fn, "perm");
+    TFG_NEED(status, true, fn, "status");
+    if (num_ids > 0)
+        TFG_TRY(check_workspace(fn, workspace, workspace_bytes, tfg::group_ids_workspace_bytes(num_rows, num_ids), 256));
+    TFG_DEBUG(debug_extent(fn, "ids", ids, (id32 ? sizeof(int32_t) : sizeof(int64_t)) * size_t(num_ids)));
+    TFG_DEBUG(debug_extent(fn, "rowptr", rowptr, sizeof(int32_t) * size_t(num_rows + 1)));
+    TFG_DEBUG(debug_extent(fn, "sorted_ids", sorted_ids, sizeof(int32_t) * size_t(num_ids)));
+    TFG_DEBUG(debug_extent(fn, "perm", perm, sizeof(int32_t) * size_t(num_ids)));
+    return cuda_result(tfg::launch_group_ids(ids, id32, num_ids, num_rows, padding_id, rowptr, sorted_ids, perm, workspace,
+                                             status, reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+}  // namespace
+
+int tfg_embedding_lookup(const int64_t *ids, int64_t num_ids, const void *table, int table_dtype, int64_t num_rows,
+                         int64_t num_features, float scale, int64_t padding_id, void *out, int out_dtype,
+                         int32_t *status, tfg_stream_t stream) {
+    return lookup_common("tfg_embedding_lookup", ids, false, num_ids, table, table_dtype, num_rows, num_features, scale,
+                         padding_id, out, out_dtype, status, stream);
+}
+
+int tfg_embedding_lookup32(const int32_t *ids, int64_t num_ids, const void *table, int table_dtype, int64_t num_rows,
+                           int64_t num_features, float scale, int64_t padding_id, void *out, int out_dtype,
+                           int32_t *status, tfg_stream_t stream) {
+    return lookup_common("tfg_embedding_lookup32", ids, true, num_ids, table, table_dtype, num_rows, num_features, scale,
+                         padding_id, out, out_dtype, status, stream);
+}
+
+int tfg_group_ids_workspace_size(int64_t num_rows, int64_t num_ids, size_t *bytes) {
+    const char *fn = "tfg_group_ids_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_embedding(fn, num_ids, num_rows, 1));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::group_ids_workspace_bytes(num_rows, num_ids);
+    return ok();
+}
+
+int tfg_group_ids(const int64_t *ids, int64_t num_ids, int64_t num_rows, int64_t padding_id, int32_t *rowptr,
+                  int32_t *sorted_ids, int32_t *perm, void *workspace, size_t workspace_bytes, int32_t *status,
+                  tfg_stream_t stream) {
+    return group_ids_common("tfg_group_ids", ids, false, num_ids, num_rows, padding_id, rowptr, sorted_ids, perm, workspace,
+                            workspace_bytes, status, stream);
+}
+
+int tfg_group_ids32(const int32_t *ids, int64_t num_ids, int64_t num_rows, int64_t padding_id, int32_t *rowptr,
+                    int32_t *sorted_ids, int32_t *perm, void *workspace, size_t workspace_bytes, int32_t *status,
+                    tfg_stream_t stream) {
+    return group_ids_common("tfg_group_ids32", ids, true, num_ids, num_rows, padding_id, rowptr, sorted_ids, perm, workspace,
+                            workspace_bytes, status, stream);
+}
+
+int tfg_embedding_backward_workspace_size(int64_t num_features, size_t *bytes) {
+    const char *fn = "tfg_embedding_backward_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_embedding(fn, 0, 0, num_features));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::embedding_backward_workspace_bytes(num_features);
+    return ok();
+}
+
+int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, const int32_t *perm, const void *grad_out,
+                           int grad_dtype, int64_t num_ids, int64_t num_rows, int64_t num_features, float scale,
+                           float *grad_table, void *workspace, size_t workspace_bytes, tfg_stream_t stream) {
+    const char *fn = "tfg_embedding_backward";
+    TFG_RANGE(fn);
+    TFG_TRY(check_embedding(fn, num_ids, num_rows, num_features));
+    TFG_TRY(check_dtype(fn, grad_dtype));
+    TFG_NEED(rowptr, true, fn, "rowptr");
+    TFG_NEED(sorted_ids, num_ids > 0, fn, "sorted_ids");
+    TFG_NEED(perm, num_ids > 0, fn, "perm");
+    TFG_NEED(grad_out, num_ids > 0, fn, "grad_out");
+    TFG_NEED(grad_table, num_rows > 0, fn, "grad_table");
+    TFG_TRY(check_element(fn, "grad_out", grad_out, grad_dtype));
+    TFG_TRY(check_element(fn, "grad_table", grad_table, TFG_F32));
+    const size_t grad_bytes = elem_bytes(grad_dtype) * size_t(num_ids * num_features);
+    const size_t table_bytes = sizeof(float) * size_t(num_rows * num_features);
+    if (overlap(grad_table, table_bytes, grad_out, grad_bytes))
+        return fail(TFG_ERR_INVALID_ARG, "%s: grad_table overlaps grad_out", fn);
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, tfg::embedding_backward_workspace_bytes(num_features), 16));
+    TFG_DEBUG(debug_extent(fn, "rowptr", rowptr, sizeof(int32_t) * size_t(num_rows + 1)));
+    TFG_DEBUG(debug_extent(fn, "sorted_ids", sorted_ids, sizeof(int32_t) * size_t(num_ids)));
+    TFG_DEBUG(debug_extent(fn, "perm", perm, sizeof(int32_t) * size_t(num_ids)));
+    TFG_DEBUG(debug_extent(fn, "grad_out", grad_out, grad_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_table", grad_table, table_bytes));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, tfg::embedding_backward_workspace_bytes(num_features)));
+    if (num_rows == 0) return ok();
+    return cuda_result(tfg::launch_embedding_backward(rowptr, sorted_ids, perm, grad_out, grad_dtype, num_ids, num_rows,
+                                                      num_features, scale, grad_table, workspace,
+                                                      reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+// ---- group norm -------------------------------------------------------------------
+namespace {
+constexpr int64_t kMaxGroupChannels = 1024;
+
+int check_group_norm(const char *fn, int64_t num_nodes, int64_t num_graphs, int64_t num_features, int64_t num_groups) {
+    TFG_TRY(check_counts(fn, num_nodes, 0));
+    if (num_graphs < 0) return fail(TFG_ERR_INVALID_ARG, "%s: negative graph count", fn);
+    if (num_graphs >= kIndexLimit) return fail(TFG_ERR_TOO_LARGE, "%s: too many graphs", fn);
+    TFG_TRY(check_features(fn, num_nodes > num_graphs ? num_nodes : num_graphs, num_features));
+    if (num_groups < 1 || num_features % num_groups != 0)
+        return fail(TFG_ERR_INVALID_ARG, "%s: num_groups (%lld) must divide num_features (%lld)", fn, (long long)num_groups,
+                    (long long)num_features);
+    if (num_features / num_groups > kMaxGroupChannels)
+        return fail(TFG_ERR_TOO_LARGE, "%s: at most %lld channels per group", fn, (long long)kMaxGroupChannels);
+    if (!tfg::group_norm_fits(num_nodes, num_graphs, num_features, num_groups))
+        return fail(TFG_ERR_TOO_LARGE, "%s: graphs * features too large", fn);
+    return TFG_OK;
+}
+
+int check_activation(const char *fn, int activation) {
+    if (activation < TFG_ACT_NONE || activation > TFG_ACT_GELU)
+        return fail(TFG_ERR_INVALID_ARG, "%s: unknown activation %d", fn, activation);
+    return TFG_OK;
+}
+}  // namespace
+
+int tfg_group_norm_workspace_size(int64_t num_nodes, int64_t num_graphs, int64_t num_features, int64_t num_groups,
+                                  size_t *bytes) {
+    const char *fn = "tfg_group_norm_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_group_norm(fn, num_nodes, num_graphs, num_features, num_groups));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::group_norm_workspace_bytes(num_nodes, num_graphs, num_features, num_groups);
+    return ok();
+}
+
+int tfg_group_norm(const void *x, int x_dtype, const int64_t *node_offsets, int64_t num_nodes, int64_t num_graphs,
+                   int64_t num_features, int64_t num_groups, const float *gamma, const float *beta, float eps,
+                   int activation, void *out, int out_dtype, float *mean, float *rstd, void *workspace,
+                   size_t workspace_bytes, int32_t *status, tfg_stream_t stream) {
+    const char *fn = "tfg_group_norm";
+    TFG_RANGE(fn);
+    TFG_TRY(check_group_norm(fn, num_nodes, num_graphs, num_features, num_groups));
+    TFG_TRY(check_dtype(fn, x_dtype));
+    TFG_TRY(check_dtype(fn, out_dtype));
+    TFG_TRY(check_activation(fn, activation));
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(TFG_ERR_INVALID_ARG, "%s: eps must be finite and positive", fn);
+    TFG_NEED(x, num_nodes > 0, fn, "x");
+    TFG_NEED(out, num_nodes > 0, fn, "out");
+    TFG_NEED(node_offsets, num_graphs > 0, fn, "node_offsets");
+    TFG_NEED(status, true, fn, "status");
+    if ((mean == nullptr) != (rstd == nullptr))
+        return fail(TFG_ERR_INVALID_ARG, "%s: mean and rstd are wanted both or neither", fn);
+    TFG_TRY(check_element(fn, "x", x, x_dtype));
+    TFG_TRY(check_element(fn, "out", out, out_dtype));
+    const size_t x_bytes = elem_bytes(x_dtype) * size_t(num_nodes * num_features);
+    const size_t out_bytes = elem_bytes(out_dtype) * size_t(num_nodes * num_features);
+    if (overlap(out, out_bytes, x, x_bytes)) return fail(TFG_ERR_INVALID_ARG, "%s: out overlaps x", fn);
+    const size_t need = tfg::group_norm_workspace_bytes(num_nodes, num_graphs, num_features, num_groups);
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
+    TFG_DEBUG(debug_extent(fn, "x", x, x_bytes));
+    TFG_DEBUG(debug_extent(fn, "out", out, out_bytes));
+    TFG_DEBUG(debug_extent(fn, "node_offsets", node_offsets, sizeof(int64_t) * size_t(num_graphs + 1)));
+    TFG_DEBUG(debug_extent(fn, "gamma", gamma, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "beta", beta, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "mean", mean, sizeof(float) * size_t(num_graphs * num_groups)));
+    TFG_DEBUG(debug_extent(fn, "rstd", rstd, sizeof(float) * size_t(num_graphs * num_groups)));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
+    return cuda_result(tfg::launch_group_norm(x, x_dtype, node_offsets, num_nodes, num_graphs, num_features, num_groups,
+                                              gamma, beta, eps, activation, out, out_dtype, mean, rstd, workspace, status,
+                                              reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int tfg_group_norm_backward_workspace_size(int64_t num_nodes, int64_t num_graphs, int64_t num_features, int64_t num_groups,
+                                           size_t *bytes) {
+    const char *fn = "tfg_group_norm_backward_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_group_norm(fn, num_nodes, num_graphs, num_features, num_groups));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::group_norm_backward_workspace_bytes(num_nodes, num_graphs, num_features, num_groups);
+    return ok();
+}
+
+int tfg_group_norm_backward(const void *x, int x_dtype, const int64_t *node_offsets, int64_t num_nodes,
+                            int64_t num_graphs, int64_t num_features, int64_t num_groups, const float *gamma,
+                            const float *beta, const float *mean, const float *rstd, int activation, const void *grad_out,
+                            int grad_dtype, void *grad_x, float *grad_gamma, float *grad_beta, void *workspace,
+                            size_t workspace_bytes, tfg_stream_t stream) {
+    const char *fn = "tfg_group_norm_backward";
+    TFG_RANGE(fn);
+    TFG_TRY(check_group_norm(fn, num_nodes, num_graphs, num_features, num_groups));
+    TFG_TRY(check_dtype(fn, x_dtype));
+    TFG_TRY(check_dtype(fn, grad_dtype));
+    TFG_TRY(check_activation(fn, activation));
+    TFG_NEED(x, num_nodes > 0, fn, "x");
+    TFG_NEED(grad_out, num_nodes > 0, fn, "grad_out");
+    TFG_NEED(grad_x, num_nodes > 0, fn, "grad_x");
+    TFG_NEED(node_offsets, num_graphs > 0, fn, "node_offsets");
+    TFG_NEED(mean, num_graphs > 0, fn, "mean");
+    TFG_NEED(rstd, num_graphs > 0, fn, "rstd");
+    if ((grad_gamma == nullptr) != (grad_beta == nullptr))
+        return fail(TFG_ERR_INVALID_ARG, "%s: grad_gamma and grad_beta are wanted both or neither", fn);
+    TFG_TRY(check_element(fn, "x", x, x_dtype));
+    TFG_TRY(check_element(fn, "grad_out", grad_out, grad_dtype));
+    TFG_TRY(check_element(fn, "grad_x", grad_x, grad_dtype));
+    const size_t x_bytes = elem_bytes(x_dtype) * size_t(num_nodes * num_features);
+    const size_t g_bytes = elem_bytes(grad_dtype) * size_t(num_nodes * num_features);
+    if (overlap(grad_x, g_bytes, x, x_bytes) || overlap(grad_x, g_bytes, grad_out, g_bytes))
+        return fail(TFG_ERR_INVALID_ARG, "%s: grad_x overlaps an input", fn);
+    const size_t need = tfg::group_norm_backward_workspace_bytes(num_nodes, num_graphs, num_features, num_groups);
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
+    TFG_DEBUG(debug_extent(fn, "x", x, x_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_out", grad_out, g_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_x", grad_x, g_bytes));
+    TFG_DEBUG(debug_extent(fn, "node_offsets", node_offsets, sizeof(int64_t) * size_t(num_graphs + 1)));
+    TFG_DEBUG(debug_extent(fn, "gamma", gamma, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "beta", beta, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "mean", mean, sizeof(float) * size_t(num_graphs * num_groups)));
+    TFG_DEBUG(debug_extent(fn, "rstd", rstd, sizeof(float) * size_t(num_graphs * num_groups)));
+    TFG_DEBUG(debug_extent(fn, "grad_gamma", grad_gamma, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "grad_beta", grad_beta, sizeof(float) * size_t(num_features)));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
+    return cuda_result(tfg::launch_group_norm_backward(x, x_dtype, node_offsets, num_nodes, num_graphs, num_features,
+                                                       num_groups, gamma, beta, mean, rstd, activation, grad_out, grad_dtype,
+                                                       grad_x, grad_gamma, grad_beta, workspace,
+                                                       reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+// ---- global norm and clipping -----------------------------------------------------
+namespace {
+constexpr int64_t kMaxTensors = int64_t(1) << 20;
+
+int check_tensors(const char *fn, int64_t num_tensors, const void *const *tensors, const int64_t *sizes, const int *dtypes) {
+    if (num_tensors < 0) return fail(TFG_ERR_INVALID_ARG, "%s: negative tensor count", fn);
+    if (num_tensors > kMaxTensors) return fail(TFG_ERR_TOO_LARGE, "%s: at most %lld tensors", fn, (long long)kMaxTensors);
+    TFG_NEED(tensors, num_tensors > 0, fn, "tensors");
+    TFG_NEED(sizes, num_tensors > 0, fn, "sizes");
+    TFG_NEED(dtypes, num_tensors > 0, fn, "dtypes");
+    int64_t total = 0;
+    for (int64_t i = 0; i < num_tensors; ++i) {
+        if (sizes[i] < 0) return fail(TFG_ERR_INVALID_ARG, "%s: tensor %lld has a negative size", fn, (long long)i);
+        if (sizes[i] >= (int64_t(1) << 46) || (total += sizes[i]) >= (int64_t(1) << 46))
+            return fail(TFG_ERR_TOO_LARGE, "%s: too many values", fn);
+        TFG_TRY(check_dtype(fn, dtypes[i]));
+        if (sizes[i] > 0 && tensors[i] == nullptr)
+            return fail(TFG_ERR_INVALID_ARG, "%s: tensor %lld must not be NULL", fn, (long long)i);
+        TFG_TRY(check_element(fn, "a tensor", tensors[i], dtypes[i]));
+        TFG_DEBUG(debug_extent(fn, "a tensor", tensors[i], elem_bytes(dtypes[i]) * size_t(sizes[i])));
+    }
+    return TFG_OK;
+}
+
+// A range of bytes that a call reads (out = -1) or writes (out = the tensor's number).
+struct Extent {
+    uintptr_t at;
+    size_t bytes;
+    int64_t tensor;
+    bool out;
+};
+
+// Outputs may share bytes with nothing but the very tensor they are scaled from.
+int check_outs(const char *fn, int64_t num_tensors, const void *const *tensors, const int64_t *sizes, const int *dtypes,
+               void *const *outs) {
+    std::unique_ptr<Extent[]> all(new (std::nothrow) Extent[size_t(2 * num_tensors)]);
+    if (!all) return fail(TFG_ERR_TOO_LARGE, "%s: no host memory for %lld tensors", fn, (long long)num_tensors);
+    int64_t m = 0;
+    for (int64_t i = 0; i < num_tensors; ++i) {
+        if (sizes[i] == 0) continue;
+        if (outs[i] == nullptr) return fail(TFG_ERR_INVALID_ARG, "%s: output %lld must not be NULL", fn, (long long)i);
+        TFG_TRY(check_element(fn, "an output", outs[i], dtypes[i]));
+        const size_t bytes = elem_bytes(dtypes[i]) * size_t(sizes[i]);
+        TFG_DEBUG(debug_extent(fn, "an output", outs[i], bytes));
+        if (outs[i] != tensors[i]) all[m++] = {reinterpret_cast<uintptr_t>(tensors[i]), bytes, i, false};
+        all[m++] = {reinterpret_cast<uintptr_t>(outs[i]), bytes, i, true};
+    }
+    std::sort(all.get(), all.get() + m, [](const Extent &a, const Extent &b) { return a.at < b.at; });
+    // in order of their begin, a range that reaches past another's begin overlaps it: it is
+    // enough to keep the furthest end of the outputs and of all ranges so far
+    uintptr_t end_out = 0, end_any = 0;
+    for (int64_t i = 0; i < m; ++i) {
+        if (all[i].at < end_out || (all[i].out && all[i].at < end_any))
+            return fail(TFG_ERR_INVALID_ARG, "%s: output of tensor %lld overlaps another tensor", fn, (long long)all[i].tensor);
+        const uintptr_t end = all[i].at + all[i].bytes;
+        if (end > end_any) end_any = end;
+        if (all[i].out && end > end_out) end_out = end;
+    }
+    return TFG_OK;
+}
+}  // namespace
+
+int tfg_global_norm_workspace_size(int64_t num_tensors, size_t *bytes) {
+    const char *fn = "tfg_global_norm_workspace_size";
+    TFG_RANGE(fn);
+    if (num_tensors < 0) return fail(TFG_ERR_INVALID_ARG, "%s: negative tensor count", fn);
+    if (num_tensors > kMaxTensors) return fail(TFG_ERR_TOO_LARGE, "%s: at most %lld tensors", fn, (long long)kMaxTensors);
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::global_norm_workspace_bytes(num_tensors);
+    return ok();
+}
+
+int tfg_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes, const int *dtypes, float *norm,
+                    void *workspace, size_t workspace_bytes, tfg_stream_t stream) {
+    const char *fn = "tfg_global_norm";
+    TFG_RANGE(fn);
+    TFG_TRY(check_tensors(fn, num_tensors, tensors, sizes, dtypes));
+    TFG_NEED(norm, true, fn, "norm");
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, tfg::global_norm_workspace_bytes(num_tensors), 16));
+    TFG_DEBUG(debug_extent(fn, "norm", norm, sizeof(float)));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, tfg::global_norm_workspace_bytes(num_tensors)));
+    return cuda_result(tfg::launch_global_norm(num_tensors, tensors, sizes, dtypes, 0.f, nullptr, norm, workspace,
+                                               reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes, const int *dtypes,
+                            float clip_norm, void *const *outs, float *norm, void *workspace, size_t workspace_bytes,
+                            tfg_stream_t stream) {
+    const char *fn = "tfg_clip_by_global_norm";
+    TFG_RANGE(fn);
+    TFG_TRY(check_tensors(fn, num_tensors, tensors, sizes, dtypes));
+    if (!(clip_norm > 0.f) || !std::isfinite(clip_norm))
+        return fail(TFG_ERR_INVALID_ARG, "%s: clip_norm must be finite and positive", fn);
+    TFG_NEED(outs, num_tensors > 0, fn, "outs");
+    TFG_NEED(norm, true, fn, "norm");
+    TFG_TRY(check_outs(fn, num_tensors, tensors, sizes, dtypes, outs));
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, tfg::global_norm_workspace_bytes(num_tensors), 16));
+    TFG_DEBUG(debug_extent(fn, "norm", norm, sizeof(float)));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, tfg::global_norm_workspace_bytes(num_tensors)));
+    void *none = nullptr;                         // no tensors: outs may be NULL, the norm is written all the same
+    return cuda_result(tfg::launch_global_norm(num_tensors, tensors, sizes, dtypes, clip_norm, outs ? outs : &none, norm,
+                                               workspace, reinterpret_cast<cudaStream_t>(stream)),
                        fn);
 }
 

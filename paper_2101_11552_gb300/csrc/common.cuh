@@ -311,6 +311,29 @@ cudaError_t launch_dot_softmax_backward(const int32_t *rowptr, const int32_t *co
                                         int64_t n, int64_t e, int heads, int channels, float scale,
                                         const float *out, const float *grad_out, float *grad_q,
                                         float *grad_k, float *grad_v, void *ws, cudaStream_t s);
+cudaError_t launch_embedding_lookup(const void *ids, bool id32, int64_t n, const void *table, int table_dtype,
+                                    int64_t rows, int64_t f, float scale, int64_t padding, void *out, int out_dtype,
+                                    int32_t *status, cudaStream_t s);
+size_t group_ids_workspace_bytes(int64_t rows, int64_t n);
+cudaError_t launch_group_ids(const void *ids, bool id32, int64_t n, int64_t rows, int64_t padding, int32_t *rowptr,
+                             int32_t *sorted_ids, int32_t *perm, void *ws, int32_t *status, cudaStream_t s);
+size_t embedding_backward_workspace_bytes(int64_t f);
+cudaError_t launch_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, const int32_t *perm,
+                                      const void *g, int g_dtype, int64_t n, int64_t rows, int64_t f, float scale,
+                                      float *out, void *ws, cudaStream_t s);
+bool group_norm_fits(int64_t n, int64_t graphs, int64_t f, int64_t groups);
+size_t group_norm_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t groups);
+cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets, int64_t n, int64_t graphs, int64_t f,
+                              int64_t groups, const float *gamma, const float *beta, float eps, int act, void *out,
+                              int out_dtype, float *mean, float *rstd, void *ws, int32_t *status, cudaStream_t s);
+size_t group_norm_backward_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t groups);
+cudaError_t launch_group_norm_backward(const void *x, int x_dtype, const int64_t *offsets, int64_t n, int64_t graphs,
+                                       int64_t f, int64_t groups, const float *gamma, const float *beta,
+                                       const float *mean, const float *rstd, int act, const void *g, int g_dtype,
+                                       void *grad_x, float *grad_gamma, float *grad_beta, void *ws, cudaStream_t s);
+size_t global_norm_workspace_bytes(int64_t tensors);
+cudaError_t launch_global_norm(int64_t tensors, const void *const *in, const int64_t *sizes, const int *dtypes,
+                               float clip, void *const *outs, float *norm, void *ws, cudaStream_t s);
 cudaError_t launch_gather_xor(const int32_t *col, int64_t e, const void *x, int64_t row_bytes,
                               uint32_t *out, cudaStream_t s);
 cudaError_t launch_segment_pool(const void *x, int x_dtype, const int64_t *batch, int64_t n,

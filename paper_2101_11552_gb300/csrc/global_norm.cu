@@ -1,0 +1,341 @@
+// The norm over all gradients of a model, and gradients clipped by it.
+//
+//   norm = sqrt(sum over tensors t, values i of t_i^2)
+//   out  = t * clip_norm / max(norm, clip_norm)
+//
+// Training a model on top of the aggregations ends each step with it (the gradient of
+// every layer is an output of the backward calls).  Two launches: partial sums of
+// squares, one per CTA; then every CTA of the second adds the partials in the same fixed
+// order and scales its share.  Both walk chunks of kChunk values across all tensors, so
+// that a model of many small tensors costs no more launches than one large tensor.
+//
+// Precision.  A thread adds 64 squares in fp32 and carries the sums of those in two
+// floats (the rounding error of every addition is kept), so long gradients lose nothing;
+// squares that leave the range of fp32 (values above 1e15 or all below 1e-13 or so) are
+// taken again in fp64.  The partials, the root and the factor are fp64, and the factor is
+// rounded once to fp32.
+#include "widen.cuh"
+
+namespace tfg {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kPerThread = 64;                    // values of a chunk that a thread sums
+constexpr int kChunk = kNormThreads * kPerThread;
+constexpr int kNormCtas = 1216;                   // eight a multiprocessor: partials of one launch
+constexpr int kListSmall = 32, kListLarge = 512;  // tensors of a launch (parameters of 1 and 16 KB)
+
+// The tensors of one launch, passed by value: nothing is copied to the device and a
+// captured launch keeps its list.  first[t] is the first chunk of tensor t.
+template <int CAP>
+struct TensorList {
+    const void *in[CAP];
+    void *out[CAP];
+    int64_t size[CAP];
+    int64_t first[CAP + 1];
+    uint8_t bf16[CAP];
+    int count;
+};
+
+// The tensor of a chunk: the last one that begins at or before it.
+template <int CAP>
+__device__ __forceinline__ int tensor_of(const TensorList<CAP> &list, int64_t chunk, int from) {
+    int lo = from, hi = list.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (list.first[mid] <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// ---- sums of squares --------------------------------------------------------------
+struct SquareSum {
+    float hi = 0.f, lo = 0.f;                     // sum = hi + lo
+    double wide = 0.0;                            // what left the range of fp32
+
+    __device__ __forceinline__ void add(float s) {
+        const float t = hi + s;                   // two-sum: t + e == hi + s
+        const float b = t - hi;
+        lo += (hi - (t - b)) + (s - b);
+        hi = t;
+    }
+    __device__ __forceinline__ double total() const { return static_cast<double>(hi) + lo + wide; }
+};
+
+// Squares of a thread's values of one chunk.  In range: the sum is below 2^100 and either
+// large enough that squares lost below 2^-149 do not count, or of zeros alone.
+template <int N>
+__device__ __forceinline__ void add_squares(SquareSum &acc, const float (&v)[N]) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i & 3] = fmaf(v[i], v[i], s[i & 3]);
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    if (sum > 8.3e-25f && sum < 1.2e30f) {        // 2^-80, 2^100
+        acc.add(sum);
+        return;
+    }
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(v[i]));
+    if (most == 0.f && sum == 0.f) return;        // zeros (a NaN makes the sum a NaN)
+    double w = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w += static_cast<double>(v[i]) * v[i];
+    acc.wide += w;
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void square_chunk(SquareSum &acc, const T *p, int64_t left) {
+    constexpr int kLoads = 32 / VEC;              // half a thread's values at a time
+#pragma unroll
+    for (int h = 0; h < kPerThread / 32; ++h) {
+        typename VecLoad<T, VEC>::Raw raw[kLoads];
+        const int64_t base = static_cast<int64_t>(h) * 32 * kNormThreads;
+        if (base >= left) break;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int64_t at = base + (static_cast<int64_t>(i) * kNormThreads + threadIdx.x) * VEC;
+            raw[i] = VecLoad<T, VEC>::zero();
+            if (at + VEC <= left) raw[i] = VecLoad<T, VEC>::raw(p + at);
+        }
+        float v[32];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            float w[VEC];
+            VecLoad<T, VEC>::widen(raw[i], w);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) v[i * VEC + q] = w[q];
+        }
+        add_squares<32>(acc, v);
+    }
+    if (VEC > 1 && left < kChunk && left % VEC != 0 && static_cast<int64_t>(threadIdx.x) < left % VEC) {
+        float v[1];
+        VecLoad<T, 1>::load(p + left / VEC * VEC + threadIdx.x, v);
+        add_squares<1>(acc, v);
+    }
+}
+
+// Sum over the CTA in a fixed order; thread 0 has it.
+__device__ __forceinline__ double cta_sum(double v, double *s_warp) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += lane_xor(v, o);
+    if (lane == 0) s_warp[warp] = v;
+    __syncthreads();
+    double t = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kNormThreads / 32; ++w) t += s_warp[w];
+    __syncthreads();
+    return t;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kNormThreads)
+sum_squares(const __grid_constant__ TensorList<CAP> list, double *__restrict__ partial) {
+    __shared__ double s_warp[kNormThreads / 32];
+    SquareSum acc;
+    const int64_t chunks = list.first[list.count];
+    int t = 0;
+    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        t = tensor_of(list, c, t);
+        const int64_t at = (c - list.first[t]) * kChunk;
+        const int64_t left = min64(kChunk, list.size[t] - at);
+        const bool aligned = reinterpret_cast<uintptr_t>(list.in[t]) % 16 == 0;
+        if (list.bf16[t]) {
+            const uint16_t *p = static_cast<const uint16_t *>(list.in[t]) + at;
+            if (aligned) square_chunk<uint16_t, 8>(acc, p, left);
+            else square_chunk<uint16_t, 1>(acc, p, left);
+        } else {
+            const float *p = static_cast<const float *>(list.in[t]) + at;
+            if (aligned) square_chunk<float, 4>(acc, p, left);
+            else square_chunk<float, 1>(acc, p, left);
+        }
+    }
+    const double sum = cta_sum(acc.total(), s_warp);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+// Sum of all partials, the same in every CTA.
+__device__ __forceinline__ double add_partials(const double *__restrict__ partial, int n, double *s_warp) {
+    double v = 0.0;
+    for (int i = threadIdx.x; i < n; i += kNormThreads) v += __ldg(partial + i);
+    return cta_sum(v, s_warp);
+}
+
+__global__ void __launch_bounds__(kNormThreads)
+write_norm(const double *__restrict__ partial, int n, float *__restrict__ norm) {
+    __shared__ double s_warp[kNormThreads / 32];
+    const double sum = add_partials(partial, n, s_warp);
+    if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+}
+
+// ---- scaling ----------------------------------------------------------------------
+// Plain loads: out may be the tensor itself, and then what is read is written here.
+template <typename T, int VEC>
+__device__ __forceinline__ typename VecLoad<T, VEC>::Raw plain_load(const T *p) {
+    if constexpr (VEC == 1) {
+        if constexpr (sizeof(T) == 2) return static_cast<uint32_t>(*p) << 16;
+        else return *p;
+    } else {
+        return *reinterpret_cast<const typename VecLoad<T, VEC>::Raw *>(p);
+    }
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, float factor) {
+    constexpr int kLoads = 32 / VEC;
+#pragma unroll
+    for (int h = 0; h < kPerThread / 32; ++h) {
+        typename VecLoad<T, VEC>::Raw raw[kLoads];
+        const int64_t base = static_cast<int64_t>(h) * 32 * kNormThreads;
+        if (base >= left) break;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int64_t at = base + (static_cast<int64_t>(i) * kNormThreads + threadIdx.x) * VEC;
+            raw[i] = VecLoad<T, VEC>::zero();
+            if (at + VEC <= left) raw[i] = plain_load<T, VEC>(p + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int64_t at = base + (static_cast<int64_t>(i) * kNormThreads + threadIdx.x) * VEC;
+            if (at + VEC > left) continue;
+            float v[VEC];
+            VecLoad<T, VEC>::widen(raw[i], v);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) v[q] *= factor;
+            store_vec<VEC>(o + at, v);
+        }
+    }
+    if (VEC > 1 && left < kChunk && static_cast<int64_t>(threadIdx.x) < left % VEC) {
+        const int64_t at = left / VEC * VEC + threadIdx.x;
+        float v[1];
+        VecLoad<T, 1>::widen(plain_load<T, 1>(p + at), v);
+        v[0] *= factor;
+        store_vec<1>(o + at, v);
+    }
+}
+
+// norm: written by the first CTA where it is not null (the first of several launches).
+template <int CAP>
+__global__ void __launch_bounds__(kNormThreads)
+scale_by_norm(const __grid_constant__ TensorList<CAP> list, const double *__restrict__ partial, int n, float clip,
+              float *__restrict__ norm) {
+    __shared__ double s_warp[kNormThreads / 32];
+    __shared__ float s_factor;
+    const double sum = add_partials(partial, n, s_warp);
+    if (threadIdx.x == 0) {
+        const double root = sqrt(sum);
+        const float rounded = static_cast<float>(root);
+        if (norm && blockIdx.x == 0) *norm = rounded;
+        // a norm that is no finite number leaves nothing to keep: NaN everywhere
+        float factor = isfinite(rounded) ? 1.f : __int_as_float(0x7fc00000);
+        if (isfinite(rounded) && root > clip) factor = static_cast<float>(clip / root);
+        s_factor = factor;
+    }
+    __syncthreads();
+    const float factor = s_factor;
+    const int64_t chunks = list.first[list.count];
+    int t = 0;
+    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        t = tensor_of(list, c, t);
+        if (factor == 1.f && list.in[t] == list.out[t]) continue;      // in place and nothing to do
+        const int64_t at = (c - list.first[t]) * kChunk;
+        const int64_t left = min64(kChunk, list.size[t] - at);
+        const bool aligned = (reinterpret_cast<uintptr_t>(list.in[t]) | reinterpret_cast<uintptr_t>(list.out[t])) % 16 == 0;
+        if (list.bf16[t]) {
+            const uint16_t *p = static_cast<const uint16_t *>(list.in[t]) + at;
+            uint16_t *o = static_cast<uint16_t *>(list.out[t]) + at;
+            if (aligned) scale_chunk<uint16_t, 8>(p, o, left, factor);
+            else scale_chunk<uint16_t, 1>(p, o, left, factor);
+        } else {
+            const float *p = static_cast<const float *>(list.in[t]) + at;
+            float *o = static_cast<float *>(list.out[t]) + at;
+            if (aligned) scale_chunk<float, 4>(p, o, left, factor);
+            else scale_chunk<float, 1>(p, o, left, factor);
+        }
+    }
+}
+
+int64_t chunks_of(int64_t size) { return (size + kChunk - 1) / kChunk; }
+int ctas_for(int64_t chunks) { return static_cast<int>(min64(chunks, kNormCtas)); }
+
+template <int CAP>
+int64_t fill(TensorList<CAP> &list, int64_t from, int64_t to, const void *const *in, void *const *out,
+             const int64_t *sizes, const int *dtypes) {
+    int64_t chunk = 0;
+    list.count = 0;
+    for (int64_t t = from; t < to; ++t) {
+        if (sizes[t] == 0) continue;              // no chunk: the search would not tell it from its neighbour
+        const int i = list.count++;
+        list.in[i] = in[t];
+        list.out[i] = out ? out[t] : nullptr;
+        list.size[i] = sizes[t];
+        list.first[i] = chunk;
+        list.bf16[i] = dtypes[t] == TFG_BF16;
+        chunk += chunks_of(sizes[t]);
+    }
+    list.first[list.count] = chunk;
+    return chunk;
+}
+
+template <int CAP>
+cudaError_t squares_of(int64_t from, int64_t to, const void *const *in, const int64_t *sizes, const int *dtypes,
+                       double *partial, int *ctas, cudaStream_t s) {
+    TensorList<CAP> list;
+    *ctas = ctas_for(fill(list, from, to, in, nullptr, sizes, dtypes));
+    if (*ctas == 0) return cudaSuccess;
+    sum_squares<CAP><<<*ctas, kNormThreads, 0, s>>>(list, partial);
+    return cudaGetLastError();
+}
+
+template <int CAP>
+cudaError_t scale_of(int64_t from, int64_t to, const void *const *in, void *const *out, const int64_t *sizes,
+                     const int *dtypes, const double *partial, int n, float clip, float *norm, cudaStream_t s) {
+    TensorList<CAP> list;
+    const int ctas = ctas_for(fill(list, from, to, in, out, sizes, dtypes));
+    if (ctas == 0 && !norm) return cudaSuccess;
+    scale_by_norm<CAP><<<ctas > 0 ? ctas : 1, kNormThreads, 0, s>>>(list, partial, n, clip, norm);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t global_norm_workspace_bytes(int64_t tensors) {
+    const int64_t launches = (tensors + kListLarge - 1) / kListLarge;
+    return sizeof(double) * kNormCtas * size_t(launches < 1 ? 1 : launches);
+}
+
+// outs null: the norm alone.
+cudaError_t launch_global_norm(int64_t tensors, const void *const *in, const int64_t *sizes, const int *dtypes,
+                               float clip, void *const *outs, float *norm, void *ws, cudaStream_t s) {
+    double *partial = static_cast<double *>(ws);
+    int n = 0;
+    for (int64_t from = 0; from < tensors; from += kListLarge) {
+        const int64_t to = min64(tensors, from + kListLarge);
+        int ctas = 0;
+        const cudaError_t err = to - from <= kListSmall
+                                    ? squares_of<kListSmall>(from, to, in, sizes, dtypes, partial + n, &ctas, s)
+                                    : squares_of<kListLarge>(from, to, in, sizes, dtypes, partial + n, &ctas, s);
+        if (err != cudaSuccess) return err;
+        n += ctas;
+    }
+    if (!outs) {
+        write_norm<<<1, kNormThreads, 0, s>>>(partial, n, norm);
+        return cudaGetLastError();
+    }
+    int64_t from = 0;
+    do {
+        const int64_t to = min64(tensors, from + kListLarge);
+        float *first = from == 0 ? norm : nullptr;
+        const cudaError_t err =
+            to - from <= kListSmall
+                ? scale_of<kListSmall>(from, to, in, outs, sizes, dtypes, partial, n, clip, first, s)
+                : scale_of<kListLarge>(from, to, in, outs, sizes, dtypes, partial, n, clip, first, s);
+        if (err != cudaSuccess) return err;
+        from = to;
+    } while (from < tensors);
+    return cudaSuccess;
+}
+
+}  // namespace tfg

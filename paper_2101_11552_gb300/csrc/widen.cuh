@@ -1,0 +1,73 @@
+// Rows read and fp32 results stored in either storage type, shared by the operators whose outputs
+// may be fp32 or bf16 (embedding lookup, group norm, clipped gradients).
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace tfg {
+
+// Two fp32 values rounded to nearest even, packed as the two bf16 halves of a word.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+
+// Makes the compiler take v for new, so that values widened from it in one pass are not
+// kept in registers for the next one (a held bf16 vector would take twice its room).
+__device__ __forceinline__ void renew(uint32_t &v) { asm volatile("" : "+r"(v)); }
+__device__ __forceinline__ void renew(float &v) { asm volatile("" : "+f"(v)); }
+__device__ __forceinline__ void renew(float4 &v) { renew(v.x); renew(v.y); renew(v.z); renew(v.w); }
+__device__ __forceinline__ void renew(uint2 &v) { renew(v.x); renew(v.y); }
+__device__ __forceinline__ void renew(uint4 &v) { renew(v.x); renew(v.y); renew(v.z); renew(v.w); }
+
+// VEC values of a row as they lie in memory, and widened: VecLoad with its eight fp32 values
+// as two 16-byte loads, for rows that are 16-byte but not 32-byte aligned.
+template <typename TT, int VEC> struct RowVec;
+template <> struct RowVec<float, 8> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = __ldg(reinterpret_cast<const float4 *>(p));
+        b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    __device__ __forceinline__ void renewed() { renew(a); renew(b); }
+};
+template <typename TT, int VEC> struct RowVec {
+    typename VecLoad<TT, VEC>::Raw r;
+    __device__ __forceinline__ void load(const TT *p) { r = VecLoad<TT, VEC>::raw(p); }
+    __device__ __forceinline__ void widen(float (&v)[VEC]) const { VecLoad<TT, VEC>::widen(r, v); }
+    __device__ __forceinline__ void renewed() { renew(r); }
+};
+
+// VEC values to p (fp32, or bf16 bits), p aligned to the vector it is stored as: 16 bytes,
+// or 8 for four bf16 values.  The one rounding of a bf16 result is here.
+template <int VEC>
+__device__ __forceinline__ void store_vec(float *p, const float (&v)[VEC]) {
+    if constexpr (VEC % 4 == 0) {
+#pragma unroll
+        for (int q = 0; q < VEC; q += 4)
+            *reinterpret_cast<float4 *>(p + q) = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) p[q] = v[q];
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(uint16_t *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 8) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
+                                                   pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else if constexpr (VEC == 4) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) p[q] = static_cast<uint16_t>(pack_bf16(v[q], 0.f));
+    }
+}
+
+}  // namespace tfg

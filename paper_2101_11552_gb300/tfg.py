@@ -12,6 +12,7 @@ CUDA tensors on the same device; calls are asynchronous on the current stream.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -32,6 +33,8 @@ TFG_ERR_UNSORTED = -6
 TFG_ERR_TIMEOUT = -7
 TFG_F32, TFG_BF16 = 0, 1
 REDUCERS = {"sum": 0, "mean": 1, "max": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+NO_PADDING = -(1 << 63)       # padding_id of a list without padding
 
 _lock = threading.Lock()
 _lib: Optional[ctypes.CDLL] = None
@@ -101,6 +104,20 @@ def _load(path: str) -> ctypes.CDLL:
         "tfg_batch_graphs_workspace_size": [I64, ctypes.POINTER(SZ)],
         "tfg_batch_graphs": [I64, P, P, P, I64, I64, P, P, P, P, SZ, P, P],
         "tfg_gather_xor": [P, I64, P, I64, I64, P, P],
+        "tfg_embedding_lookup": [P, I64, P, I, I64, I64, F, I64, P, I, P, P],
+        "tfg_embedding_lookup32": [P, I64, P, I, I64, I64, F, I64, P, I, P, P],
+        "tfg_group_ids_workspace_size": [I64, I64, ctypes.POINTER(SZ)],
+        "tfg_group_ids": [P, I64, I64, I64, P, P, P, P, SZ, P, P],
+        "tfg_group_ids32": [P, I64, I64, I64, P, P, P, P, SZ, P, P],
+        "tfg_embedding_backward_workspace_size": [I64, ctypes.POINTER(SZ)],
+        "tfg_embedding_backward": [P, P, P, P, I, I64, I64, I64, F, P, P, SZ, P],
+        "tfg_group_norm_workspace_size": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
+        "tfg_group_norm": [P, I, P, I64, I64, I64, I64, P, P, F, I, P, I, P, P, P, SZ, P, P],
+        "tfg_group_norm_backward_workspace_size": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
+        "tfg_group_norm_backward": [P, I, P, I64, I64, I64, I64, P, P, P, P, I, P, I, P, P, P, P, SZ, P],
+        "tfg_global_norm_workspace_size": [I64, ctypes.POINTER(SZ)],
+        "tfg_global_norm": [I64, P, P, P, P, P, SZ, P],
+        "tfg_clip_by_global_norm": [I64, P, P, P, F, P, P, P, SZ, P],
         "tfg_edge_softmax_backward_workspace_size": [I64, I, I, ctypes.POINTER(SZ)],
         "tfg_edge_softmax_aggregate_backward": [P, P, P, P, P, I, I64, I64, I, I, P, P, F,
                                                 P, P, P, P, P, P, SZ, P],
@@ -651,3 +668,258 @@ def tfg_dot_edge_softmax_aggregate_backward(rowptr, col, rowptr_src, col_src, q,
         _x_dtype(q), n, col.numel(), heads, channels, float(scale), _ptr(out), _ptr(grad_out),
         _ptr(grads[0]), _ptr(grads[1]), _ptr(grads[2]), _ptr(ws), ws.numel(), _stream(dev)))
     return tuple(grads)
+
+
+def _run(dev: torch.device, fn, *args):
+    """Call the C entry point with ``dev`` as the current device (its stream is dev's)."""
+    if dev.index == torch.cuda.current_device():
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args))
+
+
+def _dtype_code(dtype: torch.dtype) -> int:
+    if dtype == torch.float32:
+        return TFG_F32
+    if dtype == torch.bfloat16:
+        return TFG_BF16
+    raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
+
+
+def _workspace(workspace, need: int, dev: torch.device):
+    """The caller's workspace, checked for its kind, or a new one."""
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    _need_cuda("workspace", workspace, torch.uint8, dev)
+    return workspace
+
+
+def _need_out(name: str, out, shape, dtype, dev):
+    """An output tensor: the caller's, which must be what would be allocated, or a new one."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _need_cuda(name, out, dtype, dev)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(out.shape)}")
+    return out
+
+
+def _need_ids(ids) -> bool:
+    """Whether the ids are int32 (else int64)."""
+    _need_cuda("ids", ids)
+    if ids.dtype not in (torch.int64, torch.int32):
+        raise TypeError("ids must be int64 or int32")
+    return ids.dtype == torch.int32
+
+
+def tfg_embedding_lookup(table, ids, scale: float = 1.0, padding_id: Optional[int] = None,
+                         out_dtype: Optional[torch.dtype] = None, out=None):
+    """scale * table[ids] for ids (int64 or int32) of any shape, zeros where an id is
+    ``padding_id``; the result has the shape of ids with a last dimension of F, in
+    ``out_dtype`` (the table's by default).  Returns (out, status)."""
+    id32 = _need_ids(ids)
+    dev = ids.device
+    _need_cuda("table", table, None, dev)
+    if table.dim() != 2:
+        raise ValueError("table must have shape [V, F]")
+    v, f = table.shape
+    if out_dtype is None:
+        out_dtype = table.dtype if out is None else out.dtype
+    out = _need_out("out", out, (*ids.shape, f), out_dtype, dev)
+    status = torch.empty(1, dtype=torch.int32, device=dev)
+    L = lib()
+    _run(dev, L.tfg_embedding_lookup32 if id32 else L.tfg_embedding_lookup, _ptr(ids), ids.numel(), _ptr(table),
+         _dtype_code(table.dtype), v, f, float(scale), NO_PADDING if padding_id is None else int(padding_id), _ptr(out),
+         _dtype_code(out_dtype), _ptr(status), _stream(dev))
+    return out, status
+
+
+class IdGroups(NamedTuple):
+    rowptr: torch.Tensor      # int32 [V + 1]: places of id v are rowptr[v] .. rowptr[v + 1] - 1
+    sorted_ids: torch.Tensor  # int32 [n]: the id of each place, V behind the last group
+    perm: torch.Tensor        # int32 [n]: the position that each place holds
+    status: torch.Tensor      # int32 [1] (device)
+
+
+def tfg_group_ids_workspace_size(num_rows: int, num_ids: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().tfg_group_ids_workspace_size(num_rows, num_ids, ctypes.byref(n)))
+    return n.value
+
+
+def tfg_group_ids(ids, num_rows: int, padding_id: Optional[int] = None, workspace=None) -> IdGroups:
+    """Order the positions of ``ids`` (any shape, taken flat) by id, equal ids by position."""
+    id32 = _need_ids(ids)
+    dev = ids.device
+    n = ids.numel()
+    need = tfg_group_ids_workspace_size(num_rows, n)
+    workspace = _workspace(workspace, need, dev)
+    rowptr = torch.empty(num_rows + 1, dtype=torch.int32, device=dev)
+    sorted_ids, perm = torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev)
+    status = torch.empty(1, dtype=torch.int32, device=dev)
+    L = lib()
+    _run(dev, L.tfg_group_ids32 if id32 else L.tfg_group_ids, _ptr(ids), n, num_rows,
+         NO_PADDING if padding_id is None else int(padding_id), _ptr(rowptr), _ptr(sorted_ids), _ptr(perm),
+         _ptr(workspace), workspace.numel(), _ptr(status), _stream(dev))
+    return IdGroups(rowptr, sorted_ids, perm, status)
+
+
+def tfg_embedding_backward_workspace_size(num_features: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().tfg_embedding_backward_workspace_size(num_features, ctypes.byref(n)))
+    return n.value
+
+
+def tfg_embedding_backward(groups: IdGroups, grad_out, scale: float = 1.0, out=None, workspace=None):
+    """grad_table [V, F] fp32 of tfg_embedding_lookup, for the groups of its ids
+    (tfg_group_ids with the same padding_id)."""
+    _need_cuda("grad_out", grad_out)
+    dev = grad_out.device
+    for name in ("rowptr", "sorted_ids", "perm"):
+        _need_cuda(name, getattr(groups, name), torch.int32, dev)
+    n, v = groups.perm.numel(), groups.rowptr.numel() - 1
+    f = grad_out.shape[-1]
+    if groups.sorted_ids.numel() != n or grad_out.numel() != n * f:
+        raise ValueError("grad_out must hold a row for every id of the groups")
+    out = _need_out("out", out, (v, f), torch.float32, dev)
+    workspace = _workspace(workspace, tfg_embedding_backward_workspace_size(f), dev)
+    _run(dev, lib().tfg_embedding_backward, _ptr(groups.rowptr), _ptr(groups.sorted_ids), _ptr(groups.perm),
+         _ptr(grad_out), _dtype_code(grad_out.dtype), n, v, f, float(scale), _ptr(out), _ptr(workspace),
+         workspace.numel(), _stream(dev))
+    return out
+
+
+class GroupNorm(NamedTuple):
+    out: torch.Tensor
+    mean: Optional[torch.Tensor]   # fp32 [G, K], for the backward
+    rstd: Optional[torch.Tensor]   # fp32 [G, K]
+    status: torch.Tensor           # int32 [1] (device)
+
+
+def tfg_group_norm_workspace_size(num_nodes: int, num_graphs: int, num_features: int, num_groups: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().tfg_group_norm_workspace_size(num_nodes, num_graphs, num_features, num_groups, ctypes.byref(n)))
+    return n.value
+
+
+def _norm_inputs(x, node_offsets, gamma, beta):
+    _need_cuda("x", x)
+    dev = x.device
+    if x.dim() != 2:
+        raise ValueError("x must have shape [N, F]")
+    n, f = x.shape
+    _need_cuda("node_offsets", node_offsets, torch.int64, dev)
+    if node_offsets.dim() != 1 or node_offsets.numel() < 1:
+        raise ValueError("node_offsets must have shape [G + 1]")
+    for name, w in (("gamma", gamma), ("beta", beta)):
+        if w is not None:
+            _need_cuda(name, w, torch.float32, dev)
+            if w.numel() != f:
+                raise ValueError(f"{name} must have {f} values")
+    return dev, n, f, node_offsets.numel() - 1
+
+
+def tfg_group_norm(x, node_offsets, num_groups: int, gamma=None, beta=None, eps: float = 1e-5, activation: str = "none",
+                   out_dtype: Optional[torch.dtype] = None, want_stats: bool = True, out=None,
+                   workspace=None) -> GroupNorm:
+    """Group norm over the graphs of a batch and an activation ("none", "relu", "silu",
+    "gelu").  Graph g holds the rows node_offsets[g] .. node_offsets[g + 1] - 1 of x
+    [N, F]; rows outside all graphs are left as they are in ``out`` (unset in a new one)."""
+    dev, n, f, g = _norm_inputs(x, node_offsets, gamma, beta)
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    out = _need_out("out", out, (n, f), out_dtype, dev)
+    workspace = _workspace(workspace, tfg_group_norm_workspace_size(n, g, f, num_groups), dev)
+    mean = rstd = None
+    if want_stats:
+        mean, rstd = torch.empty(2, g, num_groups, dtype=torch.float32, device=dev).unbind(0)
+    status = torch.empty(1, dtype=torch.int32, device=dev)
+    _run(dev, lib().tfg_group_norm, _ptr(x), _x_dtype(x), _ptr(node_offsets), n, g, f, num_groups, _ptr(gamma), _ptr(beta),
+         float(eps), ACTIVATIONS[activation], _ptr(out), _dtype_code(out_dtype), _ptr(mean), _ptr(rstd), _ptr(workspace),
+         workspace.numel(), _ptr(status), _stream(dev))
+    return GroupNorm(out, mean, rstd, status)
+
+
+def tfg_group_norm_backward_workspace_size(num_nodes: int, num_graphs: int, num_features: int, num_groups: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().tfg_group_norm_backward_workspace_size(num_nodes, num_graphs, num_features, num_groups,
+                                                        ctypes.byref(n)))
+    return n.value
+
+
+def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean, rstd, grad_out, activation: str = "none",
+                            want_weight_grads: bool = True, grad_x=None, workspace=None):
+    """Gradients of tfg_group_norm with the forward's arguments and statistics.  Returns
+    (grad_x [N, F] in grad_out's type, grad_gamma [F], grad_beta [F]); the last two None
+    without ``want_weight_grads``."""
+    dev, n, f, g = _norm_inputs(x, node_offsets, gamma, beta)
+    _need_cuda("grad_out", grad_out, None, dev)
+    if tuple(grad_out.shape) != (n, f):
+        raise ValueError("grad_out must have the shape of x")
+    for name, s in (("mean", mean), ("rstd", rstd)):
+        _need_cuda(name, s, torch.float32, dev)
+        if s.numel() != g * num_groups:
+            raise ValueError(f"{name} must have shape [G, num_groups]")
+    grad_x = _need_out("grad_x", grad_x, (n, f), grad_out.dtype, dev)
+    grad_gamma = grad_beta = None
+    if want_weight_grads:
+        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=dev).unbind(0)
+    workspace = _workspace(workspace, tfg_group_norm_backward_workspace_size(n, g, f, num_groups), dev)
+    _run(dev, lib().tfg_group_norm_backward, _ptr(x), _x_dtype(x), _ptr(node_offsets), n, g, f, num_groups, _ptr(gamma),
+         _ptr(beta), _ptr(mean), _ptr(rstd), ACTIVATIONS[activation], _ptr(grad_out), _dtype_code(grad_out.dtype),
+         _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta), _ptr(workspace), workspace.numel(), _stream(dev))
+    return grad_x, grad_gamma, grad_beta
+
+
+def tfg_global_norm_workspace_size(num_tensors: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().tfg_global_norm_workspace_size(num_tensors, ctypes.byref(n)))
+    return n.value
+
+
+_GRADIENT_TYPES = {torch.float32: TFG_F32, torch.bfloat16: TFG_BF16}
+
+
+def _tensor_list(name: str, tensors, dev):
+    """(pointers, sizes, type codes) of a list of contiguous tensors on one device, as the
+    host arrays that the C calls read."""
+    for t in tensors:
+        _need_cuda(name, t, None, dev)
+        if t.dtype not in _GRADIENT_TYPES:
+            raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return (array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", [t.numel() for t in tensors]),
+            array.array("i", [_GRADIENT_TYPES[t.dtype] for t in tensors]))
+
+
+def _host(a: array.array):
+    return ctypes.c_void_p(a.buffer_info()[0])
+
+
+def tfg_global_norm(tensors, workspace=None) -> torch.Tensor:
+    """sqrt of the sum of all squares over a list of tensors (fp32 or bf16), fp32 [1]."""
+    tensors = list(tensors)
+    dev = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
+    ptrs, sizes, codes = _tensor_list("tensors", tensors, dev)
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), dev)
+    _run(dev, lib().tfg_global_norm, len(tensors), _host(ptrs), _host(sizes), _host(codes), _ptr(norm), _ptr(workspace),
+         workspace.numel(), _stream(dev))
+    return norm
+
+
+def tfg_clip_by_global_norm(tensors, clip_norm: float, outs=None, workspace=None):
+    """tensors * clip_norm / max(global norm, clip_norm): new tensors, or ``outs`` (which may
+    be the tensors themselves, in place).  Returns (outs, norm [1] before clipping)."""
+    tensors = list(tensors)
+    dev = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
+    ptrs, sizes, codes = _tensor_list("tensors", tensors, dev)
+    outs = [torch.empty_like(t) for t in tensors] if outs is None else list(outs)
+    out_ptrs, out_sizes, out_codes = _tensor_list("outs", outs, dev)
+    if out_sizes != sizes or out_codes != codes:
+        raise ValueError("outs must have the sizes and types of tensors")
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), dev)
+    _run(dev, lib().tfg_clip_by_global_norm, len(tensors), _host(ptrs), _host(sizes), _host(codes), float(clip_norm),
+         _host(out_ptrs), _ptr(norm), _ptr(workspace), workspace.numel(), _stream(dev))
+    return outs, norm
