@@ -6,20 +6,19 @@
 // F channels fall into groups of C, and statistics are taken over the n_g * C values of
 // a (graph, group).
 //
-// Work split.  A team of threads (a warp, or a CTA) takes the rows of one graph and a
-// tile of channels -- whole groups -- at once: every thread keeps the vectors of one
-// column of the tile in registers, so that x is read from memory once although mean and
-// centred squares are two passes.  A graph of more rows than a team holds ("large") is
-// cut along a grid of row shares over all rows; the teams of its shares write partial
-// statistics, a second kernel joins them in a fixed order, and a third one reads the
-// shares again and applies them.  A share is no longer than what a team holds, so it
-// meets at most two large graphs: one that covers its first row (slot 0) and one that
-// begins behind it and runs past its end (slot 1).  Whether there are large graphs only
-// the device knows; the host leaves the two later kernels out where all rows together fit
-// a team.
+// Work split.  A team of threads (a warp, or a CTA) takes a graph and a tile of channels,
+// whole groups of them: the threads of a row read vectors side by side and step down the
+// rows, several rows of loads in flight.  A team reads its rows twice, for the sums and
+// to apply them; the second time they come from L1 or L2, which costs less than the
+// registers to hold them did (fewer resident teams: 110-row graphs, F = 128 fp32, 82 us
+// held, see group_norm.cu).  A graph of more than `most` rows ("large") is cut along a
+// grid of row shares over all rows; the teams of its shares write partial statistics, a
+// second kernel joins them in a fixed order, and a third one applies them, last share
+// first, whose rows L2 still holds.  A share is `most` rows long, so it meets at most two
+// large graphs: one that covers its first row (slot 0) and one that begins behind it and
+// runs past its end (slot 1).  Whether there are large graphs only the device knows; the
+// host leaves the two later kernels out where all rows together are at most `most`.
 #pragma once
-
-#include <cuda_bf16.h>
 
 #include "widen.cuh"
 
@@ -28,15 +27,15 @@ namespace {
 
 constexpr int kActNone = TFG_ACT_NONE, kActRelu = TFG_ACT_RELU, kActSilu = TFG_ACT_SILU, kActGelu = TFG_ACT_GELU;
 
-// Activations in fp32.  exp and erf are the CUDA math library's; the quotient of the
-// sigmoid is __fdividef (2 ulp; 0 where the divisor passes 2^126, where y e^y is below
-// 1e-36 anyway).  1 + erf leaves the gelu an absolute error of about |y| 2^-24 for
-// negative y.
-__device__ __forceinline__ float sigmoid_of(float y) { return __fdividef(1.f, 1.f + expf(-y)); }
+// Activations in fp32.  The sigmoid's exponential is __expf (2 ulp and |y| u: its relative
+// error, times |y| (1 - sigmoid) at most, stays below 3 u of max(|y|, 1)) and its quotient
+// __fdividef (2 ulp; 0 where the divisor passes 2^126, where y e^y is below 1e-36 anyway).
+// 1 + erf leaves the gelu an absolute error of about |y| u for negative y.
+__device__ __forceinline__ float sigmoid_of(float y) { return __fdividef(1.f, 1.f + __expf(-y)); }
 template <int ACT>
 __device__ __forceinline__ float activate(float y) {
     if constexpr (ACT == kActRelu) return y <= 0.f ? 0.f : y;      // a NaN stays
-    else if constexpr (ACT == kActSilu) return __fdividef(y, 1.f + expf(-y));
+    else if constexpr (ACT == kActSilu) return __fdividef(y, 1.f + __expf(-y));
     else if constexpr (ACT == kActGelu) return 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
     else return y;
 }
@@ -47,7 +46,7 @@ __device__ __forceinline__ float activation_slope(float y) {
         const float p = sigmoid_of(y);
         return p * fmaf(y, 1.f - p, 1.f);
     } else if constexpr (ACT == kActGelu) {
-        const float d = 0.39894228040143268f * expf(-0.5f * y * y);
+        const float d = 0.39894228040143268f * __expf(-0.5f * y * y);
         return fmaf(y, d, 0.5f * (1.f + erff(y * 0.70710678118654752f)));
     } else return 1.f;
 }
@@ -56,19 +55,22 @@ __device__ __forceinline__ float activation_slope(float y) {
 struct NormPlan {
     int vec;              // values of a thread's vector
     int team;             // threads of a team
-    int held;             // vectors a thread holds
     int row_vecs;         // vectors of a tile's row
     int cols;             // channels of a tile
     int tiles;
-    int rows_at_once;     // rows a team reads at once
-    int64_t cap;          // rows a team holds
-    int64_t share;        // rows of a share, at most cap
+    int rows_at_once;     // rows a team reads side by side
+    int lanes;            // vectors of a group (1 where a vector holds several groups)
+    bool shuffles;        // groups and rows are powers of two of lanes: sums by lane exchanges
+    int64_t most;         // rows of a share, and of a graph that is not large
     int64_t shares;       // 0: no graph can be large
 };
 
-constexpr int kNormTeamThreads = 128;             // threads of a CTA of warp teams
-// Resident CTAs asked for: 128 registers a thread (64 in teams of 1,024).
-constexpr int team_ctas(int team) { return team == 1024 ? 1 : (team == 256 ? 2 : 4); }
+// The rows of a large graph that share s holds in a slot, written by the first kernel.
+struct alignas(16) Piece {
+    int64_t a, b;         // rows, a == b: none
+    int64_t graph;
+    int64_t first_share;  // the share in which the graph begins
+};
 
 struct NormArgs {
     const void *x;
@@ -81,9 +83,10 @@ struct NormArgs {
     int32_t *status;
     void *out;
     const void *g;                                // backward: dL/dout
+    const float *mean_in, *rstd_in;               // backward: the forward's statistics
+    Piece *pieces;                                // [share][slot]
     float2 *part;                                 // [share][slot][group]
     float2 *joined;                               // [share of the graph's first row][group]
-    const float *mean_in, *rstd_in;               // backward: the forward's statistics
     float2 *channel_part;                         // backward: [chain][F], sums for gamma and beta
     int64_t chains;                               // backward: teams a tile's units are dealt to
     NormPlan p;
@@ -121,35 +124,44 @@ __device__ __forceinline__ int64_t warp_graph_at(const int64_t *offsets, int64_t
     return lo;
 }
 
-// The piece of a large graph that share s holds in a slot; empty if there is none.
-struct Piece {
-    int64_t a, b;         // rows
-    int64_t graph, first_share;
-    bool begins;          // the graph's first row is here
-};
-__device__ __forceinline__ Piece share_piece(const NormArgs &a, int64_t s, int slot) {
-    const int64_t r0 = s * a.p.share, r1 = min64(a.n, r0 + a.p.share);
-    Piece p{0, 0, 0, 0, false};
+__device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int slot) {
+    const int64_t r0 = s * a.p.most, r1 = min64(a.n, r0 + a.p.most);
+    Piece p{0, 0, 0, 0};
     const int64_t g = warp_graph_at(a.offsets, a.graphs, slot == 0 ? r0 : r1 - 1);
     if (g < 0) return p;
     bool bad;
     const RowRange r = graph_rows(a.offsets, g, a.n, bad);
-    if (r.b - r.a <= a.p.cap || r.b <= r0 || (slot == 1) != (r.a > r0)) return p;
+    if (r.b - r.a <= a.p.most || r.b <= r0 || (slot == 1) != (r.a > r0)) return p;
     p.a = r.a > r0 ? r.a : r0;
     p.b = r.b < r1 ? r.b : r1;
     if (p.b < p.a) p.b = p.a;
     p.graph = g;
-    p.first_share = r.a / a.p.share;
-    p.begins = r.a >= r0;
+    p.first_share = r.a / a.p.most;
     return p;
 }
 
+// The slot of share s that holds a piece of the graph whose first row is a.
+__device__ __forceinline__ int64_t slot_at(const NormArgs &p, int64_t a, int64_t s) {
+    return s * 2 + (a > s * p.p.most ? 1 : 0);
+}
+
 // ---- a team -------------------------------------------------------------------------
-// TT threads: a warp of its own shared memory in a CTA of four, or a whole CTA.
+// TT threads: a warp in a CTA of four, each with shared memory of its own, or a whole CTA.
+constexpr int kWarpTeams = 4;
+// Resident threads asked for, forward and backward: 80 and 128 registers a thread (64 in
+// teams of 1,024).
+#ifndef TFG_NORM_RESIDENT
+#define TFG_NORM_RESIDENT 768
+#endif
+#ifndef TFG_BACK_RESIDENT
+#define TFG_BACK_RESIDENT 512
+#endif
+constexpr int team_ctas(int team, int threads) { return team == 1024 ? 1 : threads / (team == 256 ? 256 : 128); }
 template <int TT>
 struct Team {
-    static constexpr int kPerCta = TT == 32 ? kNormTeamThreads / 32 : 1;
+    static constexpr int kPerCta = TT == 32 ? kWarpTeams : 1;
     static constexpr int kThreads = TT * kPerCta;
+    static constexpr int kWarps = TT / 32;
     static __device__ __forceinline__ int index() { return TT == 32 ? threadIdx.x / 32 : 0; }
     static __device__ __forceinline__ int thread() { return TT == 32 ? threadIdx.x & 31 : threadIdx.x; }
     static __device__ __forceinline__ void sync() {
@@ -158,52 +170,119 @@ struct Team {
     }
 };
 
-// Shared memory of a team: sums of the row lanes, of the channels, of the groups, each for
-// NS sums.
-template <int NS>
-__host__ __device__ constexpr int team_floats(int rows_at_once, int cols) {
-    return NS * (rows_at_once * cols + 2 * cols);
-}
-
-// Place of a thread in its team's tile.
-template <int TT, int VEC>
+// Place of a thread in its team's tile.  S: sums a thread keeps per quantity, one where
+// its vector lies in one group, else one a channel.
+template <int TT, int VEC, int S>
 struct Place {
     int sub, rl;          // vector of the row, row
     int64_t c0;           // first channel
     bool on;
-    int groups, group0;   // whole groups of the tile
-    int grp[VEC];         // the channels' groups, relative to the tile's first
+    int group0;           // first group of the tile
+    int groups;           // whole groups of the tile
+    int grp[S];           // the groups of the sums, relative to the tile's first
 
     __device__ __forceinline__ Place(const NormArgs &a, int tile) {
         const int t = Team<TT>::thread();
         rl = t / a.p.row_vecs;
         sub = t - rl * a.p.row_vecs;
-        c0 = static_cast<int64_t>(tile) * a.p.cols + sub * VEC;
+        const int64_t first = static_cast<int64_t>(tile) * a.p.cols;
+        c0 = first + sub * VEC;
         on = rl < a.p.rows_at_once && c0 < a.f;
-        group0 = static_cast<int>(static_cast<int64_t>(tile) * a.p.cols / a.c);
-        const int64_t left = a.f - static_cast<int64_t>(tile) * a.p.cols;
-        groups = static_cast<int>(min64(a.p.cols, left) / a.c);
+        group0 = static_cast<int>(first / a.c);
+        groups = static_cast<int>(min64(a.p.cols, a.f - first)) / a.c;
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) grp[q] = on ? (sub * VEC + q) / a.c : 0;
+        for (int q = 0; q < S; ++q) grp[q] = on ? (sub * VEC + q) / a.c : 0;
+    }
+    // rows of [a, b) that this thread visits: a + rl, a + rl + rows_at_once, ...
+    __device__ __forceinline__ int rows(const NormArgs &p, int64_t a, int64_t b) const {
+        const int left = static_cast<int>(b - a) - rl;
+        return on && left > 0 ? (left + p.p.rows_at_once - 1) / p.p.rows_at_once : 0;
+    }
+    // whether sum q is the one that writes its group's statistics
+    __device__ __forceinline__ bool writes(const NormArgs &a, int q) const {
+        return on && rl == 0 && (sub * VEC + q) % a.c == 0;
     }
 };
 
-// Sums over the rows of the tile: v[s] holds this thread's sums of its channels, the
-// returned array s the team's of every channel.  Collective over the team, which has to
-// pass a barrier before the next sums overwrite these.
-template <int TT, int VEC, int NS>
-__device__ __forceinline__ void channel_sums(const NormArgs &a, const Place<TT, VEC> &at, const float (&v)[NS][VEC],
-                                             float *smem, float *(&chan)[NS]) {
+// Floats of a team's shared memory for NS quantities, two buffers of the exchange.
+template <int NS>
+__host__ __device__ inline int team_floats(const NormPlan &p, int sums) {
+    return p.shuffles ? (p.team > 32 ? 2 * NS * sums * p.team : 0) : NS * (p.rows_at_once + 2) * p.cols;
+}
+
+// The same for the backward, whose channel sums take two floats per column of the team.
+__host__ __device__ inline int back_floats(const NormPlan &p, int sums, int vec) {
+    const int groups = team_floats<2>(p, sums), channels = 2 * p.team * vec;
+    return groups > channels ? groups : channels;
+}
+
+// Sums of v[s][q] over the rows and the channels of each group of the tile, to every thread
+// for its own groups.  Collective over the team.  By lane exchanges and one barrier where
+// group and row are powers of two (buffer: alternates from call to call, so that the next
+// call's barrier separates this one's reads from the writes after it), else through
+// per-channel sums in shared memory.
+template <int TT, int VEC, int S, int NS>
+__device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VEC, S> &at, float (&v)[NS][S], float *smem,
+                                           int buffer) {
     using M = Team<TT>;
     const int t = M::thread();
+    if (a.p.shuffles) {
+        if (S > 1) {                                        // channels of a group in this vector
+#pragma unroll
+            for (int o = 1; o < S; o <<= 1) {
+                if (o >= a.c) break;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    float w[S];
+#pragma unroll
+                    for (int q = 0; q < S; ++q) w[q] = v[s][q] + v[s][q ^ o];
+#pragma unroll
+                    for (int q = 0; q < S; ++q) v[s][q] = w[q];
+                }
+            }
+        }
+        const int in_group = a.p.lanes < 32 ? a.p.lanes : 32, in_row = a.p.row_vecs < 32 ? a.p.row_vecs : 32;
+        for (int o = 1; o < in_group; o <<= 1)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int q = 0; q < S; ++q) v[s][q] += lane_xor(v[s][q], o);
+        for (int o = in_row; o < 32; o <<= 1)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int q = 0; q < S; ++q) v[s][q] += lane_xor(v[s][q], o);
+        if constexpr (TT > 32) {
+            const int lane = t & 31, warp = t >> 5;
+            float *to = smem + buffer * NS * S * TT;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int q = 0; q < S; ++q) to[(s * S + q) * TT + t] = v[s][q];
+            M::sync();
+            // warps that hold other rows of this warp's columns, or other columns of its group
+            const int wide = a.p.row_vecs > 32 ? a.p.row_vecs / 32 : 1, span = a.p.lanes > 32 ? a.p.lanes / 32 : 1;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int q = 0; q < S; ++q) {
+                    float r = 0.f;
+#pragma unroll
+                    for (int w = 0; w < M::kWarps; ++w)
+                        if (w % wide / span == warp % wide / span) r += to[(s * S + q) * TT + w * 32 + lane];
+                    v[s][q] = r;
+                }
+        }
+        return;
+    }
     const int cols = a.p.cols, rows = a.p.rows_at_once;
+    M::sync();                                              // the last sums have been read
+    if (t < rows * a.p.row_vecs) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        float *red = smem + s * (rows + 2) * cols;
-        chan[s] = red + rows * cols;
-        if (t < rows * a.p.row_vecs) {
+        for (int s = 0; s < NS; ++s) {
+            float *red = smem + s * (rows + 2) * cols + at.rl * cols + at.sub * VEC;
 #pragma unroll
-            for (int q = 0; q < VEC; ++q) red[at.rl * cols + at.sub * VEC + q] = at.on ? v[s][q] : 0.f;
+            for (int q = 0; q < VEC; ++q) red[q] = S == 1 ? (q == 0 ? v[s][0] : 0.f) : v[s][S == 1 ? 0 : q];
         }
     }
     M::sync();
@@ -213,98 +292,84 @@ __device__ __forceinline__ void channel_sums(const NormArgs &a, const Place<TT, 
             const float *red = smem + s * (rows + 2) * cols + i;
             float r = 0.f;
             for (int j = 0; j < rows; ++j) r += red[j * cols];
-            chan[s][i] = r;
+            smem[s * (rows + 2) * cols + rows * cols + i] = r;
         }
     }
     M::sync();
-}
-
-// The same summed over the channels of every group: total[s][k] of the tile's group k.
-template <int TT, int VEC, int NS>
-__device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VEC> &at, const float (&v)[NS][VEC],
-                                           float *smem, float *(&total)[NS]) {
-    using M = Team<TT>;
-    const int t = M::thread();
-    float *chan[NS];
-    channel_sums<TT, VEC, NS>(a, at, v, smem, chan);
-    int width = 1;        // lanes of a group
+    int width = 1;                                          // lanes of a group
     while (width < a.c && width < 32) width <<= 1;
     for (int k0 = 0; k0 < at.groups; k0 += TT / width) {
         const int k = k0 + t / width, l = t & (width - 1);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            total[s] = chan[s] + a.p.cols;
+            float *chan = smem + s * (rows + 2) * cols + rows * cols;
             float r = 0.f;
             if (k < at.groups)
-                for (int i = l; i < a.c; i += width) r += chan[s][k * a.c + i];
+                for (int i = l; i < a.c; i += width) r += chan[k * a.c + i];
             for (int o = width >> 1; o > 0; o >>= 1) r += lane_xor(r, o);
-            if (k < at.groups && l == 0) total[s][k] = r;
+            if (k < at.groups && l == 0) chan[cols + k] = r;
         }
     }
     M::sync();
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int q = 0; q < S; ++q) v[s][q] = smem[s * (rows + 2) * cols + (rows + 1) * cols + at.grp[q]];
 }
 
 // ---- host ---------------------------------------------------------------------------
 int64_t gcd64(int64_t a, int64_t b) { return b == 0 ? a : gcd64(b, a % b); }
+bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
 
-constexpr int64_t kNormCtasWanted = 912;          // six a multiprocessor
-
-// Vectors that a thread holds of x, and in the backward of the gradient as well: what 128
-// registers a thread (64 in teams of 1,024) have room for beside the sums.
-constexpr int held_vectors(int team, int vec, bool backward) {
-    if (vec > 1) return backward ? 8 : 12;
-    return (backward ? 16 : 32) / (team == 1024 ? 2 : 1);
+// The longest vector, of at most `widest` values, that rows, pointers and groups allow: 8
+// values only where they lie in one group (sums of 8 channels a thread spill), 4 where a
+// tile of whole groups and whole vectors fits a team of 256.
+int norm_vec(int64_t f, int64_t c, int widest, bool aligned) {
+    if (widest == 8 && aligned && c % 8 == 0) return 8;
+    return widest >= 4 && aligned && f % 4 == 0 && c / gcd64(c, 4) <= 256 ? 4 : 1;
 }
 
-// Vectors of elem bytes where rows, pointers and groups allow them: a tile of whole groups
-// and whole vectors must fit a team of 256.
-int norm_vec(int64_t f, int64_t c, int vec, bool aligned) {
-    return aligned && f % vec == 0 && c / gcd64(c, vec) <= 256 ? vec : 1;
-}
+#ifndef TFG_NORM_VECS
+#define TFG_NORM_VECS 8
+#endif
+#ifndef TFG_NORM_TEAMS
+#define TFG_NORM_TEAMS 1216
+#endif
+constexpr int kVectorsAThread = TFG_NORM_VECS;    // of a mean graph
+constexpr int64_t kShareTeams = TFG_NORM_TEAMS;
 
-// A tile is the fewest whole groups and whole vectors of 128 bytes or more; the smallest
-// team that holds twice the mean graph takes it, and the tile is widened while that stays
-// so.  Graphs no team holds are read in shares by the largest team.
-NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int elem, bool backward) {
+// Tiles of whole groups and whole vectors: 32 vectors of a row, fewer (8 at least) as long
+// as the mean graphs leave multiprocessors without a team.  The team: kVectorsAThread
+// vectors of a mean graph to a thread, or 256 threads on shares of large ones.
+NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec) {
     NormPlan p{};
     p.vec = vec;
     const int64_t unit = c / gcd64(c, vec);                     // vectors of the smallest tile
     const int64_t row = f / vec;
     const int64_t mean = graphs > 0 ? (n + graphs - 1) / graphs : 0;
+    p.lanes = static_cast<int>(c > vec ? unit : 1);
+    p.shuffles = power_of_two(c);                               // c a multiple or a divisor of vec then
     int64_t w = unit;
-    while (w < row && w * vec * elem < 128) w += unit;
-    const int teams[] = {32, 128, 256};
-    auto holds = [&](int64_t vecs, int team) {
-        return vecs <= team && held_vectors(team, vec, backward) * (team / vecs) >= 2 * mean;
-    };
-    p.team = 0;
-    for (int t : teams) {
-        if (holds(w, t)) {
-            p.team = t;
-            break;
-        }
-    }
-    if (p.team) {
-        while (w + unit <= row && holds(w + unit, p.team)) w += unit;
+    auto threads = [&](int64_t rows, int64_t vecs) { return (rows * vecs + kVectorsAThread - 1) / kVectorsAThread; };
+    if (p.shuffles) {
+        while (w < row && w < 32) w <<= 1;
+        while (w > unit && w > 8 && threads(n, row) / 128 < 2 * 152 && threads(mean, w) > 32) w >>= 1;
     } else {
-        p.team = w <= 256 ? 256 : 1024;
-        while (w + unit <= row && w + unit <= 64) w += unit;    // rows of up to 1 KB at once
+        while (w + unit <= row && w + unit <= 32) w += unit;
     }
-    p.held = held_vectors(p.team, vec, backward);
     p.row_vecs = static_cast<int>(w);
     p.cols = static_cast<int>(w * vec);
     p.tiles = static_cast<int>((f + p.cols - 1) / p.cols);
+    const int64_t t = threads(mean, w);
+    p.team = t <= 32 && w <= 32 ? 32 : (t <= 128 && w <= 128 ? 128 : 256);
+    if (w > 256) p.team = 1024;
     p.rows_at_once = p.team / p.row_vecs;
-    p.cap = int64_t(p.held) * p.rows_at_once;
-    if (n <= p.cap) {
-        p.share = p.cap;
-        p.shares = 0;
-        return p;
-    }
-    int64_t share = (n * p.tiles + kNormCtasWanted - 1) / kNormCtasWanted;
-    share = (share + p.rows_at_once - 1) / p.rows_at_once * p.rows_at_once;
-    p.share = share < p.cap ? share : p.cap;
-    p.shares = (n + p.share - 1) / p.share;
+    // a share: an equal part of all rows for every resident team, no less than a team is made for
+    int64_t most = (n * p.tiles + kShareTeams - 1) / kShareTeams;
+    const int64_t least = int64_t(p.rows_at_once) * kVectorsAThread;
+    if (most < least) most = least;
+    p.most = most;
+    p.shares = n <= most ? 0 : (n + most - 1) / most;
     return p;
 }
 
