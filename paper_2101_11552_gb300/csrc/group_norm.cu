@@ -31,8 +31,9 @@ __device__ __forceinline__ void merge(Running<S> &r, const typename VecLoad<XT, 
     float m[S] = {}, sq[S] = {};
 #pragma unroll
     for (int u = 0; u < kDepth; ++u) {
+        if (!FULL && u >= rows) break;
         float v[VEC];
-        VecLoad<XT, VEC>::widen(raw[u], v);                 // zeros behind the last row
+        VecLoad<XT, VEC>::widen(raw[u], v);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) m[q / kPer] += v[q];
     }
@@ -78,7 +79,8 @@ __device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VE
     if (i < rows) {
         typename V::Raw raw[kDepth];
 #pragma unroll
-        for (int u = 0; u < kDepth; ++u) raw[u] = i + u < rows ? V::raw(x + u * step) : V::zero();
+        for (int u = 0; u < kDepth; ++u)
+            if (i + u < rows) raw[u] = V::raw(x + u * step);
         merge<false, XT, VEC, S>(r, raw, rows - i);
     }
     const float count = static_cast<float>((b - a) * p.c);
@@ -104,11 +106,12 @@ __device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S>
     constexpr int kPer = VEC / S;
     const int rows = at.rows(p, a, b);
     if (rows == 0) return;
+    const float *gamma = p.gamma, *beta = p.beta;
     float scale[VEC], shift[VEC];
 #pragma unroll
     for (int q = 0; q < VEC; ++q) {
-        scale[q] = p.gamma ? __ldg(p.gamma + at.c0 + q) * r[q / kPer] : r[q / kPer];
-        shift[q] = p.beta ? __ldg(p.beta + at.c0 + q) : 0.f;
+        scale[q] = gamma ? __ldg(gamma + at.c0 + q) * r[q / kPer] : r[q / kPer];
+        shift[q] = beta ? __ldg(beta + at.c0 + q) : 0.f;
     }
     const int64_t first = (a + at.rl) * p.f + at.c0, step = p.p.rows_at_once * p.f;
     const XT *x = static_cast<const XT *>(p.x) + first;
@@ -153,140 +156,161 @@ template <int TT, typename XT, int VEC, int S>
 __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_NORM_RESIDENT)) norm_units(NormArgs p, int act, bool out_bf16) {
     using M = Team<TT>;
     extern __shared__ __align__(16) float s_all[];
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * M::kPerCta + M::index();
-    const int64_t unit = id / p.p.tiles;
-    const int tile = static_cast<int>(id - unit * p.p.tiles);
+    if (p.status_all && blockIdx.x == gridDim.x - 1) return check_offsets(p);
+    const uint32_t id = blockIdx.x * M::kPerCta + M::index();
+    const int64_t unit = id / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(id - static_cast<uint32_t>(unit) * p.p.tiles);
     if (unit >= p.graphs + 2 * p.p.shares) return;          // whole teams
     float *smem = s_all + M::index() * team_floats<1>(p.p, S);
     const Place<TT, VEC, S> at(p, tile);
     float mean[S], squares[S];
     const int t = M::thread();
-    if (unit < p.graphs) {
+    const int64_t slot = unit - p.graphs;                   // 2 * share + slot
+    RowRange r;
+    if (slot < 0) {
         bool bad;
-        const RowRange r = graph_rows(p.offsets, unit, p.n, bad);
+        r = graph_rows(p.offsets, unit, p.n, bad);
         if (bad && tile == 0 && t == 0) set_status(p.status, TFG_ERR_INDEX_RANGE);
         if (r.b - r.a > p.p.most) return;                   // large: the shares'
-        const int64_t out0 = unit * p.groups + at.group0;
-        if (r.a == r.b) {                                   // an empty graph has no statistics: zeros
-            for (int k = t; k < at.groups; k += TT) {
-                if (p.mean) p.mean[out0 + k] = 0.f;
-                if (p.rstd) p.rstd[out0 + k] = 0.f;
-            }
-            return;
+    } else {
+        const Piece piece = find_piece(p, slot >> 1, slot & 1);
+        if (tile == 0 && t == 0) p.pieces[slot] = piece;
+        if (piece.a == piece.b) return;
+        r = {piece.a, piece.b};
+    }
+    const int64_t out0 = unit * p.groups + at.group0;
+    if (r.a == r.b) {                                       // an empty graph has no statistics: zeros
+        for (int k = t; k < at.groups; k += TT) {
+            if (p.mean) p.mean[out0 + k] = 0.f;
+            if (p.rstd) p.rstd[out0 + k] = 0.f;
         }
-        statistics<TT, XT>(p, at, r.a, r.b, smem, mean, squares);
-        const float count = static_cast<float>((r.b - r.a) * p.c);
-        float rstd[S];
-#pragma unroll
-        for (int q = 0; q < S; ++q) {
-            rstd[q] = 1.f / sqrtf(squares[q] / count + p.eps);
-            if (p.mean && at.writes(p, q)) {
-                p.mean[out0 + at.grp[q]] = mean[q];
-                p.rstd[out0 + at.grp[q]] = rstd[q];
-            }
-        }
-        apply_act<XT>(p, at, r.a, r.b, act, out_bf16, mean, rstd);
         return;
     }
-    const int64_t slot = unit - p.graphs;                   // 2 * share + slot
-    const Piece piece = find_piece(p, slot >> 1, slot & 1);
-    if (tile == 0 && t == 0) p.pieces[slot] = piece;
-    if (piece.a == piece.b) return;
-    statistics<TT, XT>(p, at, piece.a, piece.b, smem, mean, squares);
+    statistics<TT, XT>(p, at, r.a, r.b, smem, mean, squares);
+    if (slot >= 0) {
 #pragma unroll
-    for (int q = 0; q < S; ++q)
-        if (at.writes(p, q)) p.part[slot * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
+        for (int q = 0; q < S; ++q)
+            if (at.writes(p, q)) p.part[slot * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
+        return;
+    }
+    const float count = static_cast<float>((r.b - r.a) * p.c);
+    float rstd[S];
+#pragma unroll
+    for (int q = 0; q < S; ++q) {
+        rstd[q] = 1.f / sqrtf(squares[q] / count + p.eps);
+        if (p.mean && at.writes(p, q)) {
+            p.mean[out0 + at.grp[q]] = mean[q];
+            p.rstd[out0 + at.grp[q]] = rstd[q];
+        }
+    }
+    apply_act<XT>(p, at, r.a, r.b, act, out_bf16, mean, rstd);
 }
 
-// Joins the pieces of the large graph that begins in share blockIdx.x, a warp a group:
-// the mean of the pieces' means, then their squares about it, each in a fixed order.
+// Joins the pieces of a large graph (rows r, from share s on) for group k, by a warp: the
+// mean of the pieces' means, then their squares about it, each in a fixed order.
+__device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
+    const int lane = threadIdx.x & 31;
+    const int64_t s1 = (r.b - 1) / p.p.share;
+    const float all = static_cast<float>((r.b - r.a) * p.c);
+    auto part = [&](int64_t i) { return p.part[slot_at(p, r.a, i) * p.groups + k]; };
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x, piece_values(p, r, i), sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += lane_xor(sum, o);
+    const float mean = sum / all;
+    float squares = 0.f;
+#pragma unroll 4
+    for (int64_t i = s + lane; i <= s1; i += 32) {
+        const float2 v = part(i);
+        squares += fmaf((v.x - mean) * piece_values(p, r, i), v.x - mean, v.y);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) squares += lane_xor(squares, o);
+    return make_float2(mean, 1.f / sqrtf(squares / all + p.eps));
+}
+
+// join_apart: the large graph that begins in share blockIdx.x, a warp a group.
 constexpr int kJoinWarps = 4;
 __global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t s = blockIdx.x;
     Piece piece = p.pieces[s * 2];
     if (piece.a == piece.b || piece.first_share != s) piece = p.pieces[s * 2 + 1];
     if (piece.a == piece.b || piece.first_share != s) return;
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
-    const int64_t s1 = (r.b - 1) / p.p.most;
-    const float all = static_cast<float>((r.b - r.a) * p.c);
-    auto values = [&](int64_t i) {                          // values of the piece in share i
-        const int64_t a = i * p.p.most, b = a + p.p.most;
-        return static_cast<float>(((b < r.b ? b : r.b) - (a > r.a ? a : r.a)) * p.c);
-    };
-    for (int k = blockIdx.y * kJoinWarps + warp; k < p.groups; k += gridDim.y * kJoinWarps) {
-        auto part = [&](int64_t i) { return p.part[slot_at(p, r.a, i) * p.groups + k]; };
-        float sum = 0.f;
-        for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x, values(i), sum);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += lane_xor(sum, o);
-        const float mean = sum / all;
-        float squares = 0.f;
-        for (int64_t i = s + lane; i <= s1; i += 32) {
-            const float2 v = part(i);
-            squares += fmaf((v.x - mean) * values(i), v.x - mean, v.y);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) squares += lane_xor(squares, o);
-        const float rstd = 1.f / sqrtf(squares / all + p.eps);
-        if (lane == 0) {
-            p.joined[s * p.groups + k] = make_float2(mean, rstd);
-            if (p.mean) {
-                p.mean[piece.graph * p.groups + k] = mean;
-                p.rstd[piece.graph * p.groups + k] = rstd;
-            }
-        }
+    for (int k = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kJoinWarps) {
+        const float2 v = join(p, r, s, k);
+        if ((threadIdx.x & 31) == 0) p.joined[s * p.groups + k] = v;
     }
 }
 
-// The shares' large pieces once more: last share first, whose rows L2 still holds.
+// The pieces of large graphs once more, a CTA a (slot, tile), the last slot first.
 template <int TT, typename XT, int VEC, int S>
-__global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_NORM_RESIDENT)) norm_apply(NormArgs p, int act, bool out_bf16) {
-    using M = Team<TT>;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * M::kPerCta + M::index();
-    const int64_t back = id / p.p.tiles;
-    const int tile = static_cast<int>(id - back * p.p.tiles);
-    if (back >= 2 * p.p.shares) return;
+__global__ void __launch_bounds__(TT, team_ctas(TT, TFG_NORM_RESIDENT)) norm_large(NormArgs p, int act, bool out_bf16) {
+    extern __shared__ __align__(16) float s_all[];
+    float2 *s_stat = reinterpret_cast<float2 *>(s_all);    // [tile's groups]
+    const int64_t back = blockIdx.x / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(blockIdx.x - static_cast<uint32_t>(back) * p.p.tiles);
     const Piece piece = p.pieces[2 * p.p.shares - 1 - back];
     if (piece.a == piece.b) return;
     const Place<TT, VEC, S> at(p, tile);
+    joined_statistics<TT>(p, at, piece, s_stat, join);
     float mean[S], rstd[S];
 #pragma unroll
     for (int q = 0; q < S; ++q) {
-        const float2 j = at.on ? __ldg(p.joined + piece.first_share * p.groups + at.group0 + at.grp[q]) : make_float2(0.f, 0.f);
-        mean[q] = j.x;
-        rstd[q] = j.y;
+        const float2 v = s_stat[at.grp[q]];
+        mean[q] = v.x;
+        rstd[q] = v.y;
+    }
+    // the share in which the graph begins reports its statistics
+    if (p.mean && piece.a < (piece.first_share + 1) * p.p.share) {
+        const int64_t out0 = piece.graph * p.groups + at.group0;
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            if (!at.writes(p, q)) continue;
+            p.mean[out0 + at.grp[q]] = mean[q];
+            p.rstd[out0 + at.grp[q]] = rstd[q];
+        }
     }
     apply_act<XT>(p, at, piece.a, piece.b, act, out_bf16, mean, rstd);
 }
 
 template <int TT, typename XT, int VEC, int S>
-cudaError_t launch_norm(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
+cudaError_t launch_units(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
     using M = Team<TT>;
     const int smem = M::kPerCta * team_floats<1>(p.p, S) * static_cast<int>(sizeof(float));
-    auto ctas = [](int64_t teams) { return static_cast<unsigned>((teams + M::kPerCta - 1) / M::kPerCta); };
-    norm_units<TT, XT, VEC, S><<<ctas((p.graphs + 2 * p.p.shares) * p.p.tiles), M::kThreads, smem, s>>>(p, act, out_bf16);
-    cudaError_t err = cudaGetLastError();
-    if (err != cudaSuccess || p.p.shares == 0) return err;
-    const dim3 join(static_cast<unsigned>(p.p.shares), static_cast<unsigned>(min64((p.groups + kJoinWarps - 1) / kJoinWarps, 65535)));
-    norm_join<<<join, kJoinWarps * 32, 0, s>>>(p);
-    err = cudaGetLastError();
-    if (err != cudaSuccess) return err;
-    norm_apply<TT, XT, VEC, S><<<ctas(2 * p.p.shares * p.p.tiles), M::kThreads, 0, s>>>(p, act, out_bf16);
+    const int64_t teams = (p.graphs + 2 * p.p.shares) * p.p.tiles;
+    const int64_t ctas = (teams + M::kPerCta - 1) / M::kPerCta + (p.status_all ? 1 : 0);
+    norm_units<TT, XT, VEC, S><<<static_cast<unsigned>(ctas), M::kThreads, smem, s>>>(p, act, out_bf16);
+    return cudaGetLastError();
+}
+
+template <int TT, typename XT, int VEC, int S>
+cudaError_t launch_large(NormArgs p, int act, bool out_bf16, cudaStream_t s) {
+    if (p.p.join_apart) {
+        const dim3 grid(static_cast<unsigned>(p.p.shares), static_cast<unsigned>(min64((p.groups + kJoinWarps - 1) / kJoinWarps, 65535)));
+        norm_join<<<grid, kJoinWarps * 32, 0, s>>>(p);
+        const cudaError_t err = cudaGetLastError();
+        if (err != cudaSuccess) return err;
+    }
+    p.p.rows_at_once = TT / p.p.row_vecs;
+    const int smem = p.p.tile_groups * static_cast<int>(sizeof(float2));
+    norm_large<TT, XT, VEC, S><<<static_cast<unsigned>(2 * p.p.shares * p.p.tiles), TT, smem, s>>>(p, act, out_bf16);
     return cudaGetLastError();
 }
 
 template <typename XT, int VEC, int S>
 cudaError_t launch_team(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
-    if constexpr (VEC == 1) {
-        if (p.p.team == 1024) return launch_norm<1024, XT, VEC, S>(p, act, out_bf16, s);
-    }
-    switch (p.p.team) {
-        case 32: return launch_norm<32, XT, VEC, S>(p, act, out_bf16, s);
-        case 128: return launch_norm<128, XT, VEC, S>(p, act, out_bf16, s);
-        default: return launch_norm<256, XT, VEC, S>(p, act, out_bf16, s);
-    }
+    const bool widest = VEC == 1 && p.p.team == 1024;
+    cudaError_t err;
+    if (widest) err = launch_units<VEC == 1 ? 1024 : 256, XT, VEC, S>(p, act, out_bf16, s);
+    else if (p.p.team == 32) err = launch_units<32, XT, VEC, S>(p, act, out_bf16, s);
+    else if (p.p.team == 128) err = launch_units<128, XT, VEC, S>(p, act, out_bf16, s);
+    else err = launch_units<256, XT, VEC, S>(p, act, out_bf16, s);
+    if (err != cudaSuccess || p.p.shares == 0) return err;
+    return widest ? launch_large<VEC == 1 ? 1024 : 256, XT, VEC, S>(p, act, out_bf16, s)
+                  : launch_large<kLargeTeam, XT, VEC, S>(p, act, out_bf16, s);
 }
 
 // S = 1 where a vector lies in one group.
@@ -326,8 +350,10 @@ size_t group_norm_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t 
 cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets, int64_t n, int64_t graphs, int64_t f,
                               int64_t groups, const float *gamma, const float *beta, float eps, int act, void *out,
                               int out_dtype, float *mean, float *rstd, void *ws, int32_t *status, cudaStream_t s) {
-    const cudaError_t err = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
-    if (err != cudaSuccess || graphs == 0) return err;
+    if (graphs == 0 || graphs > kStatusGraphs) {
+        const cudaError_t err = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
+        if (err != cudaSuccess || graphs == 0) return err;
+    }
     const bool aligned = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
     const int64_t c = f / groups;
     const int vec = norm_vec(f, c, x_dtype == TFG_BF16 ? 8 : 4, aligned);
@@ -344,7 +370,7 @@ cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets
     p.eps = eps;
     p.mean = mean;
     p.rstd = rstd;
-    p.status = status;
+    (graphs > kStatusGraphs ? p.status : p.status_all) = status;
     p.out = out;
     p.p = norm_plan(n, graphs, f, c, vec);
     p.pieces = static_cast<Piece *>(ws);

@@ -10,14 +10,15 @@
 // whole groups of them: the threads of a row read vectors side by side and step down the
 // rows, several rows of loads in flight.  A team reads its rows twice, for the sums and
 // to apply them; the second time they come from L1 or L2, which costs less than the
-// registers to hold them did (fewer resident teams: 110-row graphs, F = 128 fp32, 82 us
-// held, see group_norm.cu).  A graph of more than `most` rows ("large") is cut along a
-// grid of row shares over all rows; the teams of its shares write partial statistics, a
-// second kernel joins them in a fixed order, and a third one applies them, last share
-// first, whose rows L2 still holds.  A share is `most` rows long, so it meets at most two
-// large graphs: one that covers its first row (slot 0) and one that begins behind it and
-// runs past its end (slot 1).  Whether there are large graphs only the device knows; the
-// host leaves the two later kernels out where all rows together are at most `most`.
+// registers to hold them did (fewer resident teams: 1,024 graphs of 110 rows, F = 128
+// fp32, 82 us held, see group_norm.cu).  A graph of more than `most` rows ("large") is cut
+// along a grid of row shares over all rows: teams of the first kernel write partial
+// statistics of its pieces, and a second kernel joins them in a fixed order and applies
+// them, last share first, whose rows L2 still holds.  A share is at most `most` rows long,
+// so it meets at most two large graphs: one that covers its first row (slot 0) and one
+// that begins behind it and runs past its end (slot 1).  Whether there are large graphs
+// only the device knows; the host leaves the second kernel out where all rows together
+// are at most `most`, and elsewhere it ends after one look at the slots.
 #pragma once
 
 #include "widen.cuh"
@@ -27,16 +28,30 @@ namespace {
 
 constexpr int kActNone = TFG_ACT_NONE, kActRelu = TFG_ACT_RELU, kActSilu = TFG_ACT_SILU, kActGelu = TFG_ACT_GELU;
 
-// Activations in fp32.  The sigmoid's exponential is __expf (2 ulp and |y| u: its relative
-// error, times |y| (1 - sigmoid) at most, stays below 3 u of max(|y|, 1)) and its quotient
-// __fdividef (2 ulp; 0 where the divisor passes 2^126, where y e^y is below 1e-36 anyway).
+// Activations in fp32.  1 / (1 + 2^(-y log2 e)) by the hardware's exponential and reciprocal
+// (ex2.approx and rcp.approx, 2 ulp and 1 ulp, without the steps that keep subnormal
+// values): with the rounding of y log2 e the exponential is off by (2 + |y|) u relative,
+// which counts |y| (1 - sigmoid) times at most, so the sigmoid is within 4 u of itself times
+// max(|y|, 1).  Where 2^(...) passes 2^126 the sigmoid is 0 and y e^y below 1e-36.  The math
+// library's expf and quotient cost 12 instructions more a value (110-row graphs, F = 128:
+// the forward was bound by issue, 55 instructions a value).
+__device__ __forceinline__ float exp2_of(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float sigmoid_of(float y) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_of(y * -1.44269504088896341f)));
+    return r;
+}
 // 1 + erf leaves the gelu an absolute error of about |y| u for negative y.
-__device__ __forceinline__ float sigmoid_of(float y) { return __fdividef(1.f, 1.f + __expf(-y)); }
+__device__ __forceinline__ float normal_cdf(float y) { return fmaf(0.5f, erff(y * 0.70710678118654752f), 0.5f); }
 template <int ACT>
 __device__ __forceinline__ float activate(float y) {
     if constexpr (ACT == kActRelu) return y <= 0.f ? 0.f : y;      // a NaN stays
-    else if constexpr (ACT == kActSilu) return __fdividef(y, 1.f + __expf(-y));
-    else if constexpr (ACT == kActGelu) return 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
+    else if constexpr (ACT == kActSilu) return y * sigmoid_of(y);
+    else if constexpr (ACT == kActGelu) return y * normal_cdf(y);
     else return y;
 }
 template <int ACT>
@@ -46,8 +61,8 @@ __device__ __forceinline__ float activation_slope(float y) {
         const float p = sigmoid_of(y);
         return p * fmaf(y, 1.f - p, 1.f);
     } else if constexpr (ACT == kActGelu) {
-        const float d = 0.39894228040143268f * __expf(-0.5f * y * y);
-        return fmaf(y, d, 0.5f * (1.f + erff(y * 0.70710678118654752f)));
+        const float d = 0.39894228040143268f * exp2_of(y * y * -0.72134752044448170f);   // e^(-y^2 / 2)
+        return fmaf(y, d, normal_cdf(y));
     } else return 1.f;
 }
 
@@ -59,10 +74,14 @@ struct NormPlan {
     int cols;             // channels of a tile
     int tiles;
     int rows_at_once;     // rows a team reads side by side
+    int tile_groups;      // groups of a tile
     int lanes;            // vectors of a group (1 where a vector holds several groups)
     bool shuffles;        // groups and rows are powers of two of lanes: sums by lane exchanges
-    int64_t most;         // rows of a share, and of a graph that is not large
+    int log_row, log_c;   // then: logarithms of row_vecs and of the channels of a group
+    int64_t most;         // rows of a graph that is not large
+    int64_t share;        // rows of a share, at most that
     int64_t shares;       // 0: no graph can be large
+    bool join_apart;      // large graphs of so many shares that a kernel of its own joins them
 };
 
 // The rows of a large graph that share s holds in a slot, written by the first kernel.
@@ -80,15 +99,16 @@ struct NormArgs {
     const float *gamma, *beta;
     float eps;
     float *mean, *rstd;                           // [graphs, groups]
-    int32_t *status;
+    int32_t *status;      // null: checked by one CTA (status_all)
+    int32_t *status_all;
     void *out;
     const void *g;                                // backward: dL/dout
     const float *mean_in, *rstd_in;               // backward: the forward's statistics
     Piece *pieces;                                // [share][slot]
     float2 *part;                                 // [share][slot][group]
     float2 *joined;                               // [share of the graph's first row][group]
-    float2 *channel_part;                         // backward: [chain][F], sums for gamma and beta
-    int64_t chains;                               // backward: teams a tile's units are dealt to
+    float2 *channel_part;                         // backward: [batch, slot][F], sums for gamma and beta
+    int64_t batches, batch;                       // backward: batches of so many graphs
     NormPlan p;
 };
 
@@ -105,6 +125,19 @@ __device__ __forceinline__ RowRange graph_rows(const int64_t *offsets, int64_t g
     r.a = o0 < 0 ? 0 : (o0 > n ? n : o0);
     r.b = o1 < r.a ? r.a : (o1 > n ? n : o1);
     return r;
+}
+
+// The status of all offsets, by one CTA: saves the launch that clears the word.
+constexpr int64_t kStatusGraphs = 8192;
+__device__ __forceinline__ void check_offsets(const NormArgs &p) {
+    bool any = false;
+    for (int64_t g = threadIdx.x; g < p.graphs; g += blockDim.x) {
+        bool bad;
+        graph_rows(p.offsets, g, p.n, bad);
+        any |= bad;
+    }
+    const int all = __syncthreads_or(any);
+    if (threadIdx.x == 0) *p.status_all = all ? TFG_ERR_INDEX_RANGE : TFG_OK;
 }
 
 // Last graph that begins at or before row r, -1 if there is none; by the whole warp, 32
@@ -125,7 +158,7 @@ __device__ __forceinline__ int64_t warp_graph_at(const int64_t *offsets, int64_t
 }
 
 __device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int slot) {
-    const int64_t r0 = s * a.p.most, r1 = min64(a.n, r0 + a.p.most);
+    const int64_t r0 = s * a.p.share, r1 = min64(a.n, r0 + a.p.share);
     Piece p{0, 0, 0, 0};
     const int64_t g = warp_graph_at(a.offsets, a.graphs, slot == 0 ? r0 : r1 - 1);
     if (g < 0) return p;
@@ -136,13 +169,13 @@ __device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int sl
     p.b = r.b < r1 ? r.b : r1;
     if (p.b < p.a) p.b = p.a;
     p.graph = g;
-    p.first_share = r.a / a.p.most;
+    p.first_share = r.a / a.p.share;
     return p;
 }
 
 // The slot of share s that holds a piece of the graph whose first row is a.
 __device__ __forceinline__ int64_t slot_at(const NormArgs &p, int64_t a, int64_t s) {
-    return s * 2 + (a > s * p.p.most ? 1 : 0);
+    return s * 2 + (a > s * p.p.share ? 1 : 0);
 }
 
 // ---- a team -------------------------------------------------------------------------
@@ -183,15 +216,17 @@ struct Place {
 
     __device__ __forceinline__ Place(const NormArgs &a, int tile) {
         const int t = Team<TT>::thread();
-        rl = t / a.p.row_vecs;
+        rl = a.p.shuffles ? t >> a.p.log_row : t / a.p.row_vecs;
         sub = t - rl * a.p.row_vecs;
-        const int64_t first = static_cast<int64_t>(tile) * a.p.cols;
-        c0 = first + sub * VEC;
+        c0 = static_cast<int64_t>(tile) * a.p.cols + sub * VEC;
         on = rl < a.p.rows_at_once && c0 < a.f;
-        group0 = static_cast<int>(first / a.c);
-        groups = static_cast<int>(min64(a.p.cols, a.f - first)) / a.c;
+        group0 = tile * a.p.tile_groups;
+        groups = min(a.p.tile_groups, a.groups - group0);
 #pragma unroll
-        for (int q = 0; q < S; ++q) grp[q] = on ? (sub * VEC + q) / a.c : 0;
+        for (int q = 0; q < S; ++q) {
+            const int c = sub * VEC + q;
+            grp[q] = on ? (a.p.shuffles ? c >> a.p.log_c : c / a.c) : 0;
+        }
     }
     // rows of [a, b) that this thread visits: a + rl, a + rl + rows_at_once, ...
     __device__ __forceinline__ int rows(const NormArgs &p, int64_t a, int64_t b) const {
@@ -200,7 +235,7 @@ struct Place {
     }
     // whether sum q is the one that writes its group's statistics
     __device__ __forceinline__ bool writes(const NormArgs &a, int q) const {
-        return on && rl == 0 && (sub * VEC + q) % a.c == 0;
+        return on && rl == 0 && sub * VEC + q == grp[q] * a.c;
     }
 };
 
@@ -261,15 +296,22 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VE
                 for (int q = 0; q < S; ++q) to[(s * S + q) * TT + t] = v[s][q];
             M::sync();
             // warps that hold other rows of this warp's columns, or other columns of its group
-            const int wide = a.p.row_vecs > 32 ? a.p.row_vecs / 32 : 1, span = a.p.lanes > 32 ? a.p.lanes / 32 : 1;
+            const int log_wide = max(0, a.p.log_row - 5);
+            const int wide = (1 << log_wide) - 1, span = a.p.lanes > 32 ? a.p.lanes / 32 : 1;
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
                 for (int q = 0; q < S; ++q) {
+                    const float *from = to + (s * S + q) * TT + lane;
                     float r = 0.f;
+                    if (wide == 0) {                        // a warp holds whole rows
 #pragma unroll
-                    for (int w = 0; w < M::kWarps; ++w)
-                        if (w % wide / span == warp % wide / span) r += to[(s * S + q) * TT + w * 32 + lane];
+                        for (int w = 0; w < M::kWarps; ++w) r += from[w * 32];
+                    } else {
+                        const int mine = warp & wide & ~(span - 1);
+                        for (int w = 0; w < M::kWarps; ++w)
+                            if ((w & wide & ~(span - 1)) == mine) r += from[w * 32];
+                    }
                     v[s][q] = r;
                 }
         }
@@ -317,6 +359,29 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VE
         for (int q = 0; q < S; ++q) v[s][q] = smem[s * (rows + 2) * cols + (rows + 1) * cols + at.grp[q]];
 }
 
+// ---- the second kernel ---------------------------------------------------------------
+constexpr int kLargeTeam = 256;                   // its teams, but for tiles of 1,024 threads
+
+// Values of the piece of rows r in share i, and its slot.
+__device__ __forceinline__ float piece_values(const NormArgs &p, const RowRange &r, int64_t i) {
+    const int64_t a = i * p.p.share, b = a + p.p.share;
+    return static_cast<float>(((b < r.b ? b : r.b) - (a > r.a ? a : r.a)) * p.c);
+}
+
+// Joined statistics of the tile's groups of a piece's graph, s_stat[group]: join(rows, first
+// share, group) by a warp, or what a kernel of its own joined.  Collective over the CTA.
+template <int TT, typename At, typename Join>
+__device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, float2 *s_stat, Join join) {
+    bool bad;
+    const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
+    for (int k = threadIdx.x >> 5; k < at.groups; k += TT / 32) {
+        const float2 v = p.p.join_apart ? p.joined[piece.first_share * p.groups + at.group0 + k]
+                                        : join(p, r, piece.first_share, at.group0 + k);
+        if ((threadIdx.x & 31) == 0) s_stat[k] = v;
+    }
+    __syncthreads();
+}
+
 // ---- host ---------------------------------------------------------------------------
 int64_t gcd64(int64_t a, int64_t b) { return b == 0 ? a : gcd64(b, a % b); }
 bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
@@ -359,17 +424,27 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec) {
     }
     p.row_vecs = static_cast<int>(w);
     p.cols = static_cast<int>(w * vec);
+    p.tile_groups = static_cast<int>(p.cols / c);
+    while ((1 << p.log_row) < p.row_vecs) ++p.log_row;
+    while ((1 << p.log_c) < c) ++p.log_c;
     p.tiles = static_cast<int>((f + p.cols - 1) / p.cols);
     const int64_t t = threads(mean, w);
     p.team = t <= 32 && w <= 32 ? 32 : (t <= 128 && w <= 128 ? 128 : 256);
     if (w > 256) p.team = 1024;
     p.rows_at_once = p.team / p.row_vecs;
-    // a share: an equal part of all rows for every resident team, no less than a team is made for
-    int64_t most = (n * p.tiles + kShareTeams - 1) / kShareTeams;
+    // a share: an equal part of all rows for every resident team, no less than a team is made
+    // for.  Where there are enough graphs to go round, those of up to four mean ones are not
+    // large, and a share is two mean ones.
     const int64_t least = int64_t(p.rows_at_once) * kVectorsAThread;
-    if (most < least) most = least;
-    p.most = most;
-    p.shares = n <= most ? 0 : (n + most - 1) / most;
+    p.share = (n * p.tiles + kShareTeams - 1) / kShareTeams;
+    if (p.share < least) p.share = least;
+    p.most = p.share;
+    if (graphs * p.tiles >= 304 && p.share < 4 * mean) {
+        p.most = 4 * mean;
+        if (p.share < 2 * mean) p.share = 2 * mean;
+    }
+    p.shares = n <= p.most ? 0 : (n + p.share - 1) / p.share;
+    p.join_apart = mean > 128 * p.share;
     return p;
 }
 

@@ -5,9 +5,9 @@
 //   s1 = sum gamma d, s2 = sum gamma d h                        over the (graph, group)
 //   grad_x = r (gamma d - (s1 + h s2) / M)
 //
-// The units -- graphs, then shares of the large ones -- of a tile are dealt to a fixed
-// number of teams, each of which keeps its columns' sums for gamma and beta in registers
-// from unit to unit and leaves them once; a last kernel adds those of all teams in order.
+// A team takes a batch of graphs (or a piece of a large one), keeps its columns' sums for
+// gamma and beta in registers from graph to graph and leaves them once; a last kernel adds
+// those of all teams in order.
 #include "group_norm.cuh"
 
 namespace tfg {
@@ -125,43 +125,47 @@ template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
 __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_BACK_RESIDENT)) norm_back_units(NormArgs p) {
     using M = Team<TT>;
     extern __shared__ __align__(16) float s_all[];
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * M::kPerCta + M::index();
-    const int64_t chain = id / p.p.tiles;
-    const int tile = static_cast<int>(id - chain * p.p.tiles);
-    if (chain >= p.chains) return;                          // whole teams
+    const uint32_t id = blockIdx.x * M::kPerCta + M::index();
+    const int64_t row = id / static_cast<uint32_t>(p.p.tiles);   // a batch of graphs, then the slots of the shares
+    const int tile = static_cast<int>(id - static_cast<uint32_t>(row) * p.p.tiles);
+    if (row >= p.batches + 2 * p.p.shares) return;          // whole teams
     float *smem = s_all + M::index() * back_floats(p.p, S, VEC);
     const Place<TT, VEC, S> at(p, tile);
     Column<VEC, S> c;
-    c.weights(p, at);
     float weight[2][VEC] = {}, s[2][S];
+    const int64_t slot = row - p.batches;
+    Piece piece{0, 0, 0, 0};
+    if (slot >= 0) {
+        piece = find_piece(p, slot >> 1, slot & 1);
+        if (tile == 0 && M::thread() == 0) p.pieces[slot] = piece;
+        if (piece.a == piece.b) return;                     // its channels' row is not read
+    }
+    c.weights(p, at);
     int buffer = 0;
+    const int64_t first = row * p.batch, stop = slot >= 0 ? first + 1 : min64(p.graphs, first + p.batch);
 #pragma unroll 1
-    for (int64_t unit = chain; unit < p.graphs + 2 * p.p.shares; unit += p.chains) {
-        Piece rows{0, 0, 0, 0};
-        if (unit < p.graphs) {
+    for (int64_t graph = first; graph < stop; ++graph) {
+        if (slot < 0) {
             bool bad;
-            const RowRange r = graph_rows(p.offsets, unit, p.n, bad);
-            if (r.b - r.a <= p.p.most) rows = {r.a, r.b, unit, 0};
-        } else {
-            rows = find_piece(p, (unit - p.graphs) >> 1, (unit - p.graphs) & 1);
-            if (tile == 0 && M::thread() == 0) p.pieces[unit - p.graphs] = rows;
+            const RowRange r = graph_rows(p.offsets, graph, p.n, bad);
+            if (r.a == r.b || r.b - r.a > p.p.most) continue;
+            piece = {r.a, r.b, graph, 0};
         }
-        if (rows.a == rows.b) continue;
-        c.statistics(p, at, rows.graph);
-        sums<ACT, XT, GT>(p, at, c, rows.a, rows.b, smem, buffer, s, weight);
+        c.statistics(p, at, piece.graph);
+        sums<ACT, XT, GT>(p, at, c, piece.a, piece.b, smem, buffer, s, weight);
         buffer ^= 1;
-        if (unit < p.graphs) {
-            const float count = static_cast<float>((rows.b - rows.a) * p.c);
+        if (slot < 0) {
+            const float count = static_cast<float>((piece.b - piece.a) * p.c);
 #pragma unroll
             for (int q = 0; q < S; ++q) {
                 s[0][q] /= count;
                 s[1][q] /= count;
             }
-            gradient<ACT, XT, GT>(p, at, c, rows.a, rows.b, s);
+            gradient<ACT, XT, GT>(p, at, c, piece.a, piece.b, s);
         } else {
 #pragma unroll
             for (int q = 0; q < S; ++q)
-                if (at.writes(p, q)) p.part[(unit - p.graphs) * p.groups + at.group0 + at.grp[q]] = make_float2(s[0][q], s[1][q]);
+                if (at.writes(p, q)) p.part[slot * p.groups + at.group0 + at.grp[q]] = make_float2(s[0][q], s[1][q]);
         }
     }
     if (!p.channel_part) return;
@@ -183,100 +187,123 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_BACK_RES
             r.x += smem[j * cols + i];
             r.y += smem[(rows + j) * cols + i];
         }
-        p.channel_part[chain * p.f + c0 + i] = r;
+        p.channel_part[row * p.f + c0 + i] = r;
     }
 }
 
-// Sums over M of the large graph that begins in share blockIdx.x, a warp a group.
+// Sums over M of a large graph (rows r, from share s on) for group k, by a warp.
+__device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
+    const int64_t s1 = (r.b - 1) / p.p.share;
+    const float all = static_cast<float>((r.b - r.a) * p.c);
+    float x = 0.f, y = 0.f;
+#pragma unroll 4
+    for (int64_t i = s + (threadIdx.x & 31); i <= s1; i += 32) {
+        const float2 v = p.part[slot_at(p, r.a, i) * p.groups + k];
+        x += v.x;
+        y += v.y;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        x += lane_xor(x, o);
+        y += lane_xor(y, o);
+    }
+    return make_float2(x / all, y / all);
+}
+
+// join_apart: the large graph that begins in share blockIdx.x, a warp a group.
 constexpr int kBackJoinWarps = 4;
 __global__ void __launch_bounds__(kBackJoinWarps * 32) norm_back_join(NormArgs p) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t s = blockIdx.x;
     Piece piece = p.pieces[s * 2];
     if (piece.a == piece.b || piece.first_share != s) piece = p.pieces[s * 2 + 1];
     if (piece.a == piece.b || piece.first_share != s) return;
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
-    const int64_t s1 = (r.b - 1) / p.p.most;
-    const float all = static_cast<float>((r.b - r.a) * p.c);
-    for (int k = blockIdx.y * kBackJoinWarps + warp; k < p.groups; k += gridDim.y * kBackJoinWarps) {
-        float x = 0.f, y = 0.f;
-        for (int64_t i = s + lane; i <= s1; i += 32) {
-            const float2 v = p.part[slot_at(p, r.a, i) * p.groups + k];
-            x += v.x;
-            y += v.y;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            x += lane_xor(x, o);
-            y += lane_xor(y, o);
-        }
-        if (lane == 0) p.joined[s * p.groups + k] = make_float2(x / all, y / all);
+    for (int k = blockIdx.y * kBackJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kBackJoinWarps) {
+        const float2 v = join(p, r, s, k);
+        if ((threadIdx.x & 31) == 0) p.joined[s * p.groups + k] = v;
     }
 }
 
-// The shares' large pieces once more, the last first: L2 still holds them.
+// grad_gamma and grad_beta of four channels: the teams' sums, 64 interleaved in order.  Of
+// the rows behind the batches, the shares' slots, those without a piece were not written.
+constexpr int kChannelCols = 4;
+template <int TT>
+__device__ __forceinline__ void channel_gradients(const NormArgs &p, int64_t c0, float2 (&s_sum)[TT],
+                                                  float *__restrict__ grad_gamma, float *__restrict__ grad_beta) {
+    constexpr int kLines = TT / kChannelCols;
+    const int64_t c = c0 + threadIdx.x % kChannelCols;
+    const int line = threadIdx.x / kChannelCols;
+    float2 v = make_float2(0.f, 0.f);
+    auto add = [&](int64_t row) {
+        const float2 w = __ldg(p.channel_part + row * p.f + c);
+        v.x += w.x;
+        v.y += w.y;
+    };
+    if (c < p.f) {
+#pragma unroll 8
+        for (int64_t i = line; i < p.batches; i += kLines) add(i);
+#pragma unroll 4
+        for (int64_t i = line; i < 2 * p.p.shares; i += kLines)
+            if (p.pieces[i].a != p.pieces[i].b) add(p.batches + i);
+    }
+    s_sum[threadIdx.x] = v;
+    __syncthreads();
+#pragma unroll
+    for (int o = TT / 2; o >= kChannelCols; o >>= 1) {
+        if (threadIdx.x < o) {
+            s_sum[threadIdx.x].x += s_sum[threadIdx.x + o].x;
+            s_sum[threadIdx.x].y += s_sum[threadIdx.x + o].y;
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x < kChannelCols && c < p.f) {
+        grad_gamma[c] = s_sum[threadIdx.x].x;
+        grad_beta[c] = s_sum[threadIdx.x].y;
+    }
+}
+
+// The first channel_ctas CTAs add up the channels' gradients, the others take the pieces of
+// large graphs once more, a CTA a (slot, tile), the last slot first.
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
-__global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_BACK_RESIDENT)) norm_back_apply(NormArgs p) {
-    using M = Team<TT>;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * M::kPerCta + M::index();
-    const int64_t back = id / p.p.tiles;
-    const int tile = static_cast<int>(id - back * p.p.tiles);
-    if (back >= 2 * p.p.shares) return;
+__global__ void __launch_bounds__(TT, team_ctas(TT, TFG_BACK_RESIDENT))
+norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_beta) {
+    extern __shared__ __align__(16) float s_all[];
+    if (blockIdx.x < channel_ctas) {
+        __shared__ float2 s_sum[TT];
+        return channel_gradients<TT>(p, static_cast<int64_t>(blockIdx.x) * kChannelCols, s_sum, grad_gamma, grad_beta);
+    }
+    float2 *s_stat = reinterpret_cast<float2 *>(s_all);    // [tile's groups]
+    const uint32_t id = blockIdx.x - channel_ctas;
+    const int64_t back = id / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(id - static_cast<uint32_t>(back) * p.p.tiles);
     const Piece piece = p.pieces[2 * p.p.shares - 1 - back];
     if (piece.a == piece.b) return;
     const Place<TT, VEC, S> at(p, tile);
+    joined_statistics<TT>(p, at, piece, s_stat, join);
     Column<VEC, S> c;
     c.weights(p, at);
     c.statistics(p, at, piece.graph);
     float s[2][S];
 #pragma unroll
     for (int q = 0; q < S; ++q) {
-        const float2 j = at.on ? __ldg(p.joined + piece.first_share * p.groups + at.group0 + at.grp[q]) : make_float2(0.f, 0.f);
-        s[0][q] = j.x;
-        s[1][q] = j.y;
+        const float2 v = s_stat[at.grp[q]];
+        s[0][q] = v.x;
+        s[1][q] = v.y;
     }
     gradient<ACT, XT, GT>(p, at, c, piece.a, piece.b, s);
 }
 
-// grad_gamma and grad_beta: the chains' sums of every channel, 32 interleaved in order.
-constexpr int kChannelRows = 32;
-__global__ void __launch_bounds__(32 * kChannelRows)
-norm_channels(const float2 *__restrict__ part, int64_t chains, int64_t f, float *__restrict__ grad_gamma,
-              float *__restrict__ grad_beta) {
-    __shared__ float2 s_sum[kChannelRows][33];
-    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
-    float2 v = make_float2(0.f, 0.f);
-    if (c < f) {
-#pragma unroll 4
-        for (int64_t i = row; i < chains; i += kChannelRows) {
-            const float2 w = __ldg(part + i * f + c);
-            v.x += w.x;
-            v.y += w.y;
-        }
-    }
-    s_sum[row][lane] = v;
-    __syncthreads();
-    v = s_sum[lane][row];                                   // channel `row`, chain `lane`
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        v.x += lane_xor(v.x, o);
-        v.y += lane_xor(v.y, o);
-    }
-    const int64_t to = static_cast<int64_t>(blockIdx.x) * 32 + row;
-    if (lane == 0 && to < f) {
-        grad_gamma[to] = v.x;
-        grad_beta[to] = v.y;
-    }
+// Graphs of a batch: one, or so many that the batches of all tiles are twice what is
+// resident at once (a batch leaves 8 bytes a channel).
+int64_t back_batch(const NormPlan &p, int64_t graphs) {
+    const int64_t resident = team_ctas(p.team, TFG_BACK_RESIDENT) * (p.team == 32 ? kWarpTeams : 1) * 152;
+    const int64_t batches = (2 * resident + p.tiles - 1) / p.tiles;
+    return graphs <= batches ? 1 : (graphs + batches - 1) / batches;
 }
-
-// Teams a tile's units are dealt to: what is resident at once.
-int64_t back_chains(const NormPlan &p, int64_t graphs) {
-    const int64_t per_sm = team_ctas(p.team, TFG_BACK_RESIDENT) * (p.team == 32 ? kWarpTeams : 1);
-    const int64_t at_once = (per_sm * 152 + p.tiles - 1) / p.tiles;
-    const int64_t units = graphs + 2 * p.shares;
-    return units < at_once ? units : at_once;
+int64_t back_batches(const NormPlan &p, int64_t graphs) {
+    const int64_t b = back_batch(p, graphs);
+    return (graphs + b - 1) / b;
 }
 
 struct BackLayout {       // of the workspace, in bytes
@@ -286,52 +313,56 @@ struct BackLayout {       // of the workspace, in bytes
 BackLayout back_layout(const NormPlan &p, int64_t graphs, int64_t f, int64_t groups) {
     const size_t shares = size_t(p.shares);
     return {shares * 2 * sizeof(Piece), shares * 2 * size_t(groups) * sizeof(float2), shares * size_t(groups) * sizeof(float2),
-            size_t(back_chains(p, graphs) * f) * sizeof(float2)};
+            size_t((back_batches(p, graphs) + 2 * p.shares) * f) * sizeof(float2)};
 }
 
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
-cudaError_t launch_act(const NormArgs &p, float *grad_gamma, float *grad_beta, cudaStream_t s) {
+cudaError_t launch_units(const NormArgs &p, cudaStream_t s) {
     using M = Team<TT>;
     const int smem = M::kPerCta * back_floats(p.p, S, VEC) * static_cast<int>(sizeof(float));
-    auto ctas = [](int64_t teams) { return static_cast<unsigned>((teams + M::kPerCta - 1) / M::kPerCta); };
-    norm_back_units<ACT, TT, XT, GT, VEC, S><<<ctas(p.chains * p.p.tiles), M::kThreads, smem, s>>>(p);
-    cudaError_t err = cudaGetLastError();
-    if (err != cudaSuccess) return err;
-    if (p.p.shares > 0) {
-        const dim3 join(static_cast<unsigned>(p.p.shares),
-                        static_cast<unsigned>(min64((p.groups + kBackJoinWarps - 1) / kBackJoinWarps, 65535)));
-        norm_back_join<<<join, kBackJoinWarps * 32, 0, s>>>(p);
-        err = cudaGetLastError();
-        if (err != cudaSuccess) return err;
-        norm_back_apply<ACT, TT, XT, GT, VEC, S><<<ctas(2 * p.p.shares * p.p.tiles), M::kThreads, 0, s>>>(p);
-        err = cudaGetLastError();
-        if (err != cudaSuccess) return err;
-    }
-    if (grad_gamma)
-        norm_channels<<<static_cast<unsigned>((p.f + 31) / 32), 32 * kChannelRows, 0, s>>>(p.channel_part, p.chains, p.f,
-                                                                                          grad_gamma, grad_beta);
+    const int64_t teams = (p.batches + 2 * p.p.shares) * p.p.tiles;
+    norm_back_units<ACT, TT, XT, GT, VEC, S>
+        <<<static_cast<unsigned>((teams + M::kPerCta - 1) / M::kPerCta), M::kThreads, smem, s>>>(p);
     return cudaGetLastError();
 }
 
-template <int TT, typename XT, typename GT, int VEC, int S>
-cudaError_t launch_back(const NormArgs &p, int act, float *gg, float *gb, cudaStream_t s) {
-    switch (act) {
-        case kActRelu: return launch_act<kActRelu, TT, XT, GT, VEC, S>(p, gg, gb, s);
-        case kActSilu: return launch_act<kActSilu, TT, XT, GT, VEC, S>(p, gg, gb, s);
-        case kActGelu: return launch_act<kActGelu, TT, XT, GT, VEC, S>(p, gg, gb, s);
-        default: return launch_act<kActNone, TT, XT, GT, VEC, S>(p, gg, gb, s);
+template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
+cudaError_t launch_large(NormArgs p, float *grad_gamma, float *grad_beta, cudaStream_t s) {
+    if (p.p.join_apart && p.p.shares > 0) {
+        const dim3 grid(static_cast<unsigned>(p.p.shares),
+                        static_cast<unsigned>(min64((p.groups + kBackJoinWarps - 1) / kBackJoinWarps, 65535)));
+        norm_back_join<<<grid, kBackJoinWarps * 32, 0, s>>>(p);
+        const cudaError_t err = cudaGetLastError();
+        if (err != cudaSuccess) return err;
     }
+    p.p.rows_at_once = TT / p.p.row_vecs;
+    const int channel_ctas = grad_gamma ? static_cast<int>((p.f + kChannelCols - 1) / kChannelCols) : 0;
+    const int64_t ctas = channel_ctas + 2 * p.p.shares * p.p.tiles;
+    const int smem = p.p.tile_groups * static_cast<int>(sizeof(float2));
+    norm_back_large<ACT, TT, XT, GT, VEC, S><<<static_cast<unsigned>(ctas), TT, smem, s>>>(p, channel_ctas, grad_gamma, grad_beta);
+    return cudaGetLastError();
+}
+
+template <int ACT, typename XT, typename GT, int VEC, int S>
+cudaError_t launch_act(const NormArgs &p, float *gg, float *gb, cudaStream_t s) {
+    const bool widest = VEC == 1 && p.p.team == 1024;
+    cudaError_t err;
+    if (widest) err = launch_units<ACT, VEC == 1 ? 1024 : 256, XT, GT, VEC, S>(p, s);
+    else if (p.p.team == 32) err = launch_units<ACT, 32, XT, GT, VEC, S>(p, s);
+    else if (p.p.team == 128) err = launch_units<ACT, 128, XT, GT, VEC, S>(p, s);
+    else err = launch_units<ACT, 256, XT, GT, VEC, S>(p, s);
+    if (err != cudaSuccess || (p.p.shares == 0 && !gg)) return err;
+    return widest ? launch_large<ACT, VEC == 1 ? 1024 : 256, XT, GT, VEC, S>(p, gg, gb, s)
+                  : launch_large<ACT, kLargeTeam, XT, GT, VEC, S>(p, gg, gb, s);
 }
 
 template <typename XT, typename GT, int VEC, int S>
 cudaError_t launch_team(const NormArgs &p, int act, float *gg, float *gb, cudaStream_t s) {
-    if constexpr (VEC == 1) {
-        if (p.p.team == 1024) return launch_back<1024, XT, GT, VEC, S>(p, act, gg, gb, s);
-    }
-    switch (p.p.team) {
-        case 32: return launch_back<32, XT, GT, VEC, S>(p, act, gg, gb, s);
-        case 128: return launch_back<128, XT, GT, VEC, S>(p, act, gg, gb, s);
-        default: return launch_back<256, XT, GT, VEC, S>(p, act, gg, gb, s);
+    switch (act) {
+        case kActRelu: return launch_act<kActRelu, XT, GT, VEC, S>(p, gg, gb, s);
+        case kActSilu: return launch_act<kActSilu, XT, GT, VEC, S>(p, gg, gb, s);
+        case kActGelu: return launch_act<kActGelu, XT, GT, VEC, S>(p, gg, gb, s);
+        default: return launch_act<kActNone, XT, GT, VEC, S>(p, gg, gb, s);
     }
 }
 
@@ -376,7 +407,8 @@ cudaError_t launch_group_norm_backward(const void *x, int x_dtype, const int64_t
     p.g = g;
     p.out = grad_x;
     p.p = back_plan(n, graphs, f, p.c, aligned);
-    p.chains = back_chains(p.p, graphs);
+    p.batch = back_batch(p.p, graphs);
+    p.batches = back_batches(p.p, graphs);
     const BackLayout l = back_layout(p.p, graphs, f, groups);
     char *at = static_cast<char *>(ws);
     p.pieces = reinterpret_cast<Piece *>(at);
