@@ -322,6 +322,7 @@ cudaError_t launch_embedding_backward(const int32_t *rowptr, const int32_t *sort
                                       const void *g, int g_dtype, int64_t n, int64_t rows, int64_t f, float scale,
                                       float *out, void *ws, cudaStream_t s);
 bool group_norm_fits(int64_t n, int64_t graphs, int64_t f, int64_t groups);
+bool group_norm_backward_fits(int64_t n, int64_t graphs, int64_t f, int64_t groups);
 size_t group_norm_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t groups);
 cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets, int64_t n, int64_t graphs, int64_t f,
                               int64_t groups, const float *gamma, const float *beta, float eps, int act, void *out,

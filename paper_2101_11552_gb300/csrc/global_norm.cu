@@ -173,16 +173,6 @@ write_norm(const double *__restrict__ partial, int n, float *__restrict__ norm) 
 // ---- scaling ----------------------------------------------------------------------
 // Plain loads: out may be the tensor itself, and then what is read is written here.
 template <typename T, int VEC>
-__device__ __forceinline__ typename VecLoad<T, VEC>::Raw plain_load(const T *p) {
-    if constexpr (VEC == 1) {
-        if constexpr (sizeof(T) == 2) return static_cast<uint32_t>(*p) << 16;
-        else return *p;
-    } else {
-        return *reinterpret_cast<const typename VecLoad<T, VEC>::Raw *>(p);
-    }
-}
-
-template <typename T, int VEC>
 __device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, float factor) {
     constexpr int kLoads = 32 / VEC;
 #pragma unroll
@@ -194,7 +184,7 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, floa
         for (int i = 0; i < kLoads; ++i) {
             const int64_t at = base + (static_cast<int64_t>(i) * kNormThreads + threadIdx.x) * VEC;
             raw[i] = VecLoad<T, VEC>::zero();
-            if (at + VEC <= left) raw[i] = plain_load<T, VEC>(p + at);
+            if (at + VEC <= left) raw[i] = load_plain<T, VEC>(p + at);
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -210,7 +200,7 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, floa
     if (VEC > 1 && left < kChunk && static_cast<int64_t>(threadIdx.x) < left % VEC) {
         const int64_t at = left / VEC * VEC + threadIdx.x;
         float v[1];
-        VecLoad<T, 1>::widen(plain_load<T, 1>(p + at), v);
+        VecLoad<T, 1>::widen(load_plain<T, 1>(p + at), v);
         v[0] *= factor;
         store_vec<1>(o + at, v);
     }

@@ -3,207 +3,147 @@
 //   m = sum x / M, v = sum (x - m)^2 / M, r = 1 / sqrt(v + eps)    M = n_g * C values
 //   y = gamma (x - m) r + beta, out = act(y)
 //
-// One pass over a team's rows gives mean and centred squares: a thread takes kDepth rows at
-// a time, forms their mean and squares about it in registers, and merges them into its
-// running (count, mean, squares) by the pooled-variance identity
-//   delta = m_b - m_a, m = m_a + delta n_b / n, q = q_a + q_b + delta^2 n_a n_b / n,
-// so a mean far from zero costs no precision; threads, and shares of a large graph, are
-// joined by the same identity.
+// The mean first, then the squares about it, so a mean far from zero costs no precision;
+// shares of a large graph are joined by the pooled-variance identity, squares about the
+// joint mean = squares of the parts + n (mean of the part - joint mean)^2.
 #include "group_norm.cuh"
 
 namespace tfg {
 namespace {
 
-#ifndef TFG_NORM_DEPTH
-#define TFG_NORM_DEPTH 8
-#endif
-constexpr int kDepth = TFG_NORM_DEPTH;            // rows in flight per thread
-
-// This thread's count, means and centred squares.
-template <int S>
-struct Running {
-    float n = 0.f, mean[S] = {}, squares[S] = {};
-};
-
-template <bool FULL, typename XT, int VEC, int S>
-__device__ __forceinline__ void merge(Running<S> &r, const typename VecLoad<XT, VEC>::Raw (&raw)[kDepth], int rows) {
-    constexpr int kPer = VEC / S;                           // values of a sum in a vector
-    float m[S] = {}, sq[S] = {};
-#pragma unroll
-    for (int u = 0; u < kDepth; ++u) {
-        if (!FULL && u >= rows) break;
-        float v[VEC];
-        VecLoad<XT, VEC>::widen(raw[u], v);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) m[q / kPer] += v[q];
-    }
-    const float n = static_cast<float>((FULL ? kDepth : rows) * kPer);
-#pragma unroll
-    for (int q = 0; q < S; ++q) m[q] = FULL ? m[q] * (1.f / (kDepth * kPer)) : m[q] / n;
-#pragma unroll
-    for (int u = 0; u < kDepth; ++u) {
-        if (!FULL && u >= rows) break;
-        float v[VEC];
-        VecLoad<XT, VEC>::widen(raw[u], v);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) sq[q / kPer] = fmaf(v[q] - m[q / kPer], v[q] - m[q / kPer], sq[q / kPer]);
-    }
-    const float share = __fdividef(n, r.n + n);             // 1 for the first rows: exact
-#pragma unroll
-    for (int q = 0; q < S; ++q) {
-        const float delta = m[q] - r.mean[q];
-        r.mean[q] = fmaf(delta, share, r.mean[q]);
-        r.squares[q] += fmaf(delta * delta, r.n * share, sq[q]);
-    }
-    r.n += n;
-}
-
-// Means and centred squares of rows [a, b), to every thread for its groups.
+// Means and centred squares of the held rows, to every thread for its groups; per_value: one
+// over their number of values.
 template <int TT, typename XT, int VEC, int S>
-__device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t a, int64_t b, float *smem,
-                                           float (&mean)[S], float (&squares)[S]) {
-    using V = VecLoad<XT, VEC>;
-    Running<S> r;
-    const int rows = at.rows(p, a, b);
-    const XT *x = static_cast<const XT *>(p.x) + (a + at.rl) * p.f + at.c0;
-    const int64_t step = p.p.rows_at_once * p.f;
-    int i = 0;
-#pragma unroll 1
-    for (; i + kDepth <= rows; i += kDepth) {
-        typename V::Raw raw[kDepth];
+__device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
+                                           int rows, float per_value, float *smem, float (&mean)[S], float (&squares)[S]) {
+    constexpr int kPer = VEC / S;                           // values of a sum in a vector
+    float v[1][S] = {};
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float w[VEC];
+        held.widen(i, w);
 #pragma unroll
-        for (int u = 0; u < kDepth; ++u) raw[u] = V::raw(x + u * step);
-        x += kDepth * step;
-        merge<true, XT, VEC, S>(r, raw, kDepth);
+        for (int q = 0; q < VEC; ++q) v[0][q / kPer] += w[q];
     }
-    if (i < rows) {
-        typename V::Raw raw[kDepth];
-#pragma unroll
-        for (int u = 0; u < kDepth; ++u)
-            if (i + u < rows) raw[u] = V::raw(x + u * step);
-        merge<false, XT, VEC, S>(r, raw, rows - i);
-    }
-    const float count = static_cast<float>((b - a) * p.c);
-    float v[1][S];
-#pragma unroll
-    for (int q = 0; q < S; ++q) v[0][q] = r.n * r.mean[q];
     group_sums<TT, VEC, S, 1>(p, at, v, smem, 0);
 #pragma unroll
     for (int q = 0; q < S; ++q) {
-        mean[q] = v[0][q] / count;
-        const float d = r.mean[q] - mean[q];
-        v[0][q] = r.n > 0.f ? fmaf(d * d, r.n, r.squares[q]) : 0.f;
+        mean[q] = v[0][q] * per_value;
+        v[0][q] = 0.f;
+    }
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float w[VEC];
+        held.widen(i, w);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+            const float d = w[q] - mean[q / kPer];
+            v[0][q / kPer] = fmaf(d, d, v[0][q / kPer]);
+        }
     }
     group_sums<TT, VEC, S, 1>(p, at, v, smem, 1);
 #pragma unroll
     for (int q = 0; q < S; ++q) squares[q] = v[0][q];
 }
 
-template <int ACT, typename XT, typename OT, int VEC, int TT, int S>
-__device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t a, int64_t b,
-                                      const float (&m)[S], const float (&r)[S]) {
-    using V = VecLoad<XT, VEC>;
+template <int ACT, typename OT, typename XT, int VEC, int TT, int S>
+__device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held, int rows,
+                                      int64_t a, const float (&m)[S], const float (&r)[S]) {
     constexpr int kPer = VEC / S;
-    const int rows = at.rows(p, a, b);
     if (rows == 0) return;
-    const float *gamma = p.gamma, *beta = p.beta;
     float scale[VEC], shift[VEC];
+    channel_weights(p.gamma, at.c0, 1.f, scale);
+    channel_weights(p.beta, at.c0, 0.f, shift);
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-        scale[q] = gamma ? __ldg(gamma + at.c0 + q) * r[q / kPer] : r[q / kPer];
-        shift[q] = beta ? __ldg(beta + at.c0 + q) : 0.f;
-    }
-    const int64_t first = (a + at.rl) * p.f + at.c0, step = p.p.rows_at_once * p.f;
-    const XT *x = static_cast<const XT *>(p.x) + first;
-    OT *o = static_cast<OT *>(p.out) + first;
-#pragma unroll 1
-    for (int i = 0; i < rows; i += kDepth) {
-        typename V::Raw raw[kDepth];
+    for (int q = 0; q < VEC; ++q) scale[q] *= r[q / kPer];
+    const int64_t step = p.p.rows_at_once * p.f;
+    OT *o = static_cast<OT *>(p.out) + (a + at.rl) * p.f + at.c0;
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float v[VEC];
+        held.widen(i, v);
 #pragma unroll
-        for (int u = 0; u < kDepth; ++u)
-            if (i + u < rows) raw[u] = V::raw(x + u * step);
-#pragma unroll
-        for (int u = 0; u < kDepth; ++u) {
-            if (i + u >= rows) break;
-            float v[VEC];
-            V::widen(raw[u], v);
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) v[q] = activate<ACT>(fmaf(v[q] - m[q / kPer], scale[q], shift[q]));
-            store_vec<VEC>(o + u * step, v);
-        }
-        x += kDepth * step;
-        o += kDepth * step;
+        for (int q = 0; q < VEC; ++q) v[q] = activate<ACT>(fmaf(v[q] - m[q / kPer], scale[q], shift[q]));
+        store_vec<VEC>(o + i * step, v);
     }
 }
 
 template <typename XT, int VEC, int TT, int S>
-__device__ __forceinline__ void apply_act(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t a, int64_t b, int act,
-                                          bool out_bf16, const float (&m)[S], const float (&r)[S]) {
+__device__ __forceinline__ void apply_act(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
+                                          int rows, int64_t a, int act, bool out_bf16, const float (&m)[S],
+                                          const float (&r)[S]) {
     switch (act + (out_bf16 ? 4 : 0)) {
-        case kActNone: return apply<kActNone, XT, float>(p, at, a, b, m, r);
-        case kActRelu: return apply<kActRelu, XT, float>(p, at, a, b, m, r);
-        case kActSilu: return apply<kActSilu, XT, float>(p, at, a, b, m, r);
-        case kActGelu: return apply<kActGelu, XT, float>(p, at, a, b, m, r);
-        case 4 + kActNone: return apply<kActNone, XT, uint16_t>(p, at, a, b, m, r);
-        case 4 + kActRelu: return apply<kActRelu, XT, uint16_t>(p, at, a, b, m, r);
-        case 4 + kActSilu: return apply<kActSilu, XT, uint16_t>(p, at, a, b, m, r);
-        default: return apply<kActGelu, XT, uint16_t>(p, at, a, b, m, r);
+        case kActNone: return apply<kActNone, float>(p, at, held, rows, a, m, r);
+        case kActRelu: return apply<kActRelu, float>(p, at, held, rows, a, m, r);
+        case kActSilu: return apply<kActSilu, float>(p, at, held, rows, a, m, r);
+        case kActGelu: return apply<kActGelu, float>(p, at, held, rows, a, m, r);
+        case 4 + kActNone: return apply<kActNone, uint16_t>(p, at, held, rows, a, m, r);
+        case 4 + kActRelu: return apply<kActRelu, uint16_t>(p, at, held, rows, a, m, r);
+        case 4 + kActSilu: return apply<kActSilu, uint16_t>(p, at, held, rows, a, m, r);
+        default: return apply<kActGelu, uint16_t>(p, at, held, rows, a, m, r);
     }
 }
 
-// Units: the graphs, then the two slots of every share; a team takes a (unit, tile).
+// Units: the graphs, then the shares with their two slots; a team takes a (unit, tile).
 template <int TT, typename XT, int VEC, int S>
 __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_NORM_RESIDENT)) norm_units(NormArgs p, int act, bool out_bf16) {
     using M = Team<TT>;
-    extern __shared__ __align__(16) float s_all[];
+    extern __shared__ __align__(16) char s_all[];
     if (p.status_all && blockIdx.x == gridDim.x - 1) return check_offsets(p);
     const uint32_t id = blockIdx.x * M::kPerCta + M::index();
     const int64_t unit = id / static_cast<uint32_t>(p.p.tiles);
     const int tile = static_cast<int>(id - static_cast<uint32_t>(unit) * p.p.tiles);
-    if (unit >= p.graphs + 2 * p.p.shares) return;          // whole teams
-    float *smem = s_all + M::index() * team_floats<1>(p.p, S);
+    if (unit >= p.graphs + p.p.shares) return;              // whole teams
+    char *smem = s_all + M::index() * team_bytes(p.p, 1, S, VEC * sizeof(XT));
+    const Held<XT, VEC, TT> held(smem + sum_floats(p.p, 1, S) * 4);
     const Place<TT, VEC, S> at(p, tile);
-    float mean[S], squares[S];
     const int t = M::thread();
-    const int64_t slot = unit - p.graphs;                   // 2 * share + slot
-    RowRange r;
-    if (slot < 0) {
-        bool bad;
-        r = graph_rows(p.offsets, unit, p.n, bad);
-        if (bad && tile == 0 && t == 0) set_status(p.status, TFG_ERR_INDEX_RANGE);
-        if (r.b - r.a > p.p.most) return;                   // large: the shares'
-    } else {
-        const Piece piece = find_piece(p, slot >> 1, slot & 1);
-        if (tile == 0 && t == 0) p.pieces[slot] = piece;
-        if (piece.a == piece.b) return;
-        r = {piece.a, piece.b};
-    }
-    const int64_t out0 = unit * p.groups + at.group0;
-    if (r.a == r.b) {                                       // an empty graph has no statistics: zeros
-        for (int k = t; k < at.groups; k += TT) {
-            if (p.mean) p.mean[out0 + k] = 0.f;
-            if (p.rstd) p.rstd[out0 + k] = 0.f;
+    const int64_t share = unit - p.graphs;
+    int64_t covered = 0;
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        RowRange r;
+        if (share < 0) {
+            bool bad;
+            r = graph_rows(p.offsets, unit, p.n, bad);
+            if (bad && tile == 0 && t == 0) set_status(p.status, TFG_ERR_INDEX_RANGE);
+            if (r.b - r.a > p.p.most) return;               // large: the shares'
+            if (r.a == r.b) {                               // an empty graph has no statistics: zeros
+                for (int k = t; k < at.groups; k += TT) {
+                    if (p.mean) p.mean[unit * p.groups + at.group0 + k] = 0.f;
+                    if (p.rstd) p.rstd[unit * p.groups + at.group0 + k] = 0.f;
+                }
+                return;
+            }
+        } else {
+            const Piece piece = find_piece(p, share, slot, covered);
+            if (tile == 0 && t == 0) p.pieces[share * 2 + slot] = piece;
+            if (piece.a == piece.b) continue;
+            r = {piece.a, piece.b};
         }
-        return;
-    }
-    statistics<TT, XT>(p, at, r.a, r.b, smem, mean, squares);
-    if (slot >= 0) {
+        const int rows = at.rows(p, r.a, r.b);
+        const float per_value = 1.f / static_cast<float>((r.b - r.a) * p.c);
+        held.copy(static_cast<const XT *>(p.x) + (r.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
+        copies_done();
+        float mean[S], squares[S];
+        statistics(p, at, held, rows, per_value, reinterpret_cast<float *>(smem), mean, squares);
+        if (share < 0) {
+            float rstd[S];
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                rstd[q] = rsqrtf(fmaf(squares[q], per_value, p.eps));
+                if (p.mean && at.writes(p, q)) {
+                    p.mean[unit * p.groups + at.group0 + at.grp[q]] = mean[q];
+                    p.rstd[unit * p.groups + at.group0 + at.grp[q]] = rstd[q];
+                }
+            }
+            return apply_act(p, at, held, rows, r.a, act, out_bf16, mean, rstd);
+        }
 #pragma unroll
         for (int q = 0; q < S; ++q)
-            if (at.writes(p, q)) p.part[slot * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
-        return;
+            if (at.writes(p, q))
+                p.part[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
     }
-    const float count = static_cast<float>((r.b - r.a) * p.c);
-    float rstd[S];
-#pragma unroll
-    for (int q = 0; q < S; ++q) {
-        rstd[q] = 1.f / sqrtf(squares[q] / count + p.eps);
-        if (p.mean && at.writes(p, q)) {
-            p.mean[out0 + at.grp[q]] = mean[q];
-            p.rstd[out0 + at.grp[q]] = rstd[q];
-        }
-    }
-    apply_act<XT>(p, at, r.a, r.b, act, out_bf16, mean, rstd);
 }
 
 // Joins the pieces of a large graph (rows r, from share s on) for group k, by a warp: the
@@ -227,11 +167,11 @@ __device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) squares += lane_xor(squares, o);
-    return make_float2(mean, 1.f / sqrtf(squares / all + p.eps));
+    return make_float2(mean, rsqrtf(squares / all + p.eps));
 }
 
 // join_apart: the large graph that begins in share blockIdx.x, a warp a group.
-constexpr int kJoinWarps = 4;
+constexpr int kJoinWarps = 8;
 __global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
     const int64_t s = blockIdx.x;
     Piece piece = p.pieces[s * 2];
@@ -245,42 +185,53 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
     }
 }
 
-// The pieces of large graphs once more, a CTA a (slot, tile), the last slot first.
+// The pieces of large graphs once more, a CTA a (share, tile), the last share first.
 template <int TT, typename XT, int VEC, int S>
 __global__ void __launch_bounds__(TT, team_ctas(TT, TFG_NORM_RESIDENT)) norm_large(NormArgs p, int act, bool out_bf16) {
-    extern __shared__ __align__(16) float s_all[];
-    float2 *s_stat = reinterpret_cast<float2 *>(s_all);    // [tile's groups]
-    const int64_t back = blockIdx.x / static_cast<uint32_t>(p.p.tiles);
-    const int tile = static_cast<int>(blockIdx.x - static_cast<uint32_t>(back) * p.p.tiles);
-    const Piece piece = p.pieces[2 * p.p.shares - 1 - back];
-    if (piece.a == piece.b) return;
-    const Place<TT, VEC, S> at(p, tile);
-    joined_statistics<TT>(p, at, piece, s_stat, join);
-    float mean[S], rstd[S];
-#pragma unroll
-    for (int q = 0; q < S; ++q) {
-        const float2 v = s_stat[at.grp[q]];
-        mean[q] = v.x;
-        rstd[q] = v.y;
-    }
-    // the share in which the graph begins reports its statistics
-    if (p.mean && piece.a < (piece.first_share + 1) * p.p.share) {
-        const int64_t out0 = piece.graph * p.groups + at.group0;
+    extern __shared__ __align__(16) char s_all[];
+    const Held<XT, VEC, TT> held(s_all);
+    float2 *s_stat = reinterpret_cast<float2 *>(s_all + p.p.held * TT * VEC * sizeof(XT));   // [tile's groups]
+    const uint32_t back = blockIdx.x / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(blockIdx.x - back * p.p.tiles);
+    const int64_t share = p.p.shares - 1 - back;
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        const Piece piece = p.pieces[share * 2 + slot];
+        if (piece.a == piece.b) continue;
+        const Place<TT, VEC, S> at(p, tile);
+        const int rows = at.rows(p, piece.a, piece.b);
+        held.copy(static_cast<const XT *>(p.x) + (piece.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
+        __syncthreads();                                    // the last statistics have been read
+        joined_statistics<TT>(p, at, piece, s_stat, join);
+        copies_done();
+        float mean[S], rstd[S];
 #pragma unroll
         for (int q = 0; q < S; ++q) {
-            if (!at.writes(p, q)) continue;
-            p.mean[out0 + at.grp[q]] = mean[q];
-            p.rstd[out0 + at.grp[q]] = rstd[q];
+            const float2 v = s_stat[at.grp[q]];
+            mean[q] = v.x;
+            rstd[q] = v.y;
         }
+        // the share in which the graph begins reports its statistics
+        if (p.mean && piece.first_share == share) {
+            const int64_t out0 = piece.graph * p.groups + at.group0;
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                if (!at.writes(p, q)) continue;
+                p.mean[out0 + at.grp[q]] = mean[q];
+                p.rstd[out0 + at.grp[q]] = rstd[q];
+            }
+        }
+        apply_act(p, at, held, rows, piece.a, act, out_bf16, mean, rstd);
     }
-    apply_act<XT>(p, at, piece.a, piece.b, act, out_bf16, mean, rstd);
 }
 
 template <int TT, typename XT, int VEC, int S>
 cudaError_t launch_units(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
     using M = Team<TT>;
-    const int smem = M::kPerCta * team_floats<1>(p.p, S) * static_cast<int>(sizeof(float));
-    const int64_t teams = (p.graphs + 2 * p.p.shares) * p.p.tiles;
+    const int smem = M::kPerCta * team_bytes(p.p, 1, S, VEC * sizeof(XT));
+    const cudaError_t err = allow_shared(norm_units<TT, XT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
+    const int64_t teams = (p.graphs + p.p.shares) * p.p.tiles;
     const int64_t ctas = (teams + M::kPerCta - 1) / M::kPerCta + (p.status_all ? 1 : 0);
     norm_units<TT, XT, VEC, S><<<static_cast<unsigned>(ctas), M::kThreads, smem, s>>>(p, act, out_bf16);
     return cudaGetLastError();
@@ -291,12 +242,15 @@ cudaError_t launch_large(NormArgs p, int act, bool out_bf16, cudaStream_t s) {
     if (p.p.join_apart) {
         const dim3 grid(static_cast<unsigned>(p.p.shares), static_cast<unsigned>(min64((p.groups + kJoinWarps - 1) / kJoinWarps, 65535)));
         norm_join<<<grid, kJoinWarps * 32, 0, s>>>(p);
-        const cudaError_t err = cudaGetLastError();
-        if (err != cudaSuccess) return err;
+        const cudaError_t launched = cudaGetLastError();
+        if (launched != cudaSuccess) return launched;
     }
-    p.p.rows_at_once = TT / p.p.row_vecs;
-    const int smem = p.p.tile_groups * static_cast<int>(sizeof(float2));
-    norm_large<TT, XT, VEC, S><<<static_cast<unsigned>(2 * p.p.shares * p.p.tiles), TT, smem, s>>>(p, act, out_bf16);
+    set_rows_at_once(p.p, TT);
+    p.p.held = static_cast<int>((p.p.share + p.p.rows_at_once - 1) / p.p.rows_at_once);
+    const int smem = p.p.held * TT * VEC * static_cast<int>(sizeof(XT)) + p.p.tile_groups * static_cast<int>(sizeof(float2));
+    const cudaError_t err = allow_shared(norm_large<TT, XT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
+    norm_large<TT, XT, VEC, S><<<static_cast<unsigned>(p.p.shares * p.p.tiles), TT, smem, s>>>(p, act, out_bf16);
     return cudaGetLastError();
 }
 
@@ -325,24 +279,33 @@ cudaError_t launch_vec(const NormArgs &p, int act, bool out_bf16, cudaStream_t s
 
 }  // namespace
 
+namespace {
+NormPlan forward_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int elem, bool aligned) {
+    const int vec = norm_vec(f, c, 16 / elem, aligned);
+    return norm_plan(n, graphs, f, c, vec, 1, vec * elem);
+}
+}  // namespace
+
 // Whether the teams of every type and alignment fit a grid.
 bool group_norm_fits(int64_t n, int64_t graphs, int64_t f, int64_t groups) {
-    const int64_t c = f / groups;
-    for (const int vec : {4, 8, 1}) {
-        const NormPlan p = norm_plan(n, graphs, f, c, norm_vec(f, c, vec, vec > 1));
-        if ((graphs + 2 * p.shares) * p.tiles > 0x7fffffff) return false;
+    for (const int elem : {4, 2}) {
+        for (const bool aligned : {true, false}) {
+            const NormPlan p = forward_plan(n, graphs, f, f / groups, elem, aligned);
+            if ((graphs + p.shares) * p.tiles > 0x7fff0000) return false;
+        }
     }
-    return true;
+    return group_norm_backward_fits(n, graphs, f, groups);
 }
 
 // Bytes for any type and alignment of the inputs.
 size_t group_norm_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t groups) {
     size_t most = 0;
-    const int64_t c = f / groups;
-    for (const int vec : {4, 8, 1}) {
-        const NormPlan p = norm_plan(n, graphs, f, c, norm_vec(f, c, vec, vec > 1));
-        const size_t bytes = size_t(p.shares) * (2 * sizeof(Piece) + 3 * size_t(groups) * sizeof(float2));
-        if (bytes > most) most = bytes;
+    for (const int elem : {4, 2}) {
+        for (const bool aligned : {true, false}) {
+            const NormPlan p = forward_plan(n, graphs, f, f / groups, elem, aligned);
+            const size_t bytes = size_t(p.shares) * (2 * sizeof(Piece) + 3 * size_t(groups) * sizeof(float2));
+            if (bytes > most) most = bytes;
+        }
     }
     return most;
 }
@@ -354,9 +317,9 @@ cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets
         const cudaError_t err = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
         if (err != cudaSuccess || graphs == 0) return err;
     }
-    const bool aligned = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out) |
+                           reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) & 15) == 0;
     const int64_t c = f / groups;
-    const int vec = norm_vec(f, c, x_dtype == TFG_BF16 ? 8 : 4, aligned);
     NormArgs p{};
     p.x = x;
     p.offsets = offsets;
@@ -372,7 +335,7 @@ cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets
     p.rstd = rstd;
     (graphs > kStatusGraphs ? p.status : p.status_all) = status;
     p.out = out;
-    p.p = norm_plan(n, graphs, f, c, vec);
+    p.p = forward_plan(n, graphs, f, c, x_dtype == TFG_BF16 ? 2 : 4, aligned);
     p.pieces = static_cast<Piece *>(ws);
     p.part = reinterpret_cast<float2 *>(p.pieces + 2 * p.p.shares);
     p.joined = p.part + p.p.shares * 2 * groups;

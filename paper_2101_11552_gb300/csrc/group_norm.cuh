@@ -7,18 +7,21 @@
 // a (graph, group).
 //
 // Work split.  A team of threads (a warp, or a CTA) takes a graph and a tile of channels,
-// whole groups of them: the threads of a row read vectors side by side and step down the
-// rows, several rows of loads in flight.  A team reads its rows twice, for the sums and
-// to apply them; the second time they come from L1 or L2, which costs less than the
-// registers to hold them did (fewer resident teams: 1,024 graphs of 110 rows, F = 128
-// fp32, 82 us held, see group_norm.cu).  A graph of more than `most` rows ("large") is cut
-// along a grid of row shares over all rows: teams of the first kernel write partial
-// statistics of its pieces, and a second kernel joins them in a fixed order and applies
-// them, last share first, whose rows L2 still holds.  A share is at most `most` rows long,
-// so it meets at most two large graphs: one that covers its first row (slot 0) and one
-// that begins behind it and runs past its end (slot 1).  Whether there are large graphs
-// only the device knows; the host leaves the second kernel out where all rows together
-// are at most `most`, and elsewhere it ends after one look at the slots.
+// whole groups of them: the threads of a row take vectors side by side and step down the
+// rows.  Each thread copies its vectors to shared memory of its own (cp.async: all of
+// them in flight at once, no registers, no barrier), and the passes over them -- the sums,
+// and the application of the statistics -- read them from there, so that x comes from
+// memory once.  Held in registers, or read again from L2, there were too few bytes in
+// flight (1,024 graphs of 110 rows, F = 128 fp32, forward: 82 and 27 us).
+//
+// A graph of more rows than a team has room for ("large") is cut along a grid of row
+// shares over all rows: teams of the first kernel write partial statistics of its pieces,
+// and a second kernel joins them in a fixed order and applies them, last share first,
+// whose rows L2 still holds.  A share has no more rows than a team has room for, so it
+// meets at most two large graphs: one that covers its first row (slot 0) and one that
+// begins behind it and runs past its end (slot 1).  Whether there are large graphs only
+// the device knows; the host leaves the second kernel out where all rows fit a team, and
+// elsewhere it ends after one look at the slots.
 #pragma once
 
 #include "widen.cuh"
@@ -77,7 +80,8 @@ struct NormPlan {
     int tile_groups;      // groups of a tile
     int lanes;            // vectors of a group (1 where a vector holds several groups)
     bool shuffles;        // groups and rows are powers of two of lanes: sums by lane exchanges
-    int log_row, log_c;   // then: logarithms of row_vecs and of the channels of a group
+    int log_row, log_c, log_rows;   // then: logarithms of row_vecs, the channels of a group, rows_at_once
+    int held;             // rows of a thread that its shared memory has room for
     int64_t most;         // rows of a graph that is not large
     int64_t share;        // rows of a share, at most that
     int64_t shares;       // 0: no graph can be large
@@ -157,13 +161,18 @@ __device__ __forceinline__ int64_t warp_graph_at(const int64_t *offsets, int64_t
     return lo;
 }
 
-__device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int slot) {
+// covered: the rows up to which slot 0's search has told what there is; slot 1 needs no search
+// where that is the share's end.
+__device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int slot, int64_t &covered) {
     const int64_t r0 = s * a.p.share, r1 = min64(a.n, r0 + a.p.share);
     Piece p{0, 0, 0, 0};
+    if (slot == 1 && covered >= r1) return p;
     const int64_t g = warp_graph_at(a.offsets, a.graphs, slot == 0 ? r0 : r1 - 1);
+    covered = r0;
     if (g < 0) return p;
     bool bad;
     const RowRange r = graph_rows(a.offsets, g, a.n, bad);
+    covered = r.b;
     if (r.b - r.a <= a.p.most || r.b <= r0 || (slot == 1) != (r.a > r0)) return p;
     p.a = r.a > r0 ? r.a : r0;
     p.b = r.b < r1 ? r.b : r1;
@@ -181,13 +190,13 @@ __device__ __forceinline__ int64_t slot_at(const NormArgs &p, int64_t a, int64_t
 // ---- a team -------------------------------------------------------------------------
 // TT threads: a warp in a CTA of four, each with shared memory of its own, or a whole CTA.
 constexpr int kWarpTeams = 4;
-// Resident threads asked for, forward and backward: 80 and 128 registers a thread (64 in
-// teams of 1,024).
+// Resident threads asked for: 64 registers a thread forward, 80 backward (64 in teams of
+// 1,024).
 #ifndef TFG_NORM_RESIDENT
-#define TFG_NORM_RESIDENT 768
+#define TFG_NORM_RESIDENT 1024
 #endif
 #ifndef TFG_BACK_RESIDENT
-#define TFG_BACK_RESIDENT 512
+#define TFG_BACK_RESIDENT 768
 #endif
 constexpr int team_ctas(int team, int threads) { return team == 1024 ? 1 : threads / (team == 256 ? 256 : 128); }
 template <int TT>
@@ -231,7 +240,8 @@ struct Place {
     // rows of [a, b) that this thread visits: a + rl, a + rl + rows_at_once, ...
     __device__ __forceinline__ int rows(const NormArgs &p, int64_t a, int64_t b) const {
         const int left = static_cast<int>(b - a) - rl;
-        return on && left > 0 ? (left + p.p.rows_at_once - 1) / p.p.rows_at_once : 0;
+        const int up = left + p.p.rows_at_once - 1;
+        return on && left > 0 ? (p.p.shuffles ? up >> p.p.log_rows : up / p.p.rows_at_once) : 0;
     }
     // whether sum q is the one that writes its group's statistics
     __device__ __forceinline__ bool writes(const NormArgs &a, int q) const {
@@ -239,17 +249,32 @@ struct Place {
     }
 };
 
-// Floats of a team's shared memory for NS quantities, two buffers of the exchange.
-template <int NS>
-__host__ __device__ inline int team_floats(const NormPlan &p, int sums) {
-    return p.shuffles ? (p.team > 32 ? 2 * NS * sums * p.team : 0) : NS * (p.rows_at_once + 2) * p.cols;
+// Floats of shared memory that a team's sums of `quantities` take: two buffers of the
+// exchange, or per-channel sums.
+__host__ __device__ inline int sum_floats(const NormPlan &p, int quantities, int sums) {
+    return p.shuffles ? (p.team > 32 ? 2 * quantities * sums * p.team : 0) : quantities * (p.rows_at_once + 2) * p.cols;
 }
 
-// The same for the backward, whose channel sums take two floats per column of the team.
-__host__ __device__ inline int back_floats(const NormPlan &p, int sums, int vec) {
-    const int groups = team_floats<2>(p, sums), channels = 2 * p.team * vec;
-    return groups > channels ? groups : channels;
+// Bytes of shared memory of a team: sums and held rows.
+__host__ __device__ inline int team_bytes(const NormPlan &p, int quantities, int sums, int row_bytes) {
+    return (sum_floats(p, quantities, sums) * 4 + p.held * p.team * row_bytes + 15) / 16 * 16;
 }
+
+// A thread's rows in shared memory, one vector each; the team's threads side by side.
+template <typename T, int VEC, int TT>
+struct Held {
+    static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
+    T *at;
+
+    __device__ __forceinline__ explicit Held(void *team_part) : at(static_cast<T *>(team_part) + Team<TT>::thread() * VEC) {}
+    __device__ __forceinline__ void copy(const T *from, int rows, int64_t step) const {
+#pragma unroll 4
+        for (int i = 0; i < rows; ++i) copy_async<kBytes>(at + i * TT * VEC, from + i * step);
+    }
+    __device__ __forceinline__ void widen(int i, float (&v)[VEC]) const {
+        VecLoad<T, VEC>::widen(load_plain<T, VEC>(at + i * TT * VEC), v);
+    }
+};
 
 // Sums of v[s][q] over the rows and the channels of each group of the tile, to every thread
 // for its own groups.  Collective over the team.  By lane exchanges and one barrier where
@@ -359,6 +384,19 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VE
         for (int q = 0; q < S; ++q) v[s][q] = smem[s * (rows + 2) * cols + (rows + 1) * cols + at.grp[q]];
 }
 
+// gamma or beta of a thread's channels (aligned like the vectors of x), or their default.
+template <int VEC>
+__device__ __forceinline__ void channel_weights(const float *w, int64_t c0, float none, float (&v)[VEC]) {
+    if (w) {
+        RowVec<float, VEC> r;
+        r.load(w + c0);
+        r.widen(v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) v[q] = none;
+    }
+}
+
 // ---- the second kernel ---------------------------------------------------------------
 constexpr int kLargeTeam = 256;                   // its teams, but for tiles of 1,024 threads
 
@@ -386,6 +424,12 @@ __device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &a
 int64_t gcd64(int64_t a, int64_t b) { return b == 0 ? a : gcd64(b, a % b); }
 bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
 
+void set_rows_at_once(NormPlan &p, int team) {
+    p.rows_at_once = team / p.row_vecs;
+    p.log_rows = 0;
+    while ((1 << p.log_rows) < p.rows_at_once) ++p.log_rows;
+}
+
 // The longest vector, of at most `widest` values, that rows, pointers and groups allow: 8
 // values only where they lie in one group (sums of 8 channels a thread spill), 4 where a
 // tile of whole groups and whole vectors fits a team of 256.
@@ -395,32 +439,42 @@ int norm_vec(int64_t f, int64_t c, int widest, bool aligned) {
 }
 
 #ifndef TFG_NORM_VECS
-#define TFG_NORM_VECS 8
+#define TFG_NORM_VECS 16
 #endif
 #ifndef TFG_NORM_TEAMS
 #define TFG_NORM_TEAMS 1216
 #endif
+#ifndef TFG_NORM_ROOM
+#define TFG_NORM_ROOM 55
+#endif
 constexpr int kVectorsAThread = TFG_NORM_VECS;    // of a mean graph
 constexpr int64_t kShareTeams = TFG_NORM_TEAMS;
+constexpr int kNormRoom = TFG_NORM_ROOM * 1024;   // shared memory of a CTA: four on a multiprocessor
 
-// Tiles of whole groups and whole vectors: 32 vectors of a row, fewer (8 at least) as long
-// as the mean graphs leave multiprocessors without a team.  The team: kVectorsAThread
+// quantities: summed at once; row_bytes: of the vectors held per row and thread.
+// Tiles are whole groups and whole vectors: 32 vectors of a row, fewer (128 bytes at least)
+// as long as a team has no room for twice the mean graph.  The team: kVectorsAThread
 // vectors of a mean graph to a thread, or 256 threads on shares of large ones.
-NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec) {
+NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int quantities, int row_bytes) {
     NormPlan p{};
     p.vec = vec;
     const int64_t unit = c / gcd64(c, vec);                     // vectors of the smallest tile
     const int64_t row = f / vec;
     const int64_t mean = graphs > 0 ? (n + graphs - 1) / graphs : 0;
+    const int sums = c % vec == 0 ? 1 : vec;
     p.lanes = static_cast<int>(c > vec ? unit : 1);
     p.shuffles = power_of_two(c);                               // c a multiple or a divisor of vec then
+    const int64_t least = (128 * quantities + row_bytes - 1) / row_bytes;   // vectors of 128 bytes of one operand
+    auto fits = [&](int64_t vecs) { return 2 * mean * vecs * row_bytes <= kNormRoom; };
     int64_t w = unit;
-    auto threads = [&](int64_t rows, int64_t vecs) { return (rows * vecs + kVectorsAThread - 1) / kVectorsAThread; };
     if (p.shuffles) {
         while (w < row && w < 32) w <<= 1;
-        while (w > unit && w > 8 && threads(n, row) / 128 < 2 * 152 && threads(mean, w) > 32) w >>= 1;
+        int64_t narrow = w;
+        while (narrow > unit && narrow / 2 >= least && !fits(narrow)) narrow >>= 1;
+        if (fits(narrow)) w = narrow;
     } else {
-        while (w + unit <= row && w + unit <= 32) w += unit;
+        const int64_t most = fits(w < least ? least : w) ? 32 : 64;         // large graphs: whole rows at best
+        while (w + unit <= row && w + unit <= most && (w < least || most == 64 || fits(w + unit))) w += unit;
     }
     p.row_vecs = static_cast<int>(w);
     p.cols = static_cast<int>(w * vec);
@@ -428,24 +482,31 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec) {
     while ((1 << p.log_row) < p.row_vecs) ++p.log_row;
     while ((1 << p.log_c) < c) ++p.log_c;
     p.tiles = static_cast<int>((f + p.cols - 1) / p.cols);
-    const int64_t t = threads(mean, w);
+    const int64_t t = (mean * w + kVectorsAThread - 1) / kVectorsAThread;
     p.team = t <= 32 && w <= 32 ? 32 : (t <= 128 && w <= 128 ? 128 : 256);
     if (w > 256) p.team = 1024;
-    p.rows_at_once = p.team / p.row_vecs;
-    // a share: an equal part of all rows for every resident team, no less than a team is made
-    // for.  Where there are enough graphs to go round, those of up to four mean ones are not
-    // large, and a share is two mean ones.
-    const int64_t least = int64_t(p.rows_at_once) * kVectorsAThread;
+    set_rows_at_once(p, p.team);
+    const int per_cta = p.team == 32 ? kWarpTeams : 1;
+    const int64_t room = (kNormRoom / per_cta - sum_floats(p, quantities, sums) * 4) / (int64_t(p.team) * row_bytes);
+    const int64_t wanted = ((mean < 4 ? 8 : 2 * mean) + p.rows_at_once - 1) / p.rows_at_once;
+    p.held = static_cast<int>(wanted < room ? wanted : room);
+    if (p.held < 1) p.held = 1;
+    p.most = int64_t(p.held) * p.rows_at_once;
+    // a share: an equal part of all rows for every resident team, if a team has room for it
     p.share = (n * p.tiles + kShareTeams - 1) / kShareTeams;
-    if (p.share < least) p.share = least;
-    p.most = p.share;
-    if (graphs * p.tiles >= 304 && p.share < 4 * mean) {
-        p.most = 4 * mean;
-        if (p.share < 2 * mean) p.share = 2 * mean;
-    }
+    const int64_t few = int64_t(p.rows_at_once) * 4;
+    if (p.share < few) p.share = few;
+    if (p.share > p.most || 2 * mean <= p.most) p.share = p.most;
     p.shares = n <= p.most ? 0 : (n + p.share - 1) / p.share;
-    p.join_apart = mean > 128 * p.share;
+    p.join_apart = mean > 8 * p.share;
     return p;
+}
+
+// 48 KB, static shared memory with it, need no permission.
+template <typename Kernel>
+cudaError_t allow_shared(Kernel *kernel, int bytes) {
+    return bytes <= 32 * 1024 ? cudaSuccess
+                              : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 }  // namespace

@@ -13,10 +13,11 @@
 namespace tfg {
 namespace {
 
-#ifndef TFG_BACK_DEPTH
-#define TFG_BACK_DEPTH 4
-#endif
-constexpr int kBackDepth = TFG_BACK_DEPTH;        // rows of x and of the gradient in flight per thread
+// Shared memory of a team: sums and held rows, and at the end its channels' sums instead.
+__host__ __device__ inline int back_bytes(const NormPlan &p, int sums, int vec, int row_bytes) {
+    const int held = team_bytes(p, 2, sums, row_bytes), channels = 2 * p.team * vec * 4;
+    return held > channels ? held : channels;
+}
 
 template <int VEC, int S>
 struct Column {           // what a thread's channels need
@@ -24,11 +25,8 @@ struct Column {           // what a thread's channels need
 
     template <int TT>
     __device__ __forceinline__ void weights(const NormArgs &p, const Place<TT, VEC, S> &at) {
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            gamma[q] = at.on && p.gamma ? __ldg(p.gamma + at.c0 + q) : 1.f;
-            beta[q] = at.on && p.beta ? __ldg(p.beta + at.c0 + q) : 0.f;
-        }
+        channel_weights(at.on ? p.gamma : nullptr, at.c0, 1.f, gamma);
+        channel_weights(at.on ? p.beta : nullptr, at.c0, 0.f, beta);
     }
     template <int TT>
     __device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t graph) {
@@ -39,135 +37,145 @@ struct Column {           // what a thread's channels need
             rstd[q] = at.on ? __ldg(p.rstd_in + i) : 0.f;
         }
     }
-    // h and d of one vector
-    template <int ACT, typename XV, typename GV>
-    __device__ __forceinline__ void values(const XV &x, const GV &g, float (&h)[VEC], float (&d)[VEC]) const {
-        x.widen(h);
-        g.widen(d);
+    // e = x - m = h / r and d of row i; slope: gamma r
+    template <int ACT, typename XH, typename GH>
+    __device__ __forceinline__ void values(const XH &x, const GH &g, int i, const float (&slope)[VEC], float (&e)[VEC],
+                                           float (&d)[VEC]) const {
+        x.widen(i, e);
+        g.widen(i, d);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            h[q] = (h[q] - mean[q / (VEC / S)]) * rstd[q / (VEC / S)];
-            d[q] *= activation_slope<ACT>(fmaf(gamma[q], h[q], beta[q]));
+            e[q] -= mean[q / (VEC / S)];
+            d[q] *= activation_slope<ACT>(fmaf(slope[q], e[q], beta[q]));
         }
     }
 };
 
-// Calls each(row vector of x, of the gradient, offset of the row) for this thread's rows of
-// [a, b) in order, kBackDepth rows of loads at a time.
-template <typename XT, typename GT, int VEC, int TT, int S, typename Each>
-__device__ __forceinline__ void for_rows(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t a, int64_t b, Each each) {
-    const int rows = at.rows(p, a, b);
-    const int64_t step = p.p.rows_at_once * p.f;
-    int64_t first = (a + at.rl) * p.f + at.c0;
-#pragma unroll 1
-    for (int i = 0; i < rows; i += kBackDepth) {
-        RowVec<XT, VEC> x[kBackDepth];
-        RowVec<GT, VEC> g[kBackDepth];
-#pragma unroll
-        for (int u = 0; u < kBackDepth; ++u) {
-            if (i + u >= rows) continue;
-            x[u].load(static_cast<const XT *>(p.x) + first + u * step);
-            g[u].load(static_cast<const GT *>(p.g) + first + u * step);
-        }
-#pragma unroll
-        for (int u = 0; u < kBackDepth; ++u) {
-            if (i + u >= rows) break;
-            each(x[u], g[u], first + u * step);
-        }
-        first += kBackDepth * step;
-    }
-}
-
-// Sums of gamma d and gamma d h over rows [a, b) of each group, to every thread for its
+// Sums of gamma d and gamma d h over the held rows of each group, to every thread for its
 // groups; weight adds up this thread's d h and d.
 template <int ACT, typename XT, typename GT, int TT, int VEC, int S>
-__device__ __forceinline__ void sums(const NormArgs &p, const Place<TT, VEC, S> &at, const Column<VEC, S> &c, int64_t a,
-                                     int64_t b, float *smem, int buffer, float (&s)[2][S], float (&weight)[2][VEC]) {
-    float dh[VEC] = {}, db[VEC] = {};
-    for_rows<XT, GT>(p, at, a, b, [&](const auto &x, const auto &g, int64_t) {
-        float h[VEC], d[VEC];
-        c.template values<ACT>(x, g, h, d);
+__device__ __forceinline__ void sums(const NormArgs &p, const Place<TT, VEC, S> &at, const Column<VEC, S> &c,
+                                     const float (&slope)[VEC], const Held<XT, VEC, TT> &x, const Held<GT, VEC, TT> &g,
+                                     int rows, float *smem, int buffer, float (&s)[2][S], float (&weight)[2][VEC]) {
+    constexpr int kPer = VEC / S;
+    float de[VEC] = {}, db[VEC] = {};
+#pragma unroll 2
+    for (int i = 0; i < rows; ++i) {
+        float e[VEC], d[VEC];
+        c.template values<ACT>(x, g, i, slope, e, d);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            dh[q] = fmaf(d[q], h[q], dh[q]);
+            de[q] = fmaf(d[q], e[q], de[q]);
             db[q] += d[q];
         }
-    });
+    }
 #pragma unroll
     for (int q = 0; q < S; ++q) s[0][q] = s[1][q] = 0.f;
 #pragma unroll
     for (int q = 0; q < VEC; ++q) {
-        s[0][q / (VEC / S)] += c.gamma[q] * db[q];
-        s[1][q / (VEC / S)] += c.gamma[q] * dh[q];
-        weight[0][q] += dh[q];
+        s[0][q / kPer] = fmaf(c.gamma[q], db[q], s[0][q / kPer]);
+        s[1][q / kPer] = fmaf(slope[q], de[q], s[1][q / kPer]);
+        weight[0][q] = fmaf(c.rstd[q / kPer], de[q], weight[0][q]);
         weight[1][q] += db[q];
     }
     group_sums<TT, VEC, S, 2>(p, at, s, smem, buffer);
 }
 
-// grad_x of rows [a, b); s: the sums over M.
+// grad_x of the held rows from row a on, gamma r d - r s1 - (r^2 s2) e; s: the sums over M.
 template <int ACT, typename XT, typename GT, int TT, int VEC, int S>
-__device__ __forceinline__ void gradient(const NormArgs &p, const Place<TT, VEC, S> &at, const Column<VEC, S> &c, int64_t a,
-                                         int64_t b, const float (&s)[2][S]) {
-    for_rows<XT, GT>(p, at, a, b, [&](const auto &x, const auto &g, int64_t to) {
-        float h[VEC], d[VEC];
-        c.template values<ACT>(x, g, h, d);
+__device__ __forceinline__ void gradient(const NormArgs &p, const Place<TT, VEC, S> &at, const Column<VEC, S> &c,
+                                         const float (&slope)[VEC], const Held<XT, VEC, TT> &x, const Held<GT, VEC, TT> &g,
+                                         int rows, int64_t a, const float (&s)[2][S]) {
+    constexpr int kPer = VEC / S;
+    float s1[S], s2[S];
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            const int k = q / (VEC / S);
-            d[q] = c.rstd[k] * (fmaf(c.gamma[q], d[q], -s[0][k]) - h[q] * s[1][k]);
-        }
-        store_vec<VEC>(static_cast<GT *>(p.out) + to, d);
-    });
+    for (int q = 0; q < S; ++q) {
+        s1[q] = -c.rstd[q] * s[0][q];
+        s2[q] = -c.rstd[q] * (c.rstd[q] * s[1][q]);
+    }
+    const int64_t step = p.p.rows_at_once * p.f;
+    GT *to = static_cast<GT *>(p.out) + (a + at.rl) * p.f + at.c0;
+#pragma unroll 2
+    for (int i = 0; i < rows; ++i) {
+        float e[VEC], d[VEC];
+        c.template values<ACT>(x, g, i, slope, e, d);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) d[q] = fmaf(slope[q], d[q], fmaf(s2[q / kPer], e[q], s1[q / kPer]));
+        store_vec<VEC>(to + i * step, d);
+    }
+}
+
+template <typename XT, typename GT, int VEC, int TT, int S>
+__device__ __forceinline__ void copy_rows(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &x,
+                                          const Held<GT, VEC, TT> &g, int64_t a, int rows) {
+    const int64_t first = (a + at.rl) * p.f + at.c0, step = p.p.rows_at_once * p.f;
+    x.copy(static_cast<const XT *>(p.x) + first, rows, step);
+    g.copy(static_cast<const GT *>(p.g) + first, rows, step);
 }
 
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
 __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_BACK_RESIDENT)) norm_back_units(NormArgs p) {
     using M = Team<TT>;
-    extern __shared__ __align__(16) float s_all[];
+    constexpr int kRowBytes = VEC * static_cast<int>(sizeof(XT) + sizeof(GT));
+    extern __shared__ __align__(16) char s_all[];
     const uint32_t id = blockIdx.x * M::kPerCta + M::index();
-    const int64_t row = id / static_cast<uint32_t>(p.p.tiles);   // a batch of graphs, then the slots of the shares
+    const int64_t row = id / static_cast<uint32_t>(p.p.tiles);   // a batch of graphs, then the shares
     const int tile = static_cast<int>(id - static_cast<uint32_t>(row) * p.p.tiles);
-    if (row >= p.batches + 2 * p.p.shares) return;          // whole teams
-    float *smem = s_all + M::index() * back_floats(p.p, S, VEC);
+    if (row >= p.batches + p.p.shares) return;              // whole teams
+    char *own = s_all + M::index() * back_bytes(p.p, S, VEC, kRowBytes);
+    float *smem = reinterpret_cast<float *>(own);
+    char *rows_at = own + sum_floats(p.p, 2, S) * 4;
+    const Held<XT, VEC, TT> x(rows_at);
+    const Held<GT, VEC, TT> g(rows_at + p.p.held * TT * VEC * sizeof(XT));
     const Place<TT, VEC, S> at(p, tile);
     Column<VEC, S> c;
     float weight[2][VEC] = {}, s[2][S];
-    const int64_t slot = row - p.batches;
-    Piece piece{0, 0, 0, 0};
-    if (slot >= 0) {
-        piece = find_piece(p, slot >> 1, slot & 1);
-        if (tile == 0 && M::thread() == 0) p.pieces[slot] = piece;
-        if (piece.a == piece.b) return;                     // its channels' row is not read
-    }
+    const int64_t share = row - p.batches;
     c.weights(p, at);
     int buffer = 0;
-    const int64_t first = row * p.batch, stop = slot >= 0 ? first + 1 : min64(p.graphs, first + p.batch);
+    int64_t covered = 0;
+    const int64_t first = row * p.batch, stop = share >= 0 ? first + 2 : min64(p.graphs, first + p.batch);
+    bool any = share < 0;
 #pragma unroll 1
-    for (int64_t graph = first; graph < stop; ++graph) {
-        if (slot < 0) {
+    for (int64_t i = first; i < stop; ++i) {                // graphs, or the share's slots
+        Piece piece{0, 0, i, 0};
+        if (share < 0) {
             bool bad;
-            const RowRange r = graph_rows(p.offsets, graph, p.n, bad);
-            if (r.a == r.b || r.b - r.a > p.p.most) continue;
-            piece = {r.a, r.b, graph, 0};
+            const RowRange r = graph_rows(p.offsets, i, p.n, bad);
+            if (r.b - r.a > p.p.most) continue;
+            piece.a = r.a;
+            piece.b = r.b;
+        } else {
+            piece = find_piece(p, share, static_cast<int>(i - first), covered);
+            if (tile == 0 && M::thread() == 0) p.pieces[share * 2 + i - first] = piece;
         }
+        if (piece.a == piece.b) continue;
+        any = true;
+        const int rows = at.rows(p, piece.a, piece.b);
+        copy_rows(p, at, x, g, piece.a, rows);
         c.statistics(p, at, piece.graph);
-        sums<ACT, XT, GT>(p, at, c, piece.a, piece.b, smem, buffer, s, weight);
+        float slope[VEC];
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) slope[q] = c.gamma[q] * c.rstd[q / (VEC / S)];
+        copies_done();
+        sums<ACT>(p, at, c, slope, x, g, rows, smem, buffer, s, weight);
         buffer ^= 1;
-        if (slot < 0) {
-            const float count = static_cast<float>((piece.b - piece.a) * p.c);
+        if (share < 0) {
+            const float per_value = 1.f / static_cast<float>((piece.b - piece.a) * p.c);
 #pragma unroll
             for (int q = 0; q < S; ++q) {
-                s[0][q] /= count;
-                s[1][q] /= count;
+                s[0][q] *= per_value;
+                s[1][q] *= per_value;
             }
-            gradient<ACT, XT, GT>(p, at, c, piece.a, piece.b, s);
+            gradient<ACT>(p, at, c, slope, x, g, rows, piece.a, s);
         } else {
 #pragma unroll
             for (int q = 0; q < S; ++q)
-                if (at.writes(p, q)) p.part[slot * p.groups + at.group0 + at.grp[q]] = make_float2(s[0][q], s[1][q]);
+                if (at.writes(p, q))
+                    p.part[(share * 2 + i - first) * p.groups + at.group0 + at.grp[q]] = make_float2(s[0][q], s[1][q]);
         }
     }
+    if (!any) return;                                       // a share without pieces: its channels' row is not read
     if (!p.channel_part) return;
     // this team's sums of every channel, over its row lanes in order
     const int t = M::thread(), cols = p.p.cols, rows = p.p.rows_at_once;
@@ -211,7 +219,7 @@ __device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int
 }
 
 // join_apart: the large graph that begins in share blockIdx.x, a warp a group.
-constexpr int kBackJoinWarps = 4;
+constexpr int kBackJoinWarps = 8;
 __global__ void __launch_bounds__(kBackJoinWarps * 32) norm_back_join(NormArgs p) {
     const int64_t s = blockIdx.x;
     Piece piece = p.pieces[s * 2];
@@ -226,7 +234,7 @@ __global__ void __launch_bounds__(kBackJoinWarps * 32) norm_back_join(NormArgs p
 }
 
 // grad_gamma and grad_beta of four channels: the teams' sums, 64 interleaved in order.  Of
-// the rows behind the batches, the shares' slots, those without a piece were not written.
+// the rows behind the batches, the shares', those without a piece were not written.
 constexpr int kChannelCols = 4;
 template <int TT>
 __device__ __forceinline__ void channel_gradients(const NormArgs &p, int64_t c0, float2 (&s_sum)[TT],
@@ -244,8 +252,8 @@ __device__ __forceinline__ void channel_gradients(const NormArgs &p, int64_t c0,
 #pragma unroll 8
         for (int64_t i = line; i < p.batches; i += kLines) add(i);
 #pragma unroll 4
-        for (int64_t i = line; i < 2 * p.p.shares; i += kLines)
-            if (p.pieces[i].a != p.pieces[i].b) add(p.batches + i);
+        for (int64_t i = line; i < p.p.shares; i += kLines)
+            if (p.pieces[2 * i].a != p.pieces[2 * i].b || p.pieces[2 * i + 1].a != p.pieces[2 * i + 1].b) add(p.batches + i);
     }
     s_sum[threadIdx.x] = v;
     __syncthreads();
@@ -264,34 +272,46 @@ __device__ __forceinline__ void channel_gradients(const NormArgs &p, int64_t c0,
 }
 
 // The first channel_ctas CTAs add up the channels' gradients, the others take the pieces of
-// large graphs once more, a CTA a (slot, tile), the last slot first.
+// large graphs once more, a CTA a (share, tile), the last share first.
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
 __global__ void __launch_bounds__(TT, team_ctas(TT, TFG_BACK_RESIDENT))
 norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_beta) {
-    extern __shared__ __align__(16) float s_all[];
+    extern __shared__ __align__(16) char s_all[];
     if (blockIdx.x < channel_ctas) {
         __shared__ float2 s_sum[TT];
         return channel_gradients<TT>(p, static_cast<int64_t>(blockIdx.x) * kChannelCols, s_sum, grad_gamma, grad_beta);
     }
-    float2 *s_stat = reinterpret_cast<float2 *>(s_all);    // [tile's groups]
-    const uint32_t id = blockIdx.x - channel_ctas;
-    const int64_t back = id / static_cast<uint32_t>(p.p.tiles);
-    const int tile = static_cast<int>(id - static_cast<uint32_t>(back) * p.p.tiles);
-    const Piece piece = p.pieces[2 * p.p.shares - 1 - back];
-    if (piece.a == piece.b) return;
-    const Place<TT, VEC, S> at(p, tile);
-    joined_statistics<TT>(p, at, piece, s_stat, join);
-    Column<VEC, S> c;
-    c.weights(p, at);
-    c.statistics(p, at, piece.graph);
-    float s[2][S];
+    const Held<XT, VEC, TT> x(s_all);
+    const Held<GT, VEC, TT> g(s_all + p.p.held * TT * VEC * sizeof(XT));
+    float2 *s_stat = reinterpret_cast<float2 *>(s_all + p.p.held * TT * VEC * (sizeof(XT) + sizeof(GT)));   // [tile's groups]
+    const uint32_t back = (blockIdx.x - channel_ctas) / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(blockIdx.x - channel_ctas - back * p.p.tiles);
+    const int64_t share = p.p.shares - 1 - back;
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        const Piece piece = p.pieces[share * 2 + slot];
+        if (piece.a == piece.b) continue;
+        const Place<TT, VEC, S> at(p, tile);
+        const int rows = at.rows(p, piece.a, piece.b);
+        copy_rows(p, at, x, g, piece.a, rows);
+        Column<VEC, S> c;
+        c.weights(p, at);
+        c.statistics(p, at, piece.graph);
+        __syncthreads();                                    // the last sums have been read
+        joined_statistics<TT>(p, at, piece, s_stat, join);
+        copies_done();
+        float s[2][S];
 #pragma unroll
-    for (int q = 0; q < S; ++q) {
-        const float2 v = s_stat[at.grp[q]];
-        s[0][q] = v.x;
-        s[1][q] = v.y;
+        for (int q = 0; q < S; ++q) {
+            const float2 v = s_stat[at.grp[q]];
+            s[0][q] = v.x;
+            s[1][q] = v.y;
+        }
+        float slope[VEC];
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) slope[q] = c.gamma[q] * c.rstd[q / (VEC / S)];
+        gradient<ACT>(p, at, c, slope, x, g, rows, piece.a, s);
     }
-    gradient<ACT, XT, GT>(p, at, c, piece.a, piece.b, s);
 }
 
 // Graphs of a batch: one, or so many that the batches of all tiles are twice what is
@@ -313,14 +333,16 @@ struct BackLayout {       // of the workspace, in bytes
 BackLayout back_layout(const NormPlan &p, int64_t graphs, int64_t f, int64_t groups) {
     const size_t shares = size_t(p.shares);
     return {shares * 2 * sizeof(Piece), shares * 2 * size_t(groups) * sizeof(float2), shares * size_t(groups) * sizeof(float2),
-            size_t((back_batches(p, graphs) + 2 * p.shares) * f) * sizeof(float2)};
+            size_t((back_batches(p, graphs) + p.shares) * f) * sizeof(float2)};
 }
 
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
 cudaError_t launch_units(const NormArgs &p, cudaStream_t s) {
     using M = Team<TT>;
-    const int smem = M::kPerCta * back_floats(p.p, S, VEC) * static_cast<int>(sizeof(float));
-    const int64_t teams = (p.batches + 2 * p.p.shares) * p.p.tiles;
+    const int smem = M::kPerCta * back_bytes(p.p, S, VEC, VEC * static_cast<int>(sizeof(XT) + sizeof(GT)));
+    const cudaError_t err = allow_shared(norm_back_units<ACT, TT, XT, GT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
+    const int64_t teams = (p.batches + p.p.shares) * p.p.tiles;
     norm_back_units<ACT, TT, XT, GT, VEC, S>
         <<<static_cast<unsigned>((teams + M::kPerCta - 1) / M::kPerCta), M::kThreads, smem, s>>>(p);
     return cudaGetLastError();
@@ -332,13 +354,17 @@ cudaError_t launch_large(NormArgs p, float *grad_gamma, float *grad_beta, cudaSt
         const dim3 grid(static_cast<unsigned>(p.p.shares),
                         static_cast<unsigned>(min64((p.groups + kBackJoinWarps - 1) / kBackJoinWarps, 65535)));
         norm_back_join<<<grid, kBackJoinWarps * 32, 0, s>>>(p);
-        const cudaError_t err = cudaGetLastError();
-        if (err != cudaSuccess) return err;
+        const cudaError_t launched = cudaGetLastError();
+        if (launched != cudaSuccess) return launched;
     }
-    p.p.rows_at_once = TT / p.p.row_vecs;
+    set_rows_at_once(p.p, TT);
+    p.p.held = static_cast<int>((p.p.share + p.p.rows_at_once - 1) / p.p.rows_at_once);
+    if (p.p.shares == 0) p.p.held = 0;                      // channels alone
     const int channel_ctas = grad_gamma ? static_cast<int>((p.f + kChannelCols - 1) / kChannelCols) : 0;
-    const int64_t ctas = channel_ctas + 2 * p.p.shares * p.p.tiles;
-    const int smem = p.p.tile_groups * static_cast<int>(sizeof(float2));
+    const int64_t ctas = channel_ctas + p.p.shares * p.p.tiles;
+    const int smem = p.p.held * TT * VEC * static_cast<int>(sizeof(XT) + sizeof(GT)) + p.p.tile_groups * static_cast<int>(sizeof(float2));
+    const cudaError_t err = allow_shared(norm_back_large<ACT, TT, XT, GT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
     norm_back_large<ACT, TT, XT, GT, VEC, S><<<static_cast<unsigned>(ctas), TT, smem, s>>>(p, channel_ctas, grad_gamma, grad_beta);
     return cudaGetLastError();
 }
@@ -366,17 +392,30 @@ cudaError_t launch_team(const NormArgs &p, int act, float *gg, float *gb, cudaSt
     }
 }
 
-NormPlan back_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, bool aligned) {
-    return norm_plan(n, graphs, f, c, norm_vec(f, c, 4, aligned));
+NormPlan back_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int elems, bool aligned) {
+    const int vec = norm_vec(f, c, 4, aligned);
+    return norm_plan(n, graphs, f, c, vec, 2, vec * elems);
 }
 
 }  // namespace
 
+bool group_norm_backward_fits(int64_t n, int64_t graphs, int64_t f, int64_t groups) {
+    for (const int elems : {8, 6, 4}) {
+        for (const bool aligned : {true, false}) {
+            const NormPlan p = back_plan(n, graphs, f, f / groups, elems, aligned);
+            if ((back_batches(p, graphs) + p.shares) * p.tiles + (f + 3) / 4 > 0x7ff00000) return false;
+        }
+    }
+    return true;
+}
+
 size_t group_norm_backward_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t groups) {
     size_t most = 0;
-    for (const bool aligned : {true, false}) {
-        const size_t bytes = back_layout(back_plan(n, graphs, f, f / groups, aligned), graphs, f, groups).all();
-        if (bytes > most) most = bytes;
+    for (const int elems : {8, 6, 4}) {
+        for (const bool aligned : {true, false}) {
+            const size_t bytes = back_layout(back_plan(n, graphs, f, f / groups, elems, aligned), graphs, f, groups).all();
+            if (bytes > most) most = bytes;
+        }
     }
     return most;
 }
@@ -386,7 +425,8 @@ cudaError_t launch_group_norm_backward(const void *x, int x_dtype, const int64_t
                                        const float *mean, const float *rstd, int act, const void *g, int g_dtype,
                                        void *grad_x, float *grad_gamma, float *grad_beta, void *ws, cudaStream_t s) {
     const bool aligned = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(g) |
-                           reinterpret_cast<uintptr_t>(grad_x)) & 15) == 0;
+                           reinterpret_cast<uintptr_t>(grad_x) | reinterpret_cast<uintptr_t>(gamma) |
+                           reinterpret_cast<uintptr_t>(beta)) & 15) == 0;
     if (graphs == 0 || n == 0) {
         if (!grad_gamma) return cudaSuccess;
         const cudaError_t err = cudaMemsetAsync(grad_gamma, 0, sizeof(float) * size_t(f), s);
@@ -406,7 +446,7 @@ cudaError_t launch_group_norm_backward(const void *x, int x_dtype, const int64_t
     p.rstd_in = rstd;
     p.g = g;
     p.out = grad_x;
-    p.p = back_plan(n, graphs, f, p.c, aligned);
+    p.p = back_plan(n, graphs, f, p.c, (x_dtype == TFG_BF16 ? 2 : 4) + (g_dtype == TFG_BF16 ? 2 : 4), aligned);
     p.batch = back_batch(p.p, graphs);
     p.batches = back_batches(p.p, graphs);
     const BackLayout l = back_layout(p.p, graphs, f, groups);

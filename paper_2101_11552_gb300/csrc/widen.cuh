@@ -14,14 +14,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
-// Makes the compiler take v for new, so that values widened from it in one pass are not
-// kept in registers for the next one (a held bf16 vector would take twice its room).
-__device__ __forceinline__ void renew(uint32_t &v) { asm volatile("" : "+r"(v)); }
-__device__ __forceinline__ void renew(float &v) { asm volatile("" : "+f"(v)); }
-__device__ __forceinline__ void renew(float4 &v) { renew(v.x); renew(v.y); renew(v.z); renew(v.w); }
-__device__ __forceinline__ void renew(uint2 &v) { renew(v.x); renew(v.y); }
-__device__ __forceinline__ void renew(uint4 &v) { renew(v.x); renew(v.y); renew(v.z); renew(v.w); }
-
 // VEC values of a row as they lie in memory, and widened: VecLoad with its eight fp32 values
 // as two 16-byte loads, for rows that are 16-byte but not 32-byte aligned.
 template <typename TT, int VEC> struct RowVec;
@@ -35,14 +27,37 @@ template <> struct RowVec<float, 8> {
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
-    __device__ __forceinline__ void renewed() { renew(a); renew(b); }
 };
 template <typename TT, int VEC> struct RowVec {
     typename VecLoad<TT, VEC>::Raw r;
     __device__ __forceinline__ void load(const TT *p) { r = VecLoad<TT, VEC>::raw(p); }
     __device__ __forceinline__ void widen(float (&v)[VEC]) const { VecLoad<TT, VEC>::widen(r, v); }
-    __device__ __forceinline__ void renewed() { renew(r); }
 };
+
+// A vector by plain loads: from shared memory, or from memory that the kernel also writes.
+template <typename T, int VEC>
+__device__ __forceinline__ typename VecLoad<T, VEC>::Raw load_plain(const T *p) {
+    if constexpr (VEC == 1) {
+        if constexpr (sizeof(T) == 2) return static_cast<uint32_t>(*p) << 16;
+        else return *p;
+    } else {
+        return *reinterpret_cast<const typename VecLoad<T, VEC>::Raw *>(p);
+    }
+}
+
+// Copies of 4, 8 or 16 bytes to shared memory that go on while the thread does; one bf16
+// value is too short for one and is copied at once.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *shared, const void *global) {
+    if constexpr (BYTES == 2) {
+        *static_cast<uint16_t *>(shared) = __ldg(static_cast<const uint16_t *>(global));
+    } else {
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(shared));
+        if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(global) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(global), "n"(BYTES) : "memory");
+    }
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // VEC values to p (fp32, or bf16 bits), p aligned to the vector it is stored as: 16 bytes,
 // or 8 for four bf16 values.  The one rounding of a bf16 result is here.
