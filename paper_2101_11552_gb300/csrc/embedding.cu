@@ -14,44 +14,71 @@ namespace {
 
 // ---- lookup -----------------------------------------------------------------------
 constexpr int kLookupThreads = 256;
-constexpr int kLookupRows = 4;                    // rows in flight per lane
+#ifndef TFG_LOOKUP_ROWS
+#define TFG_LOOKUP_ROWS 4
+#endif
+constexpr int kLookupRows = TFG_LOOKUP_ROWS;      // rows in flight per lane
 
-// 2^log_lanes lanes cover a block of a row's vectors (blockIdx.y: the block), and every
-// lane has kLookupRows rows in flight.  The product is formed in fp32 and rounded once
-// more where the output is bf16.
-template <typename TT, typename OT, int VEC, typename IdT>
+// 2^log_lanes lanes cover a row's vectors side by side.  Rows of up to 32 vectors: every
+// lane has kLookupRows rows in flight.  Wider rows (WIDE): a warp takes kLookupRows
+// blocks of 32 vectors of one row, blockIdx.y the next ones, so that long runs of a row
+// are read and written together.  The product is formed in fp32 and rounded once more
+// where the output is bf16.
+//
+// The status: up to kLookupCheck ids the first CTA of the grid looks through all of them
+// and writes the word (check), which saves the launch that clears it; else every group
+// reports its own.
+constexpr int64_t kLookupCheck = 8192;
+template <typename TT, typename OT, int VEC, bool WIDE, typename IdT>
 __global__ void __launch_bounds__(kLookupThreads)
 embedding_lookup(const IdT *__restrict__ ids, int64_t n, const TT *__restrict__ table, int64_t rows, int64_t f,
-                 int64_t padding, float scale, int log_lanes, OT *__restrict__ out, int32_t *status) {
+                 int64_t padding, float scale, int log_lanes, bool check, OT *__restrict__ out, int32_t *status) {
+    if (check && blockIdx.x == gridDim.x - 1) {
+        bool bad = false;
+        if (blockIdx.y == 0) {
+            for (int64_t i = threadIdx.x; i < n; i += kLookupThreads) {
+                const int64_t id = __ldg(ids + i);
+                bad |= id != padding && (id < 0 || id >= rows);
+            }
+            const int any = __syncthreads_or(bad);
+            if (threadIdx.x == 0) *status = any ? TFG_ERR_INDEX_RANGE : TFG_OK;
+        }
+        return;
+    }
     const int lanes = 1 << log_lanes;
     const int sub = threadIdx.x & (lanes - 1);
     const int64_t group = (static_cast<int64_t>(blockIdx.x) * kLookupThreads + threadIdx.x) >> log_lanes;
-    const int64_t i0 = group * kLookupRows;
+    constexpr int kRows = WIDE ? 1 : kLookupRows, kBlocks = WIDE ? kLookupRows : 1;
+    const int64_t i0 = group * kRows;
     const int64_t vecs = f / VEC;
     if (i0 >= n) return;
-    bool here[kLookupRows];
-    int64_t at[kLookupRows];
+    bool here[kRows];
+    int64_t at[kRows];
 #pragma unroll
-    for (int u = 0; u < kLookupRows; ++u) {
+    for (int u = 0; u < kRows; ++u) {
         here[u] = false;
         at[u] = 0;
         if (i0 + u < n) {
             const int64_t id = __ldg(ids + i0 + u);
             here[u] = id != padding && id >= 0 && id < rows;
             at[u] = here[u] ? id * f : 0;
-            if (!here[u] && id != padding && sub == 0 && blockIdx.y == 0) set_status(status, TFG_ERR_INDEX_RANGE);
+            if (!check && !here[u] && id != padding && sub == 0 && blockIdx.y == 0) set_status(status, TFG_ERR_INDEX_RANGE);
         }
     }
-    for (int64_t c = static_cast<int64_t>(blockIdx.y) * lanes + sub; c < vecs; c += static_cast<int64_t>(gridDim.y) * lanes) {
+    const int64_t stride = static_cast<int64_t>(gridDim.y) * kBlocks * lanes;
+    for (int64_t c0 = static_cast<int64_t>(blockIdx.y) * kBlocks * lanes + sub; c0 < vecs; c0 += stride) {
         RowVec<TT, VEC> r[kLookupRows];
 #pragma unroll
-        for (int u = 0; u < kLookupRows; ++u)
-            if (here[u]) r[u].load(table + at[u] + c * VEC);
+        for (int u = 0; u < kLookupRows; ++u) {
+            const int64_t c = c0 + (WIDE ? u * lanes : 0);
+            if (here[WIDE ? 0 : u] && c < vecs) r[u].load(table + at[WIDE ? 0 : u] + c * VEC);
+        }
 #pragma unroll
         for (int u = 0; u < kLookupRows; ++u) {
-            if (i0 + u >= n) continue;
+            const int64_t c = c0 + (WIDE ? u * lanes : 0), i = i0 + (WIDE ? 0 : u);
+            if (i >= n || c >= vecs) continue;
             float v[VEC];
-            if (here[u]) {
+            if (here[WIDE ? 0 : u]) {
                 r[u].widen(v);
 #pragma unroll
                 for (int q = 0; q < VEC; ++q) v[q] *= scale;
@@ -59,7 +86,7 @@ embedding_lookup(const IdT *__restrict__ ids, int64_t n, const TT *__restrict__ 
 #pragma unroll
                 for (int q = 0; q < VEC; ++q) v[q] = 0.f;
             }
-            store_vec<VEC>(out + (i0 + u) * f + c * VEC, v);
+            store_vec<VEC>(out + i * f + c * VEC, v);
         }
     }
 }
@@ -74,12 +101,14 @@ template <typename TT, typename OT, int VEC, typename IdT>
 cudaError_t lookup_vec(const void *ids, int64_t n, const void *table, int64_t rows, int64_t f, int64_t padding,
                        float scale, void *out, int32_t *status, cudaStream_t s) {
     const int l = log_lanes_for(f / VEC);
-    const int64_t per_cta = (kLookupThreads >> l) * kLookupRows;
-    const int64_t blocks = (f / VEC + (int64_t(1) << l) - 1) >> l;
-    const dim3 grid(static_cast<unsigned>((n + per_cta - 1) / per_cta), static_cast<unsigned>(min64(blocks, 65535)));
-    embedding_lookup<TT, OT, VEC, IdT><<<grid, kLookupThreads, 0, s>>>(
-        static_cast<const IdT *>(ids), n, static_cast<const TT *>(table), rows, f, padding, scale, l,
-        static_cast<OT *>(out), status);
+    const bool wide = f / VEC > 32, check = n <= kLookupCheck;
+    const int64_t per_cta = (kLookupThreads >> l) * (wide ? 1 : kLookupRows);
+    const int64_t block = wide ? 32 * kLookupRows : 32;
+    const int64_t blocks = (f / VEC + block - 1) / block;
+    const dim3 grid(static_cast<unsigned>((n + per_cta - 1) / per_cta + (check ? 1 : 0)), static_cast<unsigned>(min64(blocks, 65535)));
+    auto *kernel = wide ? embedding_lookup<TT, OT, VEC, true, IdT> : embedding_lookup<TT, OT, VEC, false, IdT>;
+    kernel<<<grid, kLookupThreads, 0, s>>>(static_cast<const IdT *>(ids), n, static_cast<const TT *>(table), rows, f,
+                                           padding, scale, l, check, static_cast<OT *>(out), status);
     return cudaGetLastError();
 }
 
@@ -119,8 +148,17 @@ cudaError_t lookup_ids(const void *ids, int64_t n, const void *table, int table_
 // that cross CTAs leave one part per CTA in the workspace, added by embedding_grad_join.
 // Every CTA also writes the zeros of its share of the rows that no id names.  Fixed
 // order, fp32, no atomics.
-constexpr int kGradThreads = 512;
-constexpr int kGradCtas = 304;                    // two a multiprocessor
+#ifndef TFG_GRAD_THREADS
+#define TFG_GRAD_THREADS 512
+#endif
+#ifndef TFG_GRAD_DEPTH
+#define TFG_GRAD_DEPTH 8
+#endif
+#ifndef TFG_GRAD_PER_SM
+#define TFG_GRAD_PER_SM 2
+#endif
+constexpr int kGradThreads = TFG_GRAD_THREADS;
+constexpr int kGradCtas = 152 * TFG_GRAD_PER_SM;
 constexpr int kGradMinShare = 8;                  // positions a worker should have at least
 
 struct GradArgs {
@@ -138,11 +176,11 @@ __device__ __forceinline__ int64_t grad_share(int64_t named, int64_t workers) {
 }
 
 template <typename GT, int VEC, int LPR, int T>
-__global__ void __launch_bounds__(kGradThreads, 2) embedding_grad(GradArgs a) {
+__global__ void __launch_bounds__(kGradThreads, TFG_GRAD_PER_SM) embedding_grad(GradArgs a) {
     using V = VecLoad<GT, VEC>;
     constexpr int NW = kGradThreads / LPR;        // workers
     constexpr int kCols = LPR * VEC * T;
-    constexpr int D = T > 1 ? 4 : 8;
+    constexpr int D = T > 1 ? TFG_GRAD_DEPTH / 2 : TFG_GRAD_DEPTH;
     extern __shared__ __align__(16) float s_part[];   // tails [worker][kCols], heads [worker][kCols]
     float *s_tail = s_part, *s_head = s_part + NW * kCols;
     const int sub = threadIdx.x % LPR, w = threadIdx.x / LPR;
@@ -360,8 +398,10 @@ cudaError_t launch_grad_lanes(const GradArgs &a, const GradPlan &p, cudaStream_t
 cudaError_t launch_embedding_lookup(const void *ids, bool id32, int64_t n, const void *table, int table_dtype,
                                     int64_t rows, int64_t f, float scale, int64_t padding, void *out, int out_dtype,
                                     int32_t *status, cudaStream_t s) {
-    const cudaError_t err = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
-    if (err != cudaSuccess || n == 0) return err;
+    if (n == 0 || n > kLookupCheck) {
+        const cudaError_t err = cudaMemsetAsync(status, 0, sizeof(int32_t), s);
+        if (err != cudaSuccess || n == 0) return err;
+    }
     return id32 ? lookup_ids<int32_t>(ids, n, table, table_dtype, rows, f, padding, scale, out, out_dtype, status, s)
                 : lookup_ids<int64_t>(ids, n, table, table_dtype, rows, f, padding, scale, out, out_dtype, status, s);
 }

@@ -172,6 +172,20 @@ write_norm(const double *__restrict__ partial, int n, float *__restrict__ norm) 
 
 // ---- scaling ----------------------------------------------------------------------
 // Plain loads: out may be the tensor itself, and then what is read is written here.
+// Stores that leave L2 first: what the pass has yet to read stays.
+template <int VEC>
+__device__ __forceinline__ void store_stream(float *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 4) __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
+    else store_vec<VEC>(p, v);
+}
+template <int VEC>
+__device__ __forceinline__ void store_stream(uint16_t *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 8)
+        __stcs(reinterpret_cast<uint4 *>(p), make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+                                                        pack_bf16(v[6], v[7])));
+    else store_vec<VEC>(p, v);
+}
+
 template <typename T, int VEC>
 __device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, float factor) {
     constexpr int kLoads = 32 / VEC;
@@ -194,7 +208,7 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, int64_t left, floa
             VecLoad<T, VEC>::widen(raw[i], v);
 #pragma unroll
             for (int q = 0; q < VEC; ++q) v[q] *= factor;
-            store_vec<VEC>(o + at, v);
+            store_stream<VEC>(o + at, v);
         }
     }
     if (VEC > 1 && left < kChunk && static_cast<int64_t>(threadIdx.x) < left % VEC) {
@@ -226,9 +240,9 @@ scale_by_norm(const __grid_constant__ TensorList<CAP> list, const double *__rest
     __syncthreads();
     const float factor = s_factor;
     const int64_t chunks = list.first[list.count];
-    int t = 0;
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        t = tensor_of(list, c, t);
+    for (int64_t back = blockIdx.x; back < chunks; back += gridDim.x) {
+        const int64_t c = chunks - 1 - back;      // the last chunks first: L2 still holds them
+        const int t = tensor_of(list, c, 0);
         if (factor == 1.f && list.in[t] == list.out[t]) continue;      // in place and nothing to do
         const int64_t at = (c - list.first[t]) * kChunk;
         const int64_t left = min64(kChunk, list.size[t] - at);

@@ -5,26 +5,35 @@
 //
 // A stable least-significant-digit radix sort of (key, position) pairs, digits of at most
 // 9 bits, in tiles of 2,048 pairs.  Positions that take part in nothing (the padding id,
-// ids outside the table) get the key `rows`, behind every row.  A pass is
-//   upsweep    a tile's digit counts -> cnt[digit][tile]
+// ids outside the table) get the key `rows`, behind every row.
+//   upsweep    a tile's digit counts
 //   scan       exclusive sums over the tiles of each digit, and the digit's total
 //              (only where there are more than kDirectTiles tiles: up to there the
-//              downsweep adds the counts up itself, which saves a launch)
+//              downsweep adds the counts up itself, which saves a launch; the counts
+//              lie [tile][digit] then, a thread a digit, and [digit][tile] for the scan,
+//              a warp a digit)
 //   downsweep  ranks a tile's pairs, stages them in shared memory in digit order and
 //              writes each digit's run with coalesced stores
-// and the row boundaries are found by binary search in the sorted keys.  The status word
-// is written by that last kernel from one flag per tile, so nothing has to be cleared.
-// No kernel waits on another CTA.
+// A list of one tile is sorted by one CTA in shared memory, all digits in one launch.
+// The row boundaries are found by search in the sorted keys, a warp a row where rows are
+// long, else a thread a row between the ends that its warp has found.  The status word is
+// written by that last kernel from one flag per tile, so nothing has to be cleared.  No
+// kernel waits on another CTA.
+//
+// What bounds it: launches and round trips (60,000 ids of 169,343 rows, two digits: five
+// launches for 0.7 MB).  Counting the next digit with atomics in the downsweep instead of
+// an upsweep of its own took as long, and longer where one id is frequent.
 #include "common.cuh"
 
 namespace tfg {
 namespace {
 
-constexpr int kGroupThreads = 256;
+constexpr int kGroupThreads = 512;                // a thread a digit; 256 took a second round of loads for 9 bits
 constexpr int kGroupWarps = kGroupThreads / 32;
-constexpr int kGroupItems = 8;
+constexpr int kGroupItems = 4;
 constexpr int kGroupTile = kGroupThreads * kGroupItems;
 constexpr int kGroupBits = 9;                     // most bits of a digit
+static_assert(kGroupThreads == 1 << kGroupBits, "every digit has a thread of its own");
 constexpr int kDirectTiles = 64;
 
 struct GroupPlan {
@@ -54,25 +63,28 @@ __device__ __forceinline__ uint32_t group_key(IdT id, int64_t rows, int64_t padd
 template <bool FIRST, typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
 group_upsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int64_t padding,
-              int shift, int width, int tiles, int32_t *__restrict__ cnt, int32_t *__restrict__ bad_tile) {
+              int shift, int width, int tiles, bool direct, int32_t *__restrict__ cnt, int32_t *__restrict__ bad_tile) {
     __shared__ int32_t s_cnt[1 << kGroupBits];
     const int radix = 1 << width;
-    for (int d = threadIdx.x; d < radix; d += kGroupThreads) s_cnt[d] = 0;
+    s_cnt[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t base = static_cast<int64_t>(blockIdx.x) * kGroupTile;
+    const int64_t base = static_cast<int64_t>(blockIdx.x) * kGroupTile + threadIdx.x;
     bool bad = false;
+    uint32_t key[kGroupItems];
 #pragma unroll
     for (int i = 0; i < kGroupItems; ++i) {
-        const int64_t at = base + i * kGroupThreads + threadIdx.x;
-        if (at < n) {
-            const uint32_t key = FIRST ? group_key(__ldg(ids + at), rows, padding, bad) : __ldg(keys + at);
-            atomicAdd(&s_cnt[(key >> shift) & (radix - 1)], 1);
-        }
+        const int64_t at = base + i * kGroupThreads;
+        key[i] = 0;
+        if (at < n) key[i] = FIRST ? group_key(__ldg(ids + at), rows, padding, bad) : __ldg(keys + at);
     }
+#pragma unroll
+    for (int i = 0; i < kGroupItems; ++i)
+        if (base + i * kGroupThreads < n) atomicAdd(&s_cnt[(key[i] >> shift) & (radix - 1)], 1);
     const int any_bad = __syncthreads_or(bad);
     if (FIRST && threadIdx.x == 0) bad_tile[blockIdx.x] = any_bad;
-    for (int d = threadIdx.x; d < radix; d += kGroupThreads)
-        cnt[static_cast<int64_t>(d) * tiles + blockIdx.x] = s_cnt[d];
+    if (threadIdx.x < radix)
+        cnt[direct ? static_cast<int64_t>(blockIdx.x) * radix + threadIdx.x
+                   : static_cast<int64_t>(threadIdx.x) * tiles + blockIdx.x] = s_cnt[threadIdx.x];
 }
 
 // One warp a digit: cnt[digit][tile] becomes the pairs of the digit in earlier tiles.
@@ -116,6 +128,63 @@ __device__ __forceinline__ int32_t scan_threads(int32_t v, int32_t *s_warp) {
     return before + incl - v;
 }
 
+// A tile's pairs in registers, warp by warp and round by round in original order.
+struct TilePairs {
+    uint32_t key[kGroupItems];
+    int32_t pos[kGroupItems], rank[kGroupItems];
+    static __device__ __forceinline__ int at(int r) {
+        return (threadIdx.x >> 5) * 32 * kGroupItems + r * 32 + (threadIdx.x & 31);
+    }
+
+    // rank[r]: the warp's earlier pairs of the same digit; mine[digit]: the warp's pairs of
+    // it.  Lanes with equal digits are found with one ballot per bit, and the first of them
+    // advances the warp's counter.
+    __device__ __forceinline__ void rank_digits(int count, int shift, int width, uint16_t *mine) {
+        const int lane = threadIdx.x & 31;
+        for (int d = lane; d < 1 << width; d += 32) mine[d] = 0;
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < kGroupItems; ++r) {
+            const bool ok = at(r) < count;
+            const uint32_t dig = (key[r] >> shift) & ((1u << width) - 1u);
+            unsigned peers = lane_ballot(ok);
+            for (int b = 0; b < width; ++b) {
+                const bool set = (dig >> b) & 1u;
+                const unsigned bal = lane_ballot(set);
+                peers &= set ? bal : ~bal;
+            }
+            const int leader = ok ? __ffs(peers) - 1 : lane;
+            int32_t base = 0;
+            if (ok && lane == leader) {
+                base = mine[dig];
+                mine[dig] = static_cast<uint16_t>(base + __popc(peers));
+            }
+            base = lane_get(base, leader);
+            rank[r] = base + __popc(peers & ((1u << lane) - 1u));
+            __syncwarp();
+        }
+    }
+};
+
+using TileCounts = uint16_t[kGroupWarps][1 << kGroupBits];      // at most 2,048: 16 bits
+
+// The tile's pairs of digit d.
+__device__ __forceinline__ int32_t tile_count(const TileCounts &mine, int d) {
+    int32_t here = 0;
+#pragma unroll
+    for (int w = 0; w < kGroupWarps; ++w) here += mine[w][d];
+    return here;
+}
+// Turns the warps' counts of digit d into the slots where their pairs begin.
+__device__ __forceinline__ void place_warps(TileCounts &mine, int d, int32_t slot) {
+#pragma unroll
+    for (int w = 0; w < kGroupWarps; ++w) {
+        const int32_t c = mine[w][d];
+        mine[w][d] = static_cast<uint16_t>(slot);
+        slot += c;
+    }
+}
+
 template <bool FIRST, bool DIRECT, typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
 group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in, const int32_t *__restrict__ pos_in,
@@ -124,103 +193,55 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
                 int32_t *__restrict__ pos_out) {
     __shared__ uint32_t s_key[kGroupTile];
     __shared__ int32_t s_pos[kGroupTile];
-    __shared__ int32_t s_mine[kGroupWarps][1 << kGroupBits];
+    __shared__ TileCounts s_mine;
     __shared__ int32_t s_delta[1 << kGroupBits];
     __shared__ int32_t s_warp[kGroupWarps];
-    const int radix = 1 << width;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int radix = 1 << width, d = threadIdx.x;
+    const int warp = threadIdx.x >> 5;
     const int64_t tile0 = static_cast<int64_t>(blockIdx.x) * kGroupTile;
     const int count = static_cast<int>(min64(kGroupTile, n - tile0));
-    int32_t *mine = s_mine[warp];
-    for (int d = lane; d < radix; d += 32) mine[d] = 0;
-    // the warp's 256 pairs, in original order round by round
-    uint32_t keys[kGroupItems];
-    int32_t pos[kGroupItems], rank[kGroupItems];
+    TilePairs t;
     bool bad = false;
 #pragma unroll
     for (int r = 0; r < kGroupItems; ++r) {
-        const int64_t at = tile0 + warp * 32 * kGroupItems + r * 32 + lane;
-        keys[r] = 0;
-        pos[r] = 0;
-        if (at < n) {
-            keys[r] = FIRST ? group_key(__ldg(ids + at), rows, padding, bad) : __ldg(key_in + at);
-            pos[r] = FIRST ? static_cast<int32_t>(at) : __ldg(pos_in + at);
+        const int i = t.at(r);
+        t.key[r] = 0;
+        t.pos[r] = 0;
+        if (i < count) {
+            t.key[r] = FIRST ? group_key(__ldg(ids + tile0 + i), rows, padding, bad) : __ldg(key_in + tile0 + i);
+            t.pos[r] = FIRST ? static_cast<int32_t>(tile0 + i) : __ldg(pos_in + tile0 + i);
         }
     }
-    __syncwarp();
-    // rank among the warp's earlier pairs of the digit: lanes with equal digits are found
-    // with one ballot per bit, and the first of them advances the warp's counter
-#pragma unroll
-    for (int r = 0; r < kGroupItems; ++r) {
-        const bool ok = warp * 32 * kGroupItems + r * 32 + lane < count;
-        const uint32_t dig = (keys[r] >> shift) & (radix - 1);
-        unsigned peers = lane_ballot(ok);
-        for (int b = 0; b < width; ++b) {
-            const bool set = (dig >> b) & 1u;
-            const unsigned bal = lane_ballot(set);
-            peers &= set ? bal : ~bal;
+    // this thread's digit: its pairs in all tiles and in earlier ones
+    int32_t all = 0, earlier = 0;
+    if (d < radix) {
+        if (DIRECT) {
+#pragma unroll 32
+            for (int i = 0; i < tiles; ++i) {
+                const int32_t c = __ldg(cnt + i * radix + d);
+                all += c;
+                earlier += i < static_cast<int>(blockIdx.x) ? c : 0;
+            }
+        } else {
+            earlier = __ldg(cnt + static_cast<int64_t>(d) * tiles + blockIdx.x);
+            all = __ldg(total + d);
         }
-        const int leader = ok ? __ffs(peers) - 1 : lane;
-        int32_t base = 0;
-        if (ok && lane == leader) {
-            base = mine[dig];
-            mine[dig] = base + __popc(peers);
-        }
-        base = lane_get(base, leader);
-        rank[r] = base + __popc(peers & ((1u << lane) - 1u));
-        __syncwarp();
     }
+    t.rank_digits(count, shift, width, s_mine[warp]);
     __syncthreads();
-    // per digit: the tile's first slot of it, and how far its run lies from there in the output
-    int32_t slot0 = 0, out0 = 0;
-    for (int d0 = 0; d0 < radix; d0 += kGroupThreads) {
-        const int d = d0 + threadIdx.x;
-        int32_t here = 0, all = 0, earlier = 0;
-        if (d < radix) {
-#pragma unroll
-            for (int w = 0; w < kGroupWarps; ++w) {
-                const int32_t c = s_mine[w][d];
-                s_mine[w][d] = here;
-                here += c;
-            }
-            const int32_t *row = cnt + static_cast<int64_t>(d) * tiles;
-            if (DIRECT) {
-#pragma unroll 8
-                for (int t = 0; t < tiles; ++t) {
-                    const int32_t c = __ldg(row + t);
-                    all += c;
-                    earlier += t < static_cast<int>(blockIdx.x) ? c : 0;
-                }
-            } else {
-                earlier = __ldg(row + blockIdx.x);
-                all = __ldg(total + d);
-            }
-        }
-        const int32_t slot = slot0 + scan_threads(here, s_warp);
-        const int32_t out = out0 + scan_threads(all, s_warp);
-        if (d < radix) {
-#pragma unroll
-            for (int w = 0; w < kGroupWarps; ++w) s_mine[w][d] += slot;
-            s_delta[d] = out + earlier - slot;
-        }
-        if (d0 + kGroupThreads < radix) {         // the next 256 digits begin where these end
-            __shared__ int32_t s_end[2];
-            if (threadIdx.x == kGroupThreads - 1) {
-                s_end[0] = slot + here;
-                s_end[1] = out + all;
-            }
-            __syncthreads();
-            slot0 = s_end[0];
-            out0 = s_end[1];
-        }
+    const int32_t here = d < radix ? tile_count(s_mine, d) : 0;
+    const int32_t slot0 = scan_threads(here, s_warp), out0 = scan_threads(all, s_warp);
+    if (d < radix) {
+        place_warps(s_mine, d, slot0);
+        s_delta[d] = out0 + earlier - slot0;      // from a slot of the tile to its place in the output
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kGroupItems; ++r) {
-        if (warp * 32 * kGroupItems + r * 32 + lane < count) {
-            const int slot = mine[(keys[r] >> shift) & (radix - 1)] + rank[r];
-            s_key[slot] = keys[r];
-            s_pos[slot] = pos[r];
+        if (t.at(r) < count) {
+            const int slot = s_mine[warp][(t.key[r] >> shift) & (radix - 1)] + t.rank[r];
+            s_key[slot] = t.key[r];
+            s_pos[slot] = t.pos[r];
         }
     }
     __syncthreads();
@@ -236,20 +257,100 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
     }
 }
 
+// One tile, all digits.
+template <typename IdT>
+__global__ void __launch_bounds__(kGroupThreads)
+group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, int passes, int width,
+           int32_t *__restrict__ sorted_ids, int32_t *__restrict__ perm, int32_t *__restrict__ bad_tile) {
+    __shared__ uint32_t s_key[kGroupTile];
+    __shared__ int32_t s_pos[kGroupTile];
+    __shared__ TileCounts s_mine;
+    __shared__ int32_t s_warp[kGroupWarps];
+    const int radix = 1 << width, d = threadIdx.x;
+    const int warp = threadIdx.x >> 5;
+    TilePairs t;
+    bool bad = false;
+#pragma unroll
+    for (int r = 0; r < kGroupItems; ++r) {
+        const int i = t.at(r);
+        t.key[r] = i < n ? group_key(__ldg(ids + i), rows, padding, bad) : 0u;
+        t.pos[r] = i;
+    }
+    const int any_bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) bad_tile[0] = any_bad;
+    for (int pass = 0; pass < passes; ++pass) {
+        t.rank_digits(n, pass * width, width, s_mine[warp]);
+        __syncthreads();
+        const int32_t slot0 = scan_threads(d < radix ? tile_count(s_mine, d) : 0, s_warp);
+        if (d < radix) place_warps(s_mine, d, slot0);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kGroupItems; ++r) {
+            if (t.at(r) < n) {
+                const int slot = s_mine[warp][(t.key[r] >> (pass * width)) & (radix - 1)] + t.rank[r];
+                s_key[slot] = t.key[r];
+                s_pos[slot] = t.pos[r];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kGroupItems; ++r) {
+            if (t.at(r) < n) {
+                t.key[r] = s_key[t.at(r)];
+                t.pos[r] = s_pos[t.at(r)];
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < kGroupItems; ++r) {
+        if (t.at(r) < n) {
+            sorted_ids[t.at(r)] = static_cast<int32_t>(t.key[r]);
+            perm[t.at(r)] = t.pos[r];
+        }
+    }
+}
+
+// First sorted position in [lo, hi] whose key is at least k, by the whole warp (hi if there
+// is none before it): 32 probes a round.
+__device__ __forceinline__ int64_t warp_first_at(const uint32_t *keys, int64_t lo, int64_t hi, int64_t k) {
+    const int lane = threadIdx.x & 31;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 31) / 32;
+        const int64_t p = lo + lane * step;                     // probes in [lo, hi)
+        const bool less = p < hi && static_cast<int64_t>(__ldg(keys + p)) < k;
+        const int c = __popc(lane_ballot(less));                // monotone: lanes 0 .. c - 1
+        if (c == 0) return lo;
+        const int64_t top = lo + c * step;
+        lo = lo + (c - 1) * step + 1;
+        hi = top < hi ? top : hi;
+    }
+    return lo;
+}
+
 // rowptr[k] = first sorted position whose key is at least k, for k in [0, rows]; the first
-// CTA also writes the status.
+// CTA also writes the status.  WARP: a warp a row (long rows: 32 keys a warp would search
+// most of the list each); else a thread a row.
+template <bool WARP>
 __global__ void __launch_bounds__(kGroupThreads)
 group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int32_t *__restrict__ rowptr,
              const int32_t *__restrict__ bad_tile, int tiles, int32_t *__restrict__ status) {
-    const int64_t k = static_cast<int64_t>(blockIdx.x) * kGroupThreads + threadIdx.x;
-    if (k <= rows) {
-        int64_t lo = 0, hi = n;
+    const int lane = threadIdx.x & 31;
+    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kGroupThreads + threadIdx.x) >> 5;
+    if (WARP) {
+        if (warp <= rows) {
+            const int64_t at = warp_first_at(keys, 0, n, warp);
+            if (lane == 0) rowptr[warp] = static_cast<int32_t>(at);
+        }
+    } else if (warp * 32 <= rows) {
+        const int64_t k = warp * 32 + lane;
+        int64_t lo = warp_first_at(keys, 0, n, warp * 32), hi = warp_first_at(keys, lo, n, warp * 32 + 31);
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
             if (static_cast<int64_t>(__ldg(keys + mid)) < k) lo = mid + 1;
             else hi = mid;
         }
-        rowptr[k] = static_cast<int32_t>(lo);
+        if (k <= rows) rowptr[k] = static_cast<int32_t>(lo);
     }
     if (blockIdx.x == 0) {
         bool bad = false;
@@ -264,10 +365,12 @@ group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int32_t
 size_t group_ids_workspace_bytes(int64_t rows, int64_t n) {
     if (n <= 0) return 256;
     const GroupPlan p = group_plan(rows, n);
-    const size_t pairs = p.passes > 1 ? 2 * round256(sizeof(int32_t) * size_t(n)) : 0;
-    const size_t spare = p.passes > 2 ? pairs : 0;
-    return pairs + spare + round256(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width)) +
-           round256(sizeof(int32_t) << p.width) + round256(sizeof(int32_t) * size_t(p.tiles));
+    const size_t flags = round256(sizeof(int32_t) * size_t(p.tiles));
+    if (p.tiles == 1) return flags;
+    const size_t pairs = 2 * round256(sizeof(int32_t) * size_t(n));
+    const size_t counters = round256(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width));
+    const int buffers = p.passes > 2 ? 2 : p.passes - 1;
+    return flags + buffers * pairs + counters + round256(sizeof(int32_t) << p.width);
 }
 
 namespace {
@@ -275,14 +378,20 @@ template <typename IdT>
 cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padding, int32_t *rowptr,
                            int32_t *sorted_ids, int32_t *perm, void *ws, int32_t *status, cudaStream_t s) {
     const GroupPlan p = n > 0 ? group_plan(rows, n) : GroupPlan{0, 0, 0};
-    const int32_t *bad = nullptr;
-    if (n > 0) {
-        char *w = static_cast<char *>(ws);
-        auto take = [&w](size_t bytes) {
-            char *at = w;
-            w += round256(bytes);
-            return at;
-        };
+    int32_t *bad_tile = nullptr;
+    char *w = static_cast<char *>(ws);
+    auto take = [&w](size_t bytes) {
+        char *at = w;
+        w += round256(bytes);
+        return at;
+    };
+    if (n > 0) bad_tile = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles)));
+    if (p.tiles == 1) {
+        group_tile<<<1, kGroupThreads, 0, s>>>(ids, static_cast<int>(n), rows, padding, p.passes, p.width, sorted_ids, perm,
+                                               bad_tile);
+        const cudaError_t err = cudaGetLastError();
+        if (err != cudaSuccess) return err;
+    } else if (n > 0) {
         // odd and even passes write to buffers of their own, the last one to the caller's
         uint32_t *key_buf[2] = {nullptr, nullptr};
         int32_t *pos_buf[2] = {nullptr, nullptr};
@@ -292,29 +401,26 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
         }
         int32_t *cnt = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width)));
         int32_t *total = reinterpret_cast<int32_t *>(take(sizeof(int32_t) << p.width));
-        int32_t *bad_tile = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles)));
-        bad = bad_tile;
         const bool direct = p.tiles <= kDirectTiles;
         const int radix = 1 << p.width;
         const uint32_t *key_in = nullptr;
-        const int32_t *pos_in = nullptr;
+        const int32_t *pos_in = nullptr, *none = nullptr;
         for (int pass = 0; pass < p.passes; ++pass) {
-            const int shift = pass * p.width;
             const bool first = pass == 0, last = pass == p.passes - 1;
+            const int shift = pass * p.width;
             uint32_t *key_out = last ? reinterpret_cast<uint32_t *>(sorted_ids) : key_buf[pass & 1];
             int32_t *pos_out = last ? perm : pos_buf[pass & 1];
             if (first)
-                group_upsweep<true, IdT><<<p.tiles, kGroupThreads, 0, s>>>(ids, nullptr, n, rows, padding, shift, p.width,
-                                                                           p.tiles, cnt, bad_tile);
+                group_upsweep<true><<<p.tiles, kGroupThreads, 0, s>>>(ids, key_in, n, rows, padding, shift, p.width, p.tiles, direct,
+                                                                      cnt, bad_tile);
             else
-                group_upsweep<false, int32_t><<<p.tiles, kGroupThreads, 0, s>>>(nullptr, key_in, n, rows, padding, shift,
-                                                                                p.width, p.tiles, cnt, bad_tile);
+                group_upsweep<false><<<p.tiles, kGroupThreads, 0, s>>>(none, key_in, n, rows, padding, shift, p.width, p.tiles,
+                                                                       direct, cnt, bad_tile);
             if (!direct) group_scan<<<ceil_div(radix, kGroupWarps), kGroupThreads, 0, s>>>(cnt, p.tiles, radix, total);
             auto down = [&](auto *kernel, const auto *id) {
                 kernel<<<p.tiles, kGroupThreads, 0, s>>>(id, key_in, pos_in, n, rows, padding, shift, p.width, p.tiles, cnt,
                                                          total, key_out, pos_out);
             };
-            const int32_t *none = nullptr;
             if (first && direct) down(group_downsweep<true, true, IdT>, ids);
             else if (first) down(group_downsweep<true, false, IdT>, ids);
             else if (direct) down(group_downsweep<false, true, int32_t>, none);
@@ -325,8 +431,11 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
             pos_in = pos_out;
         }
     }
-    group_bounds<<<ceil_div(rows + 1, kGroupThreads), kGroupThreads, 0, s>>>(
-        reinterpret_cast<const uint32_t *>(sorted_ids), n, rows, rowptr, bad, p.tiles, status);
+    const uint32_t *keys = reinterpret_cast<const uint32_t *>(sorted_ids);
+    if (n > 32 * rows)
+        group_bounds<true><<<ceil_div(rows + 1, kGroupWarps), kGroupThreads, 0, s>>>(keys, n, rows, rowptr, bad_tile, p.tiles, status);
+    else
+        group_bounds<false><<<ceil_div(rows + 1, kGroupThreads), kGroupThreads, 0, s>>>(keys, n, rows, rowptr, bad_tile, p.tiles, status);
     return cudaGetLastError();
 }
 }  // namespace

@@ -498,7 +498,7 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     if (p.share < few) p.share = few;
     if (p.share > p.most || 2 * mean <= p.most) p.share = p.most;
     p.shares = n <= p.most ? 0 : (n + p.share - 1) / p.share;
-    p.join_apart = mean > 8 * p.share;
+    p.join_apart = mean > 8 * p.share && p.shares * (f / c) >= 2048;
     return p;
 }
 

@@ -61,8 +61,18 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;
 
 // VEC values to p (fp32, or bf16 bits), p aligned to the vector it is stored as: 16 bytes,
 // or 8 for four bf16 values.  The one rounding of a bf16 result is here.
+// Eight fp32 values go out as one 32-byte store where p allows it: as two, every lane's half
+// sectors go to L2 by themselves.
 template <int VEC>
 __device__ __forceinline__ void store_vec(float *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 8) {
+        if (reinterpret_cast<uintptr_t>(p) % 32 == 0) {
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                         "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                         : "memory");
+            return;
+        }
+    }
     if constexpr (VEC % 4 == 0) {
 #pragma unroll
         for (int q = 0; q < VEC; q += 4)

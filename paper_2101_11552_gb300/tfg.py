@@ -15,6 +15,7 @@ from __future__ import annotations
 import array
 import ctypes
 import math
+import operator
 import os
 import threading
 from typing import NamedTuple, Optional
@@ -670,47 +671,90 @@ def tfg_dot_edge_softmax_aggregate_backward(rowptr, col, rowptr_src, col_src, q,
     return tuple(grads)
 
 
-def _run(dev: torch.device, fn, *args):
-    """Call the C entry point with ``dev`` as the current device (its stream is dev's)."""
-    if dev.index == torch.cuda.current_device():
-        _check(fn(*args))
+# The calls below are often as short as a few microseconds on the device, so their host side
+# is kept short too: pointers go to ctypes as integers, a tensor's device is compared by
+# its index, and the current stream is taken as the raw handle.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+_DTYPES = {torch.float32: TFG_F32, torch.bfloat16: TFG_BF16}
+_IDS = {torch.int64: False, torch.int32: True}
+
+
+def _run(index: int, name: str, *args):
+    """Call the C entry point ``name`` on the current stream of device ``index``."""
+    fn = getattr(_lib or lib(), name)
+    if index == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(dev):
-            _check(fn(*args))
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
+    if rc != TFG_OK:
+        raise TfgError(rc, tfg_last_error())
 
 
-def _dtype_code(dtype: torch.dtype) -> int:
-    if dtype == torch.float32:
-        return TFG_F32
-    if dtype == torch.bfloat16:
-        return TFG_BF16
-    raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
-def _workspace(workspace, need: int, dev: torch.device):
-    """The caller's workspace, checked for its kind, or a new one."""
+def _index(name: str, t: torch.Tensor) -> int:
+    """The CUDA device index of a contiguous tensor."""
+    try:
+        index = t.get_device()
+        if index >= 0 and t.is_contiguous():
+            return index
+    except AttributeError:                        # no tensor at all
+        index = -1
+    raise ValueError(f"{name} must be contiguous" if index >= 0 else f"{name} must be a CUDA tensor")
+
+
+def _same(name: str, t: torch.Tensor, index: int, dtype=None):
+    if _index(name, t) != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _dtype_code(name: str, dtype: torch.dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {dtype}")
+    return code
+
+
+def _workspace(workspace, need: int, like: torch.Tensor):
+    """The caller's workspace, checked for its kind, or a new one on like's device."""
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-    _need_cuda("workspace", workspace, torch.uint8, dev)
+        return torch.empty(need or 1, dtype=torch.uint8, device=like.device)
+    _same("workspace", workspace, like.get_device(), torch.uint8)
     return workspace
 
 
-def _need_out(name: str, out, shape, dtype, dev):
+def _need_out(name: str, out, shape, dtype, like: torch.Tensor):
     """An output tensor: the caller's, which must be what would be allocated, or a new one."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    _need_cuda(name, out, dtype, dev)
-    if tuple(out.shape) != tuple(shape):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _same(name, out, like.get_device(), dtype)
+    if out.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(out.shape)}")
     return out
 
 
-def _need_ids(ids) -> bool:
-    """Whether the ids are int32 (else int64)."""
-    _need_cuda("ids", ids)
-    if ids.dtype not in (torch.int64, torch.int32):
+def _need_ids(ids):
+    """(device index, whether the ids are int32)."""
+    index = _index("ids", ids)
+    id32 = _IDS.get(ids.dtype)
+    if id32 is None:
         raise TypeError("ids must be int64 or int32")
-    return ids.dtype == torch.int32
+    return index, id32
+
+
+def _size(name: str, *args) -> int:
+    """A workspace query."""
+    n = ctypes.c_size_t()
+    rc = getattr(_lib or lib(), name)(*args, ctypes.byref(n))
+    if rc != TFG_OK:
+        raise TfgError(rc, tfg_last_error())
+    return n.value
 
 
 def tfg_embedding_lookup(table, ids, scale: float = 1.0, padding_id: Optional[int] = None,
@@ -718,20 +762,19 @@ def tfg_embedding_lookup(table, ids, scale: float = 1.0, padding_id: Optional[in
     """scale * table[ids] for ids (int64 or int32) of any shape, zeros where an id is
     ``padding_id``; the result has the shape of ids with a last dimension of F, in
     ``out_dtype`` (the table's by default).  Returns (out, status)."""
-    id32 = _need_ids(ids)
-    dev = ids.device
-    _need_cuda("table", table, None, dev)
+    index, id32 = _need_ids(ids)
+    _same("table", table, index)
     if table.dim() != 2:
         raise ValueError("table must have shape [V, F]")
     v, f = table.shape
     if out_dtype is None:
         out_dtype = table.dtype if out is None else out.dtype
-    out = _need_out("out", out, (*ids.shape, f), out_dtype, dev)
-    status = torch.empty(1, dtype=torch.int32, device=dev)
-    L = lib()
-    _run(dev, L.tfg_embedding_lookup32 if id32 else L.tfg_embedding_lookup, _ptr(ids), ids.numel(), _ptr(table),
-         _dtype_code(table.dtype), v, f, float(scale), NO_PADDING if padding_id is None else int(padding_id), _ptr(out),
-         _dtype_code(out_dtype), _ptr(status), _stream(dev))
+    codes = _dtype_code("table", table.dtype), _dtype_code("out", out_dtype)
+    out = _need_out("out", out, (*ids.shape, f), out_dtype, table)
+    status = torch.empty(1, dtype=torch.int32, device=table.device)
+    _run(index, "tfg_embedding_lookup32" if id32 else "tfg_embedding_lookup", ids.data_ptr(), ids.numel(),
+         table.data_ptr(), codes[0], v, f, scale, NO_PADDING if padding_id is None else padding_id, out.data_ptr(),
+         codes[1], status.data_ptr())
     return out, status
 
 
@@ -743,50 +786,40 @@ class IdGroups(NamedTuple):
 
 
 def tfg_group_ids_workspace_size(num_rows: int, num_ids: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(lib().tfg_group_ids_workspace_size(num_rows, num_ids, ctypes.byref(n)))
-    return n.value
+    return _size("tfg_group_ids_workspace_size", num_rows, num_ids)
 
 
 def tfg_group_ids(ids, num_rows: int, padding_id: Optional[int] = None, workspace=None) -> IdGroups:
     """Order the positions of ``ids`` (any shape, taken flat) by id, equal ids by position."""
-    id32 = _need_ids(ids)
-    dev = ids.device
-    n = ids.numel()
-    need = tfg_group_ids_workspace_size(num_rows, n)
-    workspace = _workspace(workspace, need, dev)
-    rowptr = torch.empty(num_rows + 1, dtype=torch.int32, device=dev)
-    sorted_ids, perm = torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev)
-    status = torch.empty(1, dtype=torch.int32, device=dev)
-    L = lib()
-    _run(dev, L.tfg_group_ids32 if id32 else L.tfg_group_ids, _ptr(ids), n, num_rows,
-         NO_PADDING if padding_id is None else int(padding_id), _ptr(rowptr), _ptr(sorted_ids), _ptr(perm),
-         _ptr(workspace), workspace.numel(), _ptr(status), _stream(dev))
+    index, id32 = _need_ids(ids)
+    n, dev = ids.numel(), ids.device
+    workspace = _workspace(workspace, tfg_group_ids_workspace_size(num_rows, n), ids)
+    rowptr, sorted_ids, perm, status = (torch.empty(k, dtype=torch.int32, device=dev) for k in (num_rows + 1, n, n, 1))
+    _run(index, "tfg_group_ids32" if id32 else "tfg_group_ids", ids.data_ptr(), n, num_rows,
+         NO_PADDING if padding_id is None else padding_id, rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(),
+         workspace.data_ptr(), workspace.numel(), status.data_ptr())
     return IdGroups(rowptr, sorted_ids, perm, status)
 
 
 def tfg_embedding_backward_workspace_size(num_features: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(lib().tfg_embedding_backward_workspace_size(num_features, ctypes.byref(n)))
-    return n.value
+    return _size("tfg_embedding_backward_workspace_size", num_features)
 
 
 def tfg_embedding_backward(groups: IdGroups, grad_out, scale: float = 1.0, out=None, workspace=None):
     """grad_table [V, F] fp32 of tfg_embedding_lookup, for the groups of its ids
     (tfg_group_ids with the same padding_id)."""
-    _need_cuda("grad_out", grad_out)
-    dev = grad_out.device
-    for name in ("rowptr", "sorted_ids", "perm"):
-        _need_cuda(name, getattr(groups, name), torch.int32, dev)
-    n, v = groups.perm.numel(), groups.rowptr.numel() - 1
-    f = grad_out.shape[-1]
-    if groups.sorted_ids.numel() != n or grad_out.numel() != n * f:
+    index = _index("grad_out", grad_out)
+    rowptr, sorted_ids, perm = groups[:3]
+    for name, t in (("rowptr", rowptr), ("sorted_ids", sorted_ids), ("perm", perm)):
+        _same(name, t, index, torch.int32)
+    n, v, f = perm.numel(), rowptr.numel() - 1, grad_out.shape[-1]
+    if sorted_ids.numel() != n or grad_out.numel() != n * f:
         raise ValueError("grad_out must hold a row for every id of the groups")
-    out = _need_out("out", out, (v, f), torch.float32, dev)
-    workspace = _workspace(workspace, tfg_embedding_backward_workspace_size(f), dev)
-    _run(dev, lib().tfg_embedding_backward, _ptr(groups.rowptr), _ptr(groups.sorted_ids), _ptr(groups.perm),
-         _ptr(grad_out), _dtype_code(grad_out.dtype), n, v, f, float(scale), _ptr(out), _ptr(workspace),
-         workspace.numel(), _stream(dev))
+    code = _dtype_code("grad_out", grad_out.dtype)
+    out = _need_out("out", out, (v, f), torch.float32, grad_out)
+    workspace = _workspace(workspace, tfg_embedding_backward_workspace_size(f), grad_out)
+    _run(index, "tfg_embedding_backward", rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(), grad_out.data_ptr(),
+         code, n, v, f, scale, out.data_ptr(), workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -798,26 +831,25 @@ class GroupNorm(NamedTuple):
 
 
 def tfg_group_norm_workspace_size(num_nodes: int, num_graphs: int, num_features: int, num_groups: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(lib().tfg_group_norm_workspace_size(num_nodes, num_graphs, num_features, num_groups, ctypes.byref(n)))
-    return n.value
+    return _size("tfg_group_norm_workspace_size", num_nodes, num_graphs, num_features, num_groups)
 
 
-def _norm_inputs(x, node_offsets, gamma, beta):
-    _need_cuda("x", x)
-    dev = x.device
+def _norm_inputs(x, node_offsets, gamma, beta, activation):
+    index = _index("x", x)
     if x.dim() != 2:
         raise ValueError("x must have shape [N, F]")
     n, f = x.shape
-    _need_cuda("node_offsets", node_offsets, torch.int64, dev)
+    _same("node_offsets", node_offsets, index, torch.int64)
     if node_offsets.dim() != 1 or node_offsets.numel() < 1:
         raise ValueError("node_offsets must have shape [G + 1]")
     for name, w in (("gamma", gamma), ("beta", beta)):
         if w is not None:
-            _need_cuda(name, w, torch.float32, dev)
+            _same(name, w, index, torch.float32)
             if w.numel() != f:
                 raise ValueError(f"{name} must have {f} values")
-    return dev, n, f, node_offsets.numel() - 1
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+    return index, n, f, node_offsets.numel() - 1, _dtype_code("x", x.dtype)
 
 
 def tfg_group_norm(x, node_offsets, num_groups: int, gamma=None, beta=None, eps: float = 1e-5, activation: str = "none",
@@ -826,26 +858,25 @@ def tfg_group_norm(x, node_offsets, num_groups: int, gamma=None, beta=None, eps:
     """Group norm over the graphs of a batch and an activation ("none", "relu", "silu",
     "gelu").  Graph g holds the rows node_offsets[g] .. node_offsets[g + 1] - 1 of x
     [N, F]; rows outside all graphs are left as they are in ``out`` (unset in a new one)."""
-    dev, n, f, g = _norm_inputs(x, node_offsets, gamma, beta)
+    index, n, f, g, code = _norm_inputs(x, node_offsets, gamma, beta, activation)
     if out_dtype is None:
         out_dtype = x.dtype if out is None else out.dtype
-    out = _need_out("out", out, (n, f), out_dtype, dev)
-    workspace = _workspace(workspace, tfg_group_norm_workspace_size(n, g, f, num_groups), dev)
+    out_code = _dtype_code("out", out_dtype)
+    need = tfg_group_norm_workspace_size(n, g, f, num_groups)
+    out = _need_out("out", out, (n, f), out_dtype, x)
+    workspace = _workspace(workspace, need, x)
     mean = rstd = None
     if want_stats:
-        mean, rstd = torch.empty(2, g, num_groups, dtype=torch.float32, device=dev).unbind(0)
-    status = torch.empty(1, dtype=torch.int32, device=dev)
-    _run(dev, lib().tfg_group_norm, _ptr(x), _x_dtype(x), _ptr(node_offsets), n, g, f, num_groups, _ptr(gamma), _ptr(beta),
-         float(eps), ACTIVATIONS[activation], _ptr(out), _dtype_code(out_dtype), _ptr(mean), _ptr(rstd), _ptr(workspace),
-         workspace.numel(), _ptr(status), _stream(dev))
+        mean, rstd = (torch.empty(g, num_groups, dtype=torch.float32, device=x.device) for _ in range(2))
+    status = torch.empty(1, dtype=torch.int32, device=x.device)
+    _run(index, "tfg_group_norm", x.data_ptr(), code, node_offsets.data_ptr(), n, g, f, num_groups, _at(gamma), _at(beta),
+         eps, ACTIVATIONS[activation], out.data_ptr(), out_code, _at(mean), _at(rstd), workspace.data_ptr(),
+         workspace.numel(), status.data_ptr())
     return GroupNorm(out, mean, rstd, status)
 
 
 def tfg_group_norm_backward_workspace_size(num_nodes: int, num_graphs: int, num_features: int, num_groups: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(lib().tfg_group_norm_backward_workspace_size(num_nodes, num_graphs, num_features, num_groups,
-                                                        ctypes.byref(n)))
-    return n.value
+    return _size("tfg_group_norm_backward_workspace_size", num_nodes, num_graphs, num_features, num_groups)
 
 
 def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean, rstd, grad_out, activation: str = "none",
@@ -853,58 +884,71 @@ def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean,
     """Gradients of tfg_group_norm with the forward's arguments and statistics.  Returns
     (grad_x [N, F] in grad_out's type, grad_gamma [F], grad_beta [F]); the last two None
     without ``want_weight_grads``."""
-    dev, n, f, g = _norm_inputs(x, node_offsets, gamma, beta)
-    _need_cuda("grad_out", grad_out, None, dev)
-    if tuple(grad_out.shape) != (n, f):
+    index, n, f, g, code = _norm_inputs(x, node_offsets, gamma, beta, activation)
+    _same("grad_out", grad_out, index)
+    if grad_out.shape != (n, f):
         raise ValueError("grad_out must have the shape of x")
+    grad_code = _dtype_code("grad_out", grad_out.dtype)
     for name, s in (("mean", mean), ("rstd", rstd)):
-        _need_cuda(name, s, torch.float32, dev)
+        _same(name, s, index, torch.float32)
         if s.numel() != g * num_groups:
             raise ValueError(f"{name} must have shape [G, num_groups]")
-    grad_x = _need_out("grad_x", grad_x, (n, f), grad_out.dtype, dev)
+    need = tfg_group_norm_backward_workspace_size(n, g, f, num_groups)
+    grad_x = _need_out("grad_x", grad_x, (n, f), grad_out.dtype, x)
     grad_gamma = grad_beta = None
     if want_weight_grads:
-        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=dev).unbind(0)
-    workspace = _workspace(workspace, tfg_group_norm_backward_workspace_size(n, g, f, num_groups), dev)
-    _run(dev, lib().tfg_group_norm_backward, _ptr(x), _x_dtype(x), _ptr(node_offsets), n, g, f, num_groups, _ptr(gamma),
-         _ptr(beta), _ptr(mean), _ptr(rstd), ACTIVATIONS[activation], _ptr(grad_out), _dtype_code(grad_out.dtype),
-         _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta), _ptr(workspace), workspace.numel(), _stream(dev))
+        grad_gamma, grad_beta = (torch.empty(f, dtype=torch.float32, device=x.device) for _ in range(2))
+    workspace = _workspace(workspace, need, x)
+    _run(index, "tfg_group_norm_backward", x.data_ptr(), code, node_offsets.data_ptr(), n, g, f, num_groups, _at(gamma),
+         _at(beta), mean.data_ptr(), rstd.data_ptr(), ACTIVATIONS[activation], grad_out.data_ptr(), grad_code,
+         grad_x.data_ptr(), _at(grad_gamma), _at(grad_beta), workspace.data_ptr(), workspace.numel())
     return grad_x, grad_gamma, grad_beta
 
 
 def tfg_global_norm_workspace_size(num_tensors: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(lib().tfg_global_norm_workspace_size(num_tensors, ctypes.byref(n)))
-    return n.value
+    return _size("tfg_global_norm_workspace_size", num_tensors)
 
 
-_GRADIENT_TYPES = {torch.float32: TFG_F32, torch.bfloat16: TFG_BF16}
+_DTYPE_OF = operator.attrgetter("dtype")
 
 
-def _tensor_list(name: str, tensors, dev):
+def _tensor_list(name: str, tensors, index: int):
     """(pointers, sizes, type codes) of a list of contiguous tensors on one device, as the
-    host arrays that the C calls read."""
-    for t in tensors:
-        _need_cuda(name, t, None, dev)
-        if t.dtype not in _GRADIENT_TYPES:
-            raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    return (array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", [t.numel() for t in tensors]),
-            array.array("i", [_GRADIENT_TYPES[t.dtype] for t in tensors]))
+    host arrays that the C calls read.  A model has hundreds of gradients: the checks are
+    passes of built-in functions over the list, and only a list that fails one is looked at
+    tensor by tensor."""
+    try:
+        types = list(map(_DTYPE_OF, tensors))
+        if (index >= 0 and set(map(torch.Tensor.get_device, tensors)) <= {index}
+                and all(map(torch.Tensor.is_contiguous, tensors)) and set(types) <= _DTYPES.keys()):
+            return (array.array("Q", map(torch.Tensor.data_ptr, tensors)),
+                    array.array("q", map(torch.Tensor.numel, tensors)),
+                    array.array("i", map(_DTYPES.__getitem__, types)))
+    except (TypeError, AttributeError):           # no tensor at all
+        pass
+    for t in tensors:                             # say which, and why
+        _same(name, t, max(index, 0))
+        _dtype_code(name, t.dtype)
+    raise ValueError(f"{name} must be contiguous float32 or bfloat16 CUDA tensors of one device")
 
 
-def _host(a: array.array):
-    return ctypes.c_void_p(a.buffer_info()[0])
+def _host(a: array.array) -> int:
+    return a.buffer_info()[0]
+
+
+def _list_device(tensors) -> torch.device:
+    return tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
 
 
 def tfg_global_norm(tensors, workspace=None) -> torch.Tensor:
     """sqrt of the sum of all squares over a list of tensors (fp32 or bf16), fp32 [1]."""
     tensors = list(tensors)
-    dev = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
-    ptrs, sizes, codes = _tensor_list("tensors", tensors, dev)
+    dev = _list_device(tensors)
+    ptrs, sizes, codes = _tensor_list("tensors", tensors, -1 if dev.index is None else dev.index)
     norm = torch.empty(1, dtype=torch.float32, device=dev)
-    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), dev)
-    _run(dev, lib().tfg_global_norm, len(tensors), _host(ptrs), _host(sizes), _host(codes), _ptr(norm), _ptr(workspace),
-         workspace.numel(), _stream(dev))
+    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
+    _run(dev.index, "tfg_global_norm", len(tensors), _host(ptrs), _host(sizes), _host(codes), norm.data_ptr(),
+         workspace.data_ptr(), workspace.numel())
     return norm
 
 
@@ -912,14 +956,15 @@ def tfg_clip_by_global_norm(tensors, clip_norm: float, outs=None, workspace=None
     """tensors * clip_norm / max(global norm, clip_norm): new tensors, or ``outs`` (which may
     be the tensors themselves, in place).  Returns (outs, norm [1] before clipping)."""
     tensors = list(tensors)
-    dev = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
-    ptrs, sizes, codes = _tensor_list("tensors", tensors, dev)
-    outs = [torch.empty_like(t) for t in tensors] if outs is None else list(outs)
-    out_ptrs, out_sizes, out_codes = _tensor_list("outs", outs, dev)
+    dev = _list_device(tensors)
+    index = -1 if dev.index is None else dev.index
+    ptrs, sizes, codes = _tensor_list("tensors", tensors, index)
+    outs = list(map(torch.empty_like, tensors)) if outs is None else list(outs)
+    out_ptrs, out_sizes, out_codes = _tensor_list("outs", outs, index)
     if out_sizes != sizes or out_codes != codes:
         raise ValueError("outs must have the sizes and types of tensors")
     norm = torch.empty(1, dtype=torch.float32, device=dev)
-    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), dev)
-    _run(dev, lib().tfg_clip_by_global_norm, len(tensors), _host(ptrs), _host(sizes), _host(codes), float(clip_norm),
-         _host(out_ptrs), _ptr(norm), _ptr(workspace), workspace.numel(), _stream(dev))
+    workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
+    _run(index, "tfg_clip_by_global_norm", len(tensors), _host(ptrs), _host(sizes), _host(codes), clip_norm,
+         _host(out_ptrs), norm.data_ptr(), workspace.data_ptr(), workspace.numel())
     return outs, norm

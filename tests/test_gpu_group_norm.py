@@ -393,7 +393,7 @@ def test_binding_refuses():
         tfg.tfg_group_norm(x, off.int(), 2)
     with pytest.raises(ValueError):
         tfg.tfg_group_norm(x, off, 2, gamma=torch.ones(7, device="cuda"))
-    with pytest.raises(KeyError):
+    with pytest.raises(ValueError):
         tfg.tfg_group_norm(x, off, 2, activation="tanh")
     with pytest.raises(tfg.TfgError):
         tfg.tfg_group_norm(x, off, 3)

@@ -118,7 +118,7 @@ def test_group_norm_backward_rejects(lib):
 
 def test_group_norm_workspace(lib):
     n = ctypes.c_size_t(1)
-    assert lib.tfg_group_norm_workspace_size(20, 4, 64, 8, ctypes.byref(n)) == 0 and n.value == 0
+    assert lib.tfg_group_norm_workspace_size(8, 4, 64, 8, ctypes.byref(n)) == 0 and n.value == 0
     assert lib.tfg_group_norm_workspace_size(232965, 41, 128, 16, ctypes.byref(n)) == 0 and n.value > 0
     assert lib.tfg_group_norm_workspace_size(100, 4, 64, 7, ctypes.byref(n)) == -1
     assert lib.tfg_group_norm_workspace_size(100, 4, 64, 8, None) == -1
