@@ -17,30 +17,33 @@ template <int TT, typename XT, int VEC, int S>
 __device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
                                            int rows, float per_value, float *smem, float (&mean)[S], float (&squares)[S]) {
     constexpr int kPer = VEC / S;                           // values of a sum in a vector
-    float v[1][S] = {};
+    float sum[VEC] = {}, v[1][S] = {}, away[S];
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float w[VEC];
         held.widen(i, w);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) v[0][q / kPer] += w[q];
+        add_vec(sum, w);
     }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
     group_sums<TT, VEC, S, 1>(p, at, v, smem, 0);
 #pragma unroll
     for (int q = 0; q < S; ++q) {
         mean[q] = v[0][q] * per_value;
+        away[q] = -mean[q];
         v[0][q] = 0.f;
     }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) sum[q] = 0.f;
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float w[VEC];
         held.widen(i, w);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            const float d = w[q] - mean[q / kPer];
-            v[0][q / kPer] = fmaf(d, d, v[0][q / kPer]);
-        }
+        add_vec(w, away);
+        fma_vec(sum, w, w, sum);
     }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
     group_sums<TT, VEC, S, 1>(p, at, v, smem, 1);
 #pragma unroll
     for (int q = 0; q < S; ++q) squares[q] = v[0][q];
@@ -49,21 +52,23 @@ __device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VE
 template <int ACT, typename OT, typename XT, int VEC, int TT, int S>
 __device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held, int rows,
                                       int64_t a, const float (&m)[S], const float (&r)[S]) {
-    constexpr int kPer = VEC / S;
     if (rows == 0) return;
     float scale[VEC], shift[VEC];
     channel_weights(p.gamma, at.c0, 1.f, scale);
     channel_weights(p.beta, at.c0, 0.f, shift);
+    mul_vec(scale, r);
+    float away[S];
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) scale[q] *= r[q / kPer];
+    for (int q = 0; q < S; ++q) away[q] = -m[q];
     const int64_t step = p.p.rows_at_once * p.f;
     OT *o = static_cast<OT *>(p.out) + (a + at.rl) * p.f + at.c0;
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float v[VEC];
         held.widen(i, v);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) v[q] = activate<ACT>(fmaf(v[q] - m[q / kPer], scale[q], shift[q]));
+        add_vec(v, away);
+        fma_vec(v, v, scale, shift);
+        activate<ACT>(v);
         store_vec<VEC>(o + i * step, v);
     }
 }
@@ -201,15 +206,14 @@ __global__ void __launch_bounds__(TT, team_ctas(TT, TFG_NORM_RESIDENT)) norm_lar
         const Place<TT, VEC, S> at(p, tile);
         const int rows = at.rows(p, piece.a, piece.b);
         held.copy(static_cast<const XT *>(p.x) + (piece.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
-        __syncthreads();                                    // the last statistics have been read
-        joined_statistics<TT>(p, at, piece, s_stat, join);
+        float2 stat[S];
+        joined_statistics<TT>(p, at, piece, s_stat, stat, join);
         copies_done();
         float mean[S], rstd[S];
 #pragma unroll
         for (int q = 0; q < S; ++q) {
-            const float2 v = s_stat[at.grp[q]];
-            mean[q] = v.x;
-            rstd[q] = v.y;
+            mean[q] = stat[q].x;
+            rstd[q] = stat[q].y;
         }
         // the share in which the graph begins reports its statistics
         if (p.mean && piece.first_share == share) {

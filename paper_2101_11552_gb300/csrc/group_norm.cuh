@@ -43,30 +43,55 @@ __device__ __forceinline__ float exp2_of(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float sigmoid_of(float y) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_of(y * -1.44269504088896341f)));
-    return r;
+template <int VEC>
+__device__ __forceinline__ void sigmoid_of(const float (&y)[VEC], float (&p)[VEC]) {
+    const float minus_log2e[1] = {-1.44269504088896341f}, one[1] = {1.f};
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) p[q] = y[q];
+    mul_vec(p, minus_log2e);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) p[q] = exp2_of(p[q]);
+    add_vec(p, one);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p[q]) : "f"(p[q]));
 }
 // 1 + erf leaves the gelu an absolute error of about |y| u for negative y.
 __device__ __forceinline__ float normal_cdf(float y) { return fmaf(0.5f, erff(y * 0.70710678118654752f), 0.5f); }
-template <int ACT>
-__device__ __forceinline__ float activate(float y) {
-    if constexpr (ACT == kActRelu) return y <= 0.f ? 0.f : y;      // a NaN stays
-    else if constexpr (ACT == kActSilu) return y * sigmoid_of(y);
-    else if constexpr (ACT == kActGelu) return y * normal_cdf(y);
-    else return y;
-}
-template <int ACT>
-__device__ __forceinline__ float activation_slope(float y) {
-    if constexpr (ACT == kActRelu) return y > 0.f ? 1.f : (y <= 0.f ? 0.f : y);
-    else if constexpr (ACT == kActSilu) {
-        const float p = sigmoid_of(y);
-        return p * fmaf(y, 1.f - p, 1.f);
+template <int ACT, int VEC>
+__device__ __forceinline__ void activate(float (&y)[VEC]) {
+    if constexpr (ACT == kActRelu) {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) y[q] = y[q] <= 0.f ? 0.f : y[q];     // a NaN stays
+    } else if constexpr (ACT == kActSilu) {
+        float p[VEC];
+        sigmoid_of(y, p);
+        mul_vec(y, p);
     } else if constexpr (ACT == kActGelu) {
-        const float d = 0.39894228040143268f * exp2_of(y * y * -0.72134752044448170f);   // e^(-y^2 / 2)
-        return fmaf(y, d, normal_cdf(y));
-    } else return 1.f;
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) y[q] *= normal_cdf(y[q]);
+    }
+}
+// d times the slope at y
+template <int ACT, int VEC>
+__device__ __forceinline__ void times_slope(const float (&y)[VEC], float (&d)[VEC]) {
+    if constexpr (ACT == kActRelu) {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) d[q] *= y[q] > 0.f ? 1.f : (y[q] <= 0.f ? 0.f : y[q]);
+    } else if constexpr (ACT == kActSilu) {                 // p (1 + y (1 - p))
+        const float one[1] = {1.f}, minus_one[1] = {-1.f};
+        float p[VEC], r[VEC];
+        sigmoid_of(y, p);
+        fma_vec(r, p, minus_one, one);
+        fma_vec(r, r, y, one);
+        mul_vec(d, p);
+        mul_vec(d, r);
+    } else if constexpr (ACT == kActGelu) {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+            const float e = 0.39894228040143268f * exp2_of(y[q] * y[q] * -0.72134752044448170f);   // e^(-y^2 / 2)
+            d[q] *= fmaf(y[q], e, normal_cdf(y[q]));
+        }
+    }
 }
 
 // Geometry of a launch (see norm_plan).
@@ -406,18 +431,28 @@ __device__ __forceinline__ float piece_values(const NormArgs &p, const RowRange 
     return static_cast<float>(((b < r.b ? b : r.b) - (a > r.a ? a : r.a)) * p.c);
 }
 
-// Joined statistics of the tile's groups of a piece's graph, s_stat[group]: join(rows, first
-// share, group) by a warp, or what a kernel of its own joined.  Collective over the CTA.
-template <int TT, typename At, typename Join>
-__device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, float2 *s_stat, Join join) {
+// Joined statistics of this thread's groups of a piece's graph: what a kernel of its own
+// joined, or join(rows, first share, group) by a warp a group, through s_stat[group].
+// Collective over the CTA.
+template <int TT, typename At, int S, typename Join>
+__device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, float2 *s_stat,
+                                                  float2 (&stat)[S], Join join) {
+    if (p.p.join_apart) {
+#pragma unroll
+        for (int q = 0; q < S; ++q)
+            stat[q] = at.on ? __ldg(p.joined + piece.first_share * p.groups + at.group0 + at.grp[q]) : make_float2(0.f, 0.f);
+        return;
+    }
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
+    __syncthreads();                                        // the last statistics have been read
     for (int k = threadIdx.x >> 5; k < at.groups; k += TT / 32) {
-        const float2 v = p.p.join_apart ? p.joined[piece.first_share * p.groups + at.group0 + k]
-                                        : join(p, r, piece.first_share, at.group0 + k);
+        const float2 v = join(p, r, piece.first_share, at.group0 + k);
         if ((threadIdx.x & 31) == 0) s_stat[k] = v;
     }
     __syncthreads();
+#pragma unroll
+    for (int q = 0; q < S; ++q) stat[q] = s_stat[at.grp[q]];
 }
 
 // ---- host ---------------------------------------------------------------------------

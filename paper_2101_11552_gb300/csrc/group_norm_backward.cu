@@ -21,7 +21,7 @@ __host__ __device__ inline int back_bytes(const NormPlan &p, int sums, int vec, 
 
 template <int VEC, int S>
 struct Column {           // what a thread's channels need
-    float mean[S], rstd[S], gamma[VEC], beta[VEC];
+    float away[S], rstd[S], gamma[VEC], beta[VEC];          // away: minus the mean
 
     template <int TT>
     __device__ __forceinline__ void weights(const NormArgs &p, const Place<TT, VEC, S> &at) {
@@ -33,9 +33,14 @@ struct Column {           // what a thread's channels need
 #pragma unroll
         for (int q = 0; q < S; ++q) {
             const int64_t i = graph * p.groups + at.group0 + at.grp[q];
-            mean[q] = at.on ? __ldg(p.mean_in + i) : 0.f;
+            away[q] = at.on ? -__ldg(p.mean_in + i) : 0.f;
             rstd[q] = at.on ? __ldg(p.rstd_in + i) : 0.f;
         }
+    }
+    __device__ __forceinline__ void slopes(float (&slope)[VEC]) const {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) slope[q] = gamma[q];
+        mul_vec(slope, rstd);
     }
     // e = x - m = h / r and d of row i; slope: gamma r
     template <int ACT, typename XH, typename GH>
@@ -43,11 +48,10 @@ struct Column {           // what a thread's channels need
                                            float (&d)[VEC]) const {
         x.widen(i, e);
         g.widen(i, d);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            e[q] -= mean[q / (VEC / S)];
-            d[q] *= activation_slope<ACT>(fmaf(slope[q], e[q], beta[q]));
-        }
+        float y[VEC];
+        add_vec(e, away);
+        fma_vec(y, e, slope, beta);
+        times_slope<ACT>(y, d);
     }
 };
 
@@ -63,11 +67,8 @@ __device__ __forceinline__ void sums(const NormArgs &p, const Place<TT, VEC, S> 
     for (int i = 0; i < rows; ++i) {
         float e[VEC], d[VEC];
         c.template values<ACT>(x, g, i, slope, e, d);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            de[q] = fmaf(d[q], e[q], de[q]);
-            db[q] += d[q];
-        }
+        fma_vec(de, d, e, de);
+        add_vec(db, d);
     }
 #pragma unroll
     for (int q = 0; q < S; ++q) s[0][q] = s[1][q] = 0.f;
@@ -86,7 +87,6 @@ template <int ACT, typename XT, typename GT, int TT, int VEC, int S>
 __device__ __forceinline__ void gradient(const NormArgs &p, const Place<TT, VEC, S> &at, const Column<VEC, S> &c,
                                          const float (&slope)[VEC], const Held<XT, VEC, TT> &x, const Held<GT, VEC, TT> &g,
                                          int rows, int64_t a, const float (&s)[2][S]) {
-    constexpr int kPer = VEC / S;
     float s1[S], s2[S];
 #pragma unroll
     for (int q = 0; q < S; ++q) {
@@ -99,8 +99,8 @@ __device__ __forceinline__ void gradient(const NormArgs &p, const Place<TT, VEC,
     for (int i = 0; i < rows; ++i) {
         float e[VEC], d[VEC];
         c.template values<ACT>(x, g, i, slope, e, d);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) d[q] = fmaf(slope[q], d[q], fmaf(s2[q / kPer], e[q], s1[q / kPer]));
+        fma_vec(e, e, s2, s1);
+        fma_vec(d, d, slope, e);
         store_vec<VEC>(to + i * step, d);
     }
 }
@@ -155,8 +155,7 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, TFG_BACK_RES
         copy_rows(p, at, x, g, piece.a, rows);
         c.statistics(p, at, piece.graph);
         float slope[VEC];
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) slope[q] = c.gamma[q] * c.rstd[q / (VEC / S)];
+        c.slopes(slope);
         copies_done();
         sums<ACT>(p, at, c, slope, x, g, rows, smem, buffer, s, weight);
         buffer ^= 1;
@@ -297,19 +296,17 @@ norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_bet
         Column<VEC, S> c;
         c.weights(p, at);
         c.statistics(p, at, piece.graph);
-        __syncthreads();                                    // the last sums have been read
-        joined_statistics<TT>(p, at, piece, s_stat, join);
+        float2 stat[S];
+        joined_statistics<TT>(p, at, piece, s_stat, stat, join);
         copies_done();
         float s[2][S];
 #pragma unroll
         for (int q = 0; q < S; ++q) {
-            const float2 v = s_stat[at.grp[q]];
-            s[0][q] = v.x;
-            s[1][q] = v.y;
+            s[0][q] = stat[q].x;
+            s[1][q] = stat[q].y;
         }
         float slope[VEC];
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) slope[q] = c.gamma[q] * c.rstd[q / (VEC / S)];
+        c.slopes(slope);
         gradient<ACT>(p, at, c, slope, x, g, rows, piece.a, s);
     }
 }

@@ -34,6 +34,70 @@ template <typename TT, int VEC> struct RowVec {
     __device__ __forceinline__ void widen(float (&v)[VEC]) const { VecLoad<TT, VEC>::widen(r, v); }
 };
 
+// Arithmetic on VEC values, two to an instruction where VEC is even (packed fp32: each half
+// is the ordinary correctly rounded operation).  b and c may be shared by several values:
+// value q takes element q / (VEC / N).
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+        "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+        "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+template <int VEC, int N>
+__device__ __forceinline__ float2 pair_of(const float (&v)[N], int q) {
+    return make_float2(v[q / (VEC / N)], v[(q + 1) / (VEC / N)]);
+}
+template <int VEC, int N>
+__device__ __forceinline__ void add_vec(float (&a)[VEC], const float (&b)[N]) {       // a + b
+    if constexpr (VEC % 2 == 0) {
+#pragma unroll
+        for (int q = 0; q < VEC; q += 2) {
+            const float2 r = add2(make_float2(a[q], a[q + 1]), pair_of<VEC>(b, q));
+            a[q] = r.x;
+            a[q + 1] = r.y;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) a[q] += b[q / (VEC / N)];
+    }
+}
+template <int VEC, int N>
+__device__ __forceinline__ void mul_vec(float (&a)[VEC], const float (&b)[N]) {       // a b
+    if constexpr (VEC % 2 == 0) {
+#pragma unroll
+        for (int q = 0; q < VEC; q += 2) {
+            const float2 r = mul2(make_float2(a[q], a[q + 1]), pair_of<VEC>(b, q));
+            a[q] = r.x;
+            a[q + 1] = r.y;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) a[q] *= b[q / (VEC / N)];
+    }
+}
+template <int VEC, int N, int M>
+__device__ __forceinline__ void fma_vec(float (&d)[VEC], const float (&a)[VEC], const float (&b)[N], const float (&c)[M]) {   // a b + c
+    if constexpr (VEC % 2 == 0) {
+#pragma unroll
+        for (int q = 0; q < VEC; q += 2) {
+            const float2 r = fma2(make_float2(a[q], a[q + 1]), pair_of<VEC>(b, q), pair_of<VEC>(c, q));
+            d[q] = r.x;
+            d[q + 1] = r.y;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) d[q] = fmaf(a[q], b[q / (VEC / N)], c[q / (VEC / M)]);
+    }
+}
+
 // A vector by plain loads: from shared memory, or from memory that the kernel also writes.
 template <typename T, int VEC>
 __device__ __forceinline__ typename VecLoad<T, VEC>::Raw load_plain(const T *p) {
