@@ -94,6 +94,8 @@ __device__ __forceinline__ void times_slope(const float (&y)[VEC], float (&d)[VE
     }
 }
 
+}  // namespace
+
 // Geometry of a launch (see norm_plan).
 struct NormPlan {
     int vec;              // values of a thread's vector
@@ -136,10 +138,12 @@ struct NormArgs {
     Piece *pieces;                                // [share][slot]
     float2 *part;                                 // [share][slot][group]
     float2 *joined;                               // [share of the graph's first row][group]
-    float2 *channel_part;                         // backward: [batch, slot][F], sums for gamma and beta
+    float2 *channel_part;                         // backward: [batches, then shares][F], sums for gamma and beta
     int64_t batches, batch;                       // backward: batches of so many graphs
     NormPlan p;
 };
+
+namespace {
 
 // ---- rows of graphs and shares ------------------------------------------------------
 struct RowRange {
@@ -216,13 +220,9 @@ __device__ __forceinline__ int64_t slot_at(const NormArgs &p, int64_t a, int64_t
 // TT threads: a warp in a CTA of four, each with shared memory of its own, or a whole CTA.
 constexpr int kWarpTeams = 4;
 // Resident threads asked for: 64 registers a thread forward, 80 backward (64 in teams of
-// 1,024).
-#ifndef TFG_NORM_RESIDENT
-#define TFG_NORM_RESIDENT 1024
-#endif
-#ifndef TFG_BACK_RESIDENT
-#define TFG_BACK_RESIDENT 768
-#endif
+// 1,024).  Forward 1,024 against 768: 4,096 single rows 17 / 20 us; backward 768 against 512
+// and 1,024: 41 communities, both directions, 135 / 145 / 138 us.
+constexpr int kNormResident = 1024, kBackResident = 768;
 constexpr int team_ctas(int team, int threads) { return team == 1024 ? 1 : threads / (team == 256 ? 256 : 128); }
 template <int TT>
 struct Team {
@@ -473,18 +473,16 @@ int norm_vec(int64_t f, int64_t c, int widest, bool aligned) {
     return widest >= 4 && aligned && f % 4 == 0 && c / gcd64(c, 4) <= 256 ? 4 : 1;
 }
 
-#ifndef TFG_NORM_VECS
-#define TFG_NORM_VECS 16
-#endif
-#ifndef TFG_NORM_TEAMS
-#define TFG_NORM_TEAMS 1216
-#endif
-#ifndef TFG_NORM_ROOM
-#define TFG_NORM_ROOM 55
-#endif
-constexpr int kVectorsAThread = TFG_NORM_VECS;    // of a mean graph
-constexpr int64_t kShareTeams = TFG_NORM_TEAMS;
-constexpr int kNormRoom = TFG_NORM_ROOM * 1024;   // shared memory of a CTA: four on a multiprocessor
+// Vectors of a mean graph to a thread: 16 against 8 and 32, 1,024 graphs of 110 rows 84 / 88 /
+// 140 us, 300 ragged ones of odd width 65 / 77 / 65 us (both directions).
+constexpr int kVectorsAThread = 16;
+// Shares of all rows, of every tile: two for each CTA of 256 threads that is resident.  1,216
+// against 608 and 2,432: 41 communities 135 / 137 / 150 us.
+constexpr int64_t kShareTeams = 1216;
+// Shared memory of a CTA: four on a multiprocessor.  55 KB against 40 and 74: 1,024 graphs
+// of 110 rows 84 / 141 / 95 us (40 KB have no room for the larger ones).
+constexpr int kNormRoom = 55 * 1024;
+constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: room, a row's rounding, statistics
 
 // quantities: summed at once; row_bytes: of the vectors held per row and thread.
 // Tiles are whole groups and whole vectors: 32 vectors of a row, fewer (128 bytes at least)
@@ -537,11 +535,12 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     return p;
 }
 
-// 48 KB, static shared memory with it, need no permission.
+// Launches of up to 48 KB, static shared memory with it, need no permission.  The limit is
+// the same for every launch, so that no call lowers it under another's.
 template <typename Kernel>
 cudaError_t allow_shared(Kernel *kernel, int bytes) {
     return bytes <= 32 * 1024 ? cudaSuccess
-                              : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                              : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormSharedMost);
 }
 
 }  // namespace

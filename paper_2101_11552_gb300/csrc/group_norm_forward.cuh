@@ -1,0 +1,288 @@
+// Group norm with an activation, forward: the kernels (group_norm.cuh: the work split).  A
+// translation unit for each type of x compiles them.
+//
+//   m = sum x / M, v = sum (x - m)^2 / M, r = 1 / sqrt(v + eps)    M = n_g * C values
+//   y = gamma (x - m) r + beta, out = act(y)
+//
+// The mean first, then the squares about it, so a mean far from zero costs no precision;
+// shares of a large graph are joined by the pooled-variance identity, squares about the
+// joint mean = squares of the parts + n (mean of the part - joint mean)^2.
+#pragma once
+
+#include "group_norm.cuh"
+
+namespace tfg {
+namespace {
+
+// Means and centred squares of the held rows, to every thread for its groups; per_value: one
+// over their number of values.
+template <int TT, typename XT, int VEC, int S>
+__device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
+                                           int rows, float per_value, float *smem, float (&mean)[S], float (&squares)[S]) {
+    constexpr int kPer = VEC / S;                           // values of a sum in a vector
+    float sum[VEC] = {}, v[1][S] = {}, away[S];
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float w[VEC];
+        held.widen(i, w);
+        add_vec(sum, w);
+    }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
+    group_sums<TT, VEC, S, 1>(p, at, v, smem, 0);
+#pragma unroll
+    for (int q = 0; q < S; ++q) {
+        mean[q] = v[0][q] * per_value;
+        away[q] = -mean[q];
+        v[0][q] = 0.f;
+    }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) sum[q] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float w[VEC];
+        held.widen(i, w);
+        add_vec(w, away);
+        fma_vec(sum, w, w, sum);
+    }
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
+    group_sums<TT, VEC, S, 1>(p, at, v, smem, 1);
+#pragma unroll
+    for (int q = 0; q < S; ++q) squares[q] = v[0][q];
+}
+
+template <int ACT, typename OT, typename XT, int VEC, int TT, int S>
+__device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held, int rows,
+                                      int64_t a, const float (&m)[S], const float (&r)[S]) {
+    if (rows == 0) return;
+    float scale[VEC], shift[VEC];
+    channel_weights(p.gamma, at.c0, 1.f, scale);
+    channel_weights(p.beta, at.c0, 0.f, shift);
+    mul_vec(scale, r);
+    float away[S];
+#pragma unroll
+    for (int q = 0; q < S; ++q) away[q] = -m[q];
+    const int64_t step = p.p.rows_at_once * p.f;
+    OT *o = static_cast<OT *>(p.out) + (a + at.rl) * p.f + at.c0;
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+        float v[VEC];
+        held.widen(i, v);
+        add_vec(v, away);
+        fma_vec(v, v, scale, shift);
+        activate<ACT>(v);
+        store_vec<VEC>(o + i * step, v);
+    }
+}
+
+template <typename XT, int VEC, int TT, int S>
+__device__ __forceinline__ void apply_act(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
+                                          int rows, int64_t a, int act, bool out_bf16, const float (&m)[S],
+                                          const float (&r)[S]) {
+    switch (act + (out_bf16 ? 4 : 0)) {
+        case kActNone: return apply<kActNone, float>(p, at, held, rows, a, m, r);
+        case kActRelu: return apply<kActRelu, float>(p, at, held, rows, a, m, r);
+        case kActSilu: return apply<kActSilu, float>(p, at, held, rows, a, m, r);
+        case kActGelu: return apply<kActGelu, float>(p, at, held, rows, a, m, r);
+        case 4 + kActNone: return apply<kActNone, uint16_t>(p, at, held, rows, a, m, r);
+        case 4 + kActRelu: return apply<kActRelu, uint16_t>(p, at, held, rows, a, m, r);
+        case 4 + kActSilu: return apply<kActSilu, uint16_t>(p, at, held, rows, a, m, r);
+        default: return apply<kActGelu, uint16_t>(p, at, held, rows, a, m, r);
+    }
+}
+
+// Units: the graphs, then the shares with their two slots; a team takes a (unit, tile).
+template <int TT, typename XT, int VEC, int S>
+__global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kNormResident)) norm_units(NormArgs p, int act, bool out_bf16) {
+    using M = Team<TT>;
+    extern __shared__ __align__(16) char s_all[];
+    if (p.status_all && blockIdx.x == gridDim.x - 1) return check_offsets(p);
+    const uint32_t id = blockIdx.x * M::kPerCta + M::index();
+    const int64_t unit = id / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(id - static_cast<uint32_t>(unit) * p.p.tiles);
+    if (unit >= p.graphs + p.p.shares) return;              // whole teams
+    char *smem = s_all + M::index() * team_bytes(p.p, 1, S, VEC * sizeof(XT));
+    const Held<XT, VEC, TT> held(smem + sum_floats(p.p, 1, S) * 4);
+    const Place<TT, VEC, S> at(p, tile);
+    const int t = M::thread();
+    const int64_t share = unit - p.graphs;
+    int64_t covered = 0;
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        RowRange r;
+        if (share < 0) {
+            bool bad;
+            r = graph_rows(p.offsets, unit, p.n, bad);
+            if (bad && tile == 0 && t == 0) set_status(p.status, TFG_ERR_INDEX_RANGE);
+            if (r.b - r.a > p.p.most) return;               // large: the shares'
+            if (r.a == r.b) {                               // an empty graph has no statistics: zeros
+                for (int k = t; k < at.groups; k += TT) {
+                    if (p.mean) p.mean[unit * p.groups + at.group0 + k] = 0.f;
+                    if (p.rstd) p.rstd[unit * p.groups + at.group0 + k] = 0.f;
+                }
+                return;
+            }
+        } else {
+            const Piece piece = find_piece(p, share, slot, covered);
+            if (tile == 0 && t == 0) p.pieces[share * 2 + slot] = piece;
+            if (piece.a == piece.b) continue;
+            r = {piece.a, piece.b};
+        }
+        const int rows = at.rows(p, r.a, r.b);
+        const float per_value = 1.f / static_cast<float>((r.b - r.a) * p.c);
+        held.copy(static_cast<const XT *>(p.x) + (r.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
+        copies_done();
+        float mean[S], squares[S];
+        statistics(p, at, held, rows, per_value, reinterpret_cast<float *>(smem), mean, squares);
+        if (share < 0) {
+            float rstd[S];
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                rstd[q] = rsqrtf(fmaf(squares[q], per_value, p.eps));
+                if (p.mean && at.writes(p, q)) {
+                    p.mean[unit * p.groups + at.group0 + at.grp[q]] = mean[q];
+                    p.rstd[unit * p.groups + at.group0 + at.grp[q]] = rstd[q];
+                }
+            }
+            return apply_act(p, at, held, rows, r.a, act, out_bf16, mean, rstd);
+        }
+#pragma unroll
+        for (int q = 0; q < S; ++q)
+            if (at.writes(p, q))
+                p.part[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
+    }
+}
+
+// Joins the pieces of a large graph (rows r, from share s on) for group k, by a warp: the
+// mean of the pieces' means, then their squares about it, each in a fixed order.
+__device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
+    const int lane = threadIdx.x & 31;
+    const int64_t s1 = (r.b - 1) / p.p.share;
+    const float all = static_cast<float>((r.b - r.a) * p.c);
+    auto part = [&](int64_t i) { return p.part[slot_at(p, r.a, i) * p.groups + k]; };
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x, piece_values(p, r, i), sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += lane_xor(sum, o);
+    const float mean = sum / all;
+    float squares = 0.f;
+#pragma unroll 4
+    for (int64_t i = s + lane; i <= s1; i += 32) {
+        const float2 v = part(i);
+        squares += fmaf((v.x - mean) * piece_values(p, r, i), v.x - mean, v.y);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) squares += lane_xor(squares, o);
+    return make_float2(mean, rsqrtf(squares / all + p.eps));
+}
+
+// join_apart: the large graph that begins in share blockIdx.x, a warp a group.
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
+    const int64_t s = blockIdx.x;
+    Piece piece = p.pieces[s * 2];
+    if (piece.a == piece.b || piece.first_share != s) piece = p.pieces[s * 2 + 1];
+    if (piece.a == piece.b || piece.first_share != s) return;
+    bool bad;
+    const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
+    for (int k = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kJoinWarps) {
+        const float2 v = join(p, r, s, k);
+        if ((threadIdx.x & 31) == 0) p.joined[s * p.groups + k] = v;
+    }
+}
+
+// The pieces of large graphs once more, a CTA a (share, tile), the last share first.
+template <int TT, typename XT, int VEC, int S>
+__global__ void __launch_bounds__(TT, team_ctas(TT, kNormResident)) norm_large(NormArgs p, int act, bool out_bf16) {
+    extern __shared__ __align__(16) char s_all[];
+    const Held<XT, VEC, TT> held(s_all);
+    float2 *s_stat = reinterpret_cast<float2 *>(s_all + p.p.held * TT * VEC * sizeof(XT));   // [tile's groups]
+    const uint32_t back = blockIdx.x / static_cast<uint32_t>(p.p.tiles);
+    const int tile = static_cast<int>(blockIdx.x - back * p.p.tiles);
+    const int64_t share = p.p.shares - 1 - back;
+#pragma unroll 1
+    for (int slot = 0; slot < 2; ++slot) {
+        const Piece piece = p.pieces[share * 2 + slot];
+        if (piece.a == piece.b) continue;
+        const Place<TT, VEC, S> at(p, tile);
+        const int rows = at.rows(p, piece.a, piece.b);
+        held.copy(static_cast<const XT *>(p.x) + (piece.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
+        float2 stat[S];
+        joined_statistics<TT>(p, at, piece, s_stat, stat, join);
+        copies_done();
+        float mean[S], rstd[S];
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            mean[q] = stat[q].x;
+            rstd[q] = stat[q].y;
+        }
+        // the share in which the graph begins reports its statistics
+        if (p.mean && piece.first_share == share) {
+            const int64_t out0 = piece.graph * p.groups + at.group0;
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                if (!at.writes(p, q)) continue;
+                p.mean[out0 + at.grp[q]] = mean[q];
+                p.rstd[out0 + at.grp[q]] = rstd[q];
+            }
+        }
+        apply_act(p, at, held, rows, piece.a, act, out_bf16, mean, rstd);
+    }
+}
+
+template <int TT, typename XT, int VEC, int S>
+cudaError_t launch_units(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
+    using M = Team<TT>;
+    const int smem = M::kPerCta * team_bytes(p.p, 1, S, VEC * sizeof(XT));
+    const cudaError_t err = allow_shared(norm_units<TT, XT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
+    const int64_t teams = (p.graphs + p.p.shares) * p.p.tiles;
+    const int64_t ctas = (teams + M::kPerCta - 1) / M::kPerCta + (p.status_all ? 1 : 0);
+    norm_units<TT, XT, VEC, S><<<static_cast<unsigned>(ctas), M::kThreads, smem, s>>>(p, act, out_bf16);
+    return cudaGetLastError();
+}
+
+template <int TT, typename XT, int VEC, int S>
+cudaError_t launch_large(NormArgs p, int act, bool out_bf16, cudaStream_t s) {
+    if (p.p.join_apart) {
+        const dim3 grid(static_cast<unsigned>(p.p.shares), static_cast<unsigned>(min64((p.groups + kJoinWarps - 1) / kJoinWarps, 65535)));
+        norm_join<<<grid, kJoinWarps * 32, 0, s>>>(p);
+        const cudaError_t launched = cudaGetLastError();
+        if (launched != cudaSuccess) return launched;
+    }
+    set_rows_at_once(p.p, TT);
+    p.p.held = static_cast<int>((p.p.share + p.p.rows_at_once - 1) / p.p.rows_at_once);
+    const int smem = p.p.held * TT * VEC * static_cast<int>(sizeof(XT)) + p.p.tile_groups * static_cast<int>(sizeof(float2));
+    const cudaError_t err = allow_shared(norm_large<TT, XT, VEC, S>, smem);
+    if (err != cudaSuccess) return err;
+    norm_large<TT, XT, VEC, S><<<static_cast<unsigned>(p.p.shares * p.p.tiles), TT, smem, s>>>(p, act, out_bf16);
+    return cudaGetLastError();
+}
+
+template <typename XT, int VEC, int S>
+cudaError_t launch_team(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
+    const bool widest = VEC == 1 && p.p.team == 1024;
+    cudaError_t err;
+    if (widest) err = launch_units<VEC == 1 ? 1024 : 256, XT, VEC, S>(p, act, out_bf16, s);
+    else if (p.p.team == 32) err = launch_units<32, XT, VEC, S>(p, act, out_bf16, s);
+    else if (p.p.team == 128) err = launch_units<128, XT, VEC, S>(p, act, out_bf16, s);
+    else err = launch_units<256, XT, VEC, S>(p, act, out_bf16, s);
+    if (err != cudaSuccess || p.p.shares == 0) return err;
+    return widest ? launch_large<VEC == 1 ? 1024 : 256, XT, VEC, S>(p, act, out_bf16, s)
+                  : launch_large<kLargeTeam, XT, VEC, S>(p, act, out_bf16, s);
+}
+
+// S = 1 where a vector lies in one group.
+template <typename XT>
+cudaError_t launch_vec(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
+    if constexpr (sizeof(XT) == 2) {
+        if (p.p.vec == 8) return launch_team<XT, 8, 1>(p, act, out_bf16, s);
+    }
+    if (p.p.vec == 1) return launch_team<XT, 1, 1>(p, act, out_bf16, s);
+    return p.c % 4 == 0 ? launch_team<XT, 4, 1>(p, act, out_bf16, s) : launch_team<XT, 4, 4>(p, act, out_bf16, s);
+}
+
+}  // namespace
+}  // namespace tfg

@@ -1,9 +1,9 @@
 """Group norm with an activation, forward and backward, against plain 64-bit forms.
 
 Tolerances are first-order error bounds, formed element by element in 64 bits, u = 2^-24.
-No chain of fp32 additions here is longer than 512 (32 rows a thread, at most 256 row lanes,
-1,024 / 32 channels a lane and a butterfly, or a share in 32 and a butterfly), so a sum of
-terms t is off by at most K sum |t| with K = 520 u.  Then, with A = mean |x| of the (graph,
+No chain of fp32 additions here is longer than 512 (at most 220 rows a thread, 256 row lanes
+and 1,024 / 32 channels a lane, never all three at once, then butterflies and one share in
+32), so a sum of terms t is off by at most K sum |t| with K = 520 u.  Then, with A = mean |x| of the (graph,
 group) and dm = K A the error of its mean,
   dr / r <= (K + 4 u) / 2 + (dm r)^2 / 2 + 2 u   (squares about m, a division, a root)
   eh = r dm + |h| (dr / r + 2 u),   ey = |gamma| eh + 2 u (|gamma h| + |beta|)
