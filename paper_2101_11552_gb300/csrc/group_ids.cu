@@ -22,7 +22,9 @@
 //
 // What bounds it: launches and round trips (60,000 ids of 169,343 rows, two digits: five
 // launches for 0.7 MB).  Counting the next digit with atomics in the downsweep instead of
-// an upsweep of its own took as long, and longer where one id is frequent.
+// an upsweep of its own took as long, and longer where one id is frequent; all digits in
+// one launch by a cluster of eight CTAs that write the pairs into one another's shared
+// memory took 46 us against 24 (the scattered remote stores).
 #include "common.cuh"
 
 namespace tfg {

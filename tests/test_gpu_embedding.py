@@ -99,6 +99,14 @@ def test_lookup_groups_and_gradient(n, rows, f, kind, pad, table_t, out_t, id_t)
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 8191, 16384, 16385, 32769, 65536, 65537, 100_001, 131_072, 131_073, 400_000])
+@pytest.mark.parametrize("rows,kind", [(3, "uniform"), (511, "skew"), (512, "one"), (40_000, "uniform"), (300_000, "skew")])
+def test_grouping_sizes(n, rows, kind):
+    """One CTA and many, counts added up by the downsweep or scanned, one to three digits."""
+    ids = make_ids(n, rows, kind, -1, np.random.default_rng(n + rows))
+    check_groups(tfg.tfg_group_ids(torch.as_tensor(ids).cuda(), rows, padding_id=-1), ids, rows, -1)
+
+
 def test_many_passes_of_the_sort():
     """Tables of more than 2^18 rows take three digits; counters over more than 64 tiles the
     scan kernel."""
