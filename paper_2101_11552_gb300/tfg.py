@@ -913,23 +913,26 @@ _DTYPE_OF = operator.attrgetter("dtype")
 
 
 def _tensor_list(name: str, tensors, index: int):
-    """(pointers, sizes, type codes) of a list of contiguous tensors on one device, as the
-    host arrays that the C calls read.  A model has hundreds of gradients: the checks are
-    passes of built-in functions over the list, and only a list that fails one is looked at
-    tensor by tensor."""
+    """(pointers, sizes, types) of a list of contiguous tensors on one device, the first two
+    as the host arrays that the C calls read.  A model has hundreds of gradients: the checks
+    are passes of built-in functions over the list, and only a list that fails one is looked
+    at tensor by tensor."""
     try:
         types = list(map(_DTYPE_OF, tensors))
         if (index >= 0 and set(map(torch.Tensor.get_device, tensors)) <= {index}
                 and all(map(torch.Tensor.is_contiguous, tensors)) and set(types) <= _DTYPES.keys()):
             return (array.array("Q", map(torch.Tensor.data_ptr, tensors)),
-                    array.array("q", map(torch.Tensor.numel, tensors)),
-                    array.array("i", map(_DTYPES.__getitem__, types)))
+                    array.array("q", map(torch.Tensor.numel, tensors)), types)
     except (TypeError, AttributeError):           # no tensor at all
         pass
     for t in tensors:                             # say which, and why
         _same(name, t, max(index, 0))
         _dtype_code(name, t.dtype)
     raise ValueError(f"{name} must be contiguous float32 or bfloat16 CUDA tensors of one device")
+
+
+def _codes(types) -> array.array:
+    return array.array("i", map(_DTYPES.__getitem__, types))
 
 
 def _host(a: array.array) -> int:
@@ -944,7 +947,8 @@ def tfg_global_norm(tensors, workspace=None) -> torch.Tensor:
     """sqrt of the sum of all squares over a list of tensors (fp32 or bf16), fp32 [1]."""
     tensors = list(tensors)
     dev = _list_device(tensors)
-    ptrs, sizes, codes = _tensor_list("tensors", tensors, -1 if dev.index is None else dev.index)
+    ptrs, sizes, types = _tensor_list("tensors", tensors, -1 if dev.index is None else dev.index)
+    codes = _codes(types)
     norm = torch.empty(1, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
     _run(dev.index, "tfg_global_norm", len(tensors), _host(ptrs), _host(sizes), _host(codes), norm.data_ptr(),
@@ -958,10 +962,11 @@ def tfg_clip_by_global_norm(tensors, clip_norm: float, outs=None, workspace=None
     tensors = list(tensors)
     dev = _list_device(tensors)
     index = -1 if dev.index is None else dev.index
-    ptrs, sizes, codes = _tensor_list("tensors", tensors, index)
+    ptrs, sizes, types = _tensor_list("tensors", tensors, index)
+    codes = _codes(types)
     outs = list(map(torch.empty_like, tensors)) if outs is None else list(outs)
-    out_ptrs, out_sizes, out_codes = _tensor_list("outs", outs, index)
-    if out_sizes != sizes or out_codes != codes:
+    out_ptrs, out_sizes, out_types = _tensor_list("outs", outs, index)
+    if out_sizes != sizes or out_types != types:
         raise ValueError("outs must have the sizes and types of tensors")
     norm = torch.empty(1, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
