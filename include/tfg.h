@@ -622,7 +622,8 @@ int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, con
  *   nodes); both or neither may be NULL.  The derivative of TFG_ACT_RELU at 0 is 0.
  *   The offsets are the forward's: they are not reported a second time.
  * At most 1,024 channels per group (TFG_ERR_TOO_LARGE).  Statistics and sums
- * in fp32 in a fixed order: bitwise reproducible.
+ * in fp32 in a fixed order: bitwise reproducible; deviations from a mean whose
+ * squares add up past 3e38 (values of about 1e17 and more) give a rstd of 0.
  * ---------------------------------------------------------------------- */
 int tfg_group_norm_workspace_size(int64_t num_nodes, int64_t num_graphs, int64_t num_features,
                                   int64_t num_groups, size_t *bytes);
