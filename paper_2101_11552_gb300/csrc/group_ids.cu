@@ -15,10 +15,10 @@
 //   downsweep  ranks a tile's pairs, stages them in shared memory in digit order and
 //              writes each digit's run with coalesced stores
 // A list of one tile is sorted by one CTA in shared memory, all digits in one launch.
-// The row boundaries are found by search in the sorted keys, a warp a row where rows are
-// long, else a thread a row between the ends that its warp has found.  The status word is
-// written by that last kernel from one flag per tile, so nothing has to be cleared.  No
-// kernel waits on another CTA.
+// The row boundaries are the places where the digits begin if there is one digit, else they
+// are searched in the sorted keys, a thread a row, between the places where the last digit
+// begins.  The status word is written with them from one flag per tile, so nothing has to
+// be cleared.  No kernel waits on another CTA.
 //
 // What bounds it: launches and round trips (60,000 ids of 169,343 rows, two digits: five
 // launches for 0.7 MB).  Counting the next digit with atomics in the downsweep instead of
@@ -187,12 +187,28 @@ __device__ __forceinline__ void place_warps(TileCounts &mine, int d, int32_t slo
     }
 }
 
+// The status word, by one CTA.
+__device__ __forceinline__ void write_status(const int32_t *bad_tile, int tiles, int32_t *status) {
+    bool bad = false;
+    for (int t = threadIdx.x; t < tiles; t += kGroupThreads) bad |= bad_tile[t] != 0;
+    const int any_bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *status = any_bad ? TFG_ERR_INDEX_RANGE : TFG_OK;
+}
+
+// What the last pass also writes: where each value of the last digit begins, and with one
+// digit alone the row boundaries and the status.
+struct GroupEnds {
+    int32_t *begin, *rowptr;
+    const int32_t *bad_tile;
+    int32_t *status;
+};
+
 template <bool FIRST, bool DIRECT, typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
 group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in, const int32_t *__restrict__ pos_in,
                 int64_t n, int64_t rows, int64_t padding, int shift, int width, int tiles,
                 const int32_t *__restrict__ cnt, const int32_t *__restrict__ total, uint32_t *__restrict__ key_out,
-                int32_t *__restrict__ pos_out) {
+                int32_t *__restrict__ pos_out, GroupEnds ends) {
     __shared__ uint32_t s_key[kGroupTile];
     __shared__ int32_t s_pos[kGroupTile];
     __shared__ TileCounts s_mine;
@@ -218,11 +234,14 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
     int32_t all = 0, earlier = 0;
     if (d < radix) {
         if (DIRECT) {
-#pragma unroll 32
-            for (int i = 0; i < tiles; ++i) {
-                const int32_t c = __ldg(cnt + i * radix + d);
-                all += c;
-                earlier += i < static_cast<int>(blockIdx.x) ? c : 0;
+            for (int i0 = 0; i0 < tiles; i0 += 32) {       // 32 in flight, the last ones too
+#pragma unroll
+                for (int u = 0; u < 32; ++u) {
+                    const int i = i0 + u;
+                    const int32_t c = i < tiles ? __ldg(cnt + i * radix + d) : 0;
+                    all += c;
+                    earlier += i < static_cast<int>(blockIdx.x) ? c : 0;
+                }
             }
         } else {
             earlier = __ldg(cnt + static_cast<int64_t>(d) * tiles + blockIdx.x);
@@ -236,6 +255,14 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
     if (d < radix) {
         place_warps(s_mine, d, slot0);
         s_delta[d] = out0 + earlier - slot0;      // from a slot of the tile to its place in the output
+    }
+    if (blockIdx.x == 0) {
+        if (ends.begin && d < radix) ends.begin[d] = out0;
+        if (ends.begin && d == 0) ends.begin[radix] = static_cast<int32_t>(n);
+        if (ends.rowptr) {                        // one digit: it is the row
+            if (d <= rows) ends.rowptr[d] = out0;
+            write_status(ends.bad_tile, tiles, ends.status);
+        }
     }
     __syncthreads();
 #pragma unroll
@@ -263,7 +290,8 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
 template <typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
 group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, int passes, int width,
-           int32_t *__restrict__ sorted_ids, int32_t *__restrict__ perm, int32_t *__restrict__ bad_tile) {
+           int32_t *__restrict__ sorted_ids, int32_t *__restrict__ perm, int32_t *__restrict__ bad_tile,
+           int32_t *__restrict__ rowptr, int32_t *__restrict__ status) {
     __shared__ uint32_t s_key[kGroupTile];
     __shared__ int32_t s_pos[kGroupTile];
     __shared__ TileCounts s_mine;
@@ -279,12 +307,16 @@ group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, in
         t.pos[r] = i;
     }
     const int any_bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) bad_tile[0] = any_bad;
+    if (threadIdx.x == 0) {
+        if (passes == 1) *status = any_bad ? TFG_ERR_INDEX_RANGE : TFG_OK;
+        else bad_tile[0] = any_bad;
+    }
     for (int pass = 0; pass < passes; ++pass) {
         t.rank_digits(n, pass * width, width, s_mine[warp]);
         __syncthreads();
         const int32_t slot0 = scan_threads(d < radix ? tile_count(s_mine, d) : 0, s_warp);
         if (d < radix) place_warps(s_mine, d, slot0);
+        if (passes == 1 && d <= rows) rowptr[d] = slot0;        // one digit: it is the row
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kGroupItems; ++r) {
@@ -330,36 +362,57 @@ __device__ __forceinline__ int64_t warp_first_at(const uint32_t *keys, int64_t l
     return lo;
 }
 
-// rowptr[k] = first sorted position whose key is at least k, for k in [0, rows]; the first
-// CTA also writes the status.  WARP: a warp a row (long rows: 32 keys a warp would search
-// most of the list each); else a thread a row.
-template <bool WARP>
+// rowptr[k] = first sorted position whose key is at least k, for k in [0, rows], a thread a
+// row: a CTA's rows lie between the places where their last digits begin (no begin: in the
+// whole list), or more than a tile apart between the ends that two warps search.  What fits
+// a tile is searched in shared memory.  The first CTA also writes the status.
 __global__ void __launch_bounds__(kGroupThreads)
-group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int32_t *__restrict__ rowptr,
-             const int32_t *__restrict__ bad_tile, int tiles, int32_t *__restrict__ status) {
-    const int lane = threadIdx.x & 31;
-    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kGroupThreads + threadIdx.x) >> 5;
-    if (WARP) {
-        if (warp <= rows) {
-            const int64_t at = warp_first_at(keys, 0, n, warp);
-            if (lane == 0) rowptr[warp] = static_cast<int32_t>(at);
+group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, const int32_t *__restrict__ begin, int shift,
+             int32_t *__restrict__ rowptr, const int32_t *__restrict__ bad_tile, int tiles, int32_t *__restrict__ status) {
+    __shared__ uint32_t s_key[kGroupTile];
+    __shared__ int64_t s_end[2];
+    const int64_t k0 = static_cast<int64_t>(blockIdx.x) * kGroupThreads, k1 = min64(rows, k0 + kGroupThreads - 1);
+    const int64_t k = k0 + threadIdx.x;
+    int64_t lo = 0, hi = n;
+    if (begin) {
+        lo = __ldg(begin + (k0 >> shift));
+        hi = __ldg(begin + (k1 >> shift) + 1);
+    }
+    if (hi - lo > kGroupTile) {                                 // the same in all threads
+        const int end = threadIdx.x >> 5;
+        if (end < 2) {
+            const int64_t at = warp_first_at(keys, lo, hi, end == 0 ? k0 : k1 + 1);
+            if ((threadIdx.x & 31) == 0) s_end[end] = at;
         }
-    } else if (warp * 32 <= rows) {
-        const int64_t k = warp * 32 + lane;
-        int64_t lo = warp_first_at(keys, 0, n, warp * 32), hi = warp_first_at(keys, lo, n, warp * 32 + 31);
+        __syncthreads();
+        lo = s_end[0];
+        hi = s_end[1];
+    }
+    const int64_t from = lo;
+    const int count = static_cast<int>(hi - lo < kGroupTile ? hi - lo : kGroupTile);
+    if (hi - lo <= kGroupTile) {
+#pragma unroll
+        for (int i = 0; i < kGroupItems; ++i) {
+            const int at = i * kGroupThreads + threadIdx.x;
+            if (at < count) s_key[at] = __ldg(keys + from + at);
+        }
+        __syncthreads();
+        int a = 0, b = count;
+        while (a < b) {
+            const int mid = (a + b) >> 1;
+            if (static_cast<int64_t>(s_key[mid]) < k) a = mid + 1;
+            else b = mid;
+        }
+        lo = from + a;
+    } else {
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
             if (static_cast<int64_t>(__ldg(keys + mid)) < k) lo = mid + 1;
             else hi = mid;
         }
-        if (k <= rows) rowptr[k] = static_cast<int32_t>(lo);
     }
-    if (blockIdx.x == 0) {
-        bool bad = false;
-        for (int t = threadIdx.x; t < tiles; t += kGroupThreads) bad |= __ldg(bad_tile + t) != 0;
-        const int any_bad = __syncthreads_or(bad);
-        if (threadIdx.x == 0) *status = any_bad ? TFG_ERR_INDEX_RANGE : TFG_OK;
-    }
+    if (k <= rows) rowptr[k] = static_cast<int32_t>(lo);
+    if (blockIdx.x == 0) write_status(bad_tile, tiles, status);
 }
 
 }  // namespace
@@ -372,7 +425,7 @@ size_t group_ids_workspace_bytes(int64_t rows, int64_t n) {
     const size_t pairs = 2 * round256(sizeof(int32_t) * size_t(n));
     const size_t counters = round256(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width));
     const int buffers = p.passes > 2 ? 2 : p.passes - 1;
-    return flags + buffers * pairs + counters + round256(sizeof(int32_t) << p.width);
+    return flags + buffers * pairs + counters + 2 * round256((sizeof(int32_t) << p.width) + sizeof(int32_t));
 }
 
 namespace {
@@ -380,7 +433,7 @@ template <typename IdT>
 cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padding, int32_t *rowptr,
                            int32_t *sorted_ids, int32_t *perm, void *ws, int32_t *status, cudaStream_t s) {
     const GroupPlan p = n > 0 ? group_plan(rows, n) : GroupPlan{0, 0, 0};
-    int32_t *bad_tile = nullptr;
+    int32_t *bad_tile = nullptr, *begin = nullptr;
     char *w = static_cast<char *>(ws);
     auto take = [&w](size_t bytes) {
         char *at = w;
@@ -390,9 +443,9 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
     if (n > 0) bad_tile = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles)));
     if (p.tiles == 1) {
         group_tile<<<1, kGroupThreads, 0, s>>>(ids, static_cast<int>(n), rows, padding, p.passes, p.width, sorted_ids, perm,
-                                               bad_tile);
+                                               bad_tile, rowptr, status);
         const cudaError_t err = cudaGetLastError();
-        if (err != cudaSuccess) return err;
+        if (err != cudaSuccess || p.passes == 1) return err;
     } else if (n > 0) {
         // odd and even passes write to buffers of their own, the last one to the caller's
         uint32_t *key_buf[2] = {nullptr, nullptr};
@@ -402,7 +455,9 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
             pos_buf[b] = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(n)));
         }
         int32_t *cnt = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width)));
-        int32_t *total = reinterpret_cast<int32_t *>(take(sizeof(int32_t) << p.width));
+        const size_t digits = (sizeof(int32_t) << p.width) + sizeof(int32_t);
+        int32_t *total = reinterpret_cast<int32_t *>(take(digits));
+        begin = reinterpret_cast<int32_t *>(take(digits));
         const bool direct = p.tiles <= kDirectTiles;
         const int radix = 1 << p.width;
         const uint32_t *key_in = nullptr;
@@ -419,9 +474,10 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
                 group_upsweep<false><<<p.tiles, kGroupThreads, 0, s>>>(none, key_in, n, rows, padding, shift, p.width, p.tiles,
                                                                        direct, cnt, bad_tile);
             if (!direct) group_scan<<<ceil_div(radix, kGroupWarps), kGroupThreads, 0, s>>>(cnt, p.tiles, radix, total);
+            const GroupEnds ends{last && !first ? begin : nullptr, last && first ? rowptr : nullptr, bad_tile, status};
             auto down = [&](auto *kernel, const auto *id) {
                 kernel<<<p.tiles, kGroupThreads, 0, s>>>(id, key_in, pos_in, n, rows, padding, shift, p.width, p.tiles, cnt,
-                                                         total, key_out, pos_out);
+                                                         total, key_out, pos_out, ends);
             };
             if (first && direct) down(group_downsweep<true, true, IdT>, ids);
             else if (first) down(group_downsweep<true, false, IdT>, ids);
@@ -433,11 +489,9 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
             pos_in = pos_out;
         }
     }
-    const uint32_t *keys = reinterpret_cast<const uint32_t *>(sorted_ids);
-    if (n > 32 * rows)
-        group_bounds<true><<<ceil_div(rows + 1, kGroupWarps), kGroupThreads, 0, s>>>(keys, n, rows, rowptr, bad_tile, p.tiles, status);
-    else
-        group_bounds<false><<<ceil_div(rows + 1, kGroupThreads), kGroupThreads, 0, s>>>(keys, n, rows, rowptr, bad_tile, p.tiles, status);
+    if (p.tiles > 1 && p.passes == 1) return cudaSuccess;      // the last pass has written them
+    group_bounds<<<ceil_div(rows + 1, kGroupThreads), kGroupThreads, 0, s>>>(
+        reinterpret_cast<const uint32_t *>(sorted_ids), n, rows, begin, (p.passes - 1) * p.width, rowptr, bad_tile, p.tiles, status);
     return cudaGetLastError();
 }
 }  // namespace
