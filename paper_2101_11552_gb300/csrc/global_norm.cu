@@ -14,6 +14,12 @@
 // squares that leave the range of fp32 (values above 1e15 or all below 1e-13 or so) are
 // taken again in fp64.  The partials, the root and the factor are fp64, and the factor is
 // rounded once to fp32.
+//
+// What bounds it: memory.  1,000 million bf16 values: the sums 285 us (7.0 TB/s), the scaling
+// 620 us (4.0 GB read and written, 6.5 TB/s), 905 us in all; the second read is what the
+// definition costs beyond a read and a write (590 us), as the factor is known last.  85 million
+// of mixed types 94 us, the end of the first pass still in L2 for the second, which goes
+// backwards.  100,000 values in six tensors 8.9 us: two launches.
 #include "widen.cuh"
 
 namespace tfg {
@@ -23,7 +29,8 @@ constexpr int kNormThreads = 256;
 constexpr int kPerThread = 64;                    // values of a chunk that a thread sums
 constexpr int kChunk = kNormThreads * kPerThread;
 constexpr int kNormCtas = 1216;                   // eight a multiprocessor: partials of one launch
-constexpr int kListSmall = 32, kListLarge = 512;  // tensors of a launch (parameters of 1 and 16 KB)
+// Tensors of a launch, passed as 1 or 16 KB of parameters.
+constexpr int kListSmall = 32, kListLarge = 512;
 
 // The tensors of one launch, passed by value: nothing is copied to the device and a
 // captured launch keeps its list.  first[t] is the first chunk of tensor t.

@@ -20,11 +20,16 @@
 // begins.  The status word is written with them from one flag per tile, so nothing has to
 // be cleared.  No kernel waits on another CTA.
 //
-// What bounds it: launches and round trips (60,000 ids of 169,343 rows, two digits: five
-// launches for 0.7 MB).  Counting the next digit with atomics in the downsweep instead of
-// an upsweep of its own took as long, and longer where one id is frequent; all digits in
-// one launch by a cluster of eight CTAs that write the pairs into one another's shared
-// memory took 46 us against 24 (the scattered remote stores).
+// What bounds it: launches and round trips, not bytes.  112,640 ids of 119 rows (one digit,
+// two launches) 10.3 us, 60,000 of 169,343 (two digits of 9 bits, five launches) 20.6 us,
+// 131,072 of 50,000 (two of 8) 24 us; the pairs alone would take under 1 us.  A downsweep's
+// reading of the tile counts was half of its time until all of them were in flight (the
+// last, incomplete round of an unrolled loop reads one by one: 70 -> 58 us for the sampled
+// batch with its lookup and gradient, together with the boundaries between the digits'
+// begins in place of searches of the whole list).  Counting the next digit with atomics in
+// the downsweep instead of an upsweep of its own took as long, and longer where one id is
+// frequent; all digits in one launch by a cluster of eight CTAs that write the pairs into
+// one another's shared memory took 46 us against 24 (the scattered remote stores).
 #include "common.cuh"
 
 namespace tfg {
@@ -36,7 +41,7 @@ constexpr int kGroupItems = 4;
 constexpr int kGroupTile = kGroupThreads * kGroupItems;
 constexpr int kGroupBits = 9;                     // most bits of a digit
 static_assert(kGroupThreads == 1 << kGroupBits, "every digit has a thread of its own");
-constexpr int kDirectTiles = 64;
+constexpr int kDirectTiles = 64;                  // two rounds of 32 loads; the scan's launch costs 2 us
 
 struct GroupPlan {
     int passes, width, tiles;

@@ -1,5 +1,5 @@
 // Group norm with an activation over the graphs of a batch, channels last: what the
-// forward (group_norm.cu) and the backward (group_norm_backward.cu) share.
+// forward (group_norm_forward.cuh) and the backward (group_norm_backward.cuh) share.
 //
 // Graph g holds the rows node_offsets[g] .. node_offsets[g + 1] - 1 of x [N, F] (the
 // reindexing trick of tf_geometric, Section 2.1.1, keeps a graph's nodes together), the
@@ -424,6 +424,13 @@ __device__ __forceinline__ void channel_weights(const float *w, int64_t c0, floa
 
 // ---- the second kernel ---------------------------------------------------------------
 constexpr int kLargeTeam = 256;                   // its teams, but for tiles of 1,024 threads
+
+// Whether a share has no piece: both slots in one round trip, as many shares have none.
+__device__ __forceinline__ bool no_piece(const NormArgs &p, int64_t share) {
+    const longlong2 a = *reinterpret_cast<const longlong2 *>(p.pieces + share * 2);
+    const longlong2 b = *reinterpret_cast<const longlong2 *>(p.pieces + share * 2 + 1);
+    return a.x == a.y && b.x == b.y;
+}
 
 // Values of the piece of rows r in share i, and its slot.
 __device__ __forceinline__ float piece_values(const NormArgs &p, const RowRange &r, int64_t i) {

@@ -9,6 +9,12 @@
 // A team takes a batch of graphs (or a piece of a large one), keeps its columns' sums for
 // gamma and beta in registers from graph to graph and leaves them once; a last kernel adds
 // those of all teams in order.
+//
+// What bounds it: as the forward, with the slope of the activation taken twice (in the sums
+// and in grad_x: keeping it would halve the rows a team holds).  1,024 graphs of 110 rows, F =
+// 128 fp32, SiLU: 51 us (173 MB, 3.4 TB/s; first kernel 41, channels' sums 8).  41 graphs of
+// 232,965 rows, F = 128 bf16: 88 us (179 MB, 2.0 TB/s: 40, join 8, 40 for the second read).  300
+// ragged graphs of 19,717 rows, F = 123 fp32, GELU: 35 us.
 #pragma once
 
 #include "group_norm.cuh"
@@ -289,6 +295,7 @@ norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_bet
     const uint32_t back = (blockIdx.x - channel_ctas) / static_cast<uint32_t>(p.p.tiles);
     const int tile = static_cast<int>(blockIdx.x - channel_ctas - back * p.p.tiles);
     const int64_t share = p.p.shares - 1 - back;
+    if (no_piece(p, share)) return;
 #pragma unroll 1
     for (int slot = 0; slot < 2; ++slot) {
         const Piece piece = p.pieces[share * 2 + slot];
