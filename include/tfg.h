@@ -22,7 +22,10 @@
  *    dtype argument allows it.  Every reduction accumulates in fp32.
  *  - Pointers marked (device) are device memory owned by the caller; the
  *    library never allocates, frees or keeps them.  Workspace buffers are
- *    caller-provided device memory of at least the queried size.
+ *    caller-provided device memory of at least the queried size.  A workspace
+ *    is the call's until its work has run: calls in order on one stream may
+ *    share it, calls that may run at the same time (on other streams, in
+ *    graphs replayed side by side) need one each.
  *  - Every call is stateless (the functional style of Section 2.1.5): all
  *    parameters, including attention vectors, are passed per call.  The
  *    graph-level cache of Section 3 is the caller keeping the outputs of
@@ -552,7 +555,7 @@ int tfg_batch_graphs(int64_t num_graphs, const int64_t *node_counts, const int64
  *              last, from place rowptr[num_rows] on.
  *   perm       (device) int32 [num_ids].
  *   workspace  (device) >= tfg_group_ids_workspace_size() bytes, 256-byte
- *              aligned.
+ *              aligned; 0 bytes for short lists, and then it may be NULL.
  * tfg_embedding_backward: grad_out (device) [num_ids, num_features],
  *   grad_dtype TFG_F32 or TFG_BF16; grad_table (device) fp32 [num_rows,
  *   num_features], written (zeros in rows that no id names).  Sums in fp32 in

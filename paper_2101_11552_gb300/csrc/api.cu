@@ -1140,7 +1140,9 @@ int check_group_norm(const char *fn, int64_t num_nodes, int64_t num_graphs, int6
                     (long long)num_features);
     if (num_features / num_groups > kMaxGroupChannels)
         return fail(TFG_ERR_TOO_LARGE, "%s: at most %lld channels per group", fn, (long long)kMaxGroupChannels);
-    if (!tfg::group_norm_fits(num_nodes, num_graphs, num_features, num_groups))
+    // no more teams than graphs and rows, no more tiles than channels: most calls need no plan
+    if ((num_nodes + num_graphs + 2) * num_features > int64_t(0x7f000000) &&
+        !tfg::group_norm_fits(num_nodes, num_graphs, num_features, num_groups))
         return fail(TFG_ERR_TOO_LARGE, "%s: graphs * features too large", fn);
     return TFG_OK;
 }

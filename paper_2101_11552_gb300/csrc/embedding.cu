@@ -15,6 +15,8 @@
 // 5.4 TB/s), 60,000 rows of 100 into 169,343 in 28 us (80 MB, 2.8 TB/s: the second launch,
 // and chains of id -> position -> row at 12 positions a worker), 112,640 rows of 128 into 119
 // in 18.5 us (58 MB, 3.1 TB/s: the joins).
+#include <algorithm>
+
 #include "widen.cuh"
 
 namespace tfg {
@@ -158,19 +160,24 @@ cudaError_t lookup_ids(const void *ids, int64_t n, const void *table, int table_
 constexpr int kGradThreads = 512, kGradPerSm = 2; // as four CTAs of 256: 2 % slower, eight: 13 to 26 %
 constexpr int kGradCtas = 152 * kGradPerSm;
 constexpr int kGradMinShare = 8;                  // positions a worker should have at least
+// Up to so many positions a worker, one CTA takes them all: no row crosses CTAs, and the join's
+// launch is left out.  The device takes as long (150 rows of 128: 8.9 us against 10.1 with a
+// join, 2,000 of 16: 9.7 against 8.7), the host, which bounds calls so short, 3 us of 18 less.
+constexpr int kGradOneCta = 16;
 
 struct GradArgs {
     const int32_t *rowptr, *sorted_ids, *perm;
     const void *g;
     int64_t n, rows, f;
     float scale;
+    int min_share;
     float *out, *head, *tail;                     // head, tail: [CTA][column tile][tile]
 };
 
 // positions per worker, the same in both kernels
-__device__ __forceinline__ int64_t grad_share(int64_t named, int64_t workers) {
+__device__ __forceinline__ int64_t grad_share(const GradArgs &a, int64_t named, int64_t workers) {
     const int64_t p = (named + workers - 1) / workers;
-    return p > kGradMinShare ? p : kGradMinShare;
+    return p > a.min_share ? p : a.min_share;
 }
 
 template <typename GT, int VEC, int LPR, int T>
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(kGradThreads, kGradPerSm) embedding_grad(GradA
     float *out = a.out + c0;
 
     const int64_t named = min64(a.n, max(0, __ldg(a.rowptr + a.rows)));
-    const int64_t p = grad_share(named, static_cast<int64_t>(gridDim.x) * NW);
+    const int64_t p = grad_share(a, named, static_cast<int64_t>(gridDim.x) * NW);
     const int64_t W = static_cast<int64_t>(blockIdx.x) * NW + w;
     const int64_t ka = min64(named, W * p), kb = min64(named, ka + p);
     auto id_at = [&](int64_t k) { return k < named ? __ldg(a.sorted_ids + k) : -1; };
@@ -315,7 +322,7 @@ __global__ void __launch_bounds__(kJoinThreads)
 embedding_grad_join(GradArgs a, int workers, int cols, int ctas) {
     __shared__ float s_sum[kJoinChains][kJoinThreads / kJoinChains];
     const int64_t named = min64(a.n, max(0, __ldg(a.rowptr + a.rows)));
-    const int64_t share = grad_share(named, static_cast<int64_t>(ctas) * workers) * workers;
+    const int64_t share = grad_share(a, named, static_cast<int64_t>(ctas) * workers) * workers;
     const int64_t b = blockIdx.x + 1;
     const int64_t k = b * share;
     if (k >= named) return;
@@ -416,7 +423,10 @@ cudaError_t launch_embedding_backward(const int32_t *rowptr, const int32_t *sort
                                       float *out, void *ws, cudaStream_t s) {
     const bool aligned = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
     const GradPlan p = grad_plan(n, rows, f, g_dtype, aligned);
-    GradArgs a{rowptr, sorted_ids, perm, g, n, rows, f, scale, out, static_cast<float *>(ws), nullptr};
+    const int workers = kGradThreads / p.lanes;
+    const bool one_cta = n <= int64_t(workers) * kGradOneCta;
+    const int min_share = one_cta ? std::max(kGradMinShare, static_cast<int>((n + workers - 1) / workers)) : kGradMinShare;
+    GradArgs a{rowptr, sorted_ids, perm, g, n, rows, f, scale, min_share, out, static_cast<float *>(ws), nullptr};
     a.tail = a.head + int64_t(p.ctas) * p.tiles * p.cols;
     cudaError_t err;
     if (g_dtype == TFG_BF16)
@@ -428,10 +438,10 @@ cudaError_t launch_embedding_backward(const int32_t *rowptr, const int32_t *sort
         err = p.vec == 4 ? launch_grad_lanes<float, 4, 1>(a, p, s)
               : p.t == 1 ? launch_grad_lanes<float, 1, 1>(a, p, s)
                          : launch_grad_lanes<float, 1, 4>(a, p, s);
-    if (err != cudaSuccess || p.ctas == 1) return err;
+    if (err != cudaSuccess || p.ctas == 1 || one_cta) return err;
     const int64_t tiles = (f + kJoinThreads / kJoinChains - 1) / (kJoinThreads / kJoinChains);
     embedding_grad_join<<<dim3(p.ctas - 1, static_cast<unsigned>(min64(tiles, 65535))), kJoinThreads, 0, s>>>(
-        a, kGradThreads / p.lanes, p.cols, p.ctas);
+        a, workers, p.cols, p.ctas);
     return cudaGetLastError();
 }
 

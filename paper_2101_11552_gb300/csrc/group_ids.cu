@@ -291,12 +291,25 @@ group_downsweep(const IdT *__restrict__ ids, const uint32_t *__restrict__ key_in
     }
 }
 
-// One tile, all digits.
+// First of n sorted keys that is at least k.
+__device__ __forceinline__ int first_at(const uint32_t *keys, int n, int64_t k) {
+    int a = 0, b = n;
+    while (a < b) {
+        const int mid = (a + b) >> 1;
+        if (static_cast<int64_t>(keys[mid]) < k) a = mid + 1;
+        else b = mid;
+    }
+    return a;
+}
+
+// One tile, all digits, and the boundaries of up to kTileRows rows (8 a thread: about 1 us
+// where a launch takes 2).
+constexpr int64_t kTileRows = 4096;
 template <typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
 group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, int passes, int width,
-           int32_t *__restrict__ sorted_ids, int32_t *__restrict__ perm, int32_t *__restrict__ bad_tile,
-           int32_t *__restrict__ rowptr, int32_t *__restrict__ status) {
+           int32_t *__restrict__ sorted_ids, int32_t *__restrict__ perm, int32_t *__restrict__ rowptr,
+           int32_t *__restrict__ status) {
     __shared__ uint32_t s_key[kGroupTile];
     __shared__ int32_t s_pos[kGroupTile];
     __shared__ TileCounts s_mine;
@@ -312,10 +325,7 @@ group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, in
         t.pos[r] = i;
     }
     const int any_bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) {
-        if (passes == 1) *status = any_bad ? TFG_ERR_INDEX_RANGE : TFG_OK;
-        else bad_tile[0] = any_bad;
-    }
+    if (threadIdx.x == 0) *status = any_bad ? TFG_ERR_INDEX_RANGE : TFG_OK;
     for (int pass = 0; pass < passes; ++pass) {
         t.rank_digits(n, pass * width, width, s_mine[warp]);
         __syncthreads();
@@ -348,6 +358,8 @@ group_tile(const IdT *__restrict__ ids, int n, int64_t rows, int64_t padding, in
             perm[t.at(r)] = t.pos[r];
         }
     }
+    if (passes > 1 && rows < kTileRows)           // s_key holds the sorted keys
+        for (int64_t k = threadIdx.x; k <= rows; k += kGroupThreads) rowptr[k] = first_at(s_key, n, k);
 }
 
 // First sorted position in [lo, hi] whose key is at least k, by the whole warp (hi if there
@@ -402,13 +414,7 @@ group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, const i
             if (at < count) s_key[at] = __ldg(keys + from + at);
         }
         __syncthreads();
-        int a = 0, b = count;
-        while (a < b) {
-            const int mid = (a + b) >> 1;
-            if (static_cast<int64_t>(s_key[mid]) < k) a = mid + 1;
-            else b = mid;
-        }
-        lo = from + a;
+        lo = from + first_at(s_key, count, k);
     } else {
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
@@ -417,16 +423,15 @@ group_bounds(const uint32_t *__restrict__ keys, int64_t n, int64_t rows, const i
         }
     }
     if (k <= rows) rowptr[k] = static_cast<int32_t>(lo);
-    if (blockIdx.x == 0) write_status(bad_tile, tiles, status);
+    if (blockIdx.x == 0 && tiles != 1) write_status(bad_tile, tiles, status);     // one tile: written with it
 }
 
 }  // namespace
 
 size_t group_ids_workspace_bytes(int64_t rows, int64_t n) {
-    if (n <= 0) return 256;
     const GroupPlan p = group_plan(rows, n);
+    if (p.tiles <= 1) return 0;
     const size_t flags = round256(sizeof(int32_t) * size_t(p.tiles));
-    if (p.tiles == 1) return flags;
     const size_t pairs = 2 * round256(sizeof(int32_t) * size_t(n));
     const size_t counters = round256(sizeof(int32_t) * size_t(p.tiles) * (size_t(1) << p.width));
     const int buffers = p.passes > 2 ? 2 : p.passes - 1;
@@ -445,13 +450,13 @@ cudaError_t group_ids_impl(const IdT *ids, int64_t n, int64_t rows, int64_t padd
         w += round256(bytes);
         return at;
     };
-    if (n > 0) bad_tile = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles)));
     if (p.tiles == 1) {
         group_tile<<<1, kGroupThreads, 0, s>>>(ids, static_cast<int>(n), rows, padding, p.passes, p.width, sorted_ids, perm,
-                                               bad_tile, rowptr, status);
+                                               rowptr, status);
         const cudaError_t err = cudaGetLastError();
-        if (err != cudaSuccess || p.passes == 1) return err;
+        if (err != cudaSuccess || p.passes == 1 || rows < kTileRows) return err;
     } else if (n > 0) {
+        bad_tile = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * size_t(p.tiles)));
         // odd and even passes write to buffers of their own, the last one to the caller's
         uint32_t *key_buf[2] = {nullptr, nullptr};
         int32_t *pos_buf[2] = {nullptr, nullptr};

@@ -722,11 +722,16 @@ def _dtype_code(name: str, dtype: torch.dtype) -> int:
 
 
 def _workspace(workspace, need: int, like: torch.Tensor):
-    """The caller's workspace, checked for its kind, or a new one on like's device."""
+    """The caller's workspace, checked for its kind, or a new one on like's device (None for
+    0 bytes)."""
     if workspace is None:
-        return torch.empty(need or 1, dtype=torch.uint8, device=like.device)
+        return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
     _same("workspace", workspace, like.get_device(), torch.uint8)
     return workspace
+
+
+def _span(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
 
 def _need_out(name: str, out, shape, dtype, like: torch.Tensor):
@@ -797,7 +802,7 @@ def tfg_group_ids(ids, num_rows: int, padding_id: Optional[int] = None, workspac
     rowptr, sorted_ids, perm, status = (torch.empty(k, dtype=torch.int32, device=dev) for k in (num_rows + 1, n, n, 1))
     _run(index, "tfg_group_ids32" if id32 else "tfg_group_ids", ids.data_ptr(), n, num_rows,
          NO_PADDING if padding_id is None else padding_id, rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(),
-         workspace.data_ptr(), workspace.numel(), status.data_ptr())
+         *_span(workspace), status.data_ptr())
     return IdGroups(rowptr, sorted_ids, perm, status)
 
 
@@ -819,7 +824,7 @@ def tfg_embedding_backward(groups: IdGroups, grad_out, scale: float = 1.0, out=N
     out = _need_out("out", out, (v, f), torch.float32, grad_out)
     workspace = _workspace(workspace, tfg_embedding_backward_workspace_size(f), grad_out)
     _run(index, "tfg_embedding_backward", rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(), grad_out.data_ptr(),
-         code, n, v, f, scale, out.data_ptr(), workspace.data_ptr(), workspace.numel())
+         code, n, v, f, scale, out.data_ptr(), *_span(workspace))
     return out
 
 
@@ -870,8 +875,7 @@ def tfg_group_norm(x, node_offsets, num_groups: int, gamma=None, beta=None, eps:
         mean, rstd = (torch.empty(g, num_groups, dtype=torch.float32, device=x.device) for _ in range(2))
     status = torch.empty(1, dtype=torch.int32, device=x.device)
     _run(index, "tfg_group_norm", x.data_ptr(), code, node_offsets.data_ptr(), n, g, f, num_groups, _at(gamma), _at(beta),
-         eps, ACTIVATIONS[activation], out.data_ptr(), out_code, _at(mean), _at(rstd), workspace.data_ptr(),
-         workspace.numel(), status.data_ptr())
+         eps, ACTIVATIONS[activation], out.data_ptr(), out_code, _at(mean), _at(rstd), *_span(workspace), status.data_ptr())
     return GroupNorm(out, mean, rstd, status)
 
 
@@ -901,7 +905,7 @@ def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean,
     workspace = _workspace(workspace, need, x)
     _run(index, "tfg_group_norm_backward", x.data_ptr(), code, node_offsets.data_ptr(), n, g, f, num_groups, _at(gamma),
          _at(beta), mean.data_ptr(), rstd.data_ptr(), ACTIVATIONS[activation], grad_out.data_ptr(), grad_code,
-         grad_x.data_ptr(), _at(grad_gamma), _at(grad_beta), workspace.data_ptr(), workspace.numel())
+         grad_x.data_ptr(), _at(grad_gamma), _at(grad_beta), *_span(workspace))
     return grad_x, grad_gamma, grad_beta
 
 
@@ -932,7 +936,9 @@ def _tensor_list(name: str, tensors, index: int):
 
 
 def _codes(types) -> array.array:
-    return array.array("i", map(_DTYPES.__getitem__, types))
+    if len(set(types)) == 1:
+        return array.array("i", [_DTYPES[types[0]]]) * len(types)
+    return array.array("i", [_DTYPES[t] for t in types])
 
 
 def _host(a: array.array) -> int:
@@ -952,7 +958,7 @@ def tfg_global_norm(tensors, workspace=None) -> torch.Tensor:
     norm = torch.empty(1, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
     _run(dev.index, "tfg_global_norm", len(tensors), _host(ptrs), _host(sizes), _host(codes), norm.data_ptr(),
-         workspace.data_ptr(), workspace.numel())
+         *_span(workspace))
     return norm
 
 
@@ -971,5 +977,5 @@ def tfg_clip_by_global_norm(tensors, clip_norm: float, outs=None, workspace=None
     norm = torch.empty(1, dtype=torch.float32, device=dev)
     workspace = _workspace(workspace, tfg_global_norm_workspace_size(len(tensors)), norm)
     _run(index, "tfg_clip_by_global_norm", len(tensors), _host(ptrs), _host(sizes), _host(codes), clip_norm,
-         _host(out_ptrs), norm.data_ptr(), workspace.data_ptr(), workspace.numel())
+         _host(out_ptrs), norm.data_ptr(), *_span(workspace))
     return outs, norm

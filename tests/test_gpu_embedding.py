@@ -99,8 +99,8 @@ def test_lookup_groups_and_gradient(n, rows, f, kind, pad, table_t, out_t, id_t)
     assert torch.equal(got, again)
 
 
-@pytest.mark.parametrize("n", [2047, 2048, 2049, 8191, 16384, 16385, 32769, 65536, 65537, 100_001, 131_072, 131_073, 400_000])
-@pytest.mark.parametrize("rows,kind", [(3, "uniform"), (511, "skew"), (512, "one"), (40_000, "uniform"), (300_000, "skew")])
+@pytest.mark.parametrize("n", [1, 2, 700, 2047, 2048, 2049, 8191, 16384, 16385, 32769, 65536, 65537, 100_001, 131_072, 131_073, 400_000])
+@pytest.mark.parametrize("rows,kind", [(3, "uniform"), (511, "skew"), (512, "one"), (4095, "uniform"), (4096, "uniform"), (40_000, "uniform"), (300_000, "skew")])
 def test_grouping_sizes(n, rows, kind):
     """One CTA and many, counts added up by the downsweep or scanned, one to three digits."""
     ids = make_ids(n, rows, kind, -1, np.random.default_rng(n + rows))
@@ -254,5 +254,5 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         tfg.tfg_embedding_backward(groups, torch.randn(4, 4, device="cuda"))
     with pytest.raises(tfg.TfgError) as e:
-        tfg.tfg_group_ids(ids, 5, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+        tfg.tfg_group_ids(ids.repeat(1000), 5, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.code == tfg.TFG_ERR_WORKSPACE

@@ -54,8 +54,8 @@ def test_group_ids_rejects(lib, name):
     assert call(n=2**31 - 1) == -2
     for missing in ("ids", "rowptr", "sorted", "perm", "status"):
         assert call(**{missing: None}) == -1, missing
-    assert call(ws=None) == -3 and call(wsb=16) == -3 and "workspace" in err(lib)
-    assert call(ws=ctypes.c_void_p(0x80000010)) == -1
+    assert call(n=5000, ws=None) == -3 and call(n=5000, wsb=16) == -3 and "workspace" in err(lib)
+    assert call(n=5000, ws=ctypes.c_void_p(0x80000010)) == -1
 
 
 def test_group_ids_workspace(lib):
@@ -64,6 +64,7 @@ def test_group_ids_workspace(lib):
     assert ws(119, 112640, ctypes.byref(n)) == 0 and n.value > 0
     one = n.value
     assert ws(50000, 112640, ctypes.byref(n)) == 0 and n.value >= one + 8 * 112640      # two passes: a pair buffer
+    assert ws(50000, 2048, ctypes.byref(n)) == 0 and n.value == 0                       # one CTA
     assert ws(-1, 5, ctypes.byref(n)) == -1 and ws(5, 5, None) == -1 and ws(5, 2**31, ctypes.byref(n)) == -2
 
 
