@@ -108,6 +108,8 @@ struct NormPlan {
     int lanes;            // vectors of a group (1 where a vector holds several groups)
     bool shuffles;        // groups and rows are powers of two of lanes: sums by lane exchanges
     int log_row, log_c, log_rows;   // then: logarithms of row_vecs, the channels of a group, rows_at_once
+    uint32_t by_row, by_c, by_rows; // else: factors that divide by them (divisor_factor)
+    int log_width;        // and the logarithm of the lanes that add up a group's channels
     int held;             // rows of a thread that its shared memory has room for
     int64_t most;         // rows of a graph that is not large
     int64_t share;        // rows of a share, at most that
@@ -144,6 +146,17 @@ struct NormArgs {
 };
 
 namespace {
+
+// n / d = the upper half of n * factor, for n d < 2^32: factor = floor(2^32 / d) + 1 is off from 2^32 / d
+// by at most 1, so the product by n < 2^32 / d, which no quotient's fraction 1 - 1/d can carry
+// over.  Two instructions for the twenty of a division, several of which a team of few
+// values felt.  0 stands for d = 1.
+__host__ __device__ inline uint32_t divisor_factor(int d) {
+    return d == 1 ? 0u : static_cast<uint32_t>((uint64_t(1) << 32) / static_cast<uint32_t>(d)) + 1u;
+}
+__device__ __forceinline__ int quotient(int n, uint32_t factor) {
+    return factor ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), factor)) : n;
+}
 
 // ---- rows of graphs and shares ------------------------------------------------------
 struct RowRange {
@@ -250,7 +263,7 @@ struct Place {
 
     __device__ __forceinline__ Place(const NormArgs &a, int tile) {
         const int t = Team<TT>::thread();
-        rl = a.p.shuffles ? t >> a.p.log_row : t / a.p.row_vecs;
+        rl = a.p.shuffles ? t >> a.p.log_row : quotient(t, a.p.by_row);
         sub = t - rl * a.p.row_vecs;
         c0 = static_cast<int64_t>(tile) * a.p.cols + sub * VEC;
         on = rl < a.p.rows_at_once && c0 < a.f;
@@ -259,14 +272,14 @@ struct Place {
 #pragma unroll
         for (int q = 0; q < S; ++q) {
             const int c = sub * VEC + q;
-            grp[q] = on ? (a.p.shuffles ? c >> a.p.log_c : c / a.c) : 0;
+            grp[q] = on ? (a.p.shuffles ? c >> a.p.log_c : quotient(c, a.p.by_c)) : 0;
         }
     }
     // rows of [a, b) that this thread visits: a + rl, a + rl + rows_at_once, ...
     __device__ __forceinline__ int rows(const NormArgs &p, int64_t a, int64_t b) const {
         const int left = static_cast<int>(b - a) - rl;
         const int up = left + p.p.rows_at_once - 1;
-        return on && left > 0 ? (p.p.shuffles ? up >> p.p.log_rows : up / p.p.rows_at_once) : 0;
+        return on && left > 0 ? (p.p.shuffles ? up >> p.p.log_rows : quotient(up, p.p.by_rows)) : 0;
     }
     // whether sum q is the one that writes its group's statistics
     __device__ __forceinline__ bool writes(const NormArgs &a, int q) const {
@@ -388,10 +401,9 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VE
         }
     }
     M::sync();
-    int width = 1;                                          // lanes of a group
-    while (width < a.c && width < 32) width <<= 1;
-    for (int k0 = 0; k0 < at.groups; k0 += TT / width) {
-        const int k = k0 + t / width, l = t & (width - 1);
+    const int width = 1 << a.p.log_width;                   // lanes of a group
+    for (int k0 = 0; k0 < at.groups; k0 += TT >> a.p.log_width) {
+        const int k = k0 + (t >> a.p.log_width), l = t & (width - 1);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             float *chan = smem + s * (rows + 2) * cols + rows * cols;
@@ -469,6 +481,7 @@ bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
 void set_rows_at_once(NormPlan &p, int team) {
     p.rows_at_once = team / p.row_vecs;
     p.log_rows = 0;
+    p.by_rows = divisor_factor(p.rows_at_once);
     while ((1 << p.log_rows) < p.rows_at_once) ++p.log_rows;
 }
 
@@ -482,13 +495,18 @@ int norm_vec(int64_t f, int64_t c, int widest, bool aligned) {
 
 // Vectors of a mean graph to a thread: 16 against 8 and 32, 1,024 graphs of 110 rows 84 / 88 /
 // 140 us, 300 ragged ones of odd width 65 / 77 / 65 us (both directions).
-constexpr int kVectorsAThread = 16;
+// Single values (odd widths): 32 to a thread, as the fixed work of a team counts for more; 900
+// graphs of 111 rows, F = 75 fp32: 98 / 110 us, 21 of 83 rows, F = 58: 22.6 / 21.3.
+constexpr int kVectorsAThread = 16, kValuesAThread = 32;
 // Shares of all rows, of every tile: two for each CTA of 256 threads that is resident.  1,216
 // against 608 and 2,432: 41 communities 135 / 137 / 150 us.
 constexpr int64_t kShareTeams = 1216;
 // Shared memory of a CTA: four on a multiprocessor.  55 KB against 40 and 74: 1,024 graphs
 // of 110 rows 84 / 141 / 95 us (40 KB have no room for the larger ones).
 constexpr int kNormRoom = 55 * 1024;
+// Bytes a thread that kNormResident threads leave unused.  20,000 graphs of 3 rows on average, F =
+// 35 fp32, both directions: 122 us against 231 with room for 8 rows, 4,096 single rows 16.5 / 17.8.
+constexpr int kFreeShared = 216, kFewRows = 64;
 constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: room, a row's rounding, statistics
 
 // quantities: summed at once; row_bytes: of the vectors held per row and thread.
@@ -521,14 +539,23 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     p.tile_groups = static_cast<int>(p.cols / c);
     while ((1 << p.log_row) < p.row_vecs) ++p.log_row;
     while ((1 << p.log_c) < c) ++p.log_c;
+    p.by_row = divisor_factor(p.row_vecs);
+    p.by_c = divisor_factor(static_cast<int>(c));
+    p.log_width = p.log_c < 5 ? p.log_c : 5;
     p.tiles = static_cast<int>((f + p.cols - 1) / p.cols);
-    const int64_t t = (mean * w + kVectorsAThread - 1) / kVectorsAThread;
+    const int64_t per = vec == 1 ? kValuesAThread : kVectorsAThread;
+    const int64_t t = (mean * w + per - 1) / per;
     p.team = t <= 32 && w <= 32 ? 32 : (t <= 128 && w <= 128 ? 128 : 256);
     if (w > 256) p.team = 1024;
     set_rows_at_once(p, p.team);
     const int per_cta = p.team == 32 ? kWarpTeams : 1;
     const int64_t room = (kNormRoom / per_cta - sum_floats(p, quantities, sums) * 4) / (int64_t(p.team) * row_bytes);
-    const int64_t wanted = ((mean < 4 ? 8 : 2 * mean) + p.rows_at_once - 1) / p.rows_at_once;
+    // Twice the mean graph, and of kFewRows what costs no resident team: graphs of a few rows are
+    // seldom equal, and those that do not fit cost a share each.
+    const int64_t few_rows = (kFewRows + p.rows_at_once - 1) / p.rows_at_once, unused = kFreeShared / row_bytes;
+    int64_t wanted = (2 * mean + p.rows_at_once - 1) / p.rows_at_once;
+    const int64_t least_rows = few_rows < unused ? few_rows : unused;
+    if (wanted < least_rows) wanted = least_rows;
     p.held = static_cast<int>(wanted < room ? wanted : room);
     if (p.held < 1) p.held = 1;
     p.most = int64_t(p.held) * p.rows_at_once;
