@@ -512,7 +512,8 @@ constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: ro
 // quantities: summed at once; row_bytes: of the vectors held per row and thread.
 // Tiles are whole groups and whole vectors: 32 vectors of a row, fewer (128 bytes at least)
 // as long as a team has no room for twice the mean graph.  The team: kVectorsAThread
-// vectors of a mean graph to a thread, or 256 threads on shares of large ones.
+// vectors (kValuesAThread single values) of a mean graph to a thread, or 256 threads on
+// shares of large ones.
 NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int quantities, int row_bytes) {
     NormPlan p{};
     p.vec = vec;

@@ -12,9 +12,9 @@
 // F = 128 fp32, SiLU: 34 us (115 MB, 3.4 TB/s; 28 instructions a value, issue slots 45 % busy
 // with 23 % of the warps that a multiprocessor can hold, as room for the largest graph is
 // kept for each; and 4 us for a second kernel that finds no large graph).  Half as wide
-// tiles, twice the warps: 34.5 us.  41 graphs of 232,965 rows, F = 128 bf16: 47 us (119 MB, 2.6
+// tiles, twice the warps: 34.5 us.  41 graphs of 232,965 rows, F = 128 bf16: 46 us (119 MB, 2.6
 // TB/s: first pass 21, join 6, second read of x 20).  300 ragged graphs of 19,717 rows, F = 123
-// fp32 (4-byte loads, GELU): 29 us.  4,096 single rows of 1,024 bf16 in 32 groups: 17 us.  2,708
+// fp32 (4-byte loads, GELU): 27 us.  4,096 single rows of 1,024 bf16 in 32 groups: 17 us.  2,708
 // rows in one graph, F = 64: 10 us, two launches.
 #pragma once
 
