@@ -302,8 +302,9 @@ __device__ __forceinline__ int first_at(const uint32_t *keys, int n, int64_t k) 
     return a;
 }
 
-// One tile, all digits, and the boundaries of up to kTileRows rows (8 a thread: about 1 us
-// where a launch takes 2).
+// One tile, all digits, and the boundaries of up to kTileRows rows.  With a launch of their own
+// 250 ids take 8 us whatever the rows; here 8.3 us for 3,000 rows, 9.1 for 4,000, 12.6 for 8,000.
+// The launch costs the host, which bounds calls so short, 3.5 us of 24.
 constexpr int64_t kTileRows = 4096;
 template <typename IdT>
 __global__ void __launch_bounds__(kGroupThreads)
