@@ -170,3 +170,27 @@ def test_bounds_checked_build():
         assert rc == tfg.TFG_ERR_INDEX_RANGE and "table must hold" in msg, (rc, msg)
     finally:
         tfg.use_library(build.LIB_PATH)
+
+
+@pytest.mark.parametrize("n,f", [(127, 128), (128, 128), (129, 128), (255, 128), (256, 128), (257, 128), (2047, 16), (2048, 16),
+                                 (2049, 16), (1024, 24), (1025, 24)])
+@pytest.mark.parametrize("rows", [1, 3, 40_000])
+def test_gradient_around_one_cta(n, f, rows):
+    """Lists that one CTA reduces, and those one longer, whose rows may cross CTAs."""
+    ids = torch.randint(0, rows, (n,), device="cuda")
+    ids[: n // 2] = rows // 2                                 # one id with half of the positions
+    grad = torch.randn(n, f, device="cuda")
+    got = tfg.tfg_embedding_backward(tfg.tfg_group_ids(ids, rows), grad, 0.5)
+    want = torch.zeros(rows, f, dtype=torch.float64, device="cuda").index_add_(0, ids, grad.double()) * 0.5
+    size = torch.zeros(rows, f, dtype=torch.float64, device="cuda").index_add_(0, ids, grad.double().abs()) * 0.5
+    assert bool(((got.double() - want).abs() <= (n + 4) * 2.0 ** -24 * size).all())
+
+
+@pytest.mark.parametrize("f,groups,dt", [(35, 7, "f32"), (35, 7, "bf16"), (400, 25, "f32"), (75, 25, "f32"), (1023, 3, "f32")])
+def test_graphs_of_a_few_rows(f, groups, dt):
+    """Small unequal graphs: some fit a team only by the room that it has anyway, some do not."""
+    sizes = np.random.default_rng(f).geometric(1 / 3, 900) - 1
+    sizes[::100] = [63, 64, 65, 66, 130, 12, 13, 14, 200]
+    offsets = np.concatenate([[0], np.cumsum(sizes)]).tolist()
+    x, go = features(offsets[-1], f, 4, torch.bfloat16 if dt == "bf16" else torch.float32)
+    run_and_check(x, offsets, groups, torch.linspace(0.5, 1.5, f, device="cuda"), None, "silu", go, dt)
