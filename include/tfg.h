@@ -624,6 +624,10 @@ int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, con
  *   grad_gamma, grad_beta (device) fp32 [num_features], written (0 without
  *   nodes); both or neither may be NULL.  The derivative of TFG_ACT_RELU at 0 is 0.
  *   The offsets are the forward's: they are not reported a second time.
+ * An offset common to the values of a (graph, group) costs the forward nothing:
+ * the deviations are taken from the mean before its rounding to fp32, and equal
+ * values give beta.  The backward has the mean as reported: its h is off by up
+ * to |m| r 2^-24.
  * At most 1,024 channels per group (TFG_ERR_TOO_LARGE).  Statistics and sums
  * in fp32 in a fixed order: bitwise reproducible; deviations from a mean whose
  * squares add up past 3e38 (values of about 1e17 and more) give a rstd of 0.

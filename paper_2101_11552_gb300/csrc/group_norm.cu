@@ -31,7 +31,7 @@ size_t group_norm_workspace_bytes(int64_t n, int64_t graphs, int64_t f, int64_t 
     for (const int elem : {4, 2}) {
         for (const bool aligned : {true, false}) {
             const NormPlan p = forward_plan(n, graphs, f, f / groups, elem, aligned);
-            const size_t bytes = size_t(p.shares) * (2 * sizeof(Piece) + 3 * size_t(groups) * sizeof(float2));
+            const size_t bytes = size_t(p.shares) * (2 * sizeof(Piece) + 3 * size_t(groups) * sizeof(float4));
             if (bytes > most) most = bytes;
         }
     }
@@ -65,8 +65,8 @@ cudaError_t launch_group_norm(const void *x, int x_dtype, const int64_t *offsets
     p.out = out;
     p.p = forward_plan(n, graphs, f, c, x_dtype == TFG_BF16 ? 2 : 4, aligned);
     p.pieces = static_cast<Piece *>(ws);
-    p.part = reinterpret_cast<float2 *>(p.pieces + 2 * p.p.shares);
-    p.joined = p.part + p.p.shares * 2 * groups;
+    p.moments = reinterpret_cast<float4 *>(p.pieces + 2 * p.p.shares);
+    p.joined_moments = p.moments + p.p.shares * 2 * groups;
     const bool out_bf16 = out_dtype == TFG_BF16;
     return x_dtype == TFG_BF16 ? launch_group_norm_bf16(p, act, out_bf16, s) : launch_group_norm_f32(p, act, out_bf16, s);
 }

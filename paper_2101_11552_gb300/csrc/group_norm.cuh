@@ -138,8 +138,8 @@ struct NormArgs {
     const void *g;                                // backward: dL/dout
     const float *mean_in, *rstd_in;               // backward: the forward's statistics
     Piece *pieces;                                // [share][slot]
-    float2 *part;                                 // [share][slot][group]
-    float2 *joined;                               // [share of the graph's first row][group]
+    float4 *moments, *joined_moments;             // forward: [share][slot][group], [share of the graph's first row][group]
+    float2 *part, *joined;                        // backward: the same of its two sums
     float2 *channel_part;                         // backward: [batches, then shares][F], sums for gamma and beta
     int64_t batches, batch;                       // backward: batches of so many graphs
     NormPlan p;
@@ -287,15 +287,16 @@ struct Place {
     }
 };
 
-// Floats of shared memory that a team's sums of `quantities` take: two buffers of the
-// exchange, or per-channel sums.
-__host__ __device__ inline int sum_floats(const NormPlan &p, int quantities, int sums) {
-    return p.shuffles ? (p.team > 32 ? 2 * quantities * sums * p.team : 0) : quantities * (p.rows_at_once + 2) * p.cols;
+// Floats of shared memory that a team's sums take: the buffers of the exchange (one for a
+// quantity; two calls after one another take their own), or per-channel sums of two.
+constexpr int kForwardBuffers = 3, kBackBuffers = 4;       // one quantity, then two; two and two
+__host__ __device__ inline int sum_floats(const NormPlan &p, int buffers, int sums) {
+    return p.shuffles ? (p.team > 32 ? buffers * sums * p.team : 0) : 2 * (p.rows_at_once + 2) * p.cols;
 }
 
 // Bytes of shared memory of a team: sums and held rows.
-__host__ __device__ inline int team_bytes(const NormPlan &p, int quantities, int sums, int row_bytes) {
-    return (sum_floats(p, quantities, sums) * 4 + p.held * p.team * row_bytes + 15) / 16 * 16;
+__host__ __device__ inline int team_bytes(const NormPlan &p, int buffers, int sums, int row_bytes) {
+    return (sum_floats(p, buffers, sums) * 4 + p.held * p.team * row_bytes + 15) / 16 * 16;
 }
 
 // A thread's rows in shared memory, one vector each; the team's threads side by side.
@@ -316,9 +317,9 @@ struct Held {
 
 // Sums of v[s][q] over the rows and the channels of each group of the tile, to every thread
 // for its own groups.  Collective over the team.  By lane exchanges and one barrier where
-// group and row are powers of two (buffer: alternates from call to call, so that the next
-// call's barrier separates this one's reads from the writes after it), else through
-// per-channel sums in shared memory.
+// group and row are powers of two (through buffer and those behind it, others than the last
+// call's, so that this call's barrier separates that one's reads from the writes after it),
+// else through per-channel sums in shared memory.
 template <int TT, int VEC, int S, int NS>
 __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VEC, S> &at, float (&v)[NS][S], float *smem,
                                            int buffer) {
@@ -352,7 +353,7 @@ __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<TT, VE
                 for (int q = 0; q < S; ++q) v[s][q] += lane_xor(v[s][q], o);
         if constexpr (TT > 32) {
             const int lane = t & 31, warp = t >> 5;
-            float *to = smem + buffer * NS * S * TT;
+            float *to = smem + buffer * S * TT;
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -453,20 +454,20 @@ __device__ __forceinline__ float piece_values(const NormArgs &p, const RowRange 
 // Joined statistics of this thread's groups of a piece's graph: what a kernel of its own
 // joined, or join(rows, first share, group) by a warp a group, through s_stat[group].
 // Collective over the CTA.
-template <int TT, typename At, int S, typename Join>
-__device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, float2 *s_stat,
-                                                  float2 (&stat)[S], Join join) {
+template <int TT, typename At, int S, typename Stat, typename Join>
+__device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, const Stat *joined,
+                                                  Stat *s_stat, Stat (&stat)[S], Join join) {
     if (p.p.join_apart) {
 #pragma unroll
         for (int q = 0; q < S; ++q)
-            stat[q] = at.on ? __ldg(p.joined + piece.first_share * p.groups + at.group0 + at.grp[q]) : make_float2(0.f, 0.f);
+            stat[q] = at.on ? __ldg(joined + piece.first_share * p.groups + at.group0 + at.grp[q]) : Stat{};
         return;
     }
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
     __syncthreads();                                        // the last statistics have been read
     for (int k = threadIdx.x >> 5; k < at.groups; k += TT / 32) {
-        const float2 v = join(p, r, piece.first_share, at.group0 + k);
+        const Stat v = join(p, r, piece.first_share, at.group0 + k);
         if ((threadIdx.x & 31) == 0) s_stat[k] = v;
     }
     __syncthreads();
@@ -509,12 +510,12 @@ constexpr int kNormRoom = 55 * 1024;
 constexpr int kFreeShared = 216, kFewRows = 64;
 constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: room, a row's rounding, statistics
 
-// quantities: summed at once; row_bytes: of the vectors held per row and thread.
+// operands: arrays whose rows are held; row_bytes: of the vectors held per row and thread.
 // Tiles are whole groups and whole vectors: 32 vectors of a row, fewer (128 bytes at least)
 // as long as a team has no room for twice the mean graph.  The team: kVectorsAThread
 // vectors (kValuesAThread single values) of a mean graph to a thread, or 256 threads on
 // shares of large ones.
-NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int quantities, int row_bytes) {
+NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int operands, int row_bytes) {
     NormPlan p{};
     p.vec = vec;
     const int64_t unit = c / gcd64(c, vec);                     // vectors of the smallest tile
@@ -523,7 +524,7 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     const int sums = c % vec == 0 ? 1 : vec;
     p.lanes = static_cast<int>(c > vec ? unit : 1);
     p.shuffles = power_of_two(c);                               // c a multiple or a divisor of vec then
-    const int64_t least = (128 * quantities + row_bytes - 1) / row_bytes;   // vectors of 128 bytes of one operand
+    const int64_t least = (128 * operands + row_bytes - 1) / row_bytes;   // vectors of 128 bytes of one operand
     auto fits = [&](int64_t vecs) { return 2 * mean * vecs * row_bytes <= kNormRoom; };
     int64_t w = unit;
     if (p.shuffles) {
@@ -550,7 +551,7 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     if (w > 256) p.team = 1024;
     set_rows_at_once(p, p.team);
     const int per_cta = p.team == 32 ? kWarpTeams : 1;
-    const int64_t room = (kNormRoom / per_cta - sum_floats(p, quantities, sums) * 4) / (int64_t(p.team) * row_bytes);
+    const int64_t room = (kNormRoom / per_cta - sum_floats(p, operands == 1 ? kForwardBuffers : kBackBuffers, sums) * 4) / (int64_t(p.team) * row_bytes);
     // Twice the mean graph, and of kFewRows what costs no resident team: graphs of a few rows are
     // seldom equal, and those that do not fit cost a share each.
     const int64_t few_rows = (kFewRows + p.rows_at_once - 1) / p.rows_at_once, unused = kFreeShared / row_bytes;

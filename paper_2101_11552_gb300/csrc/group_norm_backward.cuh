@@ -24,7 +24,7 @@ namespace {
 
 // Shared memory of a team: sums and held rows, and at the end its channels' sums instead.
 __host__ __device__ inline int back_bytes(const NormPlan &p, int sums, int vec, int row_bytes) {
-    const int held = team_bytes(p, 2, sums, row_bytes), channels = 2 * p.team * vec * 4;
+    const int held = team_bytes(p, kBackBuffers, sums, row_bytes), channels = 2 * p.team * vec * 4;
     return held > channels ? held : channels;
 }
 
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kBackResiden
     if (row >= p.batches + p.p.shares) return;              // whole teams
     char *own = s_all + M::index() * back_bytes(p.p, S, VEC, kRowBytes);
     float *smem = reinterpret_cast<float *>(own);
-    char *rows_at = own + sum_floats(p.p, 2, S) * 4;
+    char *rows_at = own + sum_floats(p.p, kBackBuffers, S) * 4;
     const Held<XT, VEC, TT> x(rows_at);
     const Held<GT, VEC, TT> g(rows_at + p.p.held * TT * VEC * sizeof(XT));
     const Place<TT, VEC, S> at(p, tile);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kBackResiden
         c.slopes(slope);
         copies_done();
         sums<ACT>(p, at, c, slope, x, g, rows, smem, buffer, s, weight);
-        buffer ^= 1;
+        buffer ^= 2;
         if (share < 0) {
             const float per_value = 1.f / static_cast<float>((piece.b - piece.a) * p.c);
 #pragma unroll
@@ -307,7 +307,7 @@ norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_bet
         c.weights(p, at);
         c.statistics(p, at, piece.graph);
         float2 stat[S];
-        joined_statistics<TT>(p, at, piece, s_stat, stat, join);
+        joined_statistics<TT>(p, at, piece, p.joined, s_stat, stat, join);
         copies_done();
         float s[2][S];
 #pragma unroll

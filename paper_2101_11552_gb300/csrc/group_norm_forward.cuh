@@ -4,9 +4,15 @@
 //   m = sum x / M, v = sum (x - m)^2 / M, r = 1 / sqrt(v + eps)    M = n_g * C values
 //   y = gamma (x - m) r + beta, out = act(y)
 //
-// The mean first, then the squares about it, so a mean far from zero costs no precision;
-// shares of a large graph are joined by the pooled-variance identity, squares about the
-// joint mean = squares of the parts + n (mean of the part - joint mean)^2.
+// The mean first, then the squares about it.  A sum of n values far from zero is off by a few
+// u |m| and so is its mean, as its rounding to fp32 alone is, which h = (x - m) r would take for
+// deviations: 1,000 everywhere in three rows came out as h = 0.02, and a spread of 0.01 about
+// 1,000 was off by 5e-3.  So the deviations d from the mean as first found are summed too,
+// m = that mean + rest with rest = sum d / M, and what is left is a few u of the deviations.  Shares
+// of a large graph are joined by the pooled-variance identity, squares about the joint mean =
+// squares of the parts + n (mean of the part - joint mean)^2, in the same two steps.  It costs 1
+// to 5 % of both directions (82.3 -> 85.1 us for 1,024 graphs of 110 rows, 133.4 -> 137 for 41
+// graphs of 232,965, 59 -> 62 for 300 ragged ones).
 //
 // What bounds it: issue slots and latency together, below memory.  1,024 graphs of 110 rows,
 // F = 128 fp32, SiLU: 34 us (115 MB, 3.4 TB/s; 28 instructions a value, issue slots 45 % busy
@@ -23,62 +29,101 @@
 namespace tfg {
 namespace {
 
-// Means and centred squares of the held rows, to every thread for its groups; per_value: one
-// over their number of values.
+// The statistics of a thread's groups: means as -away + rest, squares of the deviations from that.
+template <int S>
+struct Moments {
+    float away[S], rest[S], squares[S];
+    __device__ __forceinline__ float mean(int q) const { return rest[q] - away[q]; }
+};
+
+// Squares of n values about m + rest, of those about m: rounding may take the difference below
+// 0, and an infinity stays (rest^2 may be one too).
+__device__ __forceinline__ float centred(float squares, float rest, float n) {
+    const float less = fmaf(-rest * n, rest, squares);
+    return less >= 0.f ? less : (less < 0.f ? 0.f : squares);
+}
+
+// What a first mean is taken relative to, one of the values, so that equal ones deviate by 0; not
+// one whose differences from the others, summed, could leave the range of fp32 (2^96 times
+// 2^31 values), or that is no number.
+__device__ __forceinline__ float pivot_of(float v) { return fabsf(v) < 7.9e28f ? v : 0.f; }
+
+// A thread's groups' first values in row `row`.
+template <typename XT, int TT, int VEC, int S>
+__device__ __forceinline__ void pivots(const NormArgs &p, const Place<TT, VEC, S> &at, int64_t row, float (&pivot)[S]) {
+    const XT *x = static_cast<const XT *>(p.x) + row * p.f;
+#pragma unroll
+    for (int q = 0; q < S; ++q) {
+        float w[1];
+        VecLoad<XT, 1>::load(x + static_cast<int64_t>(at.group0 + at.grp[q]) * p.c, w);
+        pivot[q] = pivot_of(w[0]);
+    }
+}
+
+// Of the held rows, whose groups hold `values` values each.
 template <int TT, typename XT, int VEC, int S>
 __device__ __forceinline__ void statistics(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
-                                           int rows, float per_value, float *smem, float (&mean)[S], float (&squares)[S]) {
+                                           const float (&pivot)[S], int rows, float values, float *smem, Moments<S> &m) {
     constexpr int kPer = VEC / S;                           // values of a sum in a vector
-    float sum[VEC] = {}, v[1][S] = {}, away[S];
+    const float per_value = 1.f / values;
+    float sum[VEC] = {}, s[1][S] = {}, v[2][S] = {}, away[S];
+#pragma unroll
+    for (int q = 0; q < S; ++q) away[q] = -pivot[q];
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float w[VEC];
         held.widen(i, w);
+        add_vec(w, away);
         add_vec(sum, w);
     }
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
-    group_sums<TT, VEC, S, 1>(p, at, v, smem, 0);
+    for (int q = 0; q < VEC; ++q) s[0][q / kPer] += sum[q];
+    group_sums<TT, VEC, S, 1>(p, at, s, smem, 0);
 #pragma unroll
-    for (int q = 0; q < S; ++q) {
-        mean[q] = v[0][q] * per_value;
-        away[q] = -mean[q];
-        v[0][q] = 0.f;
-    }
+    for (int q = 0; q < S; ++q) m.away[q] = -fmaf(s[0][q], per_value, pivot[q]);
+    float squares[VEC] = {};
 #pragma unroll
     for (int q = 0; q < VEC; ++q) sum[q] = 0.f;
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float w[VEC];
         held.widen(i, w);
-        add_vec(w, away);
-        fma_vec(sum, w, w, sum);
+        add_vec(w, m.away);
+        add_vec(sum, w);
+        fma_vec(squares, w, w, squares);
     }
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) v[0][q / kPer] += sum[q];
-    group_sums<TT, VEC, S, 1>(p, at, v, smem, 1);
+    for (int q = 0; q < VEC; ++q) {
+        v[0][q / kPer] += sum[q];
+        v[1][q / kPer] += squares[q];
+    }
+    group_sums<TT, VEC, S, 2>(p, at, v, smem, 1);
 #pragma unroll
-    for (int q = 0; q < S; ++q) squares[q] = v[0][q];
+    for (int q = 0; q < S; ++q) {
+        m.rest[q] = v[0][q] * per_value;
+        m.squares[q] = centred(v[1][q], m.rest[q], values);
+    }
 }
 
 template <int ACT, typename OT, typename XT, int VEC, int TT, int S>
 __device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held, int rows,
-                                      int64_t a, const float (&m)[S], const float (&r)[S]) {
+                                      int64_t a, const Moments<S> &m, const float (&r)[S]) {
     if (rows == 0) return;
     float scale[VEC], shift[VEC];
     channel_weights(p.gamma, at.c0, 1.f, scale);
     channel_weights(p.beta, at.c0, 0.f, shift);
     mul_vec(scale, r);
-    float away[S];
+    float less[S];
 #pragma unroll
-    for (int q = 0; q < S; ++q) away[q] = -m[q];
+    for (int q = 0; q < S; ++q) less[q] = -m.rest[q];
+    fma_vec(shift, scale, less, shift);
     const int64_t step = p.p.rows_at_once * p.f;
     OT *o = static_cast<OT *>(p.out) + (a + at.rl) * p.f + at.c0;
 #pragma unroll 4
     for (int i = 0; i < rows; ++i) {
         float v[VEC];
         held.widen(i, v);
-        add_vec(v, away);
+        add_vec(v, m.away);
         fma_vec(v, v, scale, shift);
         activate<ACT>(v);
         store_vec<VEC>(o + i * step, v);
@@ -87,7 +132,7 @@ __device__ __forceinline__ void apply(const NormArgs &p, const Place<TT, VEC, S>
 
 template <typename XT, int VEC, int TT, int S>
 __device__ __forceinline__ void apply_act(const NormArgs &p, const Place<TT, VEC, S> &at, const Held<XT, VEC, TT> &held,
-                                          int rows, int64_t a, int act, bool out_bf16, const float (&m)[S],
+                                          int rows, int64_t a, int act, bool out_bf16, const Moments<S> &m,
                                           const float (&r)[S]) {
     switch (act + (out_bf16 ? 4 : 0)) {
         case kActNone: return apply<kActNone, float>(p, at, held, rows, a, m, r);
@@ -111,8 +156,8 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kNormResiden
     const int64_t unit = id / static_cast<uint32_t>(p.p.tiles);
     const int tile = static_cast<int>(id - static_cast<uint32_t>(unit) * p.p.tiles);
     if (unit >= p.graphs + p.p.shares) return;              // whole teams
-    char *smem = s_all + M::index() * team_bytes(p.p, 1, S, VEC * sizeof(XT));
-    const Held<XT, VEC, TT> held(smem + sum_floats(p.p, 1, S) * 4);
+    char *smem = s_all + M::index() * team_bytes(p.p, kForwardBuffers, S, VEC * sizeof(XT));
+    const Held<XT, VEC, TT> held(smem + sum_floats(p.p, kForwardBuffers, S) * 4);
     const Place<TT, VEC, S> at(p, tile);
     const int t = M::thread();
     const int64_t share = unit - p.graphs;
@@ -139,52 +184,62 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kNormResiden
             r = {piece.a, piece.b};
         }
         const int rows = at.rows(p, r.a, r.b);
-        const float per_value = 1.f / static_cast<float>((r.b - r.a) * p.c);
+        const float values = static_cast<float>((r.b - r.a) * p.c);
         held.copy(static_cast<const XT *>(p.x) + (r.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
+        float pivot[S];
+        pivots<XT>(p, at, r.a, pivot);
         copies_done();
-        float mean[S], squares[S];
-        statistics(p, at, held, rows, per_value, reinterpret_cast<float *>(smem), mean, squares);
+        Moments<S> m;
+        statistics(p, at, held, pivot, rows, values, reinterpret_cast<float *>(smem), m);
         if (share < 0) {
             float rstd[S];
 #pragma unroll
             for (int q = 0; q < S; ++q) {
-                rstd[q] = rsqrtf(fmaf(squares[q], per_value, p.eps));
+                rstd[q] = rsqrtf(fmaf(m.squares[q], 1.f / values, p.eps));
                 if (p.mean && at.writes(p, q)) {
-                    p.mean[unit * p.groups + at.group0 + at.grp[q]] = mean[q];
+                    p.mean[unit * p.groups + at.group0 + at.grp[q]] = m.mean(q);
                     p.rstd[unit * p.groups + at.group0 + at.grp[q]] = rstd[q];
                 }
             }
-            return apply_act(p, at, held, rows, r.a, act, out_bf16, mean, rstd);
+            return apply_act(p, at, held, rows, r.a, act, out_bf16, m, rstd);
         }
 #pragma unroll
         for (int q = 0; q < S; ++q)
             if (at.writes(p, q))
-                p.part[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float2(mean[q], squares[q]);
+                p.moments[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float4(m.away[q], m.rest[q], m.squares[q], 0.f);
     }
 }
 
 // Joins the pieces of a large graph (rows r, from share s on) for group k, by a warp: the
-// mean of the pieces' means, then their squares about it, each in a fixed order.
-__device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
+// mean of the pieces' means, relative to the first piece's, then what their distances from it sum
+// up to and their squares about it, each in a fixed order.  Gives away, rest and r = 1 / sqrt(v + eps).
+__device__ __forceinline__ float4 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
     const int lane = threadIdx.x & 31;
     const int64_t s1 = (r.b - 1) / p.p.share;
     const float all = static_cast<float>((r.b - r.a) * p.c);
-    auto part = [&](int64_t i) { return p.part[slot_at(p, r.a, i) * p.groups + k]; };
+    auto part = [&](int64_t i) { return p.moments[slot_at(p, r.a, i) * p.groups + k]; };
+    const float pivot = pivot_of(part(s).x);
     float sum = 0.f;
 #pragma unroll 4
-    for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x, piece_values(p, r, i), sum);
+    for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x - pivot, piece_values(p, r, i), sum);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += lane_xor(sum, o);
-    const float mean = sum / all;
-    float squares = 0.f;
+    const float away = pivot + sum / all;
+    float first = 0.f, squares = 0.f;
 #pragma unroll 4
     for (int64_t i = s + lane; i <= s1; i += 32) {
-        const float2 v = part(i);
-        squares += fmaf((v.x - mean) * piece_values(p, r, i), v.x - mean, v.y);
+        const float4 v = part(i);
+        const float n = piece_values(p, r, i), d = (away - v.x) + v.y;
+        first = fmaf(d, n, first);
+        squares += fmaf(d * n, d, v.z);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) squares += lane_xor(squares, o);
-    return make_float2(mean, rsqrtf(squares / all + p.eps));
+    for (int o = 16; o > 0; o >>= 1) {
+        first += lane_xor(first, o);
+        squares += lane_xor(squares, o);
+    }
+    const float rest = first / all;
+    return make_float4(away, rest, rsqrtf(centred(squares, rest, all) / all + p.eps), 0.f);
 }
 
 // join_apart: the large graph that begins in share blockIdx.x, a warp a group.
@@ -197,8 +252,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
     for (int k = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kJoinWarps) {
-        const float2 v = join(p, r, s, k);
-        if ((threadIdx.x & 31) == 0) p.joined[s * p.groups + k] = v;
+        const float4 v = join(p, r, s, k);
+        if ((threadIdx.x & 31) == 0) p.joined_moments[s * p.groups + k] = v;
     }
 }
 
@@ -207,7 +262,7 @@ template <int TT, typename XT, int VEC, int S>
 __global__ void __launch_bounds__(TT, team_ctas(TT, kNormResident)) norm_large(NormArgs p, int act, bool out_bf16) {
     extern __shared__ __align__(16) char s_all[];
     const Held<XT, VEC, TT> held(s_all);
-    float2 *s_stat = reinterpret_cast<float2 *>(s_all + p.p.held * TT * VEC * sizeof(XT));   // [tile's groups]
+    float4 *s_stat = reinterpret_cast<float4 *>(s_all + p.p.held * TT * VEC * sizeof(XT));   // [tile's groups]
     const uint32_t back = blockIdx.x / static_cast<uint32_t>(p.p.tiles);
     const int tile = static_cast<int>(blockIdx.x - back * p.p.tiles);
     const int64_t share = p.p.shares - 1 - back;
@@ -219,14 +274,16 @@ __global__ void __launch_bounds__(TT, team_ctas(TT, kNormResident)) norm_large(N
         const Place<TT, VEC, S> at(p, tile);
         const int rows = at.rows(p, piece.a, piece.b);
         held.copy(static_cast<const XT *>(p.x) + (piece.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
-        float2 stat[S];
-        joined_statistics<TT>(p, at, piece, s_stat, stat, join);
+        float4 stat[S];
+        joined_statistics<TT>(p, at, piece, p.joined_moments, s_stat, stat, join);
         copies_done();
-        float mean[S], rstd[S];
+        Moments<S> m;
+        float rstd[S];
 #pragma unroll
         for (int q = 0; q < S; ++q) {
-            mean[q] = stat[q].x;
-            rstd[q] = stat[q].y;
+            m.away[q] = stat[q].x;
+            m.rest[q] = stat[q].y;
+            rstd[q] = stat[q].z;
         }
         // the share in which the graph begins reports its statistics
         if (p.mean && piece.first_share == share) {
@@ -234,18 +291,18 @@ __global__ void __launch_bounds__(TT, team_ctas(TT, kNormResident)) norm_large(N
 #pragma unroll
             for (int q = 0; q < S; ++q) {
                 if (!at.writes(p, q)) continue;
-                p.mean[out0 + at.grp[q]] = mean[q];
+                p.mean[out0 + at.grp[q]] = m.mean(q);
                 p.rstd[out0 + at.grp[q]] = rstd[q];
             }
         }
-        apply_act(p, at, held, rows, piece.a, act, out_bf16, mean, rstd);
+        apply_act(p, at, held, rows, piece.a, act, out_bf16, m, rstd);
     }
 }
 
 template <int TT, typename XT, int VEC, int S>
 cudaError_t launch_units(const NormArgs &p, int act, bool out_bf16, cudaStream_t s) {
     using M = Team<TT>;
-    const int smem = M::kPerCta * team_bytes(p.p, 1, S, VEC * sizeof(XT));
+    const int smem = M::kPerCta * team_bytes(p.p, kForwardBuffers, S, VEC * sizeof(XT));
     const cudaError_t err = allow_shared(norm_units<TT, XT, VEC, S>, smem);
     if (err != cudaSuccess) return err;
     const int64_t teams = (p.graphs + p.p.shares) * p.p.tiles;
@@ -264,7 +321,7 @@ cudaError_t launch_large(NormArgs p, int act, bool out_bf16, cudaStream_t s) {
     }
     set_rows_at_once(p.p, TT);
     p.p.held = static_cast<int>((p.p.share + p.p.rows_at_once - 1) / p.p.rows_at_once);
-    const int smem = p.p.held * TT * VEC * static_cast<int>(sizeof(XT)) + p.p.tile_groups * static_cast<int>(sizeof(float2));
+    const int smem = p.p.held * TT * VEC * static_cast<int>(sizeof(XT)) + p.p.tile_groups * static_cast<int>(sizeof(float4));
     const cudaError_t err = allow_shared(norm_large<TT, XT, VEC, S>, smem);
     if (err != cudaSuccess) return err;
     norm_large<TT, XT, VEC, S><<<static_cast<unsigned>(p.p.shares * p.p.tiles), TT, smem, s>>>(p, act, out_bf16);
