@@ -114,7 +114,7 @@ struct NormPlan {
     int64_t most;         // rows of a graph that is not large
     int64_t share;        // rows of a share, at most that
     int64_t shares;       // 0: no graph can be large
-    bool join_apart;      // large graphs of so many shares that a kernel of its own joins them
+    bool join_apart;      // there may be large graphs of so many shares that a kernel of its own joins them
 };
 
 // The rows of a large graph that share s holds in a slot, written by the first kernel.
@@ -222,11 +222,6 @@ __device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int sl
     p.graph = g;
     p.first_share = r.a / a.p.share;
     return p;
-}
-
-// The slot of share s that holds a piece of the graph whose first row is a.
-__device__ __forceinline__ int64_t slot_at(const NormArgs &p, int64_t a, int64_t s) {
-    return s * 2 + (a > s * p.p.share ? 1 : 0);
 }
 
 // ---- a team -------------------------------------------------------------------------
@@ -445,14 +440,80 @@ __device__ __forceinline__ bool no_piece(const NormArgs &p, int64_t share) {
     return a.x == a.y && b.x == b.y;
 }
 
-// Values of the piece of rows r in share i, and its slot.
-__device__ __forceinline__ float piece_values(const NormArgs &p, const RowRange &r, int64_t i) {
-    const int64_t a = i * p.p.share, b = a + p.p.share;
-    return static_cast<float>(((b < r.b ? b : r.b) - (a > r.a ? a : r.a)) * p.c);
-}
+// ---- joins of the pieces of a large graph ----------------------------------------------
+// By a warp or a CTA of TT threads: 2^log_groups groups side by side, whose parts of a piece lie side by
+// side too, and the other threads take pieces in turn.  (A warp a group, its lanes on pieces, read
+// 16 bytes of every line: 112,640 rows, one graph of 101,000 and 1,024 small ones, F = 128 fp32 in
+// 32 groups, forward 129 us against 57.)
+template <int TT>
+struct JoinPlace {
+    int log_groups, k, lane, lanes;
+    __device__ __forceinline__ explicit JoinPlace(int groups) {
+        log_groups = 0;
+        while ((1 << log_groups) < groups && (1 << log_groups) < TT) ++log_groups;
+        const int t = TT == 32 ? threadIdx.x & 31 : threadIdx.x;
+        k = t & ((1 << log_groups) - 1);
+        lane = t >> log_groups;
+        lanes = TT >> log_groups;
+    }
+    // Sums over the threads of a group, in a fixed order, to each of them.  Collective.
+    template <int N>
+    __device__ __forceinline__ void sums(float (&v)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            for (int o = 1 << log_groups; o < 32; o <<= 1) v[i] += lane_xor(v[i], o);
+        if constexpr (TT > 32) {
+            __shared__ float s_sum[N][TT];
+            const int wide = max(32, 1 << log_groups);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s_sum[i][threadIdx.x] = v[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[i] = 0.f;
+                for (int t = k; t < TT; t += wide) v[i] += s_sum[i][t];
+            }
+            __syncthreads();
+        }
+    }
+};
+
+// The parts of a large graph's pieces for one group: its rows r begin in share s, there in slot 1
+// if behind the share's first row, and go on in slot 0 of the shares behind it.
+template <typename Part>
+struct Pieces {
+    const Part *first, *rest;                               // piece j > 0 at rest + j * stride
+    int stride, last;
+
+    __device__ __forceinline__ Pieces(const NormArgs &p, const Part *parts, const RowRange &r, int64_t s, int k) {
+        stride = 2 * p.groups;
+        rest = parts + s * stride + k;
+        first = rest + (r.a > s * p.p.share ? p.groups : 0);
+        last = static_cast<int>((r.b - 1) / p.p.share - s);
+    }
+    // use(part) for those of this thread, read four at a time, the last ones too (behind the end: read, not used)
+    template <int TT, typename Use>
+    __device__ __forceinline__ void walk(const JoinPlace<TT> &at, Use use) const {
+        for (int j0 = at.lane; j0 <= last; j0 += 4 * at.lanes) {
+            Part v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = min(j0 + u * at.lanes, last);
+                v[u] = j == 0 ? *first : rest[static_cast<int64_t>(j) * stride];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j0 + u * at.lanes <= last) use(v[u]);
+        }
+    }
+};
+
+// Graphs of few pieces are joined by warps, kJoinGroups groups each: 16 rounds of their four
+// lanes a group at most, and no barrier; the others by whole CTAs.
+constexpr int kJoinFew = 64, kJoinGroups = 8;
 
 // Joined statistics of this thread's groups of a piece's graph: what a kernel of its own
-// joined, or join(rows, first share, group) by a warp a group, through s_stat[group].
+// joined, or join(place, rows, first share, group) of this CTA, through s_stat[group].
 // Collective over the CTA.
 template <int TT, typename At, int S, typename Stat, typename Join>
 __device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &at, const Piece &piece, const Stat *joined,
@@ -465,14 +526,81 @@ __device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &a
     }
     bool bad;
     const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
+    auto groups_of = [&](const auto &place, int k0, int step) {
+        for (; k0 < at.groups; k0 += step) {
+            const int k = k0 + place.k;
+            const Stat v = join(place, r, piece.first_share, at.group0 + min(k, at.groups - 1));
+            if (place.lane == 0 && k < min(at.groups, k0 + (1 << place.log_groups))) s_stat[k] = v;
+        }
+    };
     __syncthreads();                                        // the last statistics have been read
-    for (int k = threadIdx.x >> 5; k < at.groups; k += TT / 32) {
-        const Stat v = join(p, r, piece.first_share, at.group0 + k);
-        if ((threadIdx.x & 31) == 0) s_stat[k] = v;
+    if (r.b - r.a <= kJoinFew * p.p.share) {
+        groups_of(JoinPlace<32>(min(at.groups, kJoinGroups)), (threadIdx.x >> 5) * kJoinGroups, TT / 32 * kJoinGroups);
+    } else {
+        const JoinPlace<TT> place(at.groups);
+        groups_of(place, 0, 1 << place.log_groups);
     }
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < S; ++q) stat[q] = s_stat[at.grp[q]];
+}
+
+// join_apart: a CTA takes a range of shares and kJoinGroups groups and finds the shares in which
+// large graphs begin (one at most in each: such a graph has more rows than a share).  Its warps
+// join those of few pieces, a graph each, and then all of them together the long ones.  One
+// wave of CTAs whatever the number of shares.
+constexpr int kJoinThreads = 512, kJoinCtas = 608;
+struct JoinRange {
+    int64_t per_cta;      // shares
+    dim3 grid;
+};
+inline JoinRange join_range(const NormPlan &p, int groups) {
+    const int64_t y = min64((groups + kJoinGroups - 1) / kJoinGroups, 65535);
+    const int64_t per = (p.shares * y + kJoinCtas - 1) / kJoinCtas;
+    return {per, dim3(static_cast<unsigned>((p.shares + per - 1) / per), static_cast<unsigned>(y))};
+}
+
+template <typename Stat, typename Join>
+__device__ __forceinline__ void join_graphs(const NormArgs &p, int64_t per_cta, Stat *joined, Join join) {
+    __shared__ int64_t s_share[kJoinThreads], s_graph[kJoinThreads];
+    __shared__ int s_count;
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * per_cta, to = min64(p.p.shares, from + per_cta);
+    auto one = [&](const auto &place, int64_t s, const RowRange &r) {
+        for (int k0 = blockIdx.y * kJoinGroups; k0 < p.groups; k0 += gridDim.y * kJoinGroups) {
+            const int k = k0 + place.k;
+            const Stat v = join(place, r, s, min(k, p.groups - 1));
+            if (place.lane == 0 && k < min(p.groups, k0 + kJoinGroups)) joined[s * p.groups + k] = v;
+        }
+    };
+    for (int64_t s0 = from; s0 < to; s0 += kJoinThreads) {
+        if (threadIdx.x == 0) s_count = 0;
+        __syncthreads();
+        const int64_t mine = s0 + threadIdx.x;
+        if (mine < to) {
+#pragma unroll
+            for (int slot = 0; slot < 2; ++slot) {
+                const Piece piece = p.pieces[mine * 2 + slot];
+                if (piece.a == piece.b || piece.first_share != mine) continue;
+                const int at = atomicAdd(&s_count, 1);      // in any order: each is joined by itself
+                if (at < kJoinThreads) {
+                    s_share[at] = mine;
+                    s_graph[at] = piece.graph;
+                }
+            }
+        }
+        __syncthreads();
+        const int count = min(s_count, kJoinThreads);
+        bool bad;
+        for (int i = threadIdx.x >> 5; i < count; i += kJoinThreads / 32) {
+            const RowRange r = graph_rows(p.offsets, s_graph[i], p.n, bad);
+            if (r.b - r.a <= kJoinFew * p.p.share) one(JoinPlace<32>(min(p.groups, kJoinGroups)), s_share[i], r);
+        }
+        for (int i = 0; i < count; ++i) {
+            const RowRange r = graph_rows(p.offsets, s_graph[i], p.n, bad);
+            if (r.b - r.a > kJoinFew * p.p.share) one(JoinPlace<kJoinThreads>(min(p.groups, kJoinGroups)), s_share[i], r);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- host ---------------------------------------------------------------------------
@@ -509,6 +637,19 @@ constexpr int kNormRoom = 55 * 1024;
 // 35 fp32, both directions: 122 us against 231 with room for 8 rows, 4,096 single rows 16.5 / 17.8.
 constexpr int kFreeShared = 216, kFewRows = 64;
 constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: room, a row's rounding, statistics
+
+// Large graphs are joined by the second kernel itself, which saves a launch, as long as that costs
+// little even where one graph has almost all rows: up to so many parts (a piece's sums for one
+// group) read by a CTA, and by all of them.  Forward + backward in place / by a kernel of its
+// own, one graph of 90 % of the rows among small ones, F = 128 fp32:
+//   100 shares of 32 groups (20,000 rows)      14 + 17 /  17 + 20 us
+//   385 shares of 32 groups (20,000)           25 + 27 /  20 + 25      12,320 parts a CTA
+//   510 shares of 32 groups (112,640)          57 + 70 /  44 + 63      8 to 12 million in all
+//   2,013 shares of 32 groups (249,576)       243 + 584 / 94 + 181
+//   1,212 shares of one group (112,640)        42 + 72 /  41 + 80
+//   4,051 shares of one group (109,376)        94 + 163 / 50 + 174
+// A batch without large graphs pays 3 + 2 us of 29 + 50 for the kernel (112,131 rows in 1,024 graphs).
+constexpr int64_t kPartsInPlace = 12288, kReadsInPlace = 12 << 20;
 
 // operands: arrays whose rows are held; row_bytes: of the vectors held per row and thread.
 // Tiles are whole groups and whole vectors: 32 vectors of a row, fewer (128 bytes at least)
@@ -567,7 +708,10 @@ NormPlan norm_plan(int64_t n, int64_t graphs, int64_t f, int64_t c, int vec, int
     if (p.share < few) p.share = few;
     if (p.share > p.most || 2 * mean <= p.most) p.share = p.most;
     p.shares = n <= p.most ? 0 : (n + p.share - 1) / p.share;
-    p.join_apart = mean > 8 * p.share && p.shares * (f / c) >= 2048;
+    // One graph may hold almost all rows, whatever the mean: every CTA of the second kernel would
+    // read all pieces' parts of its tile.
+    const int64_t parts = p.shares * (f / c);
+    p.join_apart = (parts >= 2048 && mean > 8 * p.share) || p.shares * p.tile_groups > kPartsInPlace || parts * p.shares > kReadsInPlace;
     return p;
 }
 

@@ -207,38 +207,23 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kBackResiden
     }
 }
 
-// Sums over M of a large graph (rows r, from share s on) for group k, by a warp.
-__device__ __forceinline__ float2 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
-    const int64_t s1 = (r.b - 1) / p.p.share;
+// Sums over M of a large graph (rows r, from share s on) for group k.
+template <int TT>
+__device__ __forceinline__ float2 join(const NormArgs &p, const JoinPlace<TT> &at, const RowRange &r, int64_t s, int k) {
     const float all = static_cast<float>((r.b - r.a) * p.c);
-    float x = 0.f, y = 0.f;
-#pragma unroll 4
-    for (int64_t i = s + (threadIdx.x & 31); i <= s1; i += 32) {
-        const float2 v = p.part[slot_at(p, r.a, i) * p.groups + k];
-        x += v.x;
-        y += v.y;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        x += lane_xor(x, o);
-        y += lane_xor(y, o);
-    }
-    return make_float2(x / all, y / all);
+    float v[2] = {0.f, 0.f};
+    Pieces<float2>(p, p.part, r, s, k).walk(at, [&](const float2 &w) {
+        v[0] += w.x;
+        v[1] += w.y;
+    });
+    at.sums(v);
+    return make_float2(v[0] / all, v[1] / all);
 }
 
-// join_apart: the large graph that begins in share blockIdx.x, a warp a group.
-constexpr int kBackJoinWarps = 8;
-__global__ void __launch_bounds__(kBackJoinWarps * 32) norm_back_join(NormArgs p) {
-    const int64_t s = blockIdx.x;
-    Piece piece = p.pieces[s * 2];
-    if (piece.a == piece.b || piece.first_share != s) piece = p.pieces[s * 2 + 1];
-    if (piece.a == piece.b || piece.first_share != s) return;
-    bool bad;
-    const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
-    for (int k = blockIdx.y * kBackJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kBackJoinWarps) {
-        const float2 v = join(p, r, s, k);
-        if ((threadIdx.x & 31) == 0) p.joined[s * p.groups + k] = v;
-    }
+__global__ void __launch_bounds__(kJoinThreads) norm_back_join(NormArgs p, int64_t per_cta) {
+    join_graphs(p, per_cta, p.joined, [&](const auto &at, const RowRange &r, int64_t s, int k) {
+        return join(p, at, r, s, k);
+    });
 }
 
 // grad_gamma and grad_beta of four channels: the teams' sums, 64 interleaved in order.  Of
@@ -307,7 +292,8 @@ norm_back_large(NormArgs p, int channel_ctas, float *grad_gamma, float *grad_bet
         c.weights(p, at);
         c.statistics(p, at, piece.graph);
         float2 stat[S];
-        joined_statistics<TT>(p, at, piece, p.joined, s_stat, stat, join);
+        joined_statistics<TT>(p, at, piece, p.joined, s_stat, stat,
+                              [&](const auto &place, const RowRange &r, int64_t s, int k) { return join(p, place, r, s, k); });
         copies_done();
         float s[2][S];
 #pragma unroll
@@ -336,9 +322,8 @@ cudaError_t launch_units(const NormArgs &p, cudaStream_t s) {
 template <int ACT, int TT, typename XT, typename GT, int VEC, int S>
 cudaError_t launch_large(NormArgs p, float *grad_gamma, float *grad_beta, cudaStream_t s) {
     if (p.p.join_apart && p.p.shares > 0) {
-        const dim3 grid(static_cast<unsigned>(p.p.shares),
-                        static_cast<unsigned>(min64((p.groups + kBackJoinWarps - 1) / kBackJoinWarps, 65535)));
-        norm_back_join<<<grid, kBackJoinWarps * 32, 0, s>>>(p);
+        const JoinRange range = join_range(p.p, p.groups);
+        norm_back_join<<<range.grid, kJoinThreads, 0, s>>>(p, range.per_cta);
         const cudaError_t launched = cudaGetLastError();
         if (launched != cudaSuccess) return launched;
     }

@@ -206,55 +206,35 @@ __global__ void __launch_bounds__(Team<TT>::kThreads, team_ctas(TT, kNormResiden
 #pragma unroll
         for (int q = 0; q < S; ++q)
             if (at.writes(p, q))
-                p.moments[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float4(m.away[q], m.rest[q], m.squares[q], 0.f);
+                p.moments[(share * 2 + slot) * p.groups + at.group0 + at.grp[q]] = make_float4(m.away[q], m.rest[q], m.squares[q], values);
     }
 }
 
-// Joins the pieces of a large graph (rows r, from share s on) for group k, by a warp: the
-// mean of the pieces' means, relative to the first piece's, then what their distances from it sum
-// up to and their squares about it, each in a fixed order.  Gives away, rest and r = 1 / sqrt(v + eps).
-__device__ __forceinline__ float4 join(const NormArgs &p, const RowRange &r, int64_t s, int k) {
-    const int lane = threadIdx.x & 31;
-    const int64_t s1 = (r.b - 1) / p.p.share;
-    const float all = static_cast<float>((r.b - r.a) * p.c);
-    auto part = [&](int64_t i) { return p.moments[slot_at(p, r.a, i) * p.groups + k]; };
-    const float pivot = pivot_of(part(s).x);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int64_t i = s + lane; i <= s1; i += 32) sum = fmaf(part(i).x - pivot, piece_values(p, r, i), sum);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += lane_xor(sum, o);
-    const float away = pivot + sum / all;
-    float first = 0.f, squares = 0.f;
-#pragma unroll 4
-    for (int64_t i = s + lane; i <= s1; i += 32) {
-        const float4 v = part(i);
-        const float n = piece_values(p, r, i), d = (away - v.x) + v.y;
-        first = fmaf(d, n, first);
-        squares += fmaf(d * n, d, v.z);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        first += lane_xor(first, o);
-        squares += lane_xor(squares, o);
-    }
-    const float rest = first / all;
-    return make_float4(away, rest, rsqrtf(centred(squares, rest, all) / all + p.eps), 0.f);
+// Joins the pieces of a large graph (rows r, from share s on) for group k: the mean of the
+// pieces' means, relative to the first piece's, then what their distances from it sum up to and
+// their squares about it, each in a fixed order.  Gives away, rest and r = 1 / sqrt(v + eps).
+template <int TT>
+__device__ __forceinline__ float4 join(const NormArgs &p, const JoinPlace<TT> &at, const RowRange &r, int64_t s, int k) {
+    const Pieces<float4> pieces(p, p.moments, r, s, k);
+    const float all = static_cast<float>((r.b - r.a) * p.c), pivot = pivot_of(pieces.first->x);
+    float first[1] = {0.f}, v[2] = {0.f, 0.f};
+    pieces.walk(at, [&](const float4 &w) { first[0] = fmaf(w.x - pivot, w.w, first[0]); });
+    at.sums(first);
+    const float away = pivot + first[0] / all;
+    pieces.walk(at, [&](const float4 &w) {
+        const float d = (away - w.x) + w.y;
+        v[0] = fmaf(d, w.w, v[0]);
+        v[1] += fmaf(d * w.w, d, w.z);
+    });
+    at.sums(v);
+    const float rest = v[0] / all;
+    return make_float4(away, rest, rsqrtf(centred(v[1], rest, all) / all + p.eps), 0.f);
 }
 
-// join_apart: the large graph that begins in share blockIdx.x, a warp a group.
-constexpr int kJoinWarps = 8;
-__global__ void __launch_bounds__(kJoinWarps * 32) norm_join(NormArgs p) {
-    const int64_t s = blockIdx.x;
-    Piece piece = p.pieces[s * 2];
-    if (piece.a == piece.b || piece.first_share != s) piece = p.pieces[s * 2 + 1];
-    if (piece.a == piece.b || piece.first_share != s) return;
-    bool bad;
-    const RowRange r = graph_rows(p.offsets, piece.graph, p.n, bad);
-    for (int k = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); k < p.groups; k += gridDim.y * kJoinWarps) {
-        const float4 v = join(p, r, s, k);
-        if ((threadIdx.x & 31) == 0) p.joined_moments[s * p.groups + k] = v;
-    }
+__global__ void __launch_bounds__(kJoinThreads) norm_join(NormArgs p, int64_t per_cta) {
+    join_graphs(p, per_cta, p.joined_moments, [&](const auto &at, const RowRange &r, int64_t s, int k) {
+        return join(p, at, r, s, k);
+    });
 }
 
 // The pieces of large graphs once more, a CTA a (share, tile), the last share first.
@@ -275,7 +255,8 @@ __global__ void __launch_bounds__(TT, team_ctas(TT, kNormResident)) norm_large(N
         const int rows = at.rows(p, piece.a, piece.b);
         held.copy(static_cast<const XT *>(p.x) + (piece.a + at.rl) * p.f + at.c0, rows, p.p.rows_at_once * p.f);
         float4 stat[S];
-        joined_statistics<TT>(p, at, piece, p.joined_moments, s_stat, stat, join);
+        joined_statistics<TT>(p, at, piece, p.joined_moments, s_stat, stat,
+                              [&](const auto &place, const RowRange &r, int64_t s, int k) { return join(p, place, r, s, k); });
         copies_done();
         Moments<S> m;
         float rstd[S];
@@ -314,8 +295,8 @@ cudaError_t launch_units(const NormArgs &p, int act, bool out_bf16, cudaStream_t
 template <int TT, typename XT, int VEC, int S>
 cudaError_t launch_large(NormArgs p, int act, bool out_bf16, cudaStream_t s) {
     if (p.p.join_apart) {
-        const dim3 grid(static_cast<unsigned>(p.p.shares), static_cast<unsigned>(min64((p.groups + kJoinWarps - 1) / kJoinWarps, 65535)));
-        norm_join<<<grid, kJoinWarps * 32, 0, s>>>(p);
+        const JoinRange range = join_range(p.p, p.groups);
+        norm_join<<<range.grid, kJoinThreads, 0, s>>>(p, range.per_cta);
         const cudaError_t launched = cudaGetLastError();
         if (launched != cudaSuccess) return launched;
     }
