@@ -673,7 +673,8 @@ int tfg_group_norm_backward(const void *x, int x_dtype, const int64_t *node_offs
  *        aligned.
  * Squares are summed in fp32 with the additions' errors carried, in fp64
  * where they leave its range; the joined sum, the root and the quotient are
- * fp64.  Fixed order: bitwise reproducible.
+ * fp64, the quotient rounded to 24 bits whatever its size.  Fixed order: bitwise
+ * reproducible.
  * ---------------------------------------------------------------------- */
 int tfg_global_norm_workspace_size(int64_t num_tensors, size_t *bytes);
 int tfg_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes,

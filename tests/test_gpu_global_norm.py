@@ -171,3 +171,15 @@ def test_more_than_2_32_values():
     assert abs(float(norm) - want) <= 7 * U * want
     f = 65536.0 / want
     assert bool((x[:-1] == x[0]).all()) and abs(float(x[0]) - f) <= 2.0 ** -8 * f and abs(float(x[-1]) - 3 * f) <= 2.0 ** -8 * 3 * f
+
+
+@pytest.mark.parametrize("size,clip", [(1e36, 1e-3), (1e36, 1e-6), (3e35, 1e-9), (1e20, 1e-20), (1e30, 1e-30)])
+def test_factors_below_the_normal_numbers(size, clip):
+    """clip_norm / norm has no fp32 value of full precision; the clipped values have."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    ts = [torch.randn(k, device="cuda", generator=gen, dtype=dt) * size
+          for k, dt in ((5000, torch.float32), (999, torch.bfloat16), (1, torch.float32))]
+    outs, _ = check(ts, clip)
+    assert float(outs[0].abs().max()) > clip * 1e-2
+    before = [t.clone() for t in ts]
+    check(ts, clip, outs=ts, inputs=before)
