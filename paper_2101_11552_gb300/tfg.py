@@ -753,6 +753,14 @@ def _need_ids(ids):
     return index, id32
 
 
+def _padding(padding_id: Optional[int]) -> int:
+    if padding_id is None:
+        return NO_PADDING
+    if not NO_PADDING <= padding_id < 1 << 63:    # ctypes would pass its lowest 64 bits
+        raise ValueError(f"padding_id must be an int64, got {padding_id}")
+    return padding_id
+
+
 def _size(name: str, *args) -> int:
     """A workspace query."""
     n = ctypes.c_size_t()
@@ -778,7 +786,7 @@ def tfg_embedding_lookup(table, ids, scale: float = 1.0, padding_id: Optional[in
     out = _need_out("out", out, (*ids.shape, f), out_dtype, table)
     status = torch.empty(1, dtype=torch.int32, device=table.device)
     _run(index, "tfg_embedding_lookup32" if id32 else "tfg_embedding_lookup", ids.data_ptr(), ids.numel(),
-         table.data_ptr(), codes[0], v, f, scale, NO_PADDING if padding_id is None else padding_id, out.data_ptr(),
+         table.data_ptr(), codes[0], v, f, scale, _padding(padding_id), out.data_ptr(),
          codes[1], status.data_ptr())
     return out, status
 
@@ -801,7 +809,7 @@ def tfg_group_ids(ids, num_rows: int, padding_id: Optional[int] = None, workspac
     workspace = _workspace(workspace, tfg_group_ids_workspace_size(num_rows, n), ids)
     rowptr, sorted_ids, perm, status = (torch.empty(k, dtype=torch.int32, device=dev) for k in (num_rows + 1, n, n, 1))
     _run(index, "tfg_group_ids32" if id32 else "tfg_group_ids", ids.data_ptr(), n, num_rows,
-         NO_PADDING if padding_id is None else padding_id, rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(),
+         _padding(padding_id), rowptr.data_ptr(), sorted_ids.data_ptr(), perm.data_ptr(),
          *_span(workspace), status.data_ptr())
     return IdGroups(rowptr, sorted_ids, perm, status)
 

@@ -256,3 +256,13 @@ def test_binding_refuses():
     with pytest.raises(tfg.TfgError) as e:
         tfg.tfg_group_ids(ids.repeat(1000), 5, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.code == tfg.TFG_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("bad", [2 ** 63, 2 ** 64 - 1, 2 ** 64 + 2, -2 ** 63 - 1])
+def test_padding_ids_that_no_int64_holds_are_refused(bad):
+    """They would be taken for the id that they equal in the lowest 64 bits."""
+    table, ids = torch.randn(5, 4, device="cuda"), torch.tensor([0, 2, -1], device="cuda")
+    with pytest.raises(ValueError):
+        tfg.tfg_embedding_lookup(table, ids, padding_id=bad)
+    with pytest.raises(ValueError):
+        tfg.tfg_group_ids(ids, 5, padding_id=bad)
