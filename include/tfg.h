@@ -564,7 +564,8 @@ int tfg_batch_graphs(int64_t num_graphs, const int64_t *node_counts, const int64
  * num_rows, num_ids < 2^31 - 1; num_features <= 8,388,480 (65,535 * 128).  out and
  * grad_table must not overlap the inputs.  16-byte aligned pointers and
  * num_features a multiple of 4 (8 between bf16 arrays) select the vector
- * kernels; the results are the same.
+ * kernels.  The lookup's results are the same; the gradient's sums are split
+ * otherwise, so it is bitwise reproducible between calls of the same alignment.
  * ---------------------------------------------------------------------- */
 int tfg_embedding_lookup(const int64_t *ids, int64_t num_ids, const void *table, int table_dtype,
                          int64_t num_rows, int64_t num_features, float scale, int64_t padding_id,
@@ -626,9 +627,10 @@ int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, con
  *   The offsets are the forward's: they are not reported a second time.
  * An offset common to the values of a (graph, group) costs the forward nothing:
  * the deviations are taken from the mean before its rounding to fp32, and equal
- * values give beta.  The backward has the mean as reported: its h is off by up
+ * values give y = beta.  The backward has the mean as reported: its h is off by up
  * to |m| r 2^-24.
- * At most 1,024 channels per group (TFG_ERR_TOO_LARGE).  Statistics and sums
+ * At most 1,024 channels per group (TFG_ERR_TOO_LARGE): a CTA holds a group's
+ * part of a row, in odd widths a value a thread.  Statistics and sums
  * in fp32 in a fixed order: bitwise reproducible; deviations from a mean whose
  * squares add up past 3e38 (values of about 1e17 and more) give a rstd of 0.
  * ---------------------------------------------------------------------- */

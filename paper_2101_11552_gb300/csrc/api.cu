@@ -1128,7 +1128,7 @@ int tfg_embedding_backward(const int32_t *rowptr, const int32_t *sorted_ids, con
 
 // ---- group norm -------------------------------------------------------------------
 namespace {
-constexpr int64_t kMaxGroupChannels = 1024;
+constexpr int64_t kMaxGroupChannels = 1024;       // a row of a group, value by value, in a team of at most 1,024 threads
 
 int check_group_norm(const char *fn, int64_t num_nodes, int64_t num_graphs, int64_t num_features, int64_t num_groups) {
     TFG_TRY(check_counts(fn, num_nodes, 0));
@@ -1282,7 +1282,7 @@ int check_tensors(const char *fn, int64_t num_tensors, const void *const *tensor
     return TFG_OK;
 }
 
-// A range of bytes that a call reads (out = -1) or writes (out = the tensor's number).
+// The bytes of a tensor that a call reads, or writes (out).
 struct Extent {
     uintptr_t at;
     size_t bytes;

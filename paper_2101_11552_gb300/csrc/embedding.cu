@@ -10,7 +10,8 @@
 //
 // What bounds it.  The lookup moves bytes: 131,072 rows of 1,024 bf16 of a table of 50,000 in
 // 55 us (334 MB at the least, 6.1 TB/s; ids follow a Zipf law), 112,640 rows of 128 fp32 in 17 us
-// (58 MB, 3.4 TB/s: one short wave of latency), 64 rows in 2.8 us (the launch).  The gradient
+// (58 MB, 3.4 TB/s: issue slots 53 % busy, 64 warp instructions a row of 512 bytes), 64 rows in 2.1
+// us (the launch).  The gradient
 // writes the whole table: 131,072 bf16 rows of 1,024 into 50,000 fp32 rows in 83 us (446 MB,
 // 5.4 TB/s), 60,000 rows of 100 into 169,343 in 28 us (80 MB, 2.8 TB/s: the second launch,
 // and chains of id -> position -> row at 12 positions a worker), 112,640 rows of 128 into 119
@@ -34,7 +35,7 @@ constexpr int kLookupRows = 4;
 // are read and written together.  The product is formed in fp32 and rounded once more
 // where the output is bf16.
 //
-// The status: up to kLookupCheck ids the first CTA of the grid looks through all of them
+// The status: up to kLookupCheck ids the last CTA of the grid looks through all of them
 // and writes the word (check), which saves the launch that clears it; else every group
 // reports its own.
 constexpr int64_t kLookupCheck = 8192;

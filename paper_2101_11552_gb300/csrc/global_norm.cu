@@ -9,7 +9,7 @@
 // order and scales its share.  Both walk chunks of kChunk values across all tensors, so
 // that a model of many small tensors costs no more launches than one large tensor.
 //
-// Precision.  A thread adds 64 squares in fp32 and carries the sums of those in two
+// Precision.  A thread adds 32 squares in fp32 and carries the sums of those in two
 // floats (the rounding error of every addition is kept), so long gradients lose nothing;
 // squares that leave the range of fp32 (values above 1e15 or all below 1e-13 or so) are
 // taken again in fp64.  The partials, the root and the factor are fp64, and the factor is
@@ -18,8 +18,8 @@
 // What bounds it: memory.  1,000 million bf16 values: the sums 285 us (7.0 TB/s), the scaling
 // 620 us (4.0 GB read and written, 6.5 TB/s), 905 us in all; the second read is what the
 // definition costs beyond a read and a write (590 us), as the factor is known last.  85 million
-// of mixed types 94 us, the end of the first pass still in L2 for the second, which goes
-// backwards.  100,000 values in six tensors 8.9 us: two launches.
+// of mixed types 94 us: the second pass goes backwards, but finds little of the first in L2 (it
+// reads 156 of its 170 MB from DRAM).  100,000 values in six tensors 8.3 us: two launches.
 #include "widen.cuh"
 
 namespace tfg {
@@ -179,7 +179,7 @@ write_norm(const double *__restrict__ partial, int n, float *__restrict__ norm) 
 
 // ---- scaling ----------------------------------------------------------------------
 // Plain loads: out may be the tensor itself, and then what is read is written here.
-// Stores that leave L2 first: what the pass has yet to read stays.
+// Stores that leave L2 first, so that what the pass has yet to read may stay.
 template <int VEC>
 __device__ __forceinline__ void store_stream(float *p, const float (&v)[VEC]) {
     if constexpr (VEC == 4) __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
@@ -261,7 +261,7 @@ scale_by_norm(const __grid_constant__ TensorList<CAP> list, const double *__rest
     const Factor factor = s_factor;
     const int64_t chunks = list.first[list.count];
     for (int64_t back = blockIdx.x; back < chunks; back += gridDim.x) {
-        const int64_t c = chunks - 1 - back;      // the last chunks first: L2 still holds them
+        const int64_t c = chunks - 1 - back;      // the last chunks first: what L2 still holds
         const int t = tensor_of(list, c, 0);
         if (factor.lift * factor.f == 1.f && list.in[t] == list.out[t]) continue;      // in place and nothing to do
         const int64_t at = (c - list.first[t]) * kChunk;

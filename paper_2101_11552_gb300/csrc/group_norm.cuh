@@ -12,14 +12,15 @@
 // them in flight at once, no registers, no barrier), and the passes over them -- the sums,
 // and the application of the statistics -- read them from there, so that x comes from
 // memory once.  Held in registers, or read again from L2, there were too few bytes in
-// flight (1,024 graphs of 110 rows, F = 128 fp32, forward: 82 and 27 us).
+// flight (1,024 graphs of 110 rows, F = 128 fp32, forward: 82 and 27 us against 26 at that time).
 //
 // A graph of more rows than a team has room for ("large") is cut along a grid of row
 // shares over all rows: teams of the first kernel write partial statistics of its pieces,
-// and a second kernel joins them in a fixed order and applies them, last share first,
-// whose rows L2 still holds.  A share has no more rows than a team has room for, so it
-// meets at most two large graphs: one that covers its first row (slot 0) and one that
-// begins behind it and runs past its end (slot 1).  Whether there are large graphs only
+// and a second kernel joins them in a fixed order and applies them, last share first, as L2
+// still holds rows of those (41 communities: of 60 MB forward it reads 17.5 from DRAM again, of
+// 119 backward 67).  A share has no more rows than a team has room for, so it meets at most
+// two large graphs: one that covers its first row (slot 0) and one that begins behind it
+// and runs past its end (slot 1).  Whether there are large graphs only
 // the device knows; the host leaves the second kernel out where all rows fit a team, and
 // elsewhere it ends after one look at the slots.
 #pragma once
@@ -228,8 +229,9 @@ __device__ __forceinline__ Piece find_piece(const NormArgs &a, int64_t s, int sl
 // TT threads: a warp in a CTA of four, each with shared memory of its own, or a whole CTA.
 constexpr int kWarpTeams = 4;
 // Resident threads asked for: 64 registers a thread forward, 80 backward (64 in teams of
-// 1,024).  Forward 1,024 against 768: 4,096 single rows 17 / 20 us; backward 768 against 512
-// and 1,024: 41 communities, both directions, 135 / 145 / 138 us.
+// 1,024).  Forward 1,024 against 768: 4,096 single rows 17 / 19 us; backward 768 against 512
+// and 1,024: 41 communities, both directions, 134 / 139 / 134 us, 900 graphs of 111 rows, F = 75
+// fp32, 101 / 108 / 100, 20,000 of 3 rows 124 / 128 / 125 (1,024 graphs of 110 rows 84 / 81 / 85).
 constexpr int kNormResident = 1024, kBackResident = 768;
 constexpr int team_ctas(int team, int threads) { return team == 1024 ? 1 : threads / (team == 256 ? 256 : 128); }
 template <int TT>
@@ -446,6 +448,11 @@ __device__ __forceinline__ bool no_piece(const NormArgs &p, int64_t share) {
 // 16 bytes of every line: 112,640 rows, one graph of 101,000 and 1,024 small ones, F = 128 fp32 in
 // 32 groups, forward 129 us against 57.)
 template <int TT>
+__device__ __forceinline__ float *join_buffer() {            // for two sums: with kNormRoom, four CTAs of 256 a multiprocessor
+    __shared__ float s_sum[2 * TT];
+    return s_sum;
+}
+template <int TT>
 struct JoinPlace {
     int log_groups, k, lane, lanes;
     __device__ __forceinline__ explicit JoinPlace(int groups) {
@@ -463,15 +470,16 @@ struct JoinPlace {
         for (int i = 0; i < N; ++i)
             for (int o = 1 << log_groups; o < 32; o <<= 1) v[i] += lane_xor(v[i], o);
         if constexpr (TT > 32) {
-            __shared__ float s_sum[N][TT];
+            static_assert(N <= 2, "the buffer's sums");
+            float *s_sum = join_buffer<TT>();
             const int wide = max(32, 1 << log_groups);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s_sum[i][threadIdx.x] = v[i];
+            for (int i = 0; i < N; ++i) s_sum[i * TT + threadIdx.x] = v[i];
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = 0.f;
-                for (int t = k; t < TT; t += wide) v[i] += s_sum[i][t];
+                for (int t = k; t < TT; t += wide) v[i] += s_sum[i * TT + t];
             }
             __syncthreads();
         }
@@ -547,8 +555,8 @@ __device__ __forceinline__ void joined_statistics(const NormArgs &p, const At &a
 
 // join_apart: a CTA takes a range of shares and kJoinGroups groups and finds the shares in which
 // large graphs begin (one at most in each: such a graph has more rows than a share).  Its warps
-// join those of few pieces, a graph each, and then all of them together the long ones.  One
-// wave of CTAs whatever the number of shares.
+// join those of few pieces, a graph each, and then all of them together the long ones.  Four
+// CTAs a multiprocessor whatever the number of shares.
 constexpr int kJoinThreads = 512, kJoinCtas = 608;
 struct JoinRange {
     int64_t per_cta;      // shares
@@ -622,19 +630,20 @@ int norm_vec(int64_t f, int64_t c, int widest, bool aligned) {
     return widest >= 4 && aligned && f % 4 == 0 && c / gcd64(c, 4) <= 256 ? 4 : 1;
 }
 
-// Vectors of a mean graph to a thread: 16 against 8 and 32, 1,024 graphs of 110 rows 84 / 88 /
-// 140 us, 300 ragged ones of odd width 65 / 77 / 65 us (both directions).
-// Single values (odd widths): 32 to a thread, as the fixed work of a team counts for more; 900
-// graphs of 111 rows, F = 75 fp32: 98 / 110 us, 21 of 83 rows, F = 58: 22.6 / 21.3.
+// Vectors of a mean graph to a thread: 16 against 8 and 32, 1,024 graphs of 110 rows 84 / 86 /
+// 126 us (both directions).
+// Single values (odd widths): 32 to a thread against 16, as the fixed work of a team counts for
+// more; 900 graphs of 111 rows, F = 75 fp32: 101 / 108 us, 21 of 83 rows, F = 58: 21.7 / 20.0.
 constexpr int kVectorsAThread = 16, kValuesAThread = 32;
 // Shares of all rows, of every tile: two for each CTA of 256 threads that is resident.  1,216
-// against 608 and 2,432: 41 communities 135 / 137 / 150 us.
+// against 608 and 2,432: 41 communities 134 / 134 / 142 us, 1,024 graphs of 110 rows 84 / 83 / 91.
 constexpr int64_t kShareTeams = 1216;
 // Shared memory of a CTA: four on a multiprocessor.  55 KB against 40 and 74: 1,024 graphs
-// of 110 rows 84 / 141 / 95 us (40 KB have no room for the larger ones).
+// of 110 rows 84 / 145 / 92 us (40 KB have no room for the larger ones), 41 communities 134 / 150 /
+// 131; 74 KB hold all 900 graphs of 111 rows of an odd width: 101 / 110 / 80.
 constexpr int kNormRoom = 55 * 1024;
 // Bytes a thread that kNormResident threads leave unused.  20,000 graphs of 3 rows on average, F =
-// 35 fp32, both directions: 122 us against 231 with room for 8 rows, 4,096 single rows 16.5 / 17.8.
+// 35 fp32, both directions: 124 us against 196 with room for 8 rows, 4,096 single rows 17.1 / 17.9.
 constexpr int kFreeShared = 216, kFewRows = 64;
 constexpr int kNormSharedMost = 96 * 1024;        // allowed to every launch: room, a row's rounding, statistics
 

@@ -12,9 +12,9 @@
 //
 // What bounds it: as the forward, with the slope of the activation taken twice (in the sums
 // and in grad_x: keeping it would halve the rows a team holds).  1,024 graphs of 110 rows, F =
-// 128 fp32, SiLU: 51 us (173 MB, 3.4 TB/s; first kernel 41, channels' sums 8).  41 graphs of
-// 232,965 rows, F = 128 bf16: 88 us (179 MB, 2.0 TB/s: 40, join 8, 40 for the second read).  300
-// ragged graphs of 19,717 rows, F = 123 fp32, GELU: 35 us.
+// 128 fp32, SiLU: 50 us (173 MB, 3.5 TB/s; first kernel 41, channels' sums 8).  41 graphs of
+// 232,965 rows, F = 128 bf16: 87 us (179 MB, 2.1 TB/s: 40, the join, 40 for the second read).  300
+// ragged graphs of 19,717 rows, F = 123 fp32, GELU: 31 us.
 #pragma once
 
 #include "group_norm.cuh"

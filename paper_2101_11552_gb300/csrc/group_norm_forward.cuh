@@ -6,22 +6,21 @@
 //
 // The mean first, then the squares about it.  A sum of n values far from zero is off by a few
 // u |m| and so is its mean, as its rounding to fp32 alone is, which h = (x - m) r would take for
-// deviations: 1,000 everywhere in three rows came out as h = 0.02, and a spread of 0.01 about
-// 1,000 was off by 5e-3.  So the deviations d from the mean as first found are summed too,
+// deviations: 1,000 everywhere in five rows of three channels is then h = 0.019, and with a
+// spread of 0.01 about 1,000 the h of 800 values are off by up to 0.01.  So the deviations d from the mean as first found are summed too,
 // m = that mean + rest with rest = sum d / M, and what is left is a few u of the deviations.  Shares
 // of a large graph are joined by the pooled-variance identity, squares about the joint mean =
-// squares of the parts + n (mean of the part - joint mean)^2, in the same two steps.  It costs 1
-// to 5 % of both directions (82.3 -> 85.1 us for 1,024 graphs of 110 rows, 133.4 -> 137 for 41
-// graphs of 232,965, 59 -> 62 for 300 ragged ones).
+// squares of the parts + n (mean of the part - joint mean)^2, in the same two steps.  It costs 2
+// instructions a value, 1 to 5 % of both directions (1,024 graphs of 110 rows 82.3 -> 85.1 us).
 //
 // What bounds it: issue slots and latency together, below memory.  1,024 graphs of 110 rows,
-// F = 128 fp32, SiLU: 34 us (115 MB, 3.4 TB/s; 28 instructions a value, issue slots 45 % busy
+// F = 128 fp32, SiLU: 34 us (115 MB, 3.4 TB/s; 30 instructions a value, issue slots 47 % busy
 // with 23 % of the warps that a multiprocessor can hold, as room for the largest graph is
 // kept for each; and 4 us for a second kernel that finds no large graph).  Half as wide
-// tiles, twice the warps: 34.5 us.  41 graphs of 232,965 rows, F = 128 bf16: 46 us (119 MB, 2.6
-// TB/s: first pass 21, join 6, second read of x 20).  300 ragged graphs of 19,717 rows, F = 123
-// fp32 (4-byte loads, GELU): 27 us.  4,096 single rows of 1,024 bf16 in 32 groups: 17 us.  2,708
-// rows in one graph, F = 64: 10 us, two launches.
+// tiles, twice the warps: 34.5 us.  41 graphs of 232,965 rows, F = 128 bf16: 48 us (119 MB, 2.5
+// TB/s: first pass 21, second read of x 20, the join between them).  300 ragged graphs of
+// 19,717 rows, F = 123 fp32 (4-byte loads, GELU): 26 us.  4,096 single rows of 1,024 bf16 in 32
+// groups: 17 us.  2,708 rows in one graph, F = 64: 10 us, two launches.
 #pragma once
 
 #include "group_norm.cuh"

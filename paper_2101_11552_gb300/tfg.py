@@ -870,7 +870,8 @@ def tfg_group_norm(x, node_offsets, num_groups: int, gamma=None, beta=None, eps:
                    workspace=None) -> GroupNorm:
     """Group norm over the graphs of a batch and an activation ("none", "relu", "silu",
     "gelu").  Graph g holds the rows node_offsets[g] .. node_offsets[g + 1] - 1 of x
-    [N, F]; rows outside all graphs are left as they are in ``out`` (unset in a new one)."""
+    [N, F]; rows outside all graphs are left as they are in ``out`` (unset in a new one: give
+    a padded batch whose rows are all read later an ``out`` of zeros)."""
     index, n, f, g, code = _norm_inputs(x, node_offsets, gamma, beta, activation)
     if out_dtype is None:
         out_dtype = x.dtype if out is None else out.dtype
@@ -895,7 +896,8 @@ def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean,
                             want_weight_grads: bool = True, grad_x=None, workspace=None):
     """Gradients of tfg_group_norm with the forward's arguments and statistics.  Returns
     (grad_x [N, F] in grad_out's type, grad_gamma [F], grad_beta [F]); the last two None
-    without ``want_weight_grads``."""
+    without ``want_weight_grads``.  Rows outside all graphs are left as they are in
+    ``grad_x`` (unset in a new one)."""
     index, n, f, g, code = _norm_inputs(x, node_offsets, gamma, beta, activation)
     _same("grad_out", grad_out, index)
     if grad_out.shape != (n, f):
