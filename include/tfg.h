@@ -74,6 +74,10 @@ typedef enum { TFG_SUM = 0, TFG_MEAN = 1, TFG_MAX = 2 } tfg_reduce;
  * y (1 + erf(y / sqrt 2)) / 2. */
 typedef enum { TFG_ACT_NONE = 0, TFG_ACT_RELU = 1, TFG_ACT_SILU = 2, TFG_ACT_GELU = 3 } tfg_activation;
 
+/* Gates of tfg_gated_recurrence: a = 1 / (1 + exp(-z)) with the input (1 - a) x,
+ * a = exp(z) with the input x. */
+typedef enum { TFG_GATE_SIGMOID = 0, TFG_GATE_EXP = 1 } tfg_gate;
+
 /* Library version (major * 10000 + minor * 100 + patch). */
 int tfg_version(void);
 
@@ -685,6 +689,183 @@ int tfg_global_norm(int64_t num_tensors, const void *const *tensors, const int64
 int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, const int64_t *sizes,
                             const int *dtypes, float clip_norm, void *const *outs, float *norm,
                             void *workspace, size_t workspace_bytes, tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm of rows, with the addition of the residual stream in the same pass:
+ * before and behind the aggregations and attention layers of a deep model.
+ *   s = x + residual (rounded to the stream's type), or x without a residual
+ *   m = mean of the row's values of s, v = mean of (s - m)^2, r = (v + eps)^(-1/2)
+ *   out = gamma (s - m) r + beta
+ *
+ *   x (device) [num_rows, num_features] row-major, TFG_F32 or TFG_BF16.
+ *   residual (device) [num_rows, num_features] of sum_dtype, or NULL.
+ *   sum (device) [num_rows, num_features] of sum_dtype: s, written; may be
+ *        residual (the stream updated in place).  Without a residual sum must be
+ *        NULL and sum_dtype is not looked at.
+ *   gamma, beta (device) fp32 [num_features], or NULL for 1 and 0.
+ *   eps: finite, > 0.
+ *   out (device) [num_rows, num_features], out_dtype; must not overlap an
+ *        input or sum.
+ *   mean, rstd (device) fp32 [num_rows]: m and r, written for the backward;
+ *        both or neither may be NULL.
+ * An offset common to a row's values costs nothing: deviations are taken from
+ * the mean before its rounding to fp32.
+ *
+ * tfg_layer_norm_backward: with g = dL/dout, h = (s - m) r, d = gamma g:
+ *   grad_s = r (d - mean d - h mean(d h)) + grad_sum
+ *   grad_gamma = sum over rows of g h, grad_beta = sum of g
+ *   sum: the forward's s (x without a residual), of sum_dtype; mean, rstd: the
+ *        forward's.
+ *   grad_out (device) [num_rows, num_features] of grad_dtype.
+ *   grad_sum (device) [num_rows, num_features] of grad_sum_dtype, or NULL: the
+ *        gradient that reaches s by other ways (the stream's own).
+ *   grad_s (device) [num_rows, num_features] of grad_sum_dtype, the gradient of
+ *        x and of the residual alike; may be grad_sum, must not overlap
+ *        another input.
+ *   grad_gamma, grad_beta (device) fp32 [num_features], written (0 without
+ *        rows); both or neither may be NULL.
+ *   workspace (device) >= tfg_layer_norm_backward_workspace_size() bytes,
+ *        16-byte aligned; not used, and may be NULL, without grad_gamma.
+ * Rows of NaN or infinities give NaN in their own row, and in grad_gamma and
+ * grad_beta.  Sums in fp32 in a fixed order: bitwise reproducible between calls
+ * of the same alignment.
+ * ---------------------------------------------------------------------- */
+int tfg_layer_norm(const void *x, int x_dtype, const void *residual, int sum_dtype, void *sum,
+                   int64_t num_rows, int64_t num_features, const float *gamma, const float *beta,
+                   float eps, void *out, int out_dtype, float *mean, float *rstd,
+                   tfg_stream_t stream);
+int tfg_layer_norm_backward_workspace_size(int64_t num_rows, int64_t num_features, size_t *bytes);
+int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, int64_t num_features,
+                            const float *gamma, const float *mean, const float *rstd,
+                            const void *grad_out, int grad_dtype, const void *grad_sum,
+                            void *grad_s, int grad_sum_dtype, float *grad_gamma, float *grad_beta,
+                            void *workspace, size_t workspace_bytes, tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Gated linear recurrence along the rows of each sequence of a batch: the
+ * events of a node, the nodes of a graph in order, the tokens of a text, packed
+ * one sequence after the other as tfg_batch_graphs packs the nodes of graphs.
+ * Channel by channel, with v before a sequence's first row its initial state:
+ *   v_t = a_t v_{t-1} + b_t,  out_t = v_t
+ *   TFG_GATE_SIGMOID: a = 1 / (1 + exp(-z)), b = (1 - a) x
+ *   TFG_GATE_EXP:     a = exp(z),            b = x
+ *
+ *   gate (z), x (device) [num_rows, num_features], both of dtype; row r
+ *        begins at r * gate_stride and r * x_stride values (at least
+ *        num_features: the halves of one projection need no copy).
+ *   node_offsets (device) int64 [num_sequences + 1], non-decreasing, in
+ *        [0, num_rows]: sequence s holds rows node_offsets[s] ..
+ *        node_offsets[s + 1] - 1.  Rows before the first and from the last
+ *        offset on are left as they were in every output.
+ *   initial (device) fp32 [num_sequences, num_features], or NULL for zeros.
+ *   out (device) [num_rows, num_features], out_dtype.
+ *   final_state (device) fp32 [num_sequences, num_features] or NULL: v behind
+ *        each sequence's last row; the initial state of an empty one.  A
+ *        sequence is continued by a call with it as initial (of one row for a
+ *        single step).
+ *   entering (device) fp32 [ceil(num_rows / TFG_RECURRENCE_TILE_ROWS),
+ *        num_features] or NULL: states that the backward starts from.
+ *   workspace (device) >= tfg_gated_recurrence_workspace_size() bytes, 16-byte
+ *        aligned; 0 bytes up to TFG_RECURRENCE_TILE_ROWS rows.
+ *   status (device) int32 [1]: 0, TFG_ERR_INDEX_RANGE when an offset lies
+ *        outside [0, num_rows] or the offsets decrease, or TFG_ERR_TIMEOUT when
+ *        a tile of rows waited in vain for the one before (the outputs are then
+ *        unspecified).
+ * Outputs overlap no input and no other output.
+ *
+ * tfg_gated_recurrence_backward: with g = dL/dout and l_t = g_t + a_{t+1} l_{t+1}
+ * (behind a sequence's last row: dL/dfinal_state):
+ *   TFG_GATE_SIGMOID: grad_gate = l (v_{t-1} - x) a (1 - a), grad_x = l (1 - a)
+ *   TFG_GATE_EXP:     grad_gate = l v_{t-1} a,               grad_x = l
+ *   grad_initial = a l of the sequence's first row
+ *   gate, x, node_offsets, initial, entering: the forward's.
+ *   grad_out (device) [num_rows, num_features] of grad_dtype, or NULL (zeros: a
+ *        loss of the final states alone); grad_final (device) fp32
+ *        [num_sequences, num_features], or NULL (zeros).
+ *   grad_gate, grad_x (device) of dtype, with row strides as the inputs'.
+ *   grad_initial (device) fp32 [num_sequences, num_features] or NULL.
+ * The states are formed again in fp32 as the forward had them: the type of out
+ * does not touch the gradients.
+ * All arithmetic in fp32 in a fixed order: bitwise reproducible between calls of
+ * the same alignment.  A gate of -inf forgets a finite state entirely.  A value that is no
+ * number stays in its channel and sequence.  ceil(num_rows / 128) *
+ * ceil(num_features / 32) < 2^31 - 2^16 (TFG_ERR_TOO_LARGE).
+ * ---------------------------------------------------------------------- */
+#define TFG_RECURRENCE_TILE_ROWS 128
+
+int tfg_gated_recurrence_workspace_size(int64_t num_rows, int64_t num_features, size_t *bytes);
+int tfg_gated_recurrence(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride,
+                         int dtype, const int64_t *node_offsets, int64_t num_rows,
+                         int64_t num_sequences, int64_t num_features, int gate_kind,
+                         const float *initial, void *out, int out_dtype, float *final_state,
+                         float *entering, void *workspace, size_t workspace_bytes, int32_t *status,
+                         tfg_stream_t stream);
+int tfg_gated_recurrence_backward(const void *gate, int64_t gate_stride, const void *x,
+                                  int64_t x_stride, int dtype, const int64_t *node_offsets,
+                                  int64_t num_rows, int64_t num_sequences, int64_t num_features,
+                                  int gate_kind, const float *initial, const float *entering,
+                                  const void *grad_out, int grad_dtype, const float *grad_final,
+                                  void *grad_gate, int64_t grad_gate_stride, void *grad_x,
+                                  int64_t grad_x_stride, float *grad_initial, void *workspace,
+                                  size_t workspace_bytes, int32_t *status, tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Distillation from a teacher's top logits: the loss that ends a training step
+ * of a small model on the classes (or the vocabulary) of a large one, of which
+ * only the K largest logits of every row were kept.  With the temperature T:
+ *   p = softmax over the row's entries of teacher / T (those that are no padding)
+ *   q = softmax over all classes of logits / T
+ *   loss = w T^2 sum_k p_k (log p_k - log q_{id_k}),  dloss/dlogits = w T (q - p)
+ *
+ *   logits (device) [num_rows, num_classes] row-major, TFG_F32 or TFG_BF16.
+ *   ids (device) int64 [num_rows, top_k], or int32 for the calls that end in
+ *        32: the classes of the teacher's logits, in any order.  A class
+ *        listed more than once counts with each of its entries.  padding_id: as
+ *        in tfg_embedding_lookup; such entries count for nothing.
+ *   teacher (device) [num_rows, top_k], TFG_F32 or TFG_BF16.  An entry of -inf
+ *        has p = 0.
+ *   temperature: from 1e-6 to 1e6.
+ *   row_weight (device) fp32 [num_rows] (w), or NULL for 1.  A row whose weight
+ *        is 0, or that has no teacher entry above -inf, has a loss of 0 and a gradient
+ *        of zeros whatever its logits hold; they are not read.
+ *   loss (device) fp32 [num_rows].
+ *   stats (device) fp32 [num_rows, 2] or NULL: for the backward, m = the
+ *        largest logit and the sum of exp((logits - m) / T); (0, 1) in rows that are
+ *        not read.
+ *   grad_logits (device) [num_rows, num_classes] of the logits' type, or NULL:
+ *        dloss/dlogits, in the same pass.
+ *   status (device) int32 [1]: 0, or TFG_ERR_INDEX_RANGE when an id lies outside
+ *        [0, num_classes) and is not padding_id (treated as padding).
+ *
+ * tfg_distillation_loss_backward: grad_logits = grad_loss dloss/dlogits for
+ *   grad_loss (device) fp32 [num_rows], from the forward's arguments and stats.
+ *   (Ids outside the range are not reported a second time.)
+ * Logits of -inf are classes without probability (an infinite loss where p > 0);
+ * a row without another, with +inf or with NaN gives NaN in that row alone.
+ * top_k <= 1,024 (TFG_ERR_TOO_LARGE).  grad_logits overlaps no input.  Sums in
+ * fp32 in a fixed order: bitwise reproducible between calls of the same alignment.
+ * ---------------------------------------------------------------------- */
+int tfg_distillation_loss(const void *logits, int dtype, int64_t num_rows, int64_t num_classes,
+                          const int64_t *ids, const void *teacher, int teacher_dtype,
+                          int64_t top_k, int64_t padding_id, float temperature,
+                          const float *row_weight, float *loss, float *stats, void *grad_logits,
+                          int32_t *status, tfg_stream_t stream);
+int tfg_distillation_loss32(const void *logits, int dtype, int64_t num_rows, int64_t num_classes,
+                            const int32_t *ids, const void *teacher, int teacher_dtype,
+                            int64_t top_k, int64_t padding_id, float temperature,
+                            const float *row_weight, float *loss, float *stats, void *grad_logits,
+                            int32_t *status, tfg_stream_t stream);
+int tfg_distillation_loss_backward(const void *logits, int dtype, int64_t num_rows,
+                                   int64_t num_classes, const int64_t *ids, const void *teacher,
+                                   int teacher_dtype, int64_t top_k, int64_t padding_id,
+                                   float temperature, const float *row_weight, const float *stats,
+                                   const float *grad_loss, void *grad_logits, tfg_stream_t stream);
+int tfg_distillation_loss_backward32(const void *logits, int dtype, int64_t num_rows,
+                                     int64_t num_classes, const int32_t *ids, const void *teacher,
+                                     int teacher_dtype, int64_t top_k, int64_t padding_id,
+                                     float temperature, const float *row_weight,
+                                     const float *stats, const float *grad_loss, void *grad_logits,
+                                     tfg_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Gather-only floor (a measurement call; the paper has no counterpart).

@@ -1258,6 +1258,414 @@ int tfg_group_norm_backward(const void *x, int x_dtype, const int64_t *node_offs
                        fn);
 }
 
+// ---- layer norm of rows ---------------------------------------------------------------
+namespace {
+int check_rows(const char *fn, int64_t num_rows, int64_t num_features) {
+    TFG_TRY(check_counts(fn, num_rows, 0));
+    return check_features(fn, num_rows, num_features);
+}
+int check_eps(const char *fn, float eps) {
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(TFG_ERR_INVALID_ARG, "%s: eps must be finite and positive", fn);
+    return TFG_OK;
+}
+int no_overlap(const char *fn, const char *out_name, const void *out, size_t out_bytes, const char *name, const void *p,
+               size_t bytes) {
+    if (p != nullptr && out != nullptr && overlap(out, out_bytes, p, bytes))
+        return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, out_name, name);
+    return TFG_OK;
+}
+}  // namespace
+
+int tfg_layer_norm(const void *x, int x_dtype, const void *residual, int sum_dtype, void *sum, int64_t num_rows,
+                   int64_t num_features, const float *gamma, const float *beta, float eps, void *out, int out_dtype,
+                   float *mean, float *rstd, tfg_stream_t stream) {
+    const char *fn = "tfg_layer_norm";
+    TFG_RANGE(fn);
+    TFG_TRY(check_rows(fn, num_rows, num_features));
+    TFG_TRY(check_dtype(fn, x_dtype));
+    TFG_TRY(check_dtype(fn, out_dtype));
+    if (residual) TFG_TRY(check_dtype(fn, sum_dtype));
+    TFG_TRY(check_eps(fn, eps));
+    TFG_NEED(x, num_rows > 0, fn, "x");
+    TFG_NEED(out, num_rows > 0, fn, "out");
+    if (num_rows > 0 && (residual == nullptr) != (sum == nullptr))
+        return fail(TFG_ERR_INVALID_ARG, "%s: residual and sum are given both or neither", fn);
+    if ((mean == nullptr) != (rstd == nullptr))
+        return fail(TFG_ERR_INVALID_ARG, "%s: mean and rstd are wanted both or neither", fn);
+    const size_t values = size_t(num_rows * num_features);
+    const size_t x_bytes = elem_bytes(x_dtype) * values, out_bytes = elem_bytes(out_dtype) * values;
+    const size_t sum_bytes = residual ? elem_bytes(sum_dtype) * values : 0, w_bytes = sizeof(float) * size_t(num_features);
+    TFG_TRY(check_element(fn, "x", x, x_dtype));
+    TFG_TRY(check_element(fn, "out", out, out_dtype));
+    if (residual) {
+        TFG_TRY(check_element(fn, "residual", residual, sum_dtype));
+        TFG_TRY(check_element(fn, "sum", sum, sum_dtype));
+        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "x", x, x_bytes));
+        if (sum != residual) TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "residual", residual, sum_bytes));
+        TFG_TRY(no_overlap(fn, "out", out, out_bytes, "residual", residual, sum_bytes));
+        TFG_TRY(no_overlap(fn, "out", out, out_bytes, "sum", sum, sum_bytes));
+        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "gamma", gamma, w_bytes));
+        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "beta", beta, w_bytes));
+    }
+    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "x", x, x_bytes));
+    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "gamma", gamma, w_bytes));
+    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "beta", beta, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "x", x, x_bytes));
+    TFG_DEBUG(debug_extent(fn, "residual", residual, sum_bytes));
+    TFG_DEBUG(debug_extent(fn, "sum", sum, sum_bytes));
+    TFG_DEBUG(debug_extent(fn, "out", out, out_bytes));
+    TFG_DEBUG(debug_extent(fn, "gamma", gamma, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "beta", beta, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "mean", mean, sizeof(float) * size_t(num_rows)));
+    TFG_DEBUG(debug_extent(fn, "rstd", rstd, sizeof(float) * size_t(num_rows)));
+    return cuda_result(tfg::launch_layer_norm(x, x_dtype, residual, sum_dtype, sum, num_rows, num_features, gamma, beta, eps,
+                                              out, out_dtype, mean, rstd, reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int tfg_layer_norm_backward_workspace_size(int64_t num_rows, int64_t num_features, size_t *bytes) {
+    const char *fn = "tfg_layer_norm_backward_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_rows(fn, num_rows, num_features));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::layer_norm_backward_workspace_bytes(num_rows, num_features);
+    return ok();
+}
+
+int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, int64_t num_features, const float *gamma,
+                            const float *mean, const float *rstd, const void *grad_out, int grad_dtype, const void *grad_sum,
+                            void *grad_s, int grad_sum_dtype, float *grad_gamma, float *grad_beta, void *workspace,
+                            size_t workspace_bytes, tfg_stream_t stream) {
+    const char *fn = "tfg_layer_norm_backward";
+    TFG_RANGE(fn);
+    TFG_TRY(check_rows(fn, num_rows, num_features));
+    TFG_TRY(check_dtype(fn, sum_dtype));
+    TFG_TRY(check_dtype(fn, grad_dtype));
+    TFG_TRY(check_dtype(fn, grad_sum_dtype));
+    TFG_NEED(sum, num_rows > 0, fn, "sum");
+    TFG_NEED(mean, num_rows > 0, fn, "mean");
+    TFG_NEED(rstd, num_rows > 0, fn, "rstd");
+    TFG_NEED(grad_out, num_rows > 0, fn, "grad_out");
+    TFG_NEED(grad_s, num_rows > 0, fn, "grad_s");
+    if ((grad_gamma == nullptr) != (grad_beta == nullptr))
+        return fail(TFG_ERR_INVALID_ARG, "%s: grad_gamma and grad_beta are wanted both or neither", fn);
+    const size_t values = size_t(num_rows * num_features);
+    const size_t s_bytes = elem_bytes(sum_dtype) * values, g_bytes = elem_bytes(grad_dtype) * values;
+    const size_t gs_bytes = elem_bytes(grad_sum_dtype) * values, w_bytes = sizeof(float) * size_t(num_features);
+    TFG_TRY(check_element(fn, "sum", sum, sum_dtype));
+    TFG_TRY(check_element(fn, "grad_out", grad_out, grad_dtype));
+    TFG_TRY(check_element(fn, "grad_sum", grad_sum, grad_sum_dtype));
+    TFG_TRY(check_element(fn, "grad_s", grad_s, grad_sum_dtype));
+    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "sum", sum, s_bytes));
+    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "grad_out", grad_out, g_bytes));
+    if (grad_s != grad_sum) TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "grad_sum", grad_sum, gs_bytes));
+    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "gamma", gamma, w_bytes));
+    const size_t need = grad_gamma ? tfg::layer_norm_backward_workspace_bytes(num_rows, num_features) : 0;
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
+    TFG_DEBUG(debug_extent(fn, "sum", sum, s_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_out", grad_out, g_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_sum", grad_sum, gs_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_s", grad_s, gs_bytes));
+    TFG_DEBUG(debug_extent(fn, "gamma", gamma, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "mean", mean, sizeof(float) * size_t(num_rows)));
+    TFG_DEBUG(debug_extent(fn, "rstd", rstd, sizeof(float) * size_t(num_rows)));
+    TFG_DEBUG(debug_extent(fn, "grad_gamma", grad_gamma, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "grad_beta", grad_beta, w_bytes));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
+    return cuda_result(tfg::launch_layer_norm_backward(sum, sum_dtype, num_rows, num_features, gamma, mean, rstd, grad_out,
+                                                       grad_dtype, grad_sum, grad_s, grad_sum_dtype, grad_gamma, grad_beta,
+                                                       workspace, reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+// ---- gated linear recurrence ----------------------------------------------------------
+namespace {
+constexpr int64_t kMaxTiles = (int64_t(1) << 31) - (int64_t(1) << 16);
+
+// An array of rows that may begin further apart than they are long.
+struct Rows {
+    const char *name;
+    const void *p;
+    size_t stride, width, extent;        // bytes; extent: from the first byte to the last
+    Rows(const char *nm, const void *ptr, int64_t n, int64_t ld, int64_t f, size_t elem)
+        : name(nm), p(ptr), stride(size_t(ld) * elem), width(size_t(f) * elem),
+          extent(n > 0 ? size_t(n - 1) * size_t(ld) * elem + size_t(f) * elem : 0) {}
+};
+
+// Whether rows of a and b share a byte; columns side by side in rows of one buffer do not.
+bool rows_overlap(const Rows &a, const Rows &b) {
+    if (a.p == nullptr || b.p == nullptr || !overlap(a.p, a.extent, b.p, b.extent)) return false;
+    if (a.stride != b.stride) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const Rows &low = pa <= pb ? a : b, &high = pa <= pb ? b : a;
+    const size_t off = (pa <= pb ? pb - pa : pa - pb) % a.stride;
+    return !(off >= low.width && off + high.width <= a.stride);
+}
+
+int check_recurrence(const char *fn, int64_t num_rows, int64_t num_sequences, int64_t num_features) {
+    TFG_TRY(check_counts(fn, num_rows, 0));
+    if (num_sequences < 0) return fail(TFG_ERR_INVALID_ARG, "%s: negative sequence count", fn);
+    if (num_sequences >= kIndexLimit - 1) return fail(TFG_ERR_TOO_LARGE, "%s: too many sequences", fn);
+    TFG_TRY(check_features(fn, num_rows > num_sequences ? num_rows : num_sequences, num_features));
+    if (((num_rows + TFG_RECURRENCE_TILE_ROWS - 1) / TFG_RECURRENCE_TILE_ROWS) * ((num_features + 31) / 32) >= kMaxTiles)
+        return fail(TFG_ERR_TOO_LARGE, "%s: num_rows * num_features too large", fn);
+    return TFG_OK;
+}
+
+int check_gate(const char *fn, int gate_kind) {
+    if (gate_kind != TFG_GATE_SIGMOID && gate_kind != TFG_GATE_EXP)
+        return fail(TFG_ERR_INVALID_ARG, "%s: unknown gate %d", fn, gate_kind);
+    return TFG_OK;
+}
+
+int check_stride(const char *fn, const char *name, int64_t num_rows, int64_t stride, int64_t num_features) {
+    if (stride < num_features)
+        return fail(TFG_ERR_INVALID_ARG, "%s: %s (%lld) must be at least num_features (%lld)", fn, name, (long long)stride,
+                    (long long)num_features);
+    if (num_rows > 0 && stride >= (int64_t(1) << 46) / num_rows)
+        return fail(TFG_ERR_TOO_LARGE, "%s: %s too large", fn, name);
+    return TFG_OK;
+}
+
+// Every output against every input and every later output.
+int check_apart(const char *fn, const Rows *outs, int num_outs, const Rows *ins, int num_ins) {
+    for (int i = 0; i < num_outs; ++i) {
+        for (int j = 0; j < num_ins; ++j)
+            if (rows_overlap(outs[i], ins[j]))
+                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, ins[j].name);
+        for (int j = i + 1; j < num_outs; ++j)
+            if (rows_overlap(outs[i], outs[j]))
+                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, outs[j].name);
+    }
+    return TFG_OK;
+}
+}  // namespace
+
+int tfg_gated_recurrence_workspace_size(int64_t num_rows, int64_t num_features, size_t *bytes) {
+    const char *fn = "tfg_gated_recurrence_workspace_size";
+    TFG_RANGE(fn);
+    TFG_TRY(check_recurrence(fn, num_rows, 0, num_features));
+    TFG_NEED(bytes, true, fn, "bytes");
+    *bytes = tfg::gated_recurrence_workspace_bytes(num_rows, num_features);
+    return ok();
+}
+
+int tfg_gated_recurrence(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int dtype,
+                         const int64_t *node_offsets, int64_t num_rows, int64_t num_sequences, int64_t num_features,
+                         int gate_kind, const float *initial, void *out, int out_dtype, float *final_state, float *entering,
+                         void *workspace, size_t workspace_bytes, int32_t *status, tfg_stream_t stream) {
+    const char *fn = "tfg_gated_recurrence";
+    TFG_RANGE(fn);
+    TFG_TRY(check_recurrence(fn, num_rows, num_sequences, num_features));
+    TFG_TRY(check_dtype(fn, dtype));
+    TFG_TRY(check_dtype(fn, out_dtype));
+    TFG_TRY(check_gate(fn, gate_kind));
+    TFG_TRY(check_stride(fn, "gate_stride", num_rows, gate_stride, num_features));
+    TFG_TRY(check_stride(fn, "x_stride", num_rows, x_stride, num_features));
+    TFG_NEED(gate, num_rows > 0, fn, "gate");
+    TFG_NEED(x, num_rows > 0, fn, "x");
+    TFG_NEED(out, num_rows > 0, fn, "out");
+    TFG_NEED(node_offsets, num_sequences > 0, fn, "node_offsets");
+    TFG_NEED(status, true, fn, "status");
+    TFG_TRY(check_element(fn, "gate", gate, dtype));
+    TFG_TRY(check_element(fn, "x", x, dtype));
+    TFG_TRY(check_element(fn, "out", out, out_dtype));
+    const int64_t n = num_rows, q = num_sequences, f = num_features;
+    const int64_t tiles = (n + TFG_RECURRENCE_TILE_ROWS - 1) / TFG_RECURRENCE_TILE_ROWS;
+    const Rows ins[] = {{"gate", gate, n, gate_stride, f, elem_bytes(dtype)}, {"x", x, n, x_stride, f, elem_bytes(dtype)},
+                        {"initial", initial, q, f, f, 4}, {"node_offsets", node_offsets, 1, q + 1, q + 1, 8}};
+    const Rows outs[] = {{"out", out, n, f, f, elem_bytes(out_dtype)}, {"final_state", final_state, q, f, f, 4},
+                         {"entering", entering, tiles, f, f, 4}};
+    TFG_TRY(check_apart(fn, outs, 3, ins, 4));
+    const size_t need = tfg::gated_recurrence_workspace_bytes(n, f);
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
+#if TFG_CHECK_BOUNDS
+    for (const Rows &r : ins) TFG_DEBUG(debug_extent(fn, r.name, r.p, r.extent));
+    for (const Rows &r : outs) TFG_DEBUG(debug_extent(fn, r.name, r.p, r.extent));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
+#endif
+    return cuda_result(tfg::launch_gated_recurrence(gate, gate_stride, x, x_stride, dtype, node_offsets, n, q, f, gate_kind,
+                                                    initial, out, out_dtype, final_state, entering, workspace, status,
+                                                    reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int tfg_gated_recurrence_backward(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int dtype,
+                                  const int64_t *node_offsets, int64_t num_rows, int64_t num_sequences, int64_t num_features,
+                                  int gate_kind, const float *initial, const float *entering, const void *grad_out,
+                                  int grad_dtype, const float *grad_final, void *grad_gate, int64_t grad_gate_stride,
+                                  void *grad_x, int64_t grad_x_stride, float *grad_initial, void *workspace,
+                                  size_t workspace_bytes, int32_t *status, tfg_stream_t stream) {
+    const char *fn = "tfg_gated_recurrence_backward";
+    TFG_RANGE(fn);
+    TFG_TRY(check_recurrence(fn, num_rows, num_sequences, num_features));
+    TFG_TRY(check_dtype(fn, dtype));
+    TFG_TRY(check_dtype(fn, grad_dtype));
+    TFG_TRY(check_gate(fn, gate_kind));
+    TFG_TRY(check_stride(fn, "gate_stride", num_rows, gate_stride, num_features));
+    TFG_TRY(check_stride(fn, "x_stride", num_rows, x_stride, num_features));
+    TFG_TRY(check_stride(fn, "grad_gate_stride", num_rows, grad_gate_stride, num_features));
+    TFG_TRY(check_stride(fn, "grad_x_stride", num_rows, grad_x_stride, num_features));
+    TFG_NEED(gate, num_rows > 0, fn, "gate");
+    TFG_NEED(x, num_rows > 0, fn, "x");
+    TFG_NEED(entering, num_rows > 0, fn, "entering");
+    TFG_NEED(grad_gate, num_rows > 0, fn, "grad_gate");
+    TFG_NEED(grad_x, num_rows > 0, fn, "grad_x");
+    TFG_NEED(node_offsets, num_sequences > 0, fn, "node_offsets");
+    TFG_NEED(status, true, fn, "status");
+    TFG_TRY(check_element(fn, "gate", gate, dtype));
+    TFG_TRY(check_element(fn, "x", x, dtype));
+    TFG_TRY(check_element(fn, "grad_out", grad_out, grad_dtype));
+    TFG_TRY(check_element(fn, "grad_gate", grad_gate, dtype));
+    TFG_TRY(check_element(fn, "grad_x", grad_x, dtype));
+    const int64_t n = num_rows, q = num_sequences, f = num_features;
+    const int64_t tiles = (n + TFG_RECURRENCE_TILE_ROWS - 1) / TFG_RECURRENCE_TILE_ROWS;
+    const size_t elem = elem_bytes(dtype);
+    const Rows ins[] = {{"gate", gate, n, gate_stride, f, elem}, {"x", x, n, x_stride, f, elem},
+                        {"initial", initial, q, f, f, 4}, {"node_offsets", node_offsets, 1, q + 1, q + 1, 8},
+                        {"entering", entering, tiles, f, f, 4}, {"grad_out", grad_out, n, f, f, elem_bytes(grad_dtype)},
+                        {"grad_final", grad_final, q, f, f, 4}};
+    const Rows outs[] = {{"grad_gate", grad_gate, n, grad_gate_stride, f, elem}, {"grad_x", grad_x, n, grad_x_stride, f, elem},
+                         {"grad_initial", grad_initial, q, f, f, 4}};
+    TFG_TRY(check_apart(fn, outs, 3, ins, 7));
+    const size_t need = tfg::gated_recurrence_workspace_bytes(n, f);
+    TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
+#if TFG_CHECK_BOUNDS
+    for (const Rows &r : ins) TFG_DEBUG(debug_extent(fn, r.name, r.p, r.extent));
+    for (const Rows &r : outs) TFG_DEBUG(debug_extent(fn, r.name, r.p, r.extent));
+    TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
+#endif
+    return cuda_result(tfg::launch_gated_recurrence_backward(gate, gate_stride, x, x_stride, dtype, node_offsets, n, q, f,
+                                                             gate_kind, initial, entering, grad_out, grad_dtype, grad_final,
+                                                             grad_gate, grad_gate_stride, grad_x, grad_x_stride, grad_initial,
+                                                             workspace, status, reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+// ---- distillation loss ----------------------------------------------------------------
+namespace {
+constexpr int64_t kMaxTop = 1024;
+
+struct Distil {
+    const void *logits;
+    int dtype;
+    int64_t num_rows, num_classes;
+    const void *ids;
+    bool id32;
+    const void *teacher;
+    int teacher_dtype;
+    int64_t top_k;
+    float temperature;
+    const float *row_weight;
+};
+
+int check_distillation(const char *fn, const Distil &a) {
+    TFG_TRY(check_counts(fn, a.num_rows, 0));
+    if (a.num_classes < 1) return fail(TFG_ERR_INVALID_ARG, "%s: at least one class", fn);
+    if (a.num_classes >= kIndexLimit - 1 || (a.num_rows > 0 && a.num_classes >= (int64_t(1) << 46) / a.num_rows))
+        return fail(TFG_ERR_TOO_LARGE, "%s: num_rows * num_classes too large", fn);
+    if (a.top_k < 1) return fail(TFG_ERR_INVALID_ARG, "%s: top_k must be at least 1", fn);
+    if (a.top_k > kMaxTop) return fail(TFG_ERR_TOO_LARGE, "%s: top_k at most %lld", fn, (long long)kMaxTop);
+    TFG_TRY(check_dtype(fn, a.dtype));
+    TFG_TRY(check_dtype(fn, a.teacher_dtype));
+    if (!(a.temperature >= 1e-6f && a.temperature <= 1e6f))
+        return fail(TFG_ERR_INVALID_ARG, "%s: temperature must be in [1e-6, 1e6]", fn);
+    TFG_NEED(a.logits, a.num_rows > 0, fn, "logits");
+    TFG_NEED(a.ids, a.num_rows > 0, fn, "ids");
+    TFG_NEED(a.teacher, a.num_rows > 0, fn, "teacher");
+    TFG_TRY(check_element(fn, "logits", a.logits, a.dtype));
+    TFG_TRY(check_element(fn, "teacher", a.teacher, a.teacher_dtype));
+    TFG_DEBUG(debug_extent(fn, "logits", a.logits, elem_bytes(a.dtype) * size_t(a.num_rows * a.num_classes)));
+    TFG_DEBUG(debug_extent(fn, "ids", a.ids, (a.id32 ? 4 : 8) * size_t(a.num_rows * a.top_k)));
+    TFG_DEBUG(debug_extent(fn, "teacher", a.teacher, elem_bytes(a.teacher_dtype) * size_t(a.num_rows * a.top_k)));
+    TFG_DEBUG(debug_extent(fn, "row_weight", a.row_weight, sizeof(float) * size_t(a.num_rows)));
+    return TFG_OK;
+}
+
+int check_grad_logits(const char *fn, const Distil &a, const void *grad) {
+    const size_t bytes = elem_bytes(a.dtype) * size_t(a.num_rows * a.num_classes), top = size_t(a.num_rows * a.top_k);
+    TFG_TRY(check_element(fn, "grad_logits", grad, a.dtype));
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "logits", a.logits, bytes));
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "ids", a.ids, (a.id32 ? 4 : 8) * top));
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "teacher", a.teacher, elem_bytes(a.teacher_dtype) * top));
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "row_weight", a.row_weight, sizeof(float) * size_t(a.num_rows)));
+    TFG_DEBUG(debug_extent(fn, "grad_logits", grad, bytes));
+    return TFG_OK;
+}
+
+int distillation_common(const char *fn, const Distil &a, int64_t padding_id, float *loss, float *stats, void *grad,
+                        int32_t *status, tfg_stream_t stream) {
+    TFG_RANGE(fn);
+    TFG_TRY(check_distillation(fn, a));
+    TFG_NEED(loss, a.num_rows > 0, fn, "loss");
+    TFG_NEED(status, true, fn, "status");
+    TFG_TRY(check_grad_logits(fn, a, grad));
+    if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(TFG_ERR_INVALID_ARG, "%s: stats must be 8-byte aligned", fn);
+    TFG_DEBUG(debug_extent(fn, "loss", loss, sizeof(float) * size_t(a.num_rows)));
+    TFG_DEBUG(debug_extent(fn, "stats", stats, 2 * sizeof(float) * size_t(a.num_rows)));
+    return cuda_result(tfg::launch_distillation(a.logits, a.dtype, a.num_rows, a.num_classes, a.ids, a.id32, a.teacher,
+                                                a.teacher_dtype, static_cast<int>(a.top_k), padding_id, a.temperature,
+                                                a.row_weight, loss, stats, grad, status, reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+
+int distillation_backward_common(const char *fn, const Distil &a, int64_t padding_id, const float *stats,
+                                 const float *grad_loss, void *grad, tfg_stream_t stream) {
+    TFG_RANGE(fn);
+    TFG_TRY(check_distillation(fn, a));
+    TFG_NEED(stats, a.num_rows > 0, fn, "stats");
+    TFG_NEED(grad_loss, a.num_rows > 0, fn, "grad_loss");
+    TFG_NEED(grad, a.num_rows > 0, fn, "grad_logits");
+    TFG_TRY(check_grad_logits(fn, a, grad));
+    const size_t bytes = elem_bytes(a.dtype) * size_t(a.num_rows * a.num_classes), row = sizeof(float) * size_t(a.num_rows);
+    if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(TFG_ERR_INVALID_ARG, "%s: stats must be 8-byte aligned", fn);
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "stats", stats, 2 * row));
+    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "grad_loss", grad_loss, row));
+    TFG_DEBUG(debug_extent(fn, "stats", stats, 2 * row));
+    TFG_DEBUG(debug_extent(fn, "grad_loss", grad_loss, row));
+    return cuda_result(tfg::launch_distillation_backward(a.logits, a.dtype, a.num_rows, a.num_classes, a.ids, a.id32, a.teacher,
+                                                         a.teacher_dtype, static_cast<int>(a.top_k), padding_id, a.temperature,
+                                                         a.row_weight, stats, grad_loss, grad,
+                                                         reinterpret_cast<cudaStream_t>(stream)),
+                       fn);
+}
+}  // namespace
+
+int tfg_distillation_loss(const void *logits, int dtype, int64_t num_rows, int64_t num_classes, const int64_t *ids,
+                          const void *teacher, int teacher_dtype, int64_t top_k, int64_t padding_id, float temperature,
+                          const float *row_weight, float *loss, float *stats, void *grad_logits, int32_t *status,
+                          tfg_stream_t stream) {
+    return distillation_common("tfg_distillation_loss", {logits, dtype, num_rows, num_classes, ids, false, teacher, teacher_dtype,
+                               top_k, temperature, row_weight}, padding_id, loss, stats, grad_logits, status, stream);
+}
+
+int tfg_distillation_loss32(const void *logits, int dtype, int64_t num_rows, int64_t num_classes, const int32_t *ids,
+                            const void *teacher, int teacher_dtype, int64_t top_k, int64_t padding_id, float temperature,
+                            const float *row_weight, float *loss, float *stats, void *grad_logits, int32_t *status,
+                            tfg_stream_t stream) {
+    return distillation_common("tfg_distillation_loss32", {logits, dtype, num_rows, num_classes, ids, true, teacher,
+                               teacher_dtype, top_k, temperature, row_weight}, padding_id, loss, stats, grad_logits, status,
+                               stream);
+}
+
+int tfg_distillation_loss_backward(const void *logits, int dtype, int64_t num_rows, int64_t num_classes, const int64_t *ids,
+                                   const void *teacher, int teacher_dtype, int64_t top_k, int64_t padding_id,
+                                   float temperature, const float *row_weight, const float *stats, const float *grad_loss,
+                                   void *grad_logits, tfg_stream_t stream) {
+    return distillation_backward_common("tfg_distillation_loss_backward", {logits, dtype, num_rows, num_classes, ids, false,
+                                        teacher, teacher_dtype, top_k, temperature, row_weight}, padding_id, stats, grad_loss,
+                                        grad_logits, stream);
+}
+
+int tfg_distillation_loss_backward32(const void *logits, int dtype, int64_t num_rows, int64_t num_classes, const int32_t *ids,
+                                     const void *teacher, int teacher_dtype, int64_t top_k, int64_t padding_id,
+                                     float temperature, const float *row_weight, const float *stats, const float *grad_loss,
+                                     void *grad_logits, tfg_stream_t stream) {
+    return distillation_backward_common("tfg_distillation_loss_backward32", {logits, dtype, num_rows, num_classes, ids, true,
+                                        teacher, teacher_dtype, top_k, temperature, row_weight}, padding_id, stats, grad_loss,
+                                        grad_logits, stream);
+}
+
 // ---- global norm and clipping -----------------------------------------------------
 namespace {
 constexpr int64_t kMaxTensors = int64_t(1) << 20;

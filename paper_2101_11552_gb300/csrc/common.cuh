@@ -191,6 +191,23 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 #endif
 }
 
+// Last graph that begins at or before row r, -1 if there is none; by the whole warp, 32
+// probes a round.
+__device__ __forceinline__ int64_t warp_graph_at(const int64_t *offsets, int64_t graphs, int64_t r) {
+    const int lane = threadIdx.x & 31;
+    int64_t lo = -1, hi = graphs - 1;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 31) / 32;
+        const int64_t at = lo + (lane + 1) * step;
+        const bool le = at <= hi && __ldg(offsets + at) <= r;
+        const int c = __popc(lane_ballot(le));
+        const int64_t top = lo + (c + 1) * step - 1;
+        lo += c * step;
+        hi = top < hi ? top : hi;
+    }
+    return lo;
+}
+
 __host__ __device__ constexpr int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 __host__ __device__ constexpr int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 
@@ -335,6 +352,32 @@ cudaError_t launch_group_norm_backward(const void *x, int x_dtype, const int64_t
 size_t global_norm_workspace_bytes(int64_t tensors);
 cudaError_t launch_global_norm(int64_t tensors, const void *const *in, const int64_t *sizes, const int *dtypes,
                                float clip, void *const *outs, float *norm, void *ws, cudaStream_t s);
+cudaError_t launch_layer_norm(const void *x, int x_dtype, const void *residual, int sum_dtype, void *sum, int64_t n,
+                              int64_t f, const float *gamma, const float *beta, float eps, void *out, int out_dtype,
+                              float *mean, float *rstd, cudaStream_t s);
+size_t layer_norm_backward_workspace_bytes(int64_t n, int64_t f);
+cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n, int64_t f, const float *gamma,
+                                       const float *mean, const float *rstd, const void *g, int g_dtype, const void *skip,
+                                       void *grad_s, int out_dtype, float *grad_gamma, float *grad_beta, void *ws,
+                                       cudaStream_t s);
+size_t gated_recurrence_workspace_bytes(int64_t n, int64_t f);
+cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
+                                    const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                    const float *initial, void *out, int out_dtype, float *final_state, float *entering,
+                                    void *ws, int32_t *status, cudaStream_t s);
+cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
+                                             const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                             const float *initial, const float *entered, const void *g, int g_dtype,
+                                             const float *grad_final, void *grad_gate, int64_t grad_gate_ld, void *grad_x,
+                                             int64_t grad_x_ld, float *grad_initial, void *ws, int32_t *status,
+                                             cudaStream_t s);
+cudaError_t launch_distillation(const void *logits, int dtype, int64_t n, int64_t v, const void *ids, bool id32,
+                                const void *teacher, int teacher_dtype, int k, int64_t padding, float tau, const float *weight,
+                                float *loss, float *stats, void *grad, int32_t *status, cudaStream_t s);
+cudaError_t launch_distillation_backward(const void *logits, int dtype, int64_t n, int64_t v, const void *ids, bool id32,
+                                         const void *teacher, int teacher_dtype, int k, int64_t padding, float tau,
+                                         const float *weight, const float *stats, const float *grad_loss, void *grad,
+                                         cudaStream_t s);
 cudaError_t launch_gather_xor(const int32_t *col, int64_t e, const void *x, int64_t row_bytes,
                               uint32_t *out, cudaStream_t s);
 cudaError_t launch_segment_pool(const void *x, int x_dtype, const int64_t *batch, int64_t n,

@@ -39,11 +39,6 @@ constexpr int kActNone = TFG_ACT_NONE, kActRelu = TFG_ACT_RELU, kActSilu = TFG_A
 // max(|y|, 1).  Where 2^(...) passes 2^126 the sigmoid is 0 and y e^y below 1e-36.  The math
 // library's expf and quotient cost 12 instructions more a value (110-row graphs, F = 128:
 // the forward was bound by issue, 55 instructions a value).
-__device__ __forceinline__ float exp2_of(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 template <int VEC>
 __device__ __forceinline__ void sigmoid_of(const float (&y)[VEC], float (&p)[VEC]) {
     const float minus_log2e[1] = {-1.44269504088896341f}, one[1] = {1.f};
@@ -185,23 +180,6 @@ __device__ __forceinline__ void check_offsets(const NormArgs &p) {
     }
     const int all = __syncthreads_or(any);
     if (threadIdx.x == 0) *p.status_all = all ? TFG_ERR_INDEX_RANGE : TFG_OK;
-}
-
-// Last graph that begins at or before row r, -1 if there is none; by the whole warp, 32
-// probes a round.
-__device__ __forceinline__ int64_t warp_graph_at(const int64_t *offsets, int64_t graphs, int64_t r) {
-    const int lane = threadIdx.x & 31;
-    int64_t lo = -1, hi = graphs - 1;
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 31) / 32;
-        const int64_t at = lo + (lane + 1) * step;
-        const bool le = at <= hi && __ldg(offsets + at) <= r;
-        const int c = __popc(lane_ballot(le));
-        const int64_t top = lo + (c + 1) * step - 1;
-        lo += c * step;
-        hi = top < hi ? top : hi;
-    }
-    return lo;
 }
 
 // covered: the rows up to which slot 0's search has told what there is; slot 1 needs no search

@@ -1,0 +1,79 @@
+// Layer norm of rows, backward: geometry, launch by type and the join of the columns' sums
+// (layer_norm_backward.cuh: the kernels).
+#include "layer_norm_backward.cuh"
+
+namespace tfg {
+
+cudaError_t launch_row_back_f32_f32(const RowBackArgs &p, cudaStream_t s);
+cudaError_t launch_row_back_f32_bf16(const RowBackArgs &p, cudaStream_t s);
+cudaError_t launch_row_back_bf16_f32(const RowBackArgs &p, cudaStream_t s);
+cudaError_t launch_row_back_bf16_bf16(const RowBackArgs &p, cudaStream_t s);
+
+namespace {
+
+constexpr int kJoinCols = 32, kJoinRows = 8;
+
+// out[c] = sum over the CTAs of part[.][c], in 8 interleaved chains joined in order.
+__global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns(const float *part, int ctas, int64_t f, float *gamma,
+                                                                     float *beta) {
+    __shared__ float s_part[kJoinRows][kJoinCols];
+    const int x = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + x;
+    float sum = 0.f;
+    if (c < 2 * f) {
+#pragma unroll 4
+        for (int b = y; b < ctas; b += kJoinRows) sum += __ldg(part + b * 2 * f + c);
+    }
+    s_part[y][x] = sum;
+    __syncthreads();
+    if (y == 0 && c < 2 * f) {
+#pragma unroll
+        for (int j = 1; j < kJoinRows; ++j) sum += s_part[j][x];
+        (c < f ? gamma[c] : beta[c - f]) = sum;
+    }
+}
+
+// CTAs of the first kernel for the given width, whatever the alignment: the least team.
+int back_ctas(int64_t n, int64_t f) {
+    const int64_t vecs = (f + 7) / 8;
+    const int64_t per_cta = vecs <= 8 ? 32 : (vecs <= 128 ? 8 : 1);
+    const int64_t most = static_cast<int64_t>(sm_count()) * 2;
+    const int64_t want = (n + per_cta - 1) / per_cta;
+    return static_cast<int>(want < 1 ? 1 : (want < most ? want : most));
+}
+
+}  // namespace
+
+size_t layer_norm_backward_workspace_bytes(int64_t n, int64_t f) {
+    return sizeof(float) * (2 * size_t(f) * back_ctas(n, f) + size_t(n));
+}
+
+cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n, int64_t f, const float *gamma,
+                                       const float *mean, const float *rstd, const void *g, int g_dtype, const void *skip,
+                                       void *grad_s, int out_dtype, float *grad_gamma, float *grad_beta, void *ws,
+                                       cudaStream_t s) {
+    if (n == 0) {
+        if (!grad_gamma) return cudaSuccess;
+        cudaError_t e = cudaMemsetAsync(grad_gamma, 0, sizeof(float) * size_t(f), s);
+        return e != cudaSuccess ? e : cudaMemsetAsync(grad_beta, 0, sizeof(float) * size_t(f), s);
+    }
+    RowBackArgs p{sum, n, f, gamma, mean, rstd, g, skip, grad_s, nullptr, nullptr, grad_gamma, grad_beta, out_dtype, 1, 1};
+    const auto fits = [&](int vec) {
+        return vec_fits(sum, sum_dtype, f, vec) && vec_fits(g, g_dtype, f, vec) && vec_fits(grad_s, out_dtype, f, vec) &&
+               (!skip || vec_fits(skip, out_dtype, f, vec)) && weights_fit(gamma);
+    };
+    p.vec = fits(8) ? 8 : (fits(4) ? 4 : 1);
+    p.ctas = back_ctas(n, f);
+    if (grad_gamma) {
+        p.part = static_cast<float *>(ws);
+        p.shift = p.part + 2 * size_t(f) * p.ctas;
+    }
+    cudaError_t e;
+    if (sum_dtype == TFG_BF16) e = g_dtype == TFG_BF16 ? launch_row_back_bf16_bf16(p, s) : launch_row_back_bf16_f32(p, s);
+    else e = g_dtype == TFG_BF16 ? launch_row_back_f32_bf16(p, s) : launch_row_back_f32_f32(p, s);
+    if (e != cudaSuccess || !grad_gamma) return e;
+    join_columns<<<ceil_div(2 * f, kJoinCols), kJoinCols * kJoinRows, 0, s>>>(p.part, p.ctas, f, grad_gamma, grad_beta);
+    return cudaGetLastError();
+}
+
+}  // namespace tfg

@@ -98,6 +98,13 @@ __device__ __forceinline__ void fma_vec(float (&d)[VEC], const float (&a)[VEC], 
     }
 }
 
+// 2^v by the hardware, within 2 ulp; below 2^-126 zero.
+__device__ __forceinline__ float exp2_of(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 // A vector by plain loads: from shared memory, or from memory that the kernel also writes.
 template <typename T, int VEC>
 __device__ __forceinline__ typename VecLoad<T, VEC>::Raw load_plain(const T *p) {

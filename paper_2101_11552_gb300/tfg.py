@@ -34,6 +34,8 @@ TFG_ERR_UNSORTED = -6
 TFG_ERR_TIMEOUT = -7
 TFG_F32, TFG_BF16 = 0, 1
 REDUCERS = {"sum": 0, "mean": 1, "max": 2}
+GATES = {"sigmoid": 0, "exp": 1}
+RECURRENCE_TILE_ROWS = 128
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 NO_PADDING = -(1 << 63)       # padding_id of a list without padding
 
@@ -119,6 +121,17 @@ def _load(path: str) -> ctypes.CDLL:
         "tfg_global_norm_workspace_size": [I64, ctypes.POINTER(SZ)],
         "tfg_global_norm": [I64, P, P, P, P, P, SZ, P],
         "tfg_clip_by_global_norm": [I64, P, P, P, F, P, P, P, SZ, P],
+        "tfg_layer_norm": [P, I, P, I, P, I64, I64, P, P, F, P, I, P, P, P],
+        "tfg_layer_norm_backward_workspace_size": [I64, I64, ctypes.POINTER(SZ)],
+        "tfg_layer_norm_backward": [P, I, I64, I64, P, P, P, P, I, P, P, I, P, P, P, SZ, P],
+        "tfg_gated_recurrence_workspace_size": [I64, I64, ctypes.POINTER(SZ)],
+        "tfg_gated_recurrence": [P, I64, P, I64, I, P, I64, I64, I64, I, P, P, I, P, P, P, SZ, P, P],
+        "tfg_gated_recurrence_backward": [P, I64, P, I64, I, P, I64, I64, I64, I, P, P, P, I, P, P, I64, P, I64, P, P, SZ, P,
+                                          P],
+        "tfg_distillation_loss": [P, I, I64, I64, P, P, I, I64, I64, F, P, P, P, P, P, P],
+        "tfg_distillation_loss32": [P, I, I64, I64, P, P, I, I64, I64, F, P, P, P, P, P, P],
+        "tfg_distillation_loss_backward": [P, I, I64, I64, P, P, I, I64, I64, F, P, P, P, P, P],
+        "tfg_distillation_loss_backward32": [P, I, I64, I64, P, P, I, I64, I64, F, P, P, P, P, P],
         "tfg_edge_softmax_backward_workspace_size": [I64, I, I, ctypes.POINTER(SZ)],
         "tfg_edge_softmax_aggregate_backward": [P, P, P, P, P, I, I64, I64, I, I, P, P, F,
                                                 P, P, P, P, P, P, SZ, P],
@@ -917,6 +930,279 @@ def tfg_group_norm_backward(x, node_offsets, num_groups: int, gamma, beta, mean,
          _at(beta), mean.data_ptr(), rstd.data_ptr(), ACTIVATIONS[activation], grad_out.data_ptr(), grad_code,
          grad_x.data_ptr(), _at(grad_gamma), _at(grad_beta), *_span(workspace))
     return grad_x, grad_gamma, grad_beta
+
+
+class LayerNorm(NamedTuple):
+    out: torch.Tensor
+    sum: torch.Tensor              # x + residual in the residual's type; x itself without a residual
+    mean: Optional[torch.Tensor]   # fp32 [N], for the backward
+    rstd: Optional[torch.Tensor]   # fp32 [N]
+
+
+def _row_array(name: str, t, index: int, shape):
+    _same(name, t, index)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dtype_code(name, t.dtype)
+
+
+def _weights(index: int, f: int, **weights):
+    for name, w in weights.items():
+        if w is not None:
+            _same(name, w, index, torch.float32)
+            if w.numel() != f:
+                raise ValueError(f"{name} must have {f} values")
+
+
+def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, out_dtype: Optional[torch.dtype] = None,
+                   want_stats: bool = True, out=None, sum_out=None) -> LayerNorm:
+    """Layer norm of the rows of x [N, F], or of x + residual, which is stored in the residual's
+    type and normalised as stored.  ``sum_out`` may be the residual itself (in place)."""
+    index = _index("x", x)
+    if x.dim() != 2:
+        raise ValueError("x must have shape [N, F]")
+    n, f = x.shape
+    code = _dtype_code("x", x.dtype)
+    _weights(index, f, gamma=gamma, beta=beta)
+    sum_code = 0
+    if residual is not None:
+        sum_code = _row_array("residual", residual, index, x.shape)
+        sum_out = _need_out("sum_out", sum_out, x.shape, residual.dtype, x)
+    elif sum_out is not None:
+        raise ValueError("sum_out is the sum with a residual: give one")
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    out_code = _dtype_code("out", out_dtype)
+    out = _need_out("out", out, x.shape, out_dtype, x)
+    mean = rstd = None
+    if want_stats:
+        mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device)
+    _run(index, "tfg_layer_norm", x.data_ptr(), code, _at(residual), sum_code, _at(sum_out), n, f, _at(gamma), _at(beta), eps,
+         out.data_ptr(), out_code, _at(mean), _at(rstd))
+    return LayerNorm(out, x if residual is None else sum_out, mean, rstd)
+
+
+def tfg_layer_norm_backward_workspace_size(num_rows: int, num_features: int) -> int:
+    return _size("tfg_layer_norm_backward_workspace_size", num_rows, num_features)
+
+
+def tfg_layer_norm_backward(sum, gamma, mean, rstd, grad_out, grad_sum=None, grad_dtype: Optional[torch.dtype] = None,
+                            want_weight_grads: bool = True, grad_x=None, workspace=None):
+    """Gradients of tfg_layer_norm from its ``sum``, mean and rstd.  ``grad_sum``: the gradient
+    that reaches the sum by other ways (the residual stream's own), added.  Returns (grad_x
+    [N, F], the gradient of x and residual alike, grad_gamma [F], grad_beta [F]), the last two None
+    without ``want_weight_grads``.  grad_x has the type of grad_sum, else ``grad_dtype`` (by
+    default grad_out's), and may be grad_sum itself (in place)."""
+    index = _index("sum", sum)
+    if sum.dim() != 2:
+        raise ValueError("sum must have shape [N, F]")
+    n, f = sum.shape
+    code = _dtype_code("sum", sum.dtype)
+    _weights(index, f, gamma=gamma)
+    for name, s in (("mean", mean), ("rstd", rstd)):
+        _same(name, s, index, torch.float32)
+        if s.numel() != n:
+            raise ValueError(f"{name} must have shape [N]")
+    grad_code = _row_array("grad_out", grad_out, index, sum.shape)
+    if grad_sum is not None:
+        _row_array("grad_sum", grad_sum, index, sum.shape)
+        if grad_dtype is not None and grad_dtype is not grad_sum.dtype:
+            raise ValueError("grad_dtype must be grad_sum's type")
+        grad_dtype = grad_sum.dtype
+    elif grad_dtype is None:
+        grad_dtype = grad_out.dtype if grad_x is None else grad_x.dtype
+    x_code = _dtype_code("grad_x", grad_dtype)
+    grad_x = _need_out("grad_x", grad_x, sum.shape, grad_dtype, sum)
+    grad_gamma = grad_beta = None
+    need = 0
+    if want_weight_grads:
+        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=sum.device)
+        need = tfg_layer_norm_backward_workspace_size(n, f)
+    workspace = _workspace(workspace, need, sum)
+    _run(index, "tfg_layer_norm_backward", sum.data_ptr(), code, n, f, _at(gamma), mean.data_ptr(), rstd.data_ptr(),
+         grad_out.data_ptr(), grad_code, _at(grad_sum), grad_x.data_ptr(), x_code, _at(grad_gamma), _at(grad_beta),
+         *_span(workspace))
+    return grad_x, grad_gamma, grad_beta
+
+
+class GatedRecurrence(NamedTuple):
+    out: torch.Tensor
+    final: Optional[torch.Tensor]         # fp32 [S, F]: the state behind each sequence
+    checkpoints: Optional[torch.Tensor]   # fp32 [tiles, F], for the backward
+    status: torch.Tensor                  # int32 [1] (device)
+
+
+def tfg_gated_recurrence_workspace_size(num_rows: int, num_features: int) -> int:
+    return _size("tfg_gated_recurrence_workspace_size", num_rows, num_features)
+
+
+def _strided_rows(name: str, t, index: int, shape=None, dtype=None) -> int:
+    """The row stride of [N, F] whose rows are contiguous, on the given device."""
+    try:
+        at, strides = t.get_device(), t.stride()
+    except AttributeError:                        # no tensor at all
+        at = -1
+    if at < 0:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if index >= 0 and at != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must have shape {'[N, F]' if shape is None else tuple(shape)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    n, f = t.shape
+    if f > 1 and strides[1] != 1 or n > 1 and strides[0] < f:
+        raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
+    return strides[0] if n > 1 else f
+
+
+def _recurrence_inputs(gate, x, node_offsets, kind, initial):
+    ld = _strided_rows("gate", gate, -1)
+    index = gate.get_device()
+    n, f = gate.shape
+    code = _dtype_code("gate", gate.dtype)
+    x_ld = _strided_rows("x", x, index, gate.shape, gate.dtype)
+    _same("node_offsets", node_offsets, index, torch.int64)
+    if node_offsets.dim() != 1 or node_offsets.numel() < 1:
+        raise ValueError("node_offsets must have shape [S + 1]")
+    s = node_offsets.numel() - 1
+    if kind not in GATES:
+        raise ValueError(f"kind must be one of {sorted(GATES)}, got {kind!r}")
+    _states(index, (s, f), initial=initial)
+    return index, n, f, s, code, (gate.data_ptr(), ld, x.data_ptr(), x_ld, code, node_offsets.data_ptr(), n, s, f, GATES[kind],
+                                  _at(initial))
+
+
+def _states(index: int, shape, **states):
+    for name, t in states.items():
+        if t is not None:
+            _same(name, t, index, torch.float32)
+            if t.shape != shape:
+                raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _tiles(n: int) -> int:
+    return -(-n // RECURRENCE_TILE_ROWS)
+
+
+def tfg_gated_recurrence(gate, x, node_offsets, kind: str = "sigmoid", initial=None,
+                         out_dtype: Optional[torch.dtype] = None, want_final: bool = True, want_checkpoints: bool = True,
+                         out=None, workspace=None) -> GatedRecurrence:
+    """v = a v + b along the rows of each sequence, channel by channel: ``kind`` "sigmoid" with
+    a = sigmoid(gate), b = (1 - a) x, or "exp" with a = exp(gate), b = x.  Sequence s holds
+    the rows node_offsets[s] .. node_offsets[s + 1] - 1 of gate and x [N, F], whose rows may
+    lie apart (the halves of one projection); ``initial`` [S, F] fp32 are the states before
+    them, zeros by default, and ``final`` those behind them.  Rows outside all sequences are left
+    as they are in ``out`` (unset in a new one)."""
+    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
+    if out_dtype is None:
+        out_dtype = gate.dtype if out is None else out.dtype
+    out_code = _dtype_code("out", out_dtype)
+    need = tfg_gated_recurrence_workspace_size(n, f)
+    out = _need_out("out", out, gate.shape, out_dtype, gate)
+    final = torch.empty(s, f, dtype=torch.float32, device=gate.device) if want_final else None
+    kept = torch.empty(_tiles(n), f, dtype=torch.float32, device=gate.device) if want_checkpoints else None
+    workspace = _workspace(workspace, need, gate)
+    status = torch.empty(1, dtype=torch.int32, device=gate.device)
+    _run(index, "tfg_gated_recurrence", *head, out.data_ptr(), out_code, _at(final), _at(kept), *_span(workspace),
+         status.data_ptr())
+    return GatedRecurrence(out, final, kept, status)
+
+
+class GatedRecurrenceGrads(NamedTuple):
+    gate: torch.Tensor
+    x: torch.Tensor
+    initial: Optional[torch.Tensor]       # fp32 [S, F], with want_initial
+
+
+def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=None, kind: str = "sigmoid", initial=None,
+                                  grad_final=None, want_initial: Optional[bool] = None, grad_gate=None, grad_x=None,
+                                  workspace=None, status=None) -> GatedRecurrenceGrads:
+    """Gradients of tfg_gated_recurrence with the forward's arguments and ``checkpoints``, from
+    ``grad_out`` [N, F] (either type; None: zeros) and ``grad_final`` [S, F] fp32 (None: zeros).
+    The states' gradient by default where there was an initial state.  ``grad_gate`` and ``grad_x``
+    may be given as buffers whose rows lie apart; rows outside all sequences are left as
+    they are in them.  ``status`` int32 [1] takes the call's status word."""
+    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
+    _states(index, (s, f), grad_final=grad_final)
+    _states(index, (_tiles(n), f), checkpoints=checkpoints)
+    if checkpoints is None:
+        raise ValueError("checkpoints are the forward's (want_checkpoints)")
+    grad_code = TFG_F32 if grad_out is None else _row_array("grad_out", grad_out, index, gate.shape)
+    grads = []
+    for name, t in (("grad_gate", grad_gate), ("grad_x", grad_x)):
+        if t is None:
+            t = torch.empty(n, f, dtype=gate.dtype, device=gate.device)
+        grads.append((t, _strided_rows(name, t, index, gate.shape, gate.dtype)))
+    if want_initial is None:
+        want_initial = initial is not None
+    grad_initial = torch.empty(s, f, dtype=torch.float32, device=gate.device) if want_initial else None
+    workspace = _workspace(workspace, tfg_gated_recurrence_workspace_size(n, f), gate)
+    status = _need_out("status", status, (1,), torch.int32, gate)
+    _run(index, "tfg_gated_recurrence_backward", *head, checkpoints.data_ptr(), _at(grad_out), grad_code, _at(grad_final),
+         grads[0][0].data_ptr(), grads[0][1], grads[1][0].data_ptr(), grads[1][1], _at(grad_initial), *_span(workspace),
+         status.data_ptr())
+    return GatedRecurrenceGrads(grads[0][0], grads[1][0], grad_initial)
+
+
+class DistillationLoss(NamedTuple):
+    loss: torch.Tensor                     # fp32 [N]
+    stats: Optional[torch.Tensor]          # fp32 [N, 2], for the backward
+    grad_logits: Optional[torch.Tensor]    # [N, V], with want_grad
+    status: torch.Tensor                   # int32 [1] (device)
+
+
+def _distillation_inputs(logits, ids, teacher, temperature, row_weight, padding_id):
+    index, id32 = _need_ids(ids)
+    _same("logits", logits, index)
+    _same("teacher", teacher, index)
+    if logits.dim() != 2 or ids.dim() != 2 or ids.shape[0] != logits.shape[0]:
+        raise ValueError("logits and ids must have shapes [N, V] and [N, K]")
+    if teacher.shape != ids.shape:
+        raise ValueError("teacher must have the shape of ids")
+    n, v = logits.shape
+    codes = _dtype_code("logits", logits.dtype), _dtype_code("teacher", teacher.dtype)
+    if row_weight is not None:
+        _same("row_weight", row_weight, index, torch.float32)
+        if row_weight.numel() != n:
+            raise ValueError("row_weight must have shape [N]")
+    return index, id32, (logits.data_ptr(), codes[0], n, v, ids.data_ptr(), teacher.data_ptr(), codes[1], ids.shape[1],
+                         _padding(padding_id), temperature, _at(row_weight))
+
+
+def tfg_distillation_loss(logits, ids, teacher, temperature: float = 1.0, row_weight=None, padding_id: Optional[int] = None,
+                          want_stats: bool = False, want_grad: bool = False, grad_logits=None) -> DistillationLoss:
+    """row_weight T^2 KL(softmax(teacher / T) over the given classes || softmax(logits / T)) of
+    each row: logits [N, V], ids (int64 or int32) and teacher [N, K], the classes and logits
+    that were kept of the teacher.  Entries whose id is ``padding_id`` count for nothing, nor do rows of weight 0.
+    ``want_grad`` (or a buffer ``grad_logits``) gives the logits' gradient of the losses' sum in the same pass;
+    ``want_stats`` what tfg_distillation_loss_backward needs."""
+    index, id32, head = _distillation_inputs(logits, ids, teacher, temperature, row_weight, padding_id)
+    if want_grad or grad_logits is not None:
+        grad_logits = _need_out("grad_logits", grad_logits, logits.shape, logits.dtype, logits)
+    n, dev = logits.shape[0], logits.device
+    loss = torch.empty(n, dtype=torch.float32, device=dev)
+    stats = torch.empty(n, 2, dtype=torch.float32, device=dev) if want_stats else None
+    status = torch.empty(1, dtype=torch.int32, device=dev)
+    _run(index, "tfg_distillation_loss32" if id32 else "tfg_distillation_loss", *head, loss.data_ptr(), _at(stats),
+         _at(grad_logits), status.data_ptr())
+    return DistillationLoss(loss, stats, grad_logits, status)
+
+
+def tfg_distillation_loss_backward(logits, ids, teacher, temperature: float, stats, grad_loss, row_weight=None,
+                                   padding_id: Optional[int] = None, grad_logits=None):
+    """grad_logits [N, V] of tfg_distillation_loss for grad_loss [N], with the forward's
+    arguments and stats."""
+    index, id32, head = _distillation_inputs(logits, ids, teacher, temperature, row_weight, padding_id)
+    n = logits.shape[0]
+    for name, t, shape in (("stats", stats, (n, 2)), ("grad_loss", grad_loss, (n,))):
+        _same(name, t, index, torch.float32)
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {shape}")
+    grad_logits = _need_out("grad_logits", grad_logits, logits.shape, logits.dtype, logits)
+    _run(index, "tfg_distillation_loss_backward32" if id32 else "tfg_distillation_loss_backward", *head, stats.data_ptr(),
+         grad_loss.data_ptr(), grad_logits.data_ptr())
+    return grad_logits
 
 
 def tfg_global_norm_workspace_size(num_tensors: int) -> int:
