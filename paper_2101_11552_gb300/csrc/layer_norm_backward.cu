@@ -11,17 +11,18 @@ cudaError_t launch_row_back_bf16_bf16(const RowBackArgs &p, cudaStream_t s);
 
 namespace {
 
-constexpr int kJoinCols = 32, kJoinRows = 8;
+constexpr int kJoinCols = 32, kJoinRows = 32;
+constexpr int kBackResident = 6;          // CTAs of a multiprocessor at most (128 threads each)
 
-// out[c] = sum over the CTAs of part[.][c], in 8 interleaved chains joined in order.
-__global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns(const float *part, int ctas, int64_t f, float *gamma,
-                                                                     float *beta) {
+// out[c] = sum over the CTAs of part[.][c], in 32 interleaved chains joined in order.
+__global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns_kernel(const float *part, int ctas, int64_t f,
+                                                                            float *gamma, float *beta) {
     __shared__ float s_part[kJoinRows][kJoinCols];
     const int x = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + x;
     float sum = 0.f;
     if (c < 2 * f) {
-#pragma unroll 4
+#pragma unroll 8
         for (int b = y; b < ctas; b += kJoinRows) sum += __ldg(part + b * 2 * f + c);
     }
     s_part[y][x] = sum;
@@ -33,19 +34,21 @@ __global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns(const float
     }
 }
 
-// CTAs of the first kernel for the given width, whatever the alignment: the least team.
-int back_ctas(int64_t n, int64_t f) {
-    const int64_t vecs = (f + 7) / 8;
-    const int64_t per_cta = vecs <= 8 ? 32 : (vecs <= 128 ? 8 : 1);
-    const int64_t most = static_cast<int64_t>(sm_count()) * 2;
-    const int64_t want = (n + per_cta - 1) / per_cta;
-    return static_cast<int>(want < 1 ? 1 : (want < most ? want : most));
-}
-
 }  // namespace
 
+cudaError_t join_columns(const float *part, int ctas, int64_t f, float *gamma, float *beta, cudaStream_t s) {
+    join_columns_kernel<<<ceil_div(2 * f, kJoinCols), kJoinCols * kJoinRows, 0, s>>>(part, ctas, f, gamma, beta);
+    return cudaGetLastError();
+}
+
+int back_ctas(int64_t n, int teams, int resident) {
+    const int64_t rounds = (n + teams - 1) / teams, sms = sm_count();
+    const int64_t few = rounds < sms ? rounds : sms, want = rounds / 4 > few ? rounds / 4 : few;
+    return static_cast<int>(want < resident * sms ? want : resident * sms);
+}
+
 size_t layer_norm_backward_workspace_bytes(int64_t n, int64_t f) {
-    return sizeof(float) * (2 * size_t(f) * back_ctas(n, f) + size_t(n));
+    return sizeof(float) * (2 * size_t(f) * size_t(back_ctas(n, 1, kBackResident)) + size_t(n));
 }
 
 cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n, int64_t f, const float *gamma,
@@ -63,17 +66,12 @@ cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n
                (!skip || vec_fits(skip, out_dtype, f, vec)) && weights_fit(gamma);
     };
     p.vec = fits(8) ? 8 : (fits(4) ? 4 : 1);
-    p.ctas = back_ctas(n, f);
     if (grad_gamma) {
         p.part = static_cast<float *>(ws);
-        p.shift = p.part + 2 * size_t(f) * p.ctas;
+        p.shift = p.part + 2 * size_t(f) * size_t(back_ctas(n, 1, kBackResident));
     }
-    cudaError_t e;
-    if (sum_dtype == TFG_BF16) e = g_dtype == TFG_BF16 ? launch_row_back_bf16_bf16(p, s) : launch_row_back_bf16_f32(p, s);
-    else e = g_dtype == TFG_BF16 ? launch_row_back_f32_bf16(p, s) : launch_row_back_f32_f32(p, s);
-    if (e != cudaSuccess || !grad_gamma) return e;
-    join_columns<<<ceil_div(2 * f, kJoinCols), kJoinCols * kJoinRows, 0, s>>>(p.part, p.ctas, f, grad_gamma, grad_beta);
-    return cudaGetLastError();
+    if (sum_dtype == TFG_BF16) return g_dtype == TFG_BF16 ? launch_row_back_bf16_bf16(p, s) : launch_row_back_bf16_f32(p, s);
+    return g_dtype == TFG_BF16 ? launch_row_back_f32_bf16(p, s) : launch_row_back_f32_f32(p, s);
 }
 
 }  // namespace tfg

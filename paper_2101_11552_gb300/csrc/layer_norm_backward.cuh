@@ -9,8 +9,11 @@
 // row: with e = r mean(s - m) taken beside the other sums, h - e is right to a few u of itself,
 // and mean(d (h - e)) = mean(d h) - e mean d needs no second pass.
 //
-// A CTA takes the rows b, b + CTAs, ..., keeps the sums of its columns for gamma and beta in
-// registers and writes them once; a second kernel adds the CTAs' in order.
+// A CTA takes the rows b, b + CTAs, ... (a row for each of its teams), keeps the sums of its columns
+// for gamma and beta in registers and writes them once; a second kernel adds the CTAs' in order.
+// The next rows' vectors are on their way to shared memory (each thread's own, without a barrier) while
+// a row is worked on: held in registers instead, 182 a thread left 8 warps on a multiprocessor
+// and loads waited for one another (8,192 rows of 8,192 bf16: 320 us).
 #pragma once
 
 #include "layer_norm.cuh"
@@ -32,93 +35,181 @@ struct RowBackArgs {
     int ctas;
 };
 
+// CTAs of the first kernel: as many as fit, with four rows for each team where there are enough.
+int back_ctas(int64_t n, int teams, int resident);
+cudaError_t join_columns(const float *part, int ctas, int64_t f, float *gamma, float *beta, cudaStream_t s);
+
 namespace {
 
-// The three sums of a row: d, d h, s - m.
+// The three sums of a row: d, d (s - m), s - m.
 template <int VEC>
-__device__ __forceinline__ void row_terms(const float (&s)[VEC], const float (&g)[VEC], const float (&w)[VEC], float m, float r,
+__device__ __forceinline__ void row_terms(const float (&s)[VEC], const float (&g)[VEC], const float (&w)[VEC], float m,
                                           float (&sum)[3]) {
+    const float away[1] = {-m};
+    float c[VEC], d[VEC];
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-        const float c = s[q] - m, d = g[q] * w[q];
-        sum[0] += d;
-        sum[1] = fmaf(d, c, sum[1]);
-        sum[2] += c;
+    for (int q = 0; q < VEC; ++q) c[q] = s[q], d[q] = g[q];
+    add_vec(c, away);
+    mul_vec(d, w);
+    float t[3][VEC];
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) t[0][q] = d[q], t[2][q] = c[q];
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) t[1][q] = d[q];
+    mul_vec(t[1], c);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int o = VEC / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int q = 0; q < o; ++q) t[k][q] += t[k][q + o];
+        sum[k] += t[k][0];
     }
 }
 
-// What the sums make of a row: h = (s - m) r - e.
+// What the sums make of a row: h = (s - m) r - e and
+// grad_s = r d + (s - m) slope + shift, slope = -r^2 mean(d h), shift = r (e mean(d h) - mean d).
 struct RowMeans {
-    float d, dh, e;
+    float e, slope, shift;
     __device__ __forceinline__ RowMeans(const float (&sum)[3], float r, float per) {
-        d = sum[0] * per;
+        const float d = sum[0] * per;
         e = sum[2] * per * r;
-        dh = fmaf(-e, d, sum[1] * r * per);
+        const float dh = fmaf(-e, d, sum[1] * r * per);
+        slope = -r * r * dh;
+        shift = r * fmaf(e, dh, -d);
     }
 };
 
+// grad_s of VEC values into o (which holds grad_sum), h into s.
+template <int VEC>
+__device__ __forceinline__ void row_gradient(float (&s)[VEC], const float (&g)[VEC], const float (&w)[VEC], float m, float r,
+                                             const RowMeans &a, float (&o)[VEC]) {
+    const float away[1] = {-m}, by[1] = {r}, less[1] = {-a.e}, slope[1] = {a.slope}, shift[1] = {a.shift};
+    float d[VEC];
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) d[q] = g[q];
+    mul_vec(d, w);
+    add_vec(s, away);
+    add_vec(o, shift);
+    fma_vec(o, s, slope, o);
+    fma_vec(o, d, by, o);
+    fma_vec(s, s, by, less);
+}
+
 template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
-__global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm_back(RowBackArgs p) {
-    constexpr int kTeams = TT < 256 ? 256 / TT : 1;
-    constexpr int kWarps = TT > 32 ? TT / 32 : 1;
+struct BackTeam {
+    static constexpr int kTeams = TT <= 32 ? 256 / TT : 1, kThreads = TT * kTeams;
+    using S = Slots<ST, VEC, NV, kThreads>;
+    using G = Slots<GT, VEC, NV, kThreads>;
+    using D = Slots<DT, VEC, NV, kThreads>;
+    static constexpr int kStageBytes = S::kAll + G::kAll + D::kAll;
+    // rows on their way: as many as leave room for a second CTA or, where a row is long, fit one
+    static constexpr int kStages = kStageBytes * 4 <= 100 * 1024 ? 4 : (kStageBytes * 2 <= 200 * 1024 ? 2 : 1);
+    static constexpr int kShared = kStages * kStageBytes;
+    // CTAs of a multiprocessor: by shared memory, and 768 threads of 80 registers
+    static constexpr int kFit = (220 * 1024) / (kShared + 3 * 1024);
+    static constexpr int kWant = 768 / kThreads > 0 ? 768 / kThreads : 1;
+    static constexpr int kCtas = kFit < 1 ? 1 : (kFit < kWant ? kFit : kWant);
+};
+
+template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
+__global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, BackTeam<ST, GT, DT, VEC, TT, NV>::kCtas)
+    row_norm_back(RowBackArgs p) {
+    using B = BackTeam<ST, GT, DT, VEC, TT, NV>;
+    constexpr int kTeams = B::kTeams, kStages = B::kStages, kWarps = TT > 32 ? TT / 32 : 1;
+    extern __shared__ __align__(16) char s_rows[];
     __shared__ float s_sum[2][3 * kWarps];
     const int t = threadIdx.x % TT, team = threadIdx.x / TT;
     const int cols = static_cast<int>(p.f);
     const float per = 1.f / static_cast<float>(p.f);
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams + team, step = static_cast<int64_t>(gridDim.x) * kTeams;
+
+    const auto copy = [&](int64_t round) {
+        const int64_t row = first + round * step;
+        if (row < p.n) {
+            char *stage = s_rows + (kStages == 1 ? 0 : (round % kStages) * B::kStageBytes);
+            const typename B::S s(stage);
+            const typename B::G g(stage + B::S::kAll);
+            const typename B::D d(stage + B::S::kAll + B::G::kAll);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * TT) * VEC;
+                if (c < cols) {
+                    s.copy(i, static_cast<const ST *>(p.s) + row * p.f + c);
+                    g.copy(i, static_cast<const GT *>(p.g) + row * p.f + c);
+                    if (p.skip) d.copy(i, static_cast<const DT *>(p.skip) + row * p.f + c);
+                }
+            }
+        }
+        copies_commit();
+    };
     float gg[NV][VEC] = {}, gb[NV][VEC] = {};
-    int parity = 0;
-    // every team of a CTA takes part in every round: the exchanges are by whole warps
-    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams; row0 < p.n; row0 += static_cast<int64_t>(gridDim.x) * kTeams) {
-        const bool live = row0 + team < p.n;
-        const int64_t row = live ? row0 + team : p.n - 1;
-        const float m = __ldg(p.mean + row), r = __ldg(p.rstd + row);
-        float s[NV][VEC], g[NV][VEC], sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * TT) * VEC;
-            if (live && c < cols) {
-                VecLoad<ST, VEC>::load(static_cast<const ST *>(p.s) + row * p.f + c, s[i]);
-                VecLoad<GT, VEC>::load(static_cast<const GT *>(p.g) + row * p.f + c, g[i]);
+    for (int k = 0; k + 1 < kStages; ++k) copy(k);
+    float m = 0.f, r = 0.f;
+    if (first < p.n) {
+        m = __ldg(p.mean + first);
+        r = __ldg(p.rstd + first);
+    }
+    const int64_t rounds = (p.n - static_cast<int64_t>(blockIdx.x) * kTeams + step - 1) / step;   // of the CTA: exchanges are by whole warps
+#pragma unroll 1
+    for (int64_t round = 0; round < rounds; ++round) {
+        copy(round + kStages - 1);
+        const int64_t row = first + round * step;
+        const bool live = row < p.n;
+        float next_m = 0.f, next_r = 0.f;
+        if (row + step < p.n) {
+            next_m = __ldg(p.mean + row + step);
+            next_r = __ldg(p.rstd + row + step);
+        }
+        char *stage = s_rows + (kStages == 1 ? 0 : (round % kStages) * B::kStageBytes);
+        const typename B::S s_at(stage);
+        const typename B::G g_at(stage + B::S::kAll);
+        const typename B::D d_at(stage + B::S::kAll + B::G::kAll);
+        copies_wait<kStages - 1>();
+        float sum[3] = {0.f, 0.f, 0.f};
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * TT) * VEC;
+                if (c < cols) {
+                    float s[VEC], g[VEC], w[VEC];
+                    s_at.widen(i, s);
+                    g_at.widen(i, g);
+                    row_weights(p.gamma, c, 1.f, w);
+                    row_terms<VEC>(s, g, w, m, sum);
+                }
             }
         }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * TT) * VEC;
-            if (live && c < cols) {
-                float w[VEC];
-                row_weights(p.gamma, c, 1.f, w);
-                row_terms<VEC>(s[i], g[i], w, m, r, sum);
-            }
-        }
-        team_sums<TT, 3>(sum, s_sum[parity]);
-        parity ^= 1;
+        team_sums<TT, 3>(sum, s_sum[round & 1]);
         const RowMeans a(sum, r, per);
-        if (!live) continue;
+        if (live) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * TT) * VEC;
-            if (c < cols) {
-                float w[VEC], o[VEC];
-                row_weights(p.gamma, c, 1.f, w);
-                if (p.skip) {
-                    load_row<VEC>(static_cast<const DT *>(p.skip) + row * p.f + c, o);
-                } else {
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * TT) * VEC;
+                if (c < cols) {
+                    float s[VEC], g[VEC], w[VEC], o[VEC];
+                    s_at.widen(i, s);
+                    g_at.widen(i, g);
+                    row_weights(p.gamma, c, 1.f, w);
+                    if (p.skip) {
+                        d_at.widen(i, o);
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < VEC; ++q) o[q] = 0.f;
+                        for (int q = 0; q < VEC; ++q) o[q] = 0.f;
+                    }
+                    row_gradient<VEC>(s, g, w, m, r, a, o);
+                    fma_vec(gg[i], g, s, gg[i]);
+                    add_vec(gb[i], g);
+                    store_vec<VEC>(static_cast<DT *>(p.grad_s) + row * p.f + c, o);
                 }
-#pragma unroll
-                for (int q = 0; q < VEC; ++q) {
-                    const float h = fmaf(s[i][q] - m, r, -a.e);
-                    gg[i][q] = fmaf(g[i][q], h, gg[i][q]);
-                    gb[i][q] += g[i][q];
-                    o[q] = fmaf(fmaf(-h, a.dh, g[i][q] * w[q] - a.d), r, o[q]);
-                }
-                store_vec<VEC>(static_cast<DT *>(p.grad_s) + row * p.f + c, o);
             }
         }
+        m = next_m;
+        r = next_r;
     }
     if (!p.part) return;
-    // the teams' sums, one team after the other
+    // the teams' sums: those of a warp by exchanges, then one warp after the other
     float *part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.f;
     if constexpr (kTeams == 1) {
 #pragma unroll
@@ -134,8 +225,17 @@ __global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm_back(RowBackArgs
     } else {
         constexpr int kCols = TT * NV * VEC;
         __shared__ float s_cols[2 * kCols];
-        for (int j = 0; j < kTeams; ++j) {
-            if (team == j) {
+#pragma unroll
+        for (int o = TT; o < 32; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int q = 0; q < VEC; ++q) {
+                    gg[i][q] += lane_xor(gg[i][q], o);
+                    gb[i][q] += lane_xor(gb[i][q], o);
+                }
+        for (int j = 0; j < B::kThreads / 32; ++j) {
+            if (static_cast<int>(threadIdx.x) / 32 == j && (threadIdx.x & 31) < TT) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -147,7 +247,7 @@ __global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm_back(RowBackArgs
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < cols; c += 256) {
+        for (int c = threadIdx.x; c < cols; c += B::kThreads) {
             const int v = c / VEC, at = ((v / TT) * VEC + c % VEC) * TT + v % TT;
             part[c] = s_cols[at];
             part[p.f + c] = s_cols[kCols + at];
@@ -168,7 +268,7 @@ __global__ void __launch_bounds__(1024) row_norm_back_long(RowBackArgs p) {
         VecLoad<ST, VEC>::load(static_cast<const ST *>(p.s) + at0 + c, s);
         VecLoad<GT, VEC>::load(static_cast<const GT *>(p.g) + at0 + c, g);
         row_weights(p.gamma, c, 1.f, w);
-        row_terms<VEC>(s, g, w, m, r, part);
+        row_terms<VEC>(s, g, w, m, part);
 #pragma unroll
         for (int k = 0; k < 3; ++k) sum[k] += part[k];
     }
@@ -186,11 +286,7 @@ __global__ void __launch_bounds__(1024) row_norm_back_long(RowBackArgs p) {
 #pragma unroll
             for (int q = 0; q < VEC; ++q) o[q] = 0.f;
         }
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            const float h = fmaf(s[q] - m, r, -a.e);
-            o[q] = fmaf(fmaf(-h, a.dh, g[q] * w[q] - a.d), r, o[q]);
-        }
+        row_gradient<VEC>(s, g, w, m, r, a, o);
         store_vec<VEC>(static_cast<DT *>(p.grad_s) + at0 + c, o);
     }
 }
@@ -214,29 +310,50 @@ __global__ void __launch_bounds__(256) long_columns(RowBackArgs p) {
     part[p.f + c] = gb;
 }
 
-}  // namespace
-
-// The geometry of the first kernel, for the workspace and the launch.
-constexpr int kBackVecs8 = 4, kBackVecs1 = 8;               // vectors that a thread holds, of 8 values, of fewer
-inline int back_held(int vec) { return vec == 8 ? kBackVecs8 : kBackVecs1; }
-inline bool back_long(int64_t f, int vec) { return (f + vec - 1) / vec > 256 * back_held(vec); }
-
-namespace {
-
+// Threads and vectors by the width: 8 values a thread, from 4,096 columns on up to 32, so that
+// a row's sums cost few barriers and many rows are on a multiprocessor (131,072 rows of 1,024:
+// a warp with 32 values a thread 599 us, 128 threads with 8 see layer_norm_backward.cu).
+template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
+cudaError_t launch_back_team(const RowBackArgs &p, cudaStream_t s) {
+    using B = BackTeam<ST, GT, DT, VEC, TT, NV>;
+    auto *kernel = row_norm_back<ST, GT, DT, VEC, TT, NV>;
+    if constexpr (B::kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, B::kShared);
+        if (e != cudaSuccess) return e;
+    }
+    RowBackArgs q = p;
+    q.ctas = back_ctas(p.n, B::kTeams, B::kCtas);
+    kernel<<<q.ctas, B::kThreads, B::kShared, s>>>(q);
+    const cudaError_t e = cudaGetLastError();
+    return e != cudaSuccess || !p.part ? e : join_columns(q.part, q.ctas, q.f, q.grad_gamma, q.grad_beta, s);
+}
 template <typename ST, typename GT, typename DT, int VEC>
 cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
-    constexpr int kHeld = VEC == 8 ? kBackVecs8 : kBackVecs1;
-    const int64_t vecs = (p.f + VEC - 1) / VEC;
-    if (vecs <= 8) row_norm_back<ST, GT, DT, VEC, 8, 1><<<p.ctas, 256, 0, s>>>(p);
-    else if (vecs <= 32) row_norm_back<ST, GT, DT, VEC, 32, 1><<<p.ctas, 256, 0, s>>>(p);
-    else if (vecs <= 32 * kHeld) row_norm_back<ST, GT, DT, VEC, 32, kHeld><<<p.ctas, 256, 0, s>>>(p);
-    else if (vecs <= 256 * kHeld) row_norm_back<ST, GT, DT, VEC, 256, kHeld><<<p.ctas, 256, 0, s>>>(p);
-    else {
-        row_norm_back_long<ST, GT, DT, VEC><<<static_cast<unsigned>(p.n), 1024, 0, s>>>(p);
-        if (p.part) {
-            const dim3 grid(static_cast<unsigned>((p.f + 255) / 256), p.ctas);
-            long_columns<ST, GT><<<grid, 256, 0, s>>>(p);
-        }
+    if constexpr (VEC == 8) {
+        if (p.f <= 64) return launch_back_team<ST, GT, DT, 8, 8, 1>(p, s);
+        if (p.f <= 256) return launch_back_team<ST, GT, DT, 8, 32, 1>(p, s);
+        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 8, 128, 1>(p, s);
+        if (p.f <= 2048) return launch_back_team<ST, GT, DT, 8, 256, 1>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 8, 512, 1>(p, s);
+        if (p.f <= 8192) return launch_back_team<ST, GT, DT, 8, 512, 2>(p, s);
+        if (p.f <= 16384) return launch_back_team<ST, GT, DT, 8, 512, 4>(p, s);
+    } else if constexpr (VEC == 4) {
+        if (p.f <= 64) return launch_back_team<ST, GT, DT, 4, 8, 2>(p, s);
+        if (p.f <= 256) return launch_back_team<ST, GT, DT, 4, 32, 2>(p, s);
+        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 4, 128, 2>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 4, 512, 2>(p, s);
+        if (p.f <= 8192) return launch_back_team<ST, GT, DT, 4, 512, 4>(p, s);
+    } else {
+        if (p.f <= 128) return launch_back_team<ST, GT, DT, 1, 32, 4>(p, s);
+        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 1, 128, 8>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 1, 512, 8>(p, s);
+    }
+    row_norm_back_long<ST, GT, DT, VEC><<<static_cast<unsigned>(p.n), 1024, 0, s>>>(p);
+    if (p.part) {
+        const int ctas = back_ctas(p.n, 1, 2);
+        long_columns<ST, GT><<<dim3(static_cast<unsigned>((p.f + 255) / 256), ctas), 256, 0, s>>>(p);
+        const cudaError_t e = cudaGetLastError();
+        return e != cudaSuccess ? e : join_columns(p.part, ctas, p.f, p.grad_gamma, p.grad_beta, s);
     }
     return cudaGetLastError();
 }

@@ -130,6 +130,39 @@ __device__ __forceinline__ void copy_async(void *shared, const void *global) {
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
+// Inputs of a CTA of THREADS in shared memory: every thread copies its own vectors and reads them back, so
+// that copies are in flight while others are worked on, without registers and without a
+// barrier.  A vector of 32 bytes lies in two halves, so that lanes side by side read 16 bytes
+// side by side.  EACH vectors a thread take kAll bytes of a CTA.
+template <typename T, int VEC, int EACH, int THREADS>
+struct Slots {
+    static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
+    static constexpr int kPart = kBytes > 16 ? 16 : kBytes, kParts = kBytes / kPart;
+    static constexpr int kAll = (EACH * kBytes * THREADS + 15) / 16 * 16;
+    char *at;
+    __device__ __forceinline__ explicit Slots(char *stage) : at(stage + threadIdx.x * kPart) {}
+    __device__ __forceinline__ void copy(int j, const T *from) const {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h)
+            copy_async<kPart>(at + (j * kParts + h) * THREADS * kPart, reinterpret_cast<const char *>(from) + h * kPart);
+    }
+    __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
+        if constexpr (kParts == 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 q = *reinterpret_cast<const float4 *>(at + (j * 2 + h) * THREADS * kPart);
+                v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
+            }
+        } else {
+            VecLoad<T, VEC>::widen(load_plain<T, VEC>(reinterpret_cast<const T *>(at + j * THREADS * kPart)), v);
+        }
+    }
+};
+// The copies issued since the last commit make a group; wait until at most LEFT groups are under way.
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
 // VEC values to p (fp32, or bf16 bits), p aligned to the vector it is stored as: 16 bytes,
 // or 8 for four bf16 values.  The one rounding of a bf16 result is here.
 // Eight fp32 values go out as one 32-byte store where p allows it: as two, every lane's half

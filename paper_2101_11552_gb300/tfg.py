@@ -976,7 +976,7 @@ def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, o
     out = _need_out("out", out, x.shape, out_dtype, x)
     mean = rstd = None
     if want_stats:
-        mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device)
+        mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
     _run(index, "tfg_layer_norm", x.data_ptr(), code, _at(residual), sum_code, _at(sum_out), n, f, _at(gamma), _at(beta), eps,
          out.data_ptr(), out_code, _at(mean), _at(rstd))
     return LayerNorm(out, x if residual is None else sum_out, mean, rstd)
@@ -1016,7 +1016,7 @@ def tfg_layer_norm_backward(sum, gamma, mean, rstd, grad_out, grad_sum=None, gra
     grad_gamma = grad_beta = None
     need = 0
     if want_weight_grads:
-        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=sum.device)
+        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=sum.device).unbind(0)
         need = tfg_layer_norm_backward_workspace_size(n, f)
     workspace = _workspace(workspace, need, sum)
     _run(index, "tfg_layer_norm_backward", sum.data_ptr(), code, n, f, _at(gamma), mean.data_ptr(), rstd.data_ptr(),
