@@ -72,7 +72,8 @@ struct alignas(16) TileRows {
     uint32_t end[kTileRows / 32];         // ends it,
     uint32_t in[kTileRows / 32];          // lies inside one
     int32_t lo, hi;                       // of the first and the last row
-    uint32_t any;                         // kAnyBegin, kAnyEnd: one of the rows does
+    uint8_t begin_warps[kTileRows / 32];  // two bits each: a row of the even, the odd warp begins a sequence,
+    uint8_t cut_warps[kTileRows / 32];    // begins or ends one
 };
 
 // Bytes of a call that links tiles: counter, maps and states (ones beforehand), plan.
@@ -91,13 +92,9 @@ struct ScanSpace {
     }
 };
 
-bool scan_vectors(const ScanArgs &p, int dtype, bool backward);
-void scan_geometry(ScanArgs &p, int dtype, bool vectors, void *ws, int32_t *status);
-cudaError_t scan_plan(const ScanArgs &p, void *ws, cudaStream_t s);
 
 namespace {
 
-constexpr uint32_t kAnyBegin = 1, kAnyEnd = 2;
 constexpr uint64_t kNoMap = ~uint64_t(0);
 constexpr uint32_t kNoState = ~uint32_t(0);
 constexpr int kWaitLimit = 1 << 21;                          // looks at a word, a second or more
@@ -161,13 +158,12 @@ __device__ __forceinline__ void decay_less_one(const float (&z)[VEC], float (&d)
     mul_vec(d, log2e);
 #pragma unroll
     for (int q = 0; q < VEC; ++q) d[q] = exp2_of(d[q]);
+    const float minus_one[1] = {-1.f};
     if constexpr (KIND == TFG_GATE_SIGMOID) {
-        const float one[1] = {1.f};
-        add_vec(d, one);
+        fma_vec(d, d, minus_one, minus_one);
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d[q]) : "f"(-d[q]));
+        for (int q = 0; q < VEC; ++q) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d[q]) : "f"(d[q]));
     } else {
-        const float minus_one[1] = {-1.f};
         add_vec(d, minus_one);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) d[q] = fabsf(z[q]) <= 0.35f ? expm1_near(z[q]) : d[q];
@@ -190,31 +186,16 @@ template <int PER>
 __device__ __forceinline__ uint32_t row_bits(const uint32_t *bits, int group) {
     return (bits[group * PER / 32] >> (group * PER % 32)) & ((1u << PER) - 1u);
 }
-// Whether a bit is set before, or from, row r on.
-__device__ __forceinline__ bool any_before(const uint32_t *bits, int r) {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < kTileRows / 32; ++i) {
-        const int left = r - i * 32;
-        any |= left > 0 && (bits[i] & (left >= 32 ? kAllLanes : (1u << left) - 1u)) != 0u;
-    }
-    return any;
+// The bits of begin_warps and cut_warps as one word, and a warp's place in it.
+__device__ __forceinline__ uint32_t warps_word(const uint8_t (&w)[kTileRows / 32]) {
+    static_assert(kTileRows / 32 == 4, "four bytes");
+    return *reinterpret_cast<const uint32_t *>(w);
 }
-__device__ __forceinline__ bool any_from(const uint32_t *bits, int r) {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < kTileRows / 32; ++i) {
-        const int skip = r - i * 32;
-        any |= skip < 32 && (skip <= 0 ? bits[i] : bits[i] >> skip) != 0u;
-    }
-    return any;
-}
-__device__ __forceinline__ bool row_bit(const uint32_t *bits, int r) { return (bits[r / 32] >> (r % 32)) & 1u; }
+__host__ __device__ constexpr int warp_bit(int warp) { return warp / 2 * 8 + warp % 2; }
 
 // Row r of a tile whose sequences lie in [lo, hi], by a warp for its 32 rows: word is the tile's
-// word of bits that they fill.  Whatever the offsets say, seq lies in [0, seqs).  Returns TileRows::any of
-// these rows.
-__device__ __forceinline__ uint32_t describe_row(const ScanArgs &p, int64_t r, int lo, int hi, int word, TileRows &t) {
+// word of bits that they fill.  Whatever the offsets say, seq lies in [0, seqs).
+__device__ __forceinline__ void describe_row(const ScanArgs &p, int64_t r, int lo, int hi, int word, TileRows &t) {
     while (lo < hi) {
         const int mid = lo + (hi - lo + 1) / 2;
         if (__ldg(p.offsets + mid) <= r) lo = mid;
@@ -234,8 +215,9 @@ __device__ __forceinline__ uint32_t describe_row(const ScanArgs &p, int64_t r, i
         t.begin[word] = bb;
         t.end[word] = eb;
         t.in[word] = ib;
+        t.begin_warps[word] = static_cast<uint8_t>(((bb & 0xffffu) ? 1 : 0) | ((bb >> 16) ? 2 : 0));
+        t.cut_warps[word] = static_cast<uint8_t>((((bb | eb) & 0xffffu) ? 1 : 0) | (((bb | eb) >> 16) ? 2 : 0));
     }
-    return (bb ? kAnyBegin : 0u) | (eb ? kAnyEnd : 0u);
 }
 
 // The rows of the one tile of a call by a whole CTA; ends with a barrier.
@@ -300,12 +282,16 @@ __device__ __forceinline__ void copy_plan(const ScanArgs &p, int64_t tile, TileR
 struct Job {
     int64_t order;
     int strip;
-    __device__ __forceinline__ Job(const ScanArgs &p, int64_t job) : order(job / p.strips), strip(static_cast<int>(job - order * p.strips)) {}
+    __device__ __forceinline__ Job(const ScanArgs &p, uint32_t job) {
+        const uint32_t o = job / static_cast<uint32_t>(p.strips);
+        order = o;
+        strip = static_cast<int>(job - o * p.strips);
+    }
 };
 
 // The job of this CTA; with a barrier where tiles are handed out.
 __device__ __forceinline__ Job next_job(const ScanArgs &p, uint32_t *s_next) {
-    if (!p.linked) return Job(p, static_cast<int64_t>(blockIdx.x) - p.checkers);
+    if (!p.linked) return Job(p, blockIdx.x - p.checkers);
     if (threadIdx.x == 0) *s_next = atomicAdd(p.next, 1u);
     __syncthreads();
     return Job(p, *s_next);
@@ -313,61 +299,105 @@ __device__ __forceinline__ Job next_job(const ScanArgs &p, uint32_t *s_next) {
 
 // The last tile before this one in its window, in order of work, that lets nothing through, by its place
 // in the window, -1 if there is none; by a whole warp.
-__device__ __forceinline__ int cut_before(const ScanArgs &p, int64_t order, uint32_t which, bool from_last) {
+template <bool UP>
+__device__ __forceinline__ int cut_before(const ScanArgs &p, int64_t order) {
     const int place = static_cast<int>(order % kWindow), lane = threadIdx.x & 31;
-    uint32_t any = 0;
+    uint32_t cut = 0;
     if (lane < place) {
         const int64_t other = order - place + lane;
-        any = __ldg(&p.plan[from_last ? p.tiles - 1 - other : other].any) & which;
+        const TileRows &t = p.plan[UP ? p.tiles - 1 - other : other];
+        cut = __ldg(reinterpret_cast<const uint32_t *>(UP ? t.cut_warps : t.begin_warps));
     }
-    return 31 - __clz(static_cast<int>(lane_ballot(any != 0u)));
+    return 31 - __clz(static_cast<int>(lane_ballot(cut != 0u)));
 }
 
-// Maps of a warp's groups of rows, scanned across the lanes: on return (a, b) is the map of the
-// rows of the groups before this one (towards FROM_TOP's end), `fresh` whether one of them cuts off
-// what enters; the whole warp's map is left by the last group for the warps' scan.
+// The state of a sequence, zeros without states.
+template <int VEC>
+__device__ __forceinline__ void state_or_zero(const float *states, int64_t seq, int64_t f, int64_t c, float (&v)[VEC]) {
+    if (states) {
+        VecLoad<float, VEC>::load(states + seq * f + c, v);
+    } else {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) v[q] = 0.f;
+    }
+}
+
+// Maps of a warp's groups of rows, composed across the lanes from where values enter (the first
+// row; UP: the last): on return (a, b) is the map of the groups up to this one, `fresh` whether
+// one of them cuts off what enters; the last group leaves the whole warp's map.
 template <int VEC, bool UP>
-__device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], uint32_t &fresh, int warp, int lane,
+__device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bool &fresh, int warp, int lane,
                                             float (*s_a)[ScanTile<VEC>::kWide], float (*s_b)[ScanTile<VEC>::kWide]) {
     constexpr int kAcross = ScanTile<VEC>::kAcross;
     const int l = threadIdx.x & 31;
 #pragma unroll
     for (int o = kAcross; o < 32; o <<= 1) {
-        const int from = UP ? l + o : l - o;                 // the neighbour nearer to where values enter
-        const bool has = UP ? from < 32 : from >= 0;
-        const uint32_t other = lane_get(fresh, from & 31);
+        const int from = (UP ? l + o : l - o) & 31;          // the neighbour nearer to where values enter
+        const bool has = UP ? l + o < 32 : l >= o, joins = has && !fresh;
+        const uint32_t other = lane_ballot(fresh) >> from & 1u;
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            const float pa = lane_get(a[q], from & 31), pb = lane_get(b[q], from & 31);
-            if (has && !fresh) {
+            const float pa = lane_get(a[q], from), pb = lane_get(b[q], from);
+            if (joins) {
                 b[q] = fmaf(a[q], pb, b[q]);
-                a[q] = other ? 0.f : a[q] * pa;
+                a[q] *= pa;                                  // not looked at behind a cut
             }
         }
-        if (has) fresh |= other;
+        fresh = fresh || (has && other);
     }
     if (UP ? l < kAcross : l >= 32 - kAcross) {
+        if constexpr (VEC % 4 == 0) {
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            s_a[warp][lane * VEC + q] = a[q];
-            s_b[warp][lane * VEC + q] = b[q];
+            for (int q = 0; q < VEC; q += 4) {
+                *reinterpret_cast<float4 *>(&s_a[warp][lane * VEC + q]) = make_float4(a[q], a[q + 1], a[q + 2], a[q + 3]);
+                *reinterpret_cast<float4 *>(&s_b[warp][lane * VEC + q]) = make_float4(b[q], b[q + 1], b[q + 2], b[q + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) {
+                s_a[warp][lane * VEC + q] = a[q];
+                s_b[warp][lane * VEC + q] = b[q];
+            }
         }
     }
-    if constexpr (kAcross == 32) {
-        fresh = 0;
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) a[q] = 1.f, b[q] = 0.f;
-    } else {
-        const int from = UP ? l + kAcross : l - kAcross;
-        const bool has = UP ? from < 32 : from >= 0;
-        const uint32_t other = lane_get(fresh, from & 31);
-        fresh = has ? other : 0u;
+}
+
+// What enters the thread's rows, into v: at the warp's first group what enters the warp (v), else what leaves
+// the group before, by the map (a, b) up to it.  By whole warps.
+template <int VEC, bool UP>
+__device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (&b)[VEC], bool fresh, float (&v)[VEC]) {
+    constexpr int kAcross = ScanTile<VEC>::kAcross;
+    if constexpr (kAcross < 32) {
+        const int l = threadIdx.x & 31, from = (UP ? l + kAcross : l - kAcross) & 31;
+        const bool has = UP ? l + kAcross < 32 : l >= kAcross;
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            const float pa = lane_get(a[q], from & 31), pb = lane_get(b[q], from & 31);
-            a[q] = has ? pa : 1.f;
-            b[q] = has ? pb : 0.f;
+            const float leaves = lane_get(fresh ? b[q] : fmaf(a[q], v[q], b[q]), from);
+            if (has) v[q] = leaves;
         }
+    }
+}
+
+// The thread's rows as one map.  PLAIN: they lie in a sequence that neither begins nor ends there.
+template <bool PLAIN, int KIND, int VEC, int EACH, typename In>
+__device__ __forceinline__ void compose_down(const ScanArgs &p, const In &x, const float (&d)[EACH][VEC], const float *initial,
+                                             const int32_t *seq, int64_t c, uint32_t begin, uint32_t in, float (&a)[VEC],
+                                             float (&b)[VEC]) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) a[q] = 1.f, b[q] = 0.f;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        if (!PLAIN && !((in >> j) & 1u)) continue;
+        if (!PLAIN && ((begin >> j) & 1u)) {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) a[q] = 0.f;
+            state_or_zero(initial, seq[j], p.f, c, b);
+        }
+        float v[VEC];
+        x.widen(j, v);
+        fma_vec(a, d[j], a, a);
+        fma_vec(b, d[j], b, b);
+        add_input<KIND>(b, d[j], v);
     }
 }
 
@@ -422,16 +452,6 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
     if (mine && place == kWindow - 1 && order + 1 < p.tiles)
         st_word(p.states + (window + 1) * p.f + c, state_word(fresh ? b : fmaf(a, state, b)));
     return state;
-}
-
-template <int VEC>
-__device__ __forceinline__ void state_or_zero(const float *states, int64_t seq, int64_t f, int64_t c, float (&v)[VEC]) {
-    if (states) {
-        VecLoad<float, VEC>::load(states + seq * f + c, v);
-    } else {
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) v[q] = 0.f;
-    }
 }
 
 }  // namespace

@@ -1,0 +1,246 @@
+// Gated linear recurrence, backward: the kernel (gated_recurrence.cuh: the method).  A translation unit for
+// each type of the inputs compiles it.
+//
+//   l_t = g_t + a_{t+1} l_{t+1} (behind a sequence's last row: dL/dfinal)
+//   sigmoid gate: dL/dz = l (v_{t-1} - x) a (1 - a), dL/dx = l (1 - a)
+//   exp gate:     dL/dz = l v_{t-1} a,              dL/dx = l
+//   dL/dinitial = a l of the sequence's first row
+//
+// The adjoint is a recurrence of the same form from the last row to the first, so tiles are
+// worked on from the last to the first.  What passes from row t to t - 1 is c = a_t l_t.  The states v
+// are made again, in fp32 as the forward had them, from the state that entered the tile, which the forward
+// keeps: one value for 128 rows in place of a read of all states, and no rounding of a
+// state stored in bf16 reaches a gradient.
+#pragma once
+
+#include "gated_recurrence.cuh"
+
+namespace tfg {
+namespace {
+
+template <typename XT, typename GT, int VEC>
+struct BackwardStage {
+    using T = ScanTile<VEC>;
+    using In = Slots<XT, VEC, T::kEach, kScanThreads>;
+    using Grad = Slots<GT, VEC, T::kEach, kScanThreads>;
+    static constexpr int kBytes = 2 * In::kAll + Grad::kAll;
+    In z, x;
+    Grad g;
+    __device__ __forceinline__ explicit BackwardStage(char *stage) : z(stage), x(stage + In::kAll), g(stage + 2 * In::kAll) {}
+    __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
+        const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
+        const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows + group * T::kEach;
+        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC;
+        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
+        const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
+        const GT *gp = static_cast<const GT *>(p.g) + r0 * p.f + c;
+#pragma unroll
+        for (int j = 0; j < T::kEach; ++j)
+            if (j < left) {
+                z.copy(j, zp + j * p.gate_ld);
+                x.copy(j, xp + j * p.x_ld);
+                if (p.g) g.copy(j, gp + j * p.f);
+                else g.zero(j);
+            }
+        if (p.linked) copy_plan(p, tile, rows);
+    }
+};
+
+constexpr int kBackwardCtas = 2;          // of a multiprocessor: 128 registers a thread
+
+// The thread's rows as one map of the adjoint, from the last to the first.
+template <bool PLAIN, int VEC, int EACH, typename Grad>
+__device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, const float (&d)[EACH][VEC], const float *grad_final,
+                                           const int32_t *seq, int64_t c, uint32_t begin, uint32_t end, uint32_t in,
+                                           float (&u)[VEC], float (&w)[VEC]) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) u[q] = 1.f, w[q] = 0.f;
+#pragma unroll
+    for (int j = EACH - 1; j >= 0; --j) {
+        if (!PLAIN && !((in >> j) & 1u)) continue;
+        if (!PLAIN && ((end >> j) & 1u)) {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) u[q] = 0.f;
+            state_or_zero(grad_final, seq[j], p.f, c, w);
+        }
+        float v[VEC];
+        g.widen(j, v);
+        add_vec(w, v);
+        fma_vec(u, d[j], u, u);
+        fma_vec(w, d[j], w, w);
+        if (!PLAIN && ((begin >> j) & 1u)) {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) u[q] = w[q] = 0.f;
+        }
+    }
+}
+
+// The gradients of the thread's rows from the state v that enters them and what enters their last, w.
+template <bool PLAIN, int KIND, typename XT, int VEC, int EACH, typename In, typename Grad>
+__device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, const Grad &g, const float (&d)[EACH][VEC],
+                                                const int32_t *seq, int64_t row, int64_t c, uint32_t begin, uint32_t end,
+                                                uint32_t in, float (&v)[VEC], float (&w)[VEC]) {
+    float before[EACH][VEC];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        if (!PLAIN && ((begin >> j) & 1u)) state_or_zero(p.initial, seq[j], p.f, c, v);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) before[j][q] = v[q];
+        if (j + 1 < EACH) {
+            float xv[VEC];
+            x.widen(j, xv);
+            fma_vec(v, d[j], v, v);
+            add_input<KIND>(v, d[j], xv);
+        }
+    }
+    XT *gate = static_cast<XT *>(p.grad_gate) + row * p.grad_gate_ld + c, *input = static_cast<XT *>(p.grad_x) + row * p.grad_x_ld + c;
+#pragma unroll
+    for (int j = EACH - 1; j >= 0; --j) {
+        if (!PLAIN && !((in >> j) & 1u)) continue;
+        if (!PLAIN && ((end >> j) & 1u)) state_or_zero(p.grad_final, seq[j], p.f, c, w);
+        float gz[VEC], gx[VEC];
+        g.widen(j, gx);
+        add_vec(w, gx);                                      // l
+        x.widen(j, gx);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+            const float less = -d[j][q];                     // 1 - a
+            if constexpr (KIND == TFG_GATE_SIGMOID) {
+                gz[q] = w[q] * (before[j][q] - gx[q]) * fmaf(less, d[j][q], less);
+                gx[q] = w[q] * less;
+            } else {
+                gz[q] = w[q] * (before[j][q] * (1.f + d[j][q]));
+                gx[q] = w[q];
+            }
+        }
+        store_vec<VEC>(gate + j * p.grad_gate_ld, gz);
+        store_vec<VEC>(input + j * p.grad_x_ld, gx);
+        fma_vec(w, d[j], w, w);
+        if (!PLAIN && ((begin >> j) & 1u)) {
+            if (p.grad_initial) store_vec<VEC>(p.grad_initial + seq[j] * p.f + c, w);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) w[q] = 0.f;
+        }
+    }
+}
+
+template <typename XT, typename GT, int VEC, int KIND>
+__global__ void __launch_bounds__(kScanThreads, kBackwardCtas) scan_backward(ScanArgs p) {
+    using T = ScanTile<VEC>;
+    using Stage = BackwardStage<XT, GT, VEC>;
+    extern __shared__ __align__(16) char s_stage[];
+    __shared__ TileRows rows;
+    __shared__ __align__(16) float s_a[kScanWarps][T::kWide], s_b[kScanWarps][T::kWide];      // of the states
+    __shared__ __align__(16) float s_u[kScanWarps][T::kWide], s_w[kScanWarps][T::kWide];      // of the adjoint
+    __shared__ float2 s_part[kScanThreads / T::kWide][T::kWide];
+    __shared__ float s_carry[T::kWide];
+    __shared__ uint32_t s_next;
+    __shared__ int s_from;
+    if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.grad_final, p.grad_initial);
+    const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
+    const Job job = next_job(p, &s_next);
+    const Stage in_stage(s_stage);
+    in_stage.copy(p, job, rows);
+    const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows;
+    const int64_t c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
+    const bool on = c < p.f, column = static_cast<int>(threadIdx.x) < T::kWide;
+    if (p.linked && warp == 0) {
+        const int from = cut_before<true>(p, job.order);
+        if (threadIdx.x == 0) s_from = from;
+    }
+    const int sc = static_cast<int>(threadIdx.x) - T::kWide;                     // threads of the next columns: states
+    float state = 0.f;
+    if (sc >= 0 && sc < T::kWide && c0 + sc < p.f) state = __ldg(p.entered + tile * p.f + c0 + sc);
+    copies_done();
+    if (p.linked) __syncthreads();                           // the plan is there
+    else find_rows(p, rows);
+    const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
+                   in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps),
+                   cut_warps = warps_word(rows.cut_warps);
+    const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
+    const int32_t *seq = rows.seq + group * T::kEach;
+
+    // the thread's maps: of the state down its rows, of the adjoint up
+    float d[T::kEach][VEC], a[VEC], b[VEC], u[VEC], w[VEC];
+#pragma unroll
+    for (int j = 0; j < T::kEach; ++j) {
+        float v[VEC];
+        in_stage.z.widen(j, v);
+        decay_less_one<KIND>(v, d[j]);
+    }
+    if (plain) {
+        compose_down<true, KIND>(p, in_stage.x, d, nullptr, seq, c, begin, in, a, b);
+        compose_up<true>(p, in_stage.g, d, nullptr, seq, c, begin, end, in, u, w);
+    } else {
+        compose_down<false, KIND>(p, in_stage.x, d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+        compose_up<false>(p, in_stage.g, d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
+    }
+    bool cut = begin != 0u, cut_up = (begin | end) != 0u;
+    scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
+    scan_groups<VEC, true>(u, w, cut_up, warp, lane, s_u, s_w);
+    __syncthreads();
+
+    // threads of the first columns: up the warps; of the next: down them, from the state kept
+    float tu = 1.f, tw = 0.f;
+    if (column) {
+#pragma unroll
+        for (int i = kScanWarps - 1; i >= 0; --i) {
+            const float gu = s_u[i][threadIdx.x], gw = s_w[i][threadIdx.x];
+            s_u[i][threadIdx.x] = tu;
+            s_w[i][threadIdx.x] = tw;
+            const bool fresh = (cut_warps >> warp_bit(i)) & 1u;
+            tw = fresh ? gw : fmaf(gu, tw, gw);
+            tu = fresh ? 0.f : tu * gu;
+        }
+    } else if (sc < T::kWide) {
+#pragma unroll
+        for (int i = 0; i < kScanWarps; ++i) {
+            const float ga = s_a[i][sc], gb = s_b[i][sc];
+            s_b[i][sc] = state;
+            state = (begin_warps >> warp_bit(i)) & 1u ? gb : fmaf(ga, state, gb);
+        }
+    }
+    const bool wants = (rows.in[kTileRows / 32 - 1] & ~rows.end[kTileRows / 32 - 1]) >> 31;
+    const float carry = enter_tile<T::kWide>(p, job.order, c0, tu, tw, cut_warps != 0u, wants, s_from, s_part);
+    if (column) s_carry[threadIdx.x] = carry;
+    __syncthreads();
+
+    float v[VEC], l[VEC];
+    const bool far = cut_warps >> warp_bit(warp) >> 1 != 0u;                     // a warp behind this one is cut
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) {
+        const int i = lane * VEC + q;
+        v[q] = s_b[warp][i];
+        l[q] = far ? s_w[warp][i] : fmaf(s_u[warp][i], s_carry[i], s_w[warp][i]);
+    }
+    enter_group<VEC, false>(a, b, cut, v);
+    enter_group<VEC, true>(u, w, cut_up, l);
+    if (!on) return;
+    const int64_t row = r0 + group * T::kEach;
+    if (plain) write_gradients<true, KIND, XT>(p, in_stage.x, in_stage.g, d, seq, row, c, begin, end, in, v, l);
+    else write_gradients<false, KIND, XT>(p, in_stage.x, in_stage.g, d, seq, row, c, begin, end, in, v, l);
+}
+
+template <typename XT, typename GT, int VEC, int KIND>
+cudaError_t launch_backward(const ScanArgs &p, cudaStream_t s) {
+    constexpr int kShared = BackwardStage<XT, GT, VEC>::kBytes;
+    if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
+        const cudaError_t e =
+            cudaFuncSetAttribute(scan_backward<XT, GT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+        if (e != cudaSuccess) return e;
+    }
+    scan_backward<XT, GT, VEC, KIND><<<static_cast<unsigned>(p.checkers + p.tiles * p.strips), kScanThreads, kShared, s>>>(p);
+    return cudaGetLastError();
+}
+template <typename XT, typename GT, int VEC>
+cudaError_t launch_backward_kind(const ScanArgs &p, int kind, cudaStream_t s) {
+    return kind == TFG_GATE_SIGMOID ? launch_backward<XT, GT, VEC, TFG_GATE_SIGMOID>(p, s)
+                                    : launch_backward<XT, GT, VEC, TFG_GATE_EXP>(p, s);
+}
+template <typename XT, int VEC>
+cudaError_t launch_backward_grad(const ScanArgs &p, int kind, cudaStream_t s) {
+    return p.out_bf16 ? launch_backward_kind<XT, uint16_t, VEC>(p, kind, s) : launch_backward_kind<XT, float, VEC>(p, kind, s);
+}
+
+}  // namespace
+}  // namespace tfg

@@ -1,0 +1,150 @@
+// Gated linear recurrence, forward: the kernel (gated_recurrence.cuh: the method).  A translation unit
+// for each type of the inputs compiles it.
+#pragma once
+
+#include "gated_recurrence.cuh"
+
+namespace tfg {
+namespace {
+
+template <typename XT, int VEC>
+struct ForwardStage {
+    using T = ScanTile<VEC>;
+    using In = Slots<XT, VEC, T::kEach, kScanThreads>;
+    static constexpr int kBytes = 2 * In::kAll;
+    In z, x;
+    __device__ __forceinline__ explicit ForwardStage(char *stage) : z(stage), x(stage + In::kAll) {}
+    __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
+        const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
+        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC, r0 = job.order * kTileRows + group * T::kEach;
+        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
+        const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
+#pragma unroll
+        for (int j = 0; j < T::kEach; ++j)
+            if (j < left) {
+                z.copy(j, zp + j * p.gate_ld);
+                x.copy(j, xp + j * p.x_ld);
+            }
+        if (p.linked) copy_plan(p, job.order, rows);
+    }
+};
+
+// CTAs of a multiprocessor: three of 80 registers a thread where a thread has 8 channels.
+template <int VEC>
+constexpr int kForwardCtas = VEC == 8 ? 3 : 4;
+
+// The rows again, from the state v that enters the thread's first.
+template <bool PLAIN, int KIND, typename OT, int VEC, int EACH, typename In>
+__device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const float (&d)[EACH][VEC], const int32_t *seq,
+                                           int64_t c, uint32_t begin, uint32_t end, uint32_t in, OT *out, float (&v)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        if (!PLAIN && !((in >> j) & 1u)) continue;
+        if (!PLAIN && ((begin >> j) & 1u)) state_or_zero(p.initial, seq[j], p.f, c, v);
+        float w[VEC];
+        x.widen(j, w);
+        fma_vec(v, d[j], v, v);
+        add_input<KIND>(v, d[j], w);
+        store_vec<VEC>(out + j * p.f, v);
+        if (!PLAIN && ((end >> j) & 1u) && p.final_state) store_vec<VEC>(p.final_state + seq[j] * p.f + c, v);
+    }
+}
+
+template <typename XT, typename OT, int VEC, int KIND>
+__global__ void __launch_bounds__(kScanThreads, kForwardCtas<VEC>) scan_forward(ScanArgs p) {
+    using T = ScanTile<VEC>;
+    using Stage = ForwardStage<XT, VEC>;
+    extern __shared__ __align__(16) char s_stage[];
+    __shared__ TileRows rows;
+    __shared__ __align__(16) float s_a[kScanWarps][T::kWide], s_b[kScanWarps][T::kWide];
+    __shared__ float2 s_part[kScanThreads / T::kWide][T::kWide];
+    __shared__ float s_state[T::kWide];
+    __shared__ uint32_t s_next;
+    __shared__ int s_from;
+    if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.initial, p.final_state);
+    const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
+    const Job job = next_job(p, &s_next);
+    const Stage in_stage(s_stage);
+    in_stage.copy(p, job, rows);
+    const int64_t r0 = job.order * kTileRows, c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
+    const bool on = c < p.f;
+    if (p.linked && warp == 0) {
+        const int from = cut_before<false>(p, job.order);
+        if (threadIdx.x == 0) s_from = from;
+    }
+    copies_done();
+    if (p.linked) __syncthreads();                           // the plan is there
+    else find_rows(p, rows);
+    const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
+                   in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps);
+    const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
+    const int32_t *seq = rows.seq + group * T::kEach;
+
+    float d[T::kEach][VEC], a[VEC], b[VEC];
+#pragma unroll
+    for (int j = 0; j < T::kEach; ++j) {
+        float v[VEC];
+        in_stage.z.widen(j, v);
+        decay_less_one<KIND>(v, d[j]);
+    }
+    if (plain) compose_down<true, KIND>(p, in_stage.x, d, nullptr, seq, c, begin, in, a, b);
+    else compose_down<false, KIND>(p, in_stage.x, d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+    bool cut = begin != 0u;
+    scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
+    __syncthreads();
+
+    // down the warps, a thread for each channel: what stands before each, and the tile's map
+    const int64_t mc = c0 + threadIdx.x;
+    const bool column = static_cast<int>(threadIdx.x) < T::kWide;
+    float ta = 1.f, tb = 0.f;
+    if (column) {
+#pragma unroll
+        for (int w = 0; w < kScanWarps; ++w) {
+            const float wa = s_a[w][threadIdx.x], wb = s_b[w][threadIdx.x];
+            s_a[w][threadIdx.x] = ta;
+            s_b[w][threadIdx.x] = tb;
+            const bool fresh = (begin_warps >> warp_bit(w)) & 1u;
+            tb = fresh ? wb : fmaf(wa, tb, wb);              // not 0 times what may be an infinity
+            ta = fresh ? 0.f : ta * wa;
+        }
+    }
+    const bool wants = (rows.in[0] & ~rows.begin[0] & 1u) != 0u;
+    const float state = enter_tile<T::kWide>(p, job.order, c0, ta, tb, begin_warps != 0u, wants, s_from, s_part);
+    if (column) s_state[threadIdx.x] = state;
+    if (column && mc < p.f && p.entering) p.entering[job.order * p.f + mc] = state;
+    __syncthreads();
+
+    float v[VEC];
+    const bool far = (begin_warps & ((1u << warp_bit(warp)) - 1u)) != 0u;
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) {
+        const int i = lane * VEC + q;
+        v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
+    }
+    enter_group<VEC, false>(a, b, cut, v);
+    if (!on) return;
+    OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
+    if (plain) write_rows<true, KIND>(p, in_stage.x, d, seq, c, begin, end, in, out, v);
+    else write_rows<false, KIND>(p, in_stage.x, d, seq, c, begin, end, in, out, v);
+}
+
+template <typename XT, typename OT, int VEC, int KIND>
+cudaError_t launch_forward(const ScanArgs &p, cudaStream_t s) {
+    constexpr int kShared = ForwardStage<XT, VEC>::kBytes;
+    if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
+        const cudaError_t e =
+            cudaFuncSetAttribute(scan_forward<XT, OT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+        if (e != cudaSuccess) return e;
+    }
+    scan_forward<XT, OT, VEC, KIND><<<static_cast<unsigned>(p.checkers + p.tiles * p.strips), kScanThreads, kShared, s>>>(p);
+    return cudaGetLastError();
+}
+template <typename XT, int VEC>
+cudaError_t launch_forward_kind(const ScanArgs &p, int kind, cudaStream_t s) {
+    if (kind == TFG_GATE_SIGMOID)
+        return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_SIGMOID>(p, s) : launch_forward<XT, float, VEC, TFG_GATE_SIGMOID>(p, s);
+    return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_EXP>(p, s) : launch_forward<XT, float, VEC, TFG_GATE_EXP>(p, s);
+}
+
+}  // namespace
+}  // namespace tfg

@@ -1,0 +1,11 @@
+// The gated recurrence, forward, for bf16 inputs.
+#include "gated_recurrence_forward.cuh"
+
+namespace tfg {
+
+cudaError_t launch_scan_forward_bf16(const ScanArgs &p, int vec, int kind, cudaStream_t s) {
+    if (vec == 8) return launch_forward_kind<uint16_t, 8>(p, kind, s);
+    return launch_forward_kind<uint16_t, 1>(p, kind, s);
+}
+
+}  // namespace tfg

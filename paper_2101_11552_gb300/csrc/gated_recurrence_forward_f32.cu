@@ -1,0 +1,12 @@
+// The gated recurrence, forward, for f32 inputs.
+#include "gated_recurrence_forward.cuh"
+
+namespace tfg {
+
+cudaError_t launch_scan_forward_f32(const ScanArgs &p, int vec, int kind, cudaStream_t s) {
+    if (vec == 8) return launch_forward_kind<float, 8>(p, kind, s);
+    if (vec == 4) return launch_forward_kind<float, 4>(p, kind, s);
+    return launch_forward_kind<float, 1>(p, kind, s);
+}
+
+}  // namespace tfg

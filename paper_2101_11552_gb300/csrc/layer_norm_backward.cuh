@@ -103,6 +103,9 @@ struct BackTeam {
     using G = Slots<GT, VEC, NV, kThreads>;
     using D = Slots<DT, VEC, NV, kThreads>;
     static constexpr int kStageBytes = S::kAll + G::kAll + D::kAll;
+    // up to 16 values a thread are kept in registers from the sums to the gradient, more are read again
+    static constexpr bool kKeeps = NV * VEC <= 16;
+    static constexpr int kKept = kKeeps ? NV : 1;
     // rows on their way: as many as leave room for a second CTA or, where a row is long, fit one
     static constexpr int kStages = kStageBytes * 4 <= 100 * 1024 ? 4 : (kStageBytes * 2 <= 200 * 1024 ? 2 : 1);
     static constexpr int kShared = kStages * kStageBytes;
@@ -143,7 +146,12 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
         }
         copies_commit();
     };
-    float gg[NV][VEC] = {}, gb[NV][VEC] = {};
+    float gg[NV][VEC] = {}, gb[NV][VEC] = {}, w[B::kKept][VEC];
+    if constexpr (B::kKeeps) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((t + i * TT) * VEC < cols) row_weights(p.gamma, (t + i * TT) * VEC, 1.f, w[i]);
+    }
 #pragma unroll
     for (int k = 0; k + 1 < kStages; ++k) copy(k);
     float m = 0.f, r = 0.f;
@@ -168,16 +176,16 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
         const typename B::D d_at(stage + B::S::kAll + B::G::kAll);
         copies_wait<kStages - 1>();
         float sum[3] = {0.f, 0.f, 0.f};
+        float s[B::kKept][VEC], g[B::kKept][VEC];
         if (live) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * TT) * VEC;
+                const int c = (t + i * TT) * VEC, k = i % B::kKept;
                 if (c < cols) {
-                    float s[VEC], g[VEC], w[VEC];
-                    s_at.widen(i, s);
-                    g_at.widen(i, g);
-                    row_weights(p.gamma, c, 1.f, w);
-                    row_terms<VEC>(s, g, w, m, sum);
+                    s_at.widen(i, s[k]);
+                    g_at.widen(i, g[k]);
+                    if (!B::kKeeps) row_weights(p.gamma, c, 1.f, w[k]);
+                    row_terms<VEC>(s[k], g[k], w[k], m, sum);
                 }
             }
         }
@@ -186,21 +194,23 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
         if (live) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * TT) * VEC;
+                const int c = (t + i * TT) * VEC, k = i % B::kKept;
                 if (c < cols) {
-                    float s[VEC], g[VEC], w[VEC], o[VEC];
-                    s_at.widen(i, s);
-                    g_at.widen(i, g);
-                    row_weights(p.gamma, c, 1.f, w);
+                    float o[VEC];
+                    if (!B::kKeeps) {
+                        s_at.widen(i, s[k]);
+                        g_at.widen(i, g[k]);
+                        row_weights(p.gamma, c, 1.f, w[k]);
+                    }
                     if (p.skip) {
                         d_at.widen(i, o);
                     } else {
 #pragma unroll
                         for (int q = 0; q < VEC; ++q) o[q] = 0.f;
                     }
-                    row_gradient<VEC>(s, g, w, m, r, a, o);
-                    fma_vec(gg[i], g, s, gg[i]);
-                    add_vec(gb[i], g);
+                    row_gradient<VEC>(s[k], g[k], w[k], m, r, a, o);
+                    fma_vec(gg[i], g[k], s[k], gg[i]);
+                    add_vec(gb[i], g[k]);
                     store_vec<VEC>(static_cast<DT *>(p.grad_s) + row * p.f + c, o);
                 }
             }

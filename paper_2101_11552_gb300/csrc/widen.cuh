@@ -146,6 +146,11 @@ struct Slots {
         for (int h = 0; h < kParts; ++h)
             copy_async<kPart>(at + (j * kParts + h) * THREADS * kPart, reinterpret_cast<const char *>(from) + h * kPart);
     }
+    __device__ __forceinline__ void zero(int j) const {
+#pragma unroll
+        for (int i = 0; i < kParts * kPart / 2; ++i)
+            *reinterpret_cast<uint16_t *>(at + (j * kParts + i * 2 / kPart) * THREADS * kPart + i * 2 % kPart) = 0;
+    }
     __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
         if constexpr (kParts == 2) {
 #pragma unroll
