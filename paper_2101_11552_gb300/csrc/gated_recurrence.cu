@@ -28,14 +28,14 @@ int scan_vector(const ScanArgs &p, int dtype, bool backward) {
     const int size = dtype == TFG_BF16 ? 2 : 4;
     const auto at = [](const void *q, int bytes) { return reinterpret_cast<uintptr_t>(q) % bytes == 0; };
     const auto fits = [&](int vec) {
-        const int bytes = vec * size > 16 ? 16 : vec * size;
-        if (p.f % vec || p.gate_ld % vec || p.x_ld % vec || !at(p.gate, bytes) || !at(p.x, bytes) || !at(p.initial, 16)) return false;
+        if (p.f % vec || p.gate_ld % vec || p.x_ld % vec || !at(p.gate, 16) || !at(p.x, 16) || !at(p.initial, 16)) return false;
         const int wide = p.out_bf16 ? vec * 2 : 16;          // bytes of a vector of out or its gradient
         if (!backward) return at(p.out, wide) && at(p.final_state, 16);
         return at(p.g, wide) && at(p.grad_final, 16) && at(p.grad_initial, 16) && p.grad_gate_ld % vec == 0 &&
-               p.grad_x_ld % vec == 0 && at(p.grad_gate, bytes) && at(p.grad_x, bytes);
+               p.grad_x_ld % vec == 0 && at(p.grad_gate, 16) && at(p.grad_x, 16);
     };
-    return fits(8) ? 8 : (dtype != TFG_BF16 && fits(4) ? 4 : 1);
+    const int vec = 16 / size;
+    return fits(vec) ? vec : 1;
 }
 
 void scan_geometry(ScanArgs &p, int vec, void *ws, int32_t *status) {

@@ -265,6 +265,7 @@ constexpr int kWarpRows = kTileRows / kScanWarps;            // rows of a warp
 
 template <int VEC>
 struct ScanTile {
+    static constexpr int kLane = VEC * 4 > 16 ? 16 : VEC * 4, kRow = VEC * 4 * kScanThreads;   // of fp32 slots
     static constexpr int kAcross = VEC == 1 ? 32 : 8;        // threads side by side in a row
     static constexpr int kEach = kTileRows * kAcross / kScanThreads;   // rows of a thread
     static constexpr int kWide = kAcross * VEC;              // channels
@@ -378,26 +379,30 @@ __device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (
     }
 }
 
-// The thread's rows as one map.  PLAIN: they lie in a sequence that neither begins nor ends there.
-template <bool PLAIN, int KIND, int VEC, int EACH, typename In>
-__device__ __forceinline__ void compose_down(const ScanArgs &p, const In &x, const float (&d)[EACH][VEC], const float *initial,
+// The thread's rows as one map, and a - 1 of each row into d, which may lie where z does.  PLAIN: the rows
+// lie in a sequence that neither begins nor ends there.
+template <bool PLAIN, int KIND, int VEC, int EACH, typename Gate, typename In, typename Decay>
+__device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, const In &x, const Decay &d, const float *initial,
                                              const int32_t *seq, int64_t c, uint32_t begin, uint32_t in, float (&a)[VEC],
                                              float (&b)[VEC]) {
 #pragma unroll
     for (int q = 0; q < VEC; ++q) a[q] = 1.f, b[q] = 0.f;
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
+        float v[VEC], dj[VEC];
+        z.widen(j, v);
+        decay_less_one<KIND>(v, dj);
+        d.put(j, dj);
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((begin >> j) & 1u)) {
 #pragma unroll
             for (int q = 0; q < VEC; ++q) a[q] = 0.f;
             state_or_zero(initial, seq[j], p.f, c, b);
         }
-        float v[VEC];
         x.widen(j, v);
-        fma_vec(a, d[j], a, a);
-        fma_vec(b, d[j], b, b);
-        add_input<KIND>(b, d[j], v);
+        fma_vec(a, dj, a, a);
+        fma_vec(b, dj, b, b);
+        add_input<KIND>(b, dj, v);
     }
 }
 

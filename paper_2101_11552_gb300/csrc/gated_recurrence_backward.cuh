@@ -18,39 +18,47 @@
 namespace tfg {
 namespace {
 
+// A tile's inputs; a - 1 takes the gates' place, in slots wide enough for it.
 template <typename XT, typename GT, int VEC>
 struct BackwardStage {
     using T = ScanTile<VEC>;
+    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kLane, T::kRow>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
     using In = Slots<XT, VEC, T::kEach, kScanThreads>;
     using Grad = Slots<GT, VEC, T::kEach, kScanThreads>;
-    static constexpr int kBytes = 2 * In::kAll + Grad::kAll;
-    In z, x;
+    static constexpr int kBytes = Decay::kAll + In::kAll + Grad::kAll;
+    Gate z;
+    Decay d;
+    In x;
     Grad g;
-    __device__ __forceinline__ explicit BackwardStage(char *stage) : z(stage), x(stage + In::kAll), g(stage + 2 * In::kAll) {}
+    __device__ __forceinline__ explicit BackwardStage(char *stage)
+        : z(stage), d(stage), x(stage + Decay::kAll), g(stage + Decay::kAll + In::kAll) {}
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows + group * T::kEach;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC;
-        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach));
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
         const GT *gp = static_cast<const GT *>(p.g) + r0 * p.f + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld);
-                x.copy(j, xp + j * p.x_ld);
-                if (p.g) g.copy(j, gp + j * p.f);
+                z.copy(j, zp + j * p.gate_ld, p.f - c);
+                x.copy(j, xp + j * p.x_ld, p.f - c);
+                if (p.g) g.copy(j, gp + j * p.f, p.f - c);
                 else g.zero(j);
             }
         if (p.linked) copy_plan(p, tile, rows);
     }
 };
 
-constexpr int kBackwardCtas = 2;          // of a multiprocessor: 128 registers a thread
+// CTAs of a multiprocessor, by shared memory: 75 KB where all is bf16 but the decay.
+template <typename XT, typename GT, int VEC>
+constexpr int kBackwardCtas = BackwardStage<XT, GT, VEC>::kBytes > 64 * 1024 ? 2 : 3;
 
 // The thread's rows as one map of the adjoint, from the last to the first.
-template <bool PLAIN, int VEC, int EACH, typename Grad>
-__device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, const float (&d)[EACH][VEC], const float *grad_final,
+template <bool PLAIN, int EACH, int VEC, typename Grad, typename Decay>
+__device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, const Decay &d, const float *grad_final,
                                            const int32_t *seq, int64_t c, uint32_t begin, uint32_t end, uint32_t in,
                                            float (&u)[VEC], float (&w)[VEC]) {
 #pragma unroll
@@ -63,11 +71,12 @@ __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, con
             for (int q = 0; q < VEC; ++q) u[q] = 0.f;
             state_or_zero(grad_final, seq[j], p.f, c, w);
         }
-        float v[VEC];
+        float v[VEC], dj[VEC];
         g.widen(j, v);
+        d.widen(j, dj);
         add_vec(w, v);
-        fma_vec(u, d[j], u, u);
-        fma_vec(w, d[j], w, w);
+        fma_vec(u, dj, u, u);
+        fma_vec(w, dj, w, w);
         if (!PLAIN && ((begin >> j) & 1u)) {
 #pragma unroll
             for (int q = 0; q < VEC; ++q) u[q] = w[q] = 0.f;
@@ -76,8 +85,8 @@ __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, con
 }
 
 // The gradients of the thread's rows from the state v that enters them and what enters their last, w.
-template <bool PLAIN, int KIND, typename XT, int VEC, int EACH, typename In, typename Grad>
-__device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, const Grad &g, const float (&d)[EACH][VEC],
+template <bool PLAIN, int KIND, typename XT, int EACH, int VEC, typename In, typename Grad, typename Decay>
+__device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, const Grad &g, const Decay &d,
                                                 const int32_t *seq, int64_t row, int64_t c, uint32_t begin, uint32_t end,
                                                 uint32_t in, float (&v)[VEC], float (&w)[VEC]) {
     float before[EACH][VEC];
@@ -87,10 +96,11 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
 #pragma unroll
         for (int q = 0; q < VEC; ++q) before[j][q] = v[q];
         if (j + 1 < EACH) {
-            float xv[VEC];
+            float xv[VEC], dj[VEC];
             x.widen(j, xv);
-            fma_vec(v, d[j], v, v);
-            add_input<KIND>(v, d[j], xv);
+            d.widen(j, dj);
+            fma_vec(v, dj, v, v);
+            add_input<KIND>(v, dj, xv);
         }
     }
     XT *gate = static_cast<XT *>(p.grad_gate) + row * p.grad_gate_ld + c, *input = static_cast<XT *>(p.grad_x) + row * p.grad_x_ld + c;
@@ -98,24 +108,25 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
     for (int j = EACH - 1; j >= 0; --j) {
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((end >> j) & 1u)) state_or_zero(p.grad_final, seq[j], p.f, c, w);
-        float gz[VEC], gx[VEC];
+        float gz[VEC], gx[VEC], dj[VEC];
         g.widen(j, gx);
         add_vec(w, gx);                                      // l
         x.widen(j, gx);
+        d.widen(j, dj);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            const float less = -d[j][q];                     // 1 - a
+            const float less = -dj[q];                     // 1 - a
             if constexpr (KIND == TFG_GATE_SIGMOID) {
-                gz[q] = w[q] * (before[j][q] - gx[q]) * fmaf(less, d[j][q], less);
+                gz[q] = w[q] * (before[j][q] - gx[q]) * fmaf(less, dj[q], less);
                 gx[q] = w[q] * less;
             } else {
-                gz[q] = w[q] * (before[j][q] * (1.f + d[j][q]));
+                gz[q] = w[q] * (before[j][q] * (1.f + dj[q]));
                 gx[q] = w[q];
             }
         }
         store_vec<VEC>(gate + j * p.grad_gate_ld, gz);
         store_vec<VEC>(input + j * p.grad_x_ld, gx);
-        fma_vec(w, d[j], w, w);
+        fma_vec(w, dj, w, w);
         if (!PLAIN && ((begin >> j) & 1u)) {
             if (p.grad_initial) store_vec<VEC>(p.grad_initial + seq[j] * p.f + c, w);
 #pragma unroll
@@ -125,7 +136,7 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
 }
 
 template <typename XT, typename GT, int VEC, int KIND>
-__global__ void __launch_bounds__(kScanThreads, kBackwardCtas) scan_backward(ScanArgs p) {
+__global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan_backward(ScanArgs p) {
     using T = ScanTile<VEC>;
     using Stage = BackwardStage<XT, GT, VEC>;
     extern __shared__ __align__(16) char s_stage[];
@@ -161,19 +172,13 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas) scan_backward(Sca
     const int32_t *seq = rows.seq + group * T::kEach;
 
     // the thread's maps: of the state down its rows, of the adjoint up
-    float d[T::kEach][VEC], a[VEC], b[VEC], u[VEC], w[VEC];
-#pragma unroll
-    for (int j = 0; j < T::kEach; ++j) {
-        float v[VEC];
-        in_stage.z.widen(j, v);
-        decay_less_one<KIND>(v, d[j]);
-    }
+    float a[VEC], b[VEC], u[VEC], w[VEC];
     if (plain) {
-        compose_down<true, KIND>(p, in_stage.x, d, nullptr, seq, c, begin, in, a, b);
-        compose_up<true>(p, in_stage.g, d, nullptr, seq, c, begin, end, in, u, w);
+        compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+        compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, u, w);
     } else {
-        compose_down<false, KIND>(p, in_stage.x, d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
-        compose_up<false>(p, in_stage.g, d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
+        compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+        compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
     }
     bool cut = begin != 0u, cut_up = (begin | end) != 0u;
     scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
@@ -217,8 +222,8 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas) scan_backward(Sca
     enter_group<VEC, true>(u, w, cut_up, l);
     if (!on) return;
     const int64_t row = r0 + group * T::kEach;
-    if (plain) write_gradients<true, KIND, XT>(p, in_stage.x, in_stage.g, d, seq, row, c, begin, end, in, v, l);
-    else write_gradients<false, KIND, XT>(p, in_stage.x, in_stage.g, d, seq, row, c, begin, end, in, v, l);
+    if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+    else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
 }
 
 template <typename XT, typename GT, int VEC, int KIND>

@@ -4,7 +4,6 @@
 namespace tfg {
 
 cudaError_t launch_scan_backward_f32(const ScanArgs &p, int vec, int kind, cudaStream_t s) {
-    if (vec == 8) return launch_backward_grad<float, 8>(p, kind, s);
     if (vec == 4) return launch_backward_grad<float, 4>(p, kind, s);
     return launch_backward_grad<float, 1>(p, kind, s);
 }

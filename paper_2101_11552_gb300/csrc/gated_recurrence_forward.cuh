@@ -7,44 +7,50 @@
 namespace tfg {
 namespace {
 
+// A tile's inputs; a - 1 takes the gates' place, in slots wide enough for it.
 template <typename XT, int VEC>
 struct ForwardStage {
     using T = ScanTile<VEC>;
+    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kLane, T::kRow>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
     using In = Slots<XT, VEC, T::kEach, kScanThreads>;
-    static constexpr int kBytes = 2 * In::kAll;
-    In z, x;
-    __device__ __forceinline__ explicit ForwardStage(char *stage) : z(stage), x(stage + In::kAll) {}
+    static constexpr int kBytes = Decay::kAll + In::kAll;
+    Gate z;
+    Decay d;
+    In x;
+    __device__ __forceinline__ explicit ForwardStage(char *stage) : z(stage), d(stage), x(stage + Decay::kAll) {}
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC, r0 = job.order * kTileRows + group * T::kEach;
-        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach));
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld);
-                x.copy(j, xp + j * p.x_ld);
+                z.copy(j, zp + j * p.gate_ld, p.f - c);
+                x.copy(j, xp + j * p.x_ld, p.f - c);
             }
         if (p.linked) copy_plan(p, job.order, rows);
     }
 };
 
-// CTAs of a multiprocessor: three of 80 registers a thread where a thread has 8 channels.
+// CTAs of a multiprocessor: as many as their shared memory allows (55 and 39 KB), 64 registers a thread.
 template <int VEC>
-constexpr int kForwardCtas = VEC == 8 ? 3 : 4;
+constexpr int kForwardCtas = 4;
 
 // The rows again, from the state v that enters the thread's first.
-template <bool PLAIN, int KIND, typename OT, int VEC, int EACH, typename In>
-__device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const float (&d)[EACH][VEC], const int32_t *seq,
-                                           int64_t c, uint32_t begin, uint32_t end, uint32_t in, OT *out, float (&v)[VEC]) {
+template <bool PLAIN, int KIND, int EACH, typename OT, int VEC, typename In, typename Decay>
+__device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const Decay &d, const int32_t *seq, int64_t c,
+                                           uint32_t begin, uint32_t end, uint32_t in, OT *out, float (&v)[VEC]) {
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((begin >> j) & 1u)) state_or_zero(p.initial, seq[j], p.f, c, v);
-        float w[VEC];
+        float w[VEC], dj[VEC];
         x.widen(j, w);
-        fma_vec(v, d[j], v, v);
-        add_input<KIND>(v, d[j], w);
+        d.widen(j, dj);
+        fma_vec(v, dj, v, v);
+        add_input<KIND>(v, dj, w);
         store_vec<VEC>(out + j * p.f, v);
         if (!PLAIN && ((end >> j) & 1u) && p.final_state) store_vec<VEC>(p.final_state + seq[j] * p.f + c, v);
     }
@@ -80,15 +86,9 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas<VEC>) scan_forward(
     const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
     const int32_t *seq = rows.seq + group * T::kEach;
 
-    float d[T::kEach][VEC], a[VEC], b[VEC];
-#pragma unroll
-    for (int j = 0; j < T::kEach; ++j) {
-        float v[VEC];
-        in_stage.z.widen(j, v);
-        decay_less_one<KIND>(v, d[j]);
-    }
-    if (plain) compose_down<true, KIND>(p, in_stage.x, d, nullptr, seq, c, begin, in, a, b);
-    else compose_down<false, KIND>(p, in_stage.x, d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+    float a[VEC], b[VEC];
+    if (plain) compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+    else compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
     bool cut = begin != 0u;
     scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
     __syncthreads();
@@ -124,8 +124,8 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas<VEC>) scan_forward(
     enter_group<VEC, false>(a, b, cut, v);
     if (!on) return;
     OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
-    if (plain) write_rows<true, KIND>(p, in_stage.x, d, seq, c, begin, end, in, out, v);
-    else write_rows<false, KIND>(p, in_stage.x, d, seq, c, begin, end, in, out, v);
+    if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+    else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
 }
 
 template <typename XT, typename OT, int VEC, int KIND>

@@ -136,12 +136,10 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
             const typename B::D d(stage + B::S::kAll + B::G::kAll);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * TT) * VEC;
-                if (c < cols) {
-                    s.copy(i, static_cast<const ST *>(p.s) + row * p.f + c);
-                    g.copy(i, static_cast<const GT *>(p.g) + row * p.f + c);
-                    if (p.skip) d.copy(i, static_cast<const DT *>(p.skip) + row * p.f + c);
-                }
+                const int c = (t + i * TT) * VEC, left = cols - c;
+                s.copy(i, static_cast<const ST *>(p.s) + row * p.f + c, left);
+                g.copy(i, static_cast<const GT *>(p.g) + row * p.f + c, left);
+                if (p.skip) d.copy(i, static_cast<const DT *>(p.skip) + row * p.f + c, left);
             }
         }
         copies_commit();
@@ -162,6 +160,7 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
     const int64_t rounds = (p.n - static_cast<int64_t>(blockIdx.x) * kTeams + step - 1) / step;   // of the CTA: exchanges are by whole warps
 #pragma unroll 1
     for (int64_t round = 0; round < rounds; ++round) {
+        __syncwarp();                                        // the slots of the last round have been read
         copy(round + kStages - 1);
         const int64_t row = first + round * step;
         const bool live = row < p.n;
@@ -175,6 +174,7 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
         const typename B::G g_at(stage + B::S::kAll);
         const typename B::D d_at(stage + B::S::kAll + B::G::kAll);
         copies_wait<kStages - 1>();
+        __syncwarp();                                        // a neighbour's copies
         float sum[3] = {0.f, 0.f, 0.f};
         float s[B::kKept][VEC], g[B::kKept][VEC];
         if (live) {

@@ -130,36 +130,60 @@ __device__ __forceinline__ void copy_async(void *shared, const void *global) {
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Inputs of a CTA of THREADS in shared memory: every thread copies its own vectors and reads them back, so
-// that copies are in flight while others are worked on, without registers and without a
-// barrier.  A vector of 32 bytes lies in two halves, so that lanes side by side read 16 bytes
-// side by side.  EACH vectors a thread take kAll bytes of a CTA.
-template <typename T, int VEC, int EACH, int THREADS>
+// Inputs of a CTA of THREADS in shared memory: every thread's vectors lie in slots of its own, and it
+// alone reads them, so that copies are in flight while others are worked on, without registers and
+// without a barrier.  A vector of 32 bytes lies in two halves, so that lanes side by side read 16 bytes
+// side by side; they are copied by pairs of lanes, 64 bytes of memory in each copy of a pair, as 16 bytes
+// of every lane's 32 would ask L2 for each sector twice.  EACH vectors a thread take kAll bytes of a CTA; LANE:
+// bytes from a thread's part to the next one's, ROW: from one of its vectors to the next.
+template <typename T, int VEC, int EACH, int THREADS, int LANE = (VEC * sizeof(T) > 16 ? 16 : VEC * sizeof(T)),
+          int ROW = (VEC * sizeof(T) > 16 ? 2 : 1) * THREADS * LANE>
 struct Slots {
     static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
     static constexpr int kPart = kBytes > 16 ? 16 : kBytes, kParts = kBytes / kPart;
-    static constexpr int kAll = (EACH * kBytes * THREADS + 15) / 16 * 16;
+    static constexpr int kAll = (EACH * ROW + 15) / 16 * 16;
     char *at;
-    __device__ __forceinline__ explicit Slots(char *stage) : at(stage + threadIdx.x * kPart) {}
-    __device__ __forceinline__ void copy(int j, const T *from) const {
-#pragma unroll
-        for (int h = 0; h < kParts; ++h)
-            copy_async<kPart>(at + (j * kParts + h) * THREADS * kPart, reinterpret_cast<const char *>(from) + h * kPart);
+    __device__ __forceinline__ explicit Slots(char *stage) : at(stage + threadIdx.x * LANE) {}
+    __device__ __forceinline__ char *part(int j, int h) const { return at + j * ROW + h * THREADS * LANE; }
+    // The vector at `from`, if left > 0 (values from there to the row's end, a multiple of VEC).  Vectors of lanes 2 i and
+    // 2 i + 1 lie side by side in a row and are copied in the same call; two halves are there
+    // for their thread after its wait and a barrier of the warp.
+    __device__ __forceinline__ void copy(int j, const T *from, int64_t left) const {
+        if constexpr (kParts == 2) {
+            const int odd = threadIdx.x & 1;
+            const char *even = reinterpret_cast<const char *>(from - odd * VEC) + odd * 16;
+            const int64_t rest = left + odd * VEC;
+            if (rest > 0) copy_async<16>(part(j, odd) - odd * LANE, even);
+            if (rest > VEC) copy_async<16>(part(j, odd) + (1 - odd) * LANE, even + 32);
+        } else {
+            if (left > 0) copy_async<kPart>(part(j, 0), from);
+        }
     }
     __device__ __forceinline__ void zero(int j) const {
 #pragma unroll
-        for (int i = 0; i < kParts * kPart / 2; ++i)
-            *reinterpret_cast<uint16_t *>(at + (j * kParts + i * 2 / kPart) * THREADS * kPart + i * 2 % kPart) = 0;
+        for (int h = 0; h < kParts; ++h)
+#pragma unroll
+            for (int i = 0; i < kPart; i += 2) *reinterpret_cast<uint16_t *>(part(j, h) + i) = 0;
+    }
+    __device__ __forceinline__ void put(int j, const float (&v)[VEC]) const {
+        static_assert(sizeof(T) == 4, "fp32 values");
+        if constexpr (VEC % 4 == 0) {
+#pragma unroll
+            for (int q = 0; q < VEC; q += 4) *reinterpret_cast<float4 *>(part(j, q / 4)) = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) reinterpret_cast<float *>(part(j, 0))[q] = v[q];
+        }
     }
     __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
         if constexpr (kParts == 2) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float4 q = *reinterpret_cast<const float4 *>(at + (j * 2 + h) * THREADS * kPart);
+                const float4 q = *reinterpret_cast<const float4 *>(part(j, h));
                 v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
             }
         } else {
-            VecLoad<T, VEC>::widen(load_plain<T, VEC>(reinterpret_cast<const T *>(at + j * THREADS * kPart)), v);
+            VecLoad<T, VEC>::widen(load_plain<T, VEC>(reinterpret_cast<const T *>(part(j, 0))), v);
         }
     }
 };
