@@ -20,8 +20,9 @@
 // many trips through L2.  A map and a state are each one word, all ones until they are published, so a
 // reader looks at the value itself: no flag, no fence, one trip.  Tiles are handed out in
 // order by a counter: a tile waits only for tiles that are already running.  It publishes before it
-// waits: CTAs that held a second tile back until the first was done (copies in flight meanwhile)
-// made a convoy of it, 213 us in place of 70 for 1,024 molecules forward.
+// waits, and asks for its next tile when its own waiting is over: CTAs that held a second tile while the first
+// waited (its copies in flight) made a convoy of it, 213 us in place of 70 for 1,024 molecules
+// forward.
 //
 // Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps
 // its distance from 1 to a few u, where a rounded a would change a memory of 1,000 steps by
@@ -92,6 +93,12 @@ struct ScanSpace {
     }
 };
 
+
+// CTAs of a launch, with at most `resident` on a multiprocessor.
+inline unsigned scan_ctas(const ScanArgs &p, int resident) {
+    const int64_t jobs = p.tiles * p.strips;
+    return static_cast<unsigned>(p.checkers + (p.linked ? min64(jobs, static_cast<int64_t>(resident) * sm_count()) : jobs));
+}
 
 namespace {
 
@@ -290,13 +297,26 @@ struct Job {
     }
 };
 
-// The job of this CTA; with a barrier where tiles are handed out.
-__device__ __forceinline__ Job next_job(const ScanArgs &p, uint32_t *s_next) {
-    if (!p.linked) return Job(p, blockIdx.x - p.checkers);
-    if (threadIdx.x == 0) *s_next = atomicAdd(p.next, 1u);
-    __syncthreads();
-    return Job(p, *s_next);
-}
+// The jobs of a CTA, one after the other.  ask: once the CTA waits for no other tile; next: by the whole CTA,
+// with a barrier (s_next and what the last job left in shared memory are free behind it).
+struct Jobs {
+    uint32_t *s_next;
+    uint32_t count, asked;
+    __device__ __forceinline__ Jobs(const ScanArgs &p, uint32_t *s)
+        : s_next(s), count(static_cast<uint32_t>(p.tiles * p.strips)), asked(blockIdx.x - p.checkers) {
+        if (p.linked) ask(p);
+    }
+    __device__ __forceinline__ void ask(const ScanArgs &p) {
+        if (threadIdx.x == 0) asked = p.linked ? atomicAdd(p.next, 1u) : count;
+    }
+    __device__ __forceinline__ bool next(const ScanArgs &p, uint32_t &job) {
+        __syncthreads();
+        if (threadIdx.x == 0) *s_next = asked;
+        __syncthreads();
+        job = *s_next;
+        return job < count;
+    }
+};
 
 // The last tile before this one in its window, in order of work, that lets nothing through, by its place
 // in the window, -1 if there is none; by a whole warp.
@@ -425,6 +445,8 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
     float state = 0.f;
     if (wants && order > 0) {
         const int first = from < 0 ? 0 : from, begin = part * kMaps;
+        uint32_t entered = 0;                                // in flight beside the maps
+        if (mine && from < 0 && window > 0) entered = ld_word(p.states + window * p.f + c);
         if (c < p.f && begin + kMaps > first && begin < place) {
             const uint64_t *maps = p.maps + (order - place + begin) * p.f + c;
             uint64_t word[kMaps];
@@ -442,8 +464,8 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
             }
             s_part[part][channel] = make_float2(ma, mb);
         }
-        if (mine && from < 0 && window > 0)
-            state = __uint_as_float(wait_for(p.states + window * p.f + c, kNoState, p.status));
+        if (entered == kNoState) entered = wait_for(p.states + window * p.f + c, kNoState, p.status);
+        state = __uint_as_float(entered);
         __syncthreads();
         if (mine) {
 #pragma unroll

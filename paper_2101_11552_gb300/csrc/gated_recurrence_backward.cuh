@@ -22,10 +22,10 @@ namespace {
 template <typename XT, typename GT, int VEC>
 struct BackwardStage {
     using T = ScanTile<VEC>;
-    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kLane, T::kRow>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
-    using In = Slots<XT, VEC, T::kEach, kScanThreads>;
-    using Grad = Slots<GT, VEC, T::kEach, kScanThreads>;
+    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using In = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using Grad = Slots<GT, VEC, T::kEach, kScanThreads, T::kAcross>;
     static constexpr int kBytes = Decay::kAll + In::kAll + Grad::kAll;
     Gate z;
     Decay d;
@@ -37,15 +37,15 @@ struct BackwardStage {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows + group * T::kEach;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach));
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = static_cast<int>(min64(p.f - c, 1 << 20));
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
         const GT *gp = static_cast<const GT *>(p.g) + r0 * p.f + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld, p.f - c);
-                x.copy(j, xp + j * p.x_ld, p.f - c);
-                if (p.g) g.copy(j, gp + j * p.f, p.f - c);
+                z.copy(j, zp + j * p.gate_ld, cols);
+                x.copy(j, xp + j * p.x_ld, cols);
+                if (p.g) g.copy(j, gp + j * p.f, cols);
                 else g.zero(j);
             }
         if (p.linked) copy_plan(p, tile, rows);
@@ -149,81 +149,87 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan
     __shared__ int s_from;
     if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.grad_final, p.grad_initial);
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
-    const Job job = next_job(p, &s_next);
     const Stage in_stage(s_stage);
-    in_stage.copy(p, job, rows);
-    const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows;
-    const int64_t c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
-    const bool on = c < p.f, column = static_cast<int>(threadIdx.x) < T::kWide;
-    if (p.linked && warp == 0) {
-        const int from = cut_before<true>(p, job.order);
-        if (threadIdx.x == 0) s_from = from;
-    }
-    const int sc = static_cast<int>(threadIdx.x) - T::kWide;                     // threads of the next columns: states
-    float state = 0.f;
-    if (sc >= 0 && sc < T::kWide && c0 + sc < p.f) state = __ldg(p.entered + tile * p.f + c0 + sc);
-    copies_done();
-    if (p.linked) __syncthreads();                           // the plan is there
-    else find_rows(p, rows);
-    const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
-                   in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps),
-                   cut_warps = warps_word(rows.cut_warps);
-    const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
-    const int32_t *seq = rows.seq + group * T::kEach;
-
-    // the thread's maps: of the state down its rows, of the adjoint up
-    float a[VEC], b[VEC], u[VEC], w[VEC];
-    if (plain) {
-        compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-        compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, u, w);
-    } else {
-        compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
-        compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
-    }
-    bool cut = begin != 0u, cut_up = (begin | end) != 0u;
-    scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
-    scan_groups<VEC, true>(u, w, cut_up, warp, lane, s_u, s_w);
-    __syncthreads();
-
-    // threads of the first columns: up the warps; of the next: down them, from the state kept
-    float tu = 1.f, tw = 0.f;
-    if (column) {
-#pragma unroll
-        for (int i = kScanWarps - 1; i >= 0; --i) {
-            const float gu = s_u[i][threadIdx.x], gw = s_w[i][threadIdx.x];
-            s_u[i][threadIdx.x] = tu;
-            s_w[i][threadIdx.x] = tw;
-            const bool fresh = (cut_warps >> warp_bit(i)) & 1u;
-            tw = fresh ? gw : fmaf(gu, tw, gw);
-            tu = fresh ? 0.f : tu * gu;
+    Jobs jobs(p, &s_next);
+    uint32_t number;
+#pragma unroll 1
+    while (jobs.next(p, number)) {
+        const Job job(p, number);
+        in_stage.copy(p, job, rows);
+        const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows;
+        const int64_t c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
+        const bool on = c < p.f, column = static_cast<int>(threadIdx.x) < T::kWide;
+        if (p.linked && warp == 0) {
+            const int from = cut_before<true>(p, job.order);
+            if (threadIdx.x == 0) s_from = from;
         }
-    } else if (sc < T::kWide) {
-#pragma unroll
-        for (int i = 0; i < kScanWarps; ++i) {
-            const float ga = s_a[i][sc], gb = s_b[i][sc];
-            s_b[i][sc] = state;
-            state = (begin_warps >> warp_bit(i)) & 1u ? gb : fmaf(ga, state, gb);
-        }
-    }
-    const bool wants = (rows.in[kTileRows / 32 - 1] & ~rows.end[kTileRows / 32 - 1]) >> 31;
-    const float carry = enter_tile<T::kWide>(p, job.order, c0, tu, tw, cut_warps != 0u, wants, s_from, s_part);
-    if (column) s_carry[threadIdx.x] = carry;
-    __syncthreads();
+        const int sc = static_cast<int>(threadIdx.x) - T::kWide;                     // threads of the next columns: states
+        float state = 0.f;
+        if (sc >= 0 && sc < T::kWide && c0 + sc < p.f) state = __ldg(p.entered + tile * p.f + c0 + sc);
+        copies_done();
+        if (p.linked) __syncthreads();                           // the plan is there
+        else find_rows(p, rows);
+        const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
+                       in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps),
+                       cut_warps = warps_word(rows.cut_warps);
+        const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
+        const int32_t *seq = rows.seq + group * T::kEach;
 
-    float v[VEC], l[VEC];
-    const bool far = cut_warps >> warp_bit(warp) >> 1 != 0u;                     // a warp behind this one is cut
+        // the thread's maps: of the state down its rows, of the adjoint up
+        float a[VEC], b[VEC], u[VEC], w[VEC];
+        if (plain) {
+            compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+            compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, u, w);
+        } else {
+            compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+            compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
+        }
+        bool cut = begin != 0u, cut_up = (begin | end) != 0u;
+        scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
+        scan_groups<VEC, true>(u, w, cut_up, warp, lane, s_u, s_w);
+        __syncthreads();
+
+        // threads of the first columns: up the warps; of the next: down them, from the state kept
+        float tu = 1.f, tw = 0.f;
+        if (column) {
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-        const int i = lane * VEC + q;
-        v[q] = s_b[warp][i];
-        l[q] = far ? s_w[warp][i] : fmaf(s_u[warp][i], s_carry[i], s_w[warp][i]);
+            for (int i = kScanWarps - 1; i >= 0; --i) {
+                const float gu = s_u[i][threadIdx.x], gw = s_w[i][threadIdx.x];
+                s_u[i][threadIdx.x] = tu;
+                s_w[i][threadIdx.x] = tw;
+                const bool fresh = (cut_warps >> warp_bit(i)) & 1u;
+                tw = fresh ? gw : fmaf(gu, tw, gw);
+                tu = fresh ? 0.f : tu * gu;
+            }
+        } else if (sc < T::kWide) {
+#pragma unroll
+            for (int i = 0; i < kScanWarps; ++i) {
+                const float ga = s_a[i][sc], gb = s_b[i][sc];
+                s_b[i][sc] = state;
+                state = (begin_warps >> warp_bit(i)) & 1u ? gb : fmaf(ga, state, gb);
+            }
+        }
+        const bool wants = (rows.in[kTileRows / 32 - 1] & ~rows.end[kTileRows / 32 - 1]) >> 31;
+        const float carry = enter_tile<T::kWide>(p, job.order, c0, tu, tw, cut_warps != 0u, wants, s_from, s_part);
+        jobs.ask(p);
+        if (column) s_carry[threadIdx.x] = carry;
+        __syncthreads();
+
+        float v[VEC], l[VEC];
+        const bool far = cut_warps >> warp_bit(warp) >> 1 != 0u;                     // a warp behind this one is cut
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+            const int i = lane * VEC + q;
+            v[q] = s_b[warp][i];
+            l[q] = far ? s_w[warp][i] : fmaf(s_u[warp][i], s_carry[i], s_w[warp][i]);
+        }
+        enter_group<VEC, false>(a, b, cut, v);
+        enter_group<VEC, true>(u, w, cut_up, l);
+        if (!on) continue;
+        const int64_t row = r0 + group * T::kEach;
+        if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+        else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
     }
-    enter_group<VEC, false>(a, b, cut, v);
-    enter_group<VEC, true>(u, w, cut_up, l);
-    if (!on) return;
-    const int64_t row = r0 + group * T::kEach;
-    if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
-    else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
 }
 
 template <typename XT, typename GT, int VEC, int KIND>
@@ -234,7 +240,7 @@ cudaError_t launch_backward(const ScanArgs &p, cudaStream_t s) {
             cudaFuncSetAttribute(scan_backward<XT, GT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
         if (e != cudaSuccess) return e;
     }
-    scan_backward<XT, GT, VEC, KIND><<<static_cast<unsigned>(p.checkers + p.tiles * p.strips), kScanThreads, kShared, s>>>(p);
+    scan_backward<XT, GT, VEC, KIND><<<scan_ctas(p, kBackwardCtas<XT, GT, VEC>), kScanThreads, kShared, s>>>(p);
     return cudaGetLastError();
 }
 template <typename XT, typename GT, int VEC>

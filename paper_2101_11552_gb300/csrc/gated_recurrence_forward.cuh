@@ -11,9 +11,9 @@ namespace {
 template <typename XT, int VEC>
 struct ForwardStage {
     using T = ScanTile<VEC>;
-    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kLane, T::kRow>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
-    using In = Slots<XT, VEC, T::kEach, kScanThreads>;
+    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using In = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross>;
     static constexpr int kBytes = Decay::kAll + In::kAll;
     Gate z;
     Decay d;
@@ -22,20 +22,19 @@ struct ForwardStage {
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC, r0 = job.order * kTileRows + group * T::kEach;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach));
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = static_cast<int>(min64(p.f - c, 1 << 20));
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld, p.f - c);
-                x.copy(j, xp + j * p.x_ld, p.f - c);
+                z.copy(j, zp + j * p.gate_ld, cols);
+                x.copy(j, xp + j * p.x_ld, cols);
             }
         if (p.linked) copy_plan(p, job.order, rows);
     }
 };
 
 // CTAs of a multiprocessor: as many as their shared memory allows (55 and 39 KB), 64 registers a thread.
-template <int VEC>
 constexpr int kForwardCtas = 4;
 
 // The rows again, from the state v that enters the thread's first.
@@ -57,7 +56,7 @@ __device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const
 }
 
 template <typename XT, typename OT, int VEC, int KIND>
-__global__ void __launch_bounds__(kScanThreads, kForwardCtas<VEC>) scan_forward(ScanArgs p) {
+__global__ void __launch_bounds__(kScanThreads, kForwardCtas) scan_forward(ScanArgs p) {
     using T = ScanTile<VEC>;
     using Stage = ForwardStage<XT, VEC>;
     extern __shared__ __align__(16) char s_stage[];
@@ -69,63 +68,69 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas<VEC>) scan_forward(
     __shared__ int s_from;
     if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.initial, p.final_state);
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
-    const Job job = next_job(p, &s_next);
     const Stage in_stage(s_stage);
-    in_stage.copy(p, job, rows);
-    const int64_t r0 = job.order * kTileRows, c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
-    const bool on = c < p.f;
-    if (p.linked && warp == 0) {
-        const int from = cut_before<false>(p, job.order);
-        if (threadIdx.x == 0) s_from = from;
-    }
-    copies_done();
-    if (p.linked) __syncthreads();                           // the plan is there
-    else find_rows(p, rows);
-    const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
-                   in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps);
-    const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
-    const int32_t *seq = rows.seq + group * T::kEach;
-
-    float a[VEC], b[VEC];
-    if (plain) compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-    else compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
-    bool cut = begin != 0u;
-    scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
-    __syncthreads();
-
-    // down the warps, a thread for each channel: what stands before each, and the tile's map
-    const int64_t mc = c0 + threadIdx.x;
-    const bool column = static_cast<int>(threadIdx.x) < T::kWide;
-    float ta = 1.f, tb = 0.f;
-    if (column) {
-#pragma unroll
-        for (int w = 0; w < kScanWarps; ++w) {
-            const float wa = s_a[w][threadIdx.x], wb = s_b[w][threadIdx.x];
-            s_a[w][threadIdx.x] = ta;
-            s_b[w][threadIdx.x] = tb;
-            const bool fresh = (begin_warps >> warp_bit(w)) & 1u;
-            tb = fresh ? wb : fmaf(wa, tb, wb);              // not 0 times what may be an infinity
-            ta = fresh ? 0.f : ta * wa;
+    Jobs jobs(p, &s_next);
+    uint32_t number;
+#pragma unroll 1
+    while (jobs.next(p, number)) {
+        const Job job(p, number);
+        in_stage.copy(p, job, rows);
+        const int64_t r0 = job.order * kTileRows, c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
+        const bool on = c < p.f;
+        if (p.linked && warp == 0) {
+            const int from = cut_before<false>(p, job.order);
+            if (threadIdx.x == 0) s_from = from;
         }
-    }
-    const bool wants = (rows.in[0] & ~rows.begin[0] & 1u) != 0u;
-    const float state = enter_tile<T::kWide>(p, job.order, c0, ta, tb, begin_warps != 0u, wants, s_from, s_part);
-    if (column) s_state[threadIdx.x] = state;
-    if (column && mc < p.f && p.entering) p.entering[job.order * p.f + mc] = state;
-    __syncthreads();
+        copies_done();
+        if (p.linked) __syncthreads();                           // the plan is there
+        else find_rows(p, rows);
+        const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
+                       in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps);
+        const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
+        const int32_t *seq = rows.seq + group * T::kEach;
 
-    float v[VEC];
-    const bool far = (begin_warps & ((1u << warp_bit(warp)) - 1u)) != 0u;
+        float a[VEC], b[VEC];
+        if (plain) compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+        else compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+        bool cut = begin != 0u;
+        scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
+        __syncthreads();
+
+        // down the warps, a thread for each channel: what stands before each, and the tile's map
+        const int64_t mc = c0 + threadIdx.x;
+        const bool column = static_cast<int>(threadIdx.x) < T::kWide;
+        float ta = 1.f, tb = 0.f;
+        if (column) {
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-        const int i = lane * VEC + q;
-        v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
+            for (int w = 0; w < kScanWarps; ++w) {
+                const float wa = s_a[w][threadIdx.x], wb = s_b[w][threadIdx.x];
+                s_a[w][threadIdx.x] = ta;
+                s_b[w][threadIdx.x] = tb;
+                const bool fresh = (begin_warps >> warp_bit(w)) & 1u;
+                tb = fresh ? wb : fmaf(wa, tb, wb);              // not 0 times what may be an infinity
+                ta = fresh ? 0.f : ta * wa;
+            }
+        }
+        const bool wants = (rows.in[0] & ~rows.begin[0] & 1u) != 0u;
+        const float state = enter_tile<T::kWide>(p, job.order, c0, ta, tb, begin_warps != 0u, wants, s_from, s_part);
+        jobs.ask(p);
+        if (column) s_state[threadIdx.x] = state;
+        if (column && mc < p.f && p.entering) p.entering[job.order * p.f + mc] = state;
+        __syncthreads();
+
+        float v[VEC];
+        const bool far = (begin_warps & ((1u << warp_bit(warp)) - 1u)) != 0u;
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) {
+            const int i = lane * VEC + q;
+            v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
+        }
+        enter_group<VEC, false>(a, b, cut, v);
+        if (!on) continue;
+        OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
+        if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+        else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
     }
-    enter_group<VEC, false>(a, b, cut, v);
-    if (!on) return;
-    OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
-    if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
-    else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
 }
 
 template <typename XT, typename OT, int VEC, int KIND>
@@ -136,7 +141,7 @@ cudaError_t launch_forward(const ScanArgs &p, cudaStream_t s) {
             cudaFuncSetAttribute(scan_forward<XT, OT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
         if (e != cudaSuccess) return e;
     }
-    scan_forward<XT, OT, VEC, KIND><<<static_cast<unsigned>(p.checkers + p.tiles * p.strips), kScanThreads, kShared, s>>>(p);
+    scan_forward<XT, OT, VEC, KIND><<<scan_ctas(p, kForwardCtas), kScanThreads, kShared, s>>>(p);
     return cudaGetLastError();
 }
 template <typename XT, int VEC>

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm(RowNormArgs p) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int q = 0; q < VEC; ++q) sum[0] += v[i][q];
-    team_sums<TT, 1>(sum, s_sum);
+    team_sums<TT, 1, 1>(sum, s_sum);
     const float per = 1.f / static_cast<float>(p.f);
     const float first = sum[0] * per;
     float dev[2] = {0.f, 0.f};
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm(RowNormArgs p) {
                 dev[1] = fmaf(v[i][q], v[i][q], dev[1]);
             }
         }
-    team_sums<TT, 2>(dev, s_sum + (TT > 32 ? TT / 32 : 1));
+    team_sums<TT, 1, 2>(dev, s_sum + (TT > 32 ? TT / 32 : 1));
     if (!live) return;
     const float d = dev[0] * per, r = row_rstd(d, dev[1] * per, p.eps);
     if (t == 0 && p.mean) {
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(1024) row_norm_long(RowNormArgs p) {
         for (int q = 0; q < VEC; ++q) part += v[q];
         sum[0] += part;
     }
-    team_sums<1024, 1>(sum, s_sum);
+    team_sums<1024, 1, 1>(sum, s_sum);
     const float first = sum[0] * per;
     for (int64_t c = threadIdx.x * VEC; c < p.f; c += step) {   // each thread reads what it wrote
         float v[VEC], part[2] = {0.f, 0.f};
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(1024) row_norm_long(RowNormArgs p) {
         dev[0] += part[0];
         dev[1] += part[1];
     }
-    team_sums<1024, 2>(dev, s_sum + 32);
+    team_sums<1024, 1, 2>(dev, s_sum + 32);
     const float d = dev[0] * per, r = row_rstd(d, dev[1] * per, p.eps);
     if (threadIdx.x == 0 && p.mean) {
         p.mean[blockIdx.x] = first + d;

@@ -10,9 +10,16 @@
 namespace tfg {
 namespace {
 
-// Adds v[s] over the TT threads of a team, to all of them, in a fixed order.  scratch: of a CTA
-// team, NS * TT / 32 floats that no other call uses before the next barrier.
-template <int TT, int NS>
+// A barrier of a team of TT threads: the whole CTA's, or one of its own where a CTA has several teams.
+template <int TT, int TEAMS>
+__device__ __forceinline__ void team_barrier() {
+    if constexpr (TEAMS == 1) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(static_cast<int>(threadIdx.x) / TT + 1), "n"(TT) : "memory");
+}
+
+// Adds v[s] over the TT threads of a team, to all of them, in a fixed order.  scratch: of a team of several
+// warps, NS * TT / 32 floats that no other call uses before the team's next barrier.
+template <int TT, int TEAMS, int NS>
 __device__ __forceinline__ void team_sums(float (&v)[NS], float *scratch) {
 #pragma unroll
     for (int o = (TT < 32 ? TT : 32) >> 1; o > 0; o >>= 1)
@@ -22,8 +29,8 @@ __device__ __forceinline__ void team_sums(float (&v)[NS], float *scratch) {
         constexpr int kWarps = TT / 32;
         if ((threadIdx.x & 31) == 0)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) scratch[s * kWarps + threadIdx.x / 32] = v[s];
-        __syncthreads();
+            for (int s = 0; s < NS; ++s) scratch[s * kWarps + threadIdx.x % TT / 32] = v[s];
+        team_barrier<TT, TEAMS>();
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             v[s] = 0.f;

@@ -12,7 +12,7 @@ cudaError_t launch_row_back_bf16_bf16(const RowBackArgs &p, cudaStream_t s);
 namespace {
 
 constexpr int kJoinCols = 32, kJoinRows = 32;
-constexpr int kBackResident = 6;          // CTAs of a multiprocessor at most (128 threads each)
+constexpr int kBackResident = 3;          // CTAs of a multiprocessor at most (256 threads each)
 
 // out[c] = sum over the CTAs of part[.][c], in 32 interleaved chains joined in order.
 __global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns_kernel(const float *part, int ctas, int64_t f,
@@ -60,12 +60,12 @@ cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n
         cudaError_t e = cudaMemsetAsync(grad_gamma, 0, sizeof(float) * size_t(f), s);
         return e != cudaSuccess ? e : cudaMemsetAsync(grad_beta, 0, sizeof(float) * size_t(f), s);
     }
-    RowBackArgs p{sum, n, f, gamma, mean, rstd, g, skip, grad_s, nullptr, nullptr, grad_gamma, grad_beta, out_dtype, 1, 1};
-    const auto fits = [&](int vec) {
-        return vec_fits(sum, sum_dtype, f, vec) && vec_fits(g, g_dtype, f, vec) && vec_fits(grad_s, out_dtype, f, vec) &&
-               (!skip || vec_fits(skip, out_dtype, f, vec)) && weights_fit(gamma);
+    RowBackArgs p{sum, n, f, gamma, mean, rstd, g, skip, grad_s, nullptr, nullptr, grad_gamma, grad_beta, out_dtype, false, 1};
+    const auto whole = [&](const void *q, int dtype) {
+        return f * (dtype == TFG_BF16 ? 2 : 4) % 16 == 0 && reinterpret_cast<uintptr_t>(q) % 16 == 0;
     };
-    p.vec = fits(8) ? 8 : (fits(4) ? 4 : 1);
+    p.bulk = whole(sum, sum_dtype) && whole(g, g_dtype) && whole(grad_s, out_dtype) && (!skip || whole(skip, out_dtype)) &&
+             reinterpret_cast<uintptr_t>(gamma) % 16 == 0;
     if (grad_gamma) {
         p.part = static_cast<float *>(ws);
         p.shift = p.part + 2 * size_t(f) * size_t(back_ctas(n, 1, kBackResident));

@@ -11,9 +11,8 @@
 //
 // A CTA takes the rows b, b + CTAs, ... (a row for each of its teams), keeps the sums of its columns
 // for gamma and beta in registers and writes them once; a second kernel adds the CTAs' in order.
-// The next rows' vectors are on their way to shared memory (each thread's own, without a barrier) while
-// a row is worked on: held in registers instead, 182 a thread left 8 warps on a multiprocessor
-// and loads waited for one another (8,192 rows of 8,192 bf16: 320 us).
+// The next rows are on their way to shared memory while a row is worked on.  Rows of whole 16 bytes come by
+// bulk copies, one for an array; others value by value, each thread's own (Slots).
 #pragma once
 
 #include "layer_norm.cuh"
@@ -31,7 +30,7 @@ struct RowBackArgs {
     float *shift;             // long rows: e of each row
     float *grad_gamma, *grad_beta;
     int out_dtype;            // of skip and grad_s
-    int vec;
+    bool bulk;                // every row of every array is whole 16 bytes
     int ctas;
 };
 
@@ -98,52 +97,92 @@ __device__ __forceinline__ void row_gradient(float (&s)[VEC], const float (&g)[V
 
 template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
 struct BackTeam {
-    static constexpr int kTeams = TT <= 32 ? 256 / TT : 1, kThreads = TT * kTeams;
-    using S = Slots<ST, VEC, NV, kThreads>;
-    using G = Slots<GT, VEC, NV, kThreads>;
-    using D = Slots<DT, VEC, NV, kThreads>;
-    static constexpr int kStageBytes = S::kAll + G::kAll + D::kAll;
-    // up to 16 values a thread are kept in registers from the sums to the gradient, more are read again
-    static constexpr bool kKeeps = NV * VEC <= 16;
+    static constexpr bool kBulk = VEC > 1;
+    static constexpr int kTeams = TT < 256 ? 256 / TT : 1, kThreads = TT * kTeams;
+    static constexpr int kUnits = TT < 32 ? kThreads / 32 : kTeams;      // of threads that one copy serves: a warp, or a team
+    static constexpr int kUnitRows = kTeams / kUnits;
+    static constexpr int kHeld = VEC * NV;                               // values a thread
+    static constexpr int kS = kThreads * kHeld * sizeof(ST), kG = kThreads * kHeld * sizeof(GT), kD = kThreads * kHeld * sizeof(DT);
+    static constexpr int kStageBytes = (kS + kG + kD + 15) / 16 * 16;
+    // up to 8 values a thread are kept in registers from the sums to the gradient, more are read again
+    static constexpr bool kKeeps = kHeld <= 8;
     static constexpr int kKept = kKeeps ? NV : 1;
-    // rows on their way: as many as leave room for a second CTA or, where a row is long, fit one
-    static constexpr int kStages = kStageBytes * 4 <= 100 * 1024 ? 4 : (kStageBytes * 2 <= 200 * 1024 ? 2 : 1);
+    // CTAs of a multiprocessor by their registers: 512 threads of 128, 768 of 80 where few values are held;
+    // rows on their way: as many as those leave room for
+    static constexpr int kWant = (kKeeps ? 768 : 512) / kThreads;
+    static constexpr int kRoom = 216 * 1024 / kWant / kStageBytes;
+    static constexpr int kStages = kRoom < 1 ? 1 : (kRoom < 4 ? kRoom : 4);
     static constexpr int kShared = kStages * kStageBytes;
-    // CTAs of a multiprocessor: by shared memory, and 768 threads of 80 registers
-    static constexpr int kFit = (220 * 1024) / (kShared + 3 * 1024);
-    static constexpr int kWant = 768 / kThreads > 0 ? 768 / kThreads : 1;
+    static constexpr int kFit = 220 * 1024 / (kShared + 3 * 1024);
     static constexpr int kCtas = kFit < 1 ? 1 : (kFit < kWant ? kFit : kWant);
 };
+
+template <typename T, int VEC>
+__device__ __forceinline__ void widen_shared(const T *p, float (&v)[VEC]) {
+    VecLoad<T, VEC>::widen(load_plain<T, VEC>(p), v);
+}
 
 template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
 __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, BackTeam<ST, GT, DT, VEC, TT, NV>::kCtas)
     row_norm_back(RowBackArgs p) {
     using B = BackTeam<ST, GT, DT, VEC, TT, NV>;
     constexpr int kTeams = B::kTeams, kStages = B::kStages, kWarps = TT > 32 ? TT / 32 : 1;
-    extern __shared__ __align__(16) char s_rows[];
-    __shared__ float s_sum[2][3 * kWarps];
+    extern __shared__ __align__(128) char s_rows[];
+    __shared__ float s_sum[2][kTeams][3 * kWarps];
+    __shared__ uint64_t s_full[kStages][B::kUnits];
     const int t = threadIdx.x % TT, team = threadIdx.x / TT;
+    const int unit = TT < 32 ? threadIdx.x / 32 : team, unit_row = TT < 32 ? (threadIdx.x & 31) / TT : 0;
     const int cols = static_cast<int>(p.f);
     const float per = 1.f / static_cast<float>(p.f);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams + team, step = static_cast<int64_t>(gridDim.x) * kTeams;
+    // rows of the CTA: exchanges are by whole warps, so all teams go through all rounds
+    const int64_t rounds = (p.n - static_cast<int64_t>(blockIdx.x) * kTeams + step - 1) / step;
+
+    // where a thread finds its vectors in a stage: the unit's rows one after the other, or slots of its own
+    const int at0 = B::kBulk ? unit * B::kUnitRows * TT * B::kHeld + unit_row * cols + t * VEC : threadIdx.x;
+    constexpr int kAtStep = B::kBulk ? TT * VEC : B::kThreads;
 
     const auto copy = [&](int64_t round) {
-        const int64_t row = first + round * step;
-        if (row < p.n) {
-            char *stage = s_rows + (kStages == 1 ? 0 : (round % kStages) * B::kStageBytes);
-            const typename B::S s(stage);
-            const typename B::G g(stage + B::S::kAll);
-            const typename B::D d(stage + B::S::kAll + B::G::kAll);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * TT) * VEC, left = cols - c;
-                s.copy(i, static_cast<const ST *>(p.s) + row * p.f + c, left);
-                g.copy(i, static_cast<const GT *>(p.g) + row * p.f + c, left);
-                if (p.skip) d.copy(i, static_cast<const DT *>(p.skip) + row * p.f + c, left);
+        if constexpr (B::kBulk) {
+            const bool leader = TT < 32 ? (threadIdx.x & 31) == 0 : t == 0;
+            const int64_t row = first + round * step;        // the leader's is the first of its unit
+            if (leader && row < p.n && round < rounds) {
+                const int stage = static_cast<int>(round % kStages);
+                char *to = s_rows + stage * B::kStageBytes;
+                const int at = unit * B::kUnitRows * TT * B::kHeld;
+                const uint32_t values = static_cast<uint32_t>(min64(p.n - row, B::kUnitRows)) * cols;
+                uint64_t *bar = &s_full[stage][unit];
+                arrive_expecting(bar, values * static_cast<uint32_t>(sizeof(ST) + sizeof(GT) + (p.skip ? sizeof(DT) : 0)));
+                bulk_copy(to + at * sizeof(ST), static_cast<const ST *>(p.s) + row * p.f, values * sizeof(ST), bar);
+                bulk_copy(to + B::kS + at * sizeof(GT), static_cast<const GT *>(p.g) + row * p.f, values * sizeof(GT), bar);
+                if (p.skip)
+                    bulk_copy(to + B::kS + B::kG + at * sizeof(DT), static_cast<const DT *>(p.skip) + row * p.f, values * sizeof(DT), bar);
             }
+        } else {
+            const int64_t row = first + round * step;
+            if (row < p.n && round < rounds) {
+                char *to = s_rows + static_cast<int>(round % kStages) * B::kStageBytes;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = t + i * TT, at = at0 + i * kAtStep;
+                    if (c < cols) {
+                        copy_async<sizeof(ST)>(to + at * sizeof(ST), static_cast<const ST *>(p.s) + row * p.f + c);
+                        copy_async<sizeof(GT)>(to + B::kS + at * sizeof(GT), static_cast<const GT *>(p.g) + row * p.f + c);
+                        if (p.skip) copy_async<sizeof(DT)>(to + B::kS + B::kG + at * sizeof(DT), static_cast<const DT *>(p.skip) + row * p.f + c);
+                    }
+                }
+            }
+            copies_commit();
         }
-        copies_commit();
     };
+    if constexpr (B::kBulk) {
+        if (threadIdx.x == 0) {
+            for (int k = 0; k < kStages; ++k)
+                for (int u = 0; u < B::kUnits; ++u) arrivals_init(&s_full[k][u], 1);
+            arrivals_ready();
+        }
+        __syncthreads();
+    }
     float gg[NV][VEC] = {}, gb[NV][VEC] = {}, w[B::kKept][VEC];
     if constexpr (B::kKeeps) {
 #pragma unroll
@@ -151,17 +190,14 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
             if ((t + i * TT) * VEC < cols) row_weights(p.gamma, (t + i * TT) * VEC, 1.f, w[i]);
     }
 #pragma unroll
-    for (int k = 0; k + 1 < kStages; ++k) copy(k);
+    for (int k = 0; k < (B::kBulk ? kStages : kStages - 1); ++k) copy(k);
     float m = 0.f, r = 0.f;
     if (first < p.n) {
         m = __ldg(p.mean + first);
         r = __ldg(p.rstd + first);
     }
-    const int64_t rounds = (p.n - static_cast<int64_t>(blockIdx.x) * kTeams + step - 1) / step;   // of the CTA: exchanges are by whole warps
 #pragma unroll 1
     for (int64_t round = 0; round < rounds; ++round) {
-        __syncwarp();                                        // the slots of the last round have been read
-        copy(round + kStages - 1);
         const int64_t row = first + round * step;
         const bool live = row < p.n;
         float next_m = 0.f, next_r = 0.f;
@@ -169,12 +205,17 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
             next_m = __ldg(p.mean + row + step);
             next_r = __ldg(p.rstd + row + step);
         }
-        char *stage = s_rows + (kStages == 1 ? 0 : (round % kStages) * B::kStageBytes);
-        const typename B::S s_at(stage);
-        const typename B::G g_at(stage + B::S::kAll);
-        const typename B::D d_at(stage + B::S::kAll + B::G::kAll);
-        copies_wait<kStages - 1>();
-        __syncwarp();                                        // a neighbour's copies
+        if constexpr (B::kBulk) {
+            // a row that does not arrive becomes NaN
+            if (live && !phase_done(&s_full[round % kStages][unit], static_cast<uint32_t>(round / kStages) & 1u)) r = NAN;
+        } else {
+            copy(round + kStages - 1);
+            copies_wait<kStages - 1>();
+        }
+        const char *stage = s_rows + static_cast<int>(round % kStages) * B::kStageBytes;
+        const ST *s_at = reinterpret_cast<const ST *>(stage) + at0;
+        const GT *g_at = reinterpret_cast<const GT *>(stage + B::kS) + at0;
+        const DT *d_at = reinterpret_cast<const DT *>(stage + B::kS + B::kG) + at0;
         float sum[3] = {0.f, 0.f, 0.f};
         float s[B::kKept][VEC], g[B::kKept][VEC];
         if (live) {
@@ -182,14 +223,14 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * TT) * VEC, k = i % B::kKept;
                 if (c < cols) {
-                    s_at.widen(i, s[k]);
-                    g_at.widen(i, g[k]);
+                    widen_shared<ST, VEC>(s_at + i * kAtStep, s[k]);
+                    widen_shared<GT, VEC>(g_at + i * kAtStep, g[k]);
                     if (!B::kKeeps) row_weights(p.gamma, c, 1.f, w[k]);
                     row_terms<VEC>(s[k], g[k], w[k], m, sum);
                 }
             }
         }
-        team_sums<TT, 3>(sum, s_sum[round & 1]);
+        team_sums<TT, kTeams, 3>(sum, s_sum[round & 1][team]);
         const RowMeans a(sum, r, per);
         if (live) {
 #pragma unroll
@@ -198,12 +239,12 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
                 if (c < cols) {
                     float o[VEC];
                     if (!B::kKeeps) {
-                        s_at.widen(i, s[k]);
-                        g_at.widen(i, g[k]);
+                        widen_shared<ST, VEC>(s_at + i * kAtStep, s[k]);
+                        widen_shared<GT, VEC>(g_at + i * kAtStep, g[k]);
                         row_weights(p.gamma, c, 1.f, w[k]);
                     }
                     if (p.skip) {
-                        d_at.widen(i, o);
+                        widen_shared<DT, VEC>(d_at + i * kAtStep, o);
                     } else {
 #pragma unroll
                         for (int q = 0; q < VEC; ++q) o[q] = 0.f;
@@ -214,6 +255,11 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
                     store_vec<VEC>(static_cast<DT *>(p.grad_s) + row * p.f + c, o);
                 }
             }
+        }
+        if constexpr (B::kBulk) {                            // the unit has read the stage: its next row
+            if constexpr (TT <= 32) __syncwarp();
+            else team_barrier<TT, kTeams>();
+            copy(round + kStages);
         }
         m = next_m;
         r = next_r;
@@ -233,8 +279,10 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
                 }
             }
     } else {
-        constexpr int kCols = TT * NV * VEC;
-        __shared__ float s_cols[2 * kCols];
+        constexpr int kCols = TT * NV * VEC, kLanes = TT < 32 ? TT : 32;
+        static_assert(2 * kCols * 4 <= B::kShared, "the rows' shared memory, when they are done");
+        float *s_cols = reinterpret_cast<float *>(s_rows);
+        __syncthreads();
 #pragma unroll
         for (int o = TT; o < 32; o <<= 1)
 #pragma unroll
@@ -244,8 +292,9 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
                     gg[i][q] += lane_xor(gg[i][q], o);
                     gb[i][q] += lane_xor(gb[i][q], o);
                 }
-        for (int j = 0; j < B::kThreads / 32; ++j) {
-            if (static_cast<int>(threadIdx.x) / 32 == j && (threadIdx.x & 31) < TT) {
+        constexpr int kPer = TT < 32 ? 32 : TT;              // threads that add at a time
+        for (int j = 0; j < B::kThreads / kPer; ++j) {
+            if (static_cast<int>(threadIdx.x) / kPer == j && (threadIdx.x & 31) < kLanes) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -282,7 +331,7 @@ __global__ void __launch_bounds__(1024) row_norm_back_long(RowBackArgs p) {
 #pragma unroll
         for (int k = 0; k < 3; ++k) sum[k] += part[k];
     }
-    team_sums<1024, 3>(sum, s_sum);
+    team_sums<1024, 1, 3>(sum, s_sum);
     const RowMeans a(sum, r, per);
     if (threadIdx.x == 0 && p.shift) p.shift[row] = a.e;
     for (int64_t c = threadIdx.x * VEC; c < p.f; c += step) {
@@ -320,9 +369,8 @@ __global__ void __launch_bounds__(256) long_columns(RowBackArgs p) {
     part[p.f + c] = gb;
 }
 
-// Threads and vectors by the width: 8 values a thread, from 4,096 columns on up to 32, so that
-// a row's sums cost few barriers and many rows are on a multiprocessor (131,072 rows of 1,024:
-// a warp with 32 values a thread 599 us, 128 threads with 8 see layer_norm_backward.cu).
+// Threads and vectors by the width: up to 32 values a thread, as what a row costs a thread besides its values (sums
+// across lanes, barriers, addresses) is as much as 15 values do.
 template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
 cudaError_t launch_back_team(const RowBackArgs &p, cudaStream_t s) {
     using B = BackTeam<ST, GT, DT, VEC, TT, NV>;
@@ -339,24 +387,21 @@ cudaError_t launch_back_team(const RowBackArgs &p, cudaStream_t s) {
 }
 template <typename ST, typename GT, typename DT, int VEC>
 cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
-    if constexpr (VEC == 8) {
-        if (p.f <= 64) return launch_back_team<ST, GT, DT, 8, 8, 1>(p, s);
-        if (p.f <= 256) return launch_back_team<ST, GT, DT, 8, 32, 1>(p, s);
-        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 8, 128, 1>(p, s);
-        if (p.f <= 2048) return launch_back_team<ST, GT, DT, 8, 256, 1>(p, s);
-        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 8, 512, 1>(p, s);
-        if (p.f <= 8192) return launch_back_team<ST, GT, DT, 8, 512, 2>(p, s);
-        if (p.f <= 16384) return launch_back_team<ST, GT, DT, 8, 512, 4>(p, s);
-    } else if constexpr (VEC == 4) {
-        if (p.f <= 64) return launch_back_team<ST, GT, DT, 4, 8, 2>(p, s);
-        if (p.f <= 256) return launch_back_team<ST, GT, DT, 4, 32, 2>(p, s);
-        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 4, 128, 2>(p, s);
-        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 4, 512, 2>(p, s);
-        if (p.f <= 8192) return launch_back_team<ST, GT, DT, 4, 512, 4>(p, s);
+    if constexpr (VEC > 1) {
+        constexpr int kN = 8 / VEC;                          // vectors of 8 values
+        if (p.f <= 64) return launch_back_team<ST, GT, DT, VEC, 8, kN>(p, s);
+        if (p.f <= 256) return launch_back_team<ST, GT, DT, VEC, 32, kN>(p, s);
+        if (p.f <= 512) return launch_back_team<ST, GT, DT, VEC, 32, 2 * kN>(p, s);
+        if (p.f <= 1024) return launch_back_team<ST, GT, DT, VEC, 32, 4 * kN>(p, s);
+        if (p.f <= 2048) return launch_back_team<ST, GT, DT, VEC, 64, 4 * kN>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, VEC, 128, 4 * kN>(p, s);
+        if (p.f <= 8192) return launch_back_team<ST, GT, DT, VEC, 256, 4 * kN>(p, s);
+        if (p.f <= 16384) return launch_back_team<ST, GT, DT, VEC, 512, 4 * kN>(p, s);
     } else {
         if (p.f <= 128) return launch_back_team<ST, GT, DT, 1, 32, 4>(p, s);
-        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 1, 128, 8>(p, s);
-        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 1, 512, 8>(p, s);
+        if (p.f <= 512) return launch_back_team<ST, GT, DT, 1, 32, 16>(p, s);
+        if (p.f <= 1024) return launch_back_team<ST, GT, DT, 1, 64, 16>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, 1, 256, 16>(p, s);
     }
     row_norm_back_long<ST, GT, DT, VEC><<<static_cast<unsigned>(p.n), 1024, 0, s>>>(p);
     if (p.part) {
@@ -368,11 +413,11 @@ cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
     return cudaGetLastError();
 }
 
+// Vectors of 16 bytes of the widest type: of fp32 vectors of 32 bytes, lanes side by side would meet on banks.
 template <typename ST, typename GT, typename DT>
 cudaError_t launch_back_types(const RowBackArgs &p, cudaStream_t s) {
-    if (p.vec == 8) return launch_back_vec<ST, GT, DT, 8>(p, s);
-    if (p.vec == 4) return launch_back_vec<ST, GT, DT, 4>(p, s);
-    return launch_back_vec<ST, GT, DT, 1>(p, s);
+    constexpr int kVec = sizeof(ST) + sizeof(GT) + sizeof(DT) == 6 ? 8 : 4;
+    return p.bulk ? launch_back_vec<ST, GT, DT, kVec>(p, s) : launch_back_vec<ST, GT, DT, 1>(p, s);
 }
 
 template <typename ST, typename GT>

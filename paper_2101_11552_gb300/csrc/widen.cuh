@@ -133,10 +133,11 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;
 // Inputs of a CTA of THREADS in shared memory: every thread's vectors lie in slots of its own, and it
 // alone reads them, so that copies are in flight while others are worked on, without registers and
 // without a barrier.  A vector of 32 bytes lies in two halves, so that lanes side by side read 16 bytes
-// side by side; they are copied by pairs of lanes, 64 bytes of memory in each copy of a pair, as 16 bytes
-// of every lane's 32 would ask L2 for each sector twice.  EACH vectors a thread take kAll bytes of a CTA; LANE:
-// bytes from a thread's part to the next one's, ROW: from one of its vectors to the next.
-template <typename T, int VEC, int EACH, int THREADS, int LANE = (VEC * sizeof(T) > 16 ? 16 : VEC * sizeof(T)),
+// side by side; lanes that hold SIDE vectors side by side in a row copy them together, 16 bytes after
+// 16 bytes: with 16 of its own 32 bytes a lane, L2 was asked for every sector twice.  EACH vectors a
+// thread take kAll bytes of a CTA; LANE: bytes from a thread's part to the next one's, ROW: from one of
+// its vectors to the next.
+template <typename T, int VEC, int EACH, int THREADS, int SIDE, int LANE = (VEC * sizeof(T) > 16 ? 16 : VEC * sizeof(T)),
           int ROW = (VEC * sizeof(T) > 16 ? 2 : 1) * THREADS * LANE>
 struct Slots {
     static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
@@ -145,16 +146,17 @@ struct Slots {
     char *at;
     __device__ __forceinline__ explicit Slots(char *stage) : at(stage + threadIdx.x * LANE) {}
     __device__ __forceinline__ char *part(int j, int h) const { return at + j * ROW + h * THREADS * LANE; }
-    // The vector at `from`, if left > 0 (values from there to the row's end, a multiple of VEC).  Vectors of lanes 2 i and
-    // 2 i + 1 lie side by side in a row and are copied in the same call; two halves are there
-    // for their thread after its wait and a barrier of the warp.
-    __device__ __forceinline__ void copy(int j, const T *from, int64_t left) const {
+    // The vector at `from`, if left > 0 (values from there to the row's end, a multiple of VEC).  Halves copied by
+    // neighbours are there for their thread after its wait and a barrier of the warp.
+    __device__ __forceinline__ void copy(int j, const T *from, int left) const {
         if constexpr (kParts == 2) {
-            const int odd = threadIdx.x & 1;
-            const char *even = reinterpret_cast<const char *>(from - odd * VEC) + odd * 16;
-            const int64_t rest = left + odd * VEC;
-            if (rest > 0) copy_async<16>(part(j, odd) - odd * LANE, even);
-            if (rest > VEC) copy_async<16>(part(j, odd) + (1 - odd) * LANE, even + 32);
+            const int l = threadIdx.x % SIDE, h = threadIdx.x & 1;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int away = k * SIDE / 2 + l / 2 - l;   // lanes to the vector whose half is copied
+                if (left - away * VEC > 0)
+                    copy_async<16>(part(j, h) + away * LANE, reinterpret_cast<const char *>(from + away * VEC) + h * 16);
+            }
         } else {
             if (left > 0) copy_async<kPart>(part(j, 0), from);
         }
@@ -191,6 +193,36 @@ struct Slots {
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// ---- bulk copies to shared memory ----------------------------------------------------------
+// One thread copies a run of bytes (16-byte aligned, a multiple of 16), which count down what a barrier in
+// shared memory expects; whoever reads them waits for the barrier's phase.
+__device__ __forceinline__ uint32_t shared_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void arrivals_init(uint64_t *bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_at(bar)), "r"(count) : "memory");
+}
+// The barriers are there for the copies; a barrier of the CTA follows.
+__device__ __forceinline__ void arrivals_ready() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void arrive_expecting(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_at(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(void *to, const void *from, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_at(to)),
+                 "l"(from), "r"(bytes), "r"(shared_at(bar))
+                 : "memory");
+}
+// Waits for the phase of the given parity to end: false after some seconds without it.
+__device__ __forceinline__ bool phase_done(uint64_t *bar, uint32_t parity) {
+    for (int i = 0; i < 1 << 20; ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(shared_at(bar)), "r"(parity)
+                     : "memory");
+        if (done) return true;
+    }
+    return false;
+}
 
 // VEC values to p (fp32, or bf16 bits), p aligned to the vector it is stored as: 16 bytes,
 // or 8 for four bf16 values.  The one rounding of a bf16 result is here.
