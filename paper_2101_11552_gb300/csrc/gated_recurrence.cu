@@ -1,5 +1,7 @@
 // Gated linear recurrence: the host side of both directions, and the kernel that describes the rows
 // (gated_recurrence.cuh: the method; gated_recurrence_forward.cuh, gated_recurrence_backward.cuh: the kernels).
+#include <mutex>
+
 #include "gated_recurrence.cuh"
 
 namespace tfg {
@@ -29,9 +31,11 @@ int scan_vector(const ScanArgs &p, int dtype, bool backward) {
     const auto at = [](const void *q, int bytes) { return reinterpret_cast<uintptr_t>(q) % bytes == 0; };
     const auto fits = [&](int vec) {
         if (p.f % vec || p.gate_ld % vec || p.x_ld % vec || !at(p.gate, 16) || !at(p.x, 16) || !at(p.initial, 16)) return false;
+        if (p.gate_ld * size >= int64_t(1) << 40 || p.x_ld * size >= int64_t(1) << 40) return false;   // strides that a map can have
         const int wide = p.out_bf16 ? vec * 2 : 16;          // bytes of a vector of out or its gradient
         if (!backward) return at(p.out, wide) && at(p.final_state, 16);
-        return at(p.g, wide) && at(p.grad_final, 16) && at(p.grad_initial, 16) && p.grad_gate_ld % vec == 0 &&
+        const int rows = p.out_bf16 ? 2 : 4;                 // dL/dout comes by copies of whole 16 bytes
+        return at(p.g, 16) && p.f * rows % 16 == 0 && at(p.grad_final, 16) && at(p.grad_initial, 16) && p.grad_gate_ld % vec == 0 &&
                p.grad_x_ld % vec == 0 && at(p.grad_gate, 16) && at(p.grad_x, 16);
     };
     const int vec = 16 / size;
@@ -58,6 +62,43 @@ void scan_geometry(ScanArgs &p, int vec, void *ws, int32_t *status) {
     }
 }
 
+using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps, looked up through the runtime (the library links no libcuda).
+EncodeTiledFn encode_tiled() {
+    static std::once_flag once;
+    static EncodeTiledFn fn = nullptr;
+    std::call_once(once, [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(f);
+    });
+    return fn;
+}
+
+// Rows of f values, ld apart, in tiles of kTileRows by `wide` channels.
+bool row_map(CUtensorMap &map, const void *rows, bool bf16, int64_t n, int64_t f, int64_t ld, int wide) {
+    const EncodeTiledFn encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(f), static_cast<cuuint64_t>(n)};
+    const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld) * (bf16 ? 2 : 4)};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(wide), kTileRows}, step[2] = {1, 1};
+    return encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(rows), dims,
+                  stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool scan_maps(const ScanArgs &p, int dtype, bool backward, ScanMaps &maps) {
+    const bool bf16 = dtype == TFG_BF16;
+    const int wide = bf16 ? ScanTile<8>::kWide : ScanTile<4>::kWide;
+    return row_map(maps.gate, p.gate, bf16, p.n, p.f, p.gate_ld, wide) && row_map(maps.x, p.x, bf16, p.n, p.f, p.x_ld, wide) &&
+           (!backward || !p.g || row_map(maps.g, p.g, p.out_bf16, p.n, p.f, p.f, wide));
+}
+
 cudaError_t scan_plan(const ScanArgs &p, void *ws, cudaStream_t s) {
     if (p.status_all) return cudaSuccess;
     const ScanSpace space(p.n, p.f);
@@ -72,10 +113,10 @@ cudaError_t scan_plan(const ScanArgs &p, void *ws, cudaStream_t s) {
 
 size_t gated_recurrence_workspace_bytes(int64_t n, int64_t f) { return ScanSpace(n, f).bytes; }
 
-cudaError_t launch_scan_forward_f32(const ScanArgs &p, int vec, int kind, cudaStream_t s);
-cudaError_t launch_scan_forward_bf16(const ScanArgs &p, int vec, int kind, cudaStream_t s);
-cudaError_t launch_scan_backward_f32(const ScanArgs &p, int vec, int kind, cudaStream_t s);
-cudaError_t launch_scan_backward_bf16(const ScanArgs &p, int vec, int kind, cudaStream_t s);
+cudaError_t launch_scan_forward_f32(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s);
+cudaError_t launch_scan_forward_bf16(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s);
+cudaError_t launch_scan_backward_f32(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s);
+cudaError_t launch_scan_backward_bf16(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s);
 
 cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
                                     const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
@@ -88,7 +129,9 @@ cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const voi
     scan_geometry(p, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);
     if (e != cudaSuccess || p.checkers + p.tiles * p.strips == 0) return e;
-    return dtype == TFG_BF16 ? launch_scan_forward_bf16(p, vec, kind, s) : launch_scan_forward_f32(p, vec, kind, s);
+    ScanMaps maps;
+    if (vec > 1 && p.tiles > 0 && !scan_maps(p, dtype, false, maps)) return cudaErrorNotSupported;
+    return dtype == TFG_BF16 ? launch_scan_forward_bf16(p, maps, vec, kind, s) : launch_scan_forward_f32(p, maps, vec, kind, s);
 }
 
 cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
@@ -106,7 +149,9 @@ cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, 
     scan_geometry(p, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);
     if (e != cudaSuccess || p.checkers + p.tiles * p.strips == 0) return e;
-    return dtype == TFG_BF16 ? launch_scan_backward_bf16(p, vec, kind, s) : launch_scan_backward_f32(p, vec, kind, s);
+    ScanMaps maps;
+    if (vec > 1 && p.tiles > 0 && !scan_maps(p, dtype, true, maps)) return cudaErrorNotSupported;
+    return dtype == TFG_BF16 ? launch_scan_backward_bf16(p, maps, vec, kind, s) : launch_scan_backward_f32(p, maps, vec, kind, s);
 }
 
 }  // namespace tfg

@@ -5,10 +5,10 @@
 //   sigmoid gate: a = 1 / (1 + e^-z), b = (1 - a) x;   exp gate: a = e^z, b = x
 //
 // A row is an affine map of the state, and maps compose: (A, B) then (a, b) is (a A, a B + b).
-// A CTA takes a tile of 128 rows by 32 or 64 channels and holds its gates and inputs in
-// registers; each thread composes the maps of its few rows, the threads' maps are composed
+// A CTA takes a tile of 128 rows by 32 or 64 channels into shared memory (one tensor copy for an array; value
+// by value where rows are not whole 16 bytes); each thread composes the maps of its few rows, the threads' maps are composed
 // down the tile in shared memory, the tile's map is published, the state that enters the tile
-// is found from what the tiles before it published, and a second walk over the registers makes the
+// is found from what the tiles before it published, and a second walk over the tile makes the
 // outputs.  So the inputs come from memory once, however long a sequence is.  A row that begins
 // a sequence forgets what comes before it, so tiles need not know sequences.
 //
@@ -93,6 +93,11 @@ struct ScanSpace {
     }
 };
 
+
+// Tensor maps of gate, x and dL/dout, for tiles of a vector width above 1.
+struct ScanMaps {
+    CUtensorMap gate, x, g;
+};
 
 // CTAs of a launch, with at most `resident` on a multiprocessor.
 inline unsigned scan_ctas(const ScanArgs &p, int resident) {
@@ -286,6 +291,43 @@ __device__ __forceinline__ void copy_plan(const ScanArgs &p, int64_t tile, TileR
                        reinterpret_cast<const char *>(p.plan + tile) + threadIdx.x * 16);
 }
 
+// A thread's vectors of a tile that lies in shared memory row by row.
+template <typename T, int VEC>
+struct TileRow {
+    static constexpr int kBytes = kTileRows * ScanTile<VEC>::kWide * static_cast<int>(sizeof(T));
+    T *at;
+    __device__ __forceinline__ explicit TileRow(char *tile)
+        : at(reinterpret_cast<T *>(tile) + threadIdx.x / ScanTile<VEC>::kAcross * ScanTile<VEC>::kEach * ScanTile<VEC>::kWide +
+             threadIdx.x % ScanTile<VEC>::kAcross * VEC) {}
+    __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
+        const T *p = at + j * ScanTile<VEC>::kWide;
+        if constexpr (VEC * sizeof(T) == 32) {
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(p + h);
+                v[h] = q.x; v[h + 1] = q.y; v[h + 2] = q.z; v[h + 3] = q.w;
+            }
+        } else {
+            VecLoad<T, VEC>::widen(load_plain<T, VEC>(p), v);
+        }
+    }
+    __device__ __forceinline__ void zero(int j) const {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) at[j * ScanTile<VEC>::kWide + q] = T(0);
+    }
+};
+// The gates of a thread, taken from their tile before the decays are written over it.
+template <typename T, int VEC>
+struct HeldGate {
+    typename VecLoad<T, VEC>::Raw r[ScanTile<VEC>::kEach];
+    __device__ __forceinline__ explicit HeldGate(char *tile) {
+        const TileRow<T, VEC> from(tile);
+#pragma unroll
+        for (int j = 0; j < ScanTile<VEC>::kEach; ++j) r[j] = load_plain<T, VEC>(from.at + j * ScanTile<VEC>::kWide);
+    }
+    __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const { VecLoad<T, VEC>::widen(r[j], v); }
+};
+
 // A job: a tile in order of work, and a strip of channels.
 struct Job {
     int64_t order;
@@ -310,6 +352,7 @@ struct Jobs {
         if (threadIdx.x == 0) asked = p.linked ? atomicAdd(p.next, 1u) : count;
     }
     __device__ __forceinline__ bool next(const ScanArgs &p, uint32_t &job) {
+        before_copies();
         __syncthreads();
         if (threadIdx.x == 0) *s_next = asked;
         __syncthreads();

@@ -18,26 +18,26 @@
 namespace tfg {
 namespace {
 
-// A tile's inputs; a - 1 takes the gates' place, in slots wide enough for it.
-template <typename XT, typename GT, int VEC>
-struct BackwardStage {
-    using T = ScanTile<VEC>;
-    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
-    using In = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross>;
-    using Grad = Slots<GT, VEC, T::kEach, kScanThreads, T::kAcross>;
+// A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
+template <typename XT, typename GT>
+struct BackwardSlots {
+    using T = ScanTile<1>;
+    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
+    using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
+    using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
+    using Grad = Slots<GT, 1, T::kEach, kScanThreads, T::kAcross>;
     static constexpr int kBytes = Decay::kAll + In::kAll + Grad::kAll;
     Gate z;
     Decay d;
     In x;
     Grad g;
-    __device__ __forceinline__ explicit BackwardStage(char *stage)
+    __device__ __forceinline__ explicit BackwardSlots(char *stage)
         : z(stage), d(stage), x(stage + Decay::kAll), g(stage + Decay::kAll + In::kAll) {}
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows + group * T::kEach;
-        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = static_cast<int>(min64(p.f - c, 1 << 20));
+        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane;
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = c < p.f ? 1 : 0;
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
         const GT *gp = static_cast<const GT *>(p.g) + r0 * p.f + c;
 #pragma unroll
@@ -46,11 +46,37 @@ struct BackwardStage {
                 z.copy(j, zp + j * p.gate_ld, cols);
                 x.copy(j, xp + j * p.x_ld, cols);
                 if (p.g) g.copy(j, gp + j * p.f, cols);
-                else g.zero(j);
             }
         if (p.linked) copy_plan(p, tile, rows);
     }
 };
+// A tile's inputs by tensor copies; the decays take the gates' place.
+template <typename XT, typename GT, int VEC>
+struct BackwardTile {
+    using T = ScanTile<VEC>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using In = TileRow<XT, VEC>;
+    using Grad = TileRow<GT, VEC>;
+    static constexpr int kBytes = Decay::kAll + In::kBytes + Grad::kBytes;
+    char *stage;
+    Decay d;
+    In x;
+    Grad g;
+    __device__ __forceinline__ explicit BackwardTile(char *s) : stage(s), d(s), x(s + Decay::kAll), g(s + Decay::kAll + In::kBytes) {}
+    __device__ __forceinline__ void copy(const ScanArgs &p, const ScanMaps &maps, const Job &job, TileRows &rows, uint64_t *bar) const {
+        if (threadIdx.x != 0) return;
+        arrive_expecting(bar, 2 * In::kBytes + (p.g ? Grad::kBytes : 0) + (p.linked ? static_cast<uint32_t>(sizeof(TileRows)) : 0u));
+        const int64_t tile = p.tiles - 1 - job.order;
+        const int c = job.strip * T::kWide, r = static_cast<int>(tile) * kTileRows;
+        tile_copy(stage, &maps.gate, c, r, bar);
+        tile_copy(stage + Decay::kAll, &maps.x, c, r, bar);
+        if (p.g) tile_copy(stage + Decay::kAll + In::kBytes, &maps.g, c, r, bar);
+        if (p.linked) bulk_copy(&rows, p.plan + tile, sizeof(TileRows), bar);
+    }
+};
+template <typename XT, typename GT, int VEC> struct BackwardStageOf { using Type = BackwardTile<XT, GT, VEC>; };
+template <typename XT, typename GT> struct BackwardStageOf<XT, GT, 1> { using Type = BackwardSlots<XT, GT>; };
+template <typename XT, typename GT, int VEC> using BackwardStage = typename BackwardStageOf<XT, GT, VEC>::Type;
 
 // CTAs of a multiprocessor, by shared memory: 75 KB where all is bf16 but the decay.
 template <typename XT, typename GT, int VEC>
@@ -136,11 +162,13 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
 }
 
 template <typename XT, typename GT, int VEC, int KIND>
-__global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan_backward(ScanArgs p) {
+__global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
+    scan_backward(ScanArgs p, const __grid_constant__ ScanMaps maps) {
     using T = ScanTile<VEC>;
     using Stage = BackwardStage<XT, GT, VEC>;
-    extern __shared__ __align__(16) char s_stage[];
+    extern __shared__ __align__(128) char s_stage[];
     __shared__ TileRows rows;
+    __shared__ uint64_t s_full;
     __shared__ __align__(16) float s_a[kScanWarps][T::kWide], s_b[kScanWarps][T::kWide];      // of the states
     __shared__ __align__(16) float s_u[kScanWarps][T::kWide], s_w[kScanWarps][T::kWide];      // of the adjoint
     __shared__ float2 s_part[kScanThreads / T::kWide][T::kWide];
@@ -151,11 +179,20 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
     const Stage in_stage(s_stage);
     Jobs jobs(p, &s_next);
-    uint32_t number;
+    if (VEC > 1 && threadIdx.x == 0) {
+        arrivals_init(&s_full, 1);
+        arrivals_ready();
+    }
+    if (!p.g) {                                              // nothing is copied there
+#pragma unroll
+        for (int j = 0; j < T::kEach; ++j) in_stage.g.zero(j);
+    }
+    uint32_t number, parity = 0;
 #pragma unroll 1
     while (jobs.next(p, number)) {
         const Job job(p, number);
-        in_stage.copy(p, job, rows);
+        if constexpr (VEC > 1) in_stage.copy(p, maps, job, rows, &s_full);
+        else in_stage.copy(p, job, rows);
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows;
         const int64_t c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
         const bool on = c < p.f, column = static_cast<int>(threadIdx.x) < T::kWide;
@@ -166,9 +203,14 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan
         const int sc = static_cast<int>(threadIdx.x) - T::kWide;                     // threads of the next columns: states
         float state = 0.f;
         if (sc >= 0 && sc < T::kWide && c0 + sc < p.f) state = __ldg(p.entered + tile * p.f + c0 + sc);
-        copies_done();
-        if (p.linked) __syncthreads();                           // the plan is there
-        else find_rows(p, rows);
+        if constexpr (VEC > 1) {
+            if (!phase_done(&s_full, parity)) set_status(p.status, TFG_ERR_TIMEOUT);
+            parity ^= 1u;
+        } else {
+            copies_done();
+            if (p.linked) __syncthreads();                       // the plan is there
+        }
+        if (!p.linked) find_rows(p, rows);
         const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
                        in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps),
                        cut_warps = warps_word(rows.cut_warps);
@@ -177,11 +219,16 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan
 
         // the thread's maps: of the state down its rows, of the adjoint up
         float a[VEC], b[VEC], u[VEC], w[VEC];
+        const auto z = [&] {
+            if constexpr (VEC > 1) return HeldGate<XT, VEC>(s_stage);
+            else return in_stage.z;
+        }();
+        if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
         if (plain) {
-            compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+            compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
             compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, u, w);
         } else {
-            compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+            compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
             compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
         }
         bool cut = begin != 0u, cut_up = (begin | end) != 0u;
@@ -233,24 +280,24 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>) scan
 }
 
 template <typename XT, typename GT, int VEC, int KIND>
-cudaError_t launch_backward(const ScanArgs &p, cudaStream_t s) {
+cudaError_t launch_backward(const ScanArgs &p, const ScanMaps &maps, cudaStream_t s) {
     constexpr int kShared = BackwardStage<XT, GT, VEC>::kBytes;
     if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
         const cudaError_t e =
             cudaFuncSetAttribute(scan_backward<XT, GT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
         if (e != cudaSuccess) return e;
     }
-    scan_backward<XT, GT, VEC, KIND><<<scan_ctas(p, kBackwardCtas<XT, GT, VEC>), kScanThreads, kShared, s>>>(p);
+    scan_backward<XT, GT, VEC, KIND><<<scan_ctas(p, kBackwardCtas<XT, GT, VEC>), kScanThreads, kShared, s>>>(p, maps);
     return cudaGetLastError();
 }
 template <typename XT, typename GT, int VEC>
-cudaError_t launch_backward_kind(const ScanArgs &p, int kind, cudaStream_t s) {
-    return kind == TFG_GATE_SIGMOID ? launch_backward<XT, GT, VEC, TFG_GATE_SIGMOID>(p, s)
-                                    : launch_backward<XT, GT, VEC, TFG_GATE_EXP>(p, s);
+cudaError_t launch_backward_kind(const ScanArgs &p, const ScanMaps &maps, int kind, cudaStream_t s) {
+    return kind == TFG_GATE_SIGMOID ? launch_backward<XT, GT, VEC, TFG_GATE_SIGMOID>(p, maps, s)
+                                    : launch_backward<XT, GT, VEC, TFG_GATE_EXP>(p, maps, s);
 }
 template <typename XT, int VEC>
-cudaError_t launch_backward_grad(const ScanArgs &p, int kind, cudaStream_t s) {
-    return p.out_bf16 ? launch_backward_kind<XT, uint16_t, VEC>(p, kind, s) : launch_backward_kind<XT, float, VEC>(p, kind, s);
+cudaError_t launch_backward_grad(const ScanArgs &p, const ScanMaps &maps, int kind, cudaStream_t s) {
+    return p.out_bf16 ? launch_backward_kind<XT, uint16_t, VEC>(p, maps, kind, s) : launch_backward_kind<XT, float, VEC>(p, maps, kind, s);
 }
 
 }  // namespace

@@ -7,22 +7,22 @@
 namespace tfg {
 namespace {
 
-// A tile's inputs; a - 1 takes the gates' place, in slots wide enough for it.
-template <typename XT, int VEC>
-struct ForwardStage {
-    using T = ScanTile<VEC>;
-    using Gate = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
-    using In = Slots<XT, VEC, T::kEach, kScanThreads, T::kAcross>;
+// A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
+template <typename XT>
+struct ForwardSlots {
+    using T = ScanTile<1>;
+    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
+    using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
+    using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
     static constexpr int kBytes = Decay::kAll + In::kAll;
     Gate z;
     Decay d;
     In x;
-    __device__ __forceinline__ explicit ForwardStage(char *stage) : z(stage), d(stage), x(stage + Decay::kAll) {}
+    __device__ __forceinline__ explicit ForwardSlots(char *stage) : z(stage), d(stage), x(stage + Decay::kAll) {}
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
-        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane * VEC, r0 = job.order * kTileRows + group * T::kEach;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = static_cast<int>(min64(p.f - c, 1 << 20));
+        const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane, r0 = job.order * kTileRows + group * T::kEach;
+        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = c < p.f ? 1 : 0;
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
@@ -33,6 +33,29 @@ struct ForwardStage {
         if (p.linked) copy_plan(p, job.order, rows);
     }
 };
+// A tile's inputs by tensor copies; the decays take the gates' place.
+template <typename XT, int VEC>
+struct ForwardTile {
+    using T = ScanTile<VEC>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using In = TileRow<XT, VEC>;
+    static constexpr int kBytes = Decay::kAll + In::kBytes;
+    char *stage;
+    Decay d;
+    In x;
+    __device__ __forceinline__ explicit ForwardTile(char *s) : stage(s), d(s), x(s + Decay::kAll) {}
+    __device__ __forceinline__ void copy(const ScanArgs &p, const ScanMaps &maps, const Job &job, TileRows &rows, uint64_t *bar) const {
+        if (threadIdx.x != 0) return;
+        arrive_expecting(bar, 2 * In::kBytes + (p.linked ? static_cast<uint32_t>(sizeof(TileRows)) : 0u));
+        const int c = job.strip * T::kWide, r = static_cast<int>(job.order) * kTileRows;
+        tile_copy(stage, &maps.gate, c, r, bar);
+        tile_copy(stage + Decay::kAll, &maps.x, c, r, bar);
+        if (p.linked) bulk_copy(&rows, p.plan + job.order, sizeof(TileRows), bar);
+    }
+};
+template <typename XT, int VEC> struct ForwardStageOf { using Type = ForwardTile<XT, VEC>; };
+template <typename XT> struct ForwardStageOf<XT, 1> { using Type = ForwardSlots<XT>; };
+template <typename XT, int VEC> using ForwardStage = typename ForwardStageOf<XT, VEC>::Type;
 
 // CTAs of a multiprocessor: as many as their shared memory allows (55 and 39 KB), 64 registers a thread.
 constexpr int kForwardCtas = 4;
@@ -56,11 +79,13 @@ __device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const
 }
 
 template <typename XT, typename OT, int VEC, int KIND>
-__global__ void __launch_bounds__(kScanThreads, kForwardCtas) scan_forward(ScanArgs p) {
+__global__ void __launch_bounds__(kScanThreads, kForwardCtas)
+    scan_forward(ScanArgs p, const __grid_constant__ ScanMaps maps) {
     using T = ScanTile<VEC>;
     using Stage = ForwardStage<XT, VEC>;
-    extern __shared__ __align__(16) char s_stage[];
+    extern __shared__ __align__(128) char s_stage[];
     __shared__ TileRows rows;
+    __shared__ uint64_t s_full;
     __shared__ __align__(16) float s_a[kScanWarps][T::kWide], s_b[kScanWarps][T::kWide];
     __shared__ float2 s_part[kScanThreads / T::kWide][T::kWide];
     __shared__ float s_state[T::kWide];
@@ -70,28 +95,43 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas) scan_forward(ScanA
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
     const Stage in_stage(s_stage);
     Jobs jobs(p, &s_next);
-    uint32_t number;
+    if (VEC > 1 && threadIdx.x == 0) {
+        arrivals_init(&s_full, 1);
+        arrivals_ready();
+    }
+    uint32_t number, parity = 0;
 #pragma unroll 1
     while (jobs.next(p, number)) {
         const Job job(p, number);
-        in_stage.copy(p, job, rows);
+        if constexpr (VEC > 1) in_stage.copy(p, maps, job, rows, &s_full);
+        else in_stage.copy(p, job, rows);
         const int64_t r0 = job.order * kTileRows, c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
         const bool on = c < p.f;
         if (p.linked && warp == 0) {
             const int from = cut_before<false>(p, job.order);
             if (threadIdx.x == 0) s_from = from;
         }
-        copies_done();
-        if (p.linked) __syncthreads();                           // the plan is there
-        else find_rows(p, rows);
+        if constexpr (VEC > 1) {
+            if (!phase_done(&s_full, parity)) set_status(p.status, TFG_ERR_TIMEOUT);
+            parity ^= 1u;
+        } else {
+            copies_done();
+            if (p.linked) __syncthreads();                       // the plan is there
+        }
+        if (!p.linked) find_rows(p, rows);
         const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
                        in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps);
         const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
         const int32_t *seq = rows.seq + group * T::kEach;
 
         float a[VEC], b[VEC];
-        if (plain) compose_down<true, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-        else compose_down<false, KIND, VEC, T::kEach>(p, in_stage.z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+        const auto z = [&] {
+            if constexpr (VEC > 1) return HeldGate<XT, VEC>(s_stage);
+            else return in_stage.z;
+        }();
+        if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
+        if (plain) compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
+        else compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
         bool cut = begin != 0u;
         scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
         __syncthreads();
@@ -134,21 +174,21 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas) scan_forward(ScanA
 }
 
 template <typename XT, typename OT, int VEC, int KIND>
-cudaError_t launch_forward(const ScanArgs &p, cudaStream_t s) {
+cudaError_t launch_forward(const ScanArgs &p, const ScanMaps &maps, cudaStream_t s) {
     constexpr int kShared = ForwardStage<XT, VEC>::kBytes;
     if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
         const cudaError_t e =
             cudaFuncSetAttribute(scan_forward<XT, OT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
         if (e != cudaSuccess) return e;
     }
-    scan_forward<XT, OT, VEC, KIND><<<scan_ctas(p, kForwardCtas), kScanThreads, kShared, s>>>(p);
+    scan_forward<XT, OT, VEC, KIND><<<scan_ctas(p, kForwardCtas), kScanThreads, kShared, s>>>(p, maps);
     return cudaGetLastError();
 }
 template <typename XT, int VEC>
-cudaError_t launch_forward_kind(const ScanArgs &p, int kind, cudaStream_t s) {
+cudaError_t launch_forward_kind(const ScanArgs &p, const ScanMaps &maps, int kind, cudaStream_t s) {
     if (kind == TFG_GATE_SIGMOID)
-        return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_SIGMOID>(p, s) : launch_forward<XT, float, VEC, TFG_GATE_SIGMOID>(p, s);
-    return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_EXP>(p, s) : launch_forward<XT, float, VEC, TFG_GATE_EXP>(p, s);
+        return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_SIGMOID>(p, maps, s) : launch_forward<XT, float, VEC, TFG_GATE_SIGMOID>(p, maps, s);
+    return p.out_bf16 ? launch_forward<XT, uint16_t, VEC, TFG_GATE_EXP>(p, maps, s) : launch_forward<XT, float, VEC, TFG_GATE_EXP>(p, maps, s);
 }
 
 }  // namespace

@@ -104,12 +104,12 @@ struct BackTeam {
     static constexpr int kHeld = VEC * NV;                               // values a thread
     static constexpr int kS = kThreads * kHeld * sizeof(ST), kG = kThreads * kHeld * sizeof(GT), kD = kThreads * kHeld * sizeof(DT);
     static constexpr int kStageBytes = (kS + kG + kD + 15) / 16 * 16;
-    // up to 8 values a thread are kept in registers from the sums to the gradient, more are read again
-    static constexpr bool kKeeps = kHeld <= 8;
+    // up to 16 values a thread are kept in registers from the sums to the gradient, more are read again
+    static constexpr bool kKeeps = kHeld <= 16;
     static constexpr int kKept = kKeeps ? NV : 1;
     // CTAs of a multiprocessor by their registers: 512 threads of 128, 768 of 80 where few values are held;
     // rows on their way: as many as those leave room for
-    static constexpr int kWant = (kKeeps ? 768 : 512) / kThreads;
+    static constexpr int kWant = (kHeld <= 8 ? 768 : 512) / kThreads;
     static constexpr int kRoom = 216 * 1024 / kWant / kStageBytes;
     static constexpr int kStages = kRoom < 1 ? 1 : (kRoom < 4 ? kRoom : 4);
     static constexpr int kShared = kStages * kStageBytes;
@@ -393,9 +393,9 @@ cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
         if (p.f <= 256) return launch_back_team<ST, GT, DT, VEC, 32, kN>(p, s);
         if (p.f <= 512) return launch_back_team<ST, GT, DT, VEC, 32, 2 * kN>(p, s);
         if (p.f <= 1024) return launch_back_team<ST, GT, DT, VEC, 32, 4 * kN>(p, s);
-        if (p.f <= 2048) return launch_back_team<ST, GT, DT, VEC, 64, 4 * kN>(p, s);
-        if (p.f <= 4096) return launch_back_team<ST, GT, DT, VEC, 128, 4 * kN>(p, s);
-        if (p.f <= 8192) return launch_back_team<ST, GT, DT, VEC, 256, 4 * kN>(p, s);
+        if (p.f <= 2048) return launch_back_team<ST, GT, DT, VEC, 128, 2 * kN>(p, s);
+        if (p.f <= 4096) return launch_back_team<ST, GT, DT, VEC, 256, 2 * kN>(p, s);
+        if (p.f <= 8192) return launch_back_team<ST, GT, DT, VEC, 512, 2 * kN>(p, s);
         if (p.f <= 16384) return launch_back_team<ST, GT, DT, VEC, 512, 4 * kN>(p, s);
     } else {
         if (p.f <= 128) return launch_back_team<ST, GT, DT, 1, 32, 4>(p, s);

@@ -2,6 +2,7 @@
 // may be fp32 or bf16 (embedding lookup, group norm, clipped gradients).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -211,6 +212,16 @@ __device__ __forceinline__ void bulk_copy(void *to, const void *from, uint32_t b
                  "l"(from), "r"(bytes), "r"(shared_at(bar))
                  : "memory");
 }
+// A tile of an array of rows by its tensor map (gated_recurrence.cu makes them): columns from x, rows from y on; zeros
+// outside the array.  x * the value's size is a multiple of 16 bytes, `to` of 128.
+__device__ __forceinline__ void tile_copy(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                     shared_at(to)),
+                 "l"(map), "r"(x), "r"(y), "r"(shared_at(bar))
+                 : "memory");
+}
+// What the thread has read and written in shared memory comes before copies issued behind a barrier that follows.
+__device__ __forceinline__ void before_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Waits for the phase of the given parity to end: false after some seconds without it.
 __device__ __forceinline__ bool phase_done(uint64_t *bar, uint32_t parity) {
     for (int i = 0; i < 1 << 20; ++i) {
