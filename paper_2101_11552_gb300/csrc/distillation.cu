@@ -9,6 +9,8 @@
 // the sum of e^((s - m) / tau), the second writes the gradient from them; the terms at the teacher's classes are
 // written over it.  q is formed from s - m, which is exact or nearly so, and loss terms from
 // (s - m) / tau - log(sum), so logits that share a large offset lose nothing.
+#include <type_traits>
+
 #include "widen.cuh"
 
 namespace tfg {
@@ -36,6 +38,16 @@ struct DistilArgs {
 constexpr int kRowThreads = 512, kDistilThreads = 256;       // a CTA for a row; teams of a warp
 constexpr int kWarpClasses = 2048, kWarpTop = 128;           // rows that a warp takes
 constexpr int kInFlight = 4;                                 // vectors that a thread loads before it uses them
+// Rows held in shared memory, and the threads of a CTA that takes one: so many that rows of the size, and the
+// threads, fill a multiprocessor (from 112 KB on one row at a time).  Longer rows are read twice.  They come in
+// copies of kChunkBytes, each with a barrier, so that the first pass begins with the first of them; the loss alone
+// needs no more than kRing of them at a time.
+constexpr int kHold128 = 16 * 1024, kHold256 = 52 * 1024, kHoldMost = 222 * 1024;
+constexpr int kChunkBytes = 16 * 1024, kChunks = (kHoldMost + kChunkBytes - 1) / kChunkBytes, kRing = 6;
+
+// What a kernel makes of a row: the loss alone, the gradient from the forward's statistics, or both; with
+// the row held, or chunks of it.
+constexpr int kLoss = 0, kBack = 1, kBoth = 2, kBothHeld = 3, kLossRing = 4;
 
 template <int TT>
 __device__ __forceinline__ void team_sync() {
@@ -65,10 +77,7 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY
 struct Running {
     float m = -INFINITY, sum = 0.f;
     template <int VEC>
-    __device__ __forceinline__ void add(const float (&s)[VEC], float scale) {
-        float most = s[0];
-#pragma unroll
-        for (int q = 1; q < VEC; ++q) most = fmaxf(most, s[q]);
+    __device__ __forceinline__ void add(const float (&s)[VEC], float most, float scale) {
         if (most > m) {
             sum *= exp2_of((m - most) * scale);              // 0 at first
             m = most;
@@ -81,11 +90,32 @@ struct Running {
         mul_vec(e, by);
 #pragma unroll
         for (int q = 0; q < VEC; ++q) e[q] = exp2_of(e[q]);
+        if constexpr (VEC == 8) {                            // pairs by packed additions
+            float2 p = add2(make_float2(e[0], e[1]), make_float2(e[4], e[5])), q = add2(make_float2(e[2], e[3]), make_float2(e[6], e[7]));
+            p = add2(p, q);
+            sum += p.x + p.y;
+        } else if constexpr (VEC == 4) {
+            const float2 p = add2(make_float2(e[0], e[1]), make_float2(e[2], e[3]));
+            sum += p.x + p.y;
+        } else {
+            sum += e[0];
+        }
+    }
+    // VEC values as they lie in memory; the largest of bf16 values two at a time.
+    template <typename XT, int VEC>
+    __device__ __forceinline__ void add_raw(const typename VecLoad<XT, VEC>::Raw &raw, float scale) {
+        float s[VEC], most;
+        VecLoad<XT, VEC>::widen(raw, s);
+        if constexpr (sizeof(XT) == 2 && VEC == 8) {
+            const auto pair = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); };
+            const __nv_bfloat162 p = __hmax2(__hmax2(pair(raw.x), pair(raw.y)), __hmax2(pair(raw.z), pair(raw.w)));
+            most = fmaxf(__low2float(p), __high2float(p));
+        } else {
+            most = s[0];
 #pragma unroll
-        for (int o = VEC / 2; o > 0; o >>= 1)
-#pragma unroll
-            for (int q = 0; q < o; ++q) e[q] += e[q + o];
-        sum += e[0];
+            for (int q = 1; q < VEC; ++q) most = fmaxf(most, s[q]);
+        }
+        add(s, most, scale);
     }
 };
 
@@ -105,6 +135,56 @@ struct RowSpan {
         }
     }
     __device__ __forceinline__ int64_t loose_at(int i) const { return i < head ? i : vecs * VEC + i; }
+};
+
+// Vectors i, i + TT, ... of a row, all in flight.
+template <int TT, typename XT, int VEC>
+__device__ __forceinline__ void load_vectors(const RowSpan<XT, VEC> &r, int64_t i, RowVec<XT, VEC> (&raw)[kInFlight]) {
+#pragma unroll
+    for (int j = 0; j < kInFlight; ++j)
+        if (i + j * TT < r.vecs) raw[j].load(r.row + r.head + (i + j * TT) * VEC);
+}
+
+// The vectors of a row in shared memory, in chunks: chunk c in slot c % SLOTS.
+template <typename XT, int VEC, int SLOTS>
+struct HeldRow {
+    static constexpr int kVecs = kChunkBytes / 16;           // of a chunk
+    char *data;
+    uint64_t *bars;
+    __device__ __forceinline__ int chunks(const RowSpan<XT, VEC> &r) const { return static_cast<int>((r.vecs + kVecs - 1) / kVecs); }
+    __device__ __forceinline__ void copy(const RowSpan<XT, VEC> &r, int chunk) const {
+        const int slot = chunk % SLOTS;
+        const int64_t first = static_cast<int64_t>(chunk) * kVecs;
+        const uint32_t bytes = static_cast<uint32_t>(min64(kVecs, r.vecs - first)) * 16;
+        arrive_expecting(&bars[slot], bytes);
+        bulk_copy(data + slot * kChunkBytes, r.row + r.head + first * VEC, bytes, &bars[slot]);
+    }
+    // false: the chunk did not arrive
+    __device__ __forceinline__ bool wait(int chunk) const {
+        return phase_done(&bars[chunk % SLOTS], static_cast<uint32_t>(chunk / SLOTS) & 1u);
+    }
+    __device__ __forceinline__ typename VecLoad<XT, VEC>::Raw raw(int i) const {
+        return load_plain<XT, VEC>(reinterpret_cast<const XT *>(data) + i * VEC);
+    }
+    __device__ __forceinline__ void widen(int64_t i, float (&v)[VEC]) const {
+        VecLoad<XT, VEC>::widen(load_plain<XT, VEC>(reinterpret_cast<const XT *>(data) + i * VEC), v);
+    }
+    __device__ __forceinline__ float value(const RowSpan<XT, VEC> &r, int64_t c) const {
+        float v[1];
+        const int64_t i = c - r.head;
+        if (i >= 0 && i < r.vecs * VEC) VecLoad<XT, 1>::widen(load_plain<XT, 1>(reinterpret_cast<const XT *>(data) + i), v);
+        else VecLoad<XT, 1>::load(r.row + c, v);
+        return v[0];
+    }
+};
+struct NotHeld {
+    template <typename R>
+    __device__ __forceinline__ float value(const R &r, int64_t c) const {
+        float v[1];
+        using XT = typename std::remove_const<typename std::remove_pointer<decltype(r.row)>::type>::type;
+        VecLoad<XT, 1>::load(r.row + c, v);
+        return v[0];
+    }
 };
 
 // The teacher's side of a row, in the team's shared memory: classes (-1: padding) and p.
@@ -147,51 +227,63 @@ __device__ __forceinline__ void load_top(const DistilArgs &a, int64_t row, int t
 }
 
 // p in place of the teacher's logits; the terms of the loss.
-template <int TT, typename XT>
-__device__ __forceinline__ float top_terms(const DistilArgs &a, const XT *row, int t, float *scratch, float m, float log_sum,
-                                           Top &top) {
+template <int TT, bool TERMS, typename Span, typename Held>
+__device__ __forceinline__ float top_terms(const DistilArgs &a, const Span &r, const Held &held, int t, float *scratch, float m,
+                                           float log_sum, Top &top) {
     float terms = 0.f;
     const float per_tau = 1.f / a.tau;
     for (int i = t; i < a.k; i += TT) {
         if (top.ids[i] < 0) continue;
         const float log_p = fmaf(top.p[i] - top.most, per_tau, -top.log_sum), p = expf(log_p);
         top.p[i] = p;
-        if (row && p != 0.f) {
-            float s[1];
-            VecLoad<XT, 1>::load(row + top.ids[i], s);
-            terms = fmaf(p, log_p - fmaf(s[0] - m, per_tau, -log_sum), terms);
-        }
+        if (TERMS && p != 0.f) terms = fmaf(p, log_p - fmaf(held.value(r, top.ids[i]) - m, per_tau, -log_sum), terms);
     }
-    return row ? team_fold<TT>(terms, scratch, Add{}) : 0.f;
+    return TERMS ? team_fold<TT>(terms, scratch, Add{}) : 0.f;
+}
+
+// f q of VEC logits in e.
+template <int VEC>
+__device__ __forceinline__ void scaled_q(float (&e)[VEC], float away, float scale, float times) {
+    const float less[1] = {away}, by[1] = {scale}, f[1] = {times};
+    add_vec(e, less);
+    mul_vec(e, by);
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) e[q] = exp2_of(e[q]);
+    mul_vec(e, f);
 }
 
 // grad = f (q - p) of a row.
-template <int TT, typename XT, int VEC>
-__device__ __forceinline__ void write_gradient(const DistilArgs &a, const RowSpan<XT, VEC> &r, XT *out, int t, float m,
-                                               float sum, float f, const Top &top) {
-    const float away[1] = {-finite_or_zero(m)}, by[1] = {a.scale}, times[1] = {f / sum};
-    for (int64_t i0 = t; i0 < r.vecs; i0 += kInFlight * TT) {
-        RowVec<XT, VEC> raw[kInFlight];
+template <int TT, bool HELD, typename XT, int VEC, typename Held>
+__device__ __forceinline__ void write_gradient(const DistilArgs &a, const RowSpan<XT, VEC> &r, const Held &held, XT *out, int t,
+                                               float m, float sum, float f, const Top &top) {
+    const float away = -finite_or_zero(m), times = f / sum;
+    XT *body = out + r.head;
+    if constexpr (HELD) {
+#pragma unroll 4
+        for (int64_t i = t; i < r.vecs; i += TT) {
+            float e[VEC];
+            held.widen(i, e);
+            scaled_q(e, away, a.scale, times);
+            store_vec<VEC>(body + i * VEC, e);
+        }
+    } else {
+        for (int64_t i0 = t; i0 < r.vecs; i0 += kInFlight * TT) {
+            RowVec<XT, VEC> raw[kInFlight];
+            load_vectors<TT>(r, i0, raw);
 #pragma unroll
-        for (int j = 0; j < kInFlight; ++j)
-            if (i0 + j * TT < r.vecs) raw[j].load(r.row + r.head + (i0 + j * TT) * VEC);
-#pragma unroll
-        for (int j = 0; j < kInFlight; ++j)
-            if (i0 + j * TT < r.vecs) {
-                float e[VEC];
-                raw[j].widen(e);
-                add_vec(e, away);
-                mul_vec(e, by);
-#pragma unroll
-                for (int q = 0; q < VEC; ++q) e[q] = exp2_of(e[q]);
-                mul_vec(e, times);
-                store_vec<VEC>(out + r.head + (i0 + j * TT) * VEC, e);
-            }
+            for (int j = 0; j < kInFlight; ++j)
+                if (i0 + j * TT < r.vecs) {
+                    float e[VEC];
+                    raw[j].widen(e);
+                    scaled_q(e, away, a.scale, times);
+                    store_vec<VEC>(body + (i0 + j * TT) * VEC, e);
+                }
+        }
     }
     if (t < r.loose) {
         float e[1];
         VecLoad<XT, 1>::load(r.row + r.loose_at(t), e);
-        e[0] = exp2_of((e[0] + away[0]) * a.scale) * times[0];
+        scaled_q(e, away, a.scale, times);
         store_vec<1>(out + r.loose_at(t), e);
     }
     team_sync<TT>();
@@ -199,10 +291,9 @@ __device__ __forceinline__ void write_gradient(const DistilArgs &a, const RowSpa
     for (int i = t; i < a.k; i += TT) {
         const int id = top.ids[i];
         if (id < 0) continue;
-        float p = 0.f, e[1];
+        float p = 0.f, e[1] = {held.value(r, id)};
         for (int j = 0; j < a.k; ++j) p += top.ids[j] == id ? top.p[j] : 0.f;
-        VecLoad<XT, 1>::load(r.row + id, e);
-        e[0] = fmaf(exp2_of((e[0] + away[0]) * a.scale), times[0], -f * p);
+        e[0] = fmaf(exp2_of((e[0] + away) * a.scale), times, -f * p);
         store_vec<1>(out + id, e);
     }
 }
@@ -225,91 +316,149 @@ __device__ __forceinline__ void check_ids(const DistilArgs &a) {
     if (threadIdx.x == 0) *a.status_all = all ? TFG_ERR_INDEX_RANGE : TFG_OK;
 }
 
-// BACK: the backward from the forward's statistics; else the loss, and with a.grad the gradient.
-template <typename XT, int VEC, int TT, bool BACK>
+template <typename XT, int VEC, int TT, int MODE>
 __global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(DistilArgs a) {
     constexpr int kTeams = TT == 32 ? kDistilThreads / 32 : 1;
-    extern __shared__ __align__(16) char s_top[];
+    constexpr bool kHeld = MODE == kBothHeld, kCopies = kHeld || MODE == kLossRing;
+    constexpr int kSlots = kHeld ? kChunks : kRing;
+    extern __shared__ __align__(128) char s_row[];
     __shared__ float s_fold[TT / 32];
+    __shared__ uint64_t s_full[kCopies ? kSlots : 1];
     if (a.status_all && blockIdx.x == gridDim.x - 1) return check_ids(a);
     const int t = threadIdx.x % TT, team = threadIdx.x / TT;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
     if (row >= a.n) return;                                  // whole teams
-    Top top;
-    top.ids = reinterpret_cast<int *>(s_top) + team * 2 * a.k;
-    top.p = reinterpret_cast<float *>(top.ids + a.k);
     const RowSpan<XT, VEC> r(static_cast<const XT *>(a.logits) + row * a.v, a.v);
     XT *out = a.grad ? static_cast<XT *>(a.grad) + row * a.v : nullptr;
     float f = a.weight ? __ldg(a.weight + row) : 1.f;
-    load_top<TT>(a, row, t, s_fold, !BACK && !a.status_all, top);
+    const HeldRow<XT, VEC, kSlots> copies{s_row, s_full};
+    const int chunks = kCopies ? copies.chunks(r) : 0;
+    if constexpr (kCopies) {
+        if (f != 0.f && t == 0) {
+            for (int c = 0; c < kSlots; ++c) arrivals_init(&s_full[c], 1);
+            arrivals_ready();
+            for (int c = 0; c < kSlots && c < chunks; ++c) copies.copy(r, c);
+        }
+    }
+    const auto held = [&] {
+        if constexpr (kHeld) return copies;
+        else return NotHeld{};
+    }();
+    const int64_t copied = kHeld ? r.vecs * 16 : (kCopies ? min64(r.vecs * 16, kRing * kChunkBytes) : 0);
+    Top top;
+    top.ids = reinterpret_cast<int *>(s_row + copied) + team * 2 * a.k;
+    top.p = reinterpret_cast<float *>(top.ids + a.k);
+    // the first vectors are on their way while the teacher's side is looked at
+    constexpr bool kStreams = MODE == kLoss || MODE == kBoth;
+    RowVec<XT, VEC> raw[kInFlight];
+    if constexpr (kStreams) {
+        if (f != 0.f) load_vectors<TT>(r, t, raw);
+    }
+    load_top<TT>(a, row, t, s_fold, MODE != kBack && !a.status_all, top);   // with barriers, behind those of the copies
     if (f == 0.f || !top.any) {                              // a row that counts for nothing is not read
-        if (!BACK && t == 0) {
+        if (MODE != kBack && t == 0) {
             a.loss[row] = 0.f;
             if (a.stats) a.stats[row] = make_float2(0.f, 1.f);
         }
         if (out) zero_row<TT>(r, out, t);
+        if constexpr (kCopies) {                             // copies under way end in this CTA's memory
+            if (f != 0.f)
+                for (int c = 0; c < kSlots && c < chunks; ++c) copies.wait(c);
+        }
         return;
     }
     float m, sum;
-    if constexpr (BACK) {
+    if constexpr (MODE == kBack) {
         const float2 s = a.stats[row];
         m = s.x;
         sum = s.y;
         f *= __ldg(a.grad_loss + row);
-        top_terms<TT, XT>(a, nullptr, t, s_fold, m, 0.f, top);
+        top_terms<TT, false>(a, r, held, t, s_fold, m, 0.f, top);
         team_sync<TT>();
     } else {
         Running run;
-        for (int64_t i0 = t; i0 < r.vecs; i0 += kInFlight * TT) {
-            RowVec<XT, VEC> raw[kInFlight];
+        if constexpr (kCopies) {
+            constexpr int kVecs = HeldRow<XT, VEC, kSlots>::kVecs;
+            static_assert(kVecs % TT == 0 || TT == 32, "a chunk is whole vectors of every thread");
+            bool there = true;
+            int64_t at = t;                                  // in the row
+            for (int c = 0; c < chunks; ++c) {
+                there = copies.wait(c) && there;
+                const int slot = c % kSlots * kVecs;
 #pragma unroll
-            for (int j = 0; j < kInFlight; ++j)
-                if (i0 + j * TT < r.vecs) raw[j].load(r.row + r.head + (i0 + j * TT) * VEC);
-#pragma unroll
-            for (int j = 0; j < kInFlight; ++j)
-                if (i0 + j * TT < r.vecs) {
-                    float s[VEC];
-                    raw[j].widen(s);
-                    run.add(s, a.scale);
+                for (int j = 0; j < kVecs / TT; ++j, at += TT)
+                    if (at < r.vecs) run.template add_raw<XT, VEC>(copies.raw(slot + t + j * TT), a.scale);
+                if (!kHeld && c + kSlots < chunks) {         // its slot is free for another
+                    __syncthreads();
+                    if (t == 0) copies.copy(r, c + kSlots);
                 }
+            }
+            if (!there) run.sum = NAN;                       // a row that does not arrive
+        } else {
+            for (int64_t i0 = t; i0 < r.vecs; i0 += kInFlight * TT) {
+                if (i0 != t) load_vectors<TT>(r, i0, raw);
+#pragma unroll
+                for (int j = 0; j < kInFlight; ++j)
+                    if (i0 + j * TT < r.vecs) run.template add_raw<XT, VEC>(raw[j].r, a.scale);
+            }
         }
         if (t < r.loose) {
             float s[1];
             VecLoad<XT, 1>::load(r.row + r.loose_at(t), s);
-            run.add(s, a.scale);
+            run.add(s, s[0], a.scale);
         }
         m = team_fold<TT>(run.m, s_fold, Larger{});
         sum = team_fold<TT>(run.sum * exp2_of((finite_or_zero(run.m) - finite_or_zero(m)) * a.scale), s_fold, Add{});
-        const float terms = top_terms<TT, XT>(a, r.row, t, s_fold, m, logf(sum), top);
+        const float terms = top_terms<TT, true>(a, r, held, t, s_fold, m, logf(sum), top);
         if (t == 0) {
             a.loss[row] = f * a.tau * a.tau * terms;
             if (a.stats) a.stats[row] = make_float2(m, sum);
         }
-        if (!out) return;
+        if (MODE == kLoss || MODE == kLossRing) return;
         team_sync<TT>();
     }
-    write_gradient<TT>(a, r, out, t, m, sum, f * a.tau, top);
+    if constexpr (MODE != kLoss && MODE != kLossRing) write_gradient<TT, kHeld>(a, r, held, out, t, m, sum, f * a.tau, top);
 }
 
-template <typename XT, int VEC, bool BACK>
-cudaError_t launch_team(const DistilArgs &a, cudaStream_t s) {
-    const int extra = a.status_all ? 1 : 0;
-    const size_t top = 8 * size_t(a.k);
-    if (a.v <= kWarpClasses && a.k <= kWarpTop) {
-        constexpr int kTeams = kDistilThreads / 32;
-        const unsigned grid = static_cast<unsigned>((a.n + kTeams - 1) / kTeams + extra);
-        distil_rows<XT, VEC, 32, BACK><<<grid, kDistilThreads, kTeams * top, s>>>(a);
-    } else {
-        distil_rows<XT, VEC, kRowThreads, BACK><<<static_cast<unsigned>(a.n + extra), kRowThreads, top, s>>>(a);
+template <typename XT, int VEC, int TT, int MODE>
+cudaError_t launch_rows(const DistilArgs &a, size_t shared, cudaStream_t s) {
+    auto *kernel = distil_rows<XT, VEC, TT, MODE>;
+    if constexpr (MODE == kBothHeld || MODE == kLossRing) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldMost);
+        if (e != cudaSuccess) return e;
     }
+    constexpr int kTeams = TT == 32 ? kDistilThreads / 32 : 1;
+    const unsigned grid = static_cast<unsigned>((a.n + kTeams - 1) / kTeams + (a.status_all ? 1 : 0));
+    kernel<<<grid, TT == 32 ? kDistilThreads : TT, shared, s>>>(a);
     return cudaGetLastError();
+}
+
+// The team goes by the row's size alone, so that a loss has the same bits with and without its gradient.
+template <typename XT, int VEC, int MODE>
+cudaError_t launch_team(const DistilArgs &a, cudaStream_t s) {
+    const size_t top = 8 * size_t(a.k);
+    if (a.v <= kWarpClasses && a.k <= kWarpTop) return launch_rows<XT, VEC, 32, MODE>(a, kDistilThreads / 32 * top, s);
+    if constexpr (VEC > 1) {
+        constexpr int kMode = MODE == kBoth ? kBothHeld : (MODE == kLoss ? kLossRing : kBack);
+        const size_t values = size_t(a.v) * sizeof(XT), row = values + top, ring = size_t(kRing) * kChunkBytes;
+        const size_t shared = kMode == kBothHeld ? row : (kMode == kBack ? top : top + (values < ring ? values : ring));
+        if (row <= kHold128) return launch_rows<XT, VEC, 128, kMode>(a, shared, s);
+        if (row <= kHold256) return launch_rows<XT, VEC, 256, kMode>(a, shared, s);
+        if (row <= kHoldMost || kMode != kBothHeld) return launch_rows<XT, VEC, kRowThreads, kMode>(a, shared, s);
+    }
+    return launch_rows<XT, VEC, kRowThreads, MODE>(a, top, s);
+}
+
+template <typename XT, int VEC>
+cudaError_t launch_mode(const DistilArgs &a, bool back, cudaStream_t s) {
+    if (back) return launch_team<XT, VEC, kBack>(a, s);
+    return a.grad ? launch_team<XT, VEC, kBoth>(a, s) : launch_team<XT, VEC, kLoss>(a, s);
 }
 
 constexpr int64_t kOneCheckerIds = 16384;
 
-template <bool BACK>
-cudaError_t launch_distil(DistilArgs &a, int dtype, int32_t *status, cudaStream_t s) {
-    if (!BACK) {
+cudaError_t launch_distil(DistilArgs &a, int dtype, bool back, int32_t *status, cudaStream_t s) {
+    if (!back) {
         a.status = status;
         if (a.n * a.k <= kOneCheckerIds) {
             a.status_all = status;
@@ -321,8 +470,8 @@ cudaError_t launch_distil(DistilArgs &a, int dtype, int32_t *status, cudaStream_
     if (a.n == 0 && !a.status_all) return cudaSuccess;
     // rows of both arrays reach their 16-byte boundaries together
     const bool vectors = !a.grad || (reinterpret_cast<uintptr_t>(a.grad) - reinterpret_cast<uintptr_t>(a.logits)) % 16 == 0;
-    if (dtype == TFG_BF16) return vectors ? launch_team<uint16_t, 8, BACK>(a, s) : launch_team<uint16_t, 1, BACK>(a, s);
-    return vectors ? launch_team<float, 4, BACK>(a, s) : launch_team<float, 1, BACK>(a, s);
+    if (dtype == TFG_BF16) return vectors ? launch_mode<uint16_t, 8>(a, back, s) : launch_mode<uint16_t, 1>(a, back, s);
+    return vectors ? launch_mode<float, 4>(a, back, s) : launch_mode<float, 1>(a, back, s);
 }
 
 }  // namespace
@@ -333,7 +482,7 @@ cudaError_t launch_distillation(const void *logits, int dtype, int64_t n, int64_
     DistilArgs a{logits, n, v, ids, id32, teacher, teacher_dtype == TFG_BF16, k, padding, tau,
                  static_cast<float>(1.4426950408889634 / tau), weight, loss, reinterpret_cast<float2 *>(stats), nullptr, grad,
                  nullptr, nullptr};
-    return launch_distil<false>(a, dtype, status, s);
+    return launch_distil(a, dtype, false, status, s);
 }
 
 cudaError_t launch_distillation_backward(const void *logits, int dtype, int64_t n, int64_t v, const void *ids, bool id32,
@@ -343,7 +492,7 @@ cudaError_t launch_distillation_backward(const void *logits, int dtype, int64_t 
     DistilArgs a{logits, n, v, ids, id32, teacher, teacher_dtype == TFG_BF16, k, padding, tau,
                  static_cast<float>(1.4426950408889634 / tau), weight, nullptr,
                  reinterpret_cast<float2 *>(const_cast<float *>(stats)), grad_loss, grad, nullptr, nullptr};
-    return launch_distil<true>(a, dtype, nullptr, s);
+    return launch_distil(a, dtype, true, nullptr, s);
 }
 
 }  // namespace tfg
