@@ -386,6 +386,16 @@ __device__ __forceinline__ void state_or_zero(const float *states, int64_t seq, 
     }
 }
 
+// States that the rows of a thread begin or end with, on their way to L1 all at once: row by row each would be
+// waited for by itself.
+template <int EACH>
+__device__ __forceinline__ void prefetch_states(const float *states, uint32_t which, const int32_t *seq, int64_t f, int64_t c) {
+    if (!states) return;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+        if ((which >> j) & 1u) asm volatile("prefetch.global.L1 [%0];" ::"l"(states + seq[j] * f + c));
+}
+
 // Maps of a warp's groups of rows, composed across the lanes from where values enter (the first
 // row; UP: the last): on return (a, b) is the map of the groups up to this one, `fresh` whether
 // one of them cuts off what enters; the last group leaves the whole warp's map.

@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         const int sc = static_cast<int>(threadIdx.x) - T::kWide;                     // threads of the next columns: states
         float state = 0.f;
         if (sc >= 0 && sc < T::kWide && c0 + sc < p.f) state = __ldg(p.entered + tile * p.f + c0 + sc);
+        if (!p.linked) find_rows(p, rows);
         if constexpr (VEC > 1) {
             if (!phase_done(&s_full, parity)) set_status(p.status, TFG_ERR_TIMEOUT);
             parity ^= 1u;
@@ -210,12 +211,13 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
             copies_done();
             if (p.linked) __syncthreads();                       // the plan is there
         }
-        if (!p.linked) find_rows(p, rows);
         const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
                        in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps),
                        cut_warps = warps_word(rows.cut_warps);
         const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
         const int32_t *seq = rows.seq + group * T::kEach;
+        if (!plain && on) prefetch_states<T::kEach>(p.initial, begin, seq, p.f, c);
+        if (!plain && on) prefetch_states<T::kEach>(p.grad_final, end, seq, p.f, c);
 
         // the thread's maps: of the state down its rows, of the adjoint up
         float a[VEC], b[VEC], u[VEC], w[VEC];

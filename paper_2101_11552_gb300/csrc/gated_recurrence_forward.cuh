@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             const int from = cut_before<false>(p, job.order);
             if (threadIdx.x == 0) s_from = from;
         }
+        if (!p.linked) find_rows(p, rows);
         if constexpr (VEC > 1) {
             if (!phase_done(&s_full, parity)) set_status(p.status, TFG_ERR_TIMEOUT);
             parity ^= 1u;
@@ -118,11 +119,11 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             copies_done();
             if (p.linked) __syncthreads();                       // the plan is there
         }
-        if (!p.linked) find_rows(p, rows);
         const uint32_t begin = row_bits<T::kEach>(rows.begin, group), end = row_bits<T::kEach>(rows.end, group),
                        in = row_bits<T::kEach>(rows.in, group), begin_warps = warps_word(rows.begin_warps);
         const bool plain = (begin | end) == 0u && in == (1u << T::kEach) - 1u;
         const int32_t *seq = rows.seq + group * T::kEach;
+        if (!plain && on) prefetch_states<T::kEach>(p.initial, begin, seq, p.f, c);
 
         float a[VEC], b[VEC];
         const auto z = [&] {

@@ -60,8 +60,8 @@ __device__ __forceinline__ float row_rstd(float d, float d2, float eps) {
 }
 
 template <typename XT, typename RT, int VEC, int TT, int NV>
-__global__ void __launch_bounds__(TT < 256 ? 256 : TT) row_norm(RowNormArgs p) {
-    constexpr int kTeams = TT < 256 ? 256 / TT : 1;
+__global__ void __launch_bounds__(TT <= 32 ? 256 : TT) row_norm(RowNormArgs p) {
+    constexpr int kTeams = TT <= 32 ? 256 / TT : 1;
     __shared__ float s_sum[3 * (TT > 32 ? TT / 32 : 1)];
     const int t = threadIdx.x % TT;
     const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams + threadIdx.x / TT;
@@ -179,8 +179,11 @@ cudaError_t launch_vec(const RowNormArgs &p, cudaStream_t s) {
     constexpr int kHeld = VEC == 8 ? 4 : 8;                  // vectors that a thread holds
     const int64_t vecs = (p.f + VEC - 1) / VEC;
     const auto ctas = [&](int teams) { return static_cast<unsigned>((p.n + teams - 1) / teams); };
+    // a few rows spread over more threads, and multiprocessors
+    const bool few = p.n <= 4 * sm_count();
     if (vecs <= 8) row_norm<XT, RT, VEC, 8, 1><<<ctas(32), 256, 0, s>>>(p);
     else if (vecs <= 32) row_norm<XT, RT, VEC, 32, 1><<<ctas(8), 256, 0, s>>>(p);
+    else if (few && vecs <= 128) row_norm<XT, RT, VEC, 128, 1><<<ctas(1), 128, 0, s>>>(p);
     else if (vecs <= 32 * kHeld) row_norm<XT, RT, VEC, 32, kHeld><<<ctas(8), 256, 0, s>>>(p);
     else if (vecs <= 256 * kHeld) row_norm<XT, RT, VEC, 256, kHeld><<<ctas(1), 256, 0, s>>>(p);
     else if (vecs <= 1024 * kHeld) row_norm<XT, RT, VEC, 1024, kHeld><<<ctas(1), 1024, 0, s>>>(p);

@@ -689,6 +689,7 @@ def tfg_dot_edge_softmax_aggregate_backward(rowptr, col, rowptr_src, col_src, q,
 # its index, and the current stream is taken as the raw handle.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _DTYPES = {torch.float32: TFG_F32, torch.bfloat16: TFG_BF16}
 _IDS = {torch.int64: False, torch.int32: True}
 
@@ -696,7 +697,7 @@ _IDS = {torch.int64: False, torch.int32: True}
 def _run(index: int, name: str, *args):
     """Call the C entry point ``name`` on the current stream of device ``index``."""
     fn = getattr(_lib or lib(), name)
-    if index == torch.cuda.current_device():
+    if index == _current_device():
         rc = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -939,19 +940,32 @@ class LayerNorm(NamedTuple):
     rstd: Optional[torch.Tensor]   # fp32 [N]
 
 
-def _row_array(name: str, t, index: int, shape):
-    _same(name, t, index)
+def _row_array(name: str, t, index: int, shape) -> int:
+    """The type code of a contiguous array of the given shape on the device."""
+    try:
+        if t.get_device() == index and t.is_contiguous() and t.shape == shape:
+            return _DTYPES[t.dtype]
+    except (AttributeError, KeyError):            # no tensor, or of another type
+        pass
+    _same(name, t, index)                         # say what it is
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return _dtype_code(name, t.dtype)
 
 
-def _weights(index: int, f: int, **weights):
-    for name, w in weights.items():
-        if w is not None:
-            _same(name, w, index, torch.float32)
-            if w.numel() != f:
-                raise ValueError(f"{name} must have {f} values")
+def _vector(name: str, t, index: int, n: int, what: str):
+    """The address of n fp32 values."""
+    try:
+        if t.get_device() == index and t.is_contiguous() and t.dtype is torch.float32 and t.numel() == n:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _same(name, t, index, torch.float32)
+    raise ValueError(f"{name} must have {what}")
+
+
+def _weight(name: str, t, index: int, f: int):
+    return None if t is None else _vector(name, t, index, f, f"{f} values")
 
 
 def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, out_dtype: Optional[torch.dtype] = None,
@@ -963,7 +977,7 @@ def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, o
         raise ValueError("x must have shape [N, F]")
     n, f = x.shape
     code = _dtype_code("x", x.dtype)
-    _weights(index, f, gamma=gamma, beta=beta)
+    weights = _weight("gamma", gamma, index, f), _weight("beta", beta, index, f)
     sum_code = 0
     if residual is not None:
         sum_code = _row_array("residual", residual, index, x.shape)
@@ -976,8 +990,9 @@ def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, o
     out = _need_out("out", out, x.shape, out_dtype, x)
     mean = rstd = None
     if want_stats:
-        mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
-    _run(index, "tfg_layer_norm", x.data_ptr(), code, _at(residual), sum_code, _at(sum_out), n, f, _at(gamma), _at(beta), eps,
+        mean = torch.empty(n, dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+    _run(index, "tfg_layer_norm", x.data_ptr(), code, _at(residual), sum_code, _at(sum_out), n, f, *weights, eps,
          out.data_ptr(), out_code, _at(mean), _at(rstd))
     return LayerNorm(out, x if residual is None else sum_out, mean, rstd)
 
@@ -998,11 +1013,8 @@ def tfg_layer_norm_backward(sum, gamma, mean, rstd, grad_out, grad_sum=None, gra
         raise ValueError("sum must have shape [N, F]")
     n, f = sum.shape
     code = _dtype_code("sum", sum.dtype)
-    _weights(index, f, gamma=gamma)
-    for name, s in (("mean", mean), ("rstd", rstd)):
-        _same(name, s, index, torch.float32)
-        if s.numel() != n:
-            raise ValueError(f"{name} must have shape [N]")
+    weight = _weight("gamma", gamma, index, f)
+    stats = _vector("mean", mean, index, n, "shape [N]"), _vector("rstd", rstd, index, n, "shape [N]")
     grad_code = _row_array("grad_out", grad_out, index, sum.shape)
     if grad_sum is not None:
         _row_array("grad_sum", grad_sum, index, sum.shape)
@@ -1016,10 +1028,11 @@ def tfg_layer_norm_backward(sum, gamma, mean, rstd, grad_out, grad_sum=None, gra
     grad_gamma = grad_beta = None
     need = 0
     if want_weight_grads:
-        grad_gamma, grad_beta = torch.empty(2, f, dtype=torch.float32, device=sum.device).unbind(0)
+        grad_gamma = torch.empty(f, dtype=torch.float32, device=sum.device)
+        grad_beta = torch.empty_like(grad_gamma)
         need = tfg_layer_norm_backward_workspace_size(n, f)
     workspace = _workspace(workspace, need, sum)
-    _run(index, "tfg_layer_norm_backward", sum.data_ptr(), code, n, f, _at(gamma), mean.data_ptr(), rstd.data_ptr(),
+    _run(index, "tfg_layer_norm_backward", sum.data_ptr(), code, n, f, weight, *stats,
          grad_out.data_ptr(), grad_code, _at(grad_sum), grad_x.data_ptr(), x_code, _at(grad_gamma), _at(grad_beta),
          *_span(workspace))
     return grad_x, grad_gamma, grad_beta
@@ -1066,19 +1079,21 @@ def _recurrence_inputs(gate, x, node_offsets, kind, initial):
     if node_offsets.dim() != 1 or node_offsets.numel() < 1:
         raise ValueError("node_offsets must have shape [S + 1]")
     s = node_offsets.numel() - 1
-    if kind not in GATES:
+    kind_code = GATES.get(kind)
+    if kind_code is None:
         raise ValueError(f"kind must be one of {sorted(GATES)}, got {kind!r}")
-    _states(index, (s, f), initial=initial)
-    return index, n, f, s, code, (gate.data_ptr(), ld, x.data_ptr(), x_ld, code, node_offsets.data_ptr(), n, s, f, GATES[kind],
-                                  _at(initial))
+    return index, n, f, s, code, (gate.data_ptr(), ld, x.data_ptr(), x_ld, code, node_offsets.data_ptr(), n, s, f, kind_code,
+                                  _states("initial", initial, index, (s, f)))
 
 
-def _states(index: int, shape, **states):
-    for name, t in states.items():
-        if t is not None:
-            _same(name, t, index, torch.float32)
-            if t.shape != shape:
-                raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+def _states(name: str, t, index: int, shape):
+    """The address of states, None without."""
+    if t is None:
+        return None
+    _same(name, t, index, torch.float32)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _tiles(n: int) -> int:
@@ -1098,7 +1113,7 @@ def tfg_gated_recurrence(gate, x, node_offsets, kind: str = "sigmoid", initial=N
     if out_dtype is None:
         out_dtype = gate.dtype if out is None else out.dtype
     out_code = _dtype_code("out", out_dtype)
-    need = tfg_gated_recurrence_workspace_size(n, f)
+    need = tfg_gated_recurrence_workspace_size(n, f) if n > RECURRENCE_TILE_ROWS else 0
     out = _need_out("out", out, gate.shape, out_dtype, gate)
     final = torch.empty(s, f, dtype=torch.float32, device=gate.device) if want_final else None
     kept = torch.empty(_tiles(n), f, dtype=torch.float32, device=gate.device) if want_checkpoints else None
@@ -1124,10 +1139,9 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     may be given as buffers whose rows lie apart; rows outside all sequences are left as
     they are in them.  ``status`` int32 [1] takes the call's status word."""
     index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
-    _states(index, (s, f), grad_final=grad_final)
-    _states(index, (_tiles(n), f), checkpoints=checkpoints)
     if checkpoints is None:
         raise ValueError("checkpoints are the forward's (want_checkpoints)")
+    last, kept = _states("grad_final", grad_final, index, (s, f)), _states("checkpoints", checkpoints, index, (_tiles(n), f))
     grad_code = TFG_F32 if grad_out is None else _row_array("grad_out", grad_out, index, gate.shape)
     grads = []
     for name, t in (("grad_gate", grad_gate), ("grad_x", grad_x)):
@@ -1139,7 +1153,7 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     grad_initial = torch.empty(s, f, dtype=torch.float32, device=gate.device) if want_initial else None
     workspace = _workspace(workspace, tfg_gated_recurrence_workspace_size(n, f), gate)
     status = _need_out("status", status, (1,), torch.int32, gate)
-    _run(index, "tfg_gated_recurrence_backward", *head, checkpoints.data_ptr(), _at(grad_out), grad_code, _at(grad_final),
+    _run(index, "tfg_gated_recurrence_backward", *head, kept, _at(grad_out), grad_code, last,
          grads[0][0].data_ptr(), grads[0][1], grads[1][0].data_ptr(), grads[1][1], _at(grad_initial), *_span(workspace),
          status.data_ptr())
     return GatedRecurrenceGrads(grads[0][0], grads[1][0], grad_initial)
