@@ -8,19 +8,19 @@ namespace tfg {
 namespace {
 
 // Clears the counter, sets maps and states to what is not there yet, and describes the rows of every
-// tile, a warp for each.
+// tile, a warp for each 32.
 __global__ void __launch_bounds__(256) scan_plan_kernel(ScanArgs p, uint4 *words, int64_t n, TileRows *plan) {
+    cudaTriggerProgrammaticLaunchCompletion();               // the tiles' kernel may be set up; it waits for this one's end
     const int64_t threads = static_cast<int64_t>(gridDim.x) * 256, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (id == 0) *p.status = TFG_OK;
     if (!p.linked) return;
     for (int64_t i = id; i < n; i += threads) words[i] = i ? make_uint4(~0u, ~0u, ~0u, ~0u) : make_uint4(0u, 0u, 0u, 0u);
-    for (int64_t tile = id / 32; tile < p.tiles; tile += threads / 32) {
-        const int64_t r0 = tile * kTileRows;
-        TileRows &t = plan[tile];
-        const int lo = static_cast<int>(warp_graph_at(p.offsets, p.seqs, r0));
-        const int hi = static_cast<int>(warp_graph_at(p.offsets, p.seqs, min64(r0 + kTileRows, p.n) - 1));
-#pragma unroll
-        for (int w = 0; w < kTileRows / 32; ++w) describe_row(p, r0 + w * 32 + (threadIdx.x & 31), lo, hi, w, t);
+    constexpr int kWords = kTileRows / 32;
+    for (int64_t word = id / 32; word < p.tiles * kWords; word += threads / 32) {
+        const int64_t tile = word / kWords, r0 = word * 32, last = min64(r0 + 32, p.n) - 1;
+        const int lo = static_cast<int>(warp_graph_at(p.offsets, p.seqs, r0 < p.n ? r0 : last));
+        const int hi = static_cast<int>(warp_graph_at(p.offsets, p.seqs, last));
+        describe_row(p, r0 + (threadIdx.x & 31), lo, hi, static_cast<int>(word % kWords), plan[tile]);
     }
 }
 
@@ -103,7 +103,7 @@ cudaError_t scan_plan(const ScanArgs &p, void *ws, cudaStream_t s) {
     if (p.status_all) return cudaSuccess;
     const ScanSpace space(p.n, p.f);
     const int64_t words = static_cast<int64_t>(space.plan / 16);
-    const int64_t ctas = min64(words / 256 + 1 + p.tiles / 8, 8 * static_cast<int64_t>(sm_count()));
+    const int64_t ctas = min64(words / 256 + 1 + p.tiles * (kTileRows / 32) / 8, 8 * static_cast<int64_t>(sm_count()));
     scan_plan_kernel<<<static_cast<unsigned>(ctas), 256, 0, s>>>(
         p, static_cast<uint4 *>(ws), words, reinterpret_cast<TileRows *>(static_cast<char *>(ws) + space.plan));
     return cudaGetLastError();

@@ -105,6 +105,26 @@ inline unsigned scan_ctas(const ScanArgs &p, int resident) {
     return static_cast<unsigned>(p.checkers + (p.linked ? min64(jobs, static_cast<int64_t>(resident) * sm_count()) : jobs));
 }
 
+// Launches a kernel of tiles so that it is set up while the plan is made; it begins with a wait for the plan.
+template <typename Kernel>
+cudaError_t launch_tiles(Kernel *kernel, const ScanArgs &p, const ScanMaps &maps, int resident, int shared, cudaStream_t s) {
+    if (shared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(scan_ctas(p, resident));
+    config.blockDim = dim3(kScanThreads);
+    config.dynamicSmemBytes = static_cast<size_t>(shared);
+    config.stream = s;
+    config.attrs = &early;
+    config.numAttrs = p.status_all ? 0 : 1;                  // no plan is made where one CTA checks all
+    return cudaLaunchKernelEx(&config, kernel, p, maps);
+}
+
 namespace {
 
 constexpr uint64_t kNoMap = ~uint64_t(0);

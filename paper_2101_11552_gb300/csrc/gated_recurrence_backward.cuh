@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
     __shared__ float s_carry[T::kWide];
     __shared__ uint32_t s_next;
     __shared__ int s_from;
+    if (!p.status_all) cudaGridDependencySynchronize();
     if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.grad_final, p.grad_initial);
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
     const Stage in_stage(s_stage);
@@ -283,14 +284,7 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
 
 template <typename XT, typename GT, int VEC, int KIND>
 cudaError_t launch_backward(const ScanArgs &p, const ScanMaps &maps, cudaStream_t s) {
-    constexpr int kShared = BackwardStage<XT, GT, VEC>::kBytes;
-    if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
-        const cudaError_t e =
-            cudaFuncSetAttribute(scan_backward<XT, GT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-        if (e != cudaSuccess) return e;
-    }
-    scan_backward<XT, GT, VEC, KIND><<<scan_ctas(p, kBackwardCtas<XT, GT, VEC>), kScanThreads, kShared, s>>>(p, maps);
-    return cudaGetLastError();
+    return launch_tiles(scan_backward<XT, GT, VEC, KIND>, p, maps, kBackwardCtas<XT, GT, VEC>, BackwardStage<XT, GT, VEC>::kBytes, s);
 }
 template <typename XT, typename GT, int VEC>
 cudaError_t launch_backward_kind(const ScanArgs &p, const ScanMaps &maps, int kind, cudaStream_t s) {

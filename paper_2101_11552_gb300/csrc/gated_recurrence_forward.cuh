@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
     __shared__ float s_state[T::kWide];
     __shared__ uint32_t s_next;
     __shared__ int s_from;
+    if (!p.status_all) cudaGridDependencySynchronize();
     if (static_cast<int>(blockIdx.x) < p.checkers) return check_sequences(p, p.initial, p.final_state);
     const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross, warp = threadIdx.x / 32;
     const Stage in_stage(s_stage);
@@ -176,14 +177,7 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
 
 template <typename XT, typename OT, int VEC, int KIND>
 cudaError_t launch_forward(const ScanArgs &p, const ScanMaps &maps, cudaStream_t s) {
-    constexpr int kShared = ForwardStage<XT, VEC>::kBytes;
-    if constexpr (kShared > 32 * 1024) {   // with the static part above the 48 KB every launch may use
-        const cudaError_t e =
-            cudaFuncSetAttribute(scan_forward<XT, OT, VEC, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-        if (e != cudaSuccess) return e;
-    }
-    scan_forward<XT, OT, VEC, KIND><<<scan_ctas(p, kForwardCtas), kScanThreads, kShared, s>>>(p, maps);
-    return cudaGetLastError();
+    return launch_tiles(scan_forward<XT, OT, VEC, KIND>, p, maps, kForwardCtas, ForwardStage<XT, VEC>::kBytes, s);
 }
 template <typename XT, int VEC>
 cudaError_t launch_forward_kind(const ScanArgs &p, const ScanMaps &maps, int kind, cudaStream_t s) {
