@@ -38,12 +38,17 @@ int scan_vector(const ScanArgs &p, int dtype, bool backward) {
         return at(p.g, 16) && p.f * rows % 16 == 0 && at(p.grad_final, 16) && at(p.grad_initial, 16) && p.grad_gate_ld % vec == 0 &&
                p.grad_x_ld % vec == 0 && at(p.grad_gate, 16) && at(p.grad_x, 16);
     };
-    const int vec = 16 / size;
-    return fits(vec) ? vec : 1;
+    return fits(16 / size) ? 4 : 1;
 }
 
-void scan_geometry(ScanArgs &p, int vec, void *ws, int32_t *status) {
-    const int wide = vec == 8 ? ScanTile<8>::kWide : (vec == 4 ? ScanTile<4>::kWide : ScanTile<1>::kWide);
+// Channels of a tile.
+int tile_channels(int dtype, int vec) {
+    if (vec == 1) return ScanTile<float, 1>::kWide;
+    return dtype == TFG_BF16 ? ScanTile<uint16_t, 4>::kWide : ScanTile<float, 4>::kWide;
+}
+
+void scan_geometry(ScanArgs &p, int dtype, int vec, void *ws, int32_t *status) {
+    const int wide = tile_channels(dtype, vec);
     p.tiles = (p.n + kTileRows - 1) / kTileRows;
     p.windows = (p.tiles + kWindow - 1) / kWindow;
     p.strips = static_cast<int>((p.f + wide - 1) / wide);
@@ -94,7 +99,7 @@ bool row_map(CUtensorMap &map, const void *rows, bool bf16, int64_t n, int64_t f
 
 bool scan_maps(const ScanArgs &p, int dtype, bool backward, ScanMaps &maps) {
     const bool bf16 = dtype == TFG_BF16;
-    const int wide = bf16 ? ScanTile<8>::kWide : ScanTile<4>::kWide;
+    const int wide = tile_channels(dtype, 4);
     return row_map(maps.gate, p.gate, bf16, p.n, p.f, p.gate_ld, wide) && row_map(maps.x, p.x, bf16, p.n, p.f, p.x_ld, wide) &&
            (!backward || !p.g || row_map(maps.g, p.g, p.out_bf16, p.n, p.f, p.f, wide));
 }
@@ -126,7 +131,7 @@ cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const voi
     p.gate = gate, p.gate_ld = gate_ld, p.x = x, p.x_ld = x_ld, p.offsets = offsets, p.n = n, p.seqs = seqs, p.f = f;
     p.initial = initial, p.out = out, p.out_bf16 = out_dtype == TFG_BF16, p.final_state = final_state, p.entering = entering;
     const int vec = scan_vector(p, dtype, false);
-    scan_geometry(p, vec, ws, status);
+    scan_geometry(p, dtype, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);
     if (e != cudaSuccess || p.checkers + p.tiles * p.strips == 0) return e;
     ScanMaps maps;
@@ -146,7 +151,7 @@ cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, 
     p.grad_gate = grad_gate, p.grad_gate_ld = grad_gate_ld, p.grad_x = grad_x, p.grad_x_ld = grad_x_ld;
     p.grad_initial = grad_initial;
     const int vec = scan_vector(p, dtype, true);
-    scan_geometry(p, vec, ws, status);
+    scan_geometry(p, dtype, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);
     if (e != cudaSuccess || p.checkers + p.tiles * p.strips == 0) return e;
     ScanMaps maps;

@@ -295,11 +295,16 @@ __device__ __forceinline__ void check_sequences(const ScanArgs &p, const float *
 constexpr int kScanWarps = kScanThreads / 32;
 constexpr int kWarpRows = kTileRows / kScanWarps;            // rows of a warp
 
-template <int VEC>
+// VEC values a thread, kAcross threads side by side in a row, kEach rows of a thread.  Tiles of bf16 have 64
+// channels in vectors of 4, so that a warp has two groups of rows and exchanges little between them (8 threads of 8
+// channels, four groups: 200 us for 131,072 x 1,024 forward, with 4 channels 184); of fp32 32 channels, as 64 would
+// leave room for three CTAs on a multiprocessor in place of four (1,024 molecules 118 us, so 109).
+template <typename XT, int N>
 struct ScanTile {
+    static constexpr int VEC = N;
     static constexpr int kLane = VEC * 4 > 16 ? 16 : VEC * 4, kRow = VEC * 4 * kScanThreads;   // of fp32 slots
-    static constexpr int kAcross = VEC == 1 ? 32 : 8;        // threads side by side in a row
-    static constexpr int kEach = kTileRows * kAcross / kScanThreads;   // rows of a thread
+    static constexpr int kAcross = VEC == 1 ? 32 : (sizeof(XT) == 2 ? 16 : 8);
+    static constexpr int kEach = kTileRows * kAcross / kScanThreads;
     static constexpr int kWide = kAcross * VEC;              // channels
 };
 
@@ -312,38 +317,29 @@ __device__ __forceinline__ void copy_plan(const ScanArgs &p, int64_t tile, TileR
 }
 
 // A thread's vectors of a tile that lies in shared memory row by row.
-template <typename T, int VEC>
+template <typename T, typename Tile>
 struct TileRow {
-    static constexpr int kBytes = kTileRows * ScanTile<VEC>::kWide * static_cast<int>(sizeof(T));
+    static constexpr int VEC = Tile::VEC, kBytes = kTileRows * Tile::kWide * static_cast<int>(sizeof(T));
     T *at;
     __device__ __forceinline__ explicit TileRow(char *tile)
-        : at(reinterpret_cast<T *>(tile) + threadIdx.x / ScanTile<VEC>::kAcross * ScanTile<VEC>::kEach * ScanTile<VEC>::kWide +
-             threadIdx.x % ScanTile<VEC>::kAcross * VEC) {}
+        : at(reinterpret_cast<T *>(tile) + threadIdx.x / Tile::kAcross * Tile::kEach * Tile::kWide + threadIdx.x % Tile::kAcross * VEC) {}
     __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
-        const T *p = at + j * ScanTile<VEC>::kWide;
-        if constexpr (VEC * sizeof(T) == 32) {
-#pragma unroll
-            for (int h = 0; h < 8; h += 4) {
-                const float4 q = *reinterpret_cast<const float4 *>(p + h);
-                v[h] = q.x; v[h + 1] = q.y; v[h + 2] = q.z; v[h + 3] = q.w;
-            }
-        } else {
-            VecLoad<T, VEC>::widen(load_plain<T, VEC>(p), v);
-        }
+        VecLoad<T, VEC>::widen(load_plain<T, VEC>(at + j * Tile::kWide), v);
     }
     __device__ __forceinline__ void zero(int j) const {
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) at[j * ScanTile<VEC>::kWide + q] = T(0);
+        for (int q = 0; q < VEC; ++q) at[j * Tile::kWide + q] = T(0);
     }
 };
 // The gates of a thread, taken from their tile before the decays are written over it.
-template <typename T, int VEC>
+template <typename T, typename Tile>
 struct HeldGate {
-    typename VecLoad<T, VEC>::Raw r[ScanTile<VEC>::kEach];
+    static constexpr int VEC = Tile::VEC;
+    typename VecLoad<T, VEC>::Raw r[Tile::kEach];
     __device__ __forceinline__ explicit HeldGate(char *tile) {
-        const TileRow<T, VEC> from(tile);
+        const TileRow<T, Tile> from(tile);
 #pragma unroll
-        for (int j = 0; j < ScanTile<VEC>::kEach; ++j) r[j] = load_plain<T, VEC>(from.at + j * ScanTile<VEC>::kWide);
+        for (int j = 0; j < Tile::kEach; ++j) r[j] = load_plain<T, VEC>(from.at + j * Tile::kWide);
     }
     __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const { VecLoad<T, VEC>::widen(r[j], v); }
 };
@@ -419,10 +415,10 @@ __device__ __forceinline__ void prefetch_states(const float *states, uint32_t wh
 // Maps of a warp's groups of rows, composed across the lanes from where values enter (the first
 // row; UP: the last): on return (a, b) is the map of the groups up to this one, `fresh` whether
 // one of them cuts off what enters; the last group leaves the whole warp's map.
-template <int VEC, bool UP>
+template <typename Tile, bool UP, int VEC>
 __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bool &fresh, int warp, int lane,
-                                            float (*s_a)[ScanTile<VEC>::kWide], float (*s_b)[ScanTile<VEC>::kWide]) {
-    constexpr int kAcross = ScanTile<VEC>::kAcross;
+                                            float (*s_a)[Tile::kWide], float (*s_b)[Tile::kWide]) {
+    constexpr int kAcross = Tile::kAcross;
     const int l = threadIdx.x & 31;
 #pragma unroll
     for (int o = kAcross; o < 32; o <<= 1) {
@@ -458,9 +454,9 @@ __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bo
 
 // What enters the thread's rows, into v: at the warp's first group what enters the warp (v), else what leaves
 // the group before, by the map (a, b) up to it.  By whole warps.
-template <int VEC, bool UP>
+template <typename Tile, bool UP, int VEC>
 __device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (&b)[VEC], bool fresh, float (&v)[VEC]) {
-    constexpr int kAcross = ScanTile<VEC>::kAcross;
+    constexpr int kAcross = Tile::kAcross;
     if constexpr (kAcross < 32) {
         const int l = threadIdx.x & 31, from = (UP ? l + kAcross : l - kAcross) & 31;
         const bool has = UP ? l + kAcross < 32 : l >= kAcross;

@@ -21,7 +21,7 @@ namespace {
 // A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
 template <typename XT, typename GT>
 struct BackwardSlots {
-    using T = ScanTile<1>;
+    using T = ScanTile<XT, 1>;
     using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
     using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
     using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
@@ -53,10 +53,10 @@ struct BackwardSlots {
 // A tile's inputs by tensor copies; the decays take the gates' place.
 template <typename XT, typename GT, int VEC>
 struct BackwardTile {
-    using T = ScanTile<VEC>;
+    using T = ScanTile<XT, VEC>;
     using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
-    using In = TileRow<XT, VEC>;
-    using Grad = TileRow<GT, VEC>;
+    using In = TileRow<XT, T>;
+    using Grad = TileRow<GT, T>;
     static constexpr int kBytes = Decay::kAll + In::kBytes + Grad::kBytes;
     char *stage;
     Decay d;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
 template <typename XT, typename GT, int VEC, int KIND>
 __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
     scan_backward(ScanArgs p, const __grid_constant__ ScanMaps maps) {
-    using T = ScanTile<VEC>;
+    using T = ScanTile<XT, VEC>;
     using Stage = BackwardStage<XT, GT, VEC>;
     extern __shared__ __align__(128) char s_stage[];
     __shared__ TileRows rows;
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         // the thread's maps: of the state down its rows, of the adjoint up
         float a[VEC], b[VEC], u[VEC], w[VEC];
         const auto z = [&] {
-            if constexpr (VEC > 1) return HeldGate<XT, VEC>(s_stage);
+            if constexpr (VEC > 1) return HeldGate<XT, T>(s_stage);
             else return in_stage.z;
         }();
         if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
             compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
         }
         bool cut = begin != 0u, cut_up = (begin | end) != 0u;
-        scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
-        scan_groups<VEC, true>(u, w, cut_up, warp, lane, s_u, s_w);
+        scan_groups<T, false>(a, b, cut, warp, lane, s_a, s_b);
+        scan_groups<T, true>(u, w, cut_up, warp, lane, s_u, s_w);
         __syncthreads();
 
         // threads of the first columns: up the warps; of the next: down them, from the state kept
@@ -273,8 +273,8 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
             v[q] = s_b[warp][i];
             l[q] = far ? s_w[warp][i] : fmaf(s_u[warp][i], s_carry[i], s_w[warp][i]);
         }
-        enter_group<VEC, false>(a, b, cut, v);
-        enter_group<VEC, true>(u, w, cut_up, l);
+        enter_group<T, false>(a, b, cut, v);
+        enter_group<T, true>(u, w, cut_up, l);
         if (!on) continue;
         const int64_t row = r0 + group * T::kEach;
         if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);

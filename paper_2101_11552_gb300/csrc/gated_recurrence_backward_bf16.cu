@@ -4,7 +4,7 @@
 namespace tfg {
 
 cudaError_t launch_scan_backward_bf16(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s) {
-    if (vec == 8) return launch_backward_grad<uint16_t, 8>(p, maps, kind, s);
+    if (vec == 4) return launch_backward_grad<uint16_t, 4>(p, maps, kind, s);
     return launch_backward_grad<uint16_t, 1>(p, maps, kind, s);
 }
 

@@ -10,7 +10,7 @@ namespace {
 // A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
 template <typename XT>
 struct ForwardSlots {
-    using T = ScanTile<1>;
+    using T = ScanTile<XT, 1>;
     using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
     using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
     using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
@@ -36,9 +36,9 @@ struct ForwardSlots {
 // A tile's inputs by tensor copies; the decays take the gates' place.
 template <typename XT, int VEC>
 struct ForwardTile {
-    using T = ScanTile<VEC>;
+    using T = ScanTile<XT, VEC>;
     using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
-    using In = TileRow<XT, VEC>;
+    using In = TileRow<XT, T>;
     static constexpr int kBytes = Decay::kAll + In::kBytes;
     char *stage;
     Decay d;
@@ -81,7 +81,7 @@ __device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const
 template <typename XT, typename OT, int VEC, int KIND>
 __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
     scan_forward(ScanArgs p, const __grid_constant__ ScanMaps maps) {
-    using T = ScanTile<VEC>;
+    using T = ScanTile<XT, VEC>;
     using Stage = ForwardStage<XT, VEC>;
     extern __shared__ __align__(128) char s_stage[];
     __shared__ TileRows rows;
@@ -128,14 +128,14 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
 
         float a[VEC], b[VEC];
         const auto z = [&] {
-            if constexpr (VEC > 1) return HeldGate<XT, VEC>(s_stage);
+            if constexpr (VEC > 1) return HeldGate<XT, T>(s_stage);
             else return in_stage.z;
         }();
         if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
         if (plain) compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
         else compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
         bool cut = begin != 0u;
-        scan_groups<VEC, false>(a, b, cut, warp, lane, s_a, s_b);
+        scan_groups<T, false>(a, b, cut, warp, lane, s_a, s_b);
         __syncthreads();
 
         // down the warps, a thread for each channel: what stands before each, and the tile's map
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             const int i = lane * VEC + q;
             v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
         }
-        enter_group<VEC, false>(a, b, cut, v);
+        enter_group<T, false>(a, b, cut, v);
         if (!on) continue;
         OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
         if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);

@@ -39,18 +39,26 @@ template <typename TT, int VEC> struct RowVec {
 // is the ordinary correctly rounded operation).  b and c may be shared by several values:
 // value q takes element q / (VEC / N).
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
+#if !defined(TFG_NO_PACKED_FMA)
     float2 d;
     asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
         "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+#else
+    return make_float2(a.x + b.x, a.y + b.y);
+#endif
 }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+#if !defined(TFG_NO_PACKED_FMA)
     float2 d;
     asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
         "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+#else
+    return make_float2(a.x * b.x, a.y * b.y);
+#endif
 }
 template <int VEC, int N>
 __device__ __forceinline__ float2 pair_of(const float (&v)[N], int q) {
