@@ -11,33 +11,44 @@ cudaError_t launch_row_back_bf16_bf16(const RowBackArgs &p, cudaStream_t s);
 
 namespace {
 
-constexpr int kJoinCols = 32, kJoinRows = 32;
+constexpr int kJoinLanes = 32, kJoinRows = 32;
 constexpr int kBackResident = 3;          // CTAs of a multiprocessor at most (256 threads each)
 
-// out[c] = sum over the CTAs of part[.][c], in 32 interleaved chains joined in order.
-__global__ void __launch_bounds__(kJoinCols *kJoinRows) join_columns_kernel(const float *part, int ctas, int64_t f,
-                                                                            float *gamma, float *beta) {
-    __shared__ float s_part[kJoinRows][kJoinCols];
-    const int x = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + x;
-    float sum = 0.f;
+// out[c] = sum over the CTAs of part[.][c], in 32 interleaved chains joined in order; V columns a thread.
+template <int V>
+__global__ void __launch_bounds__(kJoinLanes *kJoinRows) join_columns_kernel(const float *part, int ctas, int64_t f,
+                                                                             float *gamma, float *beta) {
+    __shared__ __align__(16) float s_part[kJoinRows][kJoinLanes * V];
+    const int x = threadIdx.x % kJoinLanes, y = threadIdx.x / kJoinLanes;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * kJoinLanes + x) * V;
+    float sum[V] = {};
     if (c < 2 * f) {
 #pragma unroll 8
-        for (int b = y; b < ctas; b += kJoinRows) sum += __ldg(part + b * 2 * f + c);
-    }
-    s_part[y][x] = sum;
-    __syncthreads();
-    if (y == 0 && c < 2 * f) {
+        for (int b = y; b < ctas; b += kJoinRows) {
+            float v[V];
+            VecLoad<float, V>::load(part + b * 2 * f + c, v);
 #pragma unroll
-        for (int j = 1; j < kJoinRows; ++j) sum += s_part[j][x];
-        (c < f ? gamma[c] : beta[c - f]) = sum;
+            for (int q = 0; q < V; ++q) sum[q] += v[q];
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < V; ++q) s_part[y][x * V + q] = sum[q];
+    __syncthreads();
+    const int64_t out = static_cast<int64_t>(blockIdx.x) * kJoinLanes * V + threadIdx.x;
+    if (threadIdx.x < kJoinLanes * V && out < 2 * f) {
+        float total = 0.f;
+#pragma unroll
+        for (int j = 0; j < kJoinRows; ++j) total += s_part[j][threadIdx.x];
+        (out < f ? gamma[out] : beta[out - f]) = total;
     }
 }
 
 }  // namespace
 
 cudaError_t join_columns(const float *part, int ctas, int64_t f, float *gamma, float *beta, cudaStream_t s) {
-    join_columns_kernel<<<ceil_div(2 * f, kJoinCols), kJoinCols * kJoinRows, 0, s>>>(part, ctas, f, gamma, beta);
+    // four columns a thread where that leaves a CTA for most multiprocessors
+    if (f % 2 == 0 && f >= 8192) join_columns_kernel<4><<<ceil_div(2 * f, 4 * kJoinLanes), kJoinLanes * kJoinRows, 0, s>>>(part, ctas, f, gamma, beta);
+    else join_columns_kernel<1><<<ceil_div(2 * f, kJoinLanes), kJoinLanes * kJoinRows, 0, s>>>(part, ctas, f, gamma, beta);
     return cudaGetLastError();
 }
 
