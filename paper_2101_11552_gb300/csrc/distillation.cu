@@ -9,6 +9,15 @@
 // the sum of e^((s - m) / tau), the second writes the gradient from them; the terms at the teacher's classes are
 // written over it.  q is formed from s - m, which is exact or nearly so, and loss terms from
 // (s - m) / tau - log(sum), so logits that share a large offset lose nothing.
+//
+// With the gradient a row of up to 222 KB is held in shared memory, by bulk copies that the first pass follows, and read
+// from memory once; the loss alone follows copies through a ring of six chunks.
+//
+// What bounds it: memory, and the exponentials beside it (two a value with the gradient, 16 a clock on a
+// multiprocessor).  16,384 x 50,000 bf16 with gradient, a tenth masked: 541 us (3.1 GB, 5.8 TB/s; the exponentials take
+// 319), read twice from L2 and memory 662.  4,096 x 131,072 bf16, the loss alone: 180 us (6.0 TB/s; plain loads, four
+// vectors in flight a thread, 195).  2,500 x 49,999 fp32: loss 82 us (6.1 TB/s; plain loads 105), backward 154 (6.5 TB/s).
+// 2,708 x 41 fp32, a warp a row: 8 us, latency.
 #include <type_traits>
 
 #include "widen.cuh"

@@ -1,32 +1,35 @@
 // Gated linear recurrence along the rows of each sequence of a batch: what the forward
-// (gated_recurrence.cu) and the backward (gated_recurrence_backward.cu) share.
+// (gated_recurrence_forward.cuh) and the backward (gated_recurrence_backward.cuh) share.
 //
 //   v_t = a_t v_{t-1} + b_t, channel by channel, rows node_offsets[s] .. node_offsets[s + 1] - 1
 //   sigmoid gate: a = 1 / (1 + e^-z), b = (1 - a) x;   exp gate: a = e^z, b = x
 //
 // A row is an affine map of the state, and maps compose: (A, B) then (a, b) is (a A, a B + b).
-// A CTA takes a tile of 128 rows by 32 or 64 channels into shared memory (one tensor copy for an array; value
-// by value where rows are not whole 16 bytes); each thread composes the maps of its few rows, the threads' maps are composed
-// down the tile in shared memory, the tile's map is published, the state that enters the tile
-// is found from what the tiles before it published, and a second walk over the tile makes the
-// outputs.  So the inputs come from memory once, however long a sequence is.  A row that begins
-// a sequence forgets what comes before it, so tiles need not know sequences.
+// A CTA takes tiles of 128 rows by 32 or 64 channels into shared memory (one tensor copy for an array; value by value
+// where rows are not whole 16 bytes).  Each thread composes the maps of its few rows, the threads' maps are composed down
+// the tile, the tile's map is published, the state that enters the tile is found from what the tiles before it
+// published, and a second walk over the tile makes the outputs.  So the inputs come from memory once, however long a
+// sequence is.  A row that begins a sequence forgets what comes before it, so tiles need not know sequences.
 //
-// The entering state.  Tiles stand in windows of 32.  A tile composes the maps of those before it
-// in its window, and the last one of a window publishes the state that enters the next.  A tile
-// behind the beginning of a sequence in its window needs no more than that.  What is composed
-// and in which order depends on nothing but the sizes and offsets, so results are bitwise
-// reproducible; with states passed on from tile to tile a batch of 1,000 tiles would take as
-// many trips through L2.  A map and a state are each one word, all ones until they are published, so a
-// reader looks at the value itself: no flag, no fence, one trip.  Tiles are handed out in
-// order by a counter: a tile waits only for tiles that are already running.  It publishes before it
-// waits, and asks for its next tile when its own waiting is over: CTAs that held a second tile while the first
-// waited (its copies in flight) made a convoy of it, 213 us in place of 70 for 1,024 molecules
-// forward.
+// The entering state.  Tiles stand in windows of 32.  A tile composes the maps of those before it in its window, and the
+// last one of a window publishes the state that enters the next.  A tile behind the beginning of a sequence in its window
+// needs no more than that.  What is composed and in which order depends on nothing but the sizes and offsets, so results
+// are bitwise reproducible; with states passed on from tile to tile a batch of 1,000 tiles would take as many trips
+// through L2.  A map and a state are each one word, all ones until they are published, so a reader looks at the value
+// itself: no flag, no fence, one trip.  Tiles are handed out in order by a counter: a tile waits only for tiles that are
+// already running.  It publishes before it waits, and asks for its next tile when its own waiting is over: CTAs that held
+// a second tile while the first waited made a convoy of it (1,024 molecules forward: 213 us, where one tile at a
+// time took 42).
 //
-// Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps
-// its distance from 1 to a few u, where a rounded a would change a memory of 1,000 steps by
-// 1,000 u.  All in fp32.
+// Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps its distance from 1
+// to a few u, where a rounded a would change a memory of 1,000 steps by 1,000 u.  All in fp32.
+//
+// What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 185 us
+// (805 MB, 4.4 TB/s, 26 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
+// were left without the waits for other tiles), backward 326 us (1.34 GB, 4.1 TB/s, 41 instructions).  One sequence of
+// 131,072 x 256, bf16 to fp32: 70 and 117 us.  1,024 molecules, 112,640 x 128 fp32: 37 and 62 us, and 4 us each for the
+// plan.  128 threads a tile with twice the rows each take a third fewer instructions and are slower (209 and 459 us for
+// the first, too few warps), 8 channels a thread 200 and 353, copies of 16 bytes a lane 220 and 383.
 #pragma once
 
 #include "widen.cuh"
@@ -92,7 +95,6 @@ struct ScanSpace {
         bytes = plan + sizeof(TileRows) * size_t(tiles);
     }
 };
-
 
 // Tensor maps of gate, x and dL/dout, for tiles of a vector width above 1.
 struct ScanMaps {
