@@ -12,6 +12,7 @@ log p is a difference of (t - t_max) / T and the log of a sum of k terms: el = 4
   the sum of |terms|
 A gradient stored in bf16 adds half a step, 2^-8 of it.
 """
+import gc
 import math
 
 import pytest
@@ -31,6 +32,9 @@ def _built():
         pytest.skip("no CUDA device")
     from paper_2101_11552_gb300 import build
     build.build_library()
+    yield
+    gc.collect()                                             # exceptions that tests kept, and the tensors in their frames
+    torch.cuda.empty_cache()
 
 
 def close(got, want, tol, what):

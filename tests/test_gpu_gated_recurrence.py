@@ -16,6 +16,7 @@ A result stored in bf16 adds half a step, 2^-8 of it.  Below 2^-126 the rounding
 relative: a value there is off by half a step of 2^-149 each time, 10^4 rows of four such roundings by
 less than 1e-40 (met where only the final state has a gradient and 380 rows of gates lie between).
 """
+import gc
 import pytest
 import torch
 
@@ -32,6 +33,9 @@ def _built():
         pytest.skip("no CUDA device")
     from paper_2101_11552_gb300 import build
     build.build_library()
+    yield
+    gc.collect()                                             # exceptions that tests kept, and the tensors in their frames
+    torch.cuda.empty_cache()
 
 
 def close(got, want, tol, what):

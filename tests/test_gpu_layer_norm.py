@@ -16,6 +16,7 @@ error of K r mean |c'|, |c'| <= |c| + u |m|):
   Kn = (N + 120) u of sum |t| whatever the split; terms off by |g| eh'.
 A result stored in bf16 adds half a step, 2^-8 of it.
 """
+import gc
 import pytest
 import torch
 
@@ -33,6 +34,9 @@ def _built():
         pytest.skip("no CUDA device")
     from paper_2101_11552_gb300 import build
     build.build_library()
+    yield
+    gc.collect()                                             # exceptions that tests kept, and the tensors in their frames
+    torch.cuda.empty_cache()
 
 
 def close(got, want, tol, what):

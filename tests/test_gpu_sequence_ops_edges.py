@@ -1,6 +1,7 @@
 """Calls that the documentation of the layer-norm, recurrence and distillation entry points allows and that
 ordinary batches do not make: rows apart by odd strides, arrays of more than 2^31 values, calls from
 several threads, more teacher entries than classes, statuses that earlier calls left."""
+import gc
 import threading
 
 import pytest
@@ -19,6 +20,9 @@ def _built():
     if not torch.cuda.is_available():
         pytest.skip("no CUDA device")
     build.build_library()
+    yield
+    gc.collect()                                             # exceptions that tests kept, and the tensors in their frames
+    torch.cuda.empty_cache()
 
 
 def apart(t, ld, first):

@@ -9,6 +9,7 @@ The step, for nodes in order along the sequences of a batch:
 The products are torch's in fp32.  Every operator's own test bounds its error; here gradients are held
 to 3e-5 of their 2-norm: a chain of ten fp32 steps, each within a few 1e-6.
 """
+import gc
 import os
 
 import numpy as np
@@ -29,6 +30,9 @@ def _built():
         pytest.skip("no CUDA device")
     build.build_library()
     torch.backends.cuda.matmul.allow_tf32 = False
+    yield
+    gc.collect()                                             # exceptions that tests kept, and the tensors in their frames
+    torch.cuda.empty_cache()
 
 
 def batch(seed, graphs=9):
@@ -242,6 +246,7 @@ def test_bounds_checked_build():
         assert same(job.step(), want)
         # inside one allocation, so that even a launch would stay within it: buffers that end
         # where the allocation does are refused when a call says that they hold more
+        gc.collect()
         torch.cuda.empty_cache()
         buf = torch.zeros((32 << 20) // 4, device="cuda")
         seg = [s for s in torch.cuda.memory_snapshot()
