@@ -370,9 +370,8 @@ struct Jobs {
         if (threadIdx.x == 0) asked = p.linked ? atomicAdd(p.next, 1u) : count;
     }
     __device__ __forceinline__ bool next(const ScanArgs &p, uint32_t &job) {
+        if (threadIdx.x == 0) *s_next = asked;               // the last one was read many barriers ago
         before_copies();
-        __syncthreads();
-        if (threadIdx.x == 0) *s_next = asked;
         __syncthreads();
         job = *s_next;
         return job < count;
