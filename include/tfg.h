@@ -704,10 +704,10 @@ int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, con
  *        NULL and sum_dtype is not looked at.
  *   gamma, beta (device) fp32 [num_features], or NULL for 1 and 0.
  *   eps: finite, > 0.
- *   out (device) [num_rows, num_features], out_dtype; must not overlap an
- *        input or sum.
+ *   out (device) [num_rows, num_features], out_dtype.
  *   mean, rstd (device) fp32 [num_rows]: m and r, written for the backward;
  *        both or neither may be NULL.
+ * Outputs overlap no input and no other output (but sum, which may be residual).
  * An offset common to a row's values costs nothing: deviations are taken from
  * the mean before its rounding to fp32.
  *
@@ -720,12 +720,12 @@ int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, con
  *   grad_sum (device) [num_rows, num_features] of grad_sum_dtype, or NULL: the
  *        gradient that reaches s by other ways (the stream's own).
  *   grad_s (device) [num_rows, num_features] of grad_sum_dtype, the gradient of
- *        x and of the residual alike; may be grad_sum, must not overlap
- *        another input.
+ *        x and of the residual alike; may be grad_sum.
  *   grad_gamma, grad_beta (device) fp32 [num_features], written (0 without
  *        rows); both or neither may be NULL.
  *   workspace (device) >= tfg_layer_norm_backward_workspace_size() bytes,
  *        16-byte aligned; not used, and may be NULL, without grad_gamma.
+ * Outputs overlap no input and no other output (but grad_s, which may be grad_sum).
  * Rows of NaN or infinities give NaN in their own row, and in grad_gamma and
  * grad_beta.  Sums in fp32 in a fixed order: bitwise reproducible between calls
  * of the same alignment.
@@ -842,8 +842,9 @@ int tfg_gated_recurrence_backward(const void *gate, int64_t gate_stride, const v
  *   (Ids outside the range are not reported a second time.)
  * Logits of -inf are classes without probability (an infinite loss where p > 0);
  * a row without another, with +inf or with NaN gives NaN in that row alone.
- * top_k <= 1,024 (TFG_ERR_TOO_LARGE).  grad_logits overlaps no input.  Sums in
- * fp32 in a fixed order: bitwise reproducible between calls of the same alignment.
+ * top_k <= 1,024 (TFG_ERR_TOO_LARGE).  Outputs overlap no input and no other
+ * output.  Sums in fp32 in a fixed order: bitwise reproducible between calls of
+ * the same alignment.
  * ---------------------------------------------------------------------- */
 int tfg_distillation_loss(const void *logits, int dtype, int64_t num_rows, int64_t num_classes,
                           const int64_t *ids, const void *teacher, int teacher_dtype,

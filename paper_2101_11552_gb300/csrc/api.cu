@@ -1268,10 +1268,37 @@ int check_eps(const char *fn, float eps) {
     if (!(eps > 0.f) || !std::isfinite(eps)) return fail(TFG_ERR_INVALID_ARG, "%s: eps must be finite and positive", fn);
     return TFG_OK;
 }
-int no_overlap(const char *fn, const char *out_name, const void *out, size_t out_bytes, const char *name, const void *p,
-               size_t bytes) {
-    if (p != nullptr && out != nullptr && overlap(out, out_bytes, p, bytes))
-        return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, out_name, name);
+
+// An array of rows that may begin further apart than they are long.
+struct Rows {
+    const char *name;
+    const void *p;
+    size_t stride, width, extent;        // bytes; extent: from the first byte to the last
+    Rows(const char *nm, const void *ptr, int64_t n, int64_t ld, int64_t f, size_t elem)
+        : name(nm), p(ptr), stride(size_t(ld) * elem), width(size_t(f) * elem),
+          extent(n > 0 ? size_t(n - 1) * size_t(ld) * elem + size_t(f) * elem : 0) {}
+};
+
+// Whether rows of a and b share a byte; columns side by side in rows of one buffer do not.
+bool rows_overlap(const Rows &a, const Rows &b) {
+    if (a.p == nullptr || b.p == nullptr || !overlap(a.p, a.extent, b.p, b.extent)) return false;
+    if (a.stride != b.stride) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const Rows &low = pa <= pb ? a : b, &high = pa <= pb ? b : a;
+    const size_t off = (pa <= pb ? pb - pa : pa - pb) % a.stride;
+    return !(off >= low.width && off + high.width <= a.stride);
+}
+
+// Every output against every input and every later output.
+int check_apart(const char *fn, const Rows *outs, int num_outs, const Rows *ins, int num_ins) {
+    for (int i = 0; i < num_outs; ++i) {
+        for (int j = 0; j < num_ins; ++j)
+            if (rows_overlap(outs[i], ins[j]))
+                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, ins[j].name);
+        for (int j = i + 1; j < num_outs; ++j)
+            if (rows_overlap(outs[i], outs[j]))
+                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, outs[j].name);
+    }
     return TFG_OK;
 }
 }  // namespace
@@ -1300,16 +1327,14 @@ int tfg_layer_norm(const void *x, int x_dtype, const void *residual, int sum_dty
     if (residual) {
         TFG_TRY(check_element(fn, "residual", residual, sum_dtype));
         TFG_TRY(check_element(fn, "sum", sum, sum_dtype));
-        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "x", x, x_bytes));
-        if (sum != residual) TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "residual", residual, sum_bytes));
-        TFG_TRY(no_overlap(fn, "out", out, out_bytes, "residual", residual, sum_bytes));
-        TFG_TRY(no_overlap(fn, "out", out, out_bytes, "sum", sum, sum_bytes));
-        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "gamma", gamma, w_bytes));
-        TFG_TRY(no_overlap(fn, "sum", sum, sum_bytes, "beta", beta, w_bytes));
     }
-    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "x", x, x_bytes));
-    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "gamma", gamma, w_bytes));
-    TFG_TRY(no_overlap(fn, "out", out, out_bytes, "beta", beta, w_bytes));
+    const int64_t n = num_rows, f = num_features;
+    const size_t sum_elem = residual ? elem_bytes(sum_dtype) : 0;
+    const Rows ins[] = {{"x", x, n, f, f, elem_bytes(x_dtype)}, {"residual", sum == residual ? nullptr : residual, n, f, f, sum_elem},
+                        {"gamma", gamma, 1, f, f, 4}, {"beta", beta, 1, f, f, 4}};
+    const Rows outs[] = {{"out", out, n, f, f, elem_bytes(out_dtype)}, {"sum", residual ? sum : nullptr, n, f, f, sum_elem},
+                         {"mean", mean, 1, n, n, 4}, {"rstd", rstd, 1, n, n, 4}};
+    TFG_TRY(check_apart(fn, outs, 4, ins, 4));
     TFG_DEBUG(debug_extent(fn, "x", x, x_bytes));
     TFG_DEBUG(debug_extent(fn, "residual", residual, sum_bytes));
     TFG_DEBUG(debug_extent(fn, "sum", sum, sum_bytes));
@@ -1356,10 +1381,14 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
     TFG_TRY(check_element(fn, "grad_out", grad_out, grad_dtype));
     TFG_TRY(check_element(fn, "grad_sum", grad_sum, grad_sum_dtype));
     TFG_TRY(check_element(fn, "grad_s", grad_s, grad_sum_dtype));
-    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "sum", sum, s_bytes));
-    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "grad_out", grad_out, g_bytes));
-    if (grad_s != grad_sum) TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "grad_sum", grad_sum, gs_bytes));
-    TFG_TRY(no_overlap(fn, "grad_s", grad_s, gs_bytes, "gamma", gamma, w_bytes));
+    const int64_t n = num_rows, f = num_features;
+    const size_t gs_elem = elem_bytes(grad_sum_dtype);
+    const Rows ins[] = {{"sum", sum, n, f, f, elem_bytes(sum_dtype)}, {"grad_out", grad_out, n, f, f, elem_bytes(grad_dtype)},
+                        {"grad_sum", grad_sum == grad_s ? nullptr : grad_sum, n, f, f, gs_elem}, {"gamma", gamma, 1, f, f, 4},
+                        {"mean", mean, 1, n, n, 4}, {"rstd", rstd, 1, n, n, 4}};
+    const Rows outs[] = {{"grad_s", grad_s, n, f, f, gs_elem}, {"grad_gamma", grad_gamma, 1, f, f, 4},
+                         {"grad_beta", grad_beta, 1, f, f, 4}};
+    TFG_TRY(check_apart(fn, outs, 3, ins, 6));
     const size_t need = grad_gamma ? tfg::layer_norm_backward_workspace_bytes(num_rows, num_features) : 0;
     TFG_TRY(check_workspace(fn, workspace, workspace_bytes, need, 16));
     TFG_DEBUG(debug_extent(fn, "sum", sum, s_bytes));
@@ -1381,26 +1410,6 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
 // ---- gated linear recurrence ----------------------------------------------------------
 namespace {
 constexpr int64_t kMaxTiles = (int64_t(1) << 31) - (int64_t(1) << 16);
-
-// An array of rows that may begin further apart than they are long.
-struct Rows {
-    const char *name;
-    const void *p;
-    size_t stride, width, extent;        // bytes; extent: from the first byte to the last
-    Rows(const char *nm, const void *ptr, int64_t n, int64_t ld, int64_t f, size_t elem)
-        : name(nm), p(ptr), stride(size_t(ld) * elem), width(size_t(f) * elem),
-          extent(n > 0 ? size_t(n - 1) * size_t(ld) * elem + size_t(f) * elem : 0) {}
-};
-
-// Whether rows of a and b share a byte; columns side by side in rows of one buffer do not.
-bool rows_overlap(const Rows &a, const Rows &b) {
-    if (a.p == nullptr || b.p == nullptr || !overlap(a.p, a.extent, b.p, b.extent)) return false;
-    if (a.stride != b.stride) return true;
-    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-    const Rows &low = pa <= pb ? a : b, &high = pa <= pb ? b : a;
-    const size_t off = (pa <= pb ? pb - pa : pa - pb) % a.stride;
-    return !(off >= low.width && off + high.width <= a.stride);
-}
 
 int check_recurrence(const char *fn, int64_t num_rows, int64_t num_sequences, int64_t num_features) {
     TFG_TRY(check_counts(fn, num_rows, 0));
@@ -1427,18 +1436,6 @@ int check_stride(const char *fn, const char *name, int64_t num_rows, int64_t str
     return TFG_OK;
 }
 
-// Every output against every input and every later output.
-int check_apart(const char *fn, const Rows *outs, int num_outs, const Rows *ins, int num_ins) {
-    for (int i = 0; i < num_outs; ++i) {
-        for (int j = 0; j < num_ins; ++j)
-            if (rows_overlap(outs[i], ins[j]))
-                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, ins[j].name);
-        for (int j = i + 1; j < num_outs; ++j)
-            if (rows_overlap(outs[i], outs[j]))
-                return fail(TFG_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, outs[i].name, outs[j].name);
-    }
-    return TFG_OK;
-}
 }  // namespace
 
 int tfg_gated_recurrence_workspace_size(int64_t num_rows, int64_t num_features, size_t *bytes) {
@@ -1582,14 +1579,22 @@ int check_distillation(const char *fn, const Distil &a) {
     return TFG_OK;
 }
 
-int check_grad_logits(const char *fn, const Distil &a, const void *grad) {
-    const size_t bytes = elem_bytes(a.dtype) * size_t(a.num_rows * a.num_classes), top = size_t(a.num_rows * a.top_k);
+// Outputs against the inputs: stats are one or the other.
+int check_distillation_apart(const char *fn, const Distil &a, const float *loss, const float *stats, const float *grad_loss,
+                             const void *grad) {
+    const int64_t n = a.num_rows, v = a.num_classes, k = a.top_k;
     TFG_TRY(check_element(fn, "grad_logits", grad, a.dtype));
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "logits", a.logits, bytes));
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "ids", a.ids, (a.id32 ? 4 : 8) * top));
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "teacher", a.teacher, elem_bytes(a.teacher_dtype) * top));
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "row_weight", a.row_weight, sizeof(float) * size_t(a.num_rows)));
-    TFG_DEBUG(debug_extent(fn, "grad_logits", grad, bytes));
+    if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(TFG_ERR_INVALID_ARG, "%s: stats must be 8-byte aligned", fn);
+    const Rows all_stats{"stats", stats, n, 2, 2, 4}, none{"stats", nullptr, 0, 2, 2, 4};
+    const Rows ins[] = {{"logits", a.logits, n, v, v, elem_bytes(a.dtype)}, {"ids", a.ids, n, k, k, a.id32 ? 4u : 8u},
+                        {"teacher", a.teacher, n, k, k, elem_bytes(a.teacher_dtype)}, {"row_weight", a.row_weight, 1, n, n, 4},
+                        {"grad_loss", grad_loss, 1, n, n, 4}, loss ? none : all_stats};
+    const Rows outs[] = {{"grad_logits", grad, n, v, v, elem_bytes(a.dtype)}, {"loss", loss, 1, n, n, 4}, loss ? all_stats : none};
+    TFG_TRY(check_apart(fn, outs, 3, ins, 6));
+    TFG_DEBUG(debug_extent(fn, "grad_logits", grad, outs[0].extent));
+    TFG_DEBUG(debug_extent(fn, "loss", loss, outs[1].extent));
+    TFG_DEBUG(debug_extent(fn, "stats", stats, all_stats.extent));
+    TFG_DEBUG(debug_extent(fn, "grad_loss", grad_loss, ins[4].extent));
     return TFG_OK;
 }
 
@@ -1599,10 +1604,7 @@ int distillation_common(const char *fn, const Distil &a, int64_t padding_id, flo
     TFG_TRY(check_distillation(fn, a));
     TFG_NEED(loss, a.num_rows > 0, fn, "loss");
     TFG_NEED(status, true, fn, "status");
-    TFG_TRY(check_grad_logits(fn, a, grad));
-    if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(TFG_ERR_INVALID_ARG, "%s: stats must be 8-byte aligned", fn);
-    TFG_DEBUG(debug_extent(fn, "loss", loss, sizeof(float) * size_t(a.num_rows)));
-    TFG_DEBUG(debug_extent(fn, "stats", stats, 2 * sizeof(float) * size_t(a.num_rows)));
+    TFG_TRY(check_distillation_apart(fn, a, loss, stats, nullptr, grad));
     return cuda_result(tfg::launch_distillation(a.logits, a.dtype, a.num_rows, a.num_classes, a.ids, a.id32, a.teacher,
                                                 a.teacher_dtype, static_cast<int>(a.top_k), padding_id, a.temperature,
                                                 a.row_weight, loss, stats, grad, status, reinterpret_cast<cudaStream_t>(stream)),
@@ -1616,13 +1618,7 @@ int distillation_backward_common(const char *fn, const Distil &a, int64_t paddin
     TFG_NEED(stats, a.num_rows > 0, fn, "stats");
     TFG_NEED(grad_loss, a.num_rows > 0, fn, "grad_loss");
     TFG_NEED(grad, a.num_rows > 0, fn, "grad_logits");
-    TFG_TRY(check_grad_logits(fn, a, grad));
-    const size_t bytes = elem_bytes(a.dtype) * size_t(a.num_rows * a.num_classes), row = sizeof(float) * size_t(a.num_rows);
-    if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(TFG_ERR_INVALID_ARG, "%s: stats must be 8-byte aligned", fn);
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "stats", stats, 2 * row));
-    TFG_TRY(no_overlap(fn, "grad_logits", grad, bytes, "grad_loss", grad_loss, row));
-    TFG_DEBUG(debug_extent(fn, "stats", stats, 2 * row));
-    TFG_DEBUG(debug_extent(fn, "grad_loss", grad_loss, row));
+    TFG_TRY(check_distillation_apart(fn, a, nullptr, stats, grad_loss, grad));
     return cuda_result(tfg::launch_distillation_backward(a.logits, a.dtype, a.num_rows, a.num_classes, a.ids, a.id32, a.teacher,
                                                          a.teacher_dtype, static_cast<int>(a.top_k), padding_id, a.temperature,
                                                          a.row_weight, stats, grad_loss, grad,

@@ -10,6 +10,7 @@ OTHER = ctypes.c_void_p(0x900000)
 THIRD = ctypes.c_void_p(0x2000000)
 OUT = ctypes.c_void_p(0x40000000)
 OUT2 = ctypes.c_void_p(0x50000000)
+OUT3 = ctypes.c_void_p(0x60000000)
 WS = ctypes.c_void_p(0x80000000)
 SMALL = ctypes.c_void_p(0x700000)
 
@@ -47,17 +48,22 @@ def test_layer_norm_rejects(lib):
     assert call(out=FAKE) == -1 and call(out=OTHER) == -1 and call(out=THIRD) == -1 and "overlap" in err(lib)
     assert call(sum=FAKE) == -1 and call(sum=ctypes.c_void_p(0x900004)) == -1 and "overlap" in err(lib)
     assert call(gamma=OUT) == -1 and call(beta=THIRD) == -1
+    for other in (FAKE, OTHER, THIRD, OUT, OUT2):           # statistics over an array, or over one another
+        assert call(mean=other, rstd=OUT2) == -1 and call(mean=OUT2, rstd=other) == -1 and "overlap" in err(lib), other
     assert call(x=ctypes.c_void_p(0x100002)) == -1 and call(res=ctypes.c_void_p(0x900001), sdt=1) == -1 and "aligned" in err(lib)
 
 
 def test_layer_norm_backward_rejects(lib):
     call = caller(lib.tfg_layer_norm_backward, dict(s=FAKE, sdt=0, n=100, f=24, gamma=None, mean=SMALL, rstd=SMALL, g=OTHER, gdt=0,
-                                                    skip=THIRD, gs=OUT, xdt=0, gg=OUT2, gb=OUT2, ws=WS, wsb=1 << 30, st=None))
+                                                    skip=THIRD, gs=OUT, xdt=0, gg=OUT2, gb=OUT3, ws=WS, wsb=1 << 30, st=None))
     for missing in ("s", "mean", "rstd", "g", "gs"):
         assert call(**{missing: None}) == -1, missing
     assert call(gg=None) == -1 and call(gb=None) == -1 and "both or neither" in err(lib)
     assert call(gs=FAKE) == -1 and call(gs=OTHER) == -1 and call(gs=ctypes.c_void_p(0x2000004)) == -1 and "overlap" in err(lib)
     assert call(gamma=OUT) == -1
+    for other in (FAKE, OTHER, THIRD, OUT, SMALL):
+        assert call(gg=other) == -1 and "overlap" in err(lib) and call(gb=other) == -1 and "overlap" in err(lib), other
+    assert call(gg=OUT2, gb=OUT2) == -1 and "overlap" in err(lib)
     assert call(sdt=2) == -1 and call(gdt=2) == -1 and call(xdt=2) == -1
     assert call(ws=None) == -3 and call(wsb=8) == -3 and call(ws=ctypes.c_void_p(0x80000008)) == -1
     n = ctypes.c_size_t(0)
@@ -129,6 +135,9 @@ def test_distillation_rejects(lib, suffix):
         assert call(**{missing: None}) == -1, missing
     for other in (FAKE, OTHER, THIRD):
         assert call(grad=other) == -1 and "overlap" in err(lib)
+    for other in (FAKE, OTHER, THIRD, OUT):
+        assert call(loss=other) == -1 and "overlap" in err(lib) and call(stats=other) == -1 and "overlap" in err(lib), other
+    assert call(stats=SMALL) == -1 and call(w=SMALL) == -1 and "overlap" in err(lib)
     assert call(w=OUT) == -1 and call(stats=ctypes.c_void_p(0x700004)) == -1
     assert call(logits=ctypes.c_void_p(0x100002)) == -1 and call(grad=ctypes.c_void_p(0x40000002)) == -1
     for name in ("logits", "stats", "loss", "grad"):
