@@ -172,11 +172,11 @@ struct HeldRow {
     __device__ __forceinline__ bool wait(int chunk) const {
         return phase_done(&bars[chunk % SLOTS], static_cast<uint32_t>(chunk / SLOTS) & 1u);
     }
-    __device__ __forceinline__ typename VecLoad<XT, VEC>::Raw raw(int i) const {
+    __device__ __forceinline__ typename VecLoad<XT, VEC>::Raw raw(int64_t i) const {
         return load_plain<XT, VEC>(reinterpret_cast<const XT *>(data) + i * VEC);
     }
     __device__ __forceinline__ void widen(int64_t i, float (&v)[VEC]) const {
-        VecLoad<XT, VEC>::widen(load_plain<XT, VEC>(reinterpret_cast<const XT *>(data) + i * VEC), v);
+        VecLoad<XT, VEC>::widen(raw(i), v);
     }
     __device__ __forceinline__ float value(const RowSpan<XT, VEC> &r, int64_t c) const {
         float v[1];
@@ -453,9 +453,13 @@ cudaError_t launch_team(const DistilArgs &a, cudaStream_t s) {
         const size_t shared = kMode == kBothHeld ? row : (kMode == kBack ? top : top + (values < ring ? values : ring));
         if (row <= kHold128) return launch_rows<XT, VEC, 128, kMode>(a, shared, s);
         if (row <= kHold256) return launch_rows<XT, VEC, 256, kMode>(a, shared, s);
-        if (row <= kHoldMost || kMode != kBothHeld) return launch_rows<XT, VEC, kRowThreads, kMode>(a, shared, s);
+        if constexpr (kMode == kBothHeld) {
+            if (row > kHoldMost) return launch_rows<XT, VEC, kRowThreads, MODE>(a, top, s);
+        }
+        return launch_rows<XT, VEC, kRowThreads, kMode>(a, shared, s);
+    } else {
+        return launch_rows<XT, 1, kRowThreads, MODE>(a, top, s);
     }
-    return launch_rows<XT, VEC, kRowThreads, MODE>(a, top, s);
 }
 
 template <typename XT, int VEC>

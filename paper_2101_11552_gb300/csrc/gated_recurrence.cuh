@@ -304,7 +304,7 @@ constexpr int kWarpRows = kTileRows / kScanWarps;            // rows of a warp
 template <typename XT, int N>
 struct ScanTile {
     static constexpr int VEC = N;
-    static constexpr int kLane = VEC * 4 > 16 ? 16 : VEC * 4, kRow = VEC * 4 * kScanThreads;   // of fp32 slots
+    static constexpr int kLane = VEC * 4, kRow = kLane * kScanThreads;                         // of fp32 slots
     static constexpr int kAcross = VEC == 1 ? 32 : (sizeof(XT) == 2 ? 16 : 8);
     static constexpr int kEach = kTileRows * kAcross / kScanThreads;
     static constexpr int kWide = kAcross * VEC;              // channels

@@ -22,10 +22,10 @@ namespace {
 template <typename XT, typename GT>
 struct BackwardSlots {
     using T = ScanTile<XT, 1>;
-    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
-    using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
-    using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
-    using Grad = Slots<GT, 1, T::kEach, kScanThreads, T::kAcross>;
+    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kLane, T::kRow>;
+    using Decay = Slots<float, 1, T::kEach, kScanThreads>;
+    using In = Slots<XT, 1, T::kEach, kScanThreads>;
+    using Grad = Slots<GT, 1, T::kEach, kScanThreads>;
     static constexpr int kBytes = Decay::kAll + In::kAll + Grad::kAll;
     Gate z;
     Decay d;
@@ -37,15 +37,15 @@ struct BackwardSlots {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows + group * T::kEach;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = c < p.f ? 1 : 0;
+        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
         const GT *gp = static_cast<const GT *>(p.g) + r0 * p.f + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld, cols);
-                x.copy(j, xp + j * p.x_ld, cols);
-                if (p.g) g.copy(j, gp + j * p.f, cols);
+                z.copy(j, zp + j * p.gate_ld);
+                x.copy(j, xp + j * p.x_ld);
+                if (p.g) g.copy(j, gp + j * p.f);
             }
         if (p.linked) copy_plan(p, tile, rows);
     }
@@ -54,7 +54,7 @@ struct BackwardSlots {
 template <typename XT, typename GT, int VEC>
 struct BackwardTile {
     using T = ScanTile<XT, VEC>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
     using In = TileRow<XT, T>;
     using Grad = TileRow<GT, T>;
     static constexpr int kBytes = Decay::kAll + In::kBytes + Grad::kBytes;

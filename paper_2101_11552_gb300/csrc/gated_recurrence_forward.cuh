@@ -11,9 +11,9 @@ namespace {
 template <typename XT>
 struct ForwardSlots {
     using T = ScanTile<XT, 1>;
-    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross, T::kLane, T::kRow>;
-    using Decay = Slots<float, 1, T::kEach, kScanThreads, T::kAcross>;
-    using In = Slots<XT, 1, T::kEach, kScanThreads, T::kAcross>;
+    using Gate = Slots<XT, 1, T::kEach, kScanThreads, T::kLane, T::kRow>;
+    using Decay = Slots<float, 1, T::kEach, kScanThreads>;
+    using In = Slots<XT, 1, T::kEach, kScanThreads>;
     static constexpr int kBytes = Decay::kAll + In::kAll;
     Gate z;
     Decay d;
@@ -22,13 +22,13 @@ struct ForwardSlots {
     __device__ __forceinline__ void copy(const ScanArgs &p, const Job &job, TileRows &rows) const {
         const int lane = threadIdx.x % T::kAcross, group = threadIdx.x / T::kAcross;
         const int64_t c = static_cast<int64_t>(job.strip) * T::kWide + lane, r0 = job.order * kTileRows + group * T::kEach;
-        const int left = static_cast<int>(min64(p.n - r0, T::kEach)), cols = c < p.f ? 1 : 0;
+        const int left = c < p.f ? static_cast<int>(min64(p.n - r0, T::kEach)) : 0;
         const XT *zp = static_cast<const XT *>(p.gate) + r0 * p.gate_ld + c, *xp = static_cast<const XT *>(p.x) + r0 * p.x_ld + c;
 #pragma unroll
         for (int j = 0; j < T::kEach; ++j)
             if (j < left) {
-                z.copy(j, zp + j * p.gate_ld, cols);
-                x.copy(j, xp + j * p.x_ld, cols);
+                z.copy(j, zp + j * p.gate_ld);
+                x.copy(j, xp + j * p.x_ld);
             }
         if (p.linked) copy_plan(p, job.order, rows);
     }
@@ -37,7 +37,7 @@ struct ForwardSlots {
 template <typename XT, int VEC>
 struct ForwardTile {
     using T = ScanTile<XT, VEC>;
-    using Decay = Slots<float, VEC, T::kEach, kScanThreads, T::kAcross>;
+    using Decay = Slots<float, VEC, T::kEach, kScanThreads>;
     using In = TileRow<XT, T>;
     static constexpr int kBytes = Decay::kAll + In::kBytes;
     char *stage;

@@ -139,64 +139,27 @@ __device__ __forceinline__ void copy_async(void *shared, const void *global) {
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Inputs of a CTA of THREADS in shared memory: every thread's vectors lie in slots of its own, and it
-// alone reads them, so that copies are in flight while others are worked on, without registers and
-// without a barrier.  A vector of 32 bytes lies in two halves, so that lanes side by side read 16 bytes
-// side by side; lanes that hold SIDE vectors side by side in a row copy them together, 16 bytes after
-// 16 bytes: with 16 of its own 32 bytes a lane, L2 was asked for every sector twice.  EACH vectors a
-// thread take kAll bytes of a CTA; LANE: bytes from a thread's part to the next one's, ROW: from one of
-// its vectors to the next.
-template <typename T, int VEC, int EACH, int THREADS, int SIDE, int LANE = (VEC * sizeof(T) > 16 ? 16 : VEC * sizeof(T)),
-          int ROW = (VEC * sizeof(T) > 16 ? 2 : 1) * THREADS * LANE>
+// Vectors of up to 16 bytes of a CTA of THREADS in shared memory: every thread's lie in slots of its own, and it alone
+// reads them, so that copies are in flight without registers and without a barrier.  EACH vectors a thread take kAll
+// bytes of a CTA; LANE: bytes from a thread's slot to the next one's, ROW: from one of its vectors to the next.
+template <typename T, int VEC, int EACH, int THREADS, int LANE = VEC * sizeof(T), int ROW = THREADS * LANE>
 struct Slots {
-    static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
-    static constexpr int kPart = kBytes > 16 ? 16 : kBytes, kParts = kBytes / kPart;
+    static_assert(VEC * sizeof(T) <= 16, "one copy a vector");
     static constexpr int kAll = (EACH * ROW + 15) / 16 * 16;
     char *at;
     __device__ __forceinline__ explicit Slots(char *stage) : at(stage + threadIdx.x * LANE) {}
-    __device__ __forceinline__ char *part(int j, int h) const { return at + j * ROW + h * THREADS * LANE; }
-    // The vector at `from`, if left > 0 (values from there to the row's end, a multiple of VEC).  Halves copied by
-    // neighbours are there for their thread after its wait and a barrier of the warp.
-    __device__ __forceinline__ void copy(int j, const T *from, int left) const {
-        if constexpr (kParts == 2) {
-            const int l = threadIdx.x % SIDE, h = threadIdx.x & 1;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int away = k * SIDE / 2 + l / 2 - l;   // lanes to the vector whose half is copied
-                if (left - away * VEC > 0)
-                    copy_async<16>(part(j, h) + away * LANE, reinterpret_cast<const char *>(from + away * VEC) + h * 16);
-            }
-        } else {
-            if (left > 0) copy_async<kPart>(part(j, 0), from);
-        }
-    }
+    __device__ __forceinline__ T *slot(int j) const { return reinterpret_cast<T *>(at + j * ROW); }
+    __device__ __forceinline__ void copy(int j, const T *from) const { copy_async<VEC * sizeof(T)>(slot(j), from); }
     __device__ __forceinline__ void zero(int j) const {
 #pragma unroll
-        for (int h = 0; h < kParts; ++h)
-#pragma unroll
-            for (int i = 0; i < kPart; i += 2) *reinterpret_cast<uint16_t *>(part(j, h) + i) = 0;
+        for (int q = 0; q < VEC; ++q) slot(j)[q] = T(0);
     }
     __device__ __forceinline__ void put(int j, const float (&v)[VEC]) const {
         static_assert(sizeof(T) == 4, "fp32 values");
-        if constexpr (VEC % 4 == 0) {
-#pragma unroll
-            for (int q = 0; q < VEC; q += 4) *reinterpret_cast<float4 *>(part(j, q / 4)) = make_float4(v[q], v[q + 1], v[q + 2], v[q + 3]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) reinterpret_cast<float *>(part(j, 0))[q] = v[q];
-        }
+        if constexpr (VEC == 4) *reinterpret_cast<float4 *>(slot(j)) = make_float4(v[0], v[1], v[2], v[3]);
+        else slot(j)[0] = v[0];
     }
-    __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const {
-        if constexpr (kParts == 2) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 q = *reinterpret_cast<const float4 *>(part(j, h));
-                v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
-            }
-        } else {
-            VecLoad<T, VEC>::widen(load_plain<T, VEC>(reinterpret_cast<const T *>(part(j, 0))), v);
-        }
-    }
+    __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const { VecLoad<T, VEC>::widen(load_plain<T, VEC>(slot(j)), v); }
 };
 // The copies issued since the last commit make a group; wait until at most LEFT groups are under way.
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
