@@ -24,12 +24,14 @@
 // Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps its distance from 1
 // to a few u, where a rounded a would change a memory of 1,000 steps by 1,000 u.  All in fp32.
 //
-// What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 185 us
-// (805 MB, 4.4 TB/s, 26 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
-// were left without the waits for other tiles), backward 326 us (1.34 GB, 4.1 TB/s, 41 instructions).  One sequence of
-// 131,072 x 256, bf16 to fp32: 70 and 117 us.  1,024 molecules, 112,640 x 128 fp32: 37 and 62 us, and 4 us each for the
-// plan.  128 threads a tile with twice the rows each take a third fewer instructions and are slower (209 and 459 us for
-// the first, too few warps), 8 channels a thread 200 and 353, copies of 16 bytes a lane 220 and 383.
+// What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 179 us
+// (805 MB, 4.5 TB/s, 26 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
+// were left without the waits for other tiles), backward 318 us (1.34 GB, 4.2 TB/s, 41 instructions).  One sequence of
+// 131,072 x 256, bf16 to fp32: 69 and 112 us.  1,024 molecules, 112,640 x 128 fp32: 38 and 61 us, and 4 us each for the
+// plan.  Of a tile's 18,000 cycles forward 5,000 go by before its inputs are there and 7,000 before the state that enters
+// is; tiles asked for in L2 a round ahead of their copies: 4 % of the kernel (185 and 326 us without).  128 threads a tile
+// with twice the rows each take a third fewer instructions and are slower (209 and 459 us for the first, too few warps),
+// 8 channels a thread 200 and 353, copies of 16 bytes a lane 220 and 383.
 #pragma once
 
 #include "widen.cuh"
@@ -368,6 +370,11 @@ struct Jobs {
     }
     __device__ __forceinline__ void ask(const ScanArgs &p) {
         if (threadIdx.x == 0) asked = p.linked ? atomicAdd(p.next, 1u) : count;
+    }
+    // A job that some CTA takes about when this one is done, to be asked for in L2; false behind the last.
+    __device__ __forceinline__ bool later(const ScanArgs &p, uint32_t job, uint32_t &then) const {
+        then = job + (gridDim.x - p.checkers);
+        return then < count;
     }
     __device__ __forceinline__ bool next(const ScanArgs &p, uint32_t &job) {
         if (threadIdx.x == 0) *s_next = asked;               // the last one was read many barriers ago

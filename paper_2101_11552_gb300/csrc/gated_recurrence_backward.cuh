@@ -73,6 +73,12 @@ struct BackwardTile {
         if (p.g) tile_copy(stage + Decay::kAll + In::kBytes, &maps.g, c, r, bar);
         if (p.linked) bulk_copy(&rows, p.plan + tile, sizeof(TileRows), bar);
     }
+    __device__ __forceinline__ void prefetch(const ScanArgs &p, const ScanMaps &maps, const Job &job) const {
+        const int c = job.strip * T::kWide, r = static_cast<int>(p.tiles - 1 - job.order) * kTileRows;
+        tile_prefetch(&maps.gate, c, r);
+        tile_prefetch(&maps.x, c, r);
+        if (p.g) tile_prefetch(&maps.g, c, r);
+    }
 };
 template <typename XT, typename GT, int VEC> struct BackwardStageOf { using Type = BackwardTile<XT, GT, VEC>; };
 template <typename XT, typename GT> struct BackwardStageOf<XT, GT, 1> { using Type = BackwardSlots<XT, GT>; };
@@ -192,8 +198,13 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
 #pragma unroll 1
     while (jobs.next(p, number)) {
         const Job job(p, number);
-        if constexpr (VEC > 1) in_stage.copy(p, maps, job, rows, &s_full);
-        else in_stage.copy(p, job, rows);
+        if constexpr (VEC > 1) {
+            in_stage.copy(p, maps, job, rows, &s_full);
+            uint32_t then;
+            if (threadIdx.x == 0 && jobs.later(p, number, then)) in_stage.prefetch(p, maps, Job(p, then));
+        } else {
+            in_stage.copy(p, job, rows);
+        }
         const int64_t tile = p.tiles - 1 - job.order, r0 = tile * kTileRows;
         const int64_t c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
         const bool on = c < p.f, column = static_cast<int>(threadIdx.x) < T::kWide;

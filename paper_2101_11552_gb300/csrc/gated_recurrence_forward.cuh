@@ -52,6 +52,11 @@ struct ForwardTile {
         tile_copy(stage + Decay::kAll, &maps.x, c, r, bar);
         if (p.linked) bulk_copy(&rows, p.plan + job.order, sizeof(TileRows), bar);
     }
+    __device__ __forceinline__ void prefetch(const ScanMaps &maps, const Job &job) const {
+        const int c = job.strip * T::kWide, r = static_cast<int>(job.order) * kTileRows;
+        tile_prefetch(&maps.gate, c, r);
+        tile_prefetch(&maps.x, c, r);
+    }
 };
 template <typename XT, int VEC> struct ForwardStageOf { using Type = ForwardTile<XT, VEC>; };
 template <typename XT> struct ForwardStageOf<XT, 1> { using Type = ForwardSlots<XT>; };
@@ -104,8 +109,13 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
 #pragma unroll 1
     while (jobs.next(p, number)) {
         const Job job(p, number);
-        if constexpr (VEC > 1) in_stage.copy(p, maps, job, rows, &s_full);
-        else in_stage.copy(p, job, rows);
+        if constexpr (VEC > 1) {
+            in_stage.copy(p, maps, job, rows, &s_full);
+            uint32_t then;
+            if (threadIdx.x == 0 && jobs.later(p, number, then)) in_stage.prefetch(maps, Job(p, then));
+        } else {
+            in_stage.copy(p, job, rows);
+        }
         const int64_t r0 = job.order * kTileRows, c0 = static_cast<int64_t>(job.strip) * T::kWide, c = c0 + lane * VEC;
         const bool on = c < p.f;
         if (p.linked && warp == 0) {

@@ -191,6 +191,10 @@ __device__ __forceinline__ void tile_copy(void *to, const CUtensorMap *map, int 
                  "l"(map), "r"(x), "r"(y), "r"(shared_at(bar))
                  : "memory");
 }
+// The same tile on its way to L2.
+__device__ __forceinline__ void tile_prefetch(const CUtensorMap *map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 // What the thread has read and written in shared memory comes before copies issued behind a barrier that follows.
 __device__ __forceinline__ void before_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Waits for the phase of the given parity to end: false after some seconds without it.
