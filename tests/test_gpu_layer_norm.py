@@ -12,7 +12,7 @@ error of K r mean |c'|, |c'| <= |c| + u |m|):
   eh' = r (K (mean |c| + u |m|) + 2 u (|c| + u |m|)) + |h| (dr / r + 2 u)
   s1 = mean d: K mean |d|;   s2 = mean d h: mean(|d| eh') + (K + 4 u) mean |d| (|h| + e) + 2 e K mean |d|
   grad_s: r (3 u |d| + es1 + |h| es2 + |s2| eh') + r (|d| + |s1| + |h s2|) (dr / r + 6 u) + 2 u |grad_sum|
-  columns: sums over rows in chains of N / CTAs, 32 teams and the CTAs in eight chains, at most
+  columns: sums over rows in chains of N / CTAs, 32 teams and the CTAs in 32 chains, at most
   Kn = (N + 120) u of sum |t| whatever the split; terms off by |g| eh'.
 A result stored in bf16 adds half a step, 2^-8 of it.
 """
