@@ -12,8 +12,8 @@
 //
 // What bounds it: memory, in rows of up to 1,024 columns, a warp each: 131,072 rows of 1,024 in bf16 on an fp32 stream
 // 228 us (1.61 GB, 7.1 TB/s).  8,192 rows of 8,192 bf16 95 us (537 MB, 5.7 TB/s): a CTA a row, which its two barriers
-// leave waiting.  A few rows are bound by latency and spread over 128 threads each: 8 rows of 1,024 3.1 us, a warp
-// each 6.0.  Odd widths go value by value: 19,717 rows of 123 fp32 8.7 us (19 MB).
+// leave waiting; with 512 threads of 16 values 104.  A few rows are bound by latency and spread over 128 threads each: 8
+// rows of 1,024 3.1 us, a warp each 6.0.  Odd widths go value by value: 19,717 rows of 123 fp32 8.7 us (19 MB).
 #include <type_traits>
 
 #include "layer_norm.cuh"
@@ -64,8 +64,10 @@ __device__ __forceinline__ float row_rstd(float d, float d2, float eps) {
     return rsqrtf((v < 0.f ? 0.f : v) + eps);                // rounding may take it below 0; a NaN stays
 }
 
+// 0: as many CTAs as the registers allow that the compiler takes by itself (told of one it takes 86 in place of 76, and two
+// CTAs of 256 fit where three did: 8,192 rows of 8,192 bf16 115 us).
 template <typename XT, typename RT, int VEC, int TT, int NV>
-__global__ void __launch_bounds__(TT <= 32 ? 256 : TT) row_norm(RowNormArgs p) {
+__global__ void __launch_bounds__(TT <= 32 ? 256 : TT, TT == 512 && VEC > 1 ? 2 : 0) row_norm(RowNormArgs p) {
     constexpr int kTeams = TT <= 32 ? 256 / TT : 1;
     __shared__ float s_sum[3 * (TT > 32 ? TT / 32 : 1)];
     const int t = threadIdx.x % TT;
@@ -184,13 +186,21 @@ cudaError_t launch_vec(const RowNormArgs &p, cudaStream_t s) {
     constexpr int kHeld = VEC == 8 ? 4 : 8;                  // vectors that a thread holds
     const int64_t vecs = (p.f + VEC - 1) / VEC;
     const auto ctas = [&](int teams) { return static_cast<unsigned>((p.n + teams - 1) / teams); };
-    // a few rows spread over more threads, and multiprocessors
+    // As many threads as hold the row in full vectors (250,000 rows of 128 bf16 42 us with 16, 70 with 32; 32,768 of 2,048
+    // 88 us with 64, 171 with 256; 4,096 of 16,384 118 with two CTAs of 512 on a multiprocessor, 156 with one, 164 with
+    // 1,024); a few rows spread over more of them.
     const bool few = p.n <= 4 * sm_count();
-    if (vecs <= 8) row_norm<XT, RT, VEC, 8, 1><<<ctas(32), 256, 0, s>>>(p);
+    if (vecs <= 4) row_norm<XT, RT, VEC, 4, 1><<<ctas(64), 256, 0, s>>>(p);
+    else if (vecs <= 8) row_norm<XT, RT, VEC, 8, 1><<<ctas(32), 256, 0, s>>>(p);
+    else if (vecs <= 16) row_norm<XT, RT, VEC, 16, 1><<<ctas(16), 256, 0, s>>>(p);
     else if (vecs <= 32) row_norm<XT, RT, VEC, 32, 1><<<ctas(8), 256, 0, s>>>(p);
     else if (few && vecs <= 128) row_norm<XT, RT, VEC, 128, 1><<<ctas(1), 128, 0, s>>>(p);
+    else if (vecs <= 64) row_norm<XT, RT, VEC, 32, 2><<<ctas(8), 256, 0, s>>>(p);
     else if (vecs <= 32 * kHeld) row_norm<XT, RT, VEC, 32, kHeld><<<ctas(8), 256, 0, s>>>(p);
+    else if (vecs <= 64 * kHeld) row_norm<XT, RT, VEC, 64, kHeld><<<ctas(1), 64, 0, s>>>(p);
+    else if (vecs <= 128 * kHeld) row_norm<XT, RT, VEC, 128, kHeld><<<ctas(1), 128, 0, s>>>(p);
     else if (vecs <= 256 * kHeld) row_norm<XT, RT, VEC, 256, kHeld><<<ctas(1), 256, 0, s>>>(p);
+    else if (vecs <= 512 * kHeld) row_norm<XT, RT, VEC, 512, kHeld><<<ctas(1), 512, 0, s>>>(p);
     else if (vecs <= 1024 * kHeld) row_norm<XT, RT, VEC, 1024, kHeld><<<ctas(1), 1024, 0, s>>>(p);
     else row_norm_long<XT, RT, VEC><<<ctas(1), 1024, 0, s>>>(p);
     return cudaGetLastError();

@@ -377,7 +377,8 @@ __global__ void __launch_bounds__(256) long_columns(RowBackArgs p) {
 
 // Threads and vectors by the width.  Up to 1,024 columns a warp takes a row, with up to 32 values a thread, and no barrier
 // is needed (128 threads with 8 values: 40 warp instructions a value, bound by what a row costs besides its values); wider
-// rows have 16 values a thread, so that they stay in registers between the sums and the gradient.
+// rows have 16 values a thread, so that they stay in registers between the sums and the gradient.  Narrow rows share a
+// warp, 8 values a thread (250,000 rows of 128 bf16 64 us, with 32 threads each, half of them idle, 107).
 template <typename ST, typename GT, typename DT, int VEC, int TT, int NV>
 cudaError_t launch_back_team(const RowBackArgs &p, cudaStream_t s) {
     using B = BackTeam<ST, GT, DT, VEC, TT, NV>;
@@ -396,7 +397,9 @@ template <typename ST, typename GT, typename DT, int VEC>
 cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
     if constexpr (VEC > 1) {
         constexpr int kN = 8 / VEC;                          // vectors of 8 values
+        if (p.f <= 32) return launch_back_team<ST, GT, DT, VEC, 4, kN>(p, s);
         if (p.f <= 64) return launch_back_team<ST, GT, DT, VEC, 8, kN>(p, s);
+        if (p.f <= 128) return launch_back_team<ST, GT, DT, VEC, 16, kN>(p, s);
         if (p.f <= 256) return launch_back_team<ST, GT, DT, VEC, 32, kN>(p, s);
         if (p.f <= 512) return launch_back_team<ST, GT, DT, VEC, 32, 2 * kN>(p, s);
         if (p.f <= 1024) return launch_back_team<ST, GT, DT, VEC, 32, 4 * kN>(p, s);
@@ -405,6 +408,7 @@ cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
         if (p.f <= 8192) return launch_back_team<ST, GT, DT, VEC, 512, 2 * kN>(p, s);
         if (p.f <= 16384) return launch_back_team<ST, GT, DT, VEC, 512, 4 * kN>(p, s);
     } else {
+        if (p.f <= 32) return launch_back_team<ST, GT, DT, 1, 8, 4>(p, s);
         if (p.f <= 128) return launch_back_team<ST, GT, DT, 1, 32, 4>(p, s);
         if (p.f <= 512) return launch_back_team<ST, GT, DT, 1, 32, 16>(p, s);
         if (p.f <= 1024) return launch_back_team<ST, GT, DT, 1, 64, 16>(p, s);

@@ -3,7 +3,7 @@
 Tolerances are first-order error bounds, formed element by element in 64 bits, u = 2^-24.  With
 y = (s - m) / T, e^y is off by (4 + 3 |y|) u of itself (two roundings of y, the hardware's exponential
 within 2 ulp; below 2^-126 it is 0).  The sum's chains hold V / 512 values of a thread (V / 32 in a
-warp's rows, V <= 2,048) and 64 more, K = (64 + V / 512 or 32) u, so q is off by
+warp's rows, up to 8 KB) and 64 more, K = (64 + V / 512 or 32) u, so q is off by
   eq = q ((4 + 3 |y|) u + w + K + 4 u),   w = sum_v q (4 + 3 |y|) u
 log p is a difference of (t - t_max) / T and the log of a sum of k terms: el = 4 u (|t - t_max| / T + log k +
 4) + k u; p = exp(log p): ep = p (el + 4 u).  Then
@@ -61,7 +61,7 @@ class Plain:
         q = torch.exp(y - log_sum)
         ry = torch.where(q > 0, (4 + 3 * y.abs()) * U, 0.0)
         wide = (q * ry).sum(1, keepdim=True)
-        kk = (64 + v / (32 if v <= 2048 else 512)) * U
+        kk = (64 + v / (32 if v * logits.element_size() <= 8192 else 512)) * U
         eq = q * (ry + wide + kk + 4 * U)
         top = torch.where(self.live[:, None], t, 0.0)
         log_p = torch.log_softmax(torch.where(here & self.live[:, None], top, -INF), 1)
@@ -116,7 +116,7 @@ def check(logits, ids, teacher, tau=1.0, weight=None, padding=-1, upstream=None)
     return r
 
 
-CLASSES = [1, 2, 3, 5, 7, 8, 16, 31, 32, 33, 41, 64, 100, 255, 256, 1000, 1024, 2047, 2048, 2049, 2056, 4095, 5000, 16_384, 50_001]
+CLASSES = [1, 2, 3, 5, 7, 8, 16, 31, 32, 33, 41, 64, 100, 255, 256, 1000, 1024, 2047, 2048, 2049, 2056, 4095, 4096, 4097, 4104, 5000, 16_384, 50_001]
 
 
 @pytest.mark.parametrize("v", CLASSES)

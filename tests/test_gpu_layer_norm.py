@@ -130,6 +130,15 @@ def test_widths(f, dt):
         check(features(n, f, f + n, dt), None, None, None, dt, features(n, f, 3, dt))
 
 
+@pytest.mark.parametrize("f", [1023, 1025, 1032, 2047, 2048, 2052, 2056, 4092, 4096, 4100, 4104, 8188, 8192, 8196, 8200, 16376, 16384,
+                               16388, 16392, 32764, 32768])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_widths_around_the_wide_teams(f, dt):
+    n = 700 if f <= 2056 else 23
+    check(features(n, f, 1, "bf16"), features(n, f, 2, dt), torch.linspace(0.5, 1.5, f, device="cuda"),
+          torch.linspace(-1, 1, f, device="cuda"), dt, features(n, f, 3, dt), features(n, f, 4, dt))
+
+
 @pytest.mark.parametrize("x", ["f32", "bf16"])
 @pytest.mark.parametrize("res", [None, "f32", "bf16"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
