@@ -5,7 +5,7 @@
 //   q = softmax over all V classes of the student's logits s / tau
 //   loss = w tau^2 sum_k p_k (log p_k - log q_{id_k}),  dloss/ds = w tau (q - p)
 //
-// A team of threads, a warp or a CTA, takes a row.  The first pass keeps a running maximum m and
+// A team of threads, 8, a warp or a CTA, takes a row.  The first pass keeps a running maximum m and
 // the sum of e^((s - m) / tau), the second writes the gradient from them; the terms at the teacher's classes are
 // written over it.  q is formed from s - m, which is exact or nearly so, and loss terms from
 // (s - m) / tau - log(sum), so logits that share a large offset lose nothing.
@@ -48,6 +48,9 @@ constexpr int kRowThreads = 512, kDistilThreads = 256;       // a CTA for a row;
 // Rows that a warp takes.  12,000 rows of 4,000 bf16: loss 26 us, with 128 threads a row 35; both 46, 50.  Of fp32, twice the
 // bytes: loss 41 and 40, both 89 and 64, as the second read no longer comes from L2.
 constexpr int kWarpBytes = 8192, kWarpTop = 128;
+// Rows that part of a warp takes, where there are so many that warps would take turns: 200,000 rows of 41 fp32 45 us, a warp
+// each 156; 9,000 rows take the same by either.
+constexpr int kSmallTeam = 8, kSmallClasses = 128, kSmallTop = 32;
 constexpr int kInFlight = 4;                                 // vectors that a thread loads before it uses them
 // Rows held in shared memory, and the threads of a CTA that takes one: so many that rows of the size, and the
 // threads, fill a multiprocessor (from 112 KB on one row at a time).  Longer rows are read twice.  They come in
@@ -62,13 +65,13 @@ constexpr int kLoss = 0, kBack = 1, kBoth = 2, kBothHeld = 3, kLossRing = 4;
 
 template <int TT>
 __device__ __forceinline__ void team_sync() {
-    if constexpr (TT == 32) __syncwarp();
+    if constexpr (TT <= 32) __syncwarp();
     else __syncthreads();
 }
 template <int TT, typename F>
 __device__ __forceinline__ float team_fold(float v, float *scratch, F fold) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fold(v, lane_xor(v, o));
+    for (int o = (TT < 32 ? TT : 32) / 2; o > 0; o >>= 1) v = fold(v, lane_xor(v, o));
     if constexpr (TT > 32) {
         __syncthreads();                                     // the last fold's have been read
         if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = v;
@@ -202,6 +205,7 @@ struct NotHeld {
 struct Top {
     int *ids;
     float *p;
+    int k;                    // entries
     float log_sum, most;      // of the teacher's softmax
     bool any;
 };
@@ -243,7 +247,7 @@ __device__ __forceinline__ float top_terms(const DistilArgs &a, const Span &r, c
                                            float log_sum, Top &top) {
     float terms = 0.f;
     const float per_tau = 1.f / a.tau;
-    for (int i = t; i < a.k; i += TT) {
+    for (int i = t; i < top.k; i += TT) {
         if (top.ids[i] < 0) continue;
         const float log_p = fmaf(top.p[i] - top.most, per_tau, -top.log_sum), p = expf(log_p);
         top.p[i] = p;
@@ -291,19 +295,19 @@ __device__ __forceinline__ void write_gradient(const DistilArgs &a, const RowSpa
                 }
         }
     }
-    if (t < r.loose) {
+    for (int i = t; i < r.loose; i += TT) {
         float e[1];
-        VecLoad<XT, 1>::load(r.row + r.loose_at(t), e);
+        VecLoad<XT, 1>::load(r.row + r.loose_at(i), e);
         scaled_q(e, away, a.scale, times);
-        store_vec<1>(out + r.loose_at(t), e);
+        store_vec<1>(out + r.loose_at(i), e);
     }
     team_sync<TT>();
     // a class that is listed more than once has the sum of its p, and every listing writes it
-    for (int i = t; i < a.k; i += TT) {
+    for (int i = t; i < top.k; i += TT) {
         const int id = top.ids[i];
         if (id < 0) continue;
         float p = 0.f, e[1] = {held.value(r, id)};
-        for (int j = 0; j < a.k; ++j) p += top.ids[j] == id ? top.p[j] : 0.f;
+        for (int j = 0; j < top.k; ++j) p += top.ids[j] == id ? top.p[j] : 0.f;
         e[0] = fmaf(exp2_of((e[0] + away) * a.scale), times, -f * p);
         store_vec<1>(out + id, e);
     }
@@ -313,7 +317,7 @@ template <int TT, typename XT, int VEC>
 __device__ __forceinline__ void zero_row(const RowSpan<XT, VEC> &r, XT *out, int t) {
     const float z[VEC] = {}, z1[1] = {0.f};
     for (int64_t i = t; i < r.vecs; i += TT) store_vec<VEC>(out + r.head + i * VEC, z);
-    if (t < r.loose) store_vec<1>(out + r.loose_at(t), z1);
+    for (int i = t; i < r.loose; i += TT) store_vec<1>(out + r.loose_at(i), z1);
 }
 
 __device__ __forceinline__ void check_ids(const DistilArgs &a) {
@@ -328,20 +332,24 @@ __device__ __forceinline__ void check_ids(const DistilArgs &a) {
 }
 
 template <typename XT, int VEC, int TT, int MODE>
-__global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(DistilArgs a) {
-    constexpr int kTeams = TT == 32 ? kDistilThreads / 32 : 1;
+__global__ void __launch_bounds__(TT <= 32 ? kDistilThreads : TT) distil_rows(DistilArgs a) {
+    constexpr int kTeams = TT <= 32 ? kDistilThreads / TT : 1;
     constexpr bool kHeld = MODE == kBothHeld, kCopies = kHeld || MODE == kLossRing;
     constexpr int kSlots = kHeld ? kChunks : kRing;
     extern __shared__ __align__(128) char s_row[];
-    __shared__ float s_fold[TT / 32];
+    __shared__ float s_fold[TT > 32 ? TT / 32 : 1];
     __shared__ uint64_t s_full[kCopies ? kSlots : 1];
     if (a.status_all && blockIdx.x == gridDim.x - 1) return check_ids(a);
     const int t = threadIdx.x % TT, team = threadIdx.x / TT;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team;
-    if (row >= a.n) return;                                  // whole teams
-    const RowSpan<XT, VEC> r(static_cast<const XT *>(a.logits) + row * a.v, a.v);
-    XT *out = a.grad ? static_cast<XT *>(a.grad) + row * a.v : nullptr;
-    float f = a.weight ? __ldg(a.weight + row) : 1.f;
+    // Teams of whole warps may leave; smaller ones go through all exchanges, without entries and values.
+    constexpr bool kWhole = TT >= 32;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams + team;
+    const bool mine = row0 < a.n;
+    if (kWhole && !mine) return;
+    const int64_t row = mine ? row0 : a.n - 1;
+    RowSpan<XT, VEC> r(static_cast<const XT *>(a.logits) + row * a.v, a.v);
+    XT *out = a.grad && mine ? static_cast<XT *>(a.grad) + row * a.v : nullptr;
+    float f = !mine ? 0.f : (a.weight ? __ldg(a.weight + row) : 1.f);
     const HeldRow<XT, VEC, kSlots> copies{s_row, s_full};
     const int chunks = kCopies ? copies.chunks(r) : 0;
     if constexpr (kCopies) {
@@ -359,6 +367,7 @@ __global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(Di
     Top top;
     top.ids = reinterpret_cast<int *>(s_row + copied) + team * 2 * a.k;
     top.p = reinterpret_cast<float *>(top.ids + a.k);
+    top.k = a.k;
     // the first vectors are on their way while the teacher's side is looked at
     constexpr bool kStreams = MODE == kLoss || MODE == kBoth;
     RowVec<XT, VEC> raw[kInFlight];
@@ -367,7 +376,7 @@ __global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(Di
     }
     load_top<TT>(a, row, t, s_fold, MODE != kBack && !a.status_all, top);   // with barriers, behind those of the copies
     if (f == 0.f || !top.any) {                              // a row that counts for nothing is not read
-        if (MODE != kBack && t == 0) {
+        if (MODE != kBack && t == 0 && mine) {
             a.loss[row] = 0.f;
             if (a.stats) a.stats[row] = make_float2(0.f, 1.f);
         }
@@ -376,7 +385,10 @@ __global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(Di
             if (f != 0.f)
                 for (int c = 0; c < kSlots && c < chunks; ++c) copies.wait(c);
         }
-        return;
+        if constexpr (kWhole) return;
+        out = nullptr;
+        r.vecs = r.loose = top.k = 0;
+        f = 0.f;
     }
     float m, sum;
     if constexpr (MODE == kBack) {
@@ -413,15 +425,15 @@ __global__ void __launch_bounds__(TT == 32 ? kDistilThreads : TT) distil_rows(Di
                     if (i0 + j * TT < r.vecs) run.template add_raw<XT, VEC>(raw[j].r, a.scale);
             }
         }
-        if (t < r.loose) {
+        for (int i = t; i < r.loose; i += TT) {
             float s[1];
-            VecLoad<XT, 1>::load(r.row + r.loose_at(t), s);
+            VecLoad<XT, 1>::load(r.row + r.loose_at(i), s);
             run.add(s, s[0], a.scale);
         }
         m = team_fold<TT>(run.m, s_fold, Larger{});
         sum = team_fold<TT>(run.sum * exp2_of((finite_or_zero(run.m) - finite_or_zero(m)) * a.scale), s_fold, Add{});
         const float terms = top_terms<TT, true>(a, r, held, t, s_fold, m, logf(sum), top);
-        if (t == 0) {
+        if (t == 0 && (kWhole || top.k > 0)) {
             a.loss[row] = f * a.tau * a.tau * terms;
             if (a.stats) a.stats[row] = make_float2(m, sum);
         }
@@ -438,16 +450,18 @@ cudaError_t launch_rows(const DistilArgs &a, size_t shared, cudaStream_t s) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHoldMost);
         if (e != cudaSuccess) return e;
     }
-    constexpr int kTeams = TT == 32 ? kDistilThreads / 32 : 1;
+    constexpr int kTeams = TT <= 32 ? kDistilThreads / TT : 1;
     const unsigned grid = static_cast<unsigned>((a.n + kTeams - 1) / kTeams + (a.status_all ? 1 : 0));
-    kernel<<<grid, TT == 32 ? kDistilThreads : TT, shared, s>>>(a);
+    kernel<<<grid, TT <= 32 ? kDistilThreads : TT, shared, s>>>(a);
     return cudaGetLastError();
 }
 
-// The team goes by the row's size alone, so that a loss has the same bits with and without its gradient.
+// The team goes by the rows' size and number, so that a loss has the same bits with and without its gradient.
 template <typename XT, int VEC, int MODE>
 cudaError_t launch_team(const DistilArgs &a, cudaStream_t s) {
     const size_t top = 8 * size_t(a.k);
+    if (a.v <= kSmallClasses && a.k <= kSmallTop && a.n > 64 * sm_count())
+        return launch_rows<XT, VEC, kSmallTeam, MODE>(a, kDistilThreads / kSmallTeam * top, s);
     if (a.v * static_cast<int64_t>(sizeof(XT)) <= kWarpBytes && a.k <= kWarpTop) return launch_rows<XT, VEC, 32, MODE>(a, kDistilThreads / 32 * top, s);
     if constexpr (VEC > 1) {
         constexpr int kMode = MODE == kBoth ? kBothHeld : (MODE == kLoss ? kLossRing : kBack);

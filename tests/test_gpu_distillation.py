@@ -126,6 +126,32 @@ def test_classes(v, dt):
         check(*make(n, v, k, v, dt, "bf16", id64=v % 2 == 0))
 
 
+@pytest.mark.parametrize("v", [1, 2, 5, 7, 8, 15, 33, 41, 64, 100, 127, 128, 129])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [9_729, 12_003])
+def test_many_rows_of_few_classes(v, dt, n):
+    """Rows that share a warp, rows that count for nothing between them, and the last warp's rows that are not there."""
+    logits, ids, teacher = make(n, v, min(v, 32), v, dt, "f32", id64=v % 2 == 0)
+    weight = torch.linspace(0.5, 2.0, n, device="cuda")
+    weight[::7] = 0.0
+    logits[::7] = math.nan
+    ids[3::11] = -1
+    ids[5::13, ::2] = -1
+    logits[3::11] = math.inf
+    guard = torch.full((n * v + 64,), 9.0, dtype=DT[dt], device="cuda")
+    r = check(logits, ids, teacher, 2.0, weight)
+    assert not bool(r.loss[::7].any()) and not bool(r.grad_logits[3::11].any())
+    grad = guard[32:32 + n * v].view(n, v)                   # on the boundary where the logits are
+    again = tfg.tfg_distillation_loss(logits, ids, teacher, temperature=2.0, row_weight=weight, grad_logits=grad)
+    assert torch.equal(again.loss, r.loss) and torch.equal(grad, r.grad_logits)
+    assert bool((guard[:32] == 9).all()) and bool((guard[32 + n * v:] == 9).all()), "values beside the gradient are left"
+    grad = guard[33:33 + n * v].view(n, v)
+    odd = tfg.tfg_distillation_loss(logits, ids, teacher, temperature=2.0, row_weight=weight, grad_logits=grad)
+    p = Plain(logits, ids, teacher, 2.0, weight)
+    close(odd.loss, p.loss, p.loss_tol, "loss")
+    close(grad, *p.grad(), "gradient off the boundary")
+
+
 @pytest.mark.parametrize("v,k", [(128, 128), (200, 129), (2048, 128), (1024, 1024), (2500, 1024), (60_000, 300), (41, 41)])
 @pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
 def test_top_sizes_and_temperatures(v, k, tau):
