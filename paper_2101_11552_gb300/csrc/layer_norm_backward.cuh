@@ -123,6 +123,24 @@ struct BackTeam {
     static constexpr int kCtas = kFit < 1 ? 1 : (kFit < kWant ? kFit : kWant);
 };
 
+// Values t, t + TT, ... of a row to slots `step` values apart.  There are no asynchronous copies of two bytes: those are
+// loaded all at once and then stored (4,096 rows of 4,095 bf16 103 us; one after the other each waits for memory: 165).
+template <int NV, int TT, typename T>
+__device__ __forceinline__ void copy_values(char *to, int step, const T *row, int t, int cols) {
+    if constexpr (sizeof(T) == 2) {
+        T v[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = t + i * TT < cols ? row[t + i * TT] : T(0);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (t + i * TT < cols) reinterpret_cast<T *>(to)[i * step] = v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (t + i * TT < cols) copy_async<sizeof(T)>(to + i * step * sizeof(T), row + t + i * TT);
+    }
+}
+
 template <typename T, int VEC>
 __device__ __forceinline__ void widen_shared(const T *p, float (&v)[VEC]) {
     VecLoad<T, VEC>::widen(load_plain<T, VEC>(p), v);
@@ -168,15 +186,10 @@ __global__ void __launch_bounds__(BackTeam<ST, GT, DT, VEC, TT, NV>::kThreads, B
             const int64_t row = first + round * step;
             if (row < p.n && round < rounds) {
                 char *to = s_rows + static_cast<int>(round % kStages) * B::kStageBytes;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = t + i * TT, at = at0 + i * kAtStep;
-                    if (c < cols) {
-                        copy_async<sizeof(ST)>(to + at * sizeof(ST), static_cast<const ST *>(p.s) + row * p.f + c);
-                        copy_async<sizeof(GT)>(to + B::kS + at * sizeof(GT), static_cast<const GT *>(p.g) + row * p.f + c);
-                        if (p.skip) copy_async<sizeof(DT)>(to + B::kS + B::kG + at * sizeof(DT), static_cast<const DT *>(p.skip) + row * p.f + c);
-                    }
-                }
+                copy_values<NV, TT>(to + at0 * sizeof(ST), kAtStep, static_cast<const ST *>(p.s) + row * p.f, t, cols);
+                copy_values<NV, TT>(to + B::kS + at0 * sizeof(GT), kAtStep, static_cast<const GT *>(p.g) + row * p.f, t, cols);
+                if (p.skip)
+                    copy_values<NV, TT>(to + B::kS + B::kG + at0 * sizeof(DT), kAtStep, static_cast<const DT *>(p.skip) + row * p.f, t, cols);
             }
             copies_commit();
         }
@@ -412,6 +425,7 @@ cudaError_t launch_back_vec(const RowBackArgs &p, cudaStream_t s) {
         if (p.f <= 128) return launch_back_team<ST, GT, DT, 1, 32, 4>(p, s);
         if (p.f <= 512) return launch_back_team<ST, GT, DT, 1, 32, 16>(p, s);
         if (p.f <= 1024) return launch_back_team<ST, GT, DT, 1, 64, 16>(p, s);
+        if (p.f <= 2048) return launch_back_team<ST, GT, DT, 1, 128, 16>(p, s);
         if (p.f <= 4096) return launch_back_team<ST, GT, DT, 1, 256, 16>(p, s);
     }
     row_norm_back_long<ST, GT, DT, VEC><<<static_cast<unsigned>(p.n), 1024, 0, s>>>(p);
