@@ -543,6 +543,7 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
         }
         if (entered == kNoState) entered = wait_for(p.states + window * p.f + c, kNoState, p.status);
         state = __uint_as_float(entered);
+        __syncwarp();                                        // lanes waited for words of their own, or for none
         __syncthreads();
         if (mine) {
 #pragma unroll

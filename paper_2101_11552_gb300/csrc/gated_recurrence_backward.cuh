@@ -286,10 +286,12 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         }
         enter_group<T, false>(a, b, cut, v);
         enter_group<T, true>(u, w, cut_up, l);
-        if (!on) continue;
-        const int64_t row = r0 + group * T::kEach;
-        if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
-        else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+        if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
+            const int64_t row = r0 + group * T::kEach;
+            if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+            else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+        }
+        __syncwarp();
     }
 }
 

@@ -178,10 +178,12 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
         }
         enter_group<T, false>(a, b, cut, v);
-        if (!on) continue;
-        OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
-        if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
-        else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+        if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
+            OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
+            if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+            else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+        }
+        __syncwarp();
     }
 }
 
