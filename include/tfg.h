@@ -787,7 +787,10 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
  * The states are formed again in fp32 as the forward had them: the type of out
  * does not touch the gradients.
  * All arithmetic in fp32 in a fixed order: bitwise reproducible between calls of
- * the same alignment.  A gate of -inf forgets a finite state entirely.  A value that is no
+ * the same alignment.  A gate of -inf forgets a finite state entirely.  TFG_GATE_EXP
+ * above 0 grows: states and gradients are right where they are ordinary numbers, whatever
+ * the product of the gates; from 88.8 on exp(z) is an infinity, and what follows in the
+ * sequence is no number.  A value that is no
  * number stays in its channel and sequence.  ceil(num_rows / 128) *
  * ceil(num_features / 32) < 2^31 - 2^16 (TFG_ERR_TOO_LARGE).
  * ---------------------------------------------------------------------- */

@@ -21,6 +21,13 @@
 // a second tile while the first waited made a convoy of it (1,024 molecules forward: 213 us, where one tile at a
 // time took 42).
 //
+// The decay of a composed map.  Sigmoid gates: the product of the a, at most 1.  Exponential gates: the square root of the
+// product, e^(sum of z / 2) of a thread's rows, at most the largest number.  Gates above 0 grow, and the product of 100 rows may pass
+// what fp32 holds where the states do not: a state of 0 stays 0 and one of 1e-30 comes back to ordinary size, where an
+// infinite product makes NaN of the one and an infinity of the other; and a product below 2^-126 is not lost before a large
+// state meets it.  (The logarithm in its place, an exponential for each map applied: 204 us where the root takes 196, one
+// sequence of 131,072 x 256 in both directions.)  A gate alone whose exponential passes fp32, from 88.8 on, is an infinity.
+//
 // Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps its distance from 1
 // to a few u, where a rounded a would change a memory of 1,000 steps by 1,000 u.  All in fp32.
 //
@@ -184,16 +191,16 @@ __device__ __forceinline__ float expm1_near(float z) {
     return fmaf(z * z, q, z);
 }
 
-// a - 1 of VEC gates.  Sigmoid: -1 / (1 + 2^(z log2 e)), within (|z| + 4) u of itself.  Exp:
-// further from 0 than 0.35, 2^(z log2 e) - 1.
+// a - 1 of VEC gates, and t = z log2 e.  Sigmoid: -1 / (1 + 2^t), within (|z| + 4) u of itself.  Exp:
+// further from 0 than 0.35, 2^t - 1.
 template <int KIND, int VEC>
-__device__ __forceinline__ void decay_less_one(const float (&z)[VEC], float (&d)[VEC]) {
+__device__ __forceinline__ void decay_less_one(const float (&z)[VEC], float (&d)[VEC], float (&t)[VEC]) {
     const float log2e[1] = {1.44269504088896341f};
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) d[q] = z[q];
-    mul_vec(d, log2e);
+    for (int q = 0; q < VEC; ++q) t[q] = z[q];
+    mul_vec(t, log2e);
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) d[q] = exp2_of(d[q]);
+    for (int q = 0; q < VEC; ++q) d[q] = exp2_of(t[q]);
     const float minus_one[1] = {-1.f};
     if constexpr (KIND == TFG_GATE_SIGMOID) {
         fma_vec(d, d, minus_one, minus_one);
@@ -215,6 +222,21 @@ __device__ __forceinline__ void add_input(float (&v)[VEC], const float (&d)[VEC]
     } else {
         add_vec(v, x);
     }
+}
+
+// ---- composed maps -----------------------------------------------------------------------
+// The decay of the rows of two maps, one after the other: of sigmoid gates the product of the a, of exponential gates its root.
+constexpr float kMostDecay = 3.402823466e38f;
+template <int KIND>
+__device__ __forceinline__ float both_decays(float a, float b) {
+    return KIND == TFG_GATE_EXP ? fminf(a * b, kMostDecay) : a * b;
+}
+// What the map (a, b) makes of v.  Exponential gates: v a is between v and v a^2, so nothing is lost on the way.  A product
+// held back to 2^256 makes an infinity of every v from 2^-128 on, as it should.  A gate that is NaN, or too large
+// for fp32, is NaN or an infinity in b too.
+template <int KIND>
+__device__ __forceinline__ float through(float a, float v, float b) {
+    return KIND == TFG_GATE_EXP ? fmaf(v * a, a, b) : fmaf(a, v, b);
 }
 
 // ---- the rows of a tile ----------------------------------------------------------------
@@ -423,7 +445,7 @@ __device__ __forceinline__ void prefetch_states(const float *states, uint32_t wh
 // Maps of a warp's groups of rows, composed across the lanes from where values enter (the first
 // row; UP: the last): on return (a, b) is the map of the groups up to this one, `fresh` whether
 // one of them cuts off what enters; the last group leaves the whole warp's map.
-template <typename Tile, bool UP, int VEC>
+template <typename Tile, int KIND, bool UP, int VEC>
 __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bool &fresh, int warp, int lane,
                                             float (*s_a)[Tile::kWide], float (*s_b)[Tile::kWide]) {
     constexpr int kAcross = Tile::kAcross;
@@ -437,8 +459,8 @@ __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bo
         for (int q = 0; q < VEC; ++q) {
             const float pa = lane_get(a[q], from), pb = lane_get(b[q], from);
             if (joins) {
-                b[q] = fmaf(a[q], pb, b[q]);
-                a[q] *= pa;                                  // not looked at behind a cut
+                b[q] = through<KIND>(a[q], pb, b[q]);
+                a[q] = both_decays<KIND>(a[q], pa);          // not looked at behind a cut
             }
         }
         fresh = fresh || (has && other);
@@ -462,7 +484,7 @@ __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bo
 
 // What enters the thread's rows, into v: at the warp's first group what enters the warp (v), else what leaves
 // the group before, by the map (a, b) up to it.  By whole warps.
-template <typename Tile, bool UP, int VEC>
+template <typename Tile, int KIND, bool UP, int VEC>
 __device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (&b)[VEC], bool fresh, float (&v)[VEC]) {
     constexpr int kAcross = Tile::kAcross;
     if constexpr (kAcross < 32) {
@@ -470,7 +492,7 @@ __device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (
         const bool has = UP ? l + kAcross < 32 : l >= kAcross;
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
-            const float leaves = lane_get(fresh ? b[q] : fmaf(a[q], v[q], b[q]), from);
+            const float leaves = lane_get(fresh ? b[q] : through<KIND>(a[q], v[q], b[q]), from);
             if (has) v[q] = leaves;
         }
     }
@@ -483,12 +505,12 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
                                              const int32_t *seq, int64_t c, uint32_t begin, uint32_t in, float (&a)[VEC],
                                              float (&b)[VEC]) {
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) a[q] = 1.f, b[q] = 0.f;
+    for (int q = 0; q < VEC; ++q) a[q] = KIND == TFG_GATE_EXP ? 0.f : 1.f, b[q] = 0.f;
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-        float v[VEC], dj[VEC];
+        float v[VEC], dj[VEC], t[VEC];
         z.widen(j, v);
-        decay_less_one<KIND>(v, dj);
+        decay_less_one<KIND>(v, dj, t);
         d.put(j, dj);
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((begin >> j) & 1u)) {
@@ -497,9 +519,14 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
             state_or_zero(initial, seq[j], p.f, c, b);
         }
         x.widen(j, v);
-        fma_vec(a, dj, a, a);
+        if constexpr (KIND == TFG_GATE_EXP) add_vec(a, t);
+        else fma_vec(a, dj, a, a);
         fma_vec(b, dj, b, b);
         add_input<KIND>(b, dj, v);
+    }
+    if constexpr (KIND == TFG_GATE_EXP) {
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) a[q] = fminf(exp2_of(a[q] * 0.5f), kMostDecay);
     }
 }
 
@@ -508,7 +535,7 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
 // enters the tile leaves it.  wants: the tile's first row (in order of work) goes on from
 // the tile before.  from: cut_before.  The maps are looked at by all threads, a part of the
 // window each, and the parts joined in shared memory.
-template <int WIDE>
+template <int WIDE, int KIND>
 __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, int64_t c0, float a, float b, bool fresh,
                                             bool wants, int from, float2 (*s_part)[WIDE]) {
     constexpr int kParts = kScanThreads / WIDE, kMaps = kWindow / kParts;
@@ -536,8 +563,8 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
                 if (begin + i < first || begin + i >= place) continue;
                 if (word[i] == kNoMap) word[i] = wait_for(maps + i * p.f, kNoMap, p.status);
                 const float wa = __uint_as_float(static_cast<uint32_t>(word[i])), wb = __uint_as_float(static_cast<uint32_t>(word[i] >> 32));
-                mb = begin + i == from ? wb : fmaf(wa, mb, wb);
-                ma *= wa;
+                mb = begin + i == from ? wb : through<KIND>(wa, mb, wb);
+                ma = both_decays<KIND>(ma, wa);
             }
             s_part[part][channel] = make_float2(ma, mb);
         }
@@ -550,12 +577,12 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
             for (int i = 0; i < kParts; ++i) {
                 if ((i + 1) * kMaps <= first || i * kMaps >= place) continue;
                 const float2 m = s_part[i][channel];
-                state = i * kMaps <= from ? m.y : fmaf(m.x, state, m.y);   // the part with `from` begins anew
+                state = i * kMaps <= from ? m.y : through<KIND>(m.x, state, m.y);   // the part with `from` begins anew
             }
         }
     }
     if (mine && place == kWindow - 1 && order + 1 < p.tiles)
-        st_word(p.states + (window + 1) * p.f + c, state_word(fresh ? b : fmaf(a, state, b)));
+        st_word(p.states + (window + 1) * p.f + c, state_word(fresh ? b : through<KIND>(a, state, b)));
     return state;
 }
 

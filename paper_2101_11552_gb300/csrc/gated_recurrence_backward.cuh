@@ -88,30 +88,26 @@ template <typename XT, typename GT, int VEC> using BackwardStage = typename Back
 template <typename XT, typename GT, int VEC>
 constexpr int kBackwardCtas = BackwardStage<XT, GT, VEC>::kBytes > 64 * 1024 ? 2 : 3;
 
-// The thread's rows as one map of the adjoint, from the last to the first.
+// The thread's rows as one map of the adjoint, from the last to the first: w, and its decay, which is that of the
+// states' map (no row between two that begin or end a sequence is left out of either).
 template <bool PLAIN, int EACH, int VEC, typename Grad, typename Decay>
 __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, const Decay &d, const float *grad_final,
                                            const int32_t *seq, int64_t c, uint32_t begin, uint32_t end, uint32_t in,
-                                           float (&u)[VEC], float (&w)[VEC]) {
+                                           float (&w)[VEC]) {
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) u[q] = 1.f, w[q] = 0.f;
+    for (int q = 0; q < VEC; ++q) w[q] = 0.f;
 #pragma unroll
     for (int j = EACH - 1; j >= 0; --j) {
         if (!PLAIN && !((in >> j) & 1u)) continue;
-        if (!PLAIN && ((end >> j) & 1u)) {
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) u[q] = 0.f;
-            state_or_zero(grad_final, seq[j], p.f, c, w);
-        }
+        if (!PLAIN && ((end >> j) & 1u)) state_or_zero(grad_final, seq[j], p.f, c, w);
         float v[VEC], dj[VEC];
         g.widen(j, v);
         d.widen(j, dj);
         add_vec(w, v);
-        fma_vec(u, dj, u, u);
         fma_vec(w, dj, w, w);
         if (!PLAIN && ((begin >> j) & 1u)) {
 #pragma unroll
-            for (int q = 0; q < VEC; ++q) u[q] = w[q] = 0.f;
+            for (int q = 0; q < VEC; ++q) w[q] = 0.f;
         }
     }
 }
@@ -240,14 +236,16 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
         if (plain) {
             compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-            compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, u, w);
+            compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, w);
         } else {
             compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
-            compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, u, w);
+            compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, w);
         }
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) u[q] = a[q];
         bool cut = begin != 0u, cut_up = (begin | end) != 0u;
-        scan_groups<T, false>(a, b, cut, warp, lane, s_a, s_b);
-        scan_groups<T, true>(u, w, cut_up, warp, lane, s_u, s_w);
+        scan_groups<T, KIND, false>(a, b, cut, warp, lane, s_a, s_b);
+        scan_groups<T, KIND, true>(u, w, cut_up, warp, lane, s_u, s_w);
         __syncthreads();
 
         // threads of the first columns: up the warps; of the next: down them, from the state kept
@@ -259,19 +257,19 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
                 s_u[i][threadIdx.x] = tu;
                 s_w[i][threadIdx.x] = tw;
                 const bool fresh = (cut_warps >> warp_bit(i)) & 1u;
-                tw = fresh ? gw : fmaf(gu, tw, gw);
-                tu = fresh ? 0.f : tu * gu;
+                tw = fresh ? gw : through<KIND>(gu, tw, gw);
+                tu = fresh ? 0.f : both_decays<KIND>(tu, gu);
             }
         } else if (sc < T::kWide) {
 #pragma unroll
             for (int i = 0; i < kScanWarps; ++i) {
                 const float ga = s_a[i][sc], gb = s_b[i][sc];
                 s_b[i][sc] = state;
-                state = (begin_warps >> warp_bit(i)) & 1u ? gb : fmaf(ga, state, gb);
+                state = (begin_warps >> warp_bit(i)) & 1u ? gb : through<KIND>(ga, state, gb);
             }
         }
         const bool wants = (rows.in[kTileRows / 32 - 1] & ~rows.end[kTileRows / 32 - 1]) >> 31;
-        const float carry = enter_tile<T::kWide>(p, job.order, c0, tu, tw, cut_warps != 0u, wants, s_from, s_part);
+        const float carry = enter_tile<T::kWide, KIND>(p, job.order, c0, tu, tw, cut_warps != 0u, wants, s_from, s_part);
         jobs.ask(p);
         if (column) s_carry[threadIdx.x] = carry;
         __syncthreads();
@@ -282,10 +280,10 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         for (int q = 0; q < VEC; ++q) {
             const int i = lane * VEC + q;
             v[q] = s_b[warp][i];
-            l[q] = far ? s_w[warp][i] : fmaf(s_u[warp][i], s_carry[i], s_w[warp][i]);
+            l[q] = far ? s_w[warp][i] : through<KIND>(s_u[warp][i], s_carry[i], s_w[warp][i]);
         }
-        enter_group<T, false>(a, b, cut, v);
-        enter_group<T, true>(u, w, cut_up, l);
+        enter_group<T, KIND, false>(a, b, cut, v);
+        enter_group<T, KIND, true>(u, w, cut_up, l);
         if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
             const int64_t row = r0 + group * T::kEach;
             if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
         if (plain) compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
         else compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
         bool cut = begin != 0u;
-        scan_groups<T, false>(a, b, cut, warp, lane, s_a, s_b);
+        scan_groups<T, KIND, false>(a, b, cut, warp, lane, s_a, s_b);
         __syncthreads();
 
         // down the warps, a thread for each channel: what stands before each, and the tile's map
@@ -159,12 +159,12 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
                 s_a[w][threadIdx.x] = ta;
                 s_b[w][threadIdx.x] = tb;
                 const bool fresh = (begin_warps >> warp_bit(w)) & 1u;
-                tb = fresh ? wb : fmaf(wa, tb, wb);              // not 0 times what may be an infinity
-                ta = fresh ? 0.f : ta * wa;
+                tb = fresh ? wb : through<KIND>(wa, tb, wb);     // not 0 times what may be an infinity
+                ta = fresh ? 0.f : both_decays<KIND>(ta, wa);
             }
         }
         const bool wants = (rows.in[0] & ~rows.begin[0] & 1u) != 0u;
-        const float state = enter_tile<T::kWide>(p, job.order, c0, ta, tb, begin_warps != 0u, wants, s_from, s_part);
+        const float state = enter_tile<T::kWide, KIND>(p, job.order, c0, ta, tb, begin_warps != 0u, wants, s_from, s_part);
         jobs.ask(p);
         if (column) s_state[threadIdx.x] = state;
         if (column && mc < p.f && p.entering) p.entering[job.order * p.f + mc] = state;
@@ -175,9 +175,9 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
             const int i = lane * VEC + q;
-            v[q] = far ? s_b[warp][i] : fmaf(s_a[warp][i], s_state[i], s_b[warp][i]);
+            v[q] = far ? s_b[warp][i] : through<KIND>(s_a[warp][i], s_state[i], s_b[warp][i]);
         }
-        enter_group<T, false>(a, b, cut, v);
+        enter_group<T, KIND, false>(a, b, cut, v);
         if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
             OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
             if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
