@@ -785,7 +785,8 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
  *   grad_gate, grad_x (device) of dtype, with row strides as the inputs'.
  *   grad_initial (device) fp32 [num_sequences, num_features] or NULL.
  * The states are formed again in fp32 as the forward had them: the type of out
- * does not touch the gradients.
+ * does not touch the gradients.  What a large state or gradient leaves behind a gate
+ * far below 0 keeps its digits, and so does that gate's own gradient.
  * All arithmetic in fp32 in a fixed order: bitwise reproducible between calls of
  * the same alignment.  A gate of -inf forgets a finite state entirely.  TFG_GATE_EXP
  * above 0 grows: states and gradients are right where they are ordinary numbers, whatever

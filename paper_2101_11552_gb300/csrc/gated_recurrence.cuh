@@ -28,8 +28,10 @@
 // state meets it.  (The logarithm in its place, an exponential for each map applied: 204 us where the root takes 196, one
 // sequence of 131,072 x 256 in both directions.)  A gate alone whose exponential passes fp32, from 88.8 on, is an infinity.
 //
-// Precision.  1 - a is formed directly and the state advances as v - (1 - a) v + b: a gate near 1 keeps its distance from 1
-// to a few u, where a rounded a would change a memory of 1,000 steps by 1,000 u.  All in fp32.
+// Precision.  A decay near 1 is held as a - 1, formed directly, and the state advances as v + (a - 1) v + b: a gate near 1 keeps
+// its distance from 1 to a few u, where a rounded a would change a memory of 1,000 steps by 1,000 u.  A decay near 0 is held as a: a
+// large state cut down to what is left of it, and the gate's own gradient, which has a as a factor, keep their digits, where
+// 1 + (a - 1) is a multiple of 2^-25.  One word holds either.  All in fp32.
 //
 // What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 179 us
 // (805 MB, 4.5 TB/s, 26 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
@@ -40,6 +42,9 @@
 // with twice the rows each take a third fewer instructions and are slower (209 and 459 us for the first, too few warps),
 // 8 channels a thread 200 and 353, copies of 16 bytes a lane 220 and 383.
 #pragma once
+
+#include <type_traits>
+#include <utility>
 
 #include "widen.cuh"
 
@@ -180,47 +185,120 @@ __device__ __forceinline__ W wait_for(const W *p, W none, int32_t *status) {
 }
 
 // ---- gates ----------------------------------------------------------------------------
-// expm1(z) for |z| <= 0.35: z + z^2 q(z), q of degree 4 through the Chebyshev points of that
-// interval; within 1.5 u of itself over all fp32 values there.
-__device__ __forceinline__ float expm1_near(float z) {
-    float q = 0.0013934534508734941f;
-    q = fmaf(q, z, 0.008363769389688969f);
-    q = fmaf(q, z, 0.04166645556688309f);
-    q = fmaf(q, z, 0.16666573286056519f);
-    q = fmaf(q, z, 0.5f);
-    return fmaf(z * z, q, z);
+// How the decays of a thread's rows are held.  kLess: a - 1, for sigmoid gates that are all above kSmallGate.  kEither: a - 1
+// near 1, with the sign bit set and never 0, else a, with it clear.
+constexpr int kLess = 0, kEither = 1;
+template <int FORM> using Form = std::integral_constant<int, FORM>;
+using Yes = std::true_type;
+using No = std::false_type;
+// a = 2^-8.  a - 1 is within 2 u, which is up to 512 u of such an a; below it kEither has a few u.  Words of either kind take twice the
+// instructions to apply, and a tile that takes longer holds up those behind it: 131,072 x 1,024 bf16 with gates of mean
+// 2.5 and deviation 1.8, both directions, 510 us with words of either kind below 2^-8, 528 below 2^-7, 572 below 2^-6 and
+// 586 with no others (before there were any, 508).
+constexpr float kSmallGate = -5.55f;
+// fp32 rows with a gate as small take the code of rows that begin and end sequences: a copy of their own made the kernel too
+// long for the instructions' cache even when it was not run (1,024 molecules 110 us in place of 106, none slower with small gates
+// throughout).  In bf16 the copy costs nothing, and 131,072 x 1,024 with words of either kind below 2^-6 took 589 us by it, 738 without.
+template <typename XT> constexpr bool kSharedForm = sizeof(XT) == 4;
+
+// expm1(z) - 2^-126 for -0.35 <= z <= 0: z (1 + z q(z)), q of degree 4 through the Chebyshev points of
+// |z| <= 0.35; within 2 u of itself over all normal fp32 values there.  Never 0, so that the sign tells.
+template <int VEC>
+__device__ __forceinline__ void expm1_near(const float (&z)[VEC], float (&d)[VEC]) {
+    const float c[6] = {0.0013934534508734941f, 0.008363769389688969f, 0.04166645556688309f, 0.16666573286056519f, 0.5f, 1.f};
+    const float tiny[1] = {-1.1754943508222875e-38f};
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) d[q] = c[0];
+#pragma unroll
+    for (int k = 1; k < 6; ++k) {
+        const float ck[1] = {c[k]};
+        fma_vec(d, d, z, ck);
+    }
+    fma_vec(d, d, z, tiny);
 }
 
-// a - 1 of VEC gates, and t = z log2 e.  Sigmoid: -1 / (1 + 2^t), within (|z| + 4) u of itself.  Exp:
-// further from 0 than 0.35, 2^t - 1.
-template <int KIND, int VEC>
-__device__ __forceinline__ void decay_less_one(const float (&z)[VEC], float (&d)[VEC], float (&t)[VEC]) {
+// The words of VEC gates; beside them 1 - a of sigmoid gates held as kEither.  Sigmoid: with t = z log2 e, 1 / (1 + 2^t) is
+// 1 - a and 2^t times it a, each within (2 |z| + 10) u of itself.  Exp: a = 2^t within (2 |z| + 4) u, or a - 1 from -0.35 to 0.
+template <int KIND, int FORM, int VEC>
+__device__ __forceinline__ void decay_words(const float (&z)[VEC], float (&r)[VEC], float (&less)[VEC]) {
     const float log2e[1] = {1.44269504088896341f};
+    float e[VEC];
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) t[q] = z[q];
-    mul_vec(t, log2e);
+    for (int q = 0; q < VEC; ++q) e[q] = z[q];
+    mul_vec(e, log2e);
+    if constexpr (KIND == TFG_GATE_EXP) {
+        float near[VEC];
+        expm1_near(z, near);
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) d[q] = exp2_of(t[q]);
-    const float minus_one[1] = {-1.f};
-    if constexpr (KIND == TFG_GATE_SIGMOID) {
-        fma_vec(d, d, minus_one, minus_one);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d[q]) : "f"(d[q]));
+        for (int q = 0; q < VEC; ++q) {
+            // the bits of -0.35 and what lies between it and -0, as whole numbers
+            r[q] = __float_as_int(z[q]) <= __float_as_int(-0.35f) ? near[q] : exp2_of(e[q]);
+        }
     } else {
-        add_vec(d, minus_one);
+        const float one[1] = {FORM == kLess ? -1.f : 1.f};   // kLess: -1 / (1 + 2^t)
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) d[q] = fabsf(z[q]) <= 0.35f ? expm1_near(z[q]) : d[q];
+        for (int q = 0; q < VEC; ++q) less[q] = e[q] = exp2_of(e[q]);
+        fma_vec(less, less, one, one);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(less[q]) : "f"(less[q]));
+        if constexpr (FORM == kLess) {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) r[q] = less[q];
+        } else {
+            const float minus[1] = {-1.f}, tiny[1] = {-1.1754943508222875e-38f};
+            mul_vec(e, less);
+            fma_vec(r, less, minus, tiny);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) r[q] = z[q] < 0.f ? e[q] : r[q];
+        }
     }
 }
 
-// b of a row added to a state, d = a - 1.
-template <int KIND, int VEC>
-__device__ __forceinline__ void add_input(float (&v)[VEC], const float (&d)[VEC], const float (&x)[VEC]) {
-    if constexpr (KIND == TFG_GATE_SIGMOID) {
+// kEither: 1 where a word is a - 1, 0 where it is a.
+template <int VEC>
+__device__ __forceinline__ void whole_part(const float (&r)[VEC], float (&h)[VEC]) {
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) v[q] = fmaf(-d[q], x[q], v[q]);
+    for (int q = 0; q < VEC; ++q) asm("mul.rn.sat.f32 %0, %1, %2;" : "=f"(h[q]) : "f"(r[q]), "f"(-1.7014118346046923e38f));
+}
+// a v.
+template <int FORM, int VEC>
+__device__ __forceinline__ void decay(float (&v)[VEC], const float (&r)[VEC]) {
+    if constexpr (FORM == kLess) {
+        fma_vec(v, r, v, v);
     } else {
-        add_vec(v, x);
+        float h[VEC];
+        whole_part(r, h);
+        mul_vec(h, v);
+        fma_vec(v, r, v, h);
+    }
+}
+// 1 - a of words of either kind.
+template <int VEC>
+__device__ __forceinline__ void one_less(const float (&r)[VEC], const float (&h)[VEC], float (&less)[VEC]) {
+    const float one[1] = {1.f}, minus[1] = {-1.f};
+    fma_vec(less, h, minus, one);
+    fma_vec(less, r, minus, less);
+}
+// a v + b of a row, from its word.
+template <int KIND, int FORM, int VEC>
+__device__ __forceinline__ void advance(float (&v)[VEC], const float (&r)[VEC], const float (&x)[VEC]) {
+    float h[VEC];
+    if constexpr (FORM == kLess) {                           // v + (a - 1) (v - x)
+        const float minus[1] = {-1.f};
+        fma_vec(h, x, minus, v);
+        fma_vec(v, r, h, v);
+    } else {
+        whole_part(r, h);
+        if constexpr (KIND == TFG_GATE_SIGMOID) {
+            float less[VEC];
+            one_less(r, h, less);
+            mul_vec(h, v);
+            fma_vec(h, r, v, h);
+            fma_vec(v, less, x, h);
+        } else {
+            fma_vec(h, h, v, x);
+            fma_vec(v, r, v, h);
+        }
     }
 }
 
@@ -228,8 +306,8 @@ __device__ __forceinline__ void add_input(float (&v)[VEC], const float (&d)[VEC]
 // The decay of the rows of two maps, one after the other: of sigmoid gates the product of the a, of exponential gates its root.
 constexpr float kMostDecay = 3.402823466e38f;
 template <int KIND>
-__device__ __forceinline__ float both_decays(float a, float b) {
-    return KIND == TFG_GATE_EXP ? fminf(a * b, kMostDecay) : a * b;
+__device__ __forceinline__ float held_back(float a) {
+    return KIND == TFG_GATE_EXP ? fminf(a, kMostDecay) : a;
 }
 // What the map (a, b) makes of v.  Exponential gates: v a is between v and v a^2, so nothing is lost on the way.  A product
 // held back to 2^256 makes an infinity of every v from 2^-128 on, as it should.  A gate that is NaN, or too large
@@ -368,7 +446,42 @@ struct HeldGate {
         for (int j = 0; j < Tile::kEach; ++j) r[j] = load_plain<T, VEC>(from.at + j * Tile::kWide);
     }
     __device__ __forceinline__ void widen(int j, float (&v)[VEC]) const { VecLoad<T, VEC>::widen(r[j], v); }
+    // Whether a gate lies below kSmallGate; a NaN does not.
+    __device__ __forceinline__ bool any_small() const {
+        float least = INFINITY;
+        if constexpr (sizeof(T) == 2) {
+            const auto pair = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); };
+            __nv_bfloat162 m = pair(r[0].x);
+#pragma unroll
+            for (int j = 0; j < Tile::kEach; ++j) m = __hmin2(m, __hmin2(pair(r[j].x), pair(r[j].y)));
+            least = fminf(__low2float(m), __high2float(m));
+        } else {
+#pragma unroll
+            for (int j = 0; j < Tile::kEach; ++j) least = fminf(least, fminf(fminf(r[j].x, r[j].y), fminf(r[j].z, r[j].w)));
+        }
+        return least < kSmallGate;
+    }
 };
+
+// Whether the rows of a thread, all of one sequence (plain), have a sigmoid gate below kSmallGate in one of the tile's channels: the
+// same for all threads of the rows, and no matter what other rows hold.  By whole warps.
+template <typename Tile, typename Gate>
+__device__ __forceinline__ bool small_gates(const Gate &z, bool mine) {
+    bool small;
+    if constexpr (Tile::VEC > 1) {
+        small = z.any_small();
+    } else {
+        float least = INFINITY, v[1];
+#pragma unroll
+        for (int j = 0; j < Tile::kEach; ++j) {
+            z.widen(j, v);
+            least = fminf(least, v[0]);
+        }
+        small = least < kSmallGate;
+    }
+    constexpr uint32_t kRows = Tile::kAcross == 32 ? ~0u : (1u << (Tile::kAcross & 31)) - 1u;
+    return (lane_ballot(mine && small) >> ((threadIdx.x & 31) / Tile::kAcross * Tile::kAcross) & kRows) != 0u;
+}
 
 // A job: a tile in order of work, and a strip of channels.
 struct Job {
@@ -460,7 +573,7 @@ __device__ __forceinline__ void scan_groups(float (&a)[VEC], float (&b)[VEC], bo
             const float pa = lane_get(a[q], from), pb = lane_get(b[q], from);
             if (joins) {
                 b[q] = through<KIND>(a[q], pb, b[q]);
-                a[q] = both_decays<KIND>(a[q], pa);          // not looked at behind a cut
+                a[q] = held_back<KIND>(a[q] * pa);           // not looked at behind a cut
             }
         }
         fresh = fresh || (has && other);
@@ -498,35 +611,63 @@ __device__ __forceinline__ void enter_group(const float (&a)[VEC], const float (
     }
 }
 
-// The thread's rows as one map, and a - 1 of each row into d, which may lie where z does.  PLAIN: the rows
-// lie in a sequence that neither begins nor ends there.
-template <bool PLAIN, int KIND, int VEC, int EACH, typename Gate, typename In, typename Decay>
-__device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, const In &x, const Decay &d, const float *initial,
-                                             const int32_t *seq, int64_t c, uint32_t begin, uint32_t in, float (&a)[VEC],
-                                             float (&b)[VEC]) {
+// No adjoint beside the states' map.
+struct NoGrad {};
+
+// The thread's rows as one map, and the word of each row's decay into d, which may lie where z does.  PLAIN: the rows
+// lie in a sequence that neither begins nor ends there.  With gradients g (sigmoid gates): w is what leaves the rows upward when
+// nothing enters them, the sum of g_j times the decays of the rows up to j, and one of grad_final behind a sequence's end; its
+// own decay is a.
+template <bool PLAIN, int FORM, int KIND, int VEC, int EACH, typename Gate, typename In, typename Decay, typename Grad>
+__device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, const In &x, const Decay &d, const Grad &g,
+                                             const float *initial, const float *grad_final, const int32_t *seq, int64_t c,
+                                             uint32_t begin, uint32_t end, uint32_t in, float (&a)[VEC],
+                                             float (&b)[VEC], float (&w)[VEC]) {
+    const float half_log2e[1] = {0.72134752044448170f};
+    constexpr bool kAdjoint = !std::is_same<Grad, NoGrad>::value;
+    bool open = true;
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) a[q] = KIND == TFG_GATE_EXP ? 0.f : 1.f, b[q] = 0.f;
+    for (int q = 0; q < VEC; ++q) a[q] = KIND == TFG_GATE_EXP ? 0.f : 1.f, b[q] = w[q] = 0.f;
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-        float v[VEC], dj[VEC], t[VEC];
-        z.widen(j, v);
-        decay_less_one<KIND>(v, dj, t);
+        float v[VEC], dj[VEC], zj[VEC], less[VEC];
+        z.widen(j, zj);
+        decay_words<KIND, FORM>(zj, dj, less);
         d.put(j, dj);
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((begin >> j) & 1u)) {
 #pragma unroll
             for (int q = 0; q < VEC; ++q) a[q] = 0.f;
             state_or_zero(initial, seq[j], p.f, c, b);
+            open = false;
         }
         x.widen(j, v);
-        if constexpr (KIND == TFG_GATE_EXP) add_vec(a, t);
-        else fma_vec(a, dj, a, a);
-        fma_vec(b, dj, b, b);
-        add_input<KIND>(b, dj, v);
+        if constexpr (KIND == TFG_GATE_EXP) {
+            fma_vec(a, zj, half_log2e, a);
+            advance<KIND, kEither>(b, dj, v);
+        } else if constexpr (FORM == kEither) {
+            decay<kEither>(b, dj);
+            fma_vec(b, less, v, b);
+            decay<kEither>(a, dj);
+        } else {
+            advance<KIND, kLess>(b, dj, v);
+            decay<kLess>(a, dj);
+        }
+        if constexpr (kAdjoint) {
+            if (PLAIN || open) {
+                g.widen(j, v);
+                fma_vec(w, a, v, w);
+                if (!PLAIN && ((end >> j) & 1u)) {
+                    state_or_zero(grad_final, seq[j], p.f, c, v);
+                    fma_vec(w, a, v, w);
+                    open = false;
+                }
+            }
+        }
     }
     if constexpr (KIND == TFG_GATE_EXP) {
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) a[q] = fminf(exp2_of(a[q] * 0.5f), kMostDecay);
+        for (int q = 0; q < VEC; ++q) a[q] = fminf(exp2_of(a[q]), kMostDecay);
     }
 }
 
@@ -545,7 +686,7 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
     const int channel = threadIdx.x % WIDE, part = threadIdx.x / WIDE;
     const int64_t c = c0 + channel;
     const bool mine = part == 0 && c < p.f;
-    if (mine) st_word(p.maps + order * p.f + c, map_word(a, b));
+    if (mine) st_word(p.maps + order * p.f + c, map_word(held_back<KIND>(a), b));
     float state = 0.f;
     if (wants && order > 0) {
         const int first = from < 0 ? 0 : from, begin = part * kMaps;
@@ -564,9 +705,9 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
                 if (word[i] == kNoMap) word[i] = wait_for(maps + i * p.f, kNoMap, p.status);
                 const float wa = __uint_as_float(static_cast<uint32_t>(word[i])), wb = __uint_as_float(static_cast<uint32_t>(word[i] >> 32));
                 mb = begin + i == from ? wb : through<KIND>(wa, mb, wb);
-                ma = both_decays<KIND>(ma, wa);
+                ma *= wa;
             }
-            s_part[part][channel] = make_float2(ma, mb);
+            s_part[part][channel] = make_float2(held_back<KIND>(ma), mb);
         }
         if (entered == kNoState) entered = wait_for(p.states + window * p.f + c, kNoState, p.status);
         state = __uint_as_float(entered);
@@ -582,7 +723,7 @@ __device__ __forceinline__ float enter_tile(const ScanArgs &p, int64_t order, in
         }
     }
     if (mine && place == kWindow - 1 && order + 1 < p.tiles)
-        st_word(p.states + (window + 1) * p.f + c, state_word(fresh ? b : through<KIND>(a, state, b)));
+        st_word(p.states + (window + 1) * p.f + c, state_word(fresh ? b : through<KIND>(held_back<KIND>(a), state, b)));
     return state;
 }
 

@@ -18,7 +18,7 @@
 namespace tfg {
 namespace {
 
-// A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
+// A tile's inputs value by value; the decays take the gates' place, in slots wide enough for it.
 template <typename XT, typename GT>
 struct BackwardSlots {
     using T = ScanTile<XT, 1>;
@@ -88,9 +88,9 @@ template <typename XT, typename GT, int VEC> using BackwardStage = typename Back
 template <typename XT, typename GT, int VEC>
 constexpr int kBackwardCtas = BackwardStage<XT, GT, VEC>::kBytes > 64 * 1024 ? 2 : 3;
 
-// The thread's rows as one map of the adjoint, from the last to the first: w, and its decay, which is that of the
-// states' map (no row between two that begin or end a sequence is left out of either).
-template <bool PLAIN, int EACH, int VEC, typename Grad, typename Decay>
+// What leaves the thread's rows upward when nothing enters them, from the last row to the first (exponential gates: the
+// decays of the rows up to one, which sigmoid gates have at hand, may pass fp32).
+template <bool PLAIN, int FORM, int EACH, int VEC, typename Grad, typename Decay>
 __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, const Decay &d, const float *grad_final,
                                            const int32_t *seq, int64_t c, uint32_t begin, uint32_t end, uint32_t in,
                                            float (&w)[VEC]) {
@@ -104,7 +104,7 @@ __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, con
         g.widen(j, v);
         d.widen(j, dj);
         add_vec(w, v);
-        fma_vec(w, dj, w, w);
+        decay<FORM>(w, dj);
         if (!PLAIN && ((begin >> j) & 1u)) {
 #pragma unroll
             for (int q = 0; q < VEC; ++q) w[q] = 0.f;
@@ -112,49 +112,97 @@ __device__ __forceinline__ void compose_up(const ScanArgs &p, const Grad &g, con
     }
 }
 
-// The gradients of the thread's rows from the state v that enters them and what enters their last, w.
-template <bool PLAIN, int KIND, typename XT, int EACH, int VEC, typename In, typename Grad, typename Decay>
+// Both maps of the thread's rows: (a, b) of the states, (a, w) of the adjoint.
+template <bool PLAIN, int FORM, int KIND, int VEC, int EACH, typename Gate, typename In, typename Decay, typename Grad>
+__device__ __forceinline__ void compose_both(const ScanArgs &p, const Gate &z, const In &x, const Decay &d, const Grad &g,
+                                             const float *initial, const float *grad_final, const int32_t *seq, int64_t c,
+                                             uint32_t begin, uint32_t end, uint32_t in, float (&a)[VEC],
+                                             float (&b)[VEC], float (&w)[VEC]) {
+    if constexpr (KIND == TFG_GATE_EXP) {
+        compose_down<PLAIN, FORM, KIND, VEC, EACH>(p, z, x, d, NoGrad{}, initial, grad_final, seq, c, begin, end, in, a, b, w);
+        compose_up<PLAIN, FORM, EACH>(p, g, d, grad_final, seq, c, begin, end, in, w);
+    } else {
+        compose_down<PLAIN, FORM, KIND, VEC, EACH>(p, z, x, d, g, initial, grad_final, seq, c, begin, end, in, a, b, w);
+    }
+}
+
+// How dL/dz hangs on l in a row that v enters: sigmoid (x - v) a (1 - a), with the sign turned round; exp v a.
+template <int KIND, int FORM, int VEC>
+__device__ __forceinline__ void gate_slope(const float (&v)[VEC], const float (&r)[VEC], const float (&x)[VEC], float (&s)[VEC]) {
+    if constexpr (KIND == TFG_GATE_EXP) {
+        whole_part(r, s);
+        add_vec(s, r);
+        mul_vec(s, v);
+    } else {
+        const float minus[1] = {-1.f};
+        float t[VEC];
+        if constexpr (FORM == kLess) {                       // (v - x) d (1 + d), d = a - 1
+            fma_vec(t, r, r, r);
+            fma_vec(s, x, minus, v);
+        } else {
+            float h[VEC];
+            whole_part(r, h);
+            one_less(r, h, t);
+            add_vec(h, r);
+            mul_vec(t, h);
+            fma_vec(s, v, minus, x);
+        }
+        mul_vec(s, t);
+    }
+}
+
+// dL/dz of a row in place of its slope, dL/dx, and a l in place of l.
+template <int KIND, int FORM, int VEC>
+__device__ __forceinline__ void row_gradient(float (&l)[VEC], const float (&r)[VEC], float (&gz)[VEC], float (&gx)[VEC]) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) gx[q] = l[q];
+    if constexpr (KIND == TFG_GATE_EXP) {
+        mul_vec(gz, l);
+    } else {
+        const float minus[1] = {-1.f};
+        mul_vec(gx, minus);
+        mul_vec(gz, gx);
+        if constexpr (FORM == kLess) {
+            mul_vec(gx, r);
+        } else {
+            float less[VEC];                                 // a - 1
+            whole_part(r, less);
+            add_vec(less, minus);
+            add_vec(less, r);
+            mul_vec(gx, less);
+        }
+    }
+    decay<FORM>(l, r);
+}
+
+// The gradients of the thread's rows from the state v that enters them and what enters their last, w: the slopes down
+// the rows, then the adjoint up them.
+template <bool PLAIN, int FORM, int KIND, typename XT, int EACH, int VEC, typename In, typename Grad, typename Decay>
 __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, const Grad &g, const Decay &d,
                                                 const int32_t *seq, int64_t row, int64_t c, uint32_t begin, uint32_t end,
                                                 uint32_t in, float (&v)[VEC], float (&w)[VEC]) {
-    float before[EACH][VEC];
+    float slope[EACH][VEC];
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
         if (!PLAIN && ((begin >> j) & 1u)) state_or_zero(p.initial, seq[j], p.f, c, v);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) before[j][q] = v[q];
-        if (j + 1 < EACH) {
-            float xv[VEC], dj[VEC];
-            x.widen(j, xv);
-            d.widen(j, dj);
-            fma_vec(v, dj, v, v);
-            add_input<KIND>(v, dj, xv);
-        }
+        float xv[VEC], dj[VEC];
+        x.widen(j, xv);
+        d.widen(j, dj);
+        gate_slope<KIND, FORM>(v, dj, xv, slope[j]);
+        if (j + 1 < EACH) advance<KIND, FORM>(v, dj, xv);
     }
     XT *gate = static_cast<XT *>(p.grad_gate) + row * p.grad_gate_ld + c, *input = static_cast<XT *>(p.grad_x) + row * p.grad_x_ld + c;
 #pragma unroll
     for (int j = EACH - 1; j >= 0; --j) {
         if (!PLAIN && !((in >> j) & 1u)) continue;
         if (!PLAIN && ((end >> j) & 1u)) state_or_zero(p.grad_final, seq[j], p.f, c, w);
-        float gz[VEC], gx[VEC], dj[VEC];
+        float gx[VEC], dj[VEC];
         g.widen(j, gx);
         add_vec(w, gx);                                      // l
-        x.widen(j, gx);
         d.widen(j, dj);
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) {
-            const float less = -dj[q];                     // 1 - a
-            if constexpr (KIND == TFG_GATE_SIGMOID) {
-                gz[q] = w[q] * (before[j][q] - gx[q]) * fmaf(less, dj[q], less);
-                gx[q] = w[q] * less;
-            } else {
-                gz[q] = w[q] * (before[j][q] * (1.f + dj[q]));
-                gx[q] = w[q];
-            }
-        }
-        store_vec<VEC>(gate + j * p.grad_gate_ld, gz);
+        row_gradient<KIND, FORM>(w, dj, slope[j], gx);
+        store_vec<VEC>(gate + j * p.grad_gate_ld, slope[j]);
         store_vec<VEC>(input + j * p.grad_x_ld, gx);
-        fma_vec(w, dj, w, w);
         if (!PLAIN && ((begin >> j) & 1u)) {
             if (p.grad_initial) store_vec<VEC>(p.grad_initial + seq[j] * p.f + c, w);
 #pragma unroll
@@ -234,13 +282,16 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
             else return in_stage.z;
         }();
         if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
-        if (plain) {
-            compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-            compose_up<true, T::kEach>(p, in_stage.g, in_stage.d, nullptr, seq, c, begin, end, in, w);
-        } else {
-            compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
-            compose_up<false, T::kEach>(p, in_stage.g, in_stage.d, on ? p.grad_final : nullptr, seq, c, begin, end, in, w);
-        }
+        bool small = false;
+        if constexpr (KIND == TFG_GATE_SIGMOID) small = small_gates<T>(z, plain && on);
+        const auto compose = [&](auto is_plain, auto form) {
+            compose_both<decltype(is_plain)::value, decltype(form)::value, KIND, VEC, T::kEach>(
+                p, z, in_stage.x, in_stage.d, in_stage.g, on ? p.initial : nullptr, on ? p.grad_final : nullptr, seq, c, begin, end, in,
+                a, b, w);
+        };
+        if (!plain || (kSharedForm<XT> && small)) compose(No{}, Form<kEither>{});
+        else if (KIND == TFG_GATE_EXP || small) compose(Yes{}, Form<kEither>{});
+        else compose(Yes{}, Form<kLess>{});
 #pragma unroll
         for (int q = 0; q < VEC; ++q) u[q] = a[q];
         bool cut = begin != 0u, cut_up = (begin | end) != 0u;
@@ -254,11 +305,11 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
 #pragma unroll
             for (int i = kScanWarps - 1; i >= 0; --i) {
                 const float gu = s_u[i][threadIdx.x], gw = s_w[i][threadIdx.x];
-                s_u[i][threadIdx.x] = tu;
+                s_u[i][threadIdx.x] = held_back<KIND>(tu);
                 s_w[i][threadIdx.x] = tw;
                 const bool fresh = (cut_warps >> warp_bit(i)) & 1u;
                 tw = fresh ? gw : through<KIND>(gu, tw, gw);
-                tu = fresh ? 0.f : both_decays<KIND>(tu, gu);
+                tu = fresh ? 0.f : tu * gu;
             }
         } else if (sc < T::kWide) {
 #pragma unroll
@@ -286,8 +337,13 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         enter_group<T, KIND, true>(u, w, cut_up, l);
         if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
             const int64_t row = r0 + group * T::kEach;
-            if (plain) write_gradients<true, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
-            else write_gradients<false, KIND, XT, T::kEach>(p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+            const auto write = [&](auto is_plain, auto form) {
+                write_gradients<decltype(is_plain)::value, decltype(form)::value, KIND, XT, T::kEach>(
+                    p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+            };
+            if (!plain || (kSharedForm<XT> && small)) write(No{}, Form<kEither>{});
+            else if (KIND == TFG_GATE_EXP || small) write(Yes{}, Form<kEither>{});
+            else write(Yes{}, Form<kLess>{});
         }
         __syncwarp();
     }

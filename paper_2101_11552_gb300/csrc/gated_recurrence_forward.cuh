@@ -7,7 +7,7 @@
 namespace tfg {
 namespace {
 
-// A tile's inputs value by value; a - 1 takes the gates' place, in slots wide enough for it.
+// A tile's inputs value by value; the decays take the gates' place, in slots wide enough for it.
 template <typename XT>
 struct ForwardSlots {
     using T = ScanTile<XT, 1>;
@@ -66,7 +66,7 @@ template <typename XT, int VEC> using ForwardStage = typename ForwardStageOf<XT,
 constexpr int kForwardCtas = 4;
 
 // The rows again, from the state v that enters the thread's first.
-template <bool PLAIN, int KIND, int EACH, typename OT, int VEC, typename In, typename Decay>
+template <bool PLAIN, int FORM, int KIND, int EACH, typename OT, int VEC, typename In, typename Decay>
 __device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const Decay &d, const int32_t *seq, int64_t c,
                                            uint32_t begin, uint32_t end, uint32_t in, OT *out, float (&v)[VEC]) {
 #pragma unroll
@@ -76,8 +76,7 @@ __device__ __forceinline__ void write_rows(const ScanArgs &p, const In &x, const
         float w[VEC], dj[VEC];
         x.widen(j, w);
         d.widen(j, dj);
-        fma_vec(v, dj, v, v);
-        add_input<KIND>(v, dj, w);
+        advance<KIND, FORM>(v, dj, w);
         store_vec<VEC>(out + j * p.f, v);
         if (!PLAIN && ((end >> j) & 1u) && p.final_state) store_vec<VEC>(p.final_state + seq[j] * p.f + c, v);
     }
@@ -142,8 +141,16 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             else return in_stage.z;
         }();
         if (VEC > 1) __syncthreads();                            // the gates are held: the decays lie otherwise
-        if (plain) compose_down<true, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, nullptr, seq, c, begin, in, a, b);
-        else compose_down<false, KIND, VEC, T::kEach>(p, z, in_stage.x, in_stage.d, on ? p.initial : nullptr, seq, c, begin, in, a, b);
+        float none[VEC];
+        bool small = false;
+        if constexpr (KIND == TFG_GATE_SIGMOID) small = small_gates<T>(z, plain && on);
+        const auto compose = [&](auto is_plain, auto form) {
+            compose_down<decltype(is_plain)::value, decltype(form)::value, KIND, VEC, T::kEach>(
+                p, z, in_stage.x, in_stage.d, NoGrad{}, on ? p.initial : nullptr, nullptr, seq, c, begin, end, in, a, b, none);
+        };
+        if (!plain || (kSharedForm<XT> && small)) compose(No{}, Form<kEither>{});
+        else if (KIND == TFG_GATE_EXP || small) compose(Yes{}, Form<kEither>{});
+        else compose(Yes{}, Form<kLess>{});
         bool cut = begin != 0u;
         scan_groups<T, KIND, false>(a, b, cut, warp, lane, s_a, s_b);
         __syncthreads();
@@ -156,11 +163,11 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
 #pragma unroll
             for (int w = 0; w < kScanWarps; ++w) {
                 const float wa = s_a[w][threadIdx.x], wb = s_b[w][threadIdx.x];
-                s_a[w][threadIdx.x] = ta;
+                s_a[w][threadIdx.x] = held_back<KIND>(ta);
                 s_b[w][threadIdx.x] = tb;
                 const bool fresh = (begin_warps >> warp_bit(w)) & 1u;
                 tb = fresh ? wb : through<KIND>(wa, tb, wb);     // not 0 times what may be an infinity
-                ta = fresh ? 0.f : both_decays<KIND>(ta, wa);
+                ta = fresh ? 0.f : ta * wa;
             }
         }
         const bool wants = (rows.in[0] & ~rows.begin[0] & 1u) != 0u;
@@ -180,8 +187,13 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
         enter_group<T, KIND, false>(a, b, cut, v);
         if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
             OT *out = static_cast<OT *>(p.out) + (r0 + group * T::kEach) * p.f + c;
-            if (plain) write_rows<true, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
-            else write_rows<false, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end, in, out, v);
+            const auto write = [&](auto is_plain, auto form) {
+                write_rows<decltype(is_plain)::value, decltype(form)::value, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end,
+                                                                                             in, out, v);
+            };
+            if (!plain || (kSharedForm<XT> && small)) write(No{}, Form<kEither>{});
+            else if (KIND == TFG_GATE_EXP || small) write(Yes{}, Form<kEither>{});
+            else write(Yes{}, Form<kLess>{});
         }
         __syncwarp();
     }
