@@ -1124,10 +1124,15 @@ def tfg_gated_recurrence(gate, x, node_offsets, kind: str = "sigmoid", initial=N
     return GatedRecurrence(out, final, kept, status)
 
 
-class GatedRecurrenceGrads(NamedTuple):
+class _RecurrenceGrads(NamedTuple):
     gate: torch.Tensor
     x: torch.Tensor
     initial: Optional[torch.Tensor]       # fp32 [S, F], with want_initial
+
+
+class GatedRecurrenceGrads(_RecurrenceGrads):
+    """The three gradients as a tuple, and beside them ``status``, int32 [1] (device)."""
+    status: torch.Tensor
 
 
 def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=None, kind: str = "sigmoid", initial=None,
@@ -1137,7 +1142,8 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     ``grad_out`` [N, F] (either type; None: zeros) and ``grad_final`` [S, F] fp32 (None: zeros).
     The states' gradient by default where there was an initial state.  ``grad_gate`` and ``grad_x``
     may be given as buffers whose rows lie apart; rows outside all sequences are left as
-    they are in them.  ``status`` int32 [1] takes the call's status word."""
+    they are in them.  ``status`` int32 [1], the caller's or a new one, takes the call's status word and is
+    the result's ``status``: look at it (check_status) before the gradients are relied on."""
     index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
     if checkpoints is None:
         raise ValueError("checkpoints are the forward's (want_checkpoints)")
@@ -1156,7 +1162,9 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     _run(index, "tfg_gated_recurrence_backward", *head, kept, _at(grad_out), grad_code, last,
          grads[0][0].data_ptr(), grads[0][1], grads[1][0].data_ptr(), grads[1][1], _at(grad_initial), *_span(workspace),
          status.data_ptr())
-    return GatedRecurrenceGrads(grads[0][0], grads[1][0], grad_initial)
+    result = GatedRecurrenceGrads(grads[0][0], grads[1][0], grad_initial)
+    result.status = status
+    return result
 
 
 class DistillationLoss(NamedTuple):
