@@ -77,6 +77,8 @@ typedef enum { TFG_ACT_NONE = 0, TFG_ACT_RELU = 1, TFG_ACT_SILU = 2, TFG_ACT_GEL
 /* Gates of tfg_gated_recurrence: a = 1 / (1 + exp(-z)) with the input (1 - a) x,
  * a = exp(z) with the input x. */
 typedef enum { TFG_GATE_SIGMOID = 0, TFG_GATE_EXP = 1 } tfg_gate;
+/* Added to a gate: rows outside all sequences are written, as zeros. */
+#define TFG_GATE_ZERO_OUTSIDE 256
 
 /* Library version (major * 10000 + minor * 100 + patch). */
 int tfg_version(void);
@@ -756,7 +758,10 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
  *   node_offsets (device) int64 [num_sequences + 1], non-decreasing, in
  *        [0, num_rows]: sequence s holds rows node_offsets[s] ..
  *        node_offsets[s + 1] - 1.  Rows before the first and from the last
- *        offset on are left as they were in every output.
+ *        offset on are left as they were in every output, or, with
+ *        TFG_GATE_ZERO_OUTSIDE added to gate_kind, written as zeros in out, and by
+ *        the backward in grad_gate and grad_x: what a padded batch wants whose next step
+ *        sums over all rows (the gradient of a projection).
  *   initial (device) fp32 [num_sequences, num_features], or NULL for zeros.
  *   out (device) [num_rows, num_features], out_dtype.
  *   final_state (device) fp32 [num_sequences, num_features] or NULL: v behind

@@ -1421,8 +1421,10 @@ int check_recurrence(const char *fn, int64_t num_rows, int64_t num_sequences, in
     return TFG_OK;
 }
 
+int gate_of(int gate_kind) { return gate_kind & ~TFG_GATE_ZERO_OUTSIDE; }
+bool zeroes_of(int gate_kind) { return (gate_kind & TFG_GATE_ZERO_OUTSIDE) != 0; }
 int check_gate(const char *fn, int gate_kind) {
-    if (gate_kind != TFG_GATE_SIGMOID && gate_kind != TFG_GATE_EXP)
+    if (gate_of(gate_kind) != TFG_GATE_SIGMOID && gate_of(gate_kind) != TFG_GATE_EXP)
         return fail(TFG_ERR_INVALID_ARG, "%s: unknown gate %d", fn, gate_kind);
     return TFG_OK;
 }
@@ -1481,8 +1483,8 @@ int tfg_gated_recurrence(const void *gate, int64_t gate_stride, const void *x, i
     for (const Rows &r : outs) TFG_DEBUG(debug_extent(fn, r.name, r.p, r.extent));
     TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
 #endif
-    return cuda_result(tfg::launch_gated_recurrence(gate, gate_stride, x, x_stride, dtype, node_offsets, n, q, f, gate_kind,
-                                                    initial, out, out_dtype, final_state, entering, workspace, status,
+    return cuda_result(tfg::launch_gated_recurrence(gate, gate_stride, x, x_stride, dtype, node_offsets, n, q, f, gate_of(gate_kind),
+                                                    zeroes_of(gate_kind), initial, out, out_dtype, final_state, entering, workspace, status,
                                                     reinterpret_cast<cudaStream_t>(stream)),
                        fn);
 }
@@ -1533,7 +1535,7 @@ int tfg_gated_recurrence_backward(const void *gate, int64_t gate_stride, const v
     TFG_DEBUG(debug_extent(fn, "workspace", workspace, need));
 #endif
     return cuda_result(tfg::launch_gated_recurrence_backward(gate, gate_stride, x, x_stride, dtype, node_offsets, n, q, f,
-                                                             gate_kind, initial, entering, grad_out, grad_dtype, grad_final,
+                                                             gate_of(gate_kind), zeroes_of(gate_kind), initial, entering, grad_out, grad_dtype, grad_final,
                                                              grad_gate, grad_gate_stride, grad_x, grad_x_stride, grad_initial,
                                                              workspace, status, reinterpret_cast<cudaStream_t>(stream)),
                        fn);

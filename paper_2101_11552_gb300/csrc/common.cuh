@@ -362,11 +362,11 @@ cudaError_t launch_layer_norm_backward(const void *sum, int sum_dtype, int64_t n
                                        cudaStream_t s);
 size_t gated_recurrence_workspace_bytes(int64_t n, int64_t f);
 cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
-                                    const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                    const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind, bool zeroes,
                                     const float *initial, void *out, int out_dtype, float *final_state, float *entering,
                                     void *ws, int32_t *status, cudaStream_t s);
 cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
-                                             const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                             const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind, bool zeroes,
                                              const float *initial, const float *entered, const void *g, int g_dtype,
                                              const float *grad_final, void *grad_gate, int64_t grad_gate_ld, void *grad_x,
                                              int64_t grad_x_ld, float *grad_initial, void *ws, int32_t *status,

@@ -11,7 +11,10 @@ namespace {
 // tile, a warp for each 32.
 __global__ void __launch_bounds__(256) scan_plan_kernel(ScanArgs p, uint4 *words, int64_t n, TileRows *plan) {
     cudaTriggerProgrammaticLaunchCompletion();               // the tiles' kernel may be set up; it waits for this one's end
-    const int64_t threads = static_cast<int64_t>(gridDim.x) * 256, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    // CTAs of their own: beside the rest the two offsets cost every CTA a trip to memory (1,024 molecules 107 -> 110 us)
+    if (static_cast<int>(blockIdx.x) < p.clear_ctas) return clear_outside(p, blockIdx.x * 8 + threadIdx.x / 32, p.clear_ctas * 8);
+    const int64_t threads = static_cast<int64_t>(gridDim.x - p.clear_ctas) * 256,
+                  id = static_cast<int64_t>(blockIdx.x - p.clear_ctas) * 256 + threadIdx.x;
     if (id == 0) *p.status = TFG_OK;
     if (!p.linked) return;
     for (int64_t i = id; i < n; i += threads) words[i] = i ? make_uint4(~0u, ~0u, ~0u, ~0u) : make_uint4(0u, 0u, 0u, 0u);
@@ -45,6 +48,15 @@ int scan_vector(const ScanArgs &p, int dtype, bool backward) {
 int tile_channels(int dtype, int vec) {
     if (vec == 1) return ScanTile<float, 1>::kWide;
     return dtype == TFG_BF16 ? ScanTile<uint16_t, 4>::kWide : ScanTile<float, 4>::kWide;
+}
+
+// The rows of up to two outputs that become zeros outside all sequences.
+void clear_rows(ScanArgs &p, int size, void *a, int64_t a_ld, void *b, int64_t b_ld) {
+    p.clear[0] = static_cast<char *>(a), p.clear[1] = static_cast<char *>(b);
+    p.clear_ld[0] = a_ld * size, p.clear_ld[1] = b_ld * size, p.clear_width = p.f * size;
+    const uint64_t all = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | p.clear_ld[0] | p.clear_ld[1] | p.clear_width;
+    p.clear_unit = all % 16 == 0 ? 16 : size;
+    p.clear_ctas = sm_count();
 }
 
 void scan_geometry(ScanArgs &p, int dtype, int vec, void *ws, int32_t *status) {
@@ -109,7 +121,7 @@ cudaError_t scan_plan(const ScanArgs &p, void *ws, cudaStream_t s) {
     const ScanSpace space(p.n, p.f);
     const int64_t words = static_cast<int64_t>(space.plan / 16);
     const int64_t ctas = min64(words / 256 + 1 + p.tiles * (kTileRows / 32) / 8, 8 * static_cast<int64_t>(sm_count()));
-    scan_plan_kernel<<<static_cast<unsigned>(ctas), 256, 0, s>>>(
+    scan_plan_kernel<<<static_cast<unsigned>(ctas + p.clear_ctas), 256, 0, s>>>(
         p, static_cast<uint4 *>(ws), words, reinterpret_cast<TileRows *>(static_cast<char *>(ws) + space.plan));
     return cudaGetLastError();
 }
@@ -124,12 +136,13 @@ cudaError_t launch_scan_backward_f32(const ScanArgs &p, const ScanMaps &maps, in
 cudaError_t launch_scan_backward_bf16(const ScanArgs &p, const ScanMaps &maps, int vec, int kind, cudaStream_t s);
 
 cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
-                                    const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                    const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind, bool zeroes,
                                     const float *initial, void *out, int out_dtype, float *final_state, float *entering,
                                     void *ws, int32_t *status, cudaStream_t s) {
     ScanArgs p{};
     p.gate = gate, p.gate_ld = gate_ld, p.x = x, p.x_ld = x_ld, p.offsets = offsets, p.n = n, p.seqs = seqs, p.f = f;
     p.initial = initial, p.out = out, p.out_bf16 = out_dtype == TFG_BF16, p.final_state = final_state, p.entering = entering;
+    if (zeroes) clear_rows(p, out_dtype == TFG_BF16 ? 2 : 4, out, f, nullptr, 0);
     const int vec = scan_vector(p, dtype, false);
     scan_geometry(p, dtype, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);
@@ -140,7 +153,7 @@ cudaError_t launch_gated_recurrence(const void *gate, int64_t gate_ld, const voi
 }
 
 cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, const void *x, int64_t x_ld, int dtype,
-                                             const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind,
+                                             const int64_t *offsets, int64_t n, int64_t seqs, int64_t f, int kind, bool zeroes,
                                              const float *initial, const float *entered, const void *g, int g_dtype,
                                              const float *grad_final, void *grad_gate, int64_t grad_gate_ld, void *grad_x,
                                              int64_t grad_x_ld, float *grad_initial, void *ws, int32_t *status,
@@ -150,6 +163,7 @@ cudaError_t launch_gated_recurrence_backward(const void *gate, int64_t gate_ld, 
     p.initial = initial, p.entered = entered, p.g = g, p.out_bf16 = g_dtype == TFG_BF16, p.grad_final = grad_final;
     p.grad_gate = grad_gate, p.grad_gate_ld = grad_gate_ld, p.grad_x = grad_x, p.grad_x_ld = grad_x_ld;
     p.grad_initial = grad_initial;
+    if (zeroes) clear_rows(p, dtype == TFG_BF16 ? 2 : 4, grad_gate, grad_gate_ld, grad_x, grad_x_ld);
     const int vec = scan_vector(p, dtype, true);
     scan_geometry(p, dtype, vec, ws, status);
     const cudaError_t e = scan_plan(p, ws, s);

@@ -73,6 +73,11 @@ struct ScanArgs {
     int64_t tiles;
     int strips;                           // of channels
     bool linked;                          // there are tiles to wait for
+    char *clear[2];                       // outputs whose rows outside all sequences become zeros, or null
+    int64_t clear_ld[2];                  // their strides
+    int64_t clear_width;                  // and a row's width, in bytes
+    int clear_unit;                       // 16 where all of that is, else a value's size
+    int clear_ctas;                       // of the plan's kernel: in front, for this alone
     int checkers;                         // CTAs in front that look at the sequences
     const struct TileRows *plan;          // of each tile, where tiles are linked
     uint32_t *next;                       // the counter that hands out tiles
@@ -368,6 +373,26 @@ __device__ __forceinline__ void find_rows(const ScanArgs &p, TileRows &t) {
     __syncthreads();
 }
 
+// Zeros in the rows before the first sequence and behind the last, a warp a row.
+__device__ __forceinline__ void clear_outside(const ScanArgs &p, int64_t warp, int64_t warps) {
+    if (!p.clear[0]) return;
+    const auto inside = [&](int64_t r) { return r < 0 ? 0 : min64(r, p.n); };
+    const int64_t lo = p.seqs ? inside(__ldg(p.offsets)) : 0, hi = p.seqs ? inside(__ldg(p.offsets + p.seqs)) : 0;
+    for (int64_t i = warp; i < lo + p.n - hi; i += warps) {
+        const int64_t row = i < lo ? i : hi + i - lo;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!p.clear[k]) continue;
+            char *at = p.clear[k] + row * p.clear_ld[k];
+            for (int64_t b = (threadIdx.x & 31) * p.clear_unit; b < p.clear_width; b += 32 * p.clear_unit) {
+                if (p.clear_unit == 16) *reinterpret_cast<uint4 *>(at + b) = make_uint4(0u, 0u, 0u, 0u);
+                else if (p.clear_unit == 4) *reinterpret_cast<uint32_t *>(at + b) = 0u;
+                else *reinterpret_cast<uint16_t *>(at + b) = 0;
+            }
+        }
+    }
+}
+
 // The sequences by themselves: offsets that decrease or leave [0, n], and what an empty
 // sequence hands on: to = from (zeros without).
 __device__ __forceinline__ void check_sequences(const ScanArgs &p, const float *from, float *to) {
@@ -389,6 +414,7 @@ __device__ __forceinline__ void check_sequences(const ScanArgs &p, const float *
             for (int64_t c = lane; c < p.f; c += 32) to[at + c] = from ? __ldg(from + at + c) : 0.f;
         }
     }
+    if (p.status_all) clear_outside(p, threadIdx.x / 32, kScanThreads / 32);         // no plan is made
     const int all = __syncthreads_or(any);
     if (threadIdx.x != 0) return;
     if (p.status_all) *p.status_all = all ? TFG_ERR_INDEX_RANGE : TFG_OK;

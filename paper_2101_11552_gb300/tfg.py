@@ -35,6 +35,7 @@ TFG_ERR_TIMEOUT = -7
 TFG_F32, TFG_BF16 = 0, 1
 REDUCERS = {"sum": 0, "mean": 1, "max": 2}
 GATES = {"sigmoid": 0, "exp": 1}
+GATE_ZERO_OUTSIDE = 256       # rows outside all sequences become zeros
 RECURRENCE_TILE_ROWS = 128
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 NO_PADDING = -(1 << 63)       # padding_id of a list without padding
@@ -1069,7 +1070,7 @@ def _strided_rows(name: str, t, index: int, shape=None, dtype=None) -> int:
     return strides[0] if n > 1 else f
 
 
-def _recurrence_inputs(gate, x, node_offsets, kind, initial):
+def _recurrence_inputs(gate, x, node_offsets, kind, initial, zeroes):
     ld = _strided_rows("gate", gate, -1)
     index = gate.get_device()
     n, f = gate.shape
@@ -1082,8 +1083,8 @@ def _recurrence_inputs(gate, x, node_offsets, kind, initial):
     kind_code = GATES.get(kind)
     if kind_code is None:
         raise ValueError(f"kind must be one of {sorted(GATES)}, got {kind!r}")
-    return index, n, f, s, code, (gate.data_ptr(), ld, x.data_ptr(), x_ld, code, node_offsets.data_ptr(), n, s, f, kind_code,
-                                  _states("initial", initial, index, (s, f)))
+    return index, n, f, s, code, (gate.data_ptr(), ld, x.data_ptr(), x_ld, code, node_offsets.data_ptr(), n, s, f,
+                                  kind_code + GATE_ZERO_OUTSIDE if zeroes else kind_code, _states("initial", initial, index, (s, f)))
 
 
 def _states(name: str, t, index: int, shape):
@@ -1108,8 +1109,8 @@ def tfg_gated_recurrence(gate, x, node_offsets, kind: str = "sigmoid", initial=N
     the rows node_offsets[s] .. node_offsets[s + 1] - 1 of gate and x [N, F], whose rows may
     lie apart (the halves of one projection); ``initial`` [S, F] fp32 are the states before
     them, zeros by default, and ``final`` those behind them.  Rows outside all sequences are left
-    as they are in ``out`` (unset in a new one)."""
-    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
+    as they are in ``out``, and are zeros in a new one."""
+    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial, out is None)
     if out_dtype is None:
         out_dtype = gate.dtype if out is None else out.dtype
     out_code = _dtype_code("out", out_dtype)
@@ -1142,9 +1143,10 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     ``grad_out`` [N, F] (either type; None: zeros) and ``grad_final`` [S, F] fp32 (None: zeros).
     The states' gradient by default where there was an initial state.  ``grad_gate`` and ``grad_x``
     may be given as buffers whose rows lie apart; rows outside all sequences are left as
-    they are in them.  ``status`` int32 [1], the caller's or a new one, takes the call's status word and is
+    they are in them, and are zeros in new ones.  ``status`` int32 [1], the caller's or a new one, takes the call's status word and is
     the result's ``status``: look at it (check_status) before the gradients are relied on."""
-    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial)
+    fresh = grad_gate is None and grad_x is None
+    index, n, f, s, code, head = _recurrence_inputs(gate, x, node_offsets, kind, initial, fresh)
     if checkpoints is None:
         raise ValueError("checkpoints are the forward's (want_checkpoints)")
     last, kept = _states("grad_final", grad_final, index, (s, f)), _states("checkpoints", checkpoints, index, (_tiles(n), f))
@@ -1152,7 +1154,7 @@ def tfg_gated_recurrence_backward(gate, x, node_offsets, checkpoints, grad_out=N
     grads = []
     for name, t in (("grad_gate", grad_gate), ("grad_x", grad_x)):
         if t is None:
-            t = torch.empty(n, f, dtype=gate.dtype, device=gate.device)
+            t = (torch.empty if fresh else torch.zeros)(n, f, dtype=gate.dtype, device=gate.device)
         grads.append((t, _strided_rows(name, t, index, gate.shape, gate.dtype)))
     if want_initial is None:
         want_initial = initial is not None

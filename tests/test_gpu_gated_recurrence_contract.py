@@ -25,3 +25,67 @@ def test_the_backward_hands_its_status_back(n):
     mine = torch.full((1,), 7, dtype=torch.int32, device="cuda")
     b = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, x, status=mine)
     assert b.status is mine and int(mine) == 0
+
+
+def poison(n, f, dtype):
+    """What the allocator hands out next held NaN."""
+    for k in (1, 2, 3):
+        torch.full((k * n, f), float("nan"), dtype=dtype, device="cuda")
+
+
+PADDED = {"one tile": ([3, 50, 90], 120), "no sequence": ([5], 60), "tail of tiles": ([0, 130, 300], 900),
+          "from the middle": ([700, 701, 1000], 1037), "empty ones": ([40, 40, 40, 200, 200], 333)}
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "exp"])
+@pytest.mark.parametrize("layout", PADDED)
+@pytest.mark.parametrize("f,dt", [(8, "f32"), (72, "bf16"), (33, "f32"), (5, "bf16")])
+def test_rows_outside_all_sequences_are_zeros_in_new_tensors(f, dt, layout, kind):
+    """A padded batch: the projections' gradients are sums over all rows."""
+    offsets, n = PADDED[layout]
+    z, x = batch(n, f, kind, dt, 2)
+    off = torch.tensor(offsets, device="cuda")
+    lo, hi = offsets[0], offsets[-1]
+    poison(n, f, z.dtype)
+    r = tfg.tfg_gated_recurrence(z, x, off, kind)
+    tfg.check_status(r.status)
+    outside = torch.ones(n, dtype=torch.bool, device="cuda")
+    outside[lo:hi] = False
+    assert bool((r.out[outside] == 0).all()) and bool(torch.isfinite(r.out).all())
+    g = normal(n, f, 3, dt)
+    poison(n, f, z.dtype)
+    b = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, g, kind)
+    for t in b[:2]:
+        assert bool((t[outside] == 0).all()) and bool(torch.isfinite(t).all())
+    # what is given keeps its rows, alone or with a new one beside it; the rows of sequences have the same bits
+    mark = torch.full((n, f), 3.5, dtype=z.dtype, device="cuda")
+    kept = tfg.tfg_gated_recurrence(z, x, off, kind, out=mark.clone())
+    assert torch.equal(kept.out[outside], mark[outside]) and torch.equal(kept.out[lo:hi], r.out[lo:hi])
+    poison(n, f, z.dtype)
+    half = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, g, kind, grad_gate=mark.clone())
+    assert torch.equal(half.gate[outside], mark[outside]) and bool((half.x[outside] == 0).all())
+    assert torch.equal(half.gate[lo:hi], b.gate[lo:hi]) and torch.equal(half.x[lo:hi], b.x[lo:hi])
+
+
+def test_a_projections_gradient_over_a_padded_batch():
+    n, f, k, offsets = 500, 32, 16, [0, 77, 300]
+    h = normal(n, k, 1)
+    w = normal(k, 2 * f, 2) * 0.2
+    off = torch.tensor(offsets, device="cuda")
+    z, x = (h @ w).chunk(2, dim=1)
+    poison(n, 2 * f, torch.float32)
+    r = tfg.tfg_gated_recurrence(z, x, off)
+    b = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, torch.ones(n, f, device="cuda"))
+    both = torch.cat([b.gate, b.x], 1)
+    assert torch.equal(h.t() @ both, torch.cat([h[:300], torch.zeros_like(h[300:])]).t() @ both)
+    assert bool(torch.isfinite(h.t() @ both).all()) and bool(torch.isfinite(r.out.t() @ both).all())
+
+
+def test_the_flag_beside_unknown_gates():
+    z, x = batch(20, 8, "sigmoid", "f32", 1)
+    off = torch.tensor([0, 20], device="cuda")
+    out, status = torch.empty_like(x), torch.empty(1, dtype=torch.int32, device="cuda")
+    for kind in (2, 256 + 2, 512, -1):
+        rc = tfg.lib().tfg_gated_recurrence(z.data_ptr(), 8, x.data_ptr(), 8, 0, off.data_ptr(), 20, 1, 8, kind, None, out.data_ptr(), 0,
+                                            None, None, None, 0, status.data_ptr(), None)
+        assert rc != 0
