@@ -702,7 +702,8 @@ int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, con
  *   x (device) [num_rows, num_features] row-major, TFG_F32 or TFG_BF16.
  *   residual (device) [num_rows, num_features] of sum_dtype, or NULL.
  *   sum (device) [num_rows, num_features] of sum_dtype: s, written; may be
- *        residual (the stream updated in place).  Without a residual sum must be
+ *        residual (the stream updated in place, for serving: the backward reads
+ *        this layer's s, which the next layer's call in place would overwrite).  Without a residual sum must be
  *        NULL and sum_dtype is not looked at.
  *   gamma, beta (device) fp32 [num_features], or NULL for 1 and 0.
  *   eps: finite, > 0.
@@ -716,8 +717,9 @@ int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, con
  * tfg_layer_norm_backward: with g = dL/dout, h = (s - m) r, d = gamma g:
  *   grad_s = r (d - mean d - h mean(d h)) + grad_sum
  *   grad_gamma = sum over rows of g h, grad_beta = sum of g
- *   sum: the forward's s (x without a residual), of sum_dtype; mean, rstd: the
- *        forward's.
+ *   sum: the forward's s (x without a residual), of sum_dtype, as that call wrote
+ *        it: nothing tells whether another layer has since updated it in place;
+ *        mean, rstd: the forward's.
  *   grad_out (device) [num_rows, num_features] of grad_dtype.
  *   grad_sum (device) [num_rows, num_features] of grad_sum_dtype, or NULL: the
  *        gradient that reaches s by other ways (the stream's own).

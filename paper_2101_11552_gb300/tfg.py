@@ -972,7 +972,8 @@ def _weight(name: str, t, index: int, f: int):
 def tfg_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, out_dtype: Optional[torch.dtype] = None,
                    want_stats: bool = True, out=None, sum_out=None) -> LayerNorm:
     """Layer norm of the rows of x [N, F], or of x + residual, which is stored in the residual's
-    type and normalised as stored.  ``sum_out`` may be the residual itself (in place)."""
+    type and normalised as stored.  ``sum_out`` may be the residual itself (in place): for serving, as the
+    backward reads this layer's sum, which the next layer's update in place would overwrite."""
     index = _index("x", x)
     if x.dim() != 2:
         raise ValueError("x must have shape [N, F]")
@@ -1004,7 +1005,7 @@ def tfg_layer_norm_backward_workspace_size(num_rows: int, num_features: int) -> 
 
 def tfg_layer_norm_backward(sum, gamma, mean, rstd, grad_out, grad_sum=None, grad_dtype: Optional[torch.dtype] = None,
                             want_weight_grads: bool = True, grad_x=None, workspace=None):
-    """Gradients of tfg_layer_norm from its ``sum``, mean and rstd.  ``grad_sum``: the gradient
+    """Gradients of tfg_layer_norm from its ``sum`` as that call left it, mean and rstd.  ``grad_sum``: the gradient
     that reaches the sum by other ways (the residual stream's own), added.  Returns (grad_x
     [N, F], the gradient of x and residual alike, grad_gamma [F], grad_beta [F]), the last two None
     without ``want_weight_grads``.  grad_x has the type of grad_sum, else ``grad_dtype`` (by
