@@ -730,8 +730,10 @@ int tfg_clip_by_global_norm(int64_t num_tensors, const void *const *tensors, con
  *   workspace (device) >= tfg_layer_norm_backward_workspace_size() bytes,
  *        16-byte aligned; not used, and may be NULL, without grad_gamma.
  * Outputs overlap no input and no other output (but grad_s, which may be grad_sum).
- * Rows of NaN or infinities give NaN in their own row, and in grad_gamma and
- * grad_beta.  Sums in fp32 in a fixed order: bitwise reproducible between calls
+ * A row of sum that holds NaN or infinities gives NaN in its own row of grad_s and in
+ * grad_gamma; grad_beta, a sum of grad_out alone, does not see it.  What grad_out
+ * holds of them reaches its row and both sums.  Deviations whose squares' sum passes
+ * fp32 (values of 1e17 and more) give rstd 0, and with it out = beta.  Sums in fp32 in a fixed order: bitwise reproducible between calls
  * of the same alignment.
  * ---------------------------------------------------------------------- */
 int tfg_layer_norm(const void *x, int x_dtype, const void *residual, int sum_dtype, void *sum,
@@ -838,11 +840,12 @@ int tfg_gated_recurrence_backward(const void *gate, int64_t gate_stride, const v
  *   temperature: from 1e-6 to 1e6.
  *   row_weight (device) fp32 [num_rows] (w), or NULL for 1.  A row whose weight
  *        is 0, or that has no teacher entry above -inf, has a loss of 0 and a gradient
- *        of zeros whatever its logits hold; they are not read.
+ *        of zeros whatever its logits hold (NaN and infinities included).  The logits of
+ *        rows of weight 0 are not read; those of the others may be.
  *   loss (device) fp32 [num_rows].
  *   stats (device) fp32 [num_rows, 2] or NULL: for the backward, m = the
- *        largest logit and the sum of exp((logits - m) / T); (0, 1) in rows that are
- *        not read.
+ *        largest logit and the sum of exp((logits - m) / T); (0, 1) in rows that
+ *        count for nothing.
  *   grad_logits (device) [num_rows, num_classes] of the logits' type, or NULL:
  *        dloss/dlogits, in the same pass.
  *   status (device) int32 [1]: 0, or TFG_ERR_INDEX_RANGE when an id lies outside

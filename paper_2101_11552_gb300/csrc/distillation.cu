@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(TT <= 32 ? kDistilThreads : TT) distil_rows(Di
         if (f != 0.f) load_vectors<TT>(r, t, raw);
     }
     load_top<TT>(a, row, t, s_fold, MODE != kBack && !a.status_all, top);   // with barriers, behind those of the copies
-    if (f == 0.f || !top.any) {                              // a row that counts for nothing is not read
+    if (f == 0.f || !top.any) {                              // a row that counts for nothing
         if (MODE != kBack && t == 0 && mine) {
             a.loss[row] = 0.f;
             if (a.stats) a.stats[row] = make_float2(0.f, 1.f);

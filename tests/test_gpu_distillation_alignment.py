@@ -45,3 +45,20 @@ def test_a_slice_has_the_same_bits_with_its_gradient(n, v, dt):
             back = grad.clone()
         assert torch.equal(grad, back)
         assert bool((room[:16 + first] == 5).all()) and bool((room[16 + first + n * v:] == 5).all())
+
+
+def test_rows_that_count_for_nothing():
+    """Weight 0, or no teacher entry above -inf: zeros whatever the logits hold, and statistics of (0, 1)."""
+    for v in (41, 5000, 60_001):
+        logits = torch.randn(8, v, device="cuda")
+        logits[1], logits[2, 5], logits[3] = float("nan"), float("inf"), -float("inf")
+        ids = torch.arange(8 * 4, device="cuda").view(8, 4) % v
+        teacher, w = torch.zeros(8, 4, device="cuda"), torch.ones(8, device="cuda")
+        w[1] = w[3] = 0.0
+        teacher[2] = -float("inf")
+        r = tfg.tfg_distillation_loss(logits, ids, teacher, row_weight=w, want_stats=True, want_grad=True)
+        back = tfg.tfg_distillation_loss_backward(logits, ids, teacher, 1.0, r.stats, torch.ones(8, device="cuda"), row_weight=w)
+        for i in (1, 2, 3):
+            assert float(r.loss[i]) == 0 and r.stats[i].tolist() == [0, 1]
+            assert bool((r.grad_logits[i] == 0).all()) and bool((back[i] == 0).all())
+        assert bool(torch.isfinite(r.loss).all()) and bool(torch.isfinite(r.grad_logits).all())

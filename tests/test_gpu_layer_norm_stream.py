@@ -59,3 +59,29 @@ def test_three_layers_of_a_stream(f):
     got[0] = grad_stream
     for a, b in zip(got, want):
         assert float((a.double() - b).norm()) <= 1e-5 * float(b.norm())
+
+
+@pytest.mark.parametrize("f", [64, 37, 3001])
+def test_where_values_that_are_no_numbers_go(f):
+    """As the header says: a row of the sum that holds one reaches its own row of grad_s and grad_gamma, not grad_beta; what
+    grad_out holds of them reaches its row and both sums.  Deviations beyond fp32's squares give rstd 0."""
+    gen = torch.Generator(device="cuda").manual_seed(f)
+    x, g = (torch.randn(40, f, device="cuda", generator=gen) for _ in range(2))
+    gamma, beta = torch.rand(f, device="cuda", generator=gen), torch.rand(f, device="cuda", generator=gen)
+    x[4, f // 2] = float("nan")
+    x[9, 1] = 1e25
+    r = tfg.tfg_layer_norm(x, gamma, beta)
+    assert float(r.rstd[9]) == 0.0 and torch.equal(r.out[9], beta) and bool(torch.isnan(r.out[4]).all())
+    gx, gg, gb = tfg.tfg_layer_norm_backward(x, gamma, r.mean, r.rstd, g)
+    rest = [i for i in range(40) if i != 4]
+    assert bool(torch.isnan(gx[4]).all()) and bool(torch.isfinite(gx[rest]).all())
+    assert bool(torch.isnan(gg).all()) and bool(torch.isfinite(gb).all())
+    g[11, 2] = float("inf")
+    x[4] = 1.0
+    r = tfg.tfg_layer_norm(x, gamma, beta)
+    gx, gg, gb = tfg.tfg_layer_norm_backward(x, gamma, r.mean, r.rstd, g)
+    rest = [i for i in range(40) if i != 11]
+    assert not bool(torch.isfinite(gx[11]).any()) and bool(torch.isfinite(gx[rest]).all())
+    assert not bool(torch.isfinite(gg[2])) and not bool(torch.isfinite(gb[2]))
+    others = [c for c in range(f) if c != 2]
+    assert bool(torch.isfinite(gb[others]).all())
