@@ -48,12 +48,13 @@ def needs_build() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False, ptxas_info: bool = False,
-                  defines: tuple = (), lib_path: str | None = None) -> str:
+                  defines: tuple = (), lib_path: str | None = None, only: str = "") -> str:
     """Build libtfg.so if needed and return its path.
 
     ``defines`` (e.g. ("TFG_NO_PACKED_FMA",)) and ``lib_path`` build a variant
     of the library elsewhere, for side-by-side timing; the default build
-    defines nothing.
+    defines nothing.  With ``only`` a variant compiles the sources whose names begin so, and takes the
+    others' objects from the default build, which it makes first if needed.
     """
     out_path = lib_path or LIB_PATH
     obj_dir = OBJ_DIR if not defines else os.path.join(OBJ_DIR, "_".join(defines))
@@ -61,10 +62,14 @@ def build_library(force: bool = False, verbose: bool = False, ptxas_info: bool =
         return LIB_PATH
     nvcc = _nvcc()
     os.makedirs(obj_dir, exist_ok=True)
+    if only:
+        build_library()
     extra = ["-Xptxas", "-v"] if ptxas_info else []
     extra += [f"-D{d}" for d in defines]
 
     def compile_one(src: str) -> str:
+        if only and not os.path.basename(src).startswith(only):
+            return os.path.join(OBJ_DIR, os.path.basename(src) + ".o")
         obj = os.path.join(obj_dir, os.path.basename(src) + ".o")
         cmd = [nvcc, *ARCH, *NVCC_FLAGS, *extra, "-c", src, "-o", obj]
         res = subprocess.run(cmd, capture_output=True, text=True)

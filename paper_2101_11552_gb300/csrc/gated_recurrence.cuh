@@ -150,7 +150,10 @@ namespace {
 
 constexpr uint64_t kNoMap = ~uint64_t(0);
 constexpr uint32_t kNoState = ~uint32_t(0);
-constexpr int kWaitLimit = 1 << 21;                          // looks at a word, a second or more
+#ifndef TFG_WAIT_LOOKS
+#define TFG_WAIT_LOOKS (1 << 21)
+#endif
+constexpr int kWaitLimit = TFG_WAIT_LOOKS;                   // looks at a word after the first, a second or more
 
 // Words that other CTAs write while the kernel runs.
 __device__ __forceinline__ uint64_t ld_word(const uint64_t *p) {
