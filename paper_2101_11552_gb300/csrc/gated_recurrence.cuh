@@ -199,14 +199,14 @@ constexpr int kLess = 0, kEither = 1;
 template <int FORM> using Form = std::integral_constant<int, FORM>;
 using Yes = std::true_type;
 using No = std::false_type;
-// a = 2^-8.  a - 1 is within 2 u, which is up to 512 u of such an a; below it kEither has a few u.  Words of either kind take twice the
+// a = 2^-7.  a - 1 is within 2 u, which is up to 256 u of such an a; below it kEither has a few u.  Words of either kind take twice the
 // instructions to apply, and a tile that takes longer holds up those behind it: 131,072 x 1,024 bf16 with gates of mean
-// 2.5 and deviation 1.8, both directions, 510 us with words of either kind below 2^-8, 528 below 2^-7, 572 below 2^-6 and
-// 586 with no others (before there were any, 508).
-constexpr float kSmallGate = -5.55f;
-// fp32 rows with a gate as small take the code of rows that begin and end sequences: a copy of their own made the kernel too
-// long for the instructions' cache even when it was not run (1,024 molecules 110 us in place of 106, none slower with small gates
-// throughout).  In bf16 the copy costs nothing, and 131,072 x 1,024 with words of either kind below 2^-6 took 589 us by it, 738 without.
+// 2.5 and deviation 1.8, both directions, 484 us with words of either kind below 2^-8, 497 below 2^-7, 537 below 2^-6 and
+// 536 with no others.
+constexpr float kSmallGate = -4.85f;
+// fp32 rows with a gate as small take the code of rows that begin and end sequences: with a copy of their own the kernel runs slower even
+// where it is not taken (1,024 molecules 106 us, so 103; small gates throughout 131,072 x 512 416, so 430).  In bf16 the copy
+// costs 6 us of 131,072 x 1,024, and small gates throughout take 536 us by it, 621 without.
 template <typename XT> constexpr bool kSharedForm = sizeof(XT) == 4;
 
 // expm1(z) - 2^-126 for -0.35 <= z <= 0: z (1 + z q(z)), q of degree 4 through the Chebyshev points of

@@ -179,7 +179,7 @@ __device__ __forceinline__ void row_gradient(float (&l)[VEC], const float (&r)[V
 // the rows, then the adjoint up them.
 template <bool PLAIN, int FORM, int KIND, typename XT, int EACH, int VEC, typename In, typename Grad, typename Decay>
 __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, const Grad &g, const Decay &d,
-                                                const int32_t *seq, int64_t row, int64_t c, uint32_t begin, uint32_t end,
+                                                const int32_t *seq, XT *gate, XT *input, int64_t c, uint32_t begin, uint32_t end,
                                                 uint32_t in, float (&v)[VEC], float (&w)[VEC]) {
     float slope[EACH][VEC];
 #pragma unroll
@@ -191,7 +191,6 @@ __device__ __forceinline__ void write_gradients(const ScanArgs &p, const In &x, 
         gate_slope<KIND, FORM>(v, dj, xv, slope[j]);
         if (j + 1 < EACH) advance<KIND, FORM>(v, dj, xv);
     }
-    XT *gate = static_cast<XT *>(p.grad_gate) + row * p.grad_gate_ld + c, *input = static_cast<XT *>(p.grad_x) + row * p.grad_x_ld + c;
 #pragma unroll
     for (int j = EACH - 1; j >= 0; --j) {
         if (!PLAIN && !((in >> j) & 1u)) continue;
@@ -337,9 +336,12 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
         enter_group<T, KIND, true>(u, w, cut_up, l);
         if (on) {                                            // no way round the loop's end: the warp is whole at its barrier
             const int64_t row = r0 + group * T::kEach;
+            XT *gate = static_cast<XT *>(p.grad_gate) + row * p.grad_gate_ld + c, *input = static_cast<XT *>(p.grad_x) + row * p.grad_x_ld + c;
+            // not folded into every row's address ahead of the walks, which spilled 50 registers (bf16 80: 315 us, so 285)
+            asm volatile("" : "+l"(gate), "+l"(input));
             const auto write = [&](auto is_plain, auto form) {
                 write_gradients<decltype(is_plain)::value, decltype(form)::value, KIND, XT, T::kEach>(
-                    p, in_stage.x, in_stage.g, in_stage.d, seq, row, c, begin, end, in, v, l);
+                    p, in_stage.x, in_stage.g, in_stage.d, seq, gate, input, c, begin, end, in, v, l);
             };
             if (!plain || (kSharedForm<XT> && small)) write(No{}, Form<kEither>{});
             else if (KIND == TFG_GATE_EXP || small) write(Yes{}, Form<kEither>{});
