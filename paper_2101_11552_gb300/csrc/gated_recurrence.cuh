@@ -25,7 +25,7 @@
 // product, e^(sum of z / 2) of a thread's rows, at most the largest number.  Gates above 0 grow, and the product of 100 rows may pass
 // what fp32 holds where the states do not: a state of 0 stays 0 and one of 1e-30 comes back to ordinary size, where an
 // infinite product makes NaN of the one and an infinity of the other; and a product below 2^-126 is not lost before a large
-// state meets it.  (The logarithm in its place, an exponential for each map applied: 204 us where the root takes 196, one
+// state meets it.  (The logarithm in its place, an exponential for each map applied: 204 us where the root took 196, one
 // sequence of 131,072 x 256 in both directions.)  A gate alone whose exponential passes fp32, from 88.8 on, is an infinity.
 //
 // Precision.  A decay near 1 is held as a - 1, formed directly, and the state advances as v + (a - 1) v + b: a gate near 1 keeps
@@ -44,7 +44,6 @@
 #pragma once
 
 #include <type_traits>
-#include <utility>
 
 #include "widen.cuh"
 
@@ -209,12 +208,12 @@ constexpr float kSmallGate = -4.85f;
 // costs 6 us of 131,072 x 1,024, and small gates throughout take 536 us by it, 621 without.
 template <typename XT> constexpr bool kSharedForm = sizeof(XT) == 4;
 
-// expm1(z) - 2^-126 for -0.35 <= z <= 0: z (1 + z q(z)), q of degree 4 through the Chebyshev points of
-// |z| <= 0.35; within 2 u of itself over all normal fp32 values there.  Never 0, so that the sign tells.
+// expm1(z) + `more` for |z| <= 0.35: z (1 + z q(z)), q of degree 4 through the Chebyshev points of
+// the interval; within 2 u of itself over all normal fp32 values there.
 template <int VEC>
-__device__ __forceinline__ void expm1_near(const float (&z)[VEC], float (&d)[VEC]) {
+__device__ __forceinline__ void expm1_near(const float (&z)[VEC], float more, float (&d)[VEC]) {
     const float c[6] = {0.0013934534508734941f, 0.008363769389688969f, 0.04166645556688309f, 0.16666573286056519f, 0.5f, 1.f};
-    const float tiny[1] = {-1.1754943508222875e-38f};
+    const float last[1] = {more};
 #pragma unroll
     for (int q = 0; q < VEC; ++q) d[q] = c[0];
 #pragma unroll
@@ -222,7 +221,7 @@ __device__ __forceinline__ void expm1_near(const float (&z)[VEC], float (&d)[VEC
         const float ck[1] = {c[k]};
         fma_vec(d, d, z, ck);
     }
-    fma_vec(d, d, z, tiny);
+    fma_vec(d, d, z, last);
 }
 
 // The words of VEC gates; beside them 1 - a of sigmoid gates held as kEither.  Sigmoid: with t = z log2 e, 1 / (1 + 2^t) is
@@ -236,7 +235,7 @@ __device__ __forceinline__ void decay_words(const float (&z)[VEC], float (&r)[VE
     mul_vec(e, log2e);
     if constexpr (KIND == TFG_GATE_EXP) {
         float near[VEC];
-        expm1_near(z, near);
+        expm1_near(z, -1.1754943508222875e-38f, near);       // never 0, so that the sign tells
 #pragma unroll
         for (int q = 0; q < VEC; ++q) {
             // the bits of -0.35 and what lies between it and -0, as whole numbers
@@ -652,7 +651,7 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
                                              const float *initial, const float *grad_final, const int32_t *seq, int64_t c,
                                              uint32_t begin, uint32_t end, uint32_t in, float (&a)[VEC],
                                              float (&b)[VEC], float (&w)[VEC]) {
-    const float half_log2e[1] = {0.72134752044448170f};
+    const float half[1] = {0.5f};
     constexpr bool kAdjoint = !std::is_same<Grad, NoGrad>::value;
     bool open = true;
 #pragma unroll
@@ -672,7 +671,7 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
         }
         x.widen(j, v);
         if constexpr (KIND == TFG_GATE_EXP) {
-            fma_vec(a, zj, half_log2e, a);
+            fma_vec(a, zj, half, a);
             advance<KIND, kEither>(b, dj, v);
         } else if constexpr (FORM == kEither) {
             decay<kEither>(b, dj);
@@ -695,8 +694,15 @@ __device__ __forceinline__ void compose_down(const ScanArgs &p, const Gate &z, c
         }
     }
     if constexpr (KIND == TFG_GATE_EXP) {
+        // near 1 within u / 2 of itself, as one root stands for all groups of rows that a state passes
+        const float log2e[1] = {1.44269504088896341f};
+        float near[VEC], far[VEC];
+        expm1_near(a, 1.f, near);
 #pragma unroll
-        for (int q = 0; q < VEC; ++q) a[q] = fminf(exp2_of(a[q]), kMostDecay);
+        for (int q = 0; q < VEC; ++q) far[q] = a[q];
+        mul_vec(far, log2e);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) a[q] = fabsf(a[q]) <= 0.35f ? near[q] : fminf(exp2_of(far[q]), kMostDecay);
     }
 }
 

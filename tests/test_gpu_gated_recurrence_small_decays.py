@@ -139,3 +139,38 @@ def test_gates_of_all_sizes(f, dt, kind):
     edge = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.35, -0.35, 0.3501, -0.3501, -4.85, -1e-7], device="cuda")
     z[:, 5] = edge.repeat(n // 10)
     check(z.to(DT[dt]), normal(n, f, 5).to(DT[dt]), offsets, kind, normal(4, f, 2), normal(n, f, 3), normal(4, f, 4))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("f,dt", [(16, "f32"), (7, "f32"), (16, "bf16")])
+def test_a_long_memory_has_no_drift(f, dt, kind):
+    """Errors of a memory of L rows, as a share of the values' norm.  Gates that differ from row to row: the roundings of
+    states and of products of decays go up as often as down and come to less than u sqrt(L), 100 u for 10,000 rows; what is
+    wrong in every decay the same way comes to L times as much: half a u in each (an exponential's last bits) to 5,000 u.
+    300 u where two such errors meet.  (Under one gate throughout, a product is rounded the same way every time, too.)"""
+    n = 40_000
+    reach = torch.logspace(1.5, 4, f, dtype=torch.float64)                 # rows
+    spread = torch.exp(0.5 * normal(n, f, 3))
+    z = -spread / reach.float().cuda() if kind == "exp" else torch.log(reach.float().cuda() * spread)
+    z = z.to(DT[dt])
+    x, g, off = normal(n, f, 1).to(DT[dt]), normal(n, f, 2), torch.tensor([0, n], device="cuda")
+    r = tfg.tfg_gated_recurrence(z, x, off, kind, out_dtype=torch.float32)
+    b = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, g, kind, initial=torch.zeros(1, f, device="cuda"))
+    a, p, _, _ = gates(z, kind)
+    xs, gs = x.double().cpu(), g.double().cpu()
+    add = p * xs if kind == "sigmoid" else xs
+    v, lam = torch.zeros(n, f, dtype=torch.float64), torch.zeros(n, f, dtype=torch.float64)
+    state = torch.zeros(f, dtype=torch.float64)
+    for t in range(n):
+        state = a[t] * state + add[t]
+        v[t] = state
+    carry = torch.zeros(f, dtype=torch.float64)
+    for t in range(n - 1, -1, -1):
+        lam[t] = gs[t] + carry
+        carry = a[t] * lam[t]
+    before = torch.cat([torch.zeros(1, f, dtype=torch.float64), v[:-1]])
+    gz = lam * (before - xs) * a * p if kind == "sigmoid" else lam * before * a
+    step = 0.0 if dt == "f32" else 2.0 ** -8
+    for got, want, tol in ((r.out, v, 100 * U), (b.x, lam * p if kind == "sigmoid" else lam, 100 * U + step), (b.gate, gz, 300 * U + step)):
+        off_by = (got.double().cpu() - want).norm(dim=0) / want.norm(dim=0)
+        assert bool((off_by <= tol).all()), off_by
