@@ -79,13 +79,3 @@ def test_a_projections_gradient_over_a_padded_batch():
     both = torch.cat([b.gate, b.x], 1)
     assert torch.equal(h.t() @ both, torch.cat([h[:300], torch.zeros_like(h[300:])]).t() @ both)
     assert bool(torch.isfinite(h.t() @ both).all()) and bool(torch.isfinite(r.out.t() @ both).all())
-
-
-def test_the_flag_beside_unknown_gates():
-    z, x = batch(20, 8, "sigmoid", "f32", 1)
-    off = torch.tensor([0, 20], device="cuda")
-    out, status = torch.empty_like(x), torch.empty(1, dtype=torch.int32, device="cuda")
-    for kind in (2, 256 + 2, 512, -1):
-        rc = tfg.lib().tfg_gated_recurrence(z.data_ptr(), 8, x.data_ptr(), 8, 0, off.data_ptr(), 20, 1, 8, kind, None, out.data_ptr(), 0,
-                                            None, None, None, 0, status.data_ptr(), None)
-        assert rc != 0
