@@ -198,15 +198,13 @@ constexpr int kLess = 0, kEither = 1;
 template <int FORM> using Form = std::integral_constant<int, FORM>;
 using Yes = std::true_type;
 using No = std::false_type;
-// a = 2^-7.  a - 1 is within 2 u, which is up to 256 u of such an a; below it kEither has a few u.  Words of either kind take twice the
+// a = 2^-8.  a - 1 is within 2 u, which is up to 512 u of such an a; below it kEither has a few u.  Words of either kind take twice the
 // instructions to apply, and a tile that takes longer holds up those behind it: 131,072 x 1,024 bf16 with gates of mean
-// 2.5 and deviation 1.8, both directions, 484 us with words of either kind below 2^-8, 497 below 2^-7, 537 below 2^-6 and
-// 536 with no others.
-constexpr float kSmallGate = -4.85f;
-// fp32 rows with a gate as small take the code of rows that begin and end sequences: with a copy of their own the kernel runs slower even
-// where it is not taken (1,024 molecules 106 us, so 103; small gates throughout 131,072 x 512 416, so 430).  In bf16 the copy
-// costs 6 us of 131,072 x 1,024, and small gates throughout take 536 us by it, 621 without.
-template <typename XT> constexpr bool kSharedForm = sizeof(XT) == 4;
+// 2.5 and deviation 1.8, both directions, 472 us with words of either kind below 2^-9, 475 below 2^-8, 517 below 2^-7, 632 below 2^-6 and
+// 621 with no others.  Rows with a gate as small take the code of rows that begin and end sequences: a copy of their own (536 us with no
+// others) makes a kernel that is slower wherever the copy is not taken, by the instructions' cache (481 us; 130,000 x 512 in 4,000
+// sequences 406, so 380; 1,024 molecules fp32 106, so 103).
+constexpr float kSmallGate = -5.55f;
 
 // expm1(z) + `more` for |z| <= 0.35: z (1 + z q(z)), q of degree 4 through the Chebyshev points of
 // the interval; within 2 u of itself over all normal fp32 values there.

@@ -288,9 +288,8 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
                 p, z, in_stage.x, in_stage.d, in_stage.g, on ? p.initial : nullptr, on ? p.grad_final : nullptr, seq, c, begin, end, in,
                 a, b, w);
         };
-        if (!plain || (kSharedForm<XT> && small)) compose(No{}, Form<kEither>{});
-        else if (KIND == TFG_GATE_EXP || small) compose(Yes{}, Form<kEither>{});
-        else compose(Yes{}, Form<kLess>{});
+        if (!plain || small) compose(No{}, Form<kEither>{});
+        else compose(Yes{}, Form<KIND == TFG_GATE_EXP ? kEither : kLess>{});
 #pragma unroll
         for (int q = 0; q < VEC; ++q) u[q] = a[q];
         bool cut = begin != 0u, cut_up = (begin | end) != 0u;
@@ -343,9 +342,8 @@ __global__ void __launch_bounds__(kScanThreads, kBackwardCtas<XT, GT, VEC>)
                 write_gradients<decltype(is_plain)::value, decltype(form)::value, KIND, XT, T::kEach>(
                     p, in_stage.x, in_stage.g, in_stage.d, seq, gate, input, c, begin, end, in, v, l);
             };
-            if (!plain || (kSharedForm<XT> && small)) write(No{}, Form<kEither>{});
-            else if (KIND == TFG_GATE_EXP || small) write(Yes{}, Form<kEither>{});
-            else write(Yes{}, Form<kLess>{});
+            if (!plain || small) write(No{}, Form<kEither>{});
+            else write(Yes{}, Form<KIND == TFG_GATE_EXP ? kEither : kLess>{});
         }
         __syncwarp();
     }

@@ -148,9 +148,8 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
             compose_down<decltype(is_plain)::value, decltype(form)::value, KIND, VEC, T::kEach>(
                 p, z, in_stage.x, in_stage.d, NoGrad{}, on ? p.initial : nullptr, nullptr, seq, c, begin, end, in, a, b, none);
         };
-        if (!plain || (kSharedForm<XT> && small)) compose(No{}, Form<kEither>{});
-        else if (KIND == TFG_GATE_EXP || small) compose(Yes{}, Form<kEither>{});
-        else compose(Yes{}, Form<kLess>{});
+        if (!plain || small) compose(No{}, Form<kEither>{});
+        else compose(Yes{}, Form<KIND == TFG_GATE_EXP ? kEither : kLess>{});
         bool cut = begin != 0u;
         scan_groups<T, KIND, false>(a, b, cut, warp, lane, s_a, s_b);
         __syncthreads();
@@ -191,9 +190,8 @@ __global__ void __launch_bounds__(kScanThreads, kForwardCtas)
                 write_rows<decltype(is_plain)::value, decltype(form)::value, KIND, T::kEach>(p, in_stage.x, in_stage.d, seq, c, begin, end,
                                                                                              in, out, v);
             };
-            if (!plain || (kSharedForm<XT> && small)) write(No{}, Form<kEither>{});
-            else if (KIND == TFG_GATE_EXP || small) write(Yes{}, Form<kEither>{});
-            else write(Yes{}, Form<kLess>{});
+            if (!plain || small) write(No{}, Form<kEither>{});
+            else write(Yes{}, Form<KIND == TFG_GATE_EXP ? kEither : kLess>{});
         }
         __syncwarp();
     }

@@ -4,7 +4,7 @@ Bounds as in test_gpu_gated_recurrence.py, u = 2^-24, but every error of a gate 
 With the sigmoid gate a is e / (1 + e), e = e^z, for z < 0: z log2 e and its constant are rounded (2 |z| u of e), the exponential
 and the reciprocal are within 2 units of the last place (4 u), a sum and a product are rounded: ea = (2 |z| + 10) u a, and
 1 - a then has ep = ea + u p.  For z >= 0 it is p = 1 - a that is formed so, ep = (2 a |z| + 7) u p, and a v is taken as
-v + (a - 1) v: ea = ep.  From -4.85 to 0 a may be taken so too: e is off by (2 |z| + 4) u of itself, the sum and the reciprocal by 3 u p,
+v + (a - 1) v: ea = ep.  From -5.55 to 0 a may be taken so too: e is off by (2 |z| + 4) u of itself, the sum and the reciprocal by 3 u p,
 3 u p more in ea.  With the exp gate ea = (2 |z| + 6) u a away from 0 (the exponential and a rounding), and from -0.35 to 0
 p = a - 1 has 2 u: ea = 5 u |p|.  Hence
   E_t = a_t E_{t-1} + ea M_{t-1} + ep |x_t| + 8 u M_t,     M_t = a_t M_{t-1} + |b_t|     (exp gate: b = x, exact)
@@ -34,7 +34,7 @@ def gates(z, kind):
         a, p = torch.exp(z), torch.expm1(z)
         return a, p, torch.where((z >= -0.35) & (z < 0), 5 * U * p.abs(), (2 * far + 6) * U * a) + TINY, torch.zeros_like(a)
     a, p = torch.sigmoid(z), torch.sigmoid(-z)
-    ea, ep = (2 * far + 10) * U * a + TINY + torch.where(z >= -4.85, 3 * U * p, 0.0), (2 * a * far + 7) * U * p + TINY
+    ea, ep = (2 * far + 10) * U * a + TINY + torch.where(z >= -5.55, 3 * U * p, 0.0), (2 * a * far + 7) * U * p + TINY
     return a, p, torch.where(z < 0, ea, ep), torch.where(z < 0, ea + U * p, ep)
 
 
@@ -136,7 +136,7 @@ def test_gates_of_all_sizes(f, dt, kind):
     z = 4.0 * torch.randn(n, f, device="cuda", generator=gen)
     if kind == "exp":
         z = -z.abs() * (torch.rand(n, f, device="cuda", generator=gen) < 0.5) * 0.25
-    edge = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.35, -0.35, 0.3501, -0.3501, -4.85, -1e-7], device="cuda")
+    edge = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.35, -0.35, 0.3501, -0.3501, -5.55, -1e-7], device="cuda")
     z[:, 5] = edge.repeat(n // 10)
     check(z.to(DT[dt]), normal(n, f, 5).to(DT[dt]), offsets, kind, normal(4, f, 2), normal(n, f, 3), normal(4, f, 4))
 
