@@ -33,10 +33,10 @@
 // large state cut down to what is left of it, and the gate's own gradient, which has a as a factor, keep their digits, where
 // 1 + (a - 1) is a multiple of 2^-25.  One word holds either.  All in fp32.
 //
-// What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 188 us
-// (805 MB, 4.3 TB/s, 27 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
-// were left without the waits for other tiles), backward 295 us (1.34 GB, 4.6 TB/s, 37 instructions).  One sequence of
-// 131,072 x 256, bf16 to fp32: 70 and 112 us.  1,024 molecules, 112,640 x 128 fp32: 39 and 60 us, and 4 us each for the
+// What bounds it: instructions and latency, with memory at 60 % of its rate.  131,072 rows of 1,024 bf16: forward 182 us
+// (805 MB, 4.4 TB/s, 26 warp instructions for 32 values, half of them a tile's fixed work; of 220 us at an earlier step 168
+// were left without the waits for other tiles), backward 284 us (1.34 GB, 4.7 TB/s, 36 instructions).  One sequence of
+// 131,072 x 256, bf16 to fp32: 70 and 111 us.  1,024 molecules, 112,640 x 128 fp32: 39 and 59 us, and 4 us each for the
 // plan.  Of a tile's 18,000 cycles forward 5,000 go by before its inputs are there and 7,000 before the state that enters
 // is; tiles asked for in L2 a round ahead of their copies: 4 % of the kernel (185 us forward without, where 179 with).  128 threads a tile
 // with twice the rows each take a third fewer instructions and are slower (209 and 459 us for the first, too few warps),
