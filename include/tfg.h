@@ -800,8 +800,9 @@ int tfg_layer_norm_backward(const void *sum, int sum_dtype, int64_t num_rows, in
  * the same alignment.  A gate of -inf forgets a finite state entirely.  TFG_GATE_EXP
  * above 0 grows: states and gradients are right where they are ordinary numbers, whatever
  * the product of the gates; from 88.8 on exp(z) is an infinity, and what follows in the
- * sequence is no number.  A value that is no
- * number stays in its channel and sequence.  ceil(num_rows / 128) *
+ * sequence is no number.  A state and an input further apart than fp32 reaches
+ * (3.4e38) may make none either.  What is no number stays in its channel and
+ * sequence, and no gate touches a bit of another sequence's results.  ceil(num_rows / 128) *
  * ceil(num_features / 32) < 2^31 - 2^16 (TFG_ERR_TOO_LARGE).
  * ---------------------------------------------------------------------- */
 #define TFG_RECURRENCE_TILE_ROWS 128

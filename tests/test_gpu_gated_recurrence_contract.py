@@ -79,3 +79,37 @@ def test_a_projections_gradient_over_a_padded_batch():
     both = torch.cat([b.gate, b.x], 1)
     assert torch.equal(h.t() @ both, torch.cat([h[:300], torch.zeros_like(h[300:])]).t() @ both)
     assert bool(torch.isfinite(h.t() @ both).all()) and bool(torch.isfinite(r.out.t() @ both).all())
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "exp"])
+@pytest.mark.parametrize("f,dt", [(40, "f32"), (72, "bf16"), (33, "f32")])
+@pytest.mark.parametrize("lengths", [[50, 60, 70], [13, 3, 9], [400, 500, 30], [5000, 300, 4200]])
+def test_gates_of_a_sequence_do_not_reach_another(lengths, f, dt, kind):
+    """Nor do rows outside all sequences: the others' results stay bit for bit, whatever gates the middle one has
+    and whatever lies before and behind."""
+    lo, n = 21, 21 + sum(lengths) + 100
+    offsets = [lo]
+    for k in lengths:
+        offsets.append(offsets[-1] + k)
+    off = torch.tensor(offsets, device="cuda")
+    z, x = batch(n, f, kind, dt, 1)
+    g, gf, init = normal(n, f, 3, dt), normal(3, f, 4), normal(3, f, 5)
+    mid, used = slice(offsets[1], offsets[2]), slice(offsets[0], offsets[-1])
+    rest = torch.zeros(n, dtype=torch.bool, device="cuda")
+    rest[used] = True
+    rest[mid] = False
+
+    def run():
+        r = tfg.tfg_gated_recurrence(z, x, off, kind, initial=init)
+        b = tfg.tfg_gated_recurrence_backward(z, x, off, r.checkpoints, g, kind, initial=init, grad_final=gf)
+        return [r.out[rest], b.gate[rest], b.x[rest], r.final[[0, 2]], b.initial[[0, 2]]]
+
+    want = run()
+    assert all(bool(torch.isfinite(t).all()) for t in want)
+    for t in (z, x, g):
+        t[:offsets[0]] = float("nan")
+        t[offsets[-1]:] = float("inf")
+    assert all(torch.equal(a, b) for a, b in zip(run(), want))
+    for bad in (float("nan"), -float("inf"), float("inf"), -7.5, 95.0):
+        z[mid] = bad
+        assert all(torch.equal(a, b) for a, b in zip(run(), want)), bad
